@@ -55,7 +55,7 @@ typedef enum {
     SSAM_ERR_HIP = 6     /* a HIP runtime call failed (no device, launch failure)         */
 } ssam_status;
 
-typedef enum { SSAM_F32 = 0, SSAM_F64 = 1 } ssam_dtype;
+typedef enum { SSAM_F32 = 0, SSAM_F64 = 1, SSAM_F16 = 2, SSAM_BF16 = 3 } ssam_dtype;   /* the last two: ssam_sequence.h only, SSAM_ERR_ENUM here */
 typedef enum { SSAM_BOUNDARY_ZERO = 0, SSAM_BOUNDARY_CLAMP = 1 } ssam_boundary;
 
 #define SSAM_MAX_FILTER 32   /* largest filter width or height accepted by ssam_conv2d   */

@@ -1,0 +1,328 @@
+// What the sequence operators share: rows of channels in 32 or 16 bits, how a wave finds its piece of a sequence,
+// and the host's checks of tensors of rows.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "../../include/ssam_sequence.h"
+#include "ssam_device.h"
+
+namespace ssam {
+
+template <int CODE> struct RowTypeOf;
+template <> struct RowTypeOf<SSAM_F32> { using type = float; };
+template <> struct RowTypeOf<SSAM_F16> { using type = _Float16; };
+template <> struct RowTypeOf<SSAM_BF16> { using type = __bf16; };
+
+// V adjacent channels of a row, as they are in memory.
+template <class T, int V> using RowVec = T __attribute__((ext_vector_type(V)));
+
+// Channels p[0 .. have): zeros behind them.  A whole vector is one access at the element's alignment (global memory takes
+// unaligned vectors on this target), so rows of any stride keep 16 bytes per lane.
+template <class T, int V>
+__device__ __forceinline__ RowVec<T, V> load_row_vec(const T* __restrict__ p, int have)
+{
+    RowVec<T, V> v;
+    if (have >= V) {
+        __builtin_memcpy(&v, p, sizeof(v));
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = i < have ? p[i] : T(0);
+    }
+    return v;
+}
+
+template <class T, int V>
+__device__ __forceinline__ void store_row_vec(T* __restrict__ p, int have, const RowVec<T, V>& v)
+{
+    if (have >= V) {
+        __builtin_memcpy(p, &v, sizeof(v));
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < have) p[i] = v[i];
+    }
+}
+
+// fp32 to T: one rounding, to nearest even.
+template <class T, int V>
+__device__ __forceinline__ RowVec<T, V> rounded(const float (&x)[V])
+{
+    RowVec<T, V> v;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = (T)x[i];
+    return v;
+}
+
+// A parameter in the data's type or in fp32.
+template <class T>
+__device__ __forceinline__ float param_at(const void* p, bool f32, long long i)
+{
+    return f32 ? static_cast<const float*>(p)[i] : (float)static_cast<const T*>(p)[i];
+}
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// 2^x by the hardware instruction (1 ulp; results below 2^-126 become 0, which only ever scales a sum).
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// 1 / (1 + exp(-x)): exact limits 0 and 1, NaN kept.
+__device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + exp2_fast(-kLog2e * x)); }
+__device__ __forceinline__ float silu(float x) { return x * sigmoid(x); }
+
+// log(1 + exp(x)) = max(x, 0) + log1p(e) with e = exp(-|x|) in (0, 1].  log1p(e) = 2 atanh(s), s = e / (2 + e) <= 1/3, by its
+// series up to s^15 (the next term is below 2^-28 of the sum): the relative error stays a few 2^-24 however small e is, which
+// 1 + e in fp32 would lose -- the time steps of a trained layer are 0.001 .. 0.1, that is e of the same size.
+__device__ __forceinline__ float softplus(float x)
+{
+    const float e = exp2_fast(-kLog2e * __builtin_fabsf(x));
+    const float s = e * __builtin_amdgcn_rcpf(2.0f + e);
+    const float q = s * s;
+    float r = 1.0f / 15.0f;
+    r = r * q + 1.0f / 13.0f;
+    r = r * q + 1.0f / 11.0f;
+    r = r * q + 1.0f / 9.0f;
+    r = r * q + 1.0f / 7.0f;
+    r = r * q + 0.2f;
+    r = r * q + 1.0f / 3.0f;
+    r = r * q + 1.0f;
+    return __builtin_fmaxf(x, 0.0f) + 2.0f * s * r;   // NaN comes through e
+}
+
+// ---- sequences ---------------------------------------------------------------------------------------------------------
+// Work along time is dealt out in slots of `piece` rows.  Batch forms: slot = s * per + c for piece c of sequence s.  Packed
+// form: slot = begin / piece + s + c, which needs no prefix sum over the sequences: s's pieces end before
+// end / piece + s + 1, where those of s + 1 begin.
+struct Pieces {
+    const int* begin;   // packed form, or null
+    const int* end;     // packed form, or the lengths of a padded batch, or null
+    int sequences, rows, piece;
+    int per;            // batch forms: slots of a sequence
+};
+
+struct Piece {
+    int seq;            // -1: nothing in this slot
+    int first;          // packed form: the sequence's first row; otherwise 0
+    int len;            // rows of the sequence
+    int row0, n;        // the piece: rows row0 .. row0 + n - 1 of the sequence
+};
+
+inline long long piece_slots(const ssam_sequences& q, int piece)
+{
+    if (q.sequences <= 0) return 0;
+    if (q.d_begin) return (long long)q.rows / piece + q.sequences;
+    const long long per = ((long long)q.rows + piece - 1) / piece;
+    return (per > 0 ? per : 1) * q.sequences;
+}
+
+inline Pieces make_pieces(const ssam_sequences& q, int piece)
+{
+    const long long per = ((long long)q.rows + piece - 1) / piece;
+    return Pieces{q.d_begin, q.d_end, q.sequences, q.rows, piece, (int)(per > 0 ? per : 1)};
+}
+
+__device__ __forceinline__ int held(int v, int hi) { return v < 0 ? 0 : v > hi ? hi : v; }
+
+// First slot of sequence s (packed form).
+__device__ __forceinline__ int first_slot(const Pieces& q, int s) { return held(q.begin[s], q.rows) / q.piece + s; }
+
+__device__ __forceinline__ void span_of(const Pieces& q, int s, int& first, int& len)
+{
+    first = q.begin ? held(q.begin[s], q.rows) : 0;
+    const int end = q.end ? held(q.end[s], q.rows) : q.rows;
+    len = end > first ? end - first : 0;
+}
+
+// The piece of a slot; all 64 lanes call it together with the same slot.  The packed form looks for the last sequence whose
+// first slot is not behind this one, 64 candidates at a time.
+__device__ __forceinline__ Piece find_piece(const Pieces& q, int slot)
+{
+    Piece p{-1, 0, 0, 0, 0};
+    int s = 0, c = 0;
+    if (q.begin) {
+        const int lane = threadIdx.x & (kWave - 1);
+        int n = q.sequences;
+        while (true) {
+            const int step = (n + kWave - 1) / kWave;
+            const int i = lane * step;
+            const bool before = i < n && first_slot(q, s + i) <= slot;
+            const int hits = __builtin_popcountll(__builtin_amdgcn_ballot_w64(before));
+            if (hits == 0) return p;
+            const int skip = (hits - 1) * step;
+            s += skip;
+            n = n - skip < step ? n - skip : step;
+            if (step == 1) break;
+        }
+        s = __builtin_amdgcn_readfirstlane(s);
+        c = slot - first_slot(q, s);
+    } else {
+        s = slot / q.per;
+        c = slot - s * q.per;
+    }
+    int first, len;
+    span_of(q, s, first, len);
+    const long long row0 = (long long)c * q.piece;
+    if (c < 0 || (c > 0 && row0 >= len)) return p;
+    p.seq = s;
+    p.first = first;
+    p.len = len;
+    p.row0 = (int)row0;
+    p.n = len - p.row0 < q.piece ? len - p.row0 : q.piece;
+    return p;
+}
+
+// Address of a sequence's row 0 (batch forms: by the batch stride; packed: by its first row).
+template <class T>
+__device__ __forceinline__ T* sequence_base(const ssam_rows& r, const Pieces& q, const Piece& p)
+{
+    return static_cast<T*>(r.d) + (q.begin ? (long long)p.first * r.row : (long long)p.seq * r.batch);
+}
+
+// ---- slots -------------------------------------------------------------------------------------------------------------
+// The rows of a call that name one slot, in order.  The first of them leads: its wave takes them all, one behind the other, and
+// the waves of the others leave, so that a slot named twice is one sequence that gets two rows and never a race.  Every lane of
+// a wave asks with the same row; one round of loads covers 512 rows, and only a slot that is named again costs more.
+class SlotRows {
+public:
+    __device__ __forceinline__ SlotRows(const int* slot_of, int rows, int slots, int row)
+        : of_(slot_of), rows_(rows), at_(row + 1), mine_(slot_of ? slot_of[row] : row), again_(false)
+    {
+        leads_ = mine_ >= 0 && mine_ < slots;
+        if (!of_ || !leads_) return;
+        const int lane = threadIdx.x & (kWave - 1);
+        constexpr int kAtOnce = 8;
+        for (int b = 0; b < rows; b += kAtOnce * kWave) {
+            bool before = false, behind = false;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                const int i = b + k * kWave + lane;
+                const bool same = i < rows && of_[i] == mine_;
+                before |= same && i < row;
+                behind |= same && i > row;
+            }
+            leads_ = leads_ && __builtin_amdgcn_ballot_w64(before) == 0;
+            again_ = again_ || __builtin_amdgcn_ballot_w64(behind) != 0;
+        }
+    }
+    __device__ __forceinline__ bool leads() const { return leads_; }
+    __device__ __forceinline__ int slot() const { return mine_; }
+    // The next row of the slot, -1 behind the last.
+    __device__ __forceinline__ int next()
+    {
+        if (!again_) return -1;
+        const int lane = threadIdx.x & (kWave - 1);
+        for (; at_ < rows_; at_ += kWave) {
+            const unsigned long long m = __builtin_amdgcn_ballot_w64(at_ + lane < rows_ && of_[at_ + lane < rows_ ? at_ + lane : at_] == mine_);
+            if (m) {
+                const int r = at_ + __builtin_ctzll(m);
+                at_ = r + 1;
+                return r;
+            }
+        }
+        return -1;
+    }
+
+private:
+    const int* of_;
+    int rows_, at_, mine_;
+    bool leads_, again_;
+};
+
+// ---- host: checks ------------------------------------------------------------------------------------------------------
+inline int type_bytes(int dtype) { return dtype == SSAM_F32 ? 4 : dtype == SSAM_F16 || dtype == SSAM_BF16 ? 2 : 0; }
+
+constexpr long long kMaxChannels = 1 << 24;
+constexpr long long kMaxStride = 1LL << 40;      // elements: offsets of any row then fit 64 bits
+
+// What a tensor covers: `count` rows (batch after batch) of `width` bytes, `step` bytes apart; one = a plain range.
+struct Cover {
+    uintptr_t at;
+    long long bytes;         // from the first to behind the last
+    long long step, width;   // step 0: not a comb of rows, the whole range counts
+};
+
+inline Cover cover_plain(const void* p, long long bytes) { return Cover{(uintptr_t)p, p ? bytes : 0, 0, 0}; }
+
+inline Cover cover_rows(const ssam_rows& r, const ssam_sequences& q, long long width_elems, int esz)
+{
+    if (!r.d || q.sequences <= 0 || q.rows <= 0) return Cover{(uintptr_t)r.d, 0, 0, 0};
+    const long long width = width_elems * esz;
+    long long last = (long long)(q.rows - 1) * r.row * esz;
+    bool comb = r.row * esz >= width;
+    if (!q.d_begin && q.sequences > 1) {
+        last += (long long)(q.sequences - 1) * r.batch * esz;
+        comb = comb && r.row > 0 && r.batch % r.row == 0;      // every row of every sequence lies on the same comb
+    }
+    return Cover{(uintptr_t)r.d, last + width, comb ? r.row * esz : 0, width};
+}
+
+inline bool overlaps(const Cover& a, const Cover& b)
+{
+    if (!a.bytes || !b.bytes) return false;
+    if (a.at + (uintptr_t)a.bytes <= b.at || b.at + (uintptr_t)b.bytes <= a.at) return false;
+    if (a.step && a.step == b.step) {      // column ranges of one buffer
+        const long long off = a.at <= b.at ? (long long)((b.at - a.at) % (uintptr_t)a.step)
+                                           : a.step - 1 - (long long)((a.at - b.at - 1) % (uintptr_t)a.step);
+        return off < a.width || off + b.width > a.step;
+    }
+    return true;
+}
+
+// 0: fine, otherwise the error.  `optional`: a NULL tensor is fine.
+inline int check_rows(const ssam_rows& r, const ssam_sequences& q, int esz, bool optional)
+{
+    if (!r.d) return optional || q.sequences == 0 || q.rows == 0 ? SSAM_OK : SSAM_ERR_NULL;
+    if ((uintptr_t)r.d % esz || r.row < 0 || r.row > kMaxStride || (!q.d_begin && (r.batch < 0 || r.batch > kMaxStride))) return SSAM_ERR_DIM;
+    return SSAM_OK;
+}
+
+// A result's rows must not share elements with one another either.
+inline int check_out_rows(const ssam_rows& r, const ssam_sequences& q, long long width, int esz, bool optional)
+{
+    if (int e = check_rows(r, q, esz, optional)) return e;
+    if (!r.d) return SSAM_OK;
+    if (q.rows > 1 && r.row < width) return SSAM_ERR_DIM;
+    if (!q.d_begin && q.sequences > 1) {
+        const bool after = r.batch >= (q.rows > 0 ? (long long)(q.rows - 1) * r.row + width : width);       // sequence behind sequence
+        const bool between = r.row >= (long long)(q.sequences - 1) * r.batch + width && r.batch >= width;   // rows of the sequences in turn
+        if (!after && !between) return SSAM_ERR_DIM;
+    }
+    return SSAM_OK;
+}
+
+inline int check_sequences(const ssam_sequences& q)
+{
+    if (q.sequences < 0 || q.rows < 0 || q.rows > SSAM_MAX_EXTENT || q.sequences > SSAM_MAX_EXTENT) return SSAM_ERR_DIM;
+    if (q.d_begin && !q.d_end) return SSAM_ERR_NULL;
+    if ((uintptr_t)q.d_begin % 4 || (uintptr_t)q.d_end % 4) return SSAM_ERR_DIM;
+    return SSAM_OK;
+}
+
+inline int check_slots(int rows, int slots, const int* d_slots)
+{
+    return rows < 0 || rows > SSAM_MAX_EXTENT || slots < 0 || slots > SSAM_MAX_EXTENT || (uintptr_t)d_slots % 4 ? SSAM_ERR_DIM : SSAM_OK;
+}
+
+inline Cover cover_slots(const void* p, int slots, long long stride, long long slot, int esz)
+{
+    return cover_plain(p, slots > 0 && slot > 0 ? ((slots - 1) * stride + slot) * esz : 0);
+}
+
+template <int NA, int NB>
+inline bool any_overlap(const Cover (&outs)[NA], const Cover (&ins)[NB])
+{
+    for (int i = 0; i < NA; ++i) {
+        for (int j = 0; j < NB; ++j)
+            if (overlaps(outs[i], ins[j])) return true;
+        for (int j = 0; j < i; ++j)
+            if (overlaps(outs[i], outs[j])) return true;
+    }
+    return false;
+}
+
+constexpr long long kMaxGrid = (1LL << 24) - 1;   // blocks of 256 threads: a launch holds fewer than 2^32 threads
+
+inline int launched() { return hipGetLastError() == hipSuccess ? SSAM_OK : SSAM_ERR_HIP; }
+
+}  // namespace ssam

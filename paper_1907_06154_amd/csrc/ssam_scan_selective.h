@@ -1,0 +1,151 @@
+// What the selective scan's kernels share: how channels and states lie over the lanes of a wave, and the tensors.
+//
+// A wave holds 64 / GL channels; the GL lane groups of a channel hold NS states each, in registers.  Lane bits: the low bits
+// are channels, so that the four lanes of a quad (DPP quad_perm) work on four channels with the SAME states: a quad needs NS
+// values of b (and c) per row, every lane of it loads NS / 4 of them, and the multiply-add takes the other three from its
+// neighbours by DPP -- one 32-bit LDS read per four states instead of four.  The groups are bits 2-3 of the lane (GL = 4), bit 3
+// (GL = 2) or none, so that the sum over a channel's states is completed by rotations inside the row of 16 lanes.
+#pragma once
+#include "ssam_rows.h"
+
+namespace ssam {
+
+
+template <int GL_, int NS_>
+struct ScanShape {
+    static constexpr int GL = GL_, NS = NS_;
+    static constexpr int kStates = GL * NS;                       // states held, those of the call padded with zeros
+    static constexpr int kWaveChannels = kWave / GL;
+    static constexpr int kChannels = kWavesPerBlock * kWaveChannels;   // of a block
+};
+
+template <int GL> __device__ __forceinline__ int lane_group(int lane) { return GL == 4 ? (lane >> 2) & 3 : GL == 2 ? (lane >> 3) & 1 : 0; }
+template <int GL> __device__ __forceinline__ int lane_channel(int lane)
+{
+    return GL == 4 ? (lane & 3) + ((lane >> 4) << 2) : GL == 2 ? (lane & 7) + ((lane >> 4) << 3) : lane;
+}
+
+// The value of lane Q of the quad.
+template <int Q>
+__device__ __forceinline__ float quad_lane(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), Q * 0x55, 0xf, 0xf, true));
+}
+// The value of the lane N to the left, around the row of 16.
+template <int N>
+__device__ __forceinline__ float row_rotate(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x120 + N, 0xf, 0xf, true));
+}
+// Sum over the lane groups of a channel, in every one of them (the same bits in each: both steps add two values).
+template <int GL>
+__device__ __forceinline__ float group_sum(float v)
+{
+    if (GL >= 2) v += row_rotate<8>(v);
+    if (GL >= 4) v += row_rotate<4>(v);
+    return v;
+}
+
+// Index of the value that lane (group, quad lane) loads as number m: state group * NS + 4 m + quad lane.
+template <class Shape> __device__ __forceinline__ int own_state(int lane, int m) { return lane_group<Shape::GL>(lane) * Shape::NS + 4 * m + (lane & 3); }
+
+// A channel's NS states of this lane in an array [..][channels][states]; those behind `states` are zero / not stored.
+template <int NS>
+__device__ __forceinline__ void load_states(const float* __restrict__ a, int n0, int states, bool there, float (&h)[NS])
+{
+#pragma unroll
+    for (int m = 0; m < NS; m += 4) {
+        const RowVec<float, 4> v = load_row_vec<float, 4>(a + n0 + m, there ? states - n0 - m : 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) h[m + i] = v[i];
+    }
+}
+template <int NS>
+__device__ __forceinline__ void store_states(float* __restrict__ a, int n0, int states, bool there, const float (&h)[NS])
+{
+#pragma unroll
+    for (int m = 0; m < NS; m += 4) {
+        const RowVec<float, 4> v = {h[m], h[m + 1], h[m + 2], h[m + 3]};
+        store_row_vec<float, 4>(a + n0 + m, there ? states - n0 - m : 0, v);
+    }
+}
+
+// A decay rate for exp2.  -inf (a state that forgets at once) becomes the lowest finite value, so that a time step of zero leaves
+// the state alone there too: rows behind a sequence pass as such.
+__device__ __forceinline__ float decay_rate(float a)
+{
+    const float r = a * kLog2e;
+    return r == -__builtin_inff() ? -3.402823466e38f : r;
+}
+template <int NS>
+__device__ __forceinline__ void load_rates(const float* __restrict__ a, int n0, int states, bool there, float (&a2)[NS])
+{
+    load_states<NS>(a, n0, states, there, a2);
+#pragma unroll
+    for (int i = 0; i < NS; ++i) a2[i] = decay_rate(a2[i]);
+}
+
+// The tile of channels of a block: blocks never span two groups of b and c.
+struct ChannelTile {
+    int group, c0, n;     // group, first channel, channels
+};
+__device__ __forceinline__ ChannelTile channel_tile(int tile, int per_group, int group_channels, int wide)
+{
+    ChannelTile t;
+    t.group = tile / per_group;
+    const int at = (tile - t.group * per_group) * wide;
+    t.c0 = t.group * group_channels + at;
+    t.n = group_channels - at < wide ? group_channels - at : wide;
+    return t;
+}
+
+// f gets the lane layout for a number of states as a compile-time constant.
+template <class F>
+int with_shape(int states, F f)
+{
+    if (states <= 4) return f(ScanShape<1, 4>{});
+    if (states <= 8) return f(ScanShape<2, 4>{});
+    if (states <= 16) return f(ScanShape<4, 4>{});
+    if (states <= 32) return f(ScanShape<4, 8>{});
+    return f(ScanShape<4, 16>{});
+}
+template <class F>
+int with_row_type(int dtype, F f)
+{
+    if (dtype == SSAM_F32) return f(float());
+    if (dtype == SSAM_F16) return f(_Float16());
+    return f(__bf16());
+}
+
+inline int check_scan(int dtype, int channels, int states, int groups)
+{
+    if (dtype != SSAM_F32 && dtype != SSAM_F16 && dtype != SSAM_BF16) return SSAM_ERR_ENUM;
+    if (channels <= 0 || channels > kMaxChannels) return SSAM_ERR_DIM;
+    if (states < 1 || states > SSAM_MAX_STATES || groups < 1 || channels % groups) return SSAM_ERR_SHAPE;
+    return SSAM_OK;
+}
+
+// Blocks along the channels, and the widest channel tile.
+inline int tile_channels(int states) { return states <= 4 ? 256 : states <= 8 ? 128 : 64; }
+inline int tiles_per_group(int channels, int states, int groups)
+{
+    const int w = tile_channels(states);
+    return (channels / groups + w - 1) / w;
+}
+
+// b and c: groups x states elements, `apart` from group to group.
+inline long long group_width(int groups, int states, long long apart) { return (groups - 1) * apart + states; }
+
+// ---- sequences in pieces ------------------------------------------------------------------------------------------------
+// Rows of a piece, a multiple of 32, so that sequences x channel tiles x pieces come to about `blocks` blocks; one piece a sequence
+// where there are enough without.
+int scan_piece_rows(const ssam_sequences& q, int tiles, int blocks);
+
+// Turns what each piece adds to the state into the states between the pieces: `ends` holds [slot][channels][states], `sums`
+// [slot][channels] the time steps of a piece added up (its decay is exp(a * sum)).
+//   forward:  ends[slot] becomes the state before the piece, from `initial` (zeros without)
+//   backward: ends[slot] becomes what reaches the piece's last row from behind, from `initial` (the gradient of the last state)
+int launch_join(const Pieces& p, float* ends, const float* sums, const float* a, const float* initial, int channels, int states, bool backward,
+                hipStream_t stream);
+
+}  // namespace ssam

@@ -1,0 +1,487 @@
+// Scan with decay chosen by the input (ssam_scan_selective):
+//     h_t[n] = exp(d_t a[n]) h_{t-1}[n] + d_t u_t b_t[n],    y_t = sum_n c_t[n] h_t[n] + skip u_t
+// one channel's recurrence per group of lanes (ssam_scan_selective.h), 64 .. 256 channels to a block, states in registers.
+//
+// A block walks its rows in tiles of 2048 values: the tile's time steps, inputs and gates are requested one tile ahead, 16 bytes a
+// lane; every thread turns its eight values into (d, d u) once and puts them into LDS with the rows' b and c, the waves run the
+// recurrence from there, leave y in LDS, and the threads that loaded the values finish them (skip, gate) and store them.
+//
+// Per state and row that is one exp, two products and two multiply-adds; the exp (8 cycles of a SIMD against 2.5 - 4 of the
+// others) makes the vector unit the bound, not memory (8 bytes a value).
+#include "ssam_scan_selective.h"
+
+namespace ssam {
+namespace {
+
+constexpr int kElems = 8;                    // values of a tile that a thread loads, and stores
+constexpr int kBlocks = 1024;                // four blocks of four waves per compute unit
+
+struct ScanParams {
+    Pieces pieces;
+    ssam_rows in, dt, gate, out, b, c;
+    long long b_group, c_group;
+    const float *a, *skip, *dt_bias, *state, *starts;   // starts: [slot][channels][states], the state before each piece
+    float *final, *marks, *ends, *sums;
+    Pieces mark_slots;
+    int channels, states, group_channels, per_group, tiles, softplus;
+};
+
+// kWhole: all rows, outputs and the last state.  !kWhole: only the state that a piece adds (from zero) and its time steps' sum.
+template <class T, class Shape, bool kWhole>
+__global__ __launch_bounds__(kBlock) void scan_rows(ScanParams p)
+{
+    constexpr int GL = Shape::GL, NS = Shape::NS, NP = Shape::kStates, CB = Shape::kChannels;
+    constexpr int K = kBlock * kElems / CB;              // rows of a tile
+    constexpr int kPairs = (K * NP + kBlock - 1) / kBlock;
+    __shared__ RowVec<float, 2> dx[K][CB];               // d, d u
+    __shared__ RowVec<float, 2> bc[K][NP];
+    __shared__ float ys[kWhole ? K : 1][CB];
+
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const int slot = blockIdx.x / p.tiles;
+    const Piece q = find_piece(p.pieces, slot);
+    if (q.seq < 0) return;
+    const bool last = q.row0 + q.n >= q.len;
+    if (!kWhole && last) return;                         // nothing follows it
+    const ChannelTile ct = channel_tile(blockIdx.x % p.tiles, p.per_group, p.group_channels, CB);
+
+    // this lane's channel and states
+    const int ch = (tid >> 6) * Shape::kWaveChannels + lane_channel<GL>(lane);
+    const bool live = ch < ct.n;
+    const int n0 = lane_group<GL>(lane) * NS;
+    const long long cell = (long long)(ct.c0 + ch) * p.states;    // its row of [channels][states]
+    const long long plane = (long long)p.channels * p.states;
+    float a2[NS], h[NS];
+    load_rates<NS>(p.a + cell, n0, p.states, live, a2);
+    if (!kWhole) load_states<NS>(nullptr, 0, 0, false, h);
+    else if (p.starts) load_states<NS>(p.starts + slot * plane + cell, n0, p.states, live, h);
+    else load_states<NS>(p.state + q.seq * plane + cell, n0, p.states, live && p.state, h);
+    float sum = 0.0f;
+    float* marks = nullptr;
+    if (kWhole && p.marks) {
+        const int s0 = p.mark_slots.begin ? first_slot(p.mark_slots, q.seq) : q.seq * p.mark_slots.per;
+        marks = p.marks + (s0 + q.row0 / SSAM_MARK_ROWS) * plane + cell;
+    }
+
+    // this thread's eight values of a tile: row er, channels ec .. ec + 7
+    const int er = tid * kElems / CB, ec = tid * kElems % CB;
+    const int have = ct.n - ec < 0 ? 0 : ct.n - ec;
+    const T* __restrict__ in = sequence_base<T>(p.in, p.pieces, q) + (long long)(q.row0 + er) * p.in.row + ct.c0 + ec;
+    const T* __restrict__ dt = sequence_base<T>(p.dt, p.pieces, q) + (long long)(q.row0 + er) * p.dt.row + ct.c0 + ec;
+    const T* __restrict__ gate = kWhole && p.gate.d ? sequence_base<T>(p.gate, p.pieces, q) + (long long)(q.row0 + er) * p.gate.row + ct.c0 + ec : nullptr;
+    T* __restrict__ out = kWhole ? sequence_base<T>(p.out, p.pieces, q) + (long long)(q.row0 + er) * p.out.row + ct.c0 + ec : nullptr;
+    const T* __restrict__ pb = sequence_base<T>(p.b, p.pieces, q) + (long long)q.row0 * p.b.row + ct.group * p.b_group;
+    const T* __restrict__ pc = kWhole ? sequence_base<T>(p.c, p.pieces, q) + (long long)q.row0 * p.c.row + ct.group * p.c_group : nullptr;
+    float bias[kElems], skip[kElems];
+#pragma unroll
+    for (int e = 0; e < kElems; ++e) {
+        bias[e] = p.dt_bias && e < have ? p.dt_bias[ct.c0 + ec + e] : 0.0f;
+        skip[e] = kWhole && p.skip && e < have ? p.skip[ct.c0 + ec + e] : 0.0f;
+    }
+
+    using Vec = RowVec<T, kElems>;
+    Vec u, d, z, u_next, d_next, z_next;
+    T b_next[kPairs], c_next[kPairs];
+    auto request = [&](int row) {
+        const int there = row + er < q.n ? have : 0;
+        u_next = load_row_vec<T, kElems>(in + (long long)row * p.in.row, there);
+        d_next = load_row_vec<T, kElems>(dt + (long long)row * p.dt.row, there);
+        if (kWhole && gate) z_next = load_row_vec<T, kElems>(gate + (long long)row * p.gate.row, there);
+#pragma unroll
+        for (int e = 0; e < kPairs; ++e) {
+            const int i = tid + e * kBlock, r = i / NP, n = i % NP;
+            const bool is = i < K * NP && row + r < q.n && n < p.states;
+            b_next[e] = is ? pb[(long long)(row + r) * p.b.row + n] : T(0);
+            c_next[e] = kWhole && is ? pc[(long long)(row + r) * p.c.row + n] : T(0);
+        }
+    };
+    // Rows behind the piece and channels behind the tile get d = 0, d u = 0: the state passes them unchanged.
+    auto stage = [&](int row) {
+        u = u_next;
+        d = d_next;
+        z = z_next;
+        const int there = row + er < q.n ? have : 0;
+#pragma unroll
+        for (int e = 0; e < kElems; ++e) {
+            float v = (float)d[e] + bias[e];
+            if (p.softplus) v = softplus(v);
+            v = e < there ? v : 0.0f;
+            dx[er][ec + e] = RowVec<float, 2>{v, e < there ? v * (float)u[e] : 0.0f};
+        }
+#pragma unroll
+        for (int e = 0; e < kPairs; ++e) {
+            const int i = tid + e * kBlock;
+            if (i < K * NP) bc[i / NP][i % NP] = RowVec<float, 2>{(float)b_next[e], (float)c_next[e]};
+        }
+    };
+
+    request(0);
+    for (int row = 0; row < q.n; row += K) {
+        stage(row);
+        __syncthreads();
+        if (row + K < q.n) request(row + K);
+        if (kWhole && p.marks && K < SSAM_MARK_ROWS && row % SSAM_MARK_ROWS == 0)
+            store_states<NS>(marks + (row / SSAM_MARK_ROWS) * plane, n0, p.states, live, h);
+#pragma unroll 4
+        for (int t = 0; t < K; ++t) {
+            if (kWhole && p.marks && K >= SSAM_MARK_ROWS && t % SSAM_MARK_ROWS == 0 && row + t < q.n)
+                store_states<NS>(marks + ((row + t) / SSAM_MARK_ROWS) * plane, n0, p.states, live, h);
+            const RowVec<float, 2> dv = dx[t][ch];
+            float y = 0.0f;
+            if (!kWhole) sum += dv[0];
+#pragma unroll
+            for (int m = 0; m < NS / 4; ++m) {
+                const RowVec<float, 2> w = bc[t][own_state<Shape>(lane, m)];
+#define SSAM_STATE(Q)                                                                                  \
+    {                                                                                                  \
+        const int i = 4 * m + Q;                                                                       \
+        h[i] = __builtin_fmaf(exp2_fast(dv[0] * a2[i]), h[i], quad_lane<Q>(w[0]) * dv[1]);             \
+        if (kWhole) y = __builtin_fmaf(quad_lane<Q>(w[1]), h[i], y);                                   \
+    }
+                SSAM_STATE(0)
+                SSAM_STATE(1)
+                SSAM_STATE(2)
+                SSAM_STATE(3)
+#undef SSAM_STATE
+            }
+            if (kWhole) ys[t][ch] = group_sum<GL>(y);    // the groups of a channel write the same value
+        }
+        __syncthreads();
+        if (kWhole) {
+            const int there = row + er < q.n ? have : 0;
+            float o[kElems];
+#pragma unroll
+            for (int e = 0; e < kElems; ++e) {
+                o[e] = __builtin_fmaf(skip[e], (float)u[e], ys[er][ec + e]);
+                if (gate) o[e] *= silu((float)z[e]);
+            }
+            store_row_vec<T, kElems>(out + (long long)row * p.out.row, there, rounded<T, kElems>(o));
+        }
+    }
+    if (kWhole) {
+        if (p.final && last) store_states<NS>(p.final + q.seq * plane + cell, n0, p.states, live, h);
+    } else {
+        store_states<NS>(p.ends + slot * plane + cell, n0, p.states, live, h);
+        if (live && n0 == 0) p.sums[(long long)slot * p.channels + ct.c0 + ch] = sum;
+    }
+}
+
+// One thread per sequence, channel and state walks the pieces; their values are requested eight pieces at a time.
+template <bool kBackward>
+__global__ __launch_bounds__(kBlock) void join_pieces(Pieces pc, float* ends, const float* __restrict__ sums, const float* __restrict__ a,
+                                                      const float* initial, int channels, int states, unsigned blocks_each)
+{
+    const int seq = blockIdx.x / blocks_each;
+    const long long plane = (long long)channels * states;
+    const long long i = (long long)(blockIdx.x % blocks_each) * kBlock + threadIdx.x;
+    if (i >= plane) return;
+    int begin, len;
+    span_of(pc, seq, begin, len);
+    const long long slot0 = pc.begin ? first_slot(pc, seq) : (long long)seq * pc.per;
+    const int n = len > pc.piece ? (len + pc.piece - 1) / pc.piece : 1;
+    const int c = (int)(i / states);
+    const float a2 = decay_rate(a[i]);
+    float h = initial ? initial[seq * plane + i] : 0.0f;
+    constexpr int kAtOnce = 8;
+    for (int k = 0; k < n; k += kAtOnce) {
+        float e[kAtOnce], s[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            const bool there = k + j < n - 1;          // nothing follows the last
+            const long long at = slot0 + (kBackward ? n - 1 - (k + j) : k + j);
+            e[j] = there ? ends[at * plane + i] : 0.0f;
+            s[j] = there ? sums[at * channels + c] : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            if (k + j >= n) break;
+            ends[(slot0 + (kBackward ? n - 1 - (k + j) : k + j)) * plane + i] = h;
+            h = __builtin_fmaf(exp2_fast(a2 * s[j]), h, e[j]);
+        }
+    }
+}
+
+struct Plan {
+    int tiles, piece;
+    long long slots;
+    bool cut;              // sequences may be more than one piece
+    size_t ends, bytes;    // bytes of the pieces' states, and of the whole workspace
+};
+
+Plan plan_of(const ssam_scan_selective_args& a)
+{
+    Plan p;
+    p.tiles = tiles_per_group(a.channels, a.states, a.groups) * a.groups;
+    p.piece = scan_piece_rows(a.seq, p.tiles, kBlocks);
+    p.slots = piece_slots(a.seq, p.piece);
+    p.cut = a.seq.rows > p.piece;
+    p.ends = p.cut ? (size_t)p.slots * a.channels * a.states * sizeof(float) : 0;
+    p.bytes = p.cut ? p.ends + (size_t)p.slots * a.channels * sizeof(float) : 0;
+    return p;
+}
+
+// ---- one row per sequence ----------------------------------------------------------------------------------------------
+struct ScanStepParams {
+    int rows, slots, channels, states, group_channels, per_group, tiles, softplus;
+    const int* slot_of;
+    ssam_rows in, dt, gate, out, b, c;
+    long long b_group, c_group;
+    const float *a, *skip, *dt_bias;
+    float* state;
+    long long slot_stride, waves;
+};
+
+template <int P>
+__device__ __forceinline__ float from_part(float v, int k)   // the value of lane k of the P lanes around this one
+{
+    return __shfl(v, (int)(threadIdx.x & (kWave - 1) & ~(P - 1)) | k);
+}
+template <int P>
+__device__ __forceinline__ float part_sum(float v)
+{
+#pragma unroll
+    for (int d = 1; d < P; d *= 2) v += __shfl_xor(v, d);
+    return v;
+}
+
+// A wave takes 64 channels of a row.  Their states are 64 x 4 P consecutive floats: P lanes share a channel, four states each, and go
+// through P channels one after the other, so that every load is a run of whole lines; what belongs to a channel alone (time step,
+// gate, output) is made once, by the lane of that number, and handed round.  Bound by the state: 8 bytes per value of it.
+template <class T, int P>
+__global__ __launch_bounds__(kBlock) void scan_step(ScanStepParams p)
+{
+    const int lane = threadIdx.x & (kWave - 1);
+    const long long wave = (long long)blockIdx.x * kWavesPerBlock + (threadIdx.x >> 6);
+    if (wave >= p.waves) return;
+    const int row = (int)(wave / p.tiles);
+    SlotRows same(p.slot_of, p.rows, p.slots, row);
+    if (!same.leads()) return;
+    const ChannelTile ct = channel_tile((int)(wave % p.tiles), p.per_group, p.group_channels, kWave);
+    const bool own = lane < ct.n;
+    const int c = ct.c0 + lane;                  // the channel whose time step and output are this lane's
+    const int part = lane & (P - 1), first = lane & ~(P - 1), n0 = part * 4;
+    float* __restrict__ state = p.state + (long long)same.slot() * p.slot_stride;
+    float h[P][4], a2[P][4];
+#pragma unroll
+    for (int k = 0; k < P; ++k) {
+        const long long cell = (long long)(ct.c0 + first + k) * p.states;
+        const bool there = first + k < ct.n;
+        load_states<4>(state + cell, n0, p.states, there, h[k]);
+        load_rates<4>(p.a + cell, n0, p.states, there, a2[k]);
+    }
+    const float bias = own && p.dt_bias ? p.dt_bias[c] : 0.0f;
+    const float skip = own && p.skip ? p.skip[c] : 0.0f;
+    for (int r = row; r >= 0; r = same.next()) {
+        const float u = own ? (float)static_cast<const T*>(p.in.d)[r * p.in.row + c] : 0.0f;
+        float d = own ? (float)static_cast<const T*>(p.dt.d)[r * p.dt.row + c] + bias : 0.0f;
+        const float z = own && p.gate.d ? (float)static_cast<const T*>(p.gate.d)[r * p.gate.row + c] : 0.0f;
+        const RowVec<T, 4> b = load_row_vec<T, 4>(static_cast<const T*>(p.b.d) + r * p.b.row + ct.group * p.b_group + n0, p.states - n0);
+        const RowVec<T, 4> w = load_row_vec<T, 4>(static_cast<const T*>(p.c.d) + r * p.c.row + ct.group * p.c_group + n0, p.states - n0);
+        if (p.softplus) d = softplus(d);
+        const float x = d * u;
+        float y = 0.0f;
+#pragma unroll
+        for (int k = 0; k < P; ++k) {
+            const float dk = from_part<P>(d, k), xk = from_part<P>(x, k);
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                h[k][i] = __builtin_fmaf((float)b[i], xk, h[k][i] * exp2_fast(dk * a2[k][i]));
+                s = __builtin_fmaf((float)w[i], h[k][i], s);
+            }
+            s = part_sum<P>(s);
+            y = part == k ? s : y;
+        }
+        y = __builtin_fmaf(skip, u, y);
+        if (p.gate.d) y *= silu(z);
+        if (own) static_cast<T*>(p.out.d)[r * p.out.row + c] = (T)y;
+    }
+#pragma unroll
+    for (int k = 0; k < P; ++k)
+        store_states<4>(state + (long long)(ct.c0 + first + k) * p.states, n0, p.states, first + k < ct.n, h[k]);
+}
+
+}  // namespace
+
+int scan_piece_rows(const ssam_sequences& q, int tiles, int blocks)
+{
+    constexpr long long kShortest = 64, kLongest = 1 << 30;
+    const long long total = q.d_begin ? q.rows : (long long)q.rows * q.sequences;
+    long long piece = (total * tiles + blocks - 1) / blocks;
+    if (!q.d_begin && (long long)q.sequences * tiles >= blocks / 2) piece = q.rows;
+    piece = (piece + 31) / 32 * 32;
+    return (int)(piece < kShortest ? kShortest : piece > kLongest ? kLongest : piece);
+}
+
+int launch_join(const Pieces& p, float* ends, const float* sums, const float* a, const float* initial, int channels, int states, bool backward,
+                hipStream_t stream)
+{
+    const unsigned each = (unsigned)(((long long)channels * states + kBlock - 1) / kBlock);
+    const dim3 grid(each * (unsigned)p.sequences);
+    if (backward) hipLaunchKernelGGL((join_pieces<true>), grid, dim3(kBlock), 0, stream, p, ends, sums, a, initial, channels, states, each);
+    else hipLaunchKernelGGL((join_pieces<false>), grid, dim3(kBlock), 0, stream, p, ends, sums, a, initial, channels, states, each);
+    return launched();
+}
+
+}  // namespace ssam
+
+extern "C" {
+
+size_t ssam_scan_selective_workspace_bytes(const ssam_scan_selective_args* a)
+{
+    using namespace ssam;
+    if (!a || check_scan(a->dtype, a->channels, a->states, a->groups) || check_sequences(a->seq) || a->seq.sequences == 0) return 0;
+    return plan_of(*a).bytes;
+}
+
+long long ssam_scan_selective_marks(const ssam_scan_selective_args* a)
+{
+    using namespace ssam;
+    if (!a || check_scan(a->dtype, a->channels, a->states, a->groups) || check_sequences(a->seq)) return 0;
+    return piece_slots(a->seq, SSAM_MARK_ROWS);
+}
+
+int ssam_scan_selective(const ssam_scan_selective_args* a, void* hip_stream)
+{
+    using namespace ssam;
+    if (!a) return SSAM_ERR_NULL;
+    if (int e = check_scan(a->dtype, a->channels, a->states, a->groups)) return e;
+    if (int e = check_sequences(a->seq)) return e;
+    if (a->seq.sequences == 0) return SSAM_OK;
+    const int esz = type_bytes(a->dtype);
+    if (!a->d_a) return SSAM_ERR_NULL;
+    for (const ssam_rows* r : {&a->in, &a->dt, &a->b, &a->c})
+        if (int e = check_rows(*r, a->seq, esz, false)) return e;
+    if (int e = check_rows(a->gate, a->seq, esz, true)) return e;
+    if (int e = check_out_rows(a->out, a->seq, a->channels, esz, false)) return e;
+    if (a->b_group < 0 || a->b_group > kMaxStride || a->c_group < 0 || a->c_group > kMaxStride) return SSAM_ERR_DIM;
+    for (const void* f : {(const void*)a->d_a, (const void*)a->d_skip, (const void*)a->d_dt_bias, (const void*)a->d_state, (const void*)a->d_final,
+                          (const void*)a->d_marks})
+        if ((uintptr_t)f % 4) return SSAM_ERR_DIM;
+    const Plan plan = plan_of(*a);
+    if (plan.bytes && !a->d_work) return SSAM_ERR_NULL;
+    if (plan.bytes && (a->work_bytes < plan.bytes || (uintptr_t)a->d_work % 16)) return SSAM_ERR_DIM;
+    const long long plane = (long long)a->channels * a->states * 4, state_bytes = a->seq.sequences * plane;
+    const Cover state = cover_plain(a->d_state, state_bytes);
+    const Cover outs[] = {cover_rows(a->out, a->seq, a->channels, esz), cover_plain(a->d_final, state_bytes),
+                          cover_plain(a->d_marks, piece_slots(a->seq, SSAM_MARK_ROWS) * plane),
+                          cover_plain(plan.bytes ? a->d_work : nullptr, (long long)plan.bytes)};
+    const Cover ins[] = {cover_rows(a->in, a->seq, a->channels, esz), cover_rows(a->dt, a->seq, a->channels, esz),
+                         cover_rows(a->gate, a->seq, a->channels, esz),
+                         cover_rows(a->b, a->seq, group_width(a->groups, a->states, a->b_group), esz),
+                         cover_rows(a->c, a->seq, group_width(a->groups, a->states, a->c_group), esz), cover_plain(a->d_a, plane),
+                         cover_plain(a->d_skip, a->channels * 4LL), cover_plain(a->d_dt_bias, a->channels * 4LL)};
+    if (any_overlap(outs, ins)) return SSAM_ERR_ALIAS;
+    for (int i = 0; i < 4; ++i)
+        if (overlaps(outs[i], state) && !(i == 1 && a->d_final == a->d_state)) return SSAM_ERR_ALIAS;
+
+    ScanParams p{};
+    p.pieces = make_pieces(a->seq, plan.piece);
+    p.mark_slots = make_pieces(a->seq, SSAM_MARK_ROWS);
+    p.in = a->in;
+    p.dt = a->dt;
+    p.gate = a->gate;
+    p.out = a->out;
+    p.b = a->b;
+    p.c = a->c;
+    p.b_group = a->b_group;
+    p.c_group = a->c_group;
+    p.a = a->d_a;
+    p.skip = a->d_skip;
+    p.dt_bias = a->d_dt_bias;
+    p.state = a->d_state;
+    p.final = a->d_final;
+    p.marks = a->d_marks;
+    p.channels = a->channels;
+    p.states = a->states;
+    p.group_channels = a->channels / a->groups;
+    p.per_group = tiles_per_group(a->channels, a->states, a->groups);
+    p.tiles = plan.tiles;
+    p.softplus = a->softplus != 0;
+    const long long blocks = plan.slots * plan.tiles;
+    const long long join = (plane / 4 + kBlock - 1) / kBlock * a->seq.sequences;
+    if (blocks > kMaxGrid || (plan.cut && join > kMaxGrid) || plane / 4 >= (1LL << 31)) return SSAM_ERR_DIM;
+    hipStream_t st = (hipStream_t)hip_stream;
+    return with_row_type(a->dtype, [&](auto t) {
+        return with_shape(a->states, [&](auto shape) {
+            using T = decltype(t);
+            using S = decltype(shape);
+            if (plan.cut) {
+                p.ends = static_cast<float*>(a->d_work);
+                p.sums = reinterpret_cast<float*>(static_cast<char*>(a->d_work) + plan.ends);
+                hipLaunchKernelGGL((scan_rows<T, S, false>), dim3((unsigned)blocks), dim3(kBlock), 0, st, p);
+                if (int e = launch_join(p.pieces, p.ends, p.sums, a->d_a, a->d_state, a->channels, a->states, false, st)) return e;
+                p.starts = p.ends;
+            }
+            hipLaunchKernelGGL((scan_rows<T, S, true>), dim3((unsigned)blocks), dim3(kBlock), 0, st, p);
+            return launched();
+        });
+    });
+}
+
+int ssam_scan_selective_step(const ssam_scan_selective_step_args* a, void* hip_stream)
+{
+    using namespace ssam;
+    if (!a) return SSAM_ERR_NULL;
+    if (int e = check_scan(a->dtype, a->channels, a->states, a->groups)) return e;
+    if (int e = check_slots(a->rows, a->slots, a->d_slots)) return e;
+    if (a->rows == 0) return SSAM_OK;
+    const int esz = type_bytes(a->dtype);
+    const ssam_sequences q{1, a->rows, nullptr, nullptr};
+    if (!a->d_a || !a->d_state) return SSAM_ERR_NULL;
+    for (const ssam_rows* r : {&a->in, &a->dt, &a->b, &a->c})
+        if (int e = check_rows(*r, q, esz, false)) return e;
+    if (int e = check_rows(a->gate, q, esz, true)) return e;
+    if (int e = check_out_rows(a->out, q, a->channels, esz, false)) return e;
+    if (a->b_group < 0 || a->b_group > kMaxStride || a->c_group < 0 || a->c_group > kMaxStride) return SSAM_ERR_DIM;
+    for (const void* f : {(const void*)a->d_a, (const void*)a->d_skip, (const void*)a->d_dt_bias, (const void*)a->d_state})
+        if ((uintptr_t)f % 4) return SSAM_ERR_DIM;
+    const long long slot = (long long)a->channels * a->states;
+    if (a->slot_stride < slot || a->slot_stride > kMaxStride) return SSAM_ERR_DIM;
+    const Cover outs[] = {cover_rows(a->out, q, a->channels, esz), cover_slots(a->d_state, a->slots, a->slot_stride, slot, 4)};
+    const Cover ins[] = {cover_rows(a->in, q, a->channels, esz), cover_rows(a->dt, q, a->channels, esz), cover_rows(a->gate, q, a->channels, esz),
+                         cover_rows(a->b, q, group_width(a->groups, a->states, a->b_group), esz),
+                         cover_rows(a->c, q, group_width(a->groups, a->states, a->c_group), esz), cover_plain(a->d_a, slot * 4),
+                         cover_plain(a->d_skip, a->channels * 4LL), cover_plain(a->d_dt_bias, a->channels * 4LL),
+                         cover_plain(a->d_slots, a->rows * 4LL)};
+    if (any_overlap(outs, ins)) return SSAM_ERR_ALIAS;
+    ScanStepParams p{};
+    p.rows = a->rows;
+    p.slots = a->slots;
+    p.channels = a->channels;
+    p.states = a->states;
+    p.group_channels = a->channels / a->groups;
+    p.per_group = (p.group_channels + kWave - 1) / kWave;
+    p.tiles = p.per_group * a->groups;
+    p.softplus = a->softplus != 0;
+    p.slot_of = a->d_slots;
+    p.in = a->in;
+    p.dt = a->dt;
+    p.gate = a->gate;
+    p.out = a->out;
+    p.b = a->b;
+    p.c = a->c;
+    p.b_group = a->b_group;
+    p.c_group = a->c_group;
+    p.a = a->d_a;
+    p.skip = a->d_skip;
+    p.dt_bias = a->d_dt_bias;
+    p.state = a->d_state;
+    p.slot_stride = a->slot_stride;
+    p.waves = (long long)a->rows * p.tiles;
+    const long long blocks = (p.waves + kWavesPerBlock - 1) / kWavesPerBlock;
+    if (blocks > kMaxGrid) return SSAM_ERR_DIM;
+    return with_row_type(a->dtype, [&](auto t) {
+        using T = decltype(t);
+        const dim3 grid((unsigned)blocks), block(kBlock);
+        hipStream_t st = (hipStream_t)hip_stream;
+        if (a->states <= 4) hipLaunchKernelGGL((scan_step<T, 1>), grid, block, 0, st, p);
+        else if (a->states <= 8) hipLaunchKernelGGL((scan_step<T, 2>), grid, block, 0, st, p);
+        else if (a->states <= 16) hipLaunchKernelGGL((scan_step<T, 4>), grid, block, 0, st, p);
+        else if (a->states <= 32) hipLaunchKernelGGL((scan_step<T, 8>), grid, block, 0, st, p);
+        else hipLaunchKernelGGL((scan_step<T, 16>), grid, block, 0, st, p);
+        return launched();
+    });
+}
+
+}  // extern "C"

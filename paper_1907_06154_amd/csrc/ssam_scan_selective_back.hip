@@ -1,0 +1,578 @@
+// Gradients of the selective scan.  With dy the gradient at y, per channel and state
+//     g_t = c_t dy_t + a_{t+1} g_{t+1}                     (a_t = exp(d_t a), x_t = a_t h_{t-1}, q_t = g_t x_t)
+//     db_t = sum over channels g_t d_t u_t,  dc_t = sum over channels h_t dy_t
+//     du_t = skip dy_t + d_t s_t,  dd_t = r_t + u_t s_t    with s_t = sum_n g_t b_t, r_t = sum_n a q_t
+//     da = sum_t d_t q_t,  dskip = sum_t dy_t u_t,  ddt_t = dd_t sigmoid(dt_t + bias),  dbias = sum_t ddt_t
+// The rows run backwards, in tiles of 16; a tile starts from the forward call's mark (the state before its first row), makes
+// its 16 x and a again into registers, 64 of each, and goes back over them: every exp is computed once.  (Marks every 16 rows cost
+// 4 bytes per row, channel and 16 states, written and read once; making the states again from sparser marks costs a second exp,
+// which is worth more time than those bytes.)
+//
+// The sums over channels: a wave's 16 channels by lane swaps between its rows of 16 lanes and DPP inside quads, the block's waves
+// through LDS, the blocks of a group through the workspace and a launch that adds them in order.
+#include "ssam_scan_selective.h"
+
+namespace ssam {
+namespace {
+
+constexpr int kTile = SSAM_MARK_ROWS;
+constexpr int kBackBlocks = 512;      // two blocks of four waves per compute unit: what 256 registers leave
+
+struct BackParams {
+    Pieces pieces, mark_slots;
+    ssam_rows in, dt, gate, b, c, grad_out;
+    long long b_group, c_group;
+    const float *a, *skip, *dt_bias, *marks, *grad_final;
+    ssam_rows grad_in, grad_dt, grad_gate, grad_b, grad_c;
+    float* grad_state;
+    float *ends, *sums;               // pieces: what reaches each from behind
+    float* part_bc;                   // [tile of the group][row][group][2][states]
+    float* part_param;                // [slot][channels x states, channels (skip), channels (bias)]
+    long long rows_total;
+    int channels, states, groups, group_channels, per_group, tiles, softplus, cut;
+};
+
+// Sums of v[0 .. 3] over the four rows of 16 lanes: afterwards row 0 holds v[0]'s, row 1 v[2]'s, row 2 v[1]'s, row 3 v[3]'s.
+__device__ __forceinline__ void swap_halves(float& a, float& b)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
+    const unsigned first = r[0], second = r[1];     // (a bit cast of a vector's element itself reads element 0)
+    a = __builtin_bit_cast(float, first);
+    b = __builtin_bit_cast(float, second);
+}
+__device__ __forceinline__ void swap_rows(float& a, float& b)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
+    const unsigned first = r[0], second = r[1];     // (a bit cast of a vector's element itself reads element 0)
+    a = __builtin_bit_cast(float, first);
+    b = __builtin_bit_cast(float, second);
+}
+__device__ __forceinline__ float rows_sum(float v0, float v1, float v2, float v3)
+{
+    swap_halves(v0, v1);
+    swap_halves(v2, v3);
+    float a = v0 + v1, b = v2 + v3;
+    swap_rows(a, b);
+    return a + b;
+}
+__device__ __forceinline__ int row_state(int lane) { return ((lane >> 5) & 1) | ((lane >> 3) & 2); }   // which of the four a lane then holds
+
+template <int CTRL>
+__device__ __forceinline__ float quad_moved(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float quad_sum(float v)
+{
+    v += quad_moved<0xB1>(v);   // [1, 0, 3, 2]
+    v += quad_moved<0x4E>(v);   // [2, 3, 0, 1]
+    return v;
+}
+template <int GL>
+__device__ __forceinline__ float channels_sum(float v)   // over the channels of a row of 16 lanes
+{
+    v = quad_sum(v);
+    if (GL == 2) v += quad_moved<0x141>(v);   // the other quad of eight lanes (mirrored; a quad's lanes are equal by now)
+    return v;
+}
+
+template <class T, class Shape>
+struct BackTile {
+    static constexpr int CB = Shape::kChannels, NP = Shape::kStates;
+    static constexpr int kEach = kTile * CB / kBlock;                       // values of a thread
+    static constexpr int kPairs = (kTile * NP + kBlock - 1) / kBlock;
+    RowVec<T, kEach> u, d, z, dout;
+    T b[kPairs], c[kPairs];
+};
+
+// kWhole: everything.  !kWhole: only what a piece lets out at its first row when nothing reaches it from behind.
+template <class T, class Shape, bool kWhole>
+__global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
+{
+    constexpr int GL = Shape::GL, NS = Shape::NS, NP = Shape::kStates, CB = Shape::kChannels, K = kTile;
+    using Tile = BackTile<T, Shape>;
+    constexpr int E = Tile::kEach, kPairs = Tile::kPairs;
+    constexpr int kKept = 64 / NS;                       // rows whose x and a are kept at a time
+    __shared__ RowVec<float, 2> dx[K][CB];               // d, d u
+    __shared__ float dys[K][CB];
+    __shared__ RowVec<float, 2> bc[K][NP];
+    __shared__ float ys[kWhole ? K : 1][CB];
+    __shared__ RowVec<float, 2> rs[kWhole ? K : 1][CB];  // r, s
+    __shared__ float sum_bc[kWhole ? kWavesPerBlock : 1][K][2][NP];
+
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
+    const int slot = blockIdx.x / p.tiles;
+    const ChannelTile ct = channel_tile(blockIdx.x % p.tiles, p.per_group, p.group_channels, CB);
+    const Piece q = find_piece(p.pieces, slot);
+    const long long plane = (long long)p.channels * p.states;
+    const int ch = wave * Shape::kWaveChannels + lane_channel<GL>(lane);
+    const bool live = ch < ct.n;
+    const int n0 = lane_group<GL>(lane) * NS;
+    const long long cell = (long long)(ct.c0 + ch) * p.states;
+    float* part_param = kWhole && p.part_param ? p.part_param + slot * (plane + 2LL * p.channels) : nullptr;
+    if (q.seq < 0) {
+        if (part_param) {       // an empty slot adds zeros
+            float none[NS] = {};
+            store_states<NS>(part_param + cell, n0, p.states, live, none);
+            if (tid < ct.n) part_param[plane + ct.c0 + tid] = part_param[plane + p.channels + ct.c0 + tid] = 0.0f;
+        }
+        return;
+    }
+    if (!kWhole && q.row0 == 0) return;                  // nothing lies before it
+
+    float a2[NS], g[NS], da[NS];
+    load_rates<NS>(p.a + cell, n0, p.states, live, a2);
+    const bool last = q.row0 + q.n >= q.len;
+    if (!kWhole) load_states<NS>(nullptr, 0, 0, false, g);
+    else if (p.cut) load_states<NS>(p.ends + slot * plane + cell, n0, p.states, live, g);
+    else load_states<NS>(p.grad_final + q.seq * plane + cell, n0, p.states, live && p.grad_final && last, g);
+#pragma unroll
+    for (int i = 0; i < NS; ++i) da[i] = 0.0f;
+    float sum = 0.0f;
+    const float* marks = nullptr;
+    if (kWhole) {
+        const int s0 = p.mark_slots.begin ? first_slot(p.mark_slots, q.seq) : q.seq * p.mark_slots.per;
+        marks = p.marks + (s0 + q.row0 / K) * plane + cell;
+    }
+
+    const int er = tid * E / CB, ec = tid * E % CB;
+    const int have = ct.n - ec < 0 ? 0 : ct.n - ec;
+    const long long at = q.row0 + er;
+    const T* __restrict__ in = sequence_base<T>(p.in, p.pieces, q) + at * p.in.row + ct.c0 + ec;
+    const T* __restrict__ dt = sequence_base<T>(p.dt, p.pieces, q) + at * p.dt.row + ct.c0 + ec;
+    const T* __restrict__ gate = p.gate.d ? sequence_base<T>(p.gate, p.pieces, q) + at * p.gate.row + ct.c0 + ec : nullptr;
+    const T* __restrict__ dout = sequence_base<T>(p.grad_out, p.pieces, q) + at * p.grad_out.row + ct.c0 + ec;
+    const T* __restrict__ pb = sequence_base<T>(p.b, p.pieces, q) + (long long)q.row0 * p.b.row + ct.group * p.b_group;
+    const T* __restrict__ pc = sequence_base<T>(p.c, p.pieces, q) + (long long)q.row0 * p.c.row + ct.group * p.c_group;
+    T* __restrict__ grad_in = kWhole && p.grad_in.d ? sequence_base<T>(p.grad_in, p.pieces, q) + at * p.grad_in.row + ct.c0 + ec : nullptr;
+    T* __restrict__ grad_dt = kWhole && p.grad_dt.d ? sequence_base<T>(p.grad_dt, p.pieces, q) + at * p.grad_dt.row + ct.c0 + ec : nullptr;
+    T* __restrict__ grad_gate =
+        kWhole && p.grad_gate.d && gate ? sequence_base<T>(p.grad_gate, p.pieces, q) + at * p.grad_gate.row + ct.c0 + ec : nullptr;
+    const long long row_total = (p.pieces.begin ? (long long)q.first : (long long)q.seq * p.pieces.rows) + q.row0;
+    float* part_bc = kWhole && p.part_bc
+                         ? p.part_bc + (((long long)(blockIdx.x % p.tiles - ct.group * p.per_group) * p.rows_total + row_total) * p.groups + ct.group) *
+                                           2 * p.states
+                         : nullptr;
+    float bias[E], skip[E], dskip[E], dbias[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        bias[e] = p.dt_bias && e < have ? p.dt_bias[ct.c0 + ec + e] : 0.0f;
+        skip[e] = kWhole && p.skip && e < have ? p.skip[ct.c0 + ec + e] : 0.0f;
+        dskip[e] = dbias[e] = 0.0f;
+    }
+
+    Tile now, next;
+    float mark_next[NS];
+    auto request = [&](int row) {
+        const int there = row + er < q.n ? have : 0;
+        next.u = load_row_vec<T, E>(in + (long long)row * p.in.row, kWhole ? there : 0);
+        next.d = load_row_vec<T, E>(dt + (long long)row * p.dt.row, there);
+        next.dout = load_row_vec<T, E>(dout + (long long)row * p.grad_out.row, there);
+        next.z = load_row_vec<T, E>(gate ? gate + (long long)row * p.gate.row : nullptr, gate ? there : 0);
+#pragma unroll
+        for (int e = 0; e < kPairs; ++e) {
+            const int i = tid + e * kBlock, r = i / NP, n = i % NP;
+            const bool is = i < K * NP && row + r < q.n && n < p.states;
+            next.b[e] = kWhole && is ? pb[(long long)(row + r) * p.b.row + n] : T(0);
+            next.c[e] = is ? pc[(long long)(row + r) * p.c.row + n] : T(0);
+        }
+        if (kWhole) load_states<NS>(marks + (row / K) * plane, n0, p.states, live, mark_next);
+    };
+
+    const int tiles = (q.n + K - 1) / K;
+    if (tiles > 0) request((tiles - 1) * K);
+    for (int tile = tiles - 1; tile >= 0; --tile) {
+        const int row = tile * K;
+        const int there = row + er < q.n ? have : 0;
+        now = next;
+        float mark[NS];
+#pragma unroll
+        for (int i = 0; i < NS; ++i) mark[i] = mark_next[i];
+        float dy[E], d[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            d[e] = (float)now.d[e] + bias[e];
+            float v = p.softplus ? softplus(d[e]) : d[e];
+            v = e < there ? v : 0.0f;
+            dy[e] = (float)now.dout[e];
+            if (gate) dy[e] *= silu((float)now.z[e]);
+            dy[e] = e < there ? dy[e] : 0.0f;
+            dx[er][ec + e] = RowVec<float, 2>{v, e < there ? v * (float)now.u[e] : 0.0f};
+            dys[er][ec + e] = dy[e];
+        }
+#pragma unroll
+        for (int e = 0; e < kPairs; ++e) {
+            const int i = tid + e * kBlock;
+            if (i < K * NP) bc[i / NP][i % NP] = RowVec<float, 2>{(float)now.b[e], (float)now.c[e]};
+        }
+        __syncthreads();
+        if (tile > 0) request(row - K);
+
+        if constexpr (!kWhole) {
+#pragma unroll 4
+            for (int t = K - 1; t >= 0; --t) {
+                const float dt_ = dx[t][ch][0], dyt = dys[t][ch];
+                sum += dt_;
+#pragma unroll
+                for (int m = 0; m < NS / 4; ++m) {
+                    const float w = bc[t][own_state<Shape>(lane, m)][1];
+#define SSAM_STATE(Q) g[4 * m + Q] = (quad_lane<Q>(w) * dyt + g[4 * m + Q]) * exp2_fast(dt_ * a2[4 * m + Q]);
+                    SSAM_STATE(0)
+                    SSAM_STATE(1)
+                    SSAM_STATE(2)
+                    SSAM_STATE(3)
+#undef SSAM_STATE
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (int part = K / kKept - 1; part >= 0; --part) {
+                float h[NS], xs[kKept][NS], as[kKept][NS];
+#pragma unroll
+                for (int i = 0; i < NS; ++i) h[i] = mark[i];
+                if (kKept < K)
+                    for (int t = 0; t < part * kKept; ++t) {
+                        const RowVec<float, 2> dv = dx[t][ch];
+#pragma unroll
+                        for (int m = 0; m < NS / 4; ++m) {
+                            const float w = bc[t][own_state<Shape>(lane, m)][0];
+#define SSAM_STATE(Q) h[4 * m + Q] = __builtin_fmaf(exp2_fast(dv[0] * a2[4 * m + Q]), h[4 * m + Q], quad_lane<Q>(w) * dv[1]);
+                            SSAM_STATE(0)
+                            SSAM_STATE(1)
+                            SSAM_STATE(2)
+                            SSAM_STATE(3)
+#undef SSAM_STATE
+                        }
+                    }
+#pragma unroll
+                for (int k = 0; k < kKept; ++k) {
+                    const int t = part * kKept + k;
+                    const RowVec<float, 2> dv = dx[t][ch];
+                    float y = 0.0f;
+#pragma unroll
+                    for (int m = 0; m < NS / 4; ++m) {
+                        const RowVec<float, 2> w = bc[t][own_state<Shape>(lane, m)];
+#define SSAM_STATE(Q)                                                                \
+    {                                                                                \
+        const int i = 4 * m + Q;                                                     \
+        as[k][i] = exp2_fast(dv[0] * a2[i]);                                         \
+        xs[k][i] = as[k][i] * h[i];                                                  \
+        h[i] = xs[k][i] + quad_lane<Q>(w[0]) * dv[1];                                \
+        y += quad_lane<Q>(w[1]) * h[i];                                              \
+    }
+                        SSAM_STATE(0)
+                        SSAM_STATE(1)
+                        SSAM_STATE(2)
+                        SSAM_STATE(3)
+#undef SSAM_STATE
+                    }
+                    ys[t][ch] = group_sum<GL>(y);
+                }
+#pragma unroll
+                for (int k = kKept - 1; k >= 0; --k) {
+                    const int t = part * kKept + k;
+                    const RowVec<float, 2> dv = dx[t][ch];
+                    const float dyt = dys[t][ch];
+                    float r = 0.0f, s = 0.0f;
+#pragma unroll
+                    for (int m = 0; m < NS / 4; ++m) {
+                        const RowVec<float, 2> w = bc[t][own_state<Shape>(lane, m)];
+                        float vb[4], vc[4];
+#define SSAM_STATE(Q)                                                                \
+    {                                                                                \
+        const int i = 4 * m + Q;                                                     \
+        const float b = quad_lane<Q>(w[0]);                                          \
+        vc[Q] = (xs[k][i] + b * dv[1]) * dyt;                                        \
+        g[i] += quad_lane<Q>(w[1]) * dyt;                                            \
+        vb[Q] = g[i] * dv[1];                                                        \
+        s += b * g[i];                                                               \
+        const float qi = g[i] * xs[k][i];                                            \
+        da[i] += dv[0] * qi;                                                         \
+        r += a2[i] * qi;                                                             \
+        g[i] *= as[k][i];                                                            \
+    }
+                        SSAM_STATE(0)
+                        SSAM_STATE(1)
+                        SSAM_STATE(2)
+                        SSAM_STATE(3)
+#undef SSAM_STATE
+                        const float tb = channels_sum<GL>(rows_sum(vb[0], vb[1], vb[2], vb[3]));
+                        const float tc = channels_sum<GL>(rows_sum(vc[0], vc[1], vc[2], vc[3]));
+                        sum_bc[wave][t][lane & 1][n0 + 4 * m + row_state(lane)] = lane & 1 ? tc : tb;
+                    }
+                    r = group_sum<GL>(r);
+                    s = group_sum<GL>(s);
+                    rs[t][ch] = RowVec<float, 2>{r, s};
+                }
+            }
+        }
+        __syncthreads();
+        if constexpr (kWhole) {
+            float du[E], ddt[E], dz[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const RowVec<float, 2> v = rs[er][ec + e];
+                const float u = (float)now.u[e];
+                const float step = dx[er][ec + e][0];
+                du[e] = __builtin_fmaf(skip[e], dy[e], step * v[1]);
+                float dd = __builtin_fmaf(u, v[1], v[0] * 0.693147180559945f);   // r was made with rates for exp2
+                if (p.softplus) dd *= sigmoid(d[e]);
+                ddt[e] = dd;
+                const bool is = e < there;
+                dskip[e] += is ? dy[e] * u : 0.0f;
+                dbias[e] += is ? dd : 0.0f;
+                if (gate) {
+                    const float z = (float)now.z[e], sig = sigmoid(z);
+                    dz[e] = (float)now.dout[e] * __builtin_fmaf(skip[e], u, ys[er][ec + e]) * (sig * __builtin_fmaf(z, 1.0f - sig, 1.0f));
+                } else {
+                    dz[e] = 0.0f;
+                }
+            }
+            if (grad_in) store_row_vec<T, E>(grad_in + (long long)row * p.grad_in.row, there, rounded<T, E>(du));
+            if (grad_dt) store_row_vec<T, E>(grad_dt + (long long)row * p.grad_dt.row, there, rounded<T, E>(ddt));
+            if (grad_gate) store_row_vec<T, E>(grad_gate + (long long)row * p.grad_gate.row, there, rounded<T, E>(dz));
+            if (part_bc) {
+#pragma unroll
+                for (int i = tid; i < K * 2 * NP; i += kBlock) {
+                    const int r = i / (2 * NP), w = i / NP % 2, n = i % NP;
+                    if (row + r < q.n && n < p.states) {
+                        float v = sum_bc[0][r][w][n];
+#pragma unroll
+                        for (int k = 1; k < kWavesPerBlock; ++k) v += sum_bc[k][r][w][n];
+                        part_bc[(long long)(row + r) * p.groups * 2 * p.states + w * p.states + n] = v;
+                    }
+                }
+            }
+            __syncthreads();      // the next tile's values go where these were read
+        }
+    }
+    if constexpr (kWhole) {
+        if (p.grad_state && q.row0 == 0) store_states<NS>(p.grad_state + q.seq * plane + cell, n0, p.states, live, g);
+        if (!part_param) return;
+        store_states<NS>(part_param + cell, n0, p.states, live, da);
+        // the tile's rows of every channel, added in order
+#pragma unroll
+        for (int e = 0; e < E; ++e) rs[er][ec + e] = RowVec<float, 2>{dskip[e], dbias[e]};
+        __syncthreads();
+        if (tid < ct.n) {
+            float s0 = 0.0f, s1 = 0.0f;
+#pragma unroll
+            for (int r = 0; r < K; ++r) {
+                s0 += rs[r][tid][0];
+                s1 += rs[r][tid][1];
+            }
+            part_param[plane + ct.c0 + tid] = s0;
+            part_param[plane + p.channels + ct.c0 + tid] = s1;
+        }
+    } else {
+        store_states<NS>(p.ends + slot * plane + cell, n0, p.states, live, g);
+        if (live && n0 == 0) p.sums[(long long)slot * p.channels + ct.c0 + ch] = sum;
+    }
+}
+
+// Gradients of b and c: the tiles of a group added up, rows of one piece to a block row.
+template <class T>
+__global__ __launch_bounds__(kBlock) void back_sum_bc(BackParams p, int blocks_each)
+{
+    const int slot = blockIdx.x / blocks_each;
+    const Piece q = find_piece(p.pieces, slot);
+    if (q.seq < 0) return;
+    const long long row_total = (p.pieces.begin ? (long long)q.first : (long long)q.seq * p.pieces.rows) + q.row0;
+    const int wide = p.groups * 2 * p.states;
+    const long long end = (long long)q.n * wide, apart = p.rows_total * wide;
+    const float* from = p.part_bc + row_total * wide;
+    for (long long i = (long long)(blockIdx.x % blocks_each) * kBlock + threadIdx.x; i < end; i += (long long)blocks_each * kBlock) {
+        float v = 0.0f;
+        for (int k = 0; k < p.per_group; ++k) v += from[k * apart + i];
+        const int r = (int)(i / wide), at = (int)(i % wide), grp = at / (2 * p.states), n = at % (2 * p.states);
+        const ssam_rows& to = n < p.states ? p.grad_b : p.grad_c;
+        if (to.d)
+            sequence_base<T>(to, p.pieces, q)[(long long)(q.row0 + r) * to.row + grp * p.states + (n < p.states ? n : n - p.states)] = (T)v;
+    }
+}
+
+// Sums over the slots, 16 interleaved runs of them and then the runs, always in the same order.
+constexpr int kRuns = 16;
+__global__ __launch_bounds__(kWave* kRuns) void back_sum_params(const float* __restrict__ parts, long long slots, long long plane, int channels,
+                                                                float* grad_a, float* grad_skip, float* grad_dt_bias)
+{
+    __shared__ float run[kRuns][kWave];
+    const int lane = threadIdx.x & (kWave - 1), r = threadIdx.x >> 6;
+    const long long wide = plane + 2LL * channels;
+    const long long i = (long long)blockIdx.x * kWave + lane;
+    float s = 0.0f;
+    if (i < wide)
+        for (long long k = r; k < slots; k += kRuns) s += parts[k * wide + i];
+    run[r][lane] = s;
+    __syncthreads();
+    if (r != 0 || i >= wide) return;
+#pragma unroll
+    for (int k = 1; k < kRuns; ++k) s += run[k][lane];
+    if (i < plane) {
+        if (grad_a) grad_a[i] = s;
+    } else if (i < plane + channels) {
+        if (grad_skip) grad_skip[i - plane] = s;
+    } else if (grad_dt_bias) {
+        grad_dt_bias[i - plane - channels] = s;
+    }
+}
+
+// As with_shape, but for eight states from one on: a tile of 256 channels would not fit the LDS twice.
+template <class F>
+int with_back_shape(int states, F f)
+{
+    if (states <= 8) return f(ScanShape<2, 4>{});
+    if (states <= 16) return f(ScanShape<4, 4>{});
+    if (states <= 32) return f(ScanShape<4, 8>{});
+    return f(ScanShape<4, 16>{});
+}
+
+struct BackPlan {
+    int per_group, tiles, piece;
+    long long slots, rows_total;
+    bool cut, params, bc;
+    size_t ends, sums, part_bc, part_param, bytes;
+};
+
+size_t whole_lines(size_t bytes) { return (bytes + 127) / 128 * 128; }
+
+BackPlan plan_of(const ssam_scan_selective_backward_args& a)
+{
+    BackPlan p{};
+    const int wide = a.states <= 8 ? 128 : 64;
+    p.per_group = (a.channels / a.groups + wide - 1) / wide;
+    p.tiles = p.per_group * a.groups;
+    p.piece = scan_piece_rows(a.seq, p.tiles, kBackBlocks);
+    p.slots = piece_slots(a.seq, p.piece);
+    p.rows_total = a.seq.d_begin ? a.seq.rows : (long long)a.seq.rows * a.seq.sequences;
+    p.cut = a.seq.rows > p.piece;
+    p.params = a.d_grad_a || a.d_grad_skip || a.d_grad_dt_bias;
+    p.bc = a.grad_b.d || a.grad_c.d;
+    const size_t plane = (size_t)a.channels * a.states;
+    p.ends = p.cut ? whole_lines(p.slots * plane * 4) : 0;
+    p.sums = p.cut ? whole_lines((size_t)p.slots * a.channels * 4) : 0;
+    p.part_bc = p.bc ? whole_lines((size_t)p.per_group * p.rows_total * a.groups * 2 * a.states * 4) : 0;
+    p.part_param = p.params ? whole_lines((size_t)p.slots * (plane + 2 * (size_t)a.channels) * 4) : 0;
+    p.bytes = p.ends + p.sums + p.part_bc + p.part_param;
+    return p;
+}
+
+}  // namespace
+}  // namespace ssam
+
+extern "C" {
+
+size_t ssam_scan_selective_backward_workspace_bytes(const ssam_scan_selective_backward_args* a)
+{
+    using namespace ssam;
+    if (!a || check_scan(a->dtype, a->channels, a->states, a->groups) || check_sequences(a->seq)) return 0;
+    return plan_of(*a).bytes;
+}
+
+int ssam_scan_selective_backward(const ssam_scan_selective_backward_args* a, void* hip_stream)
+{
+    using namespace ssam;
+    if (!a) return SSAM_ERR_NULL;
+    if (int e = check_scan(a->dtype, a->channels, a->states, a->groups)) return e;
+    if (int e = check_sequences(a->seq)) return e;
+    const BackPlan plan = plan_of(*a);
+    if (a->seq.sequences == 0 && !plan.params) return SSAM_OK;
+    const int esz = type_bytes(a->dtype);
+    if (!a->d_a || (!a->d_marks && a->seq.sequences > 0)) return SSAM_ERR_NULL;
+    for (const ssam_rows* r : {&a->in, &a->dt, &a->b, &a->c, &a->grad_out})
+        if (int e = check_rows(*r, a->seq, esz, false)) return e;
+    if (int e = check_rows(a->gate, a->seq, esz, true)) return e;
+    for (const ssam_rows* r : {&a->grad_in, &a->grad_dt, &a->grad_gate})
+        if (int e = check_out_rows(*r, a->seq, a->channels, esz, true)) return e;
+    const long long bc_width = (long long)a->groups * a->states;
+    for (const ssam_rows* r : {&a->grad_b, &a->grad_c})
+        if (int e = check_out_rows(*r, a->seq, bc_width, esz, true)) return e;
+    if (a->b_group < 0 || a->b_group > kMaxStride || a->c_group < 0 || a->c_group > kMaxStride) return SSAM_ERR_DIM;
+    for (const void* f : {(const void*)a->d_a, (const void*)a->d_skip, (const void*)a->d_dt_bias, (const void*)a->d_marks, (const void*)a->d_grad_final,
+                          (const void*)a->d_grad_a, (const void*)a->d_grad_skip, (const void*)a->d_grad_dt_bias, (const void*)a->d_grad_state})
+        if ((uintptr_t)f % 4) return SSAM_ERR_DIM;
+    if (plan.bytes && !a->d_work) return SSAM_ERR_NULL;
+    if (plan.bytes && (a->work_bytes < plan.bytes || (uintptr_t)a->d_work % 16)) return SSAM_ERR_DIM;
+    const long long plane = (long long)a->channels * a->states * 4, state_bytes = a->seq.sequences * plane, wide = a->channels * 4LL;
+    const Cover outs[] = {cover_rows(a->grad_in, a->seq, a->channels, esz), cover_rows(a->grad_dt, a->seq, a->channels, esz),
+                          cover_rows(a->grad_gate, a->seq, a->channels, esz), cover_rows(a->grad_b, a->seq, bc_width, esz),
+                          cover_rows(a->grad_c, a->seq, bc_width, esz), cover_plain(a->d_grad_a, plane), cover_plain(a->d_grad_skip, wide),
+                          cover_plain(a->d_grad_dt_bias, wide), cover_plain(a->d_grad_state, state_bytes),
+                          cover_plain(plan.bytes ? a->d_work : nullptr, (long long)plan.bytes)};
+    const Cover ins[] = {cover_rows(a->in, a->seq, a->channels, esz), cover_rows(a->dt, a->seq, a->channels, esz),
+                         cover_rows(a->gate, a->seq, a->channels, esz), cover_rows(a->grad_out, a->seq, a->channels, esz),
+                         cover_rows(a->b, a->seq, group_width(a->groups, a->states, a->b_group), esz),
+                         cover_rows(a->c, a->seq, group_width(a->groups, a->states, a->c_group), esz), cover_plain(a->d_a, plane),
+                         cover_plain(a->d_skip, wide), cover_plain(a->d_dt_bias, wide),
+                         cover_plain(a->d_marks, piece_slots(a->seq, SSAM_MARK_ROWS) * plane), cover_plain(a->d_grad_final, state_bytes)};
+    if (any_overlap(outs, ins)) return SSAM_ERR_ALIAS;
+
+    BackParams p{};
+    p.pieces = make_pieces(a->seq, plan.piece);
+    p.mark_slots = make_pieces(a->seq, SSAM_MARK_ROWS);
+    p.in = a->in;
+    p.dt = a->dt;
+    p.gate = a->gate;
+    p.b = a->b;
+    p.c = a->c;
+    p.grad_out = a->grad_out;
+    p.b_group = a->b_group;
+    p.c_group = a->c_group;
+    p.a = a->d_a;
+    p.skip = a->d_skip;
+    p.dt_bias = a->d_dt_bias;
+    p.marks = a->d_marks;
+    p.grad_final = a->d_grad_final;
+    p.grad_in = a->grad_in;
+    p.grad_dt = a->grad_dt;
+    p.grad_gate = a->grad_gate;
+    p.grad_b = a->grad_b;
+    p.grad_c = a->grad_c;
+    p.grad_state = a->d_grad_state;
+    char* work = static_cast<char*>(a->d_work);
+    if (plan.cut) {
+        p.ends = reinterpret_cast<float*>(work);
+        p.sums = reinterpret_cast<float*>(work + plan.ends);
+    }
+    if (plan.bc) p.part_bc = reinterpret_cast<float*>(work + plan.ends + plan.sums);
+    if (plan.params) p.part_param = reinterpret_cast<float*>(work + plan.ends + plan.sums + plan.part_bc);
+    p.rows_total = plan.rows_total;
+    p.channels = a->channels;
+    p.states = a->states;
+    p.groups = a->groups;
+    p.group_channels = a->channels / a->groups;
+    p.per_group = plan.per_group;
+    p.tiles = plan.tiles;
+    p.softplus = a->softplus != 0;
+    p.cut = plan.cut;
+    const long long blocks = plan.slots * plan.tiles;
+    const long long join = (plane / 4 + kBlock - 1) / kBlock * a->seq.sequences;
+    const long long param_blocks = (plane / 4 + 2LL * a->channels + kWave - 1) / kWave;
+    // rows of a piece x groups x 2 x states values, at most 64 of them to a thread
+    long long each = ((long long)plan.piece * bc_width * 2 + 64 * kBlock - 1) / (64 * kBlock);
+    if (each > 64) each = 64;
+    if (blocks > kMaxGrid || (plan.cut && join > kMaxGrid) || plane / 4 >= (1LL << 31) || param_blocks > kMaxGrid / 4 || plan.slots * each > kMaxGrid)
+        return SSAM_ERR_DIM;
+    hipStream_t st = (hipStream_t)hip_stream;
+    return with_row_type(a->dtype, [&](auto t) {
+        return with_back_shape(a->states, [&](auto shape) {
+            using T = decltype(t);
+            using S = decltype(shape);
+            if (blocks) {
+                if (plan.cut) {
+                    hipLaunchKernelGGL((scan_back<T, S, false>), dim3((unsigned)blocks), dim3(kBlock), 0, st, p);
+                    if (int e = launch_join(p.pieces, p.ends, p.sums, a->d_a, a->d_grad_final, a->channels, a->states, true, st)) return e;
+                }
+                hipLaunchKernelGGL((scan_back<T, S, true>), dim3((unsigned)blocks), dim3(kBlock), 0, st, p);
+                if (plan.bc)
+                    hipLaunchKernelGGL((back_sum_bc<T>), dim3((unsigned)(plan.slots * each)), dim3(kBlock), 0, st, p, (int)each);
+            }
+            if (plan.params)
+                hipLaunchKernelGGL(back_sum_params, dim3((unsigned)param_blocks), dim3(kWave * kRuns), 0, st, p.part_param, plan.slots, plane / 4,
+                                   a->channels, a->d_grad_a, a->d_grad_skip, a->d_grad_dt_bias);
+            return launched();
+        });
+    });
+}
+
+}  // extern "C"

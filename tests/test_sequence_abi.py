@@ -1,0 +1,297 @@
+"""Host-only checks of the sequence operators: every refusal of the C ABI, the sizes it plans, the structs that the binding packs
+and the references' own gradients.  Every call here fails validation, or has nothing to do, before anything is launched."""
+import ctypes
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+import paper_1907_06154_amd as ssam
+import paper_1907_06154_amd.sequence as seq
+import sequence_reference as ref
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+OK, NULL, DIM, SHAPE, ENUM, ALIAS = range(6)
+vp, ci, ll, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_size_t
+
+
+class Rows(ctypes.Structure):
+    _fields_ = [("d", vp), ("batch", ll), ("row", ll)]
+
+
+class Seq(ctypes.Structure):
+    _fields_ = [("sequences", ci), ("rows", ci), ("begin", vp), ("end", vp)]
+
+
+def struct(name, ints, *rest):
+    return type(name, (ctypes.Structure,), {"_fields_": [(n, ci) for n in ints.split()] + [f for fields in rest for f in fields]})
+
+
+def many(kind, names):
+    return [(n, kind) for n in names.split()]
+
+
+Conv = struct("Conv", "dtype param_dtype channels taps silu", many(Seq, "seq"), many(Rows, "x out"), many(vp, "weight bias state final"))
+ConvBack = struct("ConvBack", "dtype param_dtype channels taps silu", many(Seq, "seq"), many(Rows, "x grad_out grad_in"),
+                  many(vp, "weight bias state grad_final grad_weight grad_bias grad_state work"), many(sz, "work_bytes"))
+ConvStep = struct("ConvStep", "dtype param_dtype channels taps silu rows slots", many(vp, "slot_of"), many(Rows, "x out"), many(vp, "weight bias state"),
+                  many(ll, "slot_stride"))
+Scan = struct("Scan", "dtype channels states groups softplus", many(Seq, "seq"), many(Rows, "x dt gate out b c"), many(ll, "b_group c_group"),
+              many(vp, "a skip dt_bias state final marks work"), many(sz, "work_bytes"))
+ScanBack = struct("ScanBack", "dtype channels states groups softplus", many(Seq, "seq"), many(Rows, "x dt gate b c grad_out"),
+                  many(ll, "b_group c_group"), many(vp, "a skip dt_bias marks grad_final"), many(Rows, "grad_in grad_dt grad_gate grad_b grad_c"),
+                  many(vp, "grad_a grad_skip grad_dt_bias grad_state work"), many(sz, "work_bytes"))
+ScanStep = struct("ScanStep", "dtype channels states groups softplus rows slots", many(vp, "slot_of"), many(Rows, "x dt gate out b c"),
+                  many(ll, "b_group c_group"), many(vp, "a skip dt_bias state"), many(ll, "slot_stride"))
+
+
+@pytest.fixture(scope="module")
+def L():
+    return seq._load()
+
+
+def at(k):
+    """Made-up addresses, 16 MiB apart: never dereferenced."""
+    return 0x10000000 + (k << 24)
+
+
+def call(L, name, s):
+    return getattr(L, name)(ctypes.cast(ctypes.byref(s), ctypes.c_char_p), None)
+
+
+def size(L, name, s):
+    return getattr(L, name)(ctypes.cast(ctypes.byref(s), ctypes.c_char_p))
+
+
+def test_the_binding_packs_the_structs():
+    for kind, packed in ((Conv, seq._CONV1D), (ConvBack, seq._CONV1D_BACK), (ConvStep, seq._CONV1D_STEP), (Scan, seq._SCAN), (ScanBack, seq._SCAN_BACK),
+                         (ScanStep, seq._SCAN_STEP)):
+        assert ctypes.sizeof(kind) == packed.size, kind
+        # the same order of fields: every one set to a value of its own
+        flat = []
+
+        def fill(obj):
+            for n, t in obj._fields_:
+                if issubclass(t, ctypes.Structure):
+                    fill(getattr(obj, n))
+                else:
+                    flat.append(len(flat) + 1)
+                    setattr(obj, n, len(flat))
+        s = kind()
+        fill(s)
+        assert bytes(s) == packed.pack(*flat), kind
+
+
+def test_the_header_is_c_and_has_these_sizes(tmp_path):
+    kinds = {"ssam_conv1d_args": Conv, "ssam_conv1d_backward_args": ConvBack, "ssam_conv1d_step_args": ConvStep, "ssam_scan_selective_args": Scan,
+             "ssam_scan_selective_backward_args": ScanBack, "ssam_scan_selective_step_args": ScanStep}
+    checks = "".join(f"_Static_assert(sizeof({n}) == {ctypes.sizeof(k)}, \"{n}\");\n" for n, k in kinds.items())
+    checks += "".join(f"_Static_assert(offsetof(ssam_scan_selective_backward_args, {n}) == {getattr(ScanBack, m).offset}, \"{n}\");\n"
+                      for n, m in (("grad_in", "grad_in"), ("d_grad_a", "grad_a"), ("work_bytes", "work_bytes"), ("b_group", "b_group")))
+    (tmp_path / "c.c").write_text('#include "ssam_sequence.h"\n' + checks)
+    subprocess.run(["gcc", "-std=c11", "-Wall", "-Werror", "-pedantic", "-I", os.path.join(ROOT, "include"), "-c", "-o", str(tmp_path / "c.o"),
+                    str(tmp_path / "c.c")], check=True)
+    assert seq.MARK_ROWS == 16 and seq.MAX_TAPS == 8 and seq.MAX_STATES == 64
+
+
+def conv(**change):
+    s = Conv(dtype=3, param_dtype=3, channels=64, taps=4, silu=1, seq=Seq(2, 10, None, None), x=Rows(at(0), 640, 64), out=Rows(at(1), 640, 64),
+             weight=at(2), bias=at(3), state=at(4), final=at(5))
+    for k, v in change.items():
+        setattr(s, k, v)
+    return s
+
+
+def test_conv1d_refusals(L):
+    f = lambda **c: call(L, "ssam_conv1d", conv(**c))  # noqa: E731
+    assert L.ssam_conv1d(None, None) == NULL
+    assert f(weight=None) == NULL and f(x=Rows(None, 640, 64)) == NULL and f(out=Rows(None, 640, 64)) == NULL
+    assert f(dtype=1) == ENUM and f(dtype=7) == ENUM and f(param_dtype=2) == ENUM
+    assert f(taps=0) == SHAPE and f(taps=9) == SHAPE and f(channels=0) == DIM and f(channels=1 << 25) == DIM
+    assert f(seq=Seq(-1, 10, None, None)) == DIM and f(seq=Seq(2, -1, None, None)) == DIM and f(seq=Seq(2, 10, at(8), None)) == NULL
+    assert f(seq=Seq(2, 10, at(8) + 2, at(8) + 6)) == DIM
+    assert f(x=Rows(at(0) + 1, 640, 64)) == DIM and f(x=Rows(at(0), 640, -64)) == DIM and f(weight=at(2) + 1) == DIM
+    assert f(out=Rows(at(1), 640, 63)) == DIM and f(out=Rows(at(1), 600, 64)) == DIM        # rows of the result that share elements
+    assert f(out=Rows(at(0), 640, 64)) == ALIAS and f(out=Rows(at(0) + 2 * 639, 640, 64)) == ALIAS
+    assert f(final=at(0) + 4) == ALIAS and f(final=at(4) + 16) == ALIAS and f(out=Rows(at(4), 640, 64)) == ALIAS
+    # nothing to do
+    assert f(seq=Seq(0, 10, None, None), x=Rows(None, 0, 0), out=Rows(None, 0, 0)) == OK
+    # columns of one buffer are no overlap: refused for what is checked last (more blocks than a launch holds), not for aliasing
+    wide = dict(channels=1024, seq=Seq(1, 1 << 30, None, None), weight=at(-2), bias=None, state=None, final=None, taps=1)
+    assert f(x=Rows(at(0), 0, 2048), out=Rows(at(0) + 2048, 0, 2048), **wide) == DIM
+    assert f(x=Rows(at(0), 0, 2048), out=Rows(at(0) + 2046, 0, 2048), **wide) == ALIAS
+    assert f(x=Rows(at(0) + 2048, 0, 2048), out=Rows(at(0), 0, 2048), **wide) == DIM
+    assert f(x=Rows(at(0) + 2048, 0, 2048), out=Rows(at(0) + 2, 0, 2048), **wide) == ALIAS
+
+
+def test_conv1d_backward_refusals(L):
+    def make(**change):
+        s = ConvBack(dtype=3, param_dtype=0, channels=64, taps=4, silu=1, seq=Seq(2, 10, None, None), x=Rows(at(0), 640, 64),
+                     grad_out=Rows(at(1), 640, 64), grad_in=Rows(at(2), 640, 64), weight=at(3), bias=at(4), state=at(5), grad_final=at(6),
+                     grad_weight=at(7), grad_bias=at(8), grad_state=at(9), work=at(10), work_bytes=1 << 20)
+        for k, v in change.items():
+            setattr(s, k, v)
+        return s
+    f = lambda **c: call(L, "ssam_conv1d_backward", make(**c))  # noqa: E731
+    need = size(L, "ssam_conv1d_backward_workspace_bytes", make())
+    assert need == 2 * 2 * 5 * 64 * 4                       # 2 pieces of 8 rows a sequence, 4 taps and the bias
+    assert size(L, "ssam_conv1d_backward_workspace_bytes", make(grad_weight=None, grad_bias=None)) == 0
+    assert size(L, "ssam_conv1d_backward_workspace_bytes", make(taps=9)) == 0 and L.ssam_conv1d_backward_workspace_bytes(None) == 0
+    assert f(weight=None) == NULL and f(grad_out=Rows(None, 0, 0)) == NULL and f(work=None) == NULL and f(x=Rows(None, 0, 0)) == NULL
+    assert f(work_bytes=need - 1) == DIM and f(work=at(10) + 8) == DIM and f(grad_weight=at(7) + 2) == DIM and f(grad_in=Rows(at(2), 640, 32)) == DIM
+    assert f(dtype=1) == ENUM and f(taps=0) == SHAPE
+    for k in ("grad_weight", "grad_bias", "grad_state", "work"):
+        assert f(**{k: at(0)}) == ALIAS and f(**{k: at(3)}) == ALIAS, k
+    assert f(grad_in=Rows(at(1), 640, 64)) == ALIAS and f(grad_weight=at(8)) == ALIAS
+    assert f(seq=Seq(0, 0, None, None), grad_weight=None, grad_bias=None) == OK
+
+
+def test_conv1d_step_refusals(L):
+    def make(**change):
+        s = ConvStep(dtype=2, param_dtype=2, channels=64, taps=4, silu=1, rows=5, slots=9, slot_of=at(0), x=Rows(at(1), 0, 64), out=Rows(at(2), 0, 64),
+                     weight=at(3), bias=at(4), state=at(5), slot_stride=192)
+        for k, v in change.items():
+            setattr(s, k, v)
+        return s
+    f = lambda **c: call(L, "ssam_conv1d_step", make(**c))  # noqa: E731
+    assert f(weight=None) == NULL and f(state=None) == NULL and f(x=Rows(None, 0, 64)) == NULL
+    assert f(rows=-1) == DIM and f(slots=-1) == DIM and f(slot_stride=191) == DIM and f(slot_of=at(0) + 1) == DIM and f(state=at(5) + 1) == DIM
+    assert f(dtype=1) == ENUM and f(taps=9) == SHAPE and f(channels=-4) == DIM
+    assert f(state=at(1)) == ALIAS and f(out=Rows(at(5) + 200, 0, 64)) == ALIAS and f(out=Rows(at(0), 0, 64)) == ALIAS and f(out=Rows(at(1), 0, 64)) == ALIAS
+    assert f(rows=0) == OK
+
+
+def scan(**change):
+    rows = {n: Rows(at(i), 640, 64) for i, n in enumerate(("x", "dt", "gate", "out"))}
+    s = Scan(dtype=3, channels=64, states=16, groups=2, softplus=1, seq=Seq(2, 10, None, None), b=Rows(at(4), 640, 64), c=Rows(at(4) + 64, 640, 64),
+             b_group=16, c_group=16, a=at(5), skip=at(6), dt_bias=at(7), state=at(8), final=at(9), marks=at(10), work=at(11), work_bytes=1 << 20, **rows)
+    for k, v in change.items():
+        setattr(s, k, v)
+    return s
+
+
+def test_scan_selective_refusals(L):
+    f = lambda **c: call(L, "ssam_scan_selective", scan(**c))  # noqa: E731
+    assert L.ssam_scan_selective(None, None) == NULL
+    for n in ("x", "dt", "out", "b", "c"):
+        assert f(**{n: Rows(None, 0, 0)}) == NULL, n
+        assert f(**{n: Rows(at(20) + 1, 640, 64)}) == DIM, n
+        assert f(**{n: Rows(at(20), 640, -1)}) == DIM, n
+    assert f(a=None) == NULL and f(a=at(5) + 2) == DIM and f(state=at(8) + 2) == DIM and f(b_group=-1) == DIM
+    assert f(dtype=1) == ENUM and f(dtype=-1) == ENUM
+    assert f(states=0) == SHAPE and f(states=65) == SHAPE and f(groups=0) == SHAPE and f(groups=3) == SHAPE
+    assert f(channels=0) == DIM and f(out=Rows(at(3), 640, 60)) == DIM and f(out=Rows(at(3), 64, 64)) == DIM
+    for n in ("x", "dt", "gate", "b", "c"):
+        assert f(out=getattr(scan(), n)) == ALIAS, n
+    for n in ("a", "skip", "dt_bias", "marks"):
+        assert f(final=getattr(scan(), n)) == ALIAS, n
+    assert f(final=at(8) + 64) == ALIAS and f(marks=at(8)) == ALIAS and f(out=Rows(at(8), 640, 64)) == ALIAS
+    assert f(seq=Seq(0, 0, None, None)) == OK
+    long = dict(seq=Seq(1, 4096, None, None), x=Rows(at(0), 0, 64), dt=Rows(at(1), 0, 64), out=Rows(at(3), 0, 64))
+    need = size(L, "ssam_scan_selective_workspace_bytes", scan(**long))
+    assert need > 0 and f(work=None, **long) == NULL and f(work_bytes=need - 1, **long) == DIM and f(work=at(11) + 8, **long) == DIM
+    assert f(work=at(9), **long) == ALIAS and f(work=at(8) + 64, **long) == ALIAS
+
+
+def test_scan_selective_plans(L):
+    marks = lambda **c: size(L, "ssam_scan_selective_marks", scan(**c))  # noqa: E731
+    work = lambda **c: size(L, "ssam_scan_selective_workspace_bytes", scan(**c))  # noqa: E731
+    assert marks() == 2 and marks(seq=Seq(3, 16, None, None)) == 3 and marks(seq=Seq(3, 17, None, None)) == 6 and marks(seq=Seq(3, 0, None, None)) == 3
+    assert marks(seq=Seq(3, 33, at(20), at(20) + 4)) == 5 and marks(dtype=9) == 0
+    assert work() == 0 and work(seq=Seq(1, 64, None, None)) == 0
+    # few sequences are cut into pieces: their states and their time steps' sums; many are not
+    assert work(groups=1, seq=Seq(1, 65, None, None)) == 2 * (64 * 16 + 64) * 4
+    assert work(groups=1, channels=4096, seq=Seq(16, 4096, None, None)) == 0
+    assert work(states=77) == 0 and L.ssam_scan_selective_workspace_bytes(None) == 0
+
+
+def test_scan_selective_backward_refusals(L):
+    def make(**change):
+        rows = {n: Rows(at(i), 640, 64) for i, n in enumerate(("x", "dt", "gate", "b", "c", "grad_out", "grad_in", "grad_dt", "grad_gate"))}
+        s = ScanBack(dtype=0, channels=64, states=16, groups=2, softplus=1, seq=Seq(2, 10, None, None), grad_b=Rows(at(9), 320, 32),
+                     grad_c=Rows(at(10), 320, 32), b_group=16, c_group=16, a=at(11), skip=at(12), dt_bias=at(13), marks=at(14), grad_final=at(15),
+                     grad_a=at(16), grad_skip=at(17), grad_dt_bias=at(18), grad_state=at(19), work=at(20), work_bytes=1 << 22, **rows)
+        for k, v in change.items():
+            setattr(s, k, v)
+        return s
+    f = lambda **c: call(L, "ssam_scan_selective_backward", make(**c))  # noqa: E731
+    need = size(L, "ssam_scan_selective_backward_workspace_bytes", make())
+    assert need > 0 and f(work=None) == NULL and f(work_bytes=need - 1) == DIM and f(work=at(20) + 4) == DIM
+    for n in ("x", "dt", "b", "c", "grad_out"):
+        assert f(**{n: Rows(None, 0, 0)}) == NULL and f(**{n: Rows(at(30) + 2, 640, 64)}) == DIM, n
+    assert f(a=None) == NULL and f(marks=None) == NULL and f(marks=at(14) + 2) == DIM and f(c_group=-1) == DIM
+    assert f(grad_b=Rows(at(9), 320, 31)) == DIM and f(grad_in=Rows(at(6), 640, 63)) == DIM
+    assert f(dtype=1) == ENUM and f(states=65) == SHAPE and f(groups=5) == SHAPE and f(channels=0) == DIM
+    for n in ("grad_a", "grad_skip", "grad_dt_bias", "grad_state", "work"):
+        assert f(**{n: at(0)}) == ALIAS and f(**{n: at(14)}) == ALIAS, n
+    assert f(grad_in=Rows(at(5), 640, 64)) == ALIAS and f(grad_c=Rows(at(9), 320, 32)) == ALIAS and f(grad_gate=Rows(at(2), 640, 64)) == ALIAS
+    assert f(seq=Seq(0, 0, None, None), grad_a=None, grad_skip=None, grad_dt_bias=None) == OK
+
+
+def test_scan_selective_step_refusals(L):
+    def make(**change):
+        rows = {n: Rows(at(i), 0, 64) for i, n in enumerate(("x", "dt", "gate", "out", "b", "c"))}
+        s = ScanStep(dtype=2, channels=64, states=16, groups=2, softplus=1, rows=5, slots=7, slot_of=at(6), b_group=16, c_group=16, a=at(7), skip=at(8),
+                     dt_bias=at(9), state=at(10), slot_stride=1024, **rows)
+        for k, v in change.items():
+            setattr(s, k, v)
+        return s
+    f = lambda **c: call(L, "ssam_scan_selective_step", make(**c))  # noqa: E731
+    for n in ("x", "dt", "out", "b", "c"):
+        assert f(**{n: Rows(None, 0, 0)}) == NULL and f(**{n: Rows(at(20) + 1, 0, 64)}) == DIM, n
+    assert f(a=None) == NULL and f(state=None) == NULL and f(slot_stride=1023) == DIM and f(rows=-2) == DIM and f(slots=-1) == DIM
+    assert f(dtype=1) == ENUM and f(states=0) == SHAPE and f(groups=7) == SHAPE
+    assert f(state=at(0)) == ALIAS and f(out=Rows(at(10) + 4096, 0, 64)) == ALIAS and f(out=Rows(at(2), 0, 64)) == ALIAS and f(state=at(6)) == ALIAS
+    assert f(rows=0) == OK
+
+
+def test_tensors_must_live_on_the_gpu():
+    import torch
+    x, w = torch.zeros(4, 8), torch.zeros(8, 4)
+    with pytest.raises(ValueError, match="GPU"):
+        ssam.ssam_conv1d(x, w)
+    with pytest.raises(ValueError, match="GPU"):
+        ssam.ssam_scan_selective(x, x, w, x.view(4, 1, 8), x.view(4, 1, 8))
+
+
+def test_the_references_gradients_against_differences():
+    """In 64 bits, e = 1e-6: the differences are off by e^2 and 1e-16 / e."""
+    rng = np.random.default_rng(1)
+    n, D, N, W, e = 9, 3, 4, 4, 1e-6
+    v = {"x": rng.normal(size=(n, D)), "w": rng.normal(size=(D, W)), "b": rng.normal(size=D), "s": rng.normal(size=(W - 1, D))}
+    r, rs = rng.normal(size=(n, D)), rng.normal(size=(W - 1, D))
+
+    def slopes(loss, v):
+        for k in v:
+            g = np.zeros_like(v[k])
+            for i in np.ndindex(*v[k].shape):
+                up, down = dict(v), dict(v)
+                up[k], down[k] = v[k].copy(), v[k].copy()
+                up[k][i] += e
+                down[k][i] -= e
+                g[i] = (loss(up) - loss(down)) / (2 * e)
+            yield k, g
+
+    for silu in (False, True):
+        def loss(v):
+            y, last, _ = ref.conv1d(v["x"], v["w"], v["b"], silu, v["s"])
+            return (y * r).sum() + (last * rs).sum()
+        dx, dw, db, ds = ref.conv1d_back(r, v["x"], v["w"], v["b"], silu, v["s"], rs)[0]
+        for k, g in slopes(loss, v):
+            assert np.allclose(g, {"x": dx, "w": dw, "b": db, "s": ds}[k], atol=1e-8, rtol=1e-7), (silu, k)
+    for gate in (False, True):
+        v = {"x": rng.normal(size=(n, D)), "d": rng.uniform(0.1, 1, (n, D)), "a": -rng.uniform(0.1, 2, (D, N)), "b": rng.normal(size=(n, D, N)),
+             "c": rng.normal(size=(n, D, N)), "skip": rng.normal(size=D), "state": rng.normal(size=(D, N))}
+        if gate:
+            v["gate"] = rng.normal(size=(n, D))
+        rl = rng.normal(size=(D, N))
+
+        def loss(v):
+            y, last = ref.scan(v["x"], v["d"], v["a"], v["b"], v["c"], v["skip"], v.get("gate"), v["state"])
+            return (y * r).sum() + (last * rl).sum()
+        got = ref.scan_back(r, v["x"], v["d"], v["a"], v["b"], v["c"], v["skip"], v.get("gate"), v["state"], rl)
+        size_ = ref.scan_back(r, v["x"], v["d"], v["a"], v["b"], v["c"], v["skip"], v.get("gate"), v["state"], rl, size=True)
+        for k, g in slopes(loss, v):
+            assert np.allclose(g, got[k], atol=1e-7, rtol=1e-6), (gate, k)
+            assert (np.abs(got[k]) <= size_[k] * (1 + 1e-12)).all(), k
