@@ -20,11 +20,12 @@ template <class T, int V> using RowVec = T __attribute__((ext_vector_type(V)));
 
 // Channels p[0 .. have): zeros behind them.  A whole vector is one access at the element's alignment (global memory takes
 // unaligned vectors on this target), so rows of any stride keep 16 bytes per lane.
+// (`part`: that `have` may be less, where the caller knows it does not.)
 template <class T, int V>
-__device__ __forceinline__ RowVec<T, V> load_row_vec(const T* __restrict__ p, int have)
+__device__ __forceinline__ RowVec<T, V> load_row_vec(const T* __restrict__ p, int have, bool part = true)
 {
     RowVec<T, V> v;
-    if (have >= V) {
+    if (!part || have >= V) {
         __builtin_memcpy(&v, p, sizeof(v));
     } else {
 #pragma unroll
@@ -34,9 +35,9 @@ __device__ __forceinline__ RowVec<T, V> load_row_vec(const T* __restrict__ p, in
 }
 
 template <class T, int V>
-__device__ __forceinline__ void store_row_vec(T* __restrict__ p, int have, const RowVec<T, V>& v)
+__device__ __forceinline__ void store_row_vec(T* __restrict__ p, int have, const RowVec<T, V>& v, bool part = true)
 {
-    if (have >= V) {
+    if (!part || have >= V) {
         __builtin_memcpy(p, &v, sizeof(v));
     } else {
 #pragma unroll
@@ -71,23 +72,14 @@ __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_ex
 __device__ __forceinline__ float sigmoid(float x) { return __builtin_amdgcn_rcpf(1.0f + exp2_fast(-kLog2e * x)); }
 __device__ __forceinline__ float silu(float x) { return x * sigmoid(x); }
 
-// log(1 + exp(x)) = max(x, 0) + log1p(e) with e = exp(-|x|) in (0, 1].  log1p(e) = 2 atanh(s), s = e / (2 + e) <= 1/3, by its
-// series up to s^15 (the next term is below 2^-28 of the sum): the relative error stays a few 2^-24 however small e is, which
-// 1 + e in fp32 would lose -- the time steps of a trained layer are 0.001 .. 0.1, that is e of the same size.
+// log(1 + exp(x)) = max(x, 0) + log1p(e) with e = exp(-|x|) in (0, 1].  t = 1 + e loses the low bits of a small e, and the time
+// steps of a trained layer are 0.001 .. 0.1, that is e of the same size; e - (t - 1), which is exact, puts them back (log(t) changes
+// by that over t, and where it matters t is 1).  The hardware's log2 is within 2 u of its value near 1 too, so the sum is within 4 u.
 __device__ __forceinline__ float softplus(float x)
 {
     const float e = exp2_fast(-kLog2e * __builtin_fabsf(x));
-    const float s = e * __builtin_amdgcn_rcpf(2.0f + e);
-    const float q = s * s;
-    float r = 1.0f / 15.0f;
-    r = r * q + 1.0f / 13.0f;
-    r = r * q + 1.0f / 11.0f;
-    r = r * q + 1.0f / 9.0f;
-    r = r * q + 1.0f / 7.0f;
-    r = r * q + 0.2f;
-    r = r * q + 1.0f / 3.0f;
-    r = r * q + 1.0f;
-    return __builtin_fmaxf(x, 0.0f) + 2.0f * s * r;   // NaN comes through e
+    const float t = 1.0f + e;
+    return __builtin_fmaxf(x, 0.0f) + __builtin_fmaf(0.693147180559945f, __builtin_amdgcn_logf(t), e - (t - 1.0f));   // NaN comes through e
 }
 
 // ---- sequences ---------------------------------------------------------------------------------------------------------
@@ -234,6 +226,7 @@ inline int type_bytes(int dtype) { return dtype == SSAM_F32 ? 4 : dtype == SSAM_
 
 constexpr long long kMaxChannels = 1 << 24;
 constexpr long long kMaxStride = 1LL << 40;      // elements: offsets of any row then fit 64 bits
+constexpr long long kMaxTileStride = 1 << 24;    // elements from row to row where a tile's offsets (32 rows of 4 bytes) have 32 bits
 
 // What a tensor covers: `count` rows (batch after batch) of `width` bytes, `step` bytes apart; one = a plain range.
 struct Cover {
@@ -276,6 +269,9 @@ inline int check_rows(const ssam_rows& r, const ssam_sequences& q, int esz, bool
     if ((uintptr_t)r.d % esz || r.row < 0 || r.row > kMaxStride || (!q.d_begin && (r.batch < 0 || r.batch > kMaxStride))) return SSAM_ERR_DIM;
     return SSAM_OK;
 }
+
+// Rows that are read and written in tiles.
+inline int check_tile_rows(const ssam_rows& r, const ssam_sequences& q) { return r.d && q.rows > 1 && r.row > kMaxTileStride ? SSAM_ERR_DIM : SSAM_OK; }
 
 // A result's rows must not share elements with one another either.
 inline int check_out_rows(const ssam_rows& r, const ssam_sequences& q, long long width, int esz, bool optional)

@@ -46,8 +46,57 @@ __device__ __forceinline__ float group_sum(float v)
     return v;
 }
 
-// Index of the value that lane (group, quad lane) loads as number m: state group * NS + 4 m + quad lane.
-template <class Shape> __device__ __forceinline__ int own_state(int lane, int m) { return lane_group<Shape::GL>(lane) * Shape::NS + 4 * m + (lane & 3); }
+// Four rows' y += c0 h0 + c1 h1 + c2 h2 + c3 h3 (kFirst: y = ..), with cQ the value of lane Q of the quad: multiply-adds that take it by
+// DPP themselves (the compiler moves it into a register first, twice the instructions).  A DPP read must lie two wait states behind
+// the write of its register, and the compiler counts neither into nor out of these blocks: hence the s_nop, and the order row by row.
+// y leaves only through another of these blocks or into memory, never into a DPP of the compiler's.
+template <bool kFirst>
+__device__ __forceinline__ void quad_dots(float (&y)[4], const float (&c)[4], const float (&h)[4][4])
+{
+#define SSAM_DOT(OP, Q, A, B, C, D)                                                                                \
+    OP " %0, %4, %" #A " quad_perm:[" #Q "," #Q "," #Q "," #Q "] row_mask:0xf bank_mask:0xf\n\t"                     \
+    OP " %1, %5, %" #B " quad_perm:[" #Q "," #Q "," #Q "," #Q "] row_mask:0xf bank_mask:0xf\n\t"                     \
+    OP " %2, %6, %" #C " quad_perm:[" #Q "," #Q "," #Q "," #Q "] row_mask:0xf bank_mask:0xf\n\t"                     \
+    OP " %3, %7, %" #D " quad_perm:[" #Q "," #Q "," #Q "," #Q "] row_mask:0xf bank_mask:0xf\n\t"
+#define SSAM_INPUTS                                                                                                \
+    "v"(c[0]), "v"(c[1]), "v"(c[2]), "v"(c[3]), "v"(h[0][0]), "v"(h[1][0]), "v"(h[2][0]), "v"(h[3][0]), "v"(h[0][1]), \
+        "v"(h[1][1]), "v"(h[2][1]), "v"(h[3][1]), "v"(h[0][2]), "v"(h[1][2]), "v"(h[2][2]), "v"(h[3][2]), "v"(h[0][3]), \
+        "v"(h[1][3]), "v"(h[2][3]), "v"(h[3][3])
+    if constexpr (kFirst)
+        asm("s_nop 1\n\t" SSAM_DOT("v_mul_f32_dpp", 0, 8, 9, 10, 11) SSAM_DOT("v_fmac_f32_dpp", 1, 12, 13, 14, 15)
+                SSAM_DOT("v_fmac_f32_dpp", 2, 16, 17, 18, 19) SSAM_DOT("v_fmac_f32_dpp", 3, 20, 21, 22, 23)
+            : "=&v"(y[0]), "=&v"(y[1]), "=&v"(y[2]), "=&v"(y[3])
+            : SSAM_INPUTS);
+    else
+        asm("s_nop 1\n\t" SSAM_DOT("v_fmac_f32_dpp", 0, 8, 9, 10, 11) SSAM_DOT("v_fmac_f32_dpp", 1, 12, 13, 14, 15)
+                SSAM_DOT("v_fmac_f32_dpp", 2, 16, 17, 18, 19) SSAM_DOT("v_fmac_f32_dpp", 3, 20, 21, 22, 23)
+            : "+&v"(y[0]), "+&v"(y[1]), "+&v"(y[2]), "+&v"(y[3])
+            : SSAM_INPUTS);
+#undef SSAM_DOT
+#undef SSAM_INPUTS
+}
+// group_sum of four values that quad_dots made.
+template <int GL>
+__device__ __forceinline__ void group_sums(float (&y)[4])
+{
+#define SSAM_TURN(N)                                                          \
+    "v_add_f32_dpp %0, %0, %0 row_ror:" #N " row_mask:0xf bank_mask:0xf\n\t"  \
+    "v_add_f32_dpp %1, %1, %1 row_ror:" #N " row_mask:0xf bank_mask:0xf\n\t"  \
+    "v_add_f32_dpp %2, %2, %2 row_ror:" #N " row_mask:0xf bank_mask:0xf\n\t"  \
+    "v_add_f32_dpp %3, %3, %3 row_ror:" #N " row_mask:0xf bank_mask:0xf\n\t"
+    if constexpr (GL == 4) asm("s_nop 1\n\t" SSAM_TURN(8) SSAM_TURN(4) : "+v"(y[0]), "+v"(y[1]), "+v"(y[2]), "+v"(y[3]));
+    if constexpr (GL == 2) asm("s_nop 1\n\t" SSAM_TURN(8) : "+v"(y[0]), "+v"(y[1]), "+v"(y[2]), "+v"(y[3]));
+#undef SSAM_TURN
+}
+
+// Where the values of a row's b and c lie in LDS: the NS / 4 that a lane loads side by side.  Lane (group, quad lane j) needs states
+// group * NS + 4 m + j.
+template <class Shape> __device__ __forceinline__ int pair_place(int n) { return (n / Shape::NS * 4 + n % 4) * (Shape::NS / 4) + n % Shape::NS / 4; }
+template <class Shape> __device__ __forceinline__ int own_pairs(int lane) { return (lane_group<Shape::GL>(lane) * 4 + (lane & 3)) * (Shape::NS / 4); }
+
+// Where the channels of a tile lie in LDS: a thread loads E neighbours and spreads them over the row in steps of CB / E (channel c at
+// c % E * (CB / E) + c / E), so that the lanes of a wave, each with its e-th value, write one run.  A lane works on the channel at its place.
+template <int CB, int E> __device__ __forceinline__ int placed_channel(int at) { return at % (CB / E) * E + at / (CB / E); }
 
 // A channel's NS states of this lane in an array [..][channels][states]; those behind `states` are zero / not stored.
 template <int NS>
@@ -98,6 +147,40 @@ __device__ __forceinline__ ChannelTile channel_tile(int tile, int per_group, int
     t.n = group_channels - at < wide ? group_channels - at : wide;
     return t;
 }
+
+// What a thread loads of a tile of K rows x CB channels: E neighbours of one row.  There are no branches on it: a vector that would
+// pass the tile's last channel starts further left instead (its channels are then another thread's too; both write the same values
+// to the same places), a row behind the piece is read as the piece's last.  Only tiles of fewer than E channels go by elements.
+template <class T, int K, int CB, int E>
+struct TileLane {
+    int row, col, wide;          // row of the tile; first channel; channels of the tile
+    bool narrow;
+
+    __device__ __forceinline__ TileLane(int tid, int n)
+        : row(tid * E / CB), col(tid * E % CB), wide(n), narrow(n < E)
+    {
+        if (col + E > n) col = narrow ? 0 : n - E;
+    }
+    // `base`: the tile's row 0, channel 0 (the same for all threads); `left`: rows from there to the piece's end, at least 1
+    __device__ __forceinline__ unsigned offset(long long stride, int left) const
+    {
+        return (unsigned)(row < left ? row : left - 1) * (unsigned)stride + (unsigned)col;
+    }
+    __device__ __forceinline__ RowVec<T, E> load(const T* __restrict__ base, long long stride, int left) const
+    {
+        return load_row_vec<T, E>(base + offset(stride, left), narrow ? wide : E, narrow);
+    }
+    __device__ __forceinline__ void store(T* __restrict__ base, long long stride, int left, const RowVec<T, E>& v) const
+    {
+        if (row < left) store_row_vec<T, E>(base + offset(stride, left), narrow ? wide : E, v, narrow);
+    }
+    // LDS place of its e-th channel
+    __device__ __forceinline__ int place(int e) const
+    {
+        const int c = col + e;
+        return (c % E) * (CB / E) + c / E;
+    }
+};
 
 // f gets the lane layout for a number of states as a compile-time constant.
 template <class F>

@@ -26,16 +26,21 @@ struct ScanParams {
     int channels, states, group_channels, per_group, tiles, softplus;
 };
 
+// Rows whose operands are read from LDS together, one group ahead of the arithmetic.
+constexpr int kAhead = 4;
+
 // kWhole: all rows, outputs and the last state.  !kWhole: only the state that a piece adds (from zero) and its time steps' sum.
 template <class T, class Shape, bool kWhole>
-__global__ __launch_bounds__(kBlock) void scan_rows(ScanParams p)
+__global__ __launch_bounds__(kBlock, Shape::NS <= 4 ? 3 : 2) void scan_rows(ScanParams p)
 {
-    constexpr int GL = Shape::GL, NS = Shape::NS, NP = Shape::kStates, CB = Shape::kChannels;
-    constexpr int K = kBlock * kElems / CB;              // rows of a tile
+    constexpr int GL = Shape::GL, NS = Shape::NS, NP = Shape::kStates, CB = Shape::kChannels, E = kElems;
+    constexpr int K = kBlock * E / CB;                   // rows of a tile
     constexpr int kPairs = (K * NP + kBlock - 1) / kBlock;
-    __shared__ RowVec<float, 2> dx[K][CB];               // d, d u
-    __shared__ RowVec<float, 2> bc[K][NP];
-    __shared__ float ys[kWhole ? K : 1][CB];
+    constexpr int kRow = CB + CB / E;                    // a row in LDS: padded so that the rows of a wave's writes miss one another's banks
+    using Pair = RowVec<float, 2>;
+    __shared__ Pair dx[K][kRow];                         // d, d u
+    __shared__ Pair bc[K][NP];
+    __shared__ float ys[kWhole ? K : 1][kRow];
 
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const int slot = blockIdx.x / p.tiles;
@@ -46,7 +51,8 @@ __global__ __launch_bounds__(kBlock) void scan_rows(ScanParams p)
     const ChannelTile ct = channel_tile(blockIdx.x % p.tiles, p.per_group, p.group_channels, CB);
 
     // this lane's channel and states
-    const int ch = (tid >> 6) * Shape::kWaveChannels + lane_channel<GL>(lane);
+    const int place = (tid >> 6) * Shape::kWaveChannels + lane_channel<GL>(lane);
+    const int ch = placed_channel<CB, E>(place);
     const bool live = ch < ct.n;
     const int n0 = lane_group<GL>(lane) * NS;
     const long long cell = (long long)(ct.c0 + ch) * p.states;    // its row of [channels][states]
@@ -63,55 +69,109 @@ __global__ __launch_bounds__(kBlock) void scan_rows(ScanParams p)
         marks = p.marks + (s0 + q.row0 / SSAM_MARK_ROWS) * plane + cell;
     }
 
-    // this thread's eight values of a tile: row er, channels ec .. ec + 7
-    const int er = tid * kElems / CB, ec = tid * kElems % CB;
-    const int have = ct.n - ec < 0 ? 0 : ct.n - ec;
-    const T* __restrict__ in = sequence_base<T>(p.in, p.pieces, q) + (long long)(q.row0 + er) * p.in.row + ct.c0 + ec;
-    const T* __restrict__ dt = sequence_base<T>(p.dt, p.pieces, q) + (long long)(q.row0 + er) * p.dt.row + ct.c0 + ec;
-    const T* __restrict__ gate = kWhole && p.gate.d ? sequence_base<T>(p.gate, p.pieces, q) + (long long)(q.row0 + er) * p.gate.row + ct.c0 + ec : nullptr;
-    T* __restrict__ out = kWhole ? sequence_base<T>(p.out, p.pieces, q) + (long long)(q.row0 + er) * p.out.row + ct.c0 + ec : nullptr;
-    const T* __restrict__ pb = sequence_base<T>(p.b, p.pieces, q) + (long long)q.row0 * p.b.row + ct.group * p.b_group;
-    const T* __restrict__ pc = kWhole ? sequence_base<T>(p.c, p.pieces, q) + (long long)q.row0 * p.c.row + ct.group * p.c_group : nullptr;
-    float bias[kElems], skip[kElems];
+    // this thread's eight values of a tile
+    const TileLane<T, K, CB, E> mine(tid, ct.n);
+    const T* in = sequence_base<T>(p.in, p.pieces, q) + (long long)q.row0 * p.in.row + ct.c0;
+    const T* dt = sequence_base<T>(p.dt, p.pieces, q) + (long long)q.row0 * p.dt.row + ct.c0;
+    const bool gated = kWhole && p.gate.d;
+    const T* gate = gated ? sequence_base<T>(p.gate, p.pieces, q) + (long long)q.row0 * p.gate.row + ct.c0 : nullptr;
+    T* out = kWhole ? sequence_base<T>(p.out, p.pieces, q) + (long long)q.row0 * p.out.row + ct.c0 : nullptr;
+    const T* pb = sequence_base<T>(p.b, p.pieces, q) + (long long)q.row0 * p.b.row + ct.group * p.b_group;
+    const T* pc = kWhole ? sequence_base<T>(p.c, p.pieces, q) + (long long)q.row0 * p.c.row + ct.group * p.c_group : nullptr;
+    float bias[E], skip[E];
 #pragma unroll
-    for (int e = 0; e < kElems; ++e) {
-        bias[e] = p.dt_bias && e < have ? p.dt_bias[ct.c0 + ec + e] : 0.0f;
-        skip[e] = kWhole && p.skip && e < have ? p.skip[ct.c0 + ec + e] : 0.0f;
+    for (int e = 0; e < E; ++e) {
+        const bool is = mine.col + e < ct.n;
+        bias[e] = p.dt_bias && is ? p.dt_bias[ct.c0 + mine.col + e] : 0.0f;
+        skip[e] = kWhole && p.skip && is ? p.skip[ct.c0 + mine.col + e] : 0.0f;
     }
+    // Channels behind the tile keep d = 0, d u = 0 throughout.
+    if (ct.n < CB)
+        for (int i = tid; i < K * kRow; i += kBlock) dx[i / kRow][i % kRow] = Pair{0.0f, 0.0f};
 
-    using Vec = RowVec<T, kElems>;
-    Vec u, d, z, u_next, d_next, z_next;
+    using Vec = RowVec<T, E>;
+    Vec u, z, u_next, d_next, z_next;
     T b_next[kPairs], c_next[kPairs];
     auto request = [&](int row) {
-        const int there = row + er < q.n ? have : 0;
-        u_next = load_row_vec<T, kElems>(in + (long long)row * p.in.row, there);
-        d_next = load_row_vec<T, kElems>(dt + (long long)row * p.dt.row, there);
-        if (kWhole && gate) z_next = load_row_vec<T, kElems>(gate + (long long)row * p.gate.row, there);
+        const int left = q.n - row;
+        u_next = mine.load(in + (long long)row * p.in.row, p.in.row, left);
+        d_next = mine.load(dt + (long long)row * p.dt.row, p.dt.row, left);
+        if (gated) z_next = mine.load(gate + (long long)row * p.gate.row, p.gate.row, left);
+        const T* b0 = pb + (long long)row * p.b.row;
+        const T* c0 = kWhole ? pc + (long long)row * p.c.row : nullptr;
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
-            const int i = tid + e * kBlock, r = i / NP, n = i % NP;
-            const bool is = i < K * NP && row + r < q.n && n < p.states;
-            b_next[e] = is ? pb[(long long)(row + r) * p.b.row + n] : T(0);
-            c_next[e] = kWhole && is ? pc[(long long)(row + r) * p.c.row + n] : T(0);
+            const int i = tid + e * kBlock, n = i % NP < p.states ? i % NP : p.states - 1;
+            const unsigned r = i / NP < left ? i / NP : left - 1;
+            b_next[e] = b0[r * (unsigned)p.b.row + n];
+            if (kWhole) c_next[e] = c0[r * (unsigned)p.c.row + n];
         }
     };
-    // Rows behind the piece and channels behind the tile get d = 0, d u = 0: the state passes them unchanged.
+    // Rows behind the piece get d = 0, d u = 0: the state passes them unchanged.
     auto stage = [&](int row) {
         u = u_next;
-        d = d_next;
         z = z_next;
-        const int there = row + er < q.n ? have : 0;
 #pragma unroll
-        for (int e = 0; e < kElems; ++e) {
-            float v = (float)d[e] + bias[e];
+        for (int e = 0; e < E; ++e) {
+            float v = (float)d_next[e] + bias[e];
             if (p.softplus) v = softplus(v);
-            v = e < there ? v : 0.0f;
-            dx[er][ec + e] = RowVec<float, 2>{v, e < there ? v * (float)u[e] : 0.0f};
+            dx[mine.row][mine.place(e)] = Pair{v, v * (float)u[e]};
+        }
+        if (row + mine.row >= q.n || mine.narrow) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (row + mine.row >= q.n || e >= mine.wide) dx[mine.row][mine.place(e)] = Pair{0.0f, 0.0f};
         }
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
-            const int i = tid + e * kBlock;
-            if (i < K * NP) bc[i / NP][i % NP] = RowVec<float, 2>{(float)b_next[e], (float)c_next[e]};
+            const int i = tid + e * kBlock, n = i % NP;
+            const bool is = n < p.states;
+            if (kPairs * kBlock <= K * NP || i < K * NP)
+                bc[i / NP][pair_place<Shape>(n)] = Pair{is ? (float)b_next[e] : 0.0f, kWhole && is ? (float)c_next[e] : 0.0f};
+        }
+    };
+    struct Operands {
+        Pair dv[kAhead], w[kAhead][NS / 4];
+    };
+    const int pairs = own_pairs<Shape>(lane);
+    auto fetch = [&](int t, Operands& o) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            o.dv[k] = dx[t + k][place];
+#pragma unroll
+            for (int m = 0; m < NS / 4; ++m) o.w[k][m] = bc[t + k][pairs + m];
+        }
+    };
+    auto advance = [&](int t, const Operands& o) {
+        float y[kAhead];
+        if (!kWhole)
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) sum += o.dv[k][0];
+#pragma unroll
+        for (int m = 0; m < NS / 4; ++m) {
+            float e[kAhead][4], c[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                c[k] = o.w[k][m][1];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[k][i] = exp2_fast(o.dv[k][0] * a2[4 * m + i]);
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                const float x = o.dv[k][1], b = o.w[k][m][0];
+                const float v[4] = {quad_lane<0>(b) * x, quad_lane<1>(b) * x, quad_lane<2>(b) * x, quad_lane<3>(b) * x};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[k][i] = h[4 * m + i] = __builtin_fmaf(e[k][i], h[4 * m + i], v[i]);
+            }
+            if (kWhole) {
+                if (m == 0) quad_dots<true>(y, c, e);
+                else quad_dots<false>(y, c, e);
+            }
+        }
+        if (kWhole) {
+            group_sums<GL>(y);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) ys[t + k][place] = y[k];    // the groups of a channel write the same value
         }
     };
 
@@ -122,40 +182,27 @@ __global__ __launch_bounds__(kBlock) void scan_rows(ScanParams p)
         if (row + K < q.n) request(row + K);
         if (kWhole && p.marks && K < SSAM_MARK_ROWS && row % SSAM_MARK_ROWS == 0)
             store_states<NS>(marks + (row / SSAM_MARK_ROWS) * plane, n0, p.states, live, h);
-#pragma unroll 4
-        for (int t = 0; t < K; ++t) {
-            if (kWhole && p.marks && K >= SSAM_MARK_ROWS && t % SSAM_MARK_ROWS == 0 && row + t < q.n)
+        Operands now, next;
+        fetch(0, now);
+#pragma unroll 1
+        for (int t = 0; t < K; t += 2 * kAhead) {
+            if (row + t >= q.n) break;
+            if (kWhole && p.marks && K >= SSAM_MARK_ROWS && t % SSAM_MARK_ROWS == 0)
                 store_states<NS>(marks + ((row + t) / SSAM_MARK_ROWS) * plane, n0, p.states, live, h);
-            const RowVec<float, 2> dv = dx[t][ch];
-            float y = 0.0f;
-            if (!kWhole) sum += dv[0];
-#pragma unroll
-            for (int m = 0; m < NS / 4; ++m) {
-                const RowVec<float, 2> w = bc[t][own_state<Shape>(lane, m)];
-#define SSAM_STATE(Q)                                                                                  \
-    {                                                                                                  \
-        const int i = 4 * m + Q;                                                                       \
-        h[i] = __builtin_fmaf(exp2_fast(dv[0] * a2[i]), h[i], quad_lane<Q>(w[0]) * dv[1]);             \
-        if (kWhole) y = __builtin_fmaf(quad_lane<Q>(w[1]), h[i], y);                                   \
-    }
-                SSAM_STATE(0)
-                SSAM_STATE(1)
-                SSAM_STATE(2)
-                SSAM_STATE(3)
-#undef SSAM_STATE
-            }
-            if (kWhole) ys[t][ch] = group_sum<GL>(y);    // the groups of a channel write the same value
+            fetch(t + kAhead, next);
+            advance(t, now);
+            if (t + 2 * kAhead < K) fetch(t + 2 * kAhead, now);
+            advance(t + kAhead, next);
         }
         __syncthreads();
         if (kWhole) {
-            const int there = row + er < q.n ? have : 0;
-            float o[kElems];
+            float o[E];
 #pragma unroll
-            for (int e = 0; e < kElems; ++e) {
-                o[e] = __builtin_fmaf(skip[e], (float)u[e], ys[er][ec + e]);
-                if (gate) o[e] *= silu((float)z[e]);
-            }
-            store_row_vec<T, kElems>(out + (long long)row * p.out.row, there, rounded<T, kElems>(o));
+            for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(skip[e], (float)u[e], ys[mine.row][mine.place(e)]);
+            if (gated)
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] *= silu((float)z[e]);
+            mine.store(out + (long long)row * p.out.row, p.out.row, q.n - row, rounded<T, E>(o));
         }
     }
     if (kWhole) {
@@ -354,6 +401,8 @@ int ssam_scan_selective(const ssam_scan_selective_args* a, void* hip_stream)
         if (int e = check_rows(*r, a->seq, esz, false)) return e;
     if (int e = check_rows(a->gate, a->seq, esz, true)) return e;
     if (int e = check_out_rows(a->out, a->seq, a->channels, esz, false)) return e;
+    for (const ssam_rows* r : {&a->in, &a->dt, &a->gate, &a->out, &a->b, &a->c})
+        if (int e = check_tile_rows(*r, a->seq)) return e;
     if (a->b_group < 0 || a->b_group > kMaxStride || a->c_group < 0 || a->c_group > kMaxStride) return SSAM_ERR_DIM;
     for (const void* f : {(const void*)a->d_a, (const void*)a->d_skip, (const void*)a->d_dt_bias, (const void*)a->d_state, (const void*)a->d_final,
                           (const void*)a->d_marks})

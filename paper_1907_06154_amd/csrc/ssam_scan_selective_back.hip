@@ -203,7 +203,7 @@ __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
             const int i = tid + e * kBlock;
-            if (i < K * NP) bc[i / NP][i % NP] = RowVec<float, 2>{(float)now.b[e], (float)now.c[e]};
+            if (i < K * NP) bc[i / NP][pair_place<Shape>(i % NP)] = RowVec<float, 2>{(float)now.b[e], (float)now.c[e]};
         }
         __syncthreads();
         if (tile > 0) request(row - K);
@@ -215,7 +215,7 @@ __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
                 sum += dt_;
 #pragma unroll
                 for (int m = 0; m < NS / 4; ++m) {
-                    const float w = bc[t][own_state<Shape>(lane, m)][1];
+                    const float w = bc[t][own_pairs<Shape>(lane) + m][1];
 #define SSAM_STATE(Q) g[4 * m + Q] = (quad_lane<Q>(w) * dyt + g[4 * m + Q]) * exp2_fast(dt_ * a2[4 * m + Q]);
                     SSAM_STATE(0)
                     SSAM_STATE(1)
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
                         const RowVec<float, 2> dv = dx[t][ch];
 #pragma unroll
                         for (int m = 0; m < NS / 4; ++m) {
-                            const float w = bc[t][own_state<Shape>(lane, m)][0];
+                            const float w = bc[t][own_pairs<Shape>(lane) + m][0];
 #define SSAM_STATE(Q) h[4 * m + Q] = __builtin_fmaf(exp2_fast(dv[0] * a2[4 * m + Q]), h[4 * m + Q], quad_lane<Q>(w) * dv[1]);
                             SSAM_STATE(0)
                             SSAM_STATE(1)
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
                     float y = 0.0f;
 #pragma unroll
                     for (int m = 0; m < NS / 4; ++m) {
-                        const RowVec<float, 2> w = bc[t][own_state<Shape>(lane, m)];
+                        const RowVec<float, 2> w = bc[t][own_pairs<Shape>(lane) + m];
 #define SSAM_STATE(Q)                                                                \
     {                                                                                \
         const int i = 4 * m + Q;                                                     \
@@ -276,7 +276,7 @@ __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
                     float r = 0.0f, s = 0.0f;
 #pragma unroll
                     for (int m = 0; m < NS / 4; ++m) {
-                        const RowVec<float, 2> w = bc[t][own_state<Shape>(lane, m)];
+                        const RowVec<float, 2> w = bc[t][own_pairs<Shape>(lane) + m];
                         float vb[4], vc[4];
 #define SSAM_STATE(Q)                                                                \
     {                                                                                \
