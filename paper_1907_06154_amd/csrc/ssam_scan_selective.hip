@@ -86,8 +86,10 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 4 ? 3 : 2) void scan_rows(Scan
         skip[e] = kWhole && p.skip && is ? p.skip[ct.c0 + mine.col + e] : 0.0f;
     }
     // Channels behind the tile keep d = 0, d u = 0 throughout.
-    if (ct.n < CB)
+    if (ct.n < CB) {
         for (int i = tid; i < K * kRow; i += kBlock) dx[i / kRow][i % kRow] = Pair{0.0f, 0.0f};
+        __syncthreads();                                 // before the first tile's values go there
+    }
 
     using Vec = RowVec<T, E>;
     Vec u, z, u_next, d_next, z_next;
@@ -175,7 +177,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 4 ? 3 : 2) void scan_rows(Scan
         }
     };
 
-    request(0);
+    if (q.n > 0) request(0);                             // (an empty sequence has no row to hold to)
     for (int row = 0; row < q.n; row += K) {
         stage(row);
         __syncthreads();

@@ -3,10 +3,10 @@
 //     db_t = sum over channels g_t d_t u_t,  dc_t = sum over channels h_t dy_t
 //     du_t = skip dy_t + d_t s_t,  dd_t = r_t + u_t s_t    with s_t = sum_n g_t b_t, r_t = sum_n a q_t
 //     da = sum_t d_t q_t,  dskip = sum_t dy_t u_t,  ddt_t = dd_t sigmoid(dt_t + bias),  dbias = sum_t ddt_t
-// The rows run backwards, in tiles of 16; a tile starts from the forward call's mark (the state before its first row), makes
-// its 16 x and a again into registers, 64 of each, and goes back over them: every exp is computed once.  (Marks every 16 rows cost
-// 4 bytes per row, channel and 16 states, written and read once; making the states again from sparser marks costs a second exp,
-// which is worth more time than those bytes.)
+// The rows run backwards, in tiles of 16; a tile starts from the forward call's mark (the state before its first row) and makes its
+// states again, half a tile at a time: 8 rows' states and decays in registers, 64 of them, and back over those.  (Marks every 8 rows
+// would save the second half's way to its first row, 9 of 72 cycles a state, for 4 bytes more per row, channel and 16 states, written
+// and read; keeping 16 rows takes 128 registers and spills.)
 //
 // The sums over channels: a wave's 16 channels by lane swaps between its rows of 16 lanes and DPP inside quads, the block's waves
 // through LDS, the blocks of a group through the workspace and a launch that adds them in order.
@@ -62,42 +62,25 @@ __device__ __forceinline__ float quad_moved(float v)
 {
     return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
-__device__ __forceinline__ float quad_sum(float v)
-{
-    v += quad_moved<0xB1>(v);   // [1, 0, 3, 2]
-    v += quad_moved<0x4E>(v);   // [2, 3, 0, 1]
-    return v;
-}
-template <int GL>
-__device__ __forceinline__ float channels_sum(float v)   // over the channels of a row of 16 lanes
-{
-    v = quad_sum(v);
-    if (GL == 2) v += quad_moved<0x141>(v);   // the other quad of eight lanes (mirrored; a quad's lanes are equal by now)
-    return v;
-}
-
-template <class T, class Shape>
-struct BackTile {
-    static constexpr int CB = Shape::kChannels, NP = Shape::kStates;
-    static constexpr int kEach = kTile * CB / kBlock;                       // values of a thread
-    static constexpr int kPairs = (kTile * NP + kBlock - 1) / kBlock;
-    RowVec<T, kEach> u, d, z, dout;
-    T b[kPairs], c[kPairs];
-};
+// Of eight lanes whose quads hold one value in their even and one in their odd lanes: the other quad's of the same kind.
+__device__ __forceinline__ float other_quad(float v) { return quad_moved<0x141>(quad_moved<0xB1>(v)); }
 
 // kWhole: everything.  !kWhole: only what a piece lets out at its first row when nothing reaches it from behind.
 template <class T, class Shape, bool kWhole>
 __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
 {
     constexpr int GL = Shape::GL, NS = Shape::NS, NP = Shape::kStates, CB = Shape::kChannels, K = kTile;
-    using Tile = BackTile<T, Shape>;
-    constexpr int E = Tile::kEach, kPairs = Tile::kPairs;
-    constexpr int kKept = 64 / NS;                       // rows whose x and a are kept at a time
-    __shared__ RowVec<float, 2> dx[K][CB];               // d, d u
-    __shared__ float dys[K][CB];
-    __shared__ RowVec<float, 2> bc[K][NP];
-    __shared__ float ys[kWhole ? K : 1][CB];
-    __shared__ RowVec<float, 2> rs[kWhole ? K : 1][CB];  // r, s
+    constexpr int E = K * CB / kBlock;                   // values of a thread
+    constexpr int kPairs = (K * NP + kBlock - 1) / kBlock;
+    constexpr int kKept = NS == 16 ? 4 : 32 / NS;        // rows whose states and decays are kept at a time
+    constexpr bool kMarkAhead = NS < 16;                 // the next tile's mark is requested with its rows
+    constexpr int kRow = CB + CB / E;                    // a row in LDS, padded: see scan_rows
+    using Pair = RowVec<float, 2>;
+    __shared__ Pair dx[K][kRow];                         // d, d u
+    __shared__ float dys[K][kRow];
+    __shared__ Pair bc[K][NP];
+    __shared__ float ys[kWhole ? K : 1][kRow];
+    __shared__ Pair rs[kWhole ? K : 1][kRow];            // r, s
     __shared__ float sum_bc[kWhole ? kWavesPerBlock : 1][K][2][NP];
 
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
@@ -105,7 +88,8 @@ __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
     const ChannelTile ct = channel_tile(blockIdx.x % p.tiles, p.per_group, p.group_channels, CB);
     const Piece q = find_piece(p.pieces, slot);
     const long long plane = (long long)p.channels * p.states;
-    const int ch = wave * Shape::kWaveChannels + lane_channel<GL>(lane);
+    const int place = wave * Shape::kWaveChannels + lane_channel<GL>(lane);
+    const int ch = placed_channel<CB, E>(place);
     const bool live = ch < ct.n;
     const int n0 = lane_group<GL>(lane) * NS;
     const long long cell = (long long)(ct.c0 + ch) * p.states;
@@ -135,19 +119,17 @@ __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
         marks = p.marks + (s0 + q.row0 / K) * plane + cell;
     }
 
-    const int er = tid * E / CB, ec = tid * E % CB;
-    const int have = ct.n - ec < 0 ? 0 : ct.n - ec;
-    const long long at = q.row0 + er;
-    const T* __restrict__ in = sequence_base<T>(p.in, p.pieces, q) + at * p.in.row + ct.c0 + ec;
-    const T* __restrict__ dt = sequence_base<T>(p.dt, p.pieces, q) + at * p.dt.row + ct.c0 + ec;
-    const T* __restrict__ gate = p.gate.d ? sequence_base<T>(p.gate, p.pieces, q) + at * p.gate.row + ct.c0 + ec : nullptr;
-    const T* __restrict__ dout = sequence_base<T>(p.grad_out, p.pieces, q) + at * p.grad_out.row + ct.c0 + ec;
-    const T* __restrict__ pb = sequence_base<T>(p.b, p.pieces, q) + (long long)q.row0 * p.b.row + ct.group * p.b_group;
-    const T* __restrict__ pc = sequence_base<T>(p.c, p.pieces, q) + (long long)q.row0 * p.c.row + ct.group * p.c_group;
-    T* __restrict__ grad_in = kWhole && p.grad_in.d ? sequence_base<T>(p.grad_in, p.pieces, q) + at * p.grad_in.row + ct.c0 + ec : nullptr;
-    T* __restrict__ grad_dt = kWhole && p.grad_dt.d ? sequence_base<T>(p.grad_dt, p.pieces, q) + at * p.grad_dt.row + ct.c0 + ec : nullptr;
-    T* __restrict__ grad_gate =
-        kWhole && p.grad_gate.d && gate ? sequence_base<T>(p.grad_gate, p.pieces, q) + at * p.grad_gate.row + ct.c0 + ec : nullptr;
+    const TileLane<T, K, CB, E> mine(tid, ct.n);
+    const bool gated = p.gate.d;
+    const T* in = sequence_base<T>(p.in, p.pieces, q) + (long long)q.row0 * p.in.row + ct.c0;
+    const T* dt = sequence_base<T>(p.dt, p.pieces, q) + (long long)q.row0 * p.dt.row + ct.c0;
+    const T* gate = gated ? sequence_base<T>(p.gate, p.pieces, q) + (long long)q.row0 * p.gate.row + ct.c0 : nullptr;
+    const T* dout = sequence_base<T>(p.grad_out, p.pieces, q) + (long long)q.row0 * p.grad_out.row + ct.c0;
+    const T* pb = sequence_base<T>(p.b, p.pieces, q) + (long long)q.row0 * p.b.row + ct.group * p.b_group;
+    const T* pc = sequence_base<T>(p.c, p.pieces, q) + (long long)q.row0 * p.c.row + ct.group * p.c_group;
+    T* grad_in = kWhole && p.grad_in.d ? sequence_base<T>(p.grad_in, p.pieces, q) + (long long)q.row0 * p.grad_in.row + ct.c0 : nullptr;
+    T* grad_dt = kWhole && p.grad_dt.d ? sequence_base<T>(p.grad_dt, p.pieces, q) + (long long)q.row0 * p.grad_dt.row + ct.c0 : nullptr;
+    T* grad_gate = kWhole && p.grad_gate.d && gated ? sequence_base<T>(p.grad_gate, p.pieces, q) + (long long)q.row0 * p.grad_gate.row + ct.c0 : nullptr;
     const long long row_total = (p.pieces.begin ? (long long)q.first : (long long)q.seq * p.pieces.rows) + q.row0;
     float* part_bc = kWhole && p.part_bc
                          ? p.part_bc + (((long long)(blockIdx.x % p.tiles - ct.group * p.per_group) * p.rows_total + row_total) * p.groups + ct.group) *
@@ -156,54 +138,74 @@ __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
     float bias[E], skip[E], dskip[E], dbias[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-        bias[e] = p.dt_bias && e < have ? p.dt_bias[ct.c0 + ec + e] : 0.0f;
-        skip[e] = kWhole && p.skip && e < have ? p.skip[ct.c0 + ec + e] : 0.0f;
+        const bool is = mine.col + e < ct.n;
+        bias[e] = p.dt_bias && is ? p.dt_bias[ct.c0 + mine.col + e] : 0.0f;
+        skip[e] = kWhole && p.skip && is ? p.skip[ct.c0 + mine.col + e] : 0.0f;
         dskip[e] = dbias[e] = 0.0f;
     }
+    // Channels behind the tile keep zeros throughout: they add nothing to the sums over channels.
+    if (ct.n < CB) {
+        for (int i = tid; i < K * kRow; i += kBlock) {
+            dx[i / kRow][i % kRow] = Pair{0.0f, 0.0f};
+            dys[i / kRow][i % kRow] = 0.0f;
+        }
+        __syncthreads();                                 // before the first tile's values go there
+    }
 
-    Tile now, next;
-    float mark_next[NS];
+    using Vec = RowVec<T, E>;
+    Vec u, dr, z, go, u_next, d_next, z_next, g_next;
+    T b_next[kPairs], c_next[kPairs];
+    float mark[NS], mark_next[NS];
     auto request = [&](int row) {
-        const int there = row + er < q.n ? have : 0;
-        next.u = load_row_vec<T, E>(in + (long long)row * p.in.row, kWhole ? there : 0);
-        next.d = load_row_vec<T, E>(dt + (long long)row * p.dt.row, there);
-        next.dout = load_row_vec<T, E>(dout + (long long)row * p.grad_out.row, there);
-        next.z = load_row_vec<T, E>(gate ? gate + (long long)row * p.gate.row : nullptr, gate ? there : 0);
+        const int left = q.n - row;
+        if (kWhole) u_next = mine.load(in + (long long)row * p.in.row, p.in.row, left);
+        d_next = mine.load(dt + (long long)row * p.dt.row, p.dt.row, left);
+        g_next = mine.load(dout + (long long)row * p.grad_out.row, p.grad_out.row, left);
+        if (gated) z_next = mine.load(gate + (long long)row * p.gate.row, p.gate.row, left);
+        const T* b0 = kWhole ? pb + (long long)row * p.b.row : nullptr;
+        const T* c0 = pc + (long long)row * p.c.row;
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
-            const int i = tid + e * kBlock, r = i / NP, n = i % NP;
-            const bool is = i < K * NP && row + r < q.n && n < p.states;
-            next.b[e] = kWhole && is ? pb[(long long)(row + r) * p.b.row + n] : T(0);
-            next.c[e] = is ? pc[(long long)(row + r) * p.c.row + n] : T(0);
+            const int i = tid + e * kBlock, n = i % NP < p.states ? i % NP : p.states - 1;
+            const unsigned r = i / NP < left ? i / NP : left - 1;
+            if (kWhole) b_next[e] = b0[r * (unsigned)p.b.row + n];
+            c_next[e] = c0[r * (unsigned)p.c.row + n];
         }
-        if (kWhole) load_states<NS>(marks + (row / K) * plane, n0, p.states, live, mark_next);
+        if (kWhole && kMarkAhead) load_states<NS>(marks + (row / K) * plane, n0, p.states, live, mark_next);
     };
+    const int pairs = own_pairs<Shape>(lane);
 
     const int tiles = (q.n + K - 1) / K;
     if (tiles > 0) request((tiles - 1) * K);
     for (int tile = tiles - 1; tile >= 0; --tile) {
         const int row = tile * K;
-        const int there = row + er < q.n ? have : 0;
-        now = next;
-        float mark[NS];
+        const bool behind = row + mine.row >= q.n;       // a row behind the piece: d = 0, dy = 0, it passes states and gradients unchanged
+        u = u_next;
+        dr = d_next;
+        z = z_next;
+        go = g_next;
+        if (kWhole && kMarkAhead)
 #pragma unroll
-        for (int i = 0; i < NS; ++i) mark[i] = mark_next[i];
-        float dy[E], d[E];
+            for (int i = 0; i < NS; ++i) mark[i] = mark_next[i];
+        float dy[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            d[e] = (float)now.d[e] + bias[e];
-            float v = p.softplus ? softplus(d[e]) : d[e];
-            v = e < there ? v : 0.0f;
-            dy[e] = (float)now.dout[e];
-            if (gate) dy[e] *= silu((float)now.z[e]);
-            dy[e] = e < there ? dy[e] : 0.0f;
-            dx[er][ec + e] = RowVec<float, 2>{v, e < there ? v * (float)now.u[e] : 0.0f};
-            dys[er][ec + e] = dy[e];
+            const float raw = (float)dr[e] + bias[e];
+            float v = p.softplus ? softplus(raw) : raw;
+            dy[e] = (float)go[e];
+            if (gated) dy[e] *= silu((float)z[e]);
+            const bool is = !behind && (!mine.narrow || e < mine.wide);
+            v = is ? v : 0.0f;
+            dy[e] = is ? dy[e] : 0.0f;
+            dx[mine.row][mine.place(e)] = Pair{v, is && kWhole ? v * (float)u[e] : 0.0f};
+            dys[mine.row][mine.place(e)] = dy[e];
         }
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
-            const int i = tid + e * kBlock;
-            if (i < K * NP) bc[i / NP][pair_place<Shape>(i % NP)] = RowVec<float, 2>{(float)now.b[e], (float)now.c[e]};
+            const int i = tid + e * kBlock, n = i % NP;
+            const bool is = n < p.states;
+            if (kPairs * kBlock <= K * NP || i < K * NP)
+                bc[i / NP][pair_place<Shape>(n)] = Pair{kWhole && is ? (float)b_next[e] : 0.0f, is ? (float)c_next[e] : 0.0f};
         }
         __syncthreads();
         if (tile > 0) request(row - K);
@@ -211,136 +213,125 @@ __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
         if constexpr (!kWhole) {
 #pragma unroll 4
             for (int t = K - 1; t >= 0; --t) {
-                const float dt_ = dx[t][ch][0], dyt = dys[t][ch];
+                const float dt_ = dx[t][place][0], dyt = dys[t][place];
                 sum += dt_;
 #pragma unroll
                 for (int m = 0; m < NS / 4; ++m) {
-                    const float w = bc[t][own_pairs<Shape>(lane) + m][1];
-#define SSAM_STATE(Q) g[4 * m + Q] = (quad_lane<Q>(w) * dyt + g[4 * m + Q]) * exp2_fast(dt_ * a2[4 * m + Q]);
-                    SSAM_STATE(0)
-                    SSAM_STATE(1)
-                    SSAM_STATE(2)
-                    SSAM_STATE(3)
-#undef SSAM_STATE
+                    const float w = bc[t][pairs + m][1];
+                    const float v[4] = {quad_lane<0>(w) * dyt, quad_lane<1>(w) * dyt, quad_lane<2>(w) * dyt, quad_lane<3>(w) * dyt};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) g[4 * m + i] = (v[i] + g[4 * m + i]) * exp2_fast(dt_ * a2[4 * m + i]);
                 }
             }
         } else {
 #pragma unroll 1
             for (int part = K / kKept - 1; part >= 0; --part) {
-                float h[NS], xs[kKept][NS], as[kKept][NS];
+                // the states again, from the mark: those before this part's rows in passing, then each row's
+                float h[NS], hs[kKept][NS], as[kKept][NS];
+                if (!kMarkAhead) load_states<NS>(marks + tile * plane, n0, p.states, live, mark);
 #pragma unroll
                 for (int i = 0; i < NS; ++i) h[i] = mark[i];
-                if (kKept < K)
-                    for (int t = 0; t < part * kKept; ++t) {
-                        const RowVec<float, 2> dv = dx[t][ch];
+#pragma unroll 4
+                for (int t = 0; t < part * kKept; ++t) {
+                    const Pair dv = dx[t][place];
 #pragma unroll
-                        for (int m = 0; m < NS / 4; ++m) {
-                            const float w = bc[t][own_pairs<Shape>(lane) + m][0];
-#define SSAM_STATE(Q) h[4 * m + Q] = __builtin_fmaf(exp2_fast(dv[0] * a2[4 * m + Q]), h[4 * m + Q], quad_lane<Q>(w) * dv[1]);
-                            SSAM_STATE(0)
-                            SSAM_STATE(1)
-                            SSAM_STATE(2)
-                            SSAM_STATE(3)
-#undef SSAM_STATE
-                        }
+                    for (int m = 0; m < NS / 4; ++m) {
+                        const float w = bc[t][pairs + m][0];
+                        const float v[4] = {quad_lane<0>(w) * dv[1], quad_lane<1>(w) * dv[1], quad_lane<2>(w) * dv[1], quad_lane<3>(w) * dv[1]};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) h[4 * m + i] = __builtin_fmaf(exp2_fast(dv[0] * a2[4 * m + i]), h[4 * m + i], v[i]);
                     }
+                }
 #pragma unroll
                 for (int k = 0; k < kKept; ++k) {
                     const int t = part * kKept + k;
-                    const RowVec<float, 2> dv = dx[t][ch];
-                    float y = 0.0f;
+                    const Pair dv = dx[t][place];
+                    const float* before = k ? hs[k - 1] : h;
 #pragma unroll
                     for (int m = 0; m < NS / 4; ++m) {
-                        const RowVec<float, 2> w = bc[t][own_pairs<Shape>(lane) + m];
-#define SSAM_STATE(Q)                                                                \
-    {                                                                                \
-        const int i = 4 * m + Q;                                                     \
-        as[k][i] = exp2_fast(dv[0] * a2[i]);                                         \
-        xs[k][i] = as[k][i] * h[i];                                                  \
-        h[i] = xs[k][i] + quad_lane<Q>(w[0]) * dv[1];                                \
-        y += quad_lane<Q>(w[1]) * h[i];                                              \
-    }
-                        SSAM_STATE(0)
-                        SSAM_STATE(1)
-                        SSAM_STATE(2)
-                        SSAM_STATE(3)
-#undef SSAM_STATE
+                        const float w = bc[t][pairs + m][0];
+                        const float v[4] = {quad_lane<0>(w) * dv[1], quad_lane<1>(w) * dv[1], quad_lane<2>(w) * dv[1], quad_lane<3>(w) * dv[1]};
+#pragma unroll
+                        for (int i = 4 * m; i < 4 * m + 4; ++i) {
+                            as[k][i] = exp2_fast(dv[0] * a2[i]);
+                            hs[k][i] = __builtin_fmaf(as[k][i], before[i], v[i - 4 * m]);
+                        }
                     }
-                    ys[t][ch] = group_sum<GL>(y);
                 }
 #pragma unroll
                 for (int k = kKept - 1; k >= 0; --k) {
                     const int t = part * kKept + k;
-                    const RowVec<float, 2> dv = dx[t][ch];
-                    const float dyt = dys[t][ch];
-                    float r = 0.0f, s = 0.0f;
+                    const Pair dv = dx[t][place];
+                    const float dyt = dys[t][place];
+                    const float* before = k ? hs[k - 1] : h;
+                    float r = 0.0f, s = 0.0f, y = 0.0f;
 #pragma unroll
                     for (int m = 0; m < NS / 4; ++m) {
-                        const RowVec<float, 2> w = bc[t][own_pairs<Shape>(lane) + m];
+                        const Pair w = bc[t][pairs + m];
+                        const float b[4] = {quad_lane<0>(w[0]), quad_lane<1>(w[0]), quad_lane<2>(w[0]), quad_lane<3>(w[0])};
+                        const float c[4] = {quad_lane<0>(w[1]), quad_lane<1>(w[1]), quad_lane<2>(w[1]), quad_lane<3>(w[1])};
                         float vb[4], vc[4];
-#define SSAM_STATE(Q)                                                                \
-    {                                                                                \
-        const int i = 4 * m + Q;                                                     \
-        const float b = quad_lane<Q>(w[0]);                                          \
-        vc[Q] = (xs[k][i] + b * dv[1]) * dyt;                                        \
-        g[i] += quad_lane<Q>(w[1]) * dyt;                                            \
-        vb[Q] = g[i] * dv[1];                                                        \
-        s += b * g[i];                                                               \
-        const float qi = g[i] * xs[k][i];                                            \
-        da[i] += dv[0] * qi;                                                         \
-        r += a2[i] * qi;                                                             \
-        g[i] *= as[k][i];                                                            \
-    }
-                        SSAM_STATE(0)
-                        SSAM_STATE(1)
-                        SSAM_STATE(2)
-                        SSAM_STATE(3)
-#undef SSAM_STATE
-                        const float tb = channels_sum<GL>(rows_sum(vb[0], vb[1], vb[2], vb[3]));
-                        const float tc = channels_sum<GL>(rows_sum(vc[0], vc[1], vc[2], vc[3]));
-                        sum_bc[wave][t][lane & 1][n0 + 4 * m + row_state(lane)] = lane & 1 ? tc : tb;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const int i = 4 * m + j;
+                            y = __builtin_fmaf(c[j], hs[k][i], y);
+                            vc[j] = hs[k][i] * dyt;
+                            g[i] = __builtin_fmaf(c[j], dyt, g[i]);
+                            vb[j] = g[i] * dv[1];
+                            s = __builtin_fmaf(b[j], g[i], s);
+                            g[i] *= as[k][i];                      // what reaches the row before
+                            const float qi = g[i] * before[i];
+                            da[i] = __builtin_fmaf(dv[0], qi, da[i]);
+                            r = __builtin_fmaf(a2[i], qi, r);
+                        }
+                        // b's sums end in the even lanes of a quad, c's in the odd ones
+                        const float tb = rows_sum(vb[0], vb[1], vb[2], vb[3]), tc = rows_sum(vc[0], vc[1], vc[2], vc[3]);
+                        float v = lane & 1 ? tc : tb;
+                        v += quad_moved<0xB1>(lane & 1 ? tb : tc);
+                        v += quad_moved<0x4E>(v);
+                        if (GL == 2) v += other_quad(v);
+                        sum_bc[wave][t][lane & 1][n0 + 4 * m + row_state(lane)] = v;
                     }
-                    r = group_sum<GL>(r);
-                    s = group_sum<GL>(s);
-                    rs[t][ch] = RowVec<float, 2>{r, s};
+                    ys[t][place] = group_sum<GL>(y);
+                    rs[t][place] = Pair{group_sum<GL>(r), group_sum<GL>(s)};
                 }
             }
         }
         __syncthreads();
         if constexpr (kWhole) {
             float du[E], ddt[E], dz[E];
+            const int left = q.n - row;
 #pragma unroll
             for (int e = 0; e < E; ++e) {
-                const RowVec<float, 2> v = rs[er][ec + e];
-                const float u = (float)now.u[e];
-                const float step = dx[er][ec + e][0];
-                du[e] = __builtin_fmaf(skip[e], dy[e], step * v[1]);
-                float dd = __builtin_fmaf(u, v[1], v[0] * 0.693147180559945f);   // r was made with rates for exp2
-                if (p.softplus) dd *= sigmoid(d[e]);
+                const int at = mine.place(e);
+                const Pair v = rs[mine.row][at];
+                const float ue = (float)u[e];
+                du[e] = __builtin_fmaf(skip[e], dy[e], dx[mine.row][at][0] * v[1]);
+                float dd = __builtin_fmaf(ue, v[1], v[0] * 0.693147180559945f);   // r was made with rates for exp2
+                if (p.softplus) dd *= sigmoid((float)dr[e] + bias[e]);
                 ddt[e] = dd;
-                const bool is = e < there;
-                dskip[e] += is ? dy[e] * u : 0.0f;
-                dbias[e] += is ? dd : 0.0f;
-                if (gate) {
-                    const float z = (float)now.z[e], sig = sigmoid(z);
-                    dz[e] = (float)now.dout[e] * __builtin_fmaf(skip[e], u, ys[er][ec + e]) * (sig * __builtin_fmaf(z, 1.0f - sig, 1.0f));
+                dskip[e] += behind ? 0.0f : dy[e] * ue;
+                dbias[e] += behind ? 0.0f : dd;
+                if (gated) {
+                    const float ze = (float)z[e], sig = sigmoid(ze);
+                    dz[e] = (float)go[e] * __builtin_fmaf(skip[e], ue, ys[mine.row][at]) * (sig * __builtin_fmaf(ze, 1.0f - sig, 1.0f));
                 } else {
                     dz[e] = 0.0f;
                 }
             }
-            if (grad_in) store_row_vec<T, E>(grad_in + (long long)row * p.grad_in.row, there, rounded<T, E>(du));
-            if (grad_dt) store_row_vec<T, E>(grad_dt + (long long)row * p.grad_dt.row, there, rounded<T, E>(ddt));
-            if (grad_gate) store_row_vec<T, E>(grad_gate + (long long)row * p.grad_gate.row, there, rounded<T, E>(dz));
+            if (grad_in) mine.store(grad_in + (long long)row * p.grad_in.row, p.grad_in.row, left, rounded<T, E>(du));
+            if (grad_dt) mine.store(grad_dt + (long long)row * p.grad_dt.row, p.grad_dt.row, left, rounded<T, E>(ddt));
+            if (grad_gate) mine.store(grad_gate + (long long)row * p.grad_gate.row, p.grad_gate.row, left, rounded<T, E>(dz));
             if (part_bc) {
+                float* to = part_bc + (long long)row * p.groups * 2 * p.states;
+                const unsigned wide = p.groups * 2 * p.states;
 #pragma unroll
                 for (int i = tid; i < K * 2 * NP; i += kBlock) {
                     const int r = i / (2 * NP), w = i / NP % 2, n = i % NP;
-                    if (row + r < q.n && n < p.states) {
-                        float v = sum_bc[0][r][w][n];
+                    float v = sum_bc[0][r][w][n];
 #pragma unroll
-                        for (int k = 1; k < kWavesPerBlock; ++k) v += sum_bc[k][r][w][n];
-                        part_bc[(long long)(row + r) * p.groups * 2 * p.states + w * p.states + n] = v;
-                    }
+                    for (int k = 1; k < kWavesPerBlock; ++k) v += sum_bc[k][r][w][n];
+                    if (r < left && n < p.states) to[r * wide + w * p.states + n] = v;
                 }
             }
             __syncthreads();      // the next tile's values go where these were read
@@ -352,14 +343,16 @@ __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
         store_states<NS>(part_param + cell, n0, p.states, live, da);
         // the tile's rows of every channel, added in order
 #pragma unroll
-        for (int e = 0; e < E; ++e) rs[er][ec + e] = RowVec<float, 2>{dskip[e], dbias[e]};
+        for (int e = 0; e < E; ++e)
+            if (!mine.narrow || e < mine.wide) rs[mine.row][mine.place(e)] = Pair{dskip[e], dbias[e]};
         __syncthreads();
         if (tid < ct.n) {
+            const int at = tid % E * (CB / E) + tid / E;
             float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
             for (int r = 0; r < K; ++r) {
-                s0 += rs[r][tid][0];
-                s1 += rs[r][tid][1];
+                s0 += rs[r][at][0];
+                s1 += rs[r][at][1];
             }
             part_param[plane + ct.c0 + tid] = s0;
             part_param[plane + p.channels + ct.c0 + tid] = s1;
@@ -370,24 +363,26 @@ __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
     }
 }
 
-// Gradients of b and c: the tiles of a group added up, rows of one piece to a block row.
+// Gradients of b and c: the tiles of a group added up, in order.  A block takes kSumRows rows, a thread values 256 apart, and keeps
+// eight tiles' requests in flight.
+constexpr int kSumRows = 32;
 template <class T>
-__global__ __launch_bounds__(kBlock) void back_sum_bc(BackParams p, int blocks_each)
+__global__ __launch_bounds__(kBlock) void back_sum_bc(BackParams p, Pieces rows)
 {
-    const int slot = blockIdx.x / blocks_each;
-    const Piece q = find_piece(p.pieces, slot);
+    const Piece q = find_piece(rows, blockIdx.x);
     if (q.seq < 0) return;
-    const long long row_total = (p.pieces.begin ? (long long)q.first : (long long)q.seq * p.pieces.rows) + q.row0;
+    const long long row_total = (rows.begin ? (long long)q.first : (long long)q.seq * rows.rows) + q.row0;
     const int wide = p.groups * 2 * p.states;
-    const long long end = (long long)q.n * wide, apart = p.rows_total * wide;
-    const float* from = p.part_bc + row_total * wide;
-    for (long long i = (long long)(blockIdx.x % blocks_each) * kBlock + threadIdx.x; i < end; i += (long long)blocks_each * kBlock) {
+    const long long apart = p.rows_total * wide;
+    const float* __restrict__ from = p.part_bc + row_total * wide;
+    for (int i = threadIdx.x; i < q.n * wide; i += kBlock) {
         float v = 0.0f;
+#pragma unroll 8
         for (int k = 0; k < p.per_group; ++k) v += from[k * apart + i];
-        const int r = (int)(i / wide), at = (int)(i % wide), grp = at / (2 * p.states), n = at % (2 * p.states);
+        const int r = i / wide, at = i % wide, grp = at / (2 * p.states), n = at % (2 * p.states);
         const ssam_rows& to = n < p.states ? p.grad_b : p.grad_c;
         if (to.d)
-            sequence_base<T>(to, p.pieces, q)[(long long)(q.row0 + r) * to.row + grp * p.states + (n < p.states ? n : n - p.states)] = (T)v;
+            sequence_base<T>(to, rows, q)[(long long)(q.row0 + r) * to.row + grp * p.states + (n < p.states ? n : n - p.states)] = (T)v;
     }
 }
 
@@ -484,6 +479,8 @@ int ssam_scan_selective_backward(const ssam_scan_selective_backward_args* a, voi
     if (int e = check_rows(a->gate, a->seq, esz, true)) return e;
     for (const ssam_rows* r : {&a->grad_in, &a->grad_dt, &a->grad_gate})
         if (int e = check_out_rows(*r, a->seq, a->channels, esz, true)) return e;
+    for (const ssam_rows* r : {&a->in, &a->dt, &a->gate, &a->b, &a->c, &a->grad_out, &a->grad_in, &a->grad_dt, &a->grad_gate})
+        if (int e = check_tile_rows(*r, a->seq)) return e;
     const long long bc_width = (long long)a->groups * a->states;
     for (const ssam_rows* r : {&a->grad_b, &a->grad_c})
         if (int e = check_out_rows(*r, a->seq, bc_width, esz, true)) return e;
@@ -548,10 +545,8 @@ int ssam_scan_selective_backward(const ssam_scan_selective_backward_args* a, voi
     const long long blocks = plan.slots * plan.tiles;
     const long long join = (plane / 4 + kBlock - 1) / kBlock * a->seq.sequences;
     const long long param_blocks = (plane / 4 + 2LL * a->channels + kWave - 1) / kWave;
-    // rows of a piece x groups x 2 x states values, at most 64 of them to a thread
-    long long each = ((long long)plan.piece * bc_width * 2 + 64 * kBlock - 1) / (64 * kBlock);
-    if (each > 64) each = 64;
-    if (blocks > kMaxGrid || (plan.cut && join > kMaxGrid) || plane / 4 >= (1LL << 31) || param_blocks > kMaxGrid / 4 || plan.slots * each > kMaxGrid)
+    const long long sum_blocks = plan.bc ? piece_slots(a->seq, kSumRows) : 0;
+    if (blocks > kMaxGrid || (plan.cut && join > kMaxGrid) || plane / 4 >= (1LL << 31) || param_blocks > kMaxGrid / 4 || sum_blocks > kMaxGrid)
         return SSAM_ERR_DIM;
     hipStream_t st = (hipStream_t)hip_stream;
     return with_row_type(a->dtype, [&](auto t) {
@@ -565,7 +560,7 @@ int ssam_scan_selective_backward(const ssam_scan_selective_backward_args* a, voi
                 }
                 hipLaunchKernelGGL((scan_back<T, S, true>), dim3((unsigned)blocks), dim3(kBlock), 0, st, p);
                 if (plan.bc)
-                    hipLaunchKernelGGL((back_sum_bc<T>), dim3((unsigned)(plan.slots * each)), dim3(kBlock), 0, st, p, (int)each);
+                    hipLaunchKernelGGL((back_sum_bc<T>), dim3((unsigned)sum_blocks), dim3(kBlock), 0, st, p, make_pieces(a->seq, kSumRows));
             }
             if (plan.params)
                 hipLaunchKernelGGL(back_sum_params, dim3((unsigned)param_blocks), dim3(kWave * kRuns), 0, st, p.part_param, plan.slots, plane / 4,
