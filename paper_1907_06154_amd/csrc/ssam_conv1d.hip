@@ -11,6 +11,7 @@ namespace {
 constexpr int kMarch = 4;          // rows requested together
 
 template <class T> constexpr int kChan = 16 / sizeof(T);   // channels of a lane
+constexpr int kBackChan = 4;                               // and in the backward march, which holds more of each
 
 struct Conv1dParams {
     Pieces pieces;
@@ -21,28 +22,71 @@ struct Conv1dParams {
     long long waves;
 };
 
-template <class T, int W>
-__device__ __forceinline__ void load_taps(const void* weight, bool f32, int c, int have, float (&w)[W][kChan<T>])
+// A lane's V channels.  A vector that would pass the last channel starts further left instead: its channels are then also those of the
+// lane before, and both make and store the same values.  The two are always lanes of one wave, whose loads of a state that is
+// updated in place come before its stores.  A strip of fewer than V channels is one lane's, by elements.
+template <int V>
+struct Channels {
+    int first, have;
+    bool narrow, there;
+    __device__ __forceinline__ Channels(int strip, int lane, int channels)
+    {
+        const int c0 = strip * (kWave * V), left = channels - c0;
+        first = c0 + lane * V;
+        there = first < channels;
+        narrow = left < V;
+        have = narrow ? left : V;
+        if (first + V > channels) first = narrow ? c0 : channels - V;      // lanes that have none repeat the last as well
+    }
+    template <class T> __device__ __forceinline__ RowVec<T, V> load(const T* __restrict__ p) const { return load_row_vec<T, V>(p, have, narrow); }
+    template <class T, bool kStream> __device__ __forceinline__ void store(T* __restrict__ p, const RowVec<T, V>& v) const
+    {
+        store_row_vec<T, V, kStream>(p, have, v, narrow);
+    }
+};
+
+// The taps of V channels are V * W consecutive values: W whole vectors.
+template <class P, int W, int V>
+__device__ __forceinline__ void load_taps_as(const void* weight, const Channels<V>& ch, float (&w)[W][V])
 {
+    RowVec<P, V> r[W];
 #pragma unroll
-    for (int v = 0; v < kChan<T>; ++v)
+    for (int k = 0; k < W; ++k) r[k] = load_row_vec<P, V>(static_cast<const P*>(weight) + (long long)ch.first * W + k * V, ch.have * W - k * V, ch.narrow);
 #pragma unroll
-        for (int j = 0; j < W; ++j) w[j][v] = v < have ? param_at<T>(weight, f32, (long long)(c + v) * W + j) : 0.0f;
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int j = 0; j < W; ++j) w[j][v] = (float)r[(v * W + j) / V][(v * W + j) % V];
+}
+template <class T, int W, int V>
+__device__ __forceinline__ void load_taps(const void* weight, bool f32, const Channels<V>& ch, float (&w)[W][V])
+{
+    if (f32) load_taps_as<float, W, V>(weight, ch, w);
+    else load_taps_as<T, W, V>(weight, ch, w);
 }
 
-template <class T>
-__device__ __forceinline__ void load_bias(const void* bias, bool f32, int c, int have, float (&b)[kChan<T>])
+template <class T, int V>
+__device__ __forceinline__ void load_bias(const void* bias, bool f32, const Channels<V>& ch, float (&b)[V])
 {
+    if (!bias) {
 #pragma unroll
-    for (int v = 0; v < kChan<T>; ++v) b[v] = bias && v < have ? param_at<T>(bias, f32, c + v) : 0.0f;
+        for (int v = 0; v < V; ++v) b[v] = 0.0f;
+    } else if (f32) {
+        const RowVec<float, V> r = ch.load(static_cast<const float*>(bias) + ch.first);
+#pragma unroll
+        for (int v = 0; v < V; ++v) b[v] = r[v];
+    } else {
+        const RowVec<T, V> r = ch.load(static_cast<const T*>(bias) + ch.first);
+#pragma unroll
+        for (int v = 0; v < V; ++v) b[v] = (float)r[v];
+    }
 }
 
 // Row t < 0 of sequence s: from its carried state, zeros without one.
-template <class T, int W>
-__device__ __forceinline__ RowVec<T, kChan<T>> carried_row(const void* state, int s, int t, int channels, int c, int have)
+template <class T, int W, int V>
+__device__ __forceinline__ RowVec<T, V> carried_row(const void* state, int s, int t, int channels, const Channels<V>& ch)
 {
-    if (!state) return load_row_vec<T, kChan<T>>(nullptr, 0);
-    return load_row_vec<T, kChan<T>>(static_cast<const T*>(state) + ((long long)s * (W - 1) + (W - 1 + t)) * channels + c, have);
+    if (!state) return RowVec<T, V>(T(0));
+    return ch.load(static_cast<const T*>(state) + ((long long)s * (W - 1) + (W - 1 + t)) * channels + ch.first);
 }
 
 template <class T, int W>
@@ -55,26 +99,29 @@ __global__ __launch_bounds__(kBlock) void conv1d_rows(Conv1dParams p)
     const int strip = (int)(wave % p.strips);
     const Piece q = find_piece(p.pieces, (int)(wave / p.strips));
     if (q.seq < 0) return;
-    const int c = (strip * kWave + lane) * V;
-    const int have = p.channels - c;
-    if (have <= 0) return;
-    const T* __restrict__ in = sequence_base<T>(p.in, p.pieces, q) + c;
-    T* __restrict__ out = sequence_base<T>(p.out, p.pieces, q) + c;
+    const Channels<V> ch(strip, lane, p.channels);
+    if (!ch.there) return;
+    const T* __restrict__ in = sequence_base<T>(p.in, p.pieces, q) + ch.first;
+    T* __restrict__ out = sequence_base<T>(p.out, p.pieces, q) + ch.first;
+    RowVec<T, V> win[W], next[kMarch];        // rows t - W + 1 .. t, and the rows after those in work
+    auto request = [&](int k) {               // rows behind the piece are read as its last, and not used
+#pragma unroll
+        for (int u = 0; u < kMarch; ++u) next[u] = ch.load(in + (long long)(q.row0 + (k + u < q.n ? k + u : q.n - 1)) * p.in.row);
+    };
+    if (q.n > 0) request(0);
     float w[W][V], b[V];
-    load_taps<T, W>(p.weight, p.params_f32, c, have, w);
-    load_bias<T>(p.bias, p.params_f32, c, have, b);
-    RowVec<T, V> win[W];        // rows t - W + 1 .. t
+    load_taps<T, W, V>(p.weight, p.params_f32, ch, w);
+    load_bias<T, V>(p.bias, p.params_f32, ch, b);
 #pragma unroll
     for (int j = 0; j < W - 1; ++j) {
         const int t = q.row0 - (W - 1) + j;
-        win[j + 1] = t >= 0 ? load_row_vec<T, V>(in + (long long)t * p.in.row, q.n > 0 ? have : 0)
-                            : carried_row<T, W>(p.state, q.seq, t, p.channels, c, have);
+        win[j + 1] = t >= 0 ? ch.load(in + (long long)t * p.in.row) : carried_row<T, W, V>(p.state, q.seq, t, p.channels, ch);
     }
     for (int k = 0; k < q.n; k += kMarch) {
         RowVec<T, V> x[kMarch];
 #pragma unroll
-        for (int u = 0; u < kMarch; ++u)
-            x[u] = load_row_vec<T, V>(in + (long long)(q.row0 + k + u) * p.in.row, k + u < q.n ? have : 0);
+        for (int u = 0; u < kMarch; ++u) x[u] = next[u];
+        if (k + kMarch < q.n) request(k + kMarch);
 #pragma unroll
         for (int u = 0; u < kMarch; ++u) {
 #pragma unroll
@@ -86,9 +133,12 @@ __global__ __launch_bounds__(kBlock) void conv1d_rows(Conv1dParams p)
                 float s = b[v];
 #pragma unroll
                 for (int j = 0; j < W; ++j) s = __builtin_fmaf(w[j][v], (float)win[j][v], s);
-                y[v] = p.silu ? silu(s) : s;
+                y[v] = s;
             }
-            if (k + u < q.n) store_row_vec<T, V>(out + (long long)(q.row0 + k + u) * p.out.row, have, rounded<T, V>(y));
+            if (p.silu)
+#pragma unroll
+                for (int v = 0; v < V; ++v) y[v] = silu(y[v]);
+            if (k + u < q.n) ch.template store<T, true>(out + (long long)(q.row0 + k + u) * p.out.row, rounded<T, V>(y));
         }
     }
     // The first piece's wave also hands on the state: it is the only one that reads the old one, so that both may be the same
@@ -97,9 +147,8 @@ __global__ __launch_bounds__(kBlock) void conv1d_rows(Conv1dParams p)
 #pragma unroll
         for (int j = 0; j < W - 1; ++j) {
             const int t = q.len - (W - 1) + j;
-            const RowVec<T, V> x = t >= 0 ? load_row_vec<T, V>(in + (long long)t * p.in.row, have)
-                                          : carried_row<T, W>(p.state, q.seq, t, p.channels, c, have);
-            store_row_vec<T, V>(static_cast<T*>(p.final) + ((long long)q.seq * (W - 1) + j) * p.channels + c, have, x);
+            const RowVec<T, V> x = t >= 0 ? ch.load(in + (long long)t * p.in.row) : carried_row<T, W, V>(p.state, q.seq, t, p.channels, ch);
+            ch.template store<T, false>(static_cast<T*>(p.final) + ((long long)q.seq * (W - 1) + j) * p.channels + ch.first, x);
         }
     }
 }
@@ -110,41 +159,52 @@ struct Conv1dBackParams {
     ssam_rows in, grad_out, grad_in;
     const void *weight, *bias, *state, *grad_final;
     void* grad_state;
-    float* parts;               // [slot][W + 1][channels]: this slot's sums for the weight's and the bias's gradient, or null
+    float* parts;               // [four slots][W + 1][channels]: their sums for the weight's and the bias's gradient, or null
     int channels, strips, silu, params_f32;
-    long long waves;
+    long long slots;
 };
 
 // q_t = dy_t silu'(p_t), dx_t = sum_j w[j] q_{t + W - 1 - j}, dw[j] = sum_t q_t x_{t - W + 1 + j}, db = sum_t q_t.  One march over
 // the rows of the piece and the W-1 behind it: p_t comes again from the window of inputs, and a second window holds the last W
 // q's.  dx runs W-1 rows behind the march, so the first piece also meets rows -(W-1) .. -1, the gradient of the carried rows.
-// The sums over rows stay in registers and go to `parts`, to be added slot after slot.
+// The sums over rows stay in registers; a block's four waves, four slots of one strip, add theirs in LDS, and what a block has goes
+// to `parts`, to be added block after block.
 template <class T, int W>
 __global__ __launch_bounds__(kBlock) void conv1d_back(Conv1dBackParams p)
 {
-    constexpr int V = kChan<T>;
-    const int lane = threadIdx.x & (kWave - 1);
-    const long long wave = (long long)blockIdx.x * kWavesPerBlock + (threadIdx.x >> 6);
-    if (wave >= p.waves) return;
-    const int strip = (int)(wave % p.strips);
-    const int slot = (int)(wave / p.strips);
-    const Piece q = find_piece(p.pieces, slot);
-    const int c = (strip * kWave + lane) * V;
-    const int have = p.channels - c;
-    if (have <= 0) return;
+    constexpr int V = kBackChan;
+    __shared__ RowVec<float, V> block_sums[kWavesPerBlock - 1][W + 1][kWave];
+    const int lane = threadIdx.x & (kWave - 1), in_block = threadIdx.x >> 6;
+    const int strip = blockIdx.x % p.strips;
+    const long long slot = (long long)(blockIdx.x / p.strips) * kWavesPerBlock + in_block;
+    Piece q = find_piece(p.pieces, (int)(slot < p.slots ? slot : 0));
+    const Channels<V> ch(strip, lane, p.channels);
+    if (slot >= p.slots || !ch.there) q.seq = -1;       // stays for the sums
     float dw[W + 1][V];         // the last: the bias's
 #pragma unroll
     for (int j = 0; j <= W; ++j)
 #pragma unroll
         for (int v = 0; v < V; ++v) dw[j][v] = 0.0f;
     if (q.seq >= 0) {
-        const T* __restrict__ in = sequence_base<T>(p.in, p.pieces, q) + c;
-        const T* __restrict__ dy = sequence_base<T>(p.grad_out, p.pieces, q) + c;
-        T* __restrict__ dx = p.grad_in.d ? sequence_base<T>(p.grad_in, p.pieces, q) + c : nullptr;
+        const T* __restrict__ in = sequence_base<T>(p.in, p.pieces, q) + ch.first;
+        const T* __restrict__ dy = sequence_base<T>(p.grad_out, p.pieces, q) + ch.first;
+        T* __restrict__ dx = p.grad_in.d ? sequence_base<T>(p.grad_in, p.pieces, q) + ch.first : nullptr;
+        const int rows = q.n + W - 1;       // the march: rows row0 .. row0 + rows - 1, q = 0 from len on
+        RowVec<T, V> win[W], x_next[kMarch], g_next[kMarch];
+        auto request = [&](int k) {         // rows behind the sequence are read as its last, and their q is 0
+#pragma unroll
+            for (int u = 0; u < kMarch; ++u) {
+                const int t = q.row0 + k + u < q.len ? q.row0 + k + u : q.len - 1;
+                x_next[u] = ch.load(in + (long long)t * p.in.row);
+                g_next[u] = ch.load(dy + (long long)t * p.grad_out.row);
+            }
+        };
+#pragma unroll
+        for (int u = 0; u < kMarch; ++u) x_next[u] = g_next[u] = RowVec<T, V>(T(0));
+        if (q.len > 0) request(0);
         float w[W][V], b[V], qs[W][V];
-        load_taps<T, W>(p.weight, p.params_f32, c, have, w);
-        load_bias<T>(p.bias, p.params_f32, c, have, b);
-        RowVec<T, V> win[W];
+        load_taps<T, W, V>(p.weight, p.params_f32, ch, w);
+        load_bias<T, V>(p.bias, p.params_f32, ch, b);
 #pragma unroll
         for (int j = 0; j < W; ++j)
 #pragma unroll
@@ -152,84 +212,90 @@ __global__ __launch_bounds__(kBlock) void conv1d_back(Conv1dBackParams p)
 #pragma unroll
         for (int j = 0; j < W - 1; ++j) {
             const int t = q.row0 - (W - 1) + j;
-            win[j + 1] = t >= 0 ? load_row_vec<T, V>(in + (long long)t * p.in.row, have)
-                                : carried_row<T, W>(p.state, q.seq, t, p.channels, c, have);
+            win[j + 1] = t >= 0 ? ch.load(in + (long long)t * p.in.row) : carried_row<T, W, V>(p.state, q.seq, t, p.channels, ch);
         }
-        const int rows = q.n + W - 1;       // the march: rows row0 .. row0 + rows - 1, zeros from len on
         for (int k = 0; k < rows; k += kMarch) {
             RowVec<T, V> x[kMarch], g[kMarch];
 #pragma unroll
             for (int u = 0; u < kMarch; ++u) {
-                const int t = q.row0 + k + u;
-                const int there = k + u < rows && t < q.len ? have : 0;
-                x[u] = load_row_vec<T, V>(in + (long long)t * p.in.row, there);
-                g[u] = load_row_vec<T, V>(dy + (long long)t * p.grad_out.row, there);
+                x[u] = x_next[u];
+                g[u] = g_next[u];
             }
+            if (q.len > 0 && k + kMarch < rows) request(k + kMarch);
 #pragma unroll
             for (int u = 0; u < kMarch; ++u) {
                 const int t = q.row0 + k + u;
-                if (k + u >= rows) continue;
 #pragma unroll
                 for (int j = 0; j < W - 1; ++j) win[j] = win[j + 1];
                 win[W - 1] = x[u];
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
+                for (int j = W - 1; j > 0; --j)
 #pragma unroll
-                    for (int j = W - 1; j > 0; --j) qs[j][v] = qs[j - 1][v];
-                    float d = (float)g[u][v];
-                    if (p.silu) {
+                    for (int v = 0; v < V; ++v) qs[j][v] = qs[j - 1][v];
+#pragma unroll
+                for (int v = 0; v < V; ++v) qs[0][v] = (float)g[u][v];
+                if (p.silu) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) {
                         float s = b[v];
 #pragma unroll
                         for (int j = 0; j < W; ++j) s = __builtin_fmaf(w[j][v], (float)win[j][v], s);
                         const float sig = sigmoid(s);
-                        d *= sig * __builtin_fmaf(s, 1.0f - sig, 1.0f);
+                        qs[0][v] *= sig * __builtin_fmaf(s, 1.0f - sig, 1.0f);
                     }
-                    qs[0][v] = t < q.len ? d : 0.0f;
                 }
-                if (k + u < q.n) {          // rows of this piece; those behind it are another's
+                const bool in_piece = k + u < q.n;       // rows behind it are another's
 #pragma unroll
-                    for (int v = 0; v < V; ++v) {
+                for (int v = 0; v < V; ++v) {
+                    qs[0][v] = t < q.len ? qs[0][v] : 0.0f;
+                    const float own = in_piece ? qs[0][v] : 0.0f;
 #pragma unroll
-                        for (int j = 0; j < W; ++j) dw[j][v] = __builtin_fmaf(qs[0][v], (float)win[j][v], dw[j][v]);
-                        dw[W][v] += qs[0][v];
-                    }
+                    for (int j = 0; j < W; ++j) dw[j][v] = __builtin_fmaf(own, (float)win[j][v], dw[j][v]);
+                    dw[W][v] += own;
                 }
                 const int o = t - (W - 1);  // the row whose gradient is complete
                 const bool carried = o < 0;
-                if (o < q.row0 && !carried) continue;
-                if (carried ? !p.grad_state : !dx) continue;
+                if (k + u >= rows || (o < q.row0 && !carried) || (carried ? !p.grad_state : !dx)) continue;
                 float d[V];
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    d[v] = 0.0f;
+                    d[v] = w[0][v] * qs[0][v];
 #pragma unroll
-                    for (int j = 0; j < W; ++j) d[v] = __builtin_fmaf(w[j][v], qs[j][v], d[v]);
+                    for (int j = 1; j < W; ++j) d[v] = __builtin_fmaf(w[j][v], qs[j][v], d[v]);
                 }
                 const int tail = o - (q.len - (W - 1));
                 if (p.grad_final && tail >= 0) {
-                    const RowVec<T, V> f = load_row_vec<T, V>(
-                        static_cast<const T*>(p.grad_final) + ((long long)q.seq * (W - 1) + tail) * p.channels + c, have);
+                    const RowVec<T, V> f =
+                        ch.load(static_cast<const T*>(p.grad_final) + ((long long)q.seq * (W - 1) + tail) * p.channels + ch.first);
 #pragma unroll
                     for (int v = 0; v < V; ++v) d[v] += (float)f[v];
                 }
-                T* to = carried ? static_cast<T*>(p.grad_state) + ((long long)q.seq * (W - 1) + t) * p.channels + c
+                T* to = carried ? static_cast<T*>(p.grad_state) + ((long long)q.seq * (W - 1) + t) * p.channels + ch.first
                                 : dx + (long long)o * p.grad_in.row;
-                store_row_vec<T, V>(to, have, rounded<T, V>(d));
+                ch.template store<T, true>(to, rounded<T, V>(d));
             }
         }
     }
-    if (p.parts) {
+    if (!p.parts) return;
+    RowVec<float, V> f[W + 1];
 #pragma unroll
-        for (int j = 0; j <= W; ++j) {
-            RowVec<float, V> f;
+    for (int j = 0; j <= W; ++j)
 #pragma unroll
-            for (int v = 0; v < V; ++v) f[v] = dw[j][v];
-            store_row_vec<float, V>(p.parts + ((long long)slot * (W + 1) + j) * p.channels + c, have, f);
-        }
+        for (int v = 0; v < V; ++v) f[j][v] = dw[j][v];
+    if (in_block > 0)
+#pragma unroll
+        for (int j = 0; j <= W; ++j) block_sums[in_block - 1][j][lane] = f[j];
+    __syncthreads();
+    if (in_block > 0 || !ch.there) return;
+#pragma unroll
+    for (int j = 0; j <= W; ++j) {
+#pragma unroll
+        for (int k = 0; k < kWavesPerBlock - 1; ++k) f[j] += block_sums[k][j][lane];
+        ch.template store<float, false>(p.parts + ((long long)(blockIdx.x / p.strips) * (W + 1) + j) * p.channels + ch.first, f[j]);
     }
 }
 
-// parts summed over the slots, 16 interleaved runs of them and then the runs, always in the same order.
+// parts summed over the blocks' slots, 16 interleaved runs of them and then the runs, always in the same order.
 constexpr int kRuns = 16;
 template <class T>
 __global__ __launch_bounds__(kWave* kRuns) void conv1d_back_sums(const float* __restrict__ parts, long long slots, int W, int channels,
@@ -242,6 +308,7 @@ __global__ __launch_bounds__(kWave* kRuns) void conv1d_back_sums(const float* __
     const int c = (blockIdx.x % strips) * kWave + lane;
     float s = 0.0f;
     if (c < channels)
+#pragma unroll 4
         for (long long i = r; i < slots; i += kRuns) s += parts[(i * (W + 1) + j) * channels + c];
     run[r][lane] = s;
     __syncthreads();
@@ -262,7 +329,7 @@ struct Conv1dStepParams {
     ssam_rows in, out;
     const void *weight, *bias;
     void* state;
-    long long slot_stride, waves;
+    long long slot_stride;
 };
 
 template <class T, int W>
@@ -270,24 +337,25 @@ __global__ __launch_bounds__(kBlock) void conv1d_step(Conv1dStepParams p)
 {
     constexpr int V = kChan<T>;
     const int lane = threadIdx.x & (kWave - 1);
-    const long long wave = (long long)blockIdx.x * kWavesPerBlock + (threadIdx.x >> 6);
-    if (wave >= p.waves) return;
-    const int row = (int)(wave / p.strips);
-    const int c = ((int)(wave % p.strips) * kWave + lane) * V;
-    const int have = p.channels - c;
-    SlotRows same(p.slot_of, p.rows, p.slots, row);
-    if (!same.leads()) return;
-    T* __restrict__ state = static_cast<T*>(p.state) + (long long)same.slot() * p.slot_stride + c;
+    const int row_blocks = (p.rows + kWavesPerBlock - 1) / kWavesPerBlock;      // a block's waves: the same channels of four rows
+    const int row = (int)(blockIdx.x % row_blocks) * kWavesPerBlock + (threadIdx.x >> 6);
+    if (row >= p.rows) return;
+    const Channels<V> ch((int)(blockIdx.x / row_blocks), lane, p.channels);
+    const T* in = static_cast<const T*>(p.in.d) + ch.first;
+    RowVec<T, V> x = ch.load(in + (long long)row * p.in.row);
     float w[W][V], b[V];
-    load_taps<T, W>(p.weight, p.params_f32, c, have, w);
-    load_bias<T>(p.bias, p.params_f32, c, have, b);
+    load_taps<T, W, V>(p.weight, p.params_f32, ch, w);
+    load_bias<T, V>(p.bias, p.params_f32, ch, b);
+    SlotRows same(p.slot_of, p.rows, p.slots, row);      // every lane takes part to the end: the rows of a slot are found by ballots
+    if (!same.leads()) return;
+    T* __restrict__ state = static_cast<T*>(p.state) + (long long)same.slot() * p.slot_stride + ch.first;
     RowVec<T, V> win[W];
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) win[j + 1] = load_row_vec<T, V>(state + (long long)j * p.channels, have);
-    for (int r = row; r >= 0; r = same.next()) {
+    for (int j = 0; j < W - 1; ++j) win[j + 1] = ch.load(state + (long long)j * p.channels);
+    for (int r = row;;) {
 #pragma unroll
         for (int j = 0; j < W - 1; ++j) win[j] = win[j + 1];
-        win[W - 1] = load_row_vec<T, V>(static_cast<const T*>(p.in.d) + (long long)r * p.in.row + c, have);
+        win[W - 1] = x;
         float y[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -296,12 +364,13 @@ __global__ __launch_bounds__(kBlock) void conv1d_step(Conv1dStepParams p)
             for (int j = 0; j < W; ++j) s = __builtin_fmaf(w[j][v], (float)win[j][v], s);
             y[v] = p.silu ? silu(s) : s;
         }
-        if (have > 0) store_row_vec<T, V>(static_cast<T*>(p.out.d) + (long long)r * p.out.row + c, have, rounded<T, V>(y));
+        ch.template store<T, false>(static_cast<T*>(p.out.d) + (long long)r * p.out.row + ch.first, rounded<T, V>(y));
+        r = same.next();
+        if (r < 0) break;
+        x = ch.load(in + (long long)r * p.in.row);
     }
-    if (have > 0) {
 #pragma unroll
-        for (int j = 0; j < W - 1; ++j) store_row_vec<T, V>(state + (long long)j * p.channels, have, win[j + 1]);
-    }
+    for (int j = 0; j < W - 1; ++j) ch.template store<T, false>(state + (long long)j * p.channels, win[j + 1]);
 }
 
 // ---- host --------------------------------------------------------------------------------------------------------------
@@ -339,7 +408,8 @@ int check_filter(int dtype, int param_dtype, int channels, int taps)
 
 bool misaligned(const void* p, int bytes) { return (uintptr_t)p % bytes != 0; }
 
-int strips_of(int channels, int dtype) { const int wide = kWave * 16 / type_bytes(dtype); return (channels + wide - 1) / wide; }
+int strips_of(int channels, int each) { return (channels + kWave * each - 1) / (kWave * each); }
+int forward_strips(int channels, int dtype) { return strips_of(channels, 16 / type_bytes(dtype)); }
 
 // Rows of a piece: long pieces read fewer rows twice, short ones give more waves; 4096 waves (four per SIMD) are enough.
 int piece_rows(const ssam_sequences& q, int strips, int longest)
@@ -350,12 +420,13 @@ int piece_rows(const ssam_sequences& q, int strips, int longest)
 }
 
 // Rows of a piece of the backward march, and the slots of its partial sums.
-int back_piece_rows(const ssam_conv1d_backward_args& a) { return piece_rows(a.seq, strips_of(a.channels, a.dtype), 64); }
+int back_piece_rows(const ssam_conv1d_backward_args& a) { return piece_rows(a.seq, strips_of(a.channels, kBackChan), 64); }
+long long back_parts(const ssam_conv1d_backward_args& a) { return (piece_slots(a.seq, back_piece_rows(a)) + kWavesPerBlock - 1) / kWavesPerBlock; }
 
 size_t back_bytes(const ssam_conv1d_backward_args& a)
 {
     if (!a.d_grad_weight && !a.d_grad_bias) return 0;
-    return (size_t)piece_slots(a.seq, back_piece_rows(a)) * (a.taps + 1) * a.channels * sizeof(float);
+    return (size_t)back_parts(a) * (a.taps + 1) * a.channels * sizeof(float);
 }
 
 }  // namespace
@@ -382,7 +453,7 @@ int ssam_conv1d(const ssam_conv1d_args* a, void* hip_stream)
                          cover_plain(a->d_state == a->d_final ? nullptr : a->d_state, state_bytes)};
     if (any_overlap(outs, ins) || (a->d_state && overlaps(outs[0], cover_plain(a->d_state, state_bytes)))) return SSAM_ERR_ALIAS;
     Conv1dParams p{};
-    p.strips = strips_of(a->channels, a->dtype);
+    p.strips = forward_strips(a->channels, a->dtype);
     const int piece = piece_rows(a->seq, p.strips, 32);
     p.pieces = make_pieces(a->seq, piece);
     p.in = a->in;
@@ -439,7 +510,7 @@ int ssam_conv1d_backward(const ssam_conv1d_backward_args* a, void* hip_stream)
                          cover_plain(a->d_state, state_bytes), cover_plain(a->d_grad_final, state_bytes)};
     if (any_overlap(outs, ins)) return SSAM_ERR_ALIAS;
     Conv1dBackParams p{};
-    p.strips = strips_of(a->channels, a->dtype);
+    p.strips = strips_of(a->channels, kBackChan);
     const int piece = back_piece_rows(*a);
     p.pieces = make_pieces(a->seq, piece);
     p.in = a->in;
@@ -454,16 +525,15 @@ int ssam_conv1d_backward(const ssam_conv1d_backward_args* a, void* hip_stream)
     p.channels = a->channels;
     p.silu = a->silu != 0;
     p.params_f32 = a->param_dtype == SSAM_F32;
-    const long long slots = piece_slots(a->seq, piece);
-    p.waves = slots * p.strips;
-    const long long blocks = (p.waves + kWavesPerBlock - 1) / kWavesPerBlock;
+    p.slots = piece_slots(a->seq, piece);
+    const long long parts = back_parts(*a), blocks = parts * p.strips;
     const long long sum_blocks = (long long)((a->channels + kWave - 1) / kWave) * (a->taps + 1);
     if (blocks > kMaxGrid || sum_blocks > kMaxGrid / 4) return SSAM_ERR_DIM;
     hipStream_t st = (hipStream_t)hip_stream;
     return with_type_and_taps(a->dtype, a->taps, [&](auto t, auto w) {
         if (blocks) hipLaunchKernelGGL((conv1d_back<decltype(t), decltype(w)::value>), dim3((unsigned)blocks), dim3(kBlock), 0, st, p);
         if (sums)
-            hipLaunchKernelGGL((conv1d_back_sums<decltype(t)>), dim3((unsigned)sum_blocks), dim3(kWave * kRuns), 0, st, p.parts, slots, a->taps,
+            hipLaunchKernelGGL((conv1d_back_sums<decltype(t)>), dim3((unsigned)sum_blocks), dim3(kWave * kRuns), 0, st, p.parts, parts, a->taps,
                                a->channels, a->d_grad_weight, a->d_grad_bias, p.params_f32);
         return launched();
     });
@@ -492,7 +562,7 @@ int ssam_conv1d_step(const ssam_conv1d_step_args* a, void* hip_stream)
     p.rows = a->rows;
     p.slots = a->slots;
     p.channels = a->channels;
-    p.strips = strips_of(a->channels, a->dtype);
+    p.strips = forward_strips(a->channels, a->dtype);
     p.silu = a->silu != 0;
     p.params_f32 = a->param_dtype == SSAM_F32;
     p.slot_of = a->d_slots;
@@ -502,8 +572,7 @@ int ssam_conv1d_step(const ssam_conv1d_step_args* a, void* hip_stream)
     p.bias = a->d_bias;
     p.state = a->d_state;
     p.slot_stride = a->slot_stride;
-    p.waves = (long long)a->rows * p.strips;
-    const long long blocks = (p.waves + kWavesPerBlock - 1) / kWavesPerBlock;
+    const long long blocks = ((long long)a->rows + kWavesPerBlock - 1) / kWavesPerBlock * p.strips;
     if (blocks > kMaxGrid) return SSAM_ERR_DIM;
     return with_type_and_taps(a->dtype, a->taps, [&](auto t, auto w) {
         hipLaunchKernelGGL((conv1d_step<decltype(t), decltype(w)::value>), dim3((unsigned)blocks), dim3(kBlock), 0, (hipStream_t)hip_stream, p);

@@ -24,6 +24,7 @@ template <class T, int V> using RowVec = T __attribute__((ext_vector_type(V)));
 template <class T, int V>
 __device__ __forceinline__ RowVec<T, V> load_row_vec(const T* __restrict__ p, int have, bool part = true)
 {
+    static_assert(sizeof(RowVec<T, V>) == V * sizeof(T), "a vector type of another number of elements is longer than they are");
     RowVec<T, V> v;
     if (!part || have >= V) {
         __builtin_memcpy(&v, p, sizeof(v));
@@ -34,11 +35,17 @@ __device__ __forceinline__ RowVec<T, V> load_row_vec(const T* __restrict__ p, in
     return v;
 }
 
-template <class T, int V>
+// (kStream: a result larger than the caches, not read again soon.)
+template <class T, int V, bool kStream = false>
 __device__ __forceinline__ void store_row_vec(T* __restrict__ p, int have, const RowVec<T, V>& v, bool part = true)
 {
     if (!part || have >= V) {
-        __builtin_memcpy(p, &v, sizeof(v));
+        if constexpr (kStream) {
+            typedef RowVec<T, V> Loose __attribute__((aligned(sizeof(T))));
+            __builtin_nontemporal_store(v, reinterpret_cast<Loose*>(p));
+        } else {
+            __builtin_memcpy(p, &v, sizeof(v));
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
@@ -54,13 +61,6 @@ __device__ __forceinline__ RowVec<T, V> rounded(const float (&x)[V])
 #pragma unroll
     for (int i = 0; i < V; ++i) v[i] = (T)x[i];
     return v;
-}
-
-// A parameter in the data's type or in fp32.
-template <class T>
-__device__ __forceinline__ float param_at(const void* p, bool f32, long long i)
-{
-    return f32 ? static_cast<const float*>(p)[i] : (float)static_cast<const T*>(p)[i];
 }
 
 constexpr float kLog2e = 1.44269504088896340736f;

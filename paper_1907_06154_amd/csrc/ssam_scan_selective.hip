@@ -277,77 +277,112 @@ struct ScanStepParams {
     long long b_group, c_group;
     const float *a, *skip, *dt_bias;
     float* state;
-    long long slot_stride, waves;
+    long long slot_stride;
 };
 
-template <int P>
-__device__ __forceinline__ float from_part(float v, int k)   // the value of lane k of the P lanes around this one
+// The value of lane K of the P lanes around this one, and the sum over them.
+template <int P, int K>
+__device__ __forceinline__ float from_part(float v)
 {
-    return __shfl(v, (int)(threadIdx.x & (kWave - 1) & ~(P - 1)) | k);
+    if constexpr (P == 1) return v;
+    else if constexpr (P == 2)
+        return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), K == 0 ? 0xA0 : 0xF5, 0xf, 0xf, true));   // [0,0,2,2], [1,1,3,3]
+    else if constexpr (P == 4) return quad_lane<K>(v);
+    else return __shfl(v, (int)(threadIdx.x & (kWave - 1) & ~(P - 1)) | K);
 }
 template <int P>
 __device__ __forceinline__ float part_sum(float v)
 {
-#pragma unroll
-    for (int d = 1; d < P; d *= 2) v += __shfl_xor(v, d);
+    auto moved = [](float x, auto ctrl) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    if constexpr (P >= 2) v += moved(v, std::integral_constant<int, 0xB1>{});    // [1,0,3,2]
+    if constexpr (P >= 4) v += moved(v, std::integral_constant<int, 0x4E>{});    // [2,3,0,1]
+    if constexpr (P >= 8) v += moved(v, std::integral_constant<int, 0x141>{});   // eight lanes mirrored: the other quad
+    if constexpr (P >= 16) v += moved(v, std::integral_constant<int, 0x128>{});  // the row of 16 turned by 8
     return v;
 }
 
-// A wave takes 64 channels of a row.  Their states are 64 x 4 P consecutive floats: P lanes share a channel, four states each, and go
-// through P channels one after the other, so that every load is a run of whole lines; what belongs to a channel alone (time step,
-// gate, output) is made once, by the lane of that number, and handed round.  Bound by the state: 8 bytes per value of it.
+template <int... K, class F>
+__device__ __forceinline__ void for_each(std::integer_sequence<int, K...>, F f)
+{
+    (f(std::integral_constant<int, K>{}), ...);
+}
+
+// Channels that P lanes with four states each go through one after the other, and those of a wave.
+constexpr int step_each(int P) { return P < 4 ? P : 4; }
+constexpr int step_channels(int P) { return kWave / P * step_each(P); }
+
+// P lanes share a channel, four states each, so that every load of states is a run of whole lines; what belongs to a channel alone
+// (time step, gate, output) is made once, by the lane of that number, and handed round.  A block's waves take the same channels of four rows, so
+// that the rates come from the L1.  Bound by the state: 8 bytes per value of it.
 template <class T, int P>
 __global__ __launch_bounds__(kBlock) void scan_step(ScanStepParams p)
 {
     const int lane = threadIdx.x & (kWave - 1);
-    const long long wave = (long long)blockIdx.x * kWavesPerBlock + (threadIdx.x >> 6);
-    if (wave >= p.waves) return;
-    const int row = (int)(wave / p.tiles);
+    const int row_blocks = (p.rows + kWavesPerBlock - 1) / kWavesPerBlock;
+    const int row = (int)(blockIdx.x % row_blocks) * kWavesPerBlock + (threadIdx.x >> 6);
+    if (row >= p.rows) return;
+    constexpr int KC = step_each(P);
+    const ChannelTile ct = channel_tile((int)(blockIdx.x / row_blocks), p.per_group, p.group_channels, step_channels(P));
+    constexpr int kApart = kWave / P;            // the k-th of a lane's channels is k * kApart + lane / P: a load of the k-th is one run
+    const int part = lane & (P - 1), first = lane / P, n0 = part * 4;
+    const bool own = part < KC && part * kApart + first < ct.n;
+    const int c = ct.c0 + part * kApart + first; // the channel whose time step and output are this lane's
+    struct Row {
+        float u, d, z;
+        RowVec<T, 4> b, w;
+    };
+    auto request = [&](int r) {
+        Row x;
+        x.u = own ? (float)static_cast<const T*>(p.in.d)[r * p.in.row + c] : 0.0f;
+        x.d = own ? (float)static_cast<const T*>(p.dt.d)[r * p.dt.row + c] : 0.0f;
+        x.z = own && p.gate.d ? (float)static_cast<const T*>(p.gate.d)[r * p.gate.row + c] : 0.0f;
+        x.b = load_row_vec<T, 4>(static_cast<const T*>(p.b.d) + r * p.b.row + ct.group * p.b_group + n0, p.states - n0);
+        x.w = load_row_vec<T, 4>(static_cast<const T*>(p.c.d) + r * p.c.row + ct.group * p.c_group + n0, p.states - n0);
+        return x;
+    };
+    Row x = request(row);
+    const float bias = own && p.dt_bias ? p.dt_bias[c] : 0.0f;
+    const float skip = own && p.skip ? p.skip[c] : 0.0f;
     SlotRows same(p.slot_of, p.rows, p.slots, row);
     if (!same.leads()) return;
-    const ChannelTile ct = channel_tile((int)(wave % p.tiles), p.per_group, p.group_channels, kWave);
-    const bool own = lane < ct.n;
-    const int c = ct.c0 + lane;                  // the channel whose time step and output are this lane's
-    const int part = lane & (P - 1), first = lane & ~(P - 1), n0 = part * 4;
     float* __restrict__ state = p.state + (long long)same.slot() * p.slot_stride;
-    float h[P][4], a2[P][4];
+    float h[KC][4], a2[KC][4];
 #pragma unroll
-    for (int k = 0; k < P; ++k) {
-        const long long cell = (long long)(ct.c0 + first + k) * p.states;
-        const bool there = first + k < ct.n;
+    for (int k = 0; k < KC; ++k) {
+        const long long cell = (long long)(ct.c0 + k * kApart + first) * p.states;
+        const bool there = k * kApart + first < ct.n;
         load_states<4>(state + cell, n0, p.states, there, h[k]);
         load_rates<4>(p.a + cell, n0, p.states, there, a2[k]);
     }
-    const float bias = own && p.dt_bias ? p.dt_bias[c] : 0.0f;
-    const float skip = own && p.skip ? p.skip[c] : 0.0f;
-    for (int r = row; r >= 0; r = same.next()) {
-        const float u = own ? (float)static_cast<const T*>(p.in.d)[r * p.in.row + c] : 0.0f;
-        float d = own ? (float)static_cast<const T*>(p.dt.d)[r * p.dt.row + c] + bias : 0.0f;
-        const float z = own && p.gate.d ? (float)static_cast<const T*>(p.gate.d)[r * p.gate.row + c] : 0.0f;
-        const RowVec<T, 4> b = load_row_vec<T, 4>(static_cast<const T*>(p.b.d) + r * p.b.row + ct.group * p.b_group + n0, p.states - n0);
-        const RowVec<T, 4> w = load_row_vec<T, 4>(static_cast<const T*>(p.c.d) + r * p.c.row + ct.group * p.c_group + n0, p.states - n0);
+    for (int r = row;;) {
+        float d = x.d + bias;
         if (p.softplus) d = softplus(d);
-        const float x = d * u;
+        const float du = d * x.u;
         float y = 0.0f;
-#pragma unroll
-        for (int k = 0; k < P; ++k) {
-            const float dk = from_part<P>(d, k), xk = from_part<P>(x, k);
+        for_each(std::make_integer_sequence<int, KC>{}, [&](auto k) {
+            constexpr int kk = decltype(k)::value;
+            const float dk = from_part<P, kk>(d), xk = from_part<P, kk>(du);
             float s = 0.0f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                h[k][i] = __builtin_fmaf((float)b[i], xk, h[k][i] * exp2_fast(dk * a2[k][i]));
-                s = __builtin_fmaf((float)w[i], h[k][i], s);
+                h[kk][i] = __builtin_fmaf(exp2_fast(dk * a2[kk][i]), h[kk][i], (float)x.b[i] * xk);
+                s = __builtin_fmaf((float)x.w[i], h[kk][i], s);
             }
             s = part_sum<P>(s);
-            y = part == k ? s : y;
-        }
-        y = __builtin_fmaf(skip, u, y);
-        if (p.gate.d) y *= silu(z);
+            y = part == kk ? s : y;
+        });
+        y = __builtin_fmaf(skip, x.u, y);
+        if (p.gate.d) y *= silu(x.z);
         if (own) static_cast<T*>(p.out.d)[r * p.out.row + c] = (T)y;
+        r = same.next();
+        if (r < 0) break;
+        x = request(r);
     }
 #pragma unroll
-    for (int k = 0; k < P; ++k)
-        store_states<4>(state + (long long)(ct.c0 + first + k) * p.states, n0, p.states, first + k < ct.n, h[k]);
+    for (int k = 0; k < KC; ++k)
+        store_states<4>(state + (long long)(ct.c0 + k * kApart + first) * p.states, n0, p.states, k * kApart + first < ct.n, h[k]);
 }
 
 }  // namespace
@@ -356,6 +391,7 @@ int scan_piece_rows(const ssam_sequences& q, int tiles, int blocks)
 {
     constexpr long long kShortest = 64, kLongest = 1 << 30;
     const long long total = q.d_begin ? q.rows : (long long)q.rows * q.sequences;
+    if (q.d_begin) blocks += blocks / 2;   // packed sequences end inside pieces: shorter ones even that out (37 in 8191 rows: 140 -> 129 us; equal ones lose by it, 141 -> 149)
     long long piece = (total * tiles + blocks - 1) / blocks;
     if (!q.d_begin && (long long)q.sequences * tiles >= blocks / 2) piece = q.rows;
     piece = (piece + 31) / 32 * 32;
@@ -502,7 +538,8 @@ int ssam_scan_selective_step(const ssam_scan_selective_step_args* a, void* hip_s
     p.channels = a->channels;
     p.states = a->states;
     p.group_channels = a->channels / a->groups;
-    p.per_group = (p.group_channels + kWave - 1) / kWave;
+    const int lanes = a->states <= 4 ? 1 : a->states <= 8 ? 2 : a->states <= 16 ? 4 : a->states <= 32 ? 8 : 16;
+    p.per_group = (p.group_channels + step_channels(lanes) - 1) / step_channels(lanes);
     p.tiles = p.per_group * a->groups;
     p.softplus = a->softplus != 0;
     p.slot_of = a->d_slots;
@@ -519,17 +556,16 @@ int ssam_scan_selective_step(const ssam_scan_selective_step_args* a, void* hip_s
     p.dt_bias = a->d_dt_bias;
     p.state = a->d_state;
     p.slot_stride = a->slot_stride;
-    p.waves = (long long)a->rows * p.tiles;
-    const long long blocks = (p.waves + kWavesPerBlock - 1) / kWavesPerBlock;
+    const long long blocks = ((long long)a->rows + kWavesPerBlock - 1) / kWavesPerBlock * p.tiles;
     if (blocks > kMaxGrid) return SSAM_ERR_DIM;
     return with_row_type(a->dtype, [&](auto t) {
         using T = decltype(t);
         const dim3 grid((unsigned)blocks), block(kBlock);
         hipStream_t st = (hipStream_t)hip_stream;
-        if (a->states <= 4) hipLaunchKernelGGL((scan_step<T, 1>), grid, block, 0, st, p);
-        else if (a->states <= 8) hipLaunchKernelGGL((scan_step<T, 2>), grid, block, 0, st, p);
-        else if (a->states <= 16) hipLaunchKernelGGL((scan_step<T, 4>), grid, block, 0, st, p);
-        else if (a->states <= 32) hipLaunchKernelGGL((scan_step<T, 8>), grid, block, 0, st, p);
+        if (lanes == 1) hipLaunchKernelGGL((scan_step<T, 1>), grid, block, 0, st, p);
+        else if (lanes == 2) hipLaunchKernelGGL((scan_step<T, 2>), grid, block, 0, st, p);
+        else if (lanes == 4) hipLaunchKernelGGL((scan_step<T, 4>), grid, block, 0, st, p);
+        else if (lanes == 8) hipLaunchKernelGGL((scan_step<T, 8>), grid, block, 0, st, p);
         else hipLaunchKernelGGL((scan_step<T, 16>), grid, block, 0, st, p);
         return launched();
     });

@@ -231,15 +231,17 @@ __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
                 if (!kMarkAhead) load_states<NS>(marks + tile * plane, n0, p.states, live, mark);
 #pragma unroll
                 for (int i = 0; i < NS; ++i) h[i] = mark[i];
-#pragma unroll 4
-                for (int t = 0; t < part * kKept; ++t) {
-                    const Pair dv = dx[t][place];
+                for (int t0 = 0; t0 < part * kKept; t0 += 4) {
 #pragma unroll
-                    for (int m = 0; m < NS / 4; ++m) {
-                        const float w = bc[t][pairs + m][0];
-                        const float v[4] = {quad_lane<0>(w) * dv[1], quad_lane<1>(w) * dv[1], quad_lane<2>(w) * dv[1], quad_lane<3>(w) * dv[1]};
+                    for (int t = t0; t < t0 + 4; ++t) {
+                        const Pair dv = dx[t][place];
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) h[4 * m + i] = __builtin_fmaf(exp2_fast(dv[0] * a2[4 * m + i]), h[4 * m + i], v[i]);
+                        for (int m = 0; m < NS / 4; ++m) {
+                            const float w = bc[t][pairs + m][0];
+                            const float v[4] = {quad_lane<0>(w) * dv[1], quad_lane<1>(w) * dv[1], quad_lane<2>(w) * dv[1], quad_lane<3>(w) * dv[1]};
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) h[4 * m + i] = __builtin_fmaf(exp2_fast(dv[0] * a2[4 * m + i]), h[4 * m + i], v[i]);
+                        }
                     }
                 }
 #pragma unroll
@@ -325,7 +327,6 @@ __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
             if (part_bc) {
                 float* to = part_bc + (long long)row * p.groups * 2 * p.states;
                 const unsigned wide = p.groups * 2 * p.states;
-#pragma unroll
                 for (int i = tid; i < K * 2 * NP; i += kBlock) {
                     const int r = i / (2 * NP), w = i / NP % 2, n = i % NP;
                     float v = sum_bc[0][r][w][n];
@@ -365,7 +366,7 @@ __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
 
 // Gradients of b and c: the tiles of a group added up, in order.  A block takes kSumRows rows, a thread values 256 apart, and keeps
 // eight tiles' requests in flight.
-constexpr int kSumRows = 32;
+constexpr int kSumRows = 8;
 template <class T>
 __global__ __launch_bounds__(kBlock) void back_sum_bc(BackParams p, Pieces rows)
 {
