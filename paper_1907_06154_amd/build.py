@@ -18,6 +18,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libssam.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")   # argument marshalling of the binding, a module of this interpreter
+SEQUENCE = os.path.join(HERE, "_sequence.so")   # the same for the sequence operators, which take many tensors: against torch's C++ headers
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -62,7 +63,9 @@ def build(verbose: bool = False, jobs: int = 8, extra=(), lib: str = LIB, increm
     os.makedirs(OBJ, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
     with ThreadPoolExecutor(max_workers=jobs) as pool:
+        sequence = pool.submit(build_sequence, incremental)
         objs = list(pool.map(lambda s: _compile(s, list(extra), incremental), srcs))
+        sequence.result()
     link_extra = [a for a in extra if "sanitize" in a]      # a sanitizer build links its runtime too
     cmd = ["hipcc", "--offload-arch=gfx950", "-shared", "-fPIC", *link_extra, "-o", lib, *objs]
     subprocess.run(cmd, check=True)
@@ -77,6 +80,21 @@ def build_marshal() -> None:
     subprocess.run(["gcc", "-O2", "-shared", "-fPIC", "-I" + sysconfig.get_paths()["include"], "-o", tmp,
                     os.path.join(CSRC, "ssam_marshal.c")], check=True)
     os.replace(tmp, MARSHAL)
+
+
+def build_sequence(incremental: bool = False) -> None:
+    import torch
+    src, tmp, dep = os.path.join(CSRC, "ssam_sequence_marshal.cpp"), SEQUENCE + ".tmp", os.path.join(OBJ, "ssam_sequence_marshal.cpp.o.d")
+    if incremental and os.path.exists(SEQUENCE) and os.path.exists(dep):
+        t, words = os.path.getmtime(SEQUENCE), open(dep).read().replace("\\\n", " ").split()[1:]
+        if all(os.path.exists(f) and os.path.getmtime(f) <= t for f in words):
+            return
+    home = os.path.dirname(torch.__file__)
+    inc = [os.path.join(home, "include"), os.path.join(home, "include", "torch", "csrc", "api", "include")]
+    subprocess.run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                    "-I" + sysconfig.get_paths()["include"], *[a for d in inc for a in ("-isystem", d)], "-MD", "-MF", dep, "-o", tmp, src,
+                    "-L" + os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath," + os.path.join(home, "lib")], check=True)
+    os.replace(tmp, SEQUENCE)
 
 
 if __name__ == "__main__":

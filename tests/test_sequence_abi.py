@@ -64,25 +64,6 @@ def size(L, name, s):
     return getattr(L, name)(ctypes.cast(ctypes.byref(s), ctypes.c_char_p))
 
 
-def test_the_binding_packs_the_structs():
-    for kind, packed in ((Conv, seq._CONV1D), (ConvBack, seq._CONV1D_BACK), (ConvStep, seq._CONV1D_STEP), (Scan, seq._SCAN), (ScanBack, seq._SCAN_BACK),
-                         (ScanStep, seq._SCAN_STEP)):
-        assert ctypes.sizeof(kind) == packed.size, kind
-        # the same order of fields: every one set to a value of its own
-        flat = []
-
-        def fill(obj):
-            for n, t in obj._fields_:
-                if issubclass(t, ctypes.Structure):
-                    fill(getattr(obj, n))
-                else:
-                    flat.append(len(flat) + 1)
-                    setattr(obj, n, len(flat))
-        s = kind()
-        fill(s)
-        assert bytes(s) == packed.pack(*flat), kind
-
-
 def test_the_header_is_c_and_has_these_sizes(tmp_path):
     kinds = {"ssam_conv1d_args": Conv, "ssam_conv1d_backward_args": ConvBack, "ssam_conv1d_step_args": ConvStep, "ssam_scan_selective_args": Scan,
              "ssam_scan_selective_backward_args": ScanBack, "ssam_scan_selective_step_args": ScanStep}
@@ -135,7 +116,7 @@ def test_conv1d_backward_refusals(L):
         return s
     f = lambda **c: call(L, "ssam_conv1d_backward", make(**c))  # noqa: E731
     need = size(L, "ssam_conv1d_backward_workspace_bytes", make())
-    assert need == 2 * 2 * 5 * 64 * 4                       # 2 pieces of 8 rows a sequence, 4 taps and the bias
+    assert need == 5 * 64 * 4                               # 2 pieces of 8 rows a sequence make one block; 4 taps and the bias
     assert size(L, "ssam_conv1d_backward_workspace_bytes", make(grad_weight=None, grad_bias=None)) == 0
     assert size(L, "ssam_conv1d_backward_workspace_bytes", make(taps=9)) == 0 and L.ssam_conv1d_backward_workspace_bytes(None) == 0
     assert f(weight=None) == NULL and f(grad_out=Rows(None, 0, 0)) == NULL and f(work=None) == NULL and f(x=Rows(None, 0, 0)) == NULL
@@ -253,6 +234,12 @@ def test_tensors_must_live_on_the_gpu():
         ssam.ssam_conv1d(x, w)
     with pytest.raises(ValueError, match="GPU"):
         ssam.ssam_scan_selective(x, x, w, x.view(4, 1, 8), x.view(4, 1, 8))
+    with pytest.raises(ValueError, match="GPU"):
+        ssam.ssam_scan_selective_marks(x, w)
+    with pytest.raises(TypeError, match="tensor"):
+        ssam.ssam_conv1d(None, w)
+    with pytest.raises(TypeError):
+        seq._fast.conv1d(x, w)
 
 
 def test_the_references_gradients_against_differences():

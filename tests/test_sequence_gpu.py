@@ -153,7 +153,8 @@ def test_conv1d_backward(lay, dt, W, D, silu, bias, state, form):
     assert all(torch.equal(p, q) for p, q in zip(got, again) if p is not None), "the same call twice"
 
 
-@pytest.mark.parametrize("dt,W,D,silu", [("bfloat16", 4, 520, True), ("float32", 3, 5, False), ("float16", 8, 77, True), ("bfloat16", 1, 64, True)])
+@pytest.mark.parametrize("dt,W,D,silu", [("bfloat16", 4, 520, True), ("float32", 3, 5, False), ("float16", 8, 77, True), ("bfloat16", 1, 64, True),
+                                         ("bfloat16", 4, 525, True), ("float16", 2, 515, False), ("float32", 4, 259, True)])
 def test_conv1d_step(dt, W, D, silu):
     g = torch.Generator().manual_seed(5)
     dtype = TYPES[dt]
@@ -534,6 +535,71 @@ def test_infinities_stay_in_their_sequence_and_channel():
         assert torch.equal(u[same], v[same])
         assert not torch.isfinite(u[20, 9])
     assert torch.isfinite(final[1:]).all() and torch.isfinite(final[0, :9]).all() and torch.isfinite(final[0, 10:]).all()
+
+
+def test_refusals_of_the_binding():
+    """Shapes, types, layouts: refused before anything runs."""
+    D, N = 8, 4
+    x, w = torch.zeros(6, D, device="cuda"), torch.zeros(D, 4, device="cuda")
+    a, b = torch.zeros(D, N, device="cuda"), torch.zeros(6, 1, N, device="cuda")
+    starts = torch.tensor([0, 6], dtype=torch.int32, device="cuda")
+
+    def refused(match, f, *args, error=ValueError, **kw):
+        with pytest.raises(error, match=match):
+            f(*args, **kw)
+    conv, step = ssam.ssam_conv1d, ssam.ssam_conv1d_step
+    refused("weight", conv, x, w[:7])
+    refused("weight", conv, x, w.half())
+    refused("bias", conv, x, w, bias=torch.zeros(D))
+    refused("bias", conv, x, w, bias=torch.zeros(7, device="cuda"))
+    refused("d_in", conv, x[0], w)
+    refused("contiguous channels", conv, x.t().contiguous().t(), w)
+    refused("unsupported dtype", conv, x.double(), w.double(), error=TypeError)
+    refused("d_out", conv, x, w, d_out=x[:5].clone())
+    refused("d_state", conv, x, w, d_state=torch.zeros(2, 3, D, device="cuda"))
+    refused("starts", conv, x, w, starts=starts.long())
+    refused("starts", conv, x.view(2, 3, D), w, starts=starts)
+    refused("starts", conv, x, w, starts=starts, lengths=starts)
+    refused("lengths", conv, x, w, lengths=starts)
+    refused("lengths", conv, x.view(2, 3, D), w, lengths=starts[:1])
+    refused(None, conv, x, torch.zeros(D, 9, device="cuda"), error=ssam.SsamError)
+    refused(None, conv, x, w, d_out=x, error=ssam.SsamError)
+    refused("slot for each", step, x, w, torch.zeros(5, 3, D, device="cuda"))
+    refused("d_state", step, x, w, torch.zeros(6, 2, D, device="cuda"))
+    refused("contiguous slots", step, x, w, torch.zeros(6, 3, 2 * D, device="cuda")[..., ::2])
+    refused("overlap", step, x, w, torch.zeros(3, D, device="cuda").expand(6, 3, D))
+    refused("slots", step, x, w, torch.zeros(6, 3, D, device="cuda"), slots=starts)
+    scan, back, mark = ssam.ssam_scan_selective, ssam.ssam_scan_selective_backward, ssam.ssam_scan_selective_marks
+    refused("a must", scan, x, x, a.half(), b, b)
+    refused("a must", scan, x, x, a.t(), b, b)
+    refused("d_dt", scan, x, x.half(), a, b, b)
+    refused("c and b", scan, x, x, a, b, torch.zeros(6, 2, N, device="cuda"))
+    refused("c and b", scan, x, x, a, torch.zeros(6, 1, 3, device="cuda"), torch.zeros(6, 1, 3, device="cuda"))
+    refused("b must", scan, x, x, a, b[:, 0], b)
+    refused("skip", scan, x, x, a, b, b, skip=torch.zeros(D, device="cuda").half())
+    refused("gate", scan, x, x, a, b, b, gate=x[:, :7])
+    refused("d_marks", scan, x, x, a, b, b, d_marks=torch.zeros(1, N, D, device="cuda"))
+    refused("d_marks", scan, x.repeat(8, 1), x.repeat(8, 1), a, b.repeat(8, 1, 1), b.repeat(8, 1, 1), d_marks=mark(x, a))
+    refused("d_marks", back, x, x, x, a, b, b, a)
+    refused("must be a tensor", back, None, x, x, a, b, b, mark(x, a), error=TypeError)
+    refused(None, scan, x, x, a, torch.zeros(6, 3, N, device="cuda"), torch.zeros(6, 3, N, device="cuda"), error=ssam.SsamError)
+    big = torch.zeros(400, D, device="cuda")
+    bb = torch.zeros(400, 1, N, device="cuda")
+    refused(None, scan, big, big, a, bb, bb, d_work=torch.zeros(8, device="cuda"), error=ssam.SsamError)
+
+
+def test_own_workspace_and_results():
+    D, N = 64, 16
+    g = torch.Generator().manual_seed(9)
+    x, dt = randn(g, 400, D), randn(g, 400, D)
+    b, c = randn(g, 400, 1, N), randn(g, 400, 1, N)
+    a = -(torch.rand(D, N, generator=g) + 0.1).cuda()
+    need = ssam.ssam_scan_selective_workspace_bytes(x, a)
+    assert need > 0
+    work = torch.full((need,), 255, dtype=torch.uint8, device="cuda")        # NaN everywhere
+    out = torch.full((400, D), float("nan"), device="cuda")
+    assert ssam.ssam_scan_selective(x, dt, a, b, c, softplus=True, d_work=work, d_out=out) is out
+    assert torch.equal(out, ssam.ssam_scan_selective(x, dt, a, b, c, softplus=True))
 
 
 def test_offsets_past_32_bits():
