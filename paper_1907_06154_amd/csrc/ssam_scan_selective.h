@@ -89,6 +89,48 @@ __device__ __forceinline__ void group_sums(float (&y)[4])
 #undef SSAM_TURN
 }
 
+// One row's sum of cQ h[Q], and g[Q] += cQ x: the same for single rows.
+__device__ __forceinline__ float quad_dot(float c, float h0, float h1, float h2, float h3)
+{
+    float y;
+    asm("s_nop 1\n\t"
+        "v_mul_f32_dpp %0, %1, %2 quad_perm:[0,0,0,0] row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %0, %1, %3 quad_perm:[1,1,1,1] row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %0, %1, %4 quad_perm:[2,2,2,2] row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %0, %1, %5 quad_perm:[3,3,3,3] row_mask:0xf bank_mask:0xf"
+        : "=&v"(y)
+        : "v"(c), "v"(h0), "v"(h1), "v"(h2), "v"(h3));
+    return y;
+}
+__device__ __forceinline__ void quad_add(float& g0, float& g1, float& g2, float& g3, float c, float x)
+{
+    asm("s_nop 1\n\t"
+        "v_fmac_f32_dpp %0, %4, %5 quad_perm:[0,0,0,0] row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %1, %4, %5 quad_perm:[1,1,1,1] row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %2, %4, %5 quad_perm:[2,2,2,2] row_mask:0xf bank_mask:0xf\n\t"
+        "v_fmac_f32_dpp %3, %4, %5 quad_perm:[3,3,3,3] row_mask:0xf bank_mask:0xf"
+        : "+&v"(g0), "+&v"(g1), "+&v"(g2), "+&v"(g3)
+        : "v"(c), "v"(x));
+}
+// group_sum of two values, of which these blocks may have made either.
+template <int GL>
+__device__ __forceinline__ void group_sums(float& r, float& s)
+{
+    if constexpr (GL == 4)
+        asm("s_nop 1\n\t"
+            "v_add_f32_dpp %0, %0, %0 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %1, %1, %1 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+            "s_nop 0\n\t"
+            "v_add_f32_dpp %0, %0, %0 row_ror:4 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %1, %1, %1 row_ror:4 row_mask:0xf bank_mask:0xf"
+            : "+v"(r), "+v"(s));
+    if constexpr (GL == 2)
+        asm("s_nop 1\n\t"
+            "v_add_f32_dpp %0, %0, %0 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %1, %1, %1 row_ror:8 row_mask:0xf bank_mask:0xf"
+            : "+v"(r), "+v"(s));
+}
+
 // Where the values of a row's b and c lie in LDS: the NS / 4 that a lane loads side by side.  Lane (group, quad lane j) needs states
 // group * NS + 4 m + j.
 template <class Shape> __device__ __forceinline__ int pair_place(int n) { return (n / Shape::NS * 4 + n % 4) * (Shape::NS / 4) + n % Shape::NS / 4; }

@@ -8,8 +8,8 @@
 // would save the second half's way to its first row, 9 of 72 cycles a state, for 4 bytes more per row, channel and 16 states, written
 // and read; keeping 16 rows takes 128 registers and spills.)
 //
-// The sums over channels: a wave's 16 channels by lane swaps between its rows of 16 lanes and DPP inside quads, the block's waves
-// through LDS, the blocks of a group through the workspace and a launch that adds them in order.
+// The sums over channels: a wave's and the block's waves' through LDS, the blocks of a group through the workspace and a launch that
+// adds them in order.
 #include "ssam_scan_selective.h"
 
 namespace ssam {
@@ -32,42 +32,65 @@ struct BackParams {
     int channels, states, groups, group_channels, per_group, tiles, softplus, cut;
 };
 
-// Sums of v[0 .. 3] over the four rows of 16 lanes: afterwards row 0 holds v[0]'s, row 1 v[2]'s, row 2 v[1]'s, row 3 v[3]'s.
-__device__ __forceinline__ void swap_halves(float& a, float& b)
-{
-    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
-    const unsigned first = r[0], second = r[1];     // (a bit cast of a vector's element itself reads element 0)
-    a = __builtin_bit_cast(float, first);
-    b = __builtin_bit_cast(float, second);
-}
-__device__ __forceinline__ void swap_rows(float& a, float& b)
-{
-    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
-    const unsigned first = r[0], second = r[1];     // (a bit cast of a vector's element itself reads element 0)
-    a = __builtin_bit_cast(float, first);
-    b = __builtin_bit_cast(float, second);
-}
-__device__ __forceinline__ float rows_sum(float v0, float v1, float v2, float v3)
-{
-    swap_halves(v0, v1);
-    swap_halves(v2, v3);
-    float a = v0 + v1, b = v2 + v3;
-    swap_rows(a, b);
-    return a + b;
-}
-__device__ __forceinline__ int row_state(int lane) { return ((lane >> 5) & 1) | ((lane >> 3) & 2); }   // which of the four a lane then holds
-
 template <int CTRL>
 __device__ __forceinline__ float quad_moved(float v)
 {
     return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xf, 0xf, true));
 }
-// Of eight lanes whose quads hold one value in their even and one in their odd lanes: the other quad's of the same kind.
-__device__ __forceinline__ float other_quad(float v) { return quad_moved<0x141>(quad_moved<0xB1>(v)); }
+
+// Sums over a wave's channels of four states' terms of b's and of c's gradient.  The lanes put their terms into LDS, one vector
+// each, and every output -- 4 GL states of b, as many of c -- is added up by LP lanes, eight channels each: 8 vector instructions
+// where swaps between rows of lanes and DPP took 22.  A wave reads what itself wrote (the LDS keeps a wave's order), one step later,
+// so no barrier and no wait is needed.  The vectors lie so that eight lanes' writes and 32 lanes' reads each meet every bank once.
+template <int GL>
+struct ChannelSums {
+    static constexpr int kOutputs = 8 * GL, LP = kWave / kOutputs;
+    static constexpr int kApart = 92 * 4;                // b's terms, then c's
+    static constexpr int kFloats = 2 * kApart;           // of one step
+
+    float* at;           // this wave's two steps
+    int to, from, which, i, group;
+
+    // channel c of group g
+    static __device__ __forceinline__ int vector(int c, int g) { return c % LP + LP * g + 12 * (c / LP % 2) + 24 * (c / (2 * LP)); }
+    __device__ __forceinline__ ChannelSums(float* buffer, int lane)
+    {
+        const int o = lane / LP, part = lane % LP;
+        i = o % 4;
+        group = o / 4 % GL;
+        which = o / (4 * GL);
+        at = buffer;
+        to = vector(lane_channel<GL>(lane), lane_group<GL>(lane)) * 4;
+        from = which * kApart + vector(part, group) * 4 + i;
+    }
+    __device__ __forceinline__ void put(int step, const float (&vb)[4], const float (&vc)[4]) const
+    {
+        float* p = at + (step & 1) * kFloats + to;
+        *reinterpret_cast<RowVec<float, 4>*>(p) = RowVec<float, 4>{vb[0], vb[1], vb[2], vb[3]};
+        *reinterpret_cast<RowVec<float, 4>*>(p + kApart) = RowVec<float, 4>{vc[0], vc[1], vc[2], vc[3]};
+        __builtin_amdgcn_wave_barrier();     // no instruction: the compiler keeps the other lanes' reads behind it
+    }
+    // channels part, part + LP, ..
+    __device__ __forceinline__ void take(int step, float (&t)[8]) const
+    {
+        const float* p = at + (step & 1) * kFloats + from;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t[k] = p[(12 * (k & 1) + 24 * (k >> 1)) * 4];
+    }
+    static __device__ __forceinline__ float sum(const float (&t)[8])
+    {
+        float v = ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
+        if (LP >= 2) v += quad_moved<0xB1>(v);
+        if (LP >= 4) v += quad_moved<0x4E>(v);
+        return v;
+    }
+    // the state of this lane's output, for the vector of number m
+    template <int NS> __device__ __forceinline__ int state(int m) const { return group * NS + 4 * m + i; }
+};
 
 // kWhole: everything.  !kWhole: only what a piece lets out at its first row when nothing reaches it from behind.
 template <class T, class Shape, bool kWhole>
-__global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
+__global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(BackParams p)
 {
     constexpr int GL = Shape::GL, NS = Shape::NS, NP = Shape::kStates, CB = Shape::kChannels, K = kTile;
     constexpr int E = K * CB / kBlock;                   // values of a thread
@@ -82,6 +105,7 @@ __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
     __shared__ float ys[kWhole ? K : 1][kRow];
     __shared__ Pair rs[kWhole ? K : 1][kRow];            // r, s
     __shared__ float sum_bc[kWhole ? kWavesPerBlock : 1][K][2][NP];
+    __shared__ __attribute__((aligned(16))) float terms[kWhole ? kWavesPerBlock : 1][2 * ChannelSums<GL>::kFloats];
 
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
     const int slot = blockIdx.x / p.tiles;
@@ -174,6 +198,7 @@ __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
         if (kWhole && kMarkAhead) load_states<NS>(marks + (row / K) * plane, n0, p.states, live, mark_next);
     };
     const int pairs = own_pairs<Shape>(lane);
+    const ChannelSums<GL> across(terms[kWhole ? wave : 0], lane);
 
     const int tiles = (q.n + K - 1) / K;
     if (tiles > 0) request((tiles - 1) * K);
@@ -211,92 +236,132 @@ __global__ __launch_bounds__(kBlock, 2) void scan_back(BackParams p)
         if (tile > 0) request(row - K);
 
         if constexpr (!kWhole) {
-#pragma unroll 4
-            for (int t = K - 1; t >= 0; --t) {
-                const float dt_ = dx[t][place][0], dyt = dys[t][place];
-                sum += dt_;
+#pragma unroll 1
+            for (int t0 = K - 4; t0 >= 0; t0 -= 4) {
+                float d4[4], dy4[4], c4[4][NS / 4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    d4[k] = dx[t0 + k][place][0];
+                    dy4[k] = dys[t0 + k][place];
+#pragma unroll
+                    for (int m = 0; m < NS / 4; ++m) c4[k][m] = bc[t0 + k][pairs + m][1];
+                }
 #pragma unroll
                 for (int m = 0; m < NS / 4; ++m) {
-                    const float w = bc[t][pairs + m][1];
-                    const float v[4] = {quad_lane<0>(w) * dyt, quad_lane<1>(w) * dyt, quad_lane<2>(w) * dyt, quad_lane<3>(w) * dyt};
+                    float e[4][4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) g[4 * m + i] = (v[i] + g[4 * m + i]) * exp2_fast(dt_ * a2[4 * m + i]);
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) e[k][i] = exp2_fast(d4[k] * a2[4 * m + i]);
+#pragma unroll
+                    for (int k = 3; k >= 0; --k) {
+                        quad_add(g[4 * m], g[4 * m + 1], g[4 * m + 2], g[4 * m + 3], c4[k][m], dy4[k]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) g[4 * m + i] *= e[k][i];
+                    }
                 }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum += d4[k];
             }
         } else {
 #pragma unroll 1
             for (int part = K / kKept - 1; part >= 0; --part) {
                 // the states again, from the mark: those before this part's rows in passing, then each row's
-                float h[NS], hs[kKept][NS], as[kKept][NS];
+                float h[NS], hs[kKept][NS], as[kKept][NS], dyr[kKept];
+                Pair dv[kKept], w[kKept][NS / 4];
                 if (!kMarkAhead) load_states<NS>(marks + tile * plane, n0, p.states, live, mark);
+#pragma unroll
+                for (int k = 0; k < kKept; ++k) {
+                    dv[k] = dx[part * kKept + k][place];
+                    dyr[k] = dys[part * kKept + k][place];
+#pragma unroll
+                    for (int m = 0; m < NS / 4; ++m) w[k][m] = bc[part * kKept + k][pairs + m];
+                }
 #pragma unroll
                 for (int i = 0; i < NS; ++i) h[i] = mark[i];
                 for (int t0 = 0; t0 < part * kKept; t0 += 4) {
 #pragma unroll
                     for (int t = t0; t < t0 + 4; ++t) {
-                        const Pair dv = dx[t][place];
+                        const Pair d = dx[t][place];
 #pragma unroll
                         for (int m = 0; m < NS / 4; ++m) {
-                            const float w = bc[t][pairs + m][0];
-                            const float v[4] = {quad_lane<0>(w) * dv[1], quad_lane<1>(w) * dv[1], quad_lane<2>(w) * dv[1], quad_lane<3>(w) * dv[1]};
+                            const float b = bc[t][pairs + m][0];
+                            const float v[4] = {quad_lane<0>(b) * d[1], quad_lane<1>(b) * d[1], quad_lane<2>(b) * d[1], quad_lane<3>(b) * d[1]};
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) h[4 * m + i] = __builtin_fmaf(exp2_fast(dv[0] * a2[4 * m + i]), h[4 * m + i], v[i]);
+                            for (int i = 0; i < 4; ++i) h[4 * m + i] = __builtin_fmaf(exp2_fast(d[0] * a2[4 * m + i]), h[4 * m + i], v[i]);
                         }
                     }
                 }
 #pragma unroll
                 for (int k = 0; k < kKept; ++k) {
-                    const int t = part * kKept + k;
-                    const Pair dv = dx[t][place];
                     const float* before = k ? hs[k - 1] : h;
 #pragma unroll
                     for (int m = 0; m < NS / 4; ++m) {
-                        const float w = bc[t][pairs + m][0];
-                        const float v[4] = {quad_lane<0>(w) * dv[1], quad_lane<1>(w) * dv[1], quad_lane<2>(w) * dv[1], quad_lane<3>(w) * dv[1]};
+                        const float b = w[k][m][0], x = dv[k][1];
+                        const float v[4] = {quad_lane<0>(b) * x, quad_lane<1>(b) * x, quad_lane<2>(b) * x, quad_lane<3>(b) * x};
 #pragma unroll
                         for (int i = 4 * m; i < 4 * m + 4; ++i) {
-                            as[k][i] = exp2_fast(dv[0] * a2[i]);
+                            as[k][i] = exp2_fast(dv[k][0] * a2[i]);
                             hs[k][i] = __builtin_fmaf(as[k][i], before[i], v[i - 4 * m]);
                         }
                     }
                 }
+                if (gated) {             // y, for the gate's gradient
+#pragma unroll
+                    for (int k = 0; k < kKept; k += 4) {
+                        float y[4];
+#pragma unroll
+                        for (int m = 0; m < NS / 4; ++m) {
+                            float c[4], hm[4][4];
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) {
+                                c[r] = w[k + r][m][1];
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) hm[r][i] = hs[k + r][4 * m + i];
+                            }
+                            if (m == 0) quad_dots<true>(y, c, hm);
+                            else quad_dots<false>(y, c, hm);
+                        }
+                        group_sums<GL>(y);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) ys[part * kKept + k + r][place] = y[r];
+                    }
+                }
+                float terms_of[8];
 #pragma unroll
                 for (int k = kKept - 1; k >= 0; --k) {
                     const int t = part * kKept + k;
-                    const Pair dv = dx[t][place];
-                    const float dyt = dys[t][place];
                     const float* before = k ? hs[k - 1] : h;
-                    float r = 0.0f, s = 0.0f, y = 0.0f;
+                    float r = 0.0f, s = 0.0f;
 #pragma unroll
                     for (int m = 0; m < NS / 4; ++m) {
-                        const Pair w = bc[t][pairs + m];
-                        const float b[4] = {quad_lane<0>(w[0]), quad_lane<1>(w[0]), quad_lane<2>(w[0]), quad_lane<3>(w[0])};
-                        const float c[4] = {quad_lane<0>(w[1]), quad_lane<1>(w[1]), quad_lane<2>(w[1]), quad_lane<3>(w[1])};
-                        float vb[4], vc[4];
+                        const int step = (kKept - 1 - k) * (NS / 4) + m;
+                        if (step > 0) across.take(step - 1, terms_of);       // added up below: their reads pass this step's arithmetic
+                        float *gm = g + 4 * m, vb[4], vc[4];
+                        quad_add(gm[0], gm[1], gm[2], gm[3], w[k][m][1], dyr[k]);
+                        const float sm = quad_dot(w[k][m][0], gm[0], gm[1], gm[2], gm[3]);
+                        s = m ? s + sm : sm;
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const int i = 4 * m + j;
-                            y = __builtin_fmaf(c[j], hs[k][i], y);
-                            vc[j] = hs[k][i] * dyt;
-                            g[i] = __builtin_fmaf(c[j], dyt, g[i]);
-                            vb[j] = g[i] * dv[1];
-                            s = __builtin_fmaf(b[j], g[i], s);
+                            vc[j] = hs[k][i] * dyr[k];
+                            vb[j] = g[i] * dv[k][1];
                             g[i] *= as[k][i];                      // what reaches the row before
                             const float qi = g[i] * before[i];
-                            da[i] = __builtin_fmaf(dv[0], qi, da[i]);
-                            r = __builtin_fmaf(a2[i], qi, r);
+                            da[i] = __builtin_fmaf(dv[k][0], qi, da[i]);
+                            r = i ? __builtin_fmaf(a2[i], qi, r) : a2[i] * qi;
                         }
-                        // b's sums end in the even lanes of a quad, c's in the odd ones
-                        const float tb = rows_sum(vb[0], vb[1], vb[2], vb[3]), tc = rows_sum(vc[0], vc[1], vc[2], vc[3]);
-                        float v = lane & 1 ? tc : tb;
-                        v += quad_moved<0xB1>(lane & 1 ? tb : tc);
-                        v += quad_moved<0x4E>(v);
-                        if (GL == 2) v += other_quad(v);
-                        sum_bc[wave][t][lane & 1][n0 + 4 * m + row_state(lane)] = v;
+                        across.put(step, vb, vc);
+                        if (step > 0) {
+                            const int tp = m ? t : t + 1, mp = m ? m - 1 : NS / 4 - 1;
+                            sum_bc[wave][tp][across.which][across.template state<NS>(mp)] = across.sum(terms_of);
+                        }
                     }
-                    ys[t][place] = group_sum<GL>(y);
-                    rs[t][place] = Pair{group_sum<GL>(r), group_sum<GL>(s)};
+                    group_sums<GL>(r, s);
+                    rs[t][place] = Pair{r, s};
                 }
+                across.take(kKept * (NS / 4) - 1, terms_of);
+                sum_bc[wave][part * kKept][across.which][across.template state<NS>(NS / 4 - 1)] = across.sum(terms_of);
             }
         }
         __syncthreads();
