@@ -46,10 +46,15 @@ __device__ __forceinline__ float group_sum(float v)
     return v;
 }
 
+// v[i] + b(lane i of the quad) x, i = 0 .. 3: the 4x4 matrix instruction with K = 1, sixteen outer products side by side whose lanes lie
+// as the quads do.  It takes 8 cycles where four products by DPP take 16 (full fp32; 1 x 4096 rows 140 -> 136 us).
+__device__ __forceinline__ RowVec<float, 4> quad_outer(float b, float x, RowVec<float, 4> v) { return __builtin_amdgcn_mfma_f32_4x4x1f32(b, x, v, 0, 0, 0); }
+
 // Four rows' y += c0 h0 + c1 h1 + c2 h2 + c3 h3 (kFirst: y = ..), with cQ the value of lane Q of the quad: multiply-adds that take it by
 // DPP themselves (the compiler moves it into a register first, twice the instructions).  A DPP read must lie two wait states behind
-// the write of its register, and the compiler counts neither into nor out of these blocks: hence the s_nop, and the order row by row.
-// y leaves only through another of these blocks or into memory, never into a DPP of the compiler's.
+// the write of its register, a read of what the 4x4 matrix instruction wrote five, and the compiler counts neither into nor out of
+// these blocks: hence the s_nop, of eight wait states, and the order row by row.  y leaves only through another of these blocks or
+// into memory, never into a DPP of the compiler's.
 template <bool kFirst>
 __device__ __forceinline__ void quad_dots(float (&y)[4], const float (&c)[4], const float (&h)[4][4])
 {
@@ -63,12 +68,12 @@ __device__ __forceinline__ void quad_dots(float (&y)[4], const float (&c)[4], co
         "v"(h[1][1]), "v"(h[2][1]), "v"(h[3][1]), "v"(h[0][2]), "v"(h[1][2]), "v"(h[2][2]), "v"(h[3][2]), "v"(h[0][3]), \
         "v"(h[1][3]), "v"(h[2][3]), "v"(h[3][3])
     if constexpr (kFirst)
-        asm("s_nop 1\n\t" SSAM_DOT("v_mul_f32_dpp", 0, 8, 9, 10, 11) SSAM_DOT("v_fmac_f32_dpp", 1, 12, 13, 14, 15)
+        asm("s_nop 7\n\t" SSAM_DOT("v_mul_f32_dpp", 0, 8, 9, 10, 11) SSAM_DOT("v_fmac_f32_dpp", 1, 12, 13, 14, 15)
                 SSAM_DOT("v_fmac_f32_dpp", 2, 16, 17, 18, 19) SSAM_DOT("v_fmac_f32_dpp", 3, 20, 21, 22, 23)
             : "=&v"(y[0]), "=&v"(y[1]), "=&v"(y[2]), "=&v"(y[3])
             : SSAM_INPUTS);
     else
-        asm("s_nop 1\n\t" SSAM_DOT("v_fmac_f32_dpp", 0, 8, 9, 10, 11) SSAM_DOT("v_fmac_f32_dpp", 1, 12, 13, 14, 15)
+        asm("s_nop 7\n\t" SSAM_DOT("v_fmac_f32_dpp", 0, 8, 9, 10, 11) SSAM_DOT("v_fmac_f32_dpp", 1, 12, 13, 14, 15)
                 SSAM_DOT("v_fmac_f32_dpp", 2, 16, 17, 18, 19) SSAM_DOT("v_fmac_f32_dpp", 3, 20, 21, 22, 23)
             : "+&v"(y[0]), "+&v"(y[1]), "+&v"(y[2]), "+&v"(y[3])
             : SSAM_INPUTS);

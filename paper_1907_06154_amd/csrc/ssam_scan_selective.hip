@@ -6,8 +6,9 @@
 // lane; every thread turns its eight values into (d, d u) once and puts them into LDS with the rows' b and c, the waves run the
 // recurrence from there, leave y in LDS, and the threads that loaded the values finish them (skip, gate) and store them.
 //
-// Per state and row that is one exp, two products and two multiply-adds; the exp (8 cycles of a SIMD against 2.5 - 4 of the
-// others) makes the vector unit the bound, not memory (8 bytes a value).
+// Per state and row that is one exp, three products and two sums; the exp (8 cycles of a SIMD against 2.5 - 4 of the others) makes the
+// vector unit the bound, not memory (8 bytes a value): 8 x 4096 rows of 4096 channels, 16 states, bf16 622 us, of which the unit
+// is busy 77 % with the two waves per SIMD that there are; the bytes alone would take 219.
 #include "ssam_scan_selective.h"
 
 namespace ssam {
@@ -31,7 +32,7 @@ constexpr int kAhead = 4;
 
 // kWhole: all rows, outputs and the last state.  !kWhole: only the state that a piece adds (from zero) and its time steps' sum.
 template <class T, class Shape, bool kWhole>
-__global__ __launch_bounds__(kBlock, Shape::NS <= 4 ? 3 : 2) void scan_rows(ScanParams p)
+__global__ __launch_bounds__(kBlock, Shape::NS > 4 ? 2 : sizeof(T) == 4 ? 3 : 4) void scan_rows(ScanParams p)
 {
     constexpr int GL = Shape::GL, NS = Shape::NS, NP = Shape::kStates, CB = Shape::kChannels, E = kElems;
     constexpr int K = kBlock * E / CB;                   // rows of a tile
@@ -41,6 +42,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 4 ? 3 : 2) void scan_rows(Scan
     __shared__ Pair dx[K][kRow];                         // d, d u
     __shared__ Pair bc[K][NP];
     __shared__ float ys[kWhole ? K : 1][kRow];
+    __shared__ float per_channel[kWhole ? 2 : 1][CB];    // bias of dt, skip
 
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const int slot = blockIdx.x / p.tiles;
@@ -78,18 +80,14 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 4 ? 3 : 2) void scan_rows(Scan
     T* out = kWhole ? sequence_base<T>(p.out, p.pieces, q) + (long long)q.row0 * p.out.row + ct.c0 : nullptr;
     const T* pb = sequence_base<T>(p.b, p.pieces, q) + (long long)q.row0 * p.b.row + ct.group * p.b_group;
     const T* pc = kWhole ? sequence_base<T>(p.c, p.pieces, q) + (long long)q.row0 * p.c.row + ct.group * p.c_group : nullptr;
-    float bias[E], skip[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const bool is = mine.col + e < ct.n;
-        bias[e] = p.dt_bias && is ? p.dt_bias[ct.c0 + mine.col + e] : 0.0f;
-        skip[e] = kWhole && p.skip && is ? p.skip[ct.c0 + mine.col + e] : 0.0f;
+    if (tid < CB) {
+        per_channel[0][tid] = p.dt_bias && tid < ct.n ? p.dt_bias[ct.c0 + tid] : 0.0f;
+        if (kWhole) per_channel[1][tid] = p.skip && tid < ct.n ? p.skip[ct.c0 + tid] : 0.0f;
     }
     // Channels behind the tile keep d = 0, d u = 0 throughout.
-    if (ct.n < CB) {
+    if (ct.n < CB)
         for (int i = tid; i < K * kRow; i += kBlock) dx[i / kRow][i % kRow] = Pair{0.0f, 0.0f};
-        __syncthreads();                                 // before the first tile's values go there
-    }
+    __syncthreads();                                     // before the first tile's values go there
 
     using Vec = RowVec<T, E>;
     Vec u, z, u_next, d_next, z_next;
@@ -113,12 +111,14 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 4 ? 3 : 2) void scan_rows(Scan
     auto stage = [&](int row) {
         u = u_next;
         z = z_next;
+        float v[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            float v = (float)d_next[e] + bias[e];
-            if (p.softplus) v = softplus(v);
-            dx[mine.row][mine.place(e)] = Pair{v, v * (float)u[e]};
-        }
+        for (int e = 0; e < E; ++e) v[e] = (float)d_next[e] + per_channel[0][mine.col + e];
+        if (p.softplus)
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = softplus(v[e]);
+#pragma unroll
+        for (int e = 0; e < E; ++e) dx[mine.row][mine.place(e)] = Pair{v[e], v[e] * (float)u[e]};
         if (row + mine.row >= q.n || mine.narrow) {
 #pragma unroll
             for (int e = 0; e < E; ++e)
@@ -160,10 +160,12 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 4 ? 3 : 2) void scan_rows(Scan
             }
 #pragma unroll
             for (int k = 0; k < kAhead; ++k) {
-                const float x = o.dv[k][1], b = o.w[k][m][0];
-                const float v[4] = {quad_lane<0>(b) * x, quad_lane<1>(b) * x, quad_lane<2>(b) * x, quad_lane<3>(b) * x};
+                RowVec<float, 4> v;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) e[k][i] = h[4 * m + i] = __builtin_fmaf(e[k][i], h[4 * m + i], v[i]);
+                for (int i = 0; i < 4; ++i) v[i] = e[k][i] * h[4 * m + i];
+                v = quad_outer(o.w[k][m][0], o.dv[k][1], v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[k][i] = h[4 * m + i] = v[i];
             }
             if (kWhole) {
                 if (m == 0) quad_dots<true>(y, c, e);
@@ -200,7 +202,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 4 ? 3 : 2) void scan_rows(Scan
         if (kWhole) {
             float o[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(skip[e], (float)u[e], ys[mine.row][mine.place(e)]);
+            for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(per_channel[1][mine.col + e], (float)u[e], ys[mine.row][mine.place(e)]);
             if (gated)
 #pragma unroll
                 for (int e = 0; e < E; ++e) o[e] *= silu((float)z[e]);
