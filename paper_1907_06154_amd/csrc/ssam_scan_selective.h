@@ -268,13 +268,15 @@ inline long long group_width(int groups, int states, long long apart) { return (
 
 // ---- sequences in pieces ------------------------------------------------------------------------------------------------
 // Rows of a piece, a multiple of 32, so that sequences x channel tiles x pieces come to about `blocks` blocks; one piece a sequence
-// where there are enough without.
-int scan_piece_rows(const ssam_sequences& q, int tiles, int blocks);
+// where `alone` sequences x channel tiles are there without.
+int scan_piece_rows(const ssam_sequences& q, int tiles, int blocks, int alone);
 
 // Turns what each piece adds to the state into the states between the pieces: `ends` holds [slot][channels][states], `sums`
 // [slot][channels] the time steps of a piece added up (its decay is exp(a * sum)).
-//   forward:  ends[slot] becomes the state before the piece, from `initial` (zeros without)
-//   backward: ends[slot] becomes what reaches the piece's last row from behind, from `initial` (the gradient of the last state)
+//   forward:  ends[slot] becomes the state behind the piece, from `initial` (zeros without) before the first; `initial`
+//             itself goes into the last piece's, for the first
+//   backward: ends[slot] becomes what the piece lets out at its first row, from `initial` (the gradient of the last state) behind the
+//             last piece; not for the first
 int launch_join(const Pieces& p, float* ends, const float* sums, const float* a, const float* initial, int channels, int states, bool backward,
                 hipStream_t stream);
 

@@ -16,13 +16,14 @@ namespace {
 
 constexpr int kElems = 8;                    // values of a tile that a thread loads, and stores
 constexpr int kBlocks = 1024;                // four blocks of four waves per compute unit
+constexpr int kAlone = 256;                  // sequences x channel tiles that are enough without cutting (4 x 16384 rows of 4096 channels: 435 us, cut 478)
 
 struct ScanParams {
     Pieces pieces;
     ssam_rows in, dt, gate, out, b, c;
     long long b_group, c_group;
-    const float *a, *skip, *dt_bias, *state, *starts;   // starts: [slot][channels][states], the state before each piece
-    float *final, *marks, *ends, *sums;
+    const float *a, *skip, *dt_bias, *state;
+    float *final, *marks, *ends, *sums;   // ends: [slot][channels][states], sums: [slot][channels]
     Pieces mark_slots;
     int channels, states, group_channels, per_group, tiles, softplus;
 };
@@ -62,7 +63,9 @@ __global__ __launch_bounds__(kBlock, Shape::NS > 4 ? 2 : sizeof(T) == 4 ? 3 : 4)
     float a2[NS], h[NS];
     load_rates<NS>(p.a + cell, n0, p.states, live, a2);
     if (!kWhole) load_states<NS>(nullptr, 0, 0, false, h);
-    else if (p.starts) load_states<NS>(p.starts + slot * plane + cell, n0, p.states, live, h);
+    else if (q.row0 > 0) load_states<NS>(p.ends + (slot - 1) * plane + cell, n0, p.states, live, h);
+    else if (q.n < q.len)   // not from p.state: the last piece's block may have stored p.final over it by now
+        load_states<NS>(p.ends + (slot + (q.len - 1) / p.pieces.piece) * plane + cell, n0, p.states, live, h);
     else load_states<NS>(p.state + q.seq * plane + cell, n0, p.states, live && p.state, h);
     float sum = 0.0f;
     float* marks = nullptr;
@@ -217,38 +220,41 @@ __global__ __launch_bounds__(kBlock, Shape::NS > 4 ? 2 : sizeof(T) == 4 ? 3 : 4)
     }
 }
 
-// One thread per sequence, channel and state walks the pieces; their values are requested eight pieces at a time.
+// One thread per sequence, channel and state walks the pieces; their values are requested 32 pieces at a time.
 template <bool kBackward>
 __global__ __launch_bounds__(kBlock) void join_pieces(Pieces pc, float* ends, const float* __restrict__ sums, const float* __restrict__ a,
                                                       const float* initial, int channels, int states, unsigned blocks_each)
 {
     const int seq = blockIdx.x / blocks_each;
-    const long long plane = (long long)channels * states;
-    const long long i = (long long)(blockIdx.x % blocks_each) * kBlock + threadIdx.x;
-    if (i >= plane) return;
     int begin, len;
     span_of(pc, seq, begin, len);
-    const long long slot0 = pc.begin ? first_slot(pc, seq) : (long long)seq * pc.per;
     const int n = len > pc.piece ? (len + pc.piece - 1) / pc.piece : 1;
+    const long long plane = (long long)channels * states;
+    const long long i = (long long)(blockIdx.x % blocks_each) * kBlock + threadIdx.x;
+    if (n == 1 || i >= plane) return;
+    const long long slot0 = pc.begin ? first_slot(pc, seq) : (long long)seq * pc.per;
     const int c = (int)(i / states);
     const float a2 = decay_rate(a[i]);
     float h = initial ? initial[seq * plane + i] : 0.0f;
-    constexpr int kAtOnce = 8;
-    for (int k = 0; k < n; k += kAtOnce) {
+    if (!kBackward) ends[(slot0 + n - 1) * plane + i] = h;
+    constexpr int kAtOnce = 32;
+    for (int k = 0; k < n - 1; k += kAtOnce) {          // what the last adds nothing follows
         float e[kAtOnce], s[kAtOnce];
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
-            const bool there = k + j < n - 1;          // nothing follows the last
+            const bool there = k + j < n - 1;
             const long long at = slot0 + (kBackward ? n - 1 - (k + j) : k + j);
             e[j] = there ? ends[at * plane + i] : 0.0f;
             s[j] = there ? sums[at * channels + c] : 0.0f;
         }
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
-            if (k + j >= n) break;
-            ends[(slot0 + (kBackward ? n - 1 - (k + j) : k + j)) * plane + i] = h;
-            h = __builtin_fmaf(exp2_fast(a2 * s[j]), h, e[j]);
+            if (k + j >= n - 1) break;
+            e[j] = h = __builtin_fmaf(exp2_fast(a2 * s[j]), h, e[j]);
         }
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j)
+            if (k + j < n - 1) ends[(slot0 + (kBackward ? n - 1 - (k + j) : k + j)) * plane + i] = e[j];
     }
 }
 
@@ -263,7 +269,7 @@ Plan plan_of(const ssam_scan_selective_args& a)
 {
     Plan p;
     p.tiles = tiles_per_group(a.channels, a.states, a.groups) * a.groups;
-    p.piece = scan_piece_rows(a.seq, p.tiles, kBlocks);
+    p.piece = scan_piece_rows(a.seq, p.tiles, kBlocks, kAlone);
     p.slots = piece_slots(a.seq, p.piece);
     p.cut = a.seq.rows > p.piece;
     p.ends = p.cut ? (size_t)p.slots * a.channels * a.states * sizeof(float) : 0;
@@ -389,13 +395,18 @@ __global__ __launch_bounds__(kBlock) void scan_step(ScanStepParams p)
 
 }  // namespace
 
-int scan_piece_rows(const ssam_sequences& q, int tiles, int blocks)
+int scan_piece_rows(const ssam_sequences& q, int tiles, int blocks, int alone)
 {
-    constexpr long long kShortest = 64, kLongest = 1 << 30;
-    const long long total = q.d_begin ? q.rows : (long long)q.rows * q.sequences;
-    if (q.d_begin) blocks += blocks / 2;   // packed sequences end inside pieces: shorter ones even that out (37 in 8191 rows: 140 -> 129 us; equal ones lose by it, 141 -> 149)
+    constexpr long long kShortest = 32;   // shorter ones wait for the join (369 rows of 518 channels forward and back: 69 us, with 64: 84)
+    constexpr long long kWhole = 128;     // not worth the join (128 rows of 4096 channels: 17.6 us, cut 18.7; 256 rows: 30.7, cut 22.9)
+    constexpr long long kLongest = 1 << 30;
+    const long long total = q.d_begin ? q.rows : (long long)q.rows * q.sequences, whole = (long long)q.sequences * tiles;
+    // Packed sequences end inside pieces: shorter ones even that out where there are few (37 in 8191 rows: 119 us, 139 without),
+    // and are too many where there are not (64 in 8192 rows of 4096 channels: 237, 206 without).
+    if (q.d_begin && whole < blocks) blocks += blocks / 2;
     long long piece = (total * tiles + blocks - 1) / blocks;
-    if (!q.d_begin && (long long)q.sequences * tiles >= blocks / 2) piece = q.rows;
+    if (q.rows <= kWhole) piece = kWhole;
+    else if (!q.d_begin && whole >= alone) piece = q.rows;
     piece = (piece + 31) / 32 * 32;
     return (int)(piece < kShortest ? kShortest : piece > kLongest ? kLongest : piece);
 }
@@ -500,7 +511,6 @@ int ssam_scan_selective(const ssam_scan_selective_args* a, void* hip_stream)
                 p.sums = reinterpret_cast<float*>(static_cast<char*>(a->d_work) + plan.ends);
                 hipLaunchKernelGGL((scan_rows<T, S, false>), dim3((unsigned)blocks), dim3(kBlock), 0, st, p);
                 if (int e = launch_join(p.pieces, p.ends, p.sums, a->d_a, a->d_state, a->channels, a->states, false, st)) return e;
-                p.starts = p.ends;
             }
             hipLaunchKernelGGL((scan_rows<T, S, true>), dim3((unsigned)blocks), dim3(kBlock), 0, st, p);
             return launched();

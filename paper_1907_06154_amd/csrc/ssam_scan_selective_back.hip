@@ -16,7 +16,8 @@ namespace ssam {
 namespace {
 
 constexpr int kTile = SSAM_MARK_ROWS;
-constexpr int kBackBlocks = 512;      // two blocks of four waves per compute unit: what 256 registers leave
+constexpr int kBackBlocks = 1024;     // two rounds of the two blocks per compute unit that 256 registers leave
+constexpr int kBackAlone = 512;       // sequences x channel tiles that are enough without cutting (8 x 8192 rows of 2048 channels, 256 of them: 505 us cut, 551 whole)
 
 struct BackParams {
     Pieces pieces, mark_slots;
@@ -29,7 +30,7 @@ struct BackParams {
     float* part_bc;                   // [tile of the group][row][group][2][states]
     float* part_param;                // [slot][channels x states, channels (skip), channels (bias)]
     long long rows_total;
-    int channels, states, groups, group_channels, per_group, tiles, softplus, cut;
+    int channels, states, groups, group_channels, per_group, tiles, softplus;
 };
 
 template <int CTRL>
@@ -132,8 +133,8 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
     load_rates<NS>(p.a + cell, n0, p.states, live, a2);
     const bool last = q.row0 + q.n >= q.len;
     if (!kWhole) load_states<NS>(nullptr, 0, 0, false, g);
-    else if (p.cut) load_states<NS>(p.ends + slot * plane + cell, n0, p.states, live, g);
-    else load_states<NS>(p.grad_final + q.seq * plane + cell, n0, p.states, live && p.grad_final && last, g);
+    else if (!last) load_states<NS>(p.ends + (slot + 1) * plane + cell, n0, p.states, live, g);
+    else load_states<NS>(p.grad_final + q.seq * plane + cell, n0, p.states, live && p.grad_final, g);
 #pragma unroll
     for (int i = 0; i < NS; ++i) da[i] = 0.0f;
     float sum = 0.0f;
@@ -503,7 +504,7 @@ BackPlan plan_of(const ssam_scan_selective_backward_args& a)
     const int wide = a.states <= 8 ? 128 : 64;
     p.per_group = (a.channels / a.groups + wide - 1) / wide;
     p.tiles = p.per_group * a.groups;
-    p.piece = scan_piece_rows(a.seq, p.tiles, kBackBlocks);
+    p.piece = scan_piece_rows(a.seq, p.tiles, kBackBlocks, kBackAlone);
     p.slots = piece_slots(a.seq, p.piece);
     p.rows_total = a.seq.d_begin ? a.seq.rows : (long long)a.seq.rows * a.seq.sequences;
     p.cut = a.seq.rows > p.piece;
@@ -607,7 +608,6 @@ int ssam_scan_selective_backward(const ssam_scan_selective_backward_args* a, voi
     p.per_group = plan.per_group;
     p.tiles = plan.tiles;
     p.softplus = a->softplus != 0;
-    p.cut = plan.cut;
     const long long blocks = plan.slots * plan.tiles;
     const long long join = (plane / 4 + kBlock - 1) / kBlock * a->seq.sequences;
     const long long param_blocks = (plane / 4 + 2LL * a->channels + kWave - 1) / kWave;

@@ -180,9 +180,9 @@ def test_scan_selective_plans(L):
     work = lambda **c: size(L, "ssam_scan_selective_workspace_bytes", scan(**c))  # noqa: E731
     assert marks() == 2 and marks(seq=Seq(3, 16, None, None)) == 3 and marks(seq=Seq(3, 17, None, None)) == 6 and marks(seq=Seq(3, 0, None, None)) == 3
     assert marks(seq=Seq(3, 33, at(20), at(20) + 4)) == 5 and marks(dtype=9) == 0
-    assert work() == 0 and work(seq=Seq(1, 64, None, None)) == 0
+    assert work() == 0 and work(seq=Seq(1, 128, None, None)) == 0
     # few sequences are cut into pieces: their states and their time steps' sums; many are not
-    assert work(groups=1, seq=Seq(1, 65, None, None)) == 2 * (64 * 16 + 64) * 4
+    assert work(groups=1, seq=Seq(1, 129, None, None)) == 5 * (64 * 16 + 64) * 4
     assert work(groups=1, channels=4096, seq=Seq(16, 4096, None, None)) == 0
     assert work(states=77) == 0 and L.ssam_scan_selective_workspace_bytes(None) == 0
 
