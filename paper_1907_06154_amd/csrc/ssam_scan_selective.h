@@ -10,7 +10,6 @@
 
 namespace ssam {
 
-
 template <int GL_, int NS_>
 struct ScanShape {
     static constexpr int GL = GL_, NS = NS_;
@@ -31,23 +30,9 @@ __device__ __forceinline__ float quad_lane(float v)
 {
     return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), Q * 0x55, 0xf, 0xf, true));
 }
-// The value of the lane N to the left, around the row of 16.
-template <int N>
-__device__ __forceinline__ float row_rotate(float v)
-{
-    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x120 + N, 0xf, 0xf, true));
-}
-// Sum over the lane groups of a channel, in every one of them (the same bits in each: both steps add two values).
-template <int GL>
-__device__ __forceinline__ float group_sum(float v)
-{
-    if (GL >= 2) v += row_rotate<8>(v);
-    if (GL >= 4) v += row_rotate<4>(v);
-    return v;
-}
-
 // v[i] + b(lane i of the quad) x, i = 0 .. 3: the 4x4 matrix instruction with K = 1, sixteen outer products side by side whose lanes lie
-// as the quads do.  It takes 8 cycles where four products by DPP take 16 (full fp32; 1 x 4096 rows 140 -> 136 us).
+// as the quads do.  It takes 8 cycles where four products by DPP take 16 (full fp32; 1 x 4096 rows 140 -> 136 us, the
+// gradients of 4 x 2048 rows of 2048 channels 501 -> 478).
 __device__ __forceinline__ RowVec<float, 4> quad_outer(float b, float x, RowVec<float, 4> v) { return __builtin_amdgcn_mfma_f32_4x4x1f32(b, x, v, 0, 0, 0); }
 
 // Four rows' y += c0 h0 + c1 h1 + c2 h2 + c3 h3 (kFirst: y = ..), with cQ the value of lane Q of the quad: multiply-adds that take it by
@@ -80,7 +65,8 @@ __device__ __forceinline__ void quad_dots(float (&y)[4], const float (&c)[4], co
 #undef SSAM_DOT
 #undef SSAM_INPUTS
 }
-// group_sum of four values that quad_dots made.
+// Sums over the lane groups of a channel, in every one of them (the same bits in each: both steps add two values), of four values that
+// quad_dots made.
 template <int GL>
 __device__ __forceinline__ void group_sums(float (&y)[4])
 {
@@ -94,8 +80,8 @@ __device__ __forceinline__ void group_sums(float (&y)[4])
 #undef SSAM_TURN
 }
 
-// One row's sum of cQ h[Q], and g[Q] += cQ x: the same for single rows.
-__device__ __forceinline__ float quad_dot(float c, float h0, float h1, float h2, float h3)
+// One row's sum of cQ h[Q].  Where the matrix instruction made h, `behind` is something the compiler computed from h: it has waited then.
+__device__ __forceinline__ float quad_dot(float c, float h0, float h1, float h2, float h3, float behind)
 {
     float y;
     asm("s_nop 1\n\t"
@@ -104,20 +90,10 @@ __device__ __forceinline__ float quad_dot(float c, float h0, float h1, float h2,
         "v_fmac_f32_dpp %0, %1, %4 quad_perm:[2,2,2,2] row_mask:0xf bank_mask:0xf\n\t"
         "v_fmac_f32_dpp %0, %1, %5 quad_perm:[3,3,3,3] row_mask:0xf bank_mask:0xf"
         : "=&v"(y)
-        : "v"(c), "v"(h0), "v"(h1), "v"(h2), "v"(h3));
+        : "v"(c), "v"(h0), "v"(h1), "v"(h2), "v"(h3), "v"(behind));
     return y;
 }
-__device__ __forceinline__ void quad_add(float& g0, float& g1, float& g2, float& g3, float c, float x)
-{
-    asm("s_nop 1\n\t"
-        "v_fmac_f32_dpp %0, %4, %5 quad_perm:[0,0,0,0] row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %1, %4, %5 quad_perm:[1,1,1,1] row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %2, %4, %5 quad_perm:[2,2,2,2] row_mask:0xf bank_mask:0xf\n\t"
-        "v_fmac_f32_dpp %3, %4, %5 quad_perm:[3,3,3,3] row_mask:0xf bank_mask:0xf"
-        : "+&v"(g0), "+&v"(g1), "+&v"(g2), "+&v"(g3)
-        : "v"(c), "v"(x));
-}
-// group_sum of two values, of which these blocks may have made either.
+// Two values' sums over the lane groups of a channel; these blocks may have made either.
 template <int GL>
 __device__ __forceinline__ void group_sums(float& r, float& s)
 {

@@ -256,9 +256,9 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
                         for (int i = 0; i < 4; ++i) e[k][i] = exp2_fast(d4[k] * a2[4 * m + i]);
 #pragma unroll
                     for (int k = 3; k >= 0; --k) {
-                        quad_add(g[4 * m], g[4 * m + 1], g[4 * m + 2], g[4 * m + 3], c4[k][m], dy4[k]);
+                        const RowVec<float, 4> gv = quad_outer(c4[k][m], dy4[k], RowVec<float, 4>{g[4 * m], g[4 * m + 1], g[4 * m + 2], g[4 * m + 3]});
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) g[4 * m + i] *= e[k][i];
+                        for (int i = 0; i < 4; ++i) g[4 * m + i] = gv[i] * e[k][i];
                     }
                 }
 #pragma unroll
@@ -287,7 +287,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
 #pragma unroll
                         for (int m = 0; m < NS / 4; ++m) {
                             const float b = bc[t][pairs + m][0];
-                            const float v[4] = {quad_lane<0>(b) * d[1], quad_lane<1>(b) * d[1], quad_lane<2>(b) * d[1], quad_lane<3>(b) * d[1]};
+                            const RowVec<float, 4> v = quad_outer(b, d[1], RowVec<float, 4>{});
 #pragma unroll
                             for (int i = 0; i < 4; ++i) h[4 * m + i] = __builtin_fmaf(exp2_fast(d[0] * a2[4 * m + i]), h[4 * m + i], v[i]);
                         }
@@ -299,7 +299,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
 #pragma unroll
                     for (int m = 0; m < NS / 4; ++m) {
                         const float b = w[k][m][0], x = dv[k][1];
-                        const float v[4] = {quad_lane<0>(b) * x, quad_lane<1>(b) * x, quad_lane<2>(b) * x, quad_lane<3>(b) * x};
+                        const RowVec<float, 4> v = quad_outer(b, x, RowVec<float, 4>{});
 #pragma unroll
                         for (int i = 4 * m; i < 4 * m + 4; ++i) {
                             as[k][i] = exp2_fast(dv[k][0] * a2[i]);
@@ -339,14 +339,18 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
                         const int step = (kKept - 1 - k) * (NS / 4) + m;
                         if (step > 0) across.take(step - 1, terms_of);       // added up below: their reads pass this step's arithmetic
                         float *gm = g + 4 * m, vb[4], vc[4];
-                        quad_add(gm[0], gm[1], gm[2], gm[3], w[k][m][1], dyr[k]);
-                        const float sm = quad_dot(w[k][m][0], gm[0], gm[1], gm[2], gm[3]);
+                        const RowVec<float, 4> gv = quad_outer(w[k][m][1], dyr[k], RowVec<float, 4>{gm[0], gm[1], gm[2], gm[3]});
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            gm[j] = gv[j];
+                            vc[j] = hs[k][4 * m + j] * dyr[k];
+                            vb[j] = gm[j] * dv[k][1];
+                        }
+                        const float sm = quad_dot(w[k][m][0], gm[0], gm[1], gm[2], gm[3], vb[0]);
                         s = m ? s + sm : sm;
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const int i = 4 * m + j;
-                            vc[j] = hs[k][i] * dyr[k];
-                            vb[j] = g[i] * dv[k][1];
                             g[i] *= as[k][i];                      // what reaches the row before
                             const float qi = g[i] * before[i];
                             da[i] = __builtin_fmaf(dv[k][0], qi, da[i]);
