@@ -80,17 +80,17 @@ __device__ __forceinline__ void group_sums(float (&y)[4])
 #undef SSAM_TURN
 }
 
-// One row's sum of cQ h[Q].  Where the matrix instruction made h, `behind` is something the compiler computed from h: it has waited then.
-__device__ __forceinline__ float quad_dot(float c, float h0, float h1, float h2, float h3, float behind)
+// One row's sum of cQ h[Q]; h may come from the matrix instruction, hence five wait states.
+__device__ __forceinline__ float quad_dot(float c, float h0, float h1, float h2, float h3)
 {
     float y;
-    asm("s_nop 1\n\t"
+    asm("s_nop 4\n\t"
         "v_mul_f32_dpp %0, %1, %2 quad_perm:[0,0,0,0] row_mask:0xf bank_mask:0xf\n\t"
         "v_fmac_f32_dpp %0, %1, %3 quad_perm:[1,1,1,1] row_mask:0xf bank_mask:0xf\n\t"
         "v_fmac_f32_dpp %0, %1, %4 quad_perm:[2,2,2,2] row_mask:0xf bank_mask:0xf\n\t"
         "v_fmac_f32_dpp %0, %1, %5 quad_perm:[3,3,3,3] row_mask:0xf bank_mask:0xf"
         : "=&v"(y)
-        : "v"(c), "v"(h0), "v"(h1), "v"(h2), "v"(h3), "v"(behind));
+        : "v"(c), "v"(h0), "v"(h1), "v"(h2), "v"(h3));
     return y;
 }
 // Two values' sums over the lane groups of a channel; these blocks may have made either.

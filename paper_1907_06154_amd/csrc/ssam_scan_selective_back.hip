@@ -346,7 +346,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
                             vc[j] = hs[k][4 * m + j] * dyr[k];
                             vb[j] = gm[j] * dv[k][1];
                         }
-                        const float sm = quad_dot(w[k][m][0], gm[0], gm[1], gm[2], gm[3], vb[0]);
+                        const float sm = quad_dot(w[k][m][0], gm[0], gm[1], gm[2], gm[3]);
                         s = m ? s + sm : sm;
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
