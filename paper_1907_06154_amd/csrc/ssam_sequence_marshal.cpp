@@ -258,7 +258,7 @@ PyObject* conv1d(PyObject*, PyObject* const* v, Py_ssize_t n)
 }
 
 // conv1d_backward(d_grad, d_in, weight, bias, silu, d_state, d_grad_final, starts, lengths, state_grad, d_work, stream)
-//     -> (x, weight, bias, state, workspace)
+//     -> (x, weight, bias, state)
 PyObject* conv1d_backward(PyObject*, PyObject* const* v, Py_ssize_t n)
 {
     if (!arity(n, 12)) return nullptr;
@@ -286,7 +286,7 @@ PyObject* conv1d_backward(PyObject*, PyObject* const* v, Py_ssize_t n)
             a.work_bytes = work.nbytes();
         }
         call(entry.conv1d_backward, a, v[11], "ssam_conv1d_backward");
-        return Py_BuildValue("(NNNNN)", wrap(gx), wrap(gw), wrap(gb), wrap(gs), wrap(work));
+        return Py_BuildValue("(NNNN)", wrap(gx), wrap(gw), wrap(gb), wrap(gs));
     });
 }
 
@@ -419,7 +419,7 @@ PyObject* scan_marks(PyObject*, PyObject* const* v, Py_ssize_t n)
 }
 
 // scan(d_in, d_dt, a, b, c, skip, gate, dt_bias, softplus, d_state, d_final, d_marks, starts, lengths, d_out, d_work, stream)
-//     -> (d_out, workspace)
+//     -> d_out
 PyObject* scan(PyObject*, PyObject* const* v, Py_ssize_t n)
 {
     if (!arity(n, 17)) return nullptr;
@@ -441,8 +441,11 @@ PyObject* scan(PyObject*, PyObject* const* v, Py_ssize_t n)
             s.work_bytes = work.nbytes();
         }
         call(entry.scan, s, v[16], "ssam_scan_selective");
-        if (given) Py_INCREF(v[14]);
-        return Py_BuildValue("(NN)", given ? v[14] : wrap(out), wrap(work));
+        if (given) {
+            Py_INCREF(v[14]);
+            return v[14];
+        }
+        return wrap(out);
     });
 }
 
@@ -465,7 +468,7 @@ PyObject* scan_bytes(PyObject*, PyObject* const* v, Py_ssize_t n)
 }
 
 // scan_backward(d_grad, d_in, d_dt, a, b, c, skip, gate, dt_bias, softplus, d_marks, d_grad_final, starts, lengths, state_grad, d_work,
-//     stream) -> (x, dt, a, b, c, skip, gate, dt_bias, state, workspace)
+//     stream) -> (x, dt, a, b, c, skip, gate, dt_bias, state)
 PyObject* scan_backward(PyObject*, PyObject* const* v, Py_ssize_t n)
 {
     if (!arity(n, 17)) return nullptr;
@@ -502,7 +505,7 @@ PyObject* scan_backward(PyObject*, PyObject* const* v, Py_ssize_t n)
             s.work_bytes = work.nbytes();
         }
         call(entry.scan_backward, s, v[16], "ssam_scan_selective_backward");
-        return Py_BuildValue("(NNNNNNNNNN)", wrap(gx), wrap(gdt), wrap(ga), wrap(gb), wrap(gc), wrap(gk), wrap(gz), wrap(gd), wrap(gs), wrap(work));
+        return Py_BuildValue("(NNNNNNNNN)", wrap(gx), wrap(gdt), wrap(ga), wrap(gb), wrap(gc), wrap(gk), wrap(gz), wrap(gd), wrap(gs));
     });
 }
 

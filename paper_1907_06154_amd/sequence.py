@@ -5,7 +5,8 @@ fallback, as in binding.py.
 Tensors of rows are [rows, channels] (one sequence, or several packed one behind the other: `starts`, a device tensor of
 sequences + 1 offsets) or [sequences, rows, channels] (`lengths`: how many rows of each count).  Rows and sequences may have
 any stride, channels are contiguous.  A result that is allocated here holds zeros in rows that belong to no sequence; one that
-is passed in keeps what it held there.  The kernels run on the device of their tensors, on its current stream or on `stream`.
+is passed in keeps what it held there.  The kernels run on the device of their tensors, on its current stream or on `stream`;
+what a call allocates belongs to that stream, which orders its first use and its reuse.
 """
 from __future__ import annotations
 
@@ -72,16 +73,15 @@ def _run(name: str, like, stream, args):
     if not isinstance(like, _torch.Tensor) or not like.is_cuda:
         return f(*args, 0)                       # refused there
     index = like.get_device()
+    if stream is not None:
+        if stream.device != like.device:
+            raise ValueError(f"stream must belong to {like.device}, not {stream.device}")
+        with _torch.cuda.stream(stream):         # results and workspaces too: made on another stream they could still be in use there
+            return f(*args, stream.cuda_stream)
     if _several and index != _torch.cuda.current_device():
         with _torch.cuda.device(index):
-            return f(*args, stream.cuda_stream if stream is not None else _raw_stream(index))
-    return f(*args, stream.cuda_stream if stream is not None else _raw_stream(index))
-
-
-def _keep(work, stream):
-    """A workspace dies when the call returns, while kernels that use it may be queued on another stream than the allocator's."""
-    if work is not None and stream is not None:
-        work.record_stream(stream)
+            return f(*args, _raw_stream(index))
+    return f(*args, _raw_stream(index))
 
 
 def ssam_conv1d(d_in, weight, bias=None, silu: bool = False, d_state=None, d_final=None, starts=None, lengths=None, d_out=None, stream=None):
@@ -95,9 +95,8 @@ def ssam_conv1d_backward(d_grad, d_in, weight, bias=None, silu: bool = False, d_
                          state_grad: bool = False, d_work=None, stream=None) -> Conv1dGrads:
     """Gradients of ssam_conv1d for d_grad, the gradient of its result, and d_grad_final, that of its d_final (none if absent).
     weight's and bias's come in their own type; state_grad: that of d_state (or of the zeros in its place) too."""
-    *grads, work = _run("conv1d_backward", d_in, stream, (d_grad, d_in, weight, bias, silu, d_state, d_grad_final, starts, lengths, state_grad, d_work))
-    _keep(work, stream)
-    return Conv1dGrads(*grads)
+    return Conv1dGrads(*_run("conv1d_backward", d_in, stream,
+                             (d_grad, d_in, weight, bias, silu, d_state, d_grad_final, starts, lengths, state_grad, d_work)))
 
 
 def ssam_conv1d_step(d_in, weight, d_state, bias=None, silu: bool = False, slots=None, d_out=None, stream=None):
@@ -127,9 +126,7 @@ def ssam_scan_selective(d_in, d_dt, a, b, c, skip=None, gate=None, dt_bias=None,
     softplus or as it is.  d_in, d_dt, gate: rows of channels; b, c: rows of [groups, states], channel k using group
     k // (channels // groups); a [channels, states], skip, dt_bias [channels], d_state, d_final [sequences, channels, states]: float32.
     d_final may be d_state.  d_marks (from ssam_scan_selective_marks) keeps what the gradients need."""
-    out, work = _run("scan", d_in, stream, (d_in, d_dt, a, b, c, skip, gate, dt_bias, softplus, d_state, d_final, d_marks, starts, lengths, d_out, d_work))
-    _keep(work, stream)
-    return out
+    return _run("scan", d_in, stream, (d_in, d_dt, a, b, c, skip, gate, dt_bias, softplus, d_state, d_final, d_marks, starts, lengths, d_out, d_work))
 
 
 def ssam_scan_selective_backward(d_grad, d_in, d_dt, a, b, c, d_marks, skip=None, gate=None, dt_bias=None, softplus: bool = False,
@@ -138,10 +135,8 @@ def ssam_scan_selective_backward(d_grad, d_in, d_dt, a, b, c, d_marks, skip=None
     """Gradients of ssam_scan_selective for d_grad, the gradient of its result, and d_grad_final, that of its d_final (none if absent),
     from the marks the forward call left.  Rows' gradients come in d_in's type, the parameters' in float32; state_grad: that of
     d_state (or of the zeros in its place) too."""
-    *grads, work = _run("scan_backward", d_in, stream, (d_grad, d_in, d_dt, a, b, c, skip, gate, dt_bias, softplus, d_marks, d_grad_final, starts, lengths,
-                                                        state_grad, d_work))
-    _keep(work, stream)
-    return ScanSelectiveGrads(*grads)
+    return ScanSelectiveGrads(*_run("scan_backward", d_in, stream, (d_grad, d_in, d_dt, a, b, c, skip, gate, dt_bias, softplus, d_marks, d_grad_final,
+                                                                    starts, lengths, state_grad, d_work)))
 
 
 def ssam_scan_selective_step(d_in, d_dt, a, b, c, d_state, skip=None, gate=None, dt_bias=None, softplus: bool = False, slots=None, d_out=None,

@@ -511,6 +511,36 @@ def test_on_another_stream():
     assert all(torch.equal(o, here) for o in outs)
 
 
+def test_what_a_call_allocates_belongs_to_its_stream():
+    """Results start as zeros where rows may belong to no sequence: filled on the call's stream, not behind the current one's work."""
+    D, N, T = 64, 16, 500
+    g = torch.Generator().manual_seed(8)
+    x, dt, dy = (randn(g, T, D) for _ in range(3))
+    b, c = randn(g, T, 1, N), randn(g, T, 1, N)
+    a, w = -(torch.rand(D, N, generator=g) + 0.1).cuda(), randn(g, D, 4)
+    starts = torch.tensor([0, 200, 490], dtype=torch.int32, device="cuda")
+    marks = ssam.ssam_scan_selective_marks(x, a, starts=starts)
+    pool, slots = torch.zeros(3, 3, D, device="cuda"), torch.tensor([0, 2], dtype=torch.int32, device="cuda")
+
+    def calls(stream):
+        y = ssam.ssam_scan_selective(x, dt, a, b, c, softplus=True, d_marks=marks, starts=starts, stream=stream)
+        s = ssam.ssam_scan_selective_backward(dy, x, dt, a, b, c, marks, softplus=True, starts=starts, stream=stream)
+        return [y, s.x, s.b, s.a, ssam.ssam_conv1d(x, w, starts=starts, stream=stream),
+                *ssam.ssam_conv1d_backward(dy, x, w, starts=starts, stream=stream)[:2],
+                ssam.ssam_conv1d_step(x[:2], w, pool.clone() if stream is None else pools, slots=slots, stream=stream)]
+
+    want = calls(None)
+    pools = pool.clone()
+    heavy = torch.ones(8192, 8192, device="cuda")
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    for _ in range(4):
+        heavy = heavy @ heavy * 1e-4                     # milliseconds of the current stream's
+    got = calls(other)
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
 def test_infinities_stay_in_their_sequence_and_channel():
     """A NaN or an infinity in one channel of one sequence, or in rows of no sequence, reaches nothing else."""
     D, N = 64, 16
