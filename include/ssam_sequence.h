@@ -101,6 +101,7 @@ int ssam_conv1d_step(const ssam_conv1d_step_args *args, void *hip_stream);
  * group contiguous, b_group / c_group elements from one group to the next.  a: [channels][states]; skip, dt_bias:
  * [channels] or NULL; d_state, d_final: [sequences][channels][states], the state before the first and after the last row
  * (zeros / not stored where NULL; d_final may be d_state); all of these fp32, contiguous.
+ * Of sequences of more than one row, rows lie at most 2^24 elements apart (SSAM_ERR_DIM), here and for the gradients.
  * d_marks (NULL: not wanted): the state before rows 0, 16, 32 .. of every sequence, what ssam_scan_selective_backward
  * starts from; ssam_scan_selective_marks(args) entries of [channels][states] floats.
  * d_work: ssam_scan_selective_workspace_bytes(args) bytes, 16-byte aligned (NULL where that is 0).
@@ -123,7 +124,8 @@ long long ssam_scan_selective_marks(const ssam_scan_selective_args *args);   /* 
 /* Gradients of ssam_scan_selective, from the same inputs and its marks.  grad_out: gradient of its result;
  * d_grad_final (may be NULL): of its d_final.  grad_in, grad_dt, grad_gate, grad_b, grad_c are in dtype (grad_b and
  * grad_c contiguous within a row, [groups][states]), the others fp32 in the layout of what they belong to; each may be
- * absent (NULL).  d_grad_dt_bias is the sum of grad_dt over the rows, d_grad_state the gradient of d_state.
+ * absent (NULL).  d_grad_dt_bias is the sum of grad_dt over the rows, d_grad_state the gradient of d_state.  groups x
+ * states must be below 2^27 (SSAM_ERR_DIM).
  * d_work: ssam_scan_selective_backward_workspace_bytes(args) bytes, 16-byte aligned. */
 typedef struct {
     int dtype, channels, states, groups, softplus;

@@ -70,7 +70,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS > 4 ? 2 : sizeof(T) == 4 ? 3 : 4)
     float sum = 0.0f;
     float* marks = nullptr;
     if (kWhole && p.marks) {
-        const int s0 = p.mark_slots.begin ? first_slot(p.mark_slots, q.seq) : q.seq * p.mark_slots.per;
+        const long long s0 = p.mark_slots.begin ? first_slot(p.mark_slots, q.seq) : (long long)q.seq * p.mark_slots.per;
         marks = p.marks + (s0 + q.row0 / SSAM_MARK_ROWS) * plane + cell;
     }
 
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS > 4 ? 2 : sizeof(T) == 4 ? 3 : 4)
             if (kWhole) c_next[e] = c0[r * (unsigned)p.c.row + n];
         }
     };
-    // Rows behind the piece get d = 0, d u = 0: the state passes them unchanged.
+    // Rows behind the piece get d = 0, d u = 0, b = 0: the state passes them unchanged, an infinite one too.
     auto stage = [&](int row) {
         u = u_next;
         z = z_next;
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS > 4 ? 2 : sizeof(T) == 4 ? 3 : 4)
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
             const int i = tid + e * kBlock, n = i % NP;
-            const bool is = n < p.states;
+            const bool is = n < p.states && row + i / NP < q.n;
             if (kPairs * kBlock <= K * NP || i < K * NP)
                 bc[i / NP][pair_place<Shape>(n)] = Pair{is ? (float)b_next[e] : 0.0f, kWhole && is ? (float)c_next[e] : 0.0f};
         }

@@ -17,6 +17,7 @@ namespace {
 
 constexpr int kTile = SSAM_MARK_ROWS;
 constexpr int kBackBlocks = 1024;     // two rounds of the two blocks per compute unit that 256 registers leave
+constexpr long long kMaxGroupStates = 1 << 27;   // groups x states: offsets in a tile's rows of both then have 32 bits
 constexpr int kBackAlone = 512;       // sequences x channel tiles that are enough without cutting (8 x 8192 rows of 2048 channels, 256 of them: 505 us cut, 551 whole)
 
 struct BackParams {
@@ -140,7 +141,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
     float sum = 0.0f;
     const float* marks = nullptr;
     if (kWhole) {
-        const int s0 = p.mark_slots.begin ? first_slot(p.mark_slots, q.seq) : q.seq * p.mark_slots.per;
+        const long long s0 = p.mark_slots.begin ? first_slot(p.mark_slots, q.seq) : (long long)q.seq * p.mark_slots.per;
         marks = p.marks + (s0 + q.row0 / K) * plane + cell;
     }
 
@@ -205,7 +206,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
     if (tiles > 0) request((tiles - 1) * K);
     for (int tile = tiles - 1; tile >= 0; --tile) {
         const int row = tile * K;
-        const bool behind = row + mine.row >= q.n;       // a row behind the piece: d = 0, dy = 0, it passes states and gradients unchanged
+        const bool behind = row + mine.row >= q.n;       // a row behind the piece: d = 0, dy = 0, b = c = 0, it passes states and gradients unchanged
         u = u_next;
         dr = d_next;
         z = z_next;
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
             const int i = tid + e * kBlock, n = i % NP;
-            const bool is = n < p.states;
+            const bool is = n < p.states && row + i / NP < q.n;
             if (kPairs * kBlock <= K * NP || i < K * NP)
                 bc[i / NP][pair_place<Shape>(n)] = Pair{kWhole && is ? (float)b_next[e] : 0.0f, is ? (float)c_next[e] : 0.0f};
         }
@@ -553,6 +554,7 @@ int ssam_scan_selective_backward(const ssam_scan_selective_backward_args* a, voi
     for (const ssam_rows* r : {&a->in, &a->dt, &a->gate, &a->b, &a->c, &a->grad_out, &a->grad_in, &a->grad_dt, &a->grad_gate})
         if (int e = check_tile_rows(*r, a->seq)) return e;
     const long long bc_width = (long long)a->groups * a->states;
+    if (bc_width >= kMaxGroupStates) return SSAM_ERR_DIM;
     for (const ssam_rows* r : {&a->grad_b, &a->grad_c})
         if (int e = check_out_rows(*r, a->seq, bc_width, esz, true)) return e;
     if (a->b_group < 0 || a->b_group > kMaxStride || a->c_group < 0 || a->c_group > kMaxStride) return SSAM_ERR_DIM;

@@ -169,6 +169,10 @@ def test_scan_selective_refusals(L):
         assert f(final=getattr(scan(), n)) == ALIAS, n
     assert f(final=at(8) + 64) == ALIAS and f(marks=at(8)) == ALIAS and f(out=Rows(at(8), 640, 64)) == ALIAS
     assert f(seq=Seq(0, 0, None, None)) == OK
+    # rows further apart than a tile's 32-bit offsets reach; of one row the stride does not matter
+    for n in ("x", "dt", "gate", "b", "c"):
+        far = {n: Rows(getattr(scan(), n).d, 0, (1 << 24) + 1)}
+        assert f(seq=Seq(1, 2, None, None), **far) == DIM and f(seq=Seq(1, 1, None, None), out=getattr(scan(), n), **far) == ALIAS, n
     long = dict(seq=Seq(1, 4096, None, None), x=Rows(at(0), 0, 64), dt=Rows(at(1), 0, 64), out=Rows(at(3), 0, 64))
     need = size(L, "ssam_scan_selective_workspace_bytes", scan(**long))
     assert need > 0 and f(work=None, **long) == NULL and f(work_bytes=need - 1, **long) == DIM and f(work=at(11) + 8, **long) == DIM
@@ -207,6 +211,10 @@ def test_scan_selective_backward_refusals(L):
     for n in ("grad_a", "grad_skip", "grad_dt_bias", "grad_state", "work"):
         assert f(**{n: at(0)}) == ALIAS and f(**{n: at(14)}) == ALIAS, n
     assert f(grad_in=Rows(at(5), 640, 64)) == ALIAS and f(grad_c=Rows(at(9), 320, 32)) == ALIAS and f(grad_gate=Rows(at(2), 640, 64)) == ALIAS
+    wide = dict(seq=Seq(1, 1, None, None), states=64, work=None)
+    assert f(groups=1 << 20, channels=1 << 20, **wide) == NULL and f(groups=1 << 21, channels=1 << 21, **wide) == DIM
+    for n in ("x", "dt", "gate", "b", "c", "grad_out", "grad_in", "grad_dt", "grad_gate"):
+        assert f(seq=Seq(1, 2, None, None), work=None, **{n: Rows(getattr(make(), n).d, 0, (1 << 24) + 1)}) == DIM, n
     assert f(seq=Seq(0, 0, None, None), grad_a=None, grad_skip=None, grad_dt_bias=None) == OK
 
 

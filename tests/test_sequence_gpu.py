@@ -567,6 +567,24 @@ def test_infinities_stay_in_their_sequence_and_channel():
     assert torch.isfinite(final[1:]).all() and torch.isfinite(final[0, :9]).all() and torch.isfinite(final[0, 10:]).all()
 
 
+@pytest.mark.parametrize("rows", [5, 33])
+def test_an_infinite_state_passes_the_end_of_its_sequence(rows):
+    """Tiles end behind the last row: what lies there adds nothing, not even zero times an infinity."""
+    D, N = 64, 16
+    g = torch.Generator().manual_seed(9)
+    x, dt, dy = randn(g, rows, D).abs() + 0.1, randn(g, rows, D), randn(g, rows, D).abs() + 0.1
+    b, c = randn(g, rows, 1, N), randn(g, rows, 1, N)
+    a = -(torch.rand(D, N, generator=g) + 0.1).cuda()
+    b[-1, 0, 3] = float("inf")
+    final, marks = torch.empty(1, D, N, device="cuda"), ssam.ssam_scan_selective_marks(x, a)
+    ssam.ssam_scan_selective(x, dt, a, b, c, softplus=True, d_final=final, d_marks=marks)
+    assert (final[0, :, 3] == float("inf")).all() and torch.isfinite(final[0, :, :3]).all() and torch.isfinite(final[0, :, 4:]).all()
+    b[-1, 0, 3], c[-1, 0, 3] = 0.5, float("inf")
+    got = ssam.ssam_scan_selective_backward(dy, x, dt, a, b, c, marks, softplus=True, state_grad=True)
+    assert (got.b[-1, 0, 3] == float("inf")).all() and (got.state[0, :, 3] == float("inf")).all()
+    assert torch.isfinite(got.state[0, :, :3]).all() and torch.isfinite(got.b[:, 0, :3]).all() and torch.isfinite(got.c).all()
+
+
 def test_refusals_of_the_binding():
     """Shapes, types, layouts: refused before anything runs."""
     D, N = 8, 4
