@@ -125,12 +125,14 @@ def scan_back(dout, u, d, a, b, c, skip, z, h0, dlast, size=False):
 
 
 def scan_kappa(n):
-    """Relative error of one term of a scan of n rows.  A decay is exp2(d a2): the hardware's exp2 is 2 u off; a2 is rounded twice, d
-    (a softplus: two exps, a reciprocal and a short polynomial) within 8 u and their product once, so the decay is off by another
-    11 |d a| u, and a chain of decays by 11 u times what it decayed by, X: e^-X X <= 30 e^-30 past X = 30, below u of the chain's
-    first term.  A sequence of more than 64 rows may be cut into pieces of 64 (at these sizes), whose time steps are added up: 64 additions,
-    64 u X more.  Every row adds the rounding of a product and a sum, 2 u each side: n (2 + 2) u; the gate, the products before and
-    behind: 24 u."""
+    """Relative error of one term of a scan of n rows.  A decay is exp2(d a2): the hardware's exp2 is 2 u off; a2 is rounded twice, d is
+    within 8 u (below) and their product once, so the decay is off by another 11 |d a| u, and a chain of decays by 11 u times what it
+    decayed by, X: e^-X X <= 30 e^-30 past X = 30, below u of the chain's first term.  A sequence of more than 128 rows may be cut into
+    pieces of 64 rows at most (at these sizes), whose time steps are added up: 64 additions, 64 u X more.  Every row adds the rounding of
+    a product and a sum and exp2's own: n (2 + 1.4) u; the gate, the products before and behind: 24 u.
+    A softplus, log1p(e) with e = exp2(-log2(e) |x|) where x < 0: log2(e) and its product with x are 1.3 u off, so e is off by 1.3 |x| u
+    and exp2's 2 u, the logarithm adds 4: (6 + 1.3 |x|) u.  That is 8 u to x = -1.5; below, d (1.3 |x| - 2) is at most 0.1, so that a row
+    moves a decay by 0.1 |a| u more, |a| <= 3.1: n (2 + 1.4 + 0.3) u in all, n 4 u."""
     return (4 * n + 30 * 11 + (30 * 64 if n > 64 else 0) + 24) * U
 
 
