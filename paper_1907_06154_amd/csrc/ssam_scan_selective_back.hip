@@ -4,9 +4,11 @@
 //     du_t = skip dy_t + d_t s_t,  dd_t = r_t + u_t s_t    with s_t = sum_n g_t b_t, r_t = sum_n a q_t
 //     da = sum_t d_t q_t,  dskip = sum_t dy_t u_t,  ddt_t = dd_t sigmoid(dt_t + bias),  dbias = sum_t ddt_t
 // The rows run backwards, in tiles of 16; a tile starts from the forward call's mark (the state before its first row) and makes its
-// states again, half a tile at a time: 8 rows' states and decays in registers, 64 of them, and back over those.  (Marks every 8 rows
-// would save the second half's way to its first row, 9 of 72 cycles a state, for 4 bytes more per row, channel and 16 states, written
-// and read; keeping 16 rows takes 128 registers and spills.)
+// states again, part of a tile at a time: 8 rows' states and decays in registers (up to 16 states), 64 of them, and back over those.
+// (Marks every 8 rows would save the second half's way to its first row, 9 of 72 cycles a state, for 4 bytes more per row, channel and
+// 16 states, written and read; keeping 16 rows takes 128 registers and spills.)
+// Bound by the vector units: 26 instructions per row, channel and state and two waves a SIMD, which 235 registers leave, busy 0.72 of the
+// cycles; 4 x 2048 rows of 2048 channels and 16 states 290 us, the way back over the pieces 62, the forward call 138.
 //
 // The sums over channels: a wave's and the block's waves' through LDS, the blocks of a group through the workspace and a launch that
 // adds them in order.
@@ -97,14 +99,17 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
     constexpr int GL = Shape::GL, NS = Shape::NS, NP = Shape::kStates, CB = Shape::kChannels, K = kTile;
     constexpr int E = K * CB / kBlock;                   // values of a thread
     constexpr int kPairs = (K * NP + kBlock - 1) / kBlock;
-    constexpr int kKept = NS == 16 ? 4 : 32 / NS;        // rows whose states and decays are kept at a time
+    // Rows whose states and decays are kept at a time, half of what spills (fp32 with eight values a thread: 456 us, 377 with four rows).
+    constexpr int kKept = NS == 16 || (E >= 8 && sizeof(T) == 4) ? 4 : 32 / NS;
     constexpr bool kMarkAhead = NS < 16;                 // the next tile's mark is requested with its rows
     constexpr int kRow = CB + CB / E;                    // a row in LDS, padded: see scan_rows
+    // A thread's eight values' parameters, 16 registers, come from LDS: those would spill (8 states 396 -> 330 us; four values' do not, and are held).
+    constexpr bool kFromLds = E >= 8;
     using Pair = RowVec<float, 2>;
     __shared__ Pair dx[K][kRow];                         // d, d u
-    __shared__ float dys[K][kRow];
+    __shared__ float dys[K][kRow];                       // dy; from a row's turn on its y, read and written by one wave
     __shared__ Pair bc[K][NP];
-    __shared__ float ys[kWhole ? K : 1][kRow];
+    __shared__ float per_channel[2][kFromLds ? CB : 1];  // bias of dt, skip
     __shared__ Pair rs[kWhole ? K : 1][kRow];            // r, s
     __shared__ float sum_bc[kWhole ? kWavesPerBlock : 1][K][2][NP];
     __shared__ __attribute__((aligned(16))) float terms[kWhole ? kWavesPerBlock : 1][2 * ChannelSums<GL>::kFloats];
@@ -161,22 +166,32 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
                          ? p.part_bc + (((long long)(blockIdx.x % p.tiles - ct.group * p.per_group) * p.rows_total + row_total) * p.groups + ct.group) *
                                            2 * p.states
                          : nullptr;
-    float bias[E], skip[E], dskip[E], dbias[E];
+    float bias_held[E], skip_held[E], dskip[E], dbias[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const bool is = mine.col + e < ct.n;
-        bias[e] = p.dt_bias && is ? p.dt_bias[ct.c0 + mine.col + e] : 0.0f;
-        skip[e] = kWhole && p.skip && is ? p.skip[ct.c0 + mine.col + e] : 0.0f;
-        dskip[e] = dbias[e] = 0.0f;
+    for (int e = 0; e < E; ++e) dskip[e] = dbias[e] = 0.0f;
+    auto bias_of = [&](int c) { return p.dt_bias && c < ct.n ? p.dt_bias[ct.c0 + c] : 0.0f; };
+    auto skip_of = [&](int c) { return kWhole && p.skip && c < ct.n ? p.skip[ct.c0 + c] : 0.0f; };
+    if constexpr (kFromLds) {
+        if (tid < CB) {
+            per_channel[0][tid] = bias_of(tid);
+            per_channel[1][tid] = skip_of(tid);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            bias_held[e] = bias_of(mine.col + e);
+            skip_held[e] = skip_of(mine.col + e);
+        }
     }
+    auto bias = [&](int e) { return kFromLds ? per_channel[0][mine.col + e] : bias_held[e]; };
+    auto skip = [&](int e) { return kFromLds ? per_channel[1][mine.col + e] : skip_held[e]; };
     // Channels behind the tile keep zeros throughout: they add nothing to the sums over channels.
-    if (ct.n < CB) {
+    if (ct.n < CB)
         for (int i = tid; i < K * kRow; i += kBlock) {
             dx[i / kRow][i % kRow] = Pair{0.0f, 0.0f};
             dys[i / kRow][i % kRow] = 0.0f;
         }
-        __syncthreads();                                 // before the first tile's values go there
-    }
+    __syncthreads();                                     // before the first tile's values go there
 
     using Vec = RowVec<T, E>;
     Vec u, dr, z, go, u_next, d_next, z_next, g_next;
@@ -217,7 +232,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
         float dy[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            const float raw = (float)dr[e] + bias[e];
+            const float raw = (float)dr[e] + bias(e);
             float v = p.softplus ? softplus(raw) : raw;
             dy[e] = (float)go[e];
             if (gated) dy[e] *= silu((float)z[e]);
@@ -326,7 +341,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
                         }
                         group_sums<GL>(y);
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) ys[part * kKept + k + r][place] = y[r];
+                        for (int r = 0; r < 4; ++r) dys[part * kKept + k + r][place] = y[r];
                     }
                 }
                 float terms_of[8];
@@ -379,15 +394,15 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
                 const int at = mine.place(e);
                 const Pair v = rs[mine.row][at];
                 const float ue = (float)u[e];
-                du[e] = __builtin_fmaf(skip[e], dy[e], dx[mine.row][at][0] * v[1]);
+                du[e] = __builtin_fmaf(skip(e), dy[e], dx[mine.row][at][0] * v[1]);
                 float dd = __builtin_fmaf(ue, v[1], v[0] * 0.693147180559945f);   // r was made with rates for exp2
-                if (p.softplus) dd *= sigmoid((float)dr[e] + bias[e]);
+                if (p.softplus) dd *= sigmoid((float)dr[e] + bias(e));
                 ddt[e] = dd;
                 dskip[e] += behind ? 0.0f : dy[e] * ue;
                 dbias[e] += behind ? 0.0f : dd;
                 if (gated) {
                     const float ze = (float)z[e], sig = sigmoid(ze);
-                    dz[e] = (float)go[e] * __builtin_fmaf(skip[e], ue, ys[mine.row][at]) * (sig * __builtin_fmaf(ze, 1.0f - sig, 1.0f));
+                    dz[e] = (float)go[e] * __builtin_fmaf(skip(e), ue, dys[mine.row][at]) * (sig * __builtin_fmaf(ze, 1.0f - sig, 1.0f));
                 } else {
                     dz[e] = 0.0f;
                 }
