@@ -65,19 +65,32 @@ __device__ __forceinline__ void quad_dots(float (&y)[4], const float (&c)[4], co
 #undef SSAM_DOT
 #undef SSAM_INPUTS
 }
-// Sums over the lane groups of a channel, in every one of them (the same bits in each: both steps add two values), of four values that
-// quad_dots made.
+// Sums over the lane groups of a channel of four rows' values that quad_dots made.  Each group is left with one row's sum (GL = 4) or
+// two (GL = 2): y[j], j a multiple of GL, is row j + sum_row.  The adds write only the groups (banks of four lanes) that keep that
+// row: six in place of the eight that leave every sum everywhere, and a quarter of the stores.
+template <int GL> __device__ __forceinline__ int sum_row(int lane) { return GL == 4 ? 0x1302 >> lane_group<4>(lane) * 4 & 3 : lane_group<GL>(lane); }
 template <int GL>
 __device__ __forceinline__ void group_sums(float (&y)[4])
 {
-#define SSAM_TURN(N)                                                          \
-    "v_add_f32_dpp %0, %0, %0 row_ror:" #N " row_mask:0xf bank_mask:0xf\n\t"  \
-    "v_add_f32_dpp %1, %1, %1 row_ror:" #N " row_mask:0xf bank_mask:0xf\n\t"  \
-    "v_add_f32_dpp %2, %2, %2 row_ror:" #N " row_mask:0xf bank_mask:0xf\n\t"  \
-    "v_add_f32_dpp %3, %3, %3 row_ror:" #N " row_mask:0xf bank_mask:0xf\n\t"
-    if constexpr (GL == 4) asm("s_nop 1\n\t" SSAM_TURN(8) SSAM_TURN(4) : "+v"(y[0]), "+v"(y[1]), "+v"(y[2]), "+v"(y[3]));
-    if constexpr (GL == 2) asm("s_nop 1\n\t" SSAM_TURN(8) : "+v"(y[0]), "+v"(y[1]), "+v"(y[2]), "+v"(y[3]));
-#undef SSAM_TURN
+    if constexpr (GL == 4)
+        asm("s_nop 1\n\t"
+            "v_add_f32_dpp %0, %0, %0 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %1, %1, %1 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %0, %2, %2 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"      // rows 0, 1 in two groups each
+            "v_add_f32_dpp %1, %3, %3 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"      // rows 2, 3
+            "s_nop 0\n\t"
+            "v_add_f32_dpp %0, %0, %0 row_ror:4 row_mask:0xf bank_mask:0xa\n\t"
+            "v_add_f32_dpp %0, %1, %1 row_ror:12 row_mask:0xf bank_mask:0x5"
+            : "+v"(y[0]), "+v"(y[2])
+            : "v"(y[1]), "v"(y[3]));
+    if constexpr (GL == 2)
+        asm("s_nop 1\n\t"
+            "v_add_f32_dpp %0, %0, %0 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %1, %1, %1 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %0, %2, %2 row_ror:8 row_mask:0xf bank_mask:0xc\n\t"
+            "v_add_f32_dpp %1, %3, %3 row_ror:8 row_mask:0xf bank_mask:0xc"
+            : "+v"(y[0]), "+v"(y[2])
+            : "v"(y[1]), "v"(y[3]));
 }
 
 // One row's sum of cQ h[Q]; h may come from the matrix instruction, hence five wait states.

@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS > 4 ? 2 : sizeof(T) == 4 ? 3 : 4)
     struct Operands {
         Pair dv[kAhead], w[kAhead][NS / 4];
     };
-    const int pairs = own_pairs<Shape>(lane);
+    const int pairs = own_pairs<Shape>(lane), sum_at = sum_row<GL>(lane);
     auto fetch = [&](int t, Operands& o) {
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
@@ -178,7 +178,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS > 4 ? 2 : sizeof(T) == 4 ? 3 : 4)
         if (kWhole) {
             group_sums<GL>(y);
 #pragma unroll
-            for (int k = 0; k < kAhead; ++k) ys[t + k][place] = y[k];    // the groups of a channel write the same value
+            for (int k = 0; k < kAhead; k += GL) ys[t + k + sum_at][place] = y[k];
         }
     };
 

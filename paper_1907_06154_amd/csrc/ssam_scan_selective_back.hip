@@ -214,7 +214,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
         }
         if (kWhole && kMarkAhead) load_states<NS>(marks + (row / K) * plane, n0, p.states, live, mark_next);
     };
-    const int pairs = own_pairs<Shape>(lane);
+    const int pairs = own_pairs<Shape>(lane), sum_at = sum_row<GL>(lane);
     const ChannelSums<GL> across(terms[kWhole ? wave : 0], lane);
 
     const int tiles = (q.n + K - 1) / K;
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
                         }
                         group_sums<GL>(y);
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) dys[part * kKept + k + r][place] = y[r];
+                        for (int r = 0; r < 4; r += GL) dys[part * kKept + k + r + sum_at][place] = y[r];
                     }
                 }
                 float terms_of[8];
