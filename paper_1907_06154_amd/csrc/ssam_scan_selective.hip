@@ -7,8 +7,8 @@
 // recurrence from there, leave y in LDS, and the threads that loaded the values finish them (skip, gate) and store them.
 //
 // Per state and row that is one exp, three products and two sums; the exp (8 cycles of a SIMD against 2.5 - 4 of the others) makes the
-// vector unit the bound, not memory (8 bytes a value): 8 x 4096 rows of 4096 channels, 16 states, bf16 622 us, of which the unit
-// is busy 77 % with the two waves per SIMD that there are; the bytes alone would take 219.
+// vector unit the bound, not memory (8 bytes a value): 8 x 4096 rows of 4096 channels, 16 states, bf16 600 us, of which the unit
+// is busy 77 % with the two waves per SIMD that there are, at 4.5 cycles an instruction; the bytes alone would take 219, the exps 119.
 #include "ssam_scan_selective.h"
 
 namespace ssam {
@@ -16,7 +16,7 @@ namespace {
 
 constexpr int kElems = 8;                    // values of a tile that a thread loads, and stores
 constexpr int kBlocks = 1024;                // four blocks of four waves per compute unit
-constexpr int kAlone = 256;                  // sequences x channel tiles that are enough without cutting (4 x 16384 rows of 4096 channels: 435 us, cut 478)
+constexpr int kAlone = 256;                  // sequences x channel tiles that are enough without cutting (4 sequences of 4096 rows, 4096 channels: 425 us, cut 472)
 
 struct ScanParams {
     Pieces pieces;
@@ -323,7 +323,7 @@ constexpr int step_channels(int P) { return kWave / P * step_each(P); }
 
 // P lanes share a channel, four states each, so that every load of states is a run of whole lines; what belongs to a channel alone
 // (time step, gate, output) is made once, by the lane of that number, and handed round.  A block's waves take the same channels of four rows, so
-// that the rates come from the L1.  Bound by the state: 8 bytes per value of it.
+// that the rates come from the L1.  Bound by the state: 8 bytes per value of it (256 rows of 4096 channels, 16 states: 31 us, 4.5 TB/s).
 template <class T, int P>
 __global__ __launch_bounds__(kBlock) void scan_step(ScanStepParams p)
 {
@@ -401,9 +401,10 @@ int scan_piece_rows(const ssam_sequences& q, int tiles, int blocks, int alone)
     constexpr long long kWhole = 128;     // not worth the join (128 rows of 4096 channels: 17.6 us, cut 18.7; 256 rows: 30.7, cut 22.9)
     constexpr long long kLongest = 1 << 30;
     const long long total = q.d_begin ? q.rows : (long long)q.rows * q.sequences, whole = (long long)q.sequences * tiles;
-    // Packed sequences end inside pieces: shorter ones even that out where there are few (37 in 8191 rows: 119 us, 139 without),
-    // and are too many where there are not (64 in 8192 rows of 4096 channels: 237, 206 without).
-    if (q.d_begin && whole < blocks) blocks += blocks / 2;
+    // Packed sequences end inside pieces: shorter ones even that out where there are few (37 in 8191 rows: 119 us, 139 without; 12 in
+    // 16384 rows of 4096 channels: 446, 465 with 1.5 times as many), and are too many where there are not (64 in 8192 rows of 4096
+    // channels with 1.5 times: 237, 206 without).
+    if (q.d_begin && whole < blocks) blocks *= 2;
     long long piece = (total * tiles + blocks - 1) / blocks;
     if (q.rows <= kWhole) piece = kWhole;
     else if (!q.d_begin && whole >= alone) piece = q.rows;
