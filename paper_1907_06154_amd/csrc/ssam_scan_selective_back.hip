@@ -7,8 +7,8 @@
 // states again, part of a tile at a time: 8 rows' states and decays in registers (up to 16 states), 64 of them, and back over those.
 // (Marks every 8 rows would save the second half's way to its first row, 9 of 72 cycles a state, for 4 bytes more per row, channel and
 // 16 states, written and read; keeping 16 rows takes 128 registers and spills.)
-// Bound by the vector units: 26 instructions per row, channel and state and two waves a SIMD, which 235 registers leave, busy 0.72 of the
-// cycles; 4 x 2048 rows of 2048 channels and 16 states 290 us, the way back over the pieces 62, the forward call 138.
+// Bound by vector issue: 22 instructions per row, channel and state, two waves a SIMD, which 235 registers leave; 4 x 2048 rows of 2048
+// channels and 16 states 268 us, what the pieces let out 60, the forward call 137.
 //
 // The sums over channels: a wave's and the block's waves' through LDS, the blocks of a group through the workspace and a launch that
 // adds them in order.
