@@ -8,6 +8,8 @@ profiles/measured_traffic.json, the HBM bytes per launch that bench.py reports a
     python -m paper_1907_06154_amd.profiling catalogue <single.json> <default.json> <out.md>
     python -m paper_1907_06154_amd.profiling sweep <default.json> <variant5.json> <out.md>
     python -m paper_1907_06154_amd.profiling scan <dir> <out.md>
+    python -m paper_1907_06154_amd.profiling operate <case of perf/operators.py>
+    python -m paper_1907_06154_amd.profiling operators <dir> <out.md>
     python -m paper_1907_06154_amd.profiling against <other libssam.so> <commit it was built from> <out.md>
 
 `summarize` expects three rocprofv3 runs of the same bench.py command (the commands are written
@@ -22,6 +24,9 @@ bench.py lists per case ("launch_names").
 
 `resources` compiles every translation unit for gfx950 with -Rpass-analysis=kernel-resource-usage
 (no GPU needed) and tabulates registers, LDS, scratch and waves per SIMD of every kernel.
+
+`operate` makes twelve calls of a sequence operator's case, over three sets of buffers in turn, for rocprofv3 to watch; `operators`
+tabulates such runs, <dir>/<case> (a kernel trace) and <dir>/<case>_pmc (counters, where there are any).
 
 `against` loads another build of the library beside this one and times iterations, fp64 volume filters and scans with both in
 turn, on a GPU: a list of calls, then random ones.
@@ -432,6 +437,72 @@ FILTERS = "5x6x4 on 256x256x256, 7x7x7 on 53x256x202, 7x7x7 on 202x256x53, 9x9x9
           "4x4x4 on 256x256x256, 2x2x9 on 256x256x256"
 
 
+def operate(name: str) -> None:
+    sys.path[:0] = [ROOT, os.path.join(ROOT, "perf")]
+    import torch
+    import operators
+    operators.own = True
+    case = next(c for c in operators.listed() if c["name"] == name)
+    sets = [operators.prepare(case, seed) for seed in range(3)]
+    for i in range(12):
+        operators.run(sets[i % 3])
+    torch.cuda.synchronize()
+
+
+def operator_kernel(name: str) -> str:
+    """A sequence operator's kernel: its name, element type and states (lane groups of a channel x states of a lane), or ''."""
+    m = re.search(r"(scan_step|scan_rows|scan_back|conv1d_step|conv1d_rows|conv1d_back_sums|conv1d_back|back_sum_bc|back_sum_params|join_pieces)", name)
+    if not m:
+        return ""
+    kind = {"DF16b": " bf16", "DF16_": " fp16", "<float": " fp32", "If": " fp32"}
+    text = "`" + m[1] + "`" + next((t for k, t in kind.items() if k in name[m.end():m.end() + 8] or k == "<float" and k in name), "")
+    shape = re.search(r"ScanShape(?:ILi|<)(\d+)(?:ELi|, )(\d+)", name)
+    if shape:
+        text += f" {shape[1]} x {shape[2]}" + (", everything" if re.search(r"Lb1E|, true>", name) else ", what the pieces add")
+    if m[1] == "join_pieces":
+        text += " backward" if re.search(r"Lb1E|<true>", name) else " forward"
+    return text
+
+
+def operator_summary(runs: str, out_md: str) -> None:
+    ctrs = "SQ_WAVES SQ_INSTS_VALU SQ_ACTIVE_INST_VALU SQ_WAVE_CYCLES SQ_WAIT_ANY SQ_INSTS_LDS SQ_LDS_BANK_CONFLICT SQ_LDS_IDX_ACTIVE"
+    run = "--output-format csv -d <dir>/<case>{} -o c -- python3 -m paper_1907_06154_amd.profiling operate <case>\n"
+    out = ["# Sequence operators: the kernels of a call (rocprofv3)\n", "One MI355X, per case of perf/operators.py:\n",
+           "    rocprofv3 --kernel-trace " + run.format("") + f"    rocprofv3 --pmc {ctrs} " + run.format("_pmc") +
+           "    python -m paper_1907_06154_amd.profiling operators <dir> profiles/sequence_operators.md\n",
+           "Medians over a kernel's dispatches, us from the trace, the rest from the counter run.  `vector busy` = 4 x SQ_ACTIVE_INST_VALU / (1024 SIMDs x "
+           "duration x 2.2 GHz), `LDS busy` = SQ_LDS_IDX_ACTIVE / (256 CUs x duration x 2.2 GHz), of which `conflicts` replay, `waiting` = SQ_WAIT_ANY / "
+           "SQ_WAVE_CYCLES.\n",
+           "| case | kernel | us | waves | vector instructions | LDS instructions | vector busy | LDS busy | conflicts | waiting |\n" + "|---" * 10 + "|"]
+    middle = lambda v: sorted(v)[len(v) // 2]  # noqa: E731
+    for trace in sorted(glob.glob(os.path.join(runs, "*"))):
+        if trace.endswith("_pmc") or not os.path.isdir(trace):
+            continue
+        times, counts = collections.OrderedDict(), {}
+        rows = csv.DictReader(open(one(os.path.join(trace, "**", "*kernel_trace.csv"))))
+        for r in sorted(rows, key=lambda r: int(r["Start_Timestamp"])):
+            times.setdefault(operator_kernel(r["Kernel_Name"]), []).append((int(r["End_Timestamp"]) - int(r["Start_Timestamp"])) / 1e3)
+        if os.path.isdir(trace + "_pmc"):
+            for k, c, us in counter_dispatches(trace + "_pmc"):
+                for name, v in (*c.items(), ("us", us)):
+                    counts.setdefault(operator_kernel(k), {}).setdefault(name, []).append(v)
+        for k, v in times.items():
+            if not k:
+                continue
+            line = f"| {os.path.basename(trace)} | {k} | {middle(v):.1f} |"
+            if k in counts:
+                m = {name: middle(x) for name, x in counts[k].items()}
+                cycles = m["us"] * 2200
+                line += (f" {m['SQ_WAVES']:.0f} | {m['SQ_INSTS_VALU']:.3g} | {m['SQ_INSTS_LDS']:.3g} | {m['SQ_ACTIVE_INST_VALU'] / 256 / cycles:.2f} | "
+                         f"{m['SQ_LDS_IDX_ACTIVE'] / 256 / cycles:.2f} | {m['SQ_LDS_BANK_CONFLICT'] / max(m['SQ_LDS_IDX_ACTIVE'], 1):.2f} | "
+                         f"{m['SQ_WAIT_ANY'] / max(m['SQ_WAVE_CYCLES'], 1):.2f} |")
+            else:
+                line += " |" * 7
+            out.append(line)
+    open(out_md, "w").write("\n".join(out) + "\n")
+    print("\n".join(out))
+
+
 def against(other: str, commit: str, out_md: str, seconds: float = 40.0) -> None:
     """The tables of `against`; a grid is named columns x rows (x planes)."""
     import ctypes
@@ -584,6 +655,10 @@ def main(argv) -> int:
         scan_summary(argv[1], argv[2])
     elif len(argv) == 4 and argv[0] == "against":
         against(argv[1], argv[2], argv[3])
+    elif len(argv) == 2 and argv[0] == "operate":
+        operate(argv[1])
+    elif len(argv) == 3 and argv[0] == "operators":
+        operator_summary(argv[1], argv[2])
     elif len(argv) == 2 and argv[0] == "resources":
         resources(argv[1])
     else:
