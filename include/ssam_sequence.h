@@ -106,7 +106,7 @@ int ssam_conv1d_step(const ssam_conv1d_step_args *args, void *hip_stream);
  * starts from; ssam_scan_selective_marks(args) entries of [channels][states] floats.
  * d_work: ssam_scan_selective_workspace_bytes(args) bytes, 16-byte aligned (NULL where that is 0).
  * Schedules: one launch where sequences and channels fill the device; otherwise sequences are cut along time: the state
- * that each piece adds, the states before the pieces, then all rows (three launches). */
+ * that each piece adds, the states between the pieces, then all rows (three launches). */
 typedef struct {
     int dtype, channels, states, groups, softplus;
     ssam_sequences seq;

@@ -45,6 +45,9 @@ def wide(g, lead, channels, dtype, form):
 LAYOUTS = {
     "one": ((37,), None, None), "single_row": ((1,), None, None), "batch": ((3, 21), None, None), "padded": ((4, 19), None, [19, 0, 1, 7]),
     "packed": ((90,), [2, 2, 19, 20, 20, 51, 88], None), "long": ((300,), None, None), "packed_long": ((333,), [0, 1, 200, 200, 330], None),
+    # more pieces than the join takes at a time
+    "pieces": ((2300,), None, None), "batch_pieces": ((2, 1200), None, None), "padded_pieces": ((3, 1300), None, [1300, 129, 0]),
+    "packed_pieces": ((2200,), [3, 1500, 1500, 1530, 2190], None),
 }
 
 
@@ -191,7 +194,9 @@ SCAN = [  # layout, type, channels, states, groups, softplus, gate, skip, state,
     ("one", "bfloat16", 70, 20, 1, True, True, True, True, "wide"), ("one", "float16", 260, 4, 1, True, True, True, True, "wide"),
     ("long", "float32", 64, 16, 1, True, True, True, True, "dense"), ("long", "bfloat16", 20, 32, 1, True, True, True, True, "wide"),
     ("packed_long", "float32", 70, 8, 1, True, True, True, True, "dense"), ("packed_long", "bfloat16", 12, 50, 2, True, False, True, True, "wide"),
-]
+    ("pieces", "float32", 20, 4, 1, True, True, True, True, "dense"), ("batch_pieces", "float16", 136, 8, 2, True, False, True, True, "wide"),
+    ("padded_pieces", "bfloat16", 70, 16, 1, True, True, False, True, "dense"), ("packed_pieces", "float32", 66, 20, 2, True, True, True, True, "wide"),
+    ("packed_pieces", "bfloat16", 9, 33, 3, False, True, True, False, "dense")]
 
 
 class ScanCase:
@@ -539,6 +544,29 @@ def test_what_a_call_allocates_belongs_to_its_stream():
     got = calls(other)
     torch.cuda.synchronize()
     assert all(torch.equal(p, q) for p, q in zip(got, want))
+
+
+def test_two_streams_at_once():
+    """Calls in flight together have workspaces of their own."""
+    D, N, T = 256, 16, 3000
+    g = torch.Generator().manual_seed(10)
+    sets = [[randn(g, T, D), randn(g, T, D), -(torch.rand(D, N, generator=g) + 0.1).cuda(), randn(g, T, 1, N), randn(g, T, 1, N), randn(g, T, D),
+             randn(g, D, 4)] for _ in range(2)]
+
+    def calls(x, dt, a, b, c, dy, w, stream):
+        marks = ssam.ssam_scan_selective_marks(x, a)
+        y = ssam.ssam_scan_selective(x, dt, a, b, c, softplus=True, d_marks=marks, stream=stream)
+        s = ssam.ssam_scan_selective_backward(dy, x, dt, a, b, c, marks, softplus=True, stream=stream)
+        k = ssam.ssam_conv1d_backward(dy, x, w, silu=True, stream=stream)
+        return [marks, y, *(t for t in (*s, *k) if t is not None)]
+
+    want = [calls(*s, None) for s in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [calls(*s, stream) for _ in range(4) for s, stream in zip(sets, streams)]
+    torch.cuda.synchronize()
+    for i, result in enumerate(got):
+        assert all(torch.equal(p, q) for p, q in zip(result, want[i % 2])), i
 
 
 def test_infinities_stay_in_their_sequence_and_channel():
