@@ -107,7 +107,8 @@ def ssam_conv1d_step(d_in, weight, d_state, bias=None, silu: bool = False, slots
 
 
 def ssam_scan_selective_marks(d_in, a, starts=None, lengths=None):
-    """A tensor for ssam_scan_selective's d_marks: the states before every 16th row, for ssam_scan_selective_backward."""
+    """A tensor for ssam_scan_selective's d_marks: the states before every 16th row, for ssam_scan_selective_backward; made on
+    the current stream."""
     if _fast is None:
         _load()
     return _fast.scan_marks(d_in, a, starts, lengths)
