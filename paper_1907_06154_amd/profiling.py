@@ -472,7 +472,7 @@ def operator_summary(runs: str, out_md: str) -> None:
            "    python -m paper_1907_06154_amd.profiling operators <dir> profiles/sequence_operators.md\n",
            "Medians over a kernel's dispatches, us from the trace, the rest from the counter run.  `vector busy` = 4 x SQ_ACTIVE_INST_VALU / (1024 SIMDs x "
            "duration x 2.2 GHz), `LDS busy` = SQ_LDS_IDX_ACTIVE / (256 CUs x duration x 2.2 GHz), of which `conflicts` replay, `waiting` = SQ_WAIT_ANY / "
-           "SQ_WAVE_CYCLES.\n",
+           "SQ_WAVE_CYCLES.  These are a process's first twelve calls: the long scans take up to 15 % less once the clock has settled.\n",
            "| case | kernel | us | waves | vector instructions | LDS instructions | vector busy | LDS busy | conflicts | waiting |\n" + "|---" * 10 + "|"]
     middle = lambda v: sorted(v)[len(v) // 2]  # noqa: E731
     for trace in sorted(glob.glob(os.path.join(runs, "*"))):
