@@ -42,7 +42,7 @@ typedef struct {
 } ssam_rows;
 
 typedef struct {
-    int sequences;             /* >= 0                                                         */
+    int sequences;             /* >= 0; of a batch, sequences x rows <= 2^40                   */
     int rows;                  /* batch forms: rows of a sequence; packed: rows of the tensor  */
     const int *d_begin, *d_end;
 } ssam_sequences;

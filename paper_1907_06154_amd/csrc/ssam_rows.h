@@ -226,6 +226,7 @@ inline int type_bytes(int dtype) { return dtype == SSAM_F32 ? 4 : dtype == SSAM_
 
 constexpr long long kMaxChannels = 1 << 24;
 constexpr long long kMaxStride = 1LL << 40;      // elements: offsets of any row then fit 64 bits
+constexpr long long kMaxRows = 1LL << 40;        // of a batch: their products with tiles of channels then fit 64 bits
 constexpr long long kMaxTileStride = 1 << 24;    // elements from row to row where a tile's offsets (32 rows of 4 bytes) have 32 bits
 
 // What a tensor covers: `count` rows (batch after batch) of `width` bytes, `step` bytes apart; one = a plain range.
@@ -290,6 +291,7 @@ inline int check_out_rows(const ssam_rows& r, const ssam_sequences& q, long long
 inline int check_sequences(const ssam_sequences& q)
 {
     if (q.sequences < 0 || q.rows < 0 || q.rows > SSAM_MAX_EXTENT || q.sequences > SSAM_MAX_EXTENT) return SSAM_ERR_DIM;
+    if (!q.d_begin && (long long)q.rows * q.sequences > kMaxRows) return SSAM_ERR_DIM;
     if (q.d_begin && !q.d_end) return SSAM_ERR_NULL;
     if ((uintptr_t)q.d_begin % 4 || (uintptr_t)q.d_end % 4) return SSAM_ERR_DIM;
     return SSAM_OK;

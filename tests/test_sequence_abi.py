@@ -169,6 +169,7 @@ def test_scan_selective_refusals(L):
         assert f(final=getattr(scan(), n)) == ALIAS, n
     assert f(final=at(8) + 64) == ALIAS and f(marks=at(8)) == ALIAS and f(out=Rows(at(8), 640, 64)) == ALIAS
     assert f(seq=Seq(0, 0, None, None)) == OK
+    assert f(seq=Seq(1 << 21, 1 << 20, None, None)) == DIM
     # rows further apart than a tile's 32-bit offsets reach; of one row the stride does not matter
     for n in ("x", "dt", "gate", "b", "c"):
         far = {n: Rows(getattr(scan(), n).d, 0, (1 << 24) + 1)}
@@ -184,6 +185,7 @@ def test_scan_selective_plans(L):
     work = lambda **c: size(L, "ssam_scan_selective_workspace_bytes", scan(**c))  # noqa: E731
     assert marks() == 2 and marks(seq=Seq(3, 16, None, None)) == 3 and marks(seq=Seq(3, 17, None, None)) == 6 and marks(seq=Seq(3, 0, None, None)) == 3
     assert marks(seq=Seq(3, 33, at(20), at(20) + 4)) == 5 and marks(dtype=9) == 0
+    assert marks(seq=Seq(1 << 20, 1 << 20, None, None)) == 1 << 36 and marks(seq=Seq(1 << 21, 1 << 20, None, None)) == 0
     assert work() == 0 and work(seq=Seq(1, 128, None, None)) == 0
     # few sequences are cut into pieces: their states and their time steps' sums; many are not
     assert work(groups=1, seq=Seq(1, 129, None, None)) == 5 * (64 * 16 + 64) * 4
