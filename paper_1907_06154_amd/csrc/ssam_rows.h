@@ -127,33 +127,44 @@ __device__ __forceinline__ void span_of(const Pieces& q, int s, int& first, int&
 }
 
 // The piece of a slot; all 64 lanes call it together with the same slot.  The packed form looks for the last sequence whose
-// first slot is not behind this one, 64 candidates at a time.
+// first slot is not behind this one, 64 candidates at a time; the last round's lanes hold its rows too, so that up to 64 sequences
+// take one wait for memory.
 __device__ __forceinline__ Piece find_piece(const Pieces& q, int slot)
 {
     Piece p{-1, 0, 0, 0, 0};
-    int s = 0, c = 0;
+    int s = 0, c = 0, first = 0, len = 0;
     if (q.begin) {
         const int lane = threadIdx.x & (kWave - 1);
         int n = q.sequences;
         while (true) {
             const int step = (n + kWave - 1) / kWave;
             const int i = lane * step;
-            const bool before = i < n && first_slot(q, s + i) <= slot;
-            const int hits = __builtin_popcountll(__builtin_amdgcn_ballot_w64(before));
+            int begin = 0, end = 0;
+            if (i < n) {
+                begin = q.begin[s + i];
+                if (step == 1) end = q.end[s + i];
+            }
+            begin = held(begin, q.rows);
+            end = held(end, q.rows);
+            const int hits = __builtin_popcountll(__builtin_amdgcn_ballot_w64(i < n && begin / q.piece + s + i <= slot));
             if (hits == 0) return p;
             const int skip = (hits - 1) * step;
             s += skip;
+            if (step == 1) {
+                first = __builtin_amdgcn_readlane(begin, skip);
+                const int behind = __builtin_amdgcn_readlane(end, skip);
+                len = behind > first ? behind - first : 0;
+                break;
+            }
             n = n - skip < step ? n - skip : step;
-            if (step == 1) break;
         }
         s = __builtin_amdgcn_readfirstlane(s);
-        c = slot - first_slot(q, s);
+        c = slot - (first / q.piece + s);
     } else {
         s = slot / q.per;
         c = slot - s * q.per;
+        span_of(q, s, first, len);
     }
-    int first, len;
-    span_of(q, s, first, len);
     const long long row0 = (long long)c * q.piece;
     if (c < 0 || (c > 0 && row0 >= len)) return p;
     p.seq = s;

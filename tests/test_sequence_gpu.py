@@ -48,6 +48,8 @@ LAYOUTS = {
     # more pieces than the join takes at a time
     "pieces": ((2300,), None, None), "batch_pieces": ((2, 1200), None, None), "padded_pieces": ((3, 1300), None, [1300, 129, 0]),
     "packed_pieces": ((2200,), [3, 1500, 1500, 1530, 2190], None),
+    # more packed sequences than a wave has lanes, and than two rounds of 64 tell apart; every third or fourth empty
+    "crowd": ((700,), [5 + s * 4 + s % 3 * 2 for s in range(131)], None), "swarm": ((5300,), [s - s % 4 // 3 for s in range(5201)], None),
 }
 
 
@@ -71,7 +73,8 @@ CONV = [(lay, dt, W, D, silu, bias, state, form)
             ("padded", "float32", 5, 33, True, True, True, "wide"), ("padded", "bfloat16", 4, 512, True, True, True, "dense"),
             ("packed", "float32", 4, 257, True, True, True, "dense"), ("packed", "float16", 6, 8, False, True, True, "wide"),
             ("packed", "bfloat16", 2, 100, True, True, False, "wide"), ("long", "bfloat16", 7, 40, True, True, True, "dense"),
-            ("packed_long", "float32", 4, 20, False, False, True, "dense")]]
+            ("packed_long", "float32", 4, 20, False, False, True, "dense"),
+            ("crowd", "bfloat16", 4, 130, True, True, True, "wide"), ("swarm", "float32", 3, 9, True, True, True, "dense")]]
 
 
 def conv_case(lay, dt, W, D, bias, state, form, params=None):
@@ -196,6 +199,7 @@ SCAN = [  # layout, type, channels, states, groups, softplus, gate, skip, state,
     ("packed_long", "float32", 70, 8, 1, True, True, True, True, "dense"), ("packed_long", "bfloat16", 12, 50, 2, True, False, True, True, "wide"),
     ("pieces", "float32", 20, 4, 1, True, True, True, True, "dense"), ("batch_pieces", "float16", 136, 8, 2, True, False, True, True, "wide"),
     ("padded_pieces", "bfloat16", 70, 16, 1, True, True, False, True, "dense"), ("packed_pieces", "float32", 66, 20, 2, True, True, True, True, "wide"),
+    ("crowd", "bfloat16", 65, 16, 1, True, True, True, True, "wide"), ("swarm", "float32", 6, 3, 1, True, False, True, True, "dense"),
     ("packed_pieces", "bfloat16", 9, 33, 3, False, True, True, False, "dense")]
 
 
