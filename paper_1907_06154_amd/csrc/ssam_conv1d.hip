@@ -182,7 +182,9 @@ __global__ __launch_bounds__(kBlock) void conv1d_back(Conv1dBackParams p)
 {
     constexpr int V = kBackChan;
     __shared__ RowVec<float, V> block_sums[kWavesPerBlock - 1][W + 1][kWave];
-    const int lane = threadIdx.x & (kWave - 1), in_block = threadIdx.x >> 6;
+    // The wave's number as a scalar, so that what depends on its rows is a scalar branch (8 x 2048 rows of 4096 channels, with the forward
+    // call: 139 us, with vector ones 158).
+    const int lane = threadIdx.x & (kWave - 1), in_block = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int strip = blockIdx.x % p.strips;
     const long long slot = (long long)(blockIdx.x / p.strips) * kWavesPerBlock + in_block;
     Piece q = find_piece(p.pieces, (int)(slot < p.slots ? slot : 0));
@@ -255,15 +257,18 @@ __global__ __launch_bounds__(kBlock) void conv1d_back(Conv1dBackParams p)
                         qs[0][v] *= sig * __builtin_fmaf(s, 1.0f - sig, 1.0f);
                     }
                 }
-                const bool in_piece = k + u < q.n;       // rows behind it are another's
+                // The piece's own rows alone: those behind it, and the carried ones of an empty sequence, may hold an infinity, which
+                // times zero is not zero.
+                if (k + u < q.n) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    qs[0][v] = t < q.len ? qs[0][v] : 0.0f;
-                    const float own = in_piece ? qs[0][v] : 0.0f;
+                    for (int v = 0; v < V; ++v) {
 #pragma unroll
-                    for (int j = 0; j < W; ++j) dw[j][v] = __builtin_fmaf(own, win[j][v], dw[j][v]);
-                    dw[W][v] += own;
+                        for (int j = 0; j < W; ++j) dw[j][v] = __builtin_fmaf(qs[0][v], win[j][v], dw[j][v]);
+                        dw[W][v] += qs[0][v];
+                    }
                 }
+#pragma unroll
+                for (int v = 0; v < V; ++v) qs[0][v] = t < q.len ? qs[0][v] : 0.0f;
                 const int o = t - (W - 1);  // the row whose gradient is complete
                 const bool carried = o < 0;
                 if (k + u >= rows || (o < q.row0 && !carried) || (carried ? !p.grad_state : !dx)) continue;
