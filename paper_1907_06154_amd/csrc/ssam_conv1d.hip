@@ -199,10 +199,10 @@ __global__ __launch_bounds__(kBlock) void conv1d_back(Conv1dBackParams p)
         const T* __restrict__ in = sequence_base<T>(p.in, p.pieces, q) + ch.first;
         const T* __restrict__ dy = sequence_base<T>(p.grad_out, p.pieces, q) + ch.first;
         T* __restrict__ dx = p.grad_in.d ? sequence_base<T>(p.grad_in, p.pieces, q) + ch.first : nullptr;
-        const int rows = q.n + W - 1;       // the march: rows row0 .. row0 + rows - 1, q = 0 from len on
+        const int rows = q.n + W - 1;       // the march: rows row0 .. row0 + rows - 1
         RowVec<T, V> x_next[kMarch], g_next[kMarch];
         float win[W][V];                    // widened once, not at each of its 2 W uses (fp16, three taps 152 -> 136 us with the forward call)
-        auto request = [&](int k) {         // rows behind the sequence are read as its last, and their q is 0
+        auto request = [&](int k) {         // rows behind the sequence are read as its last, and their q is not used
 #pragma unroll
             for (int u = 0; u < kMarch; ++u) {
                 const int t = q.row0 + k + u < q.len ? q.row0 + k + u : q.len - 1;
@@ -267,17 +267,25 @@ __global__ __launch_bounds__(kBlock) void conv1d_back(Conv1dBackParams p)
                         dw[W][v] += qs[0][v];
                     }
                 }
-#pragma unroll
-                for (int v = 0; v < V; ++v) qs[0][v] = t < q.len ? qs[0][v] : 0.0f;
                 const int o = t - (W - 1);  // the row whose gradient is complete
                 const bool carried = o < 0;
                 if (k + u >= rows || (o < q.row0 && !carried) || (carried ? !p.grad_state : !dx)) continue;
                 float d[V];
+                if (t < q.len && t >= W - 1) {
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    d[v] = w[0][v] * qs[0][v];
+                    for (int v = 0; v < V; ++v) {
+                        d[v] = w[0][v] * qs[0][v];
 #pragma unroll
-                    for (int j = 1; j < W; ++j) d[v] = __builtin_fmaf(w[j][v], qs[j][v], d[v]);
+                        for (int j = 1; j < W; ++j) d[v] = __builtin_fmaf(w[j][v], qs[j][v], d[v]);
+                    }
+                } else {        // only the taps that rows of the sequence lie under: another's may be infinite
+#pragma unroll
+                    for (int v = 0; v < V; ++v) d[v] = 0.0f;
+#pragma unroll
+                    for (int j = 0; j < W; ++j)
+                        if (t - j >= 0 && t - j < q.len)
+#pragma unroll
+                            for (int v = 0; v < V; ++v) d[v] = __builtin_fmaf(w[j][v], qs[j][v], d[v]);
                 }
                 const int tail = o - (q.len - (W - 1));
                 if (p.grad_final && tail >= 0) {

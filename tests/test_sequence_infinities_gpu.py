@@ -43,3 +43,25 @@ def test_the_carried_rows_of_an_empty_sequence_reach_no_tap():
     h[1] = INF
     got = ssam.ssam_conv1d_backward(dy, x, w, d_state=h, lengths=lengths)
     assert torch.equal(got.weight, clean.weight) and torch.equal(got.x, clean.x)
+
+
+@pytest.mark.parametrize("rows,W", [(5, 4), (8, 2), (9, 4), (17, 8), (2, 5), (0, 3), (64, 4)])
+def test_a_tap_reaches_the_rows_under_it_alone(rows, W):
+    """An infinite tap j: the gradient of row t has it only where row t + W - 1 - j is one of the sequence."""
+    g = torch.Generator().manual_seed(rows)
+    D, at = 70, 11
+    x, dy, w = randn(g, rows, D), randn(g, rows, D), randn(g, D, W)
+    dlast = randn(g, 1, W - 1, D)
+    clean = ssam.ssam_conv1d_backward(dy, x, w, d_grad_final=dlast, state_grad=True)
+    for j in range(W):
+        there = w[at, j].item()
+        w[at, j] = INF
+        got = ssam.ssam_conv1d_backward(dy, x, w, d_grad_final=dlast, state_grad=True)
+        w[at, j] = there
+        grads = torch.cat([got.state[0], got.x])                     # rows -(W - 1) .. rows - 1
+        want = torch.cat([clean.state[0], clean.x])
+        t = torch.arange(-(W - 1), rows, device="cuda") + W - 1 - j
+        has = (t >= 0) & (t < rows)
+        assert not torch.isfinite(grads[has, at]).any()
+        grads[has, at] = want[has, at]
+        assert torch.equal(grads, want), j
