@@ -205,7 +205,10 @@ __global__ __launch_bounds__(kBlock, Shape::NS > 4 ? 2 : sizeof(T) == 4 ? 3 : 4)
         if (kWhole) {
             float o[E];
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(per_channel[1][mine.col + e], (float)u[e], ys[mine.row][mine.place(e)]);
+            for (int e = 0; e < E; ++e) o[e] = ys[mine.row][mine.place(e)];
+            if (p.skip)         // (without one there is no such term, not one of zero times an input that may be infinite)
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] = __builtin_fmaf(per_channel[1][mine.col + e], (float)u[e], o[e]);
             if (gated)
 #pragma unroll
                 for (int e = 0; e < E; ++e) o[e] *= silu((float)z[e]);
@@ -382,7 +385,7 @@ __global__ __launch_bounds__(kBlock) void scan_step(ScanStepParams p)
             s = part_sum<P>(s);
             y = part == kk ? s : y;
         });
-        y = __builtin_fmaf(skip, x.u, y);
+        if (p.skip) y = __builtin_fmaf(skip, x.u, y);
         if (p.gate.d) y *= silu(x.z);
         if (own) static_cast<T*>(p.out.d)[r * p.out.row + c] = (T)y;
         r = same.next();

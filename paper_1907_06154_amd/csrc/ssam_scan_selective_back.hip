@@ -394,7 +394,8 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
                 const int at = mine.place(e);
                 const Pair v = rs[mine.row][at];
                 const float ue = (float)u[e];
-                du[e] = __builtin_fmaf(skip(e), dy[e], dx[mine.row][at][0] * v[1]);
+                du[e] = dx[mine.row][at][0] * v[1];
+                if (p.skip) du[e] = __builtin_fmaf(skip(e), dy[e], du[e]);
                 float dd = __builtin_fmaf(ue, v[1], v[0] * 0.693147180559945f);   // r was made with rates for exp2
                 if (p.softplus) dd *= sigmoid((float)dr[e] + bias(e));
                 ddt[e] = dd;
@@ -402,7 +403,8 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
                 dbias[e] += behind ? 0.0f : dd;
                 if (gated) {
                     const float ze = (float)z[e], sig = sigmoid(ze);
-                    dz[e] = (float)go[e] * __builtin_fmaf(skip(e), ue, dys[mine.row][at]) * (sig * __builtin_fmaf(ze, 1.0f - sig, 1.0f));
+                    const float y = dys[mine.row][at];
+                    dz[e] = (float)go[e] * (p.skip ? __builtin_fmaf(skip(e), ue, y) : y) * (sig * __builtin_fmaf(ze, 1.0f - sig, 1.0f));
                 } else {
                     dz[e] = 0.0f;
                 }

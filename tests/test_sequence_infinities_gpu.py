@@ -65,3 +65,96 @@ def test_a_tap_reaches_the_rows_under_it_alone(rows, W):
         assert not torch.isfinite(grads[has, at]).any()
         grads[has, at] = want[has, at]
         assert torch.equal(grads, want), j
+
+
+STATES = [8, 16, 32, 64]
+
+
+class Positive:
+    """A scan whose terms are all positive, so that infinities add up to infinities."""
+
+    def __init__(self, rows, N, dtype, D=70):
+        g = torch.Generator().manual_seed(N)
+        pos = lambda *s: (torch.rand(s, generator=g) + 0.25).to(dtype).cuda()  # noqa: E731
+        self.x, self.dt, self.dy, self.b, self.c = pos(rows, D), pos(rows, D) / 8, pos(rows, D), pos(rows, 1, N), pos(rows, 1, N)
+        self.a = -(torch.rand(D, N, generator=g) * 0.5 + 0.1).cuda()
+
+    def forward(self, **more):
+        return ssam.ssam_scan_selective(self.x, self.dt, self.a, self.b, self.c, **more)
+
+    def marked(self):
+        marks = ssam.ssam_scan_selective_marks(self.x, self.a)
+        self.forward(d_marks=marks)
+        return marks
+
+    def back(self, marks):
+        return ssam.ssam_scan_selective_backward(self.dy, self.x, self.dt, self.a, self.b, self.c, marks, state_grad=True)
+
+
+@pytest.mark.parametrize("N", STATES)
+def test_an_infinite_input_is_an_infinite_output(N):
+    for dtype, rows in zip(TYPES, (30, 20, 200)):
+        for name in ("x", "dt"):
+            print(dtype, name, flush=True)
+            k = Positive(rows, N, dtype)
+            clean, (t, at) = k.forward(), (7, 11)
+            getattr(k, name)[t, at] = INF
+            last = torch.empty(1, *k.a.shape, device="cuda")
+            got = k.forward(d_final=last)
+            reached = slice(t, rows) if rows < 150 else slice(t, 30)       # (a long sequence is cut; its states pass the join)
+            assert (got[reached, at] == INF).all(), got[reached, at]
+            if rows < 150:
+                assert (last[0, at] == INF).all()
+            got[t:, at] = clean[t:, at]
+            assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("N", STATES)
+def test_an_infinite_input_of_a_single_row(N):
+    for dtype in TYPES:
+        k = Positive(6, N, dtype)
+        pool = torch.rand(6, *k.a.shape, device="cuda")
+        k.x[2, 11] = INF
+        got = ssam.ssam_scan_selective_step(k.x, k.dt, k.a, k.b, k.c, pool)
+        assert got[2, 11] == INF and (pool[2, 11] == INF).all()
+        got[2, 11], pool[2, 11] = 0, 0
+        assert torch.isfinite(got).all() and torch.isfinite(pool).all()
+
+
+@pytest.mark.parametrize("N", STATES)
+def test_the_gates_gradient_without_a_skip(N):
+    for dtype in TYPES:
+        rows, t, at = 40, 21, 11
+        k = Positive(rows, N, dtype)
+        z = torch.ones_like(k.x)
+        k.x[t, at] = INF
+        marks = ssam.ssam_scan_selective_marks(k.x, k.a)
+        out = k.forward(gate=z, d_marks=marks)
+        got = ssam.ssam_scan_selective_backward(k.dy, k.x, k.dt, k.a, k.b, k.c, marks, gate=z)
+        for v in (out, got.gate):
+            assert (v[t:, at] == INF).all()
+            v[t:, at] = 0
+            assert torch.isfinite(v).all()
+
+
+@pytest.mark.parametrize("N", STATES)
+def test_an_infinite_gradient_and_an_infinite_state_on_the_way_back(N):
+    for dtype in TYPES:
+        print(dtype, flush=True)
+        rows, t, at = 40, 21, 11
+        k = Positive(rows, N, dtype)
+        marks = k.marked()
+        clean = k.back(marks)
+        there = k.dy[t, at].item()
+        k.dy[t, at] = INF
+        got = k.back(marks)
+        assert (got.x[:t + 1, at] == INF).all() and (got.state[0, at] == INF).all()
+        got.x[:t + 1, at], got.state[0, at] = clean.x[:t + 1, at], clean.state[0, at]
+        assert torch.equal(got.x, clean.x) and torch.equal(got.state, clean.state)
+        k.dy[t, at] = there
+        k.x[t, at] = INF                   # an infinite state from row t on: the rows behind it lose their time steps' gradients
+        got = k.back(k.marked())
+        assert (got.dt[t + 1:, at] == -INF).all(), got.dt[t + 1:, at]
+        got.dt[t:, at] = clean.dt[t:, at]
+        assert torch.equal(got.dt, clean.dt) and torch.equal(got.x, clean.x)
+        assert (got.c[t:] == INF).all() and torch.equal(got.c[:t], clean.c[:t])
