@@ -349,6 +349,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
                 for (int k = kKept - 1; k >= 0; --k) {
                     const int t = part * kKept + k;
                     const float* before = k ? hs[k - 1] : h;
+                    const bool own = row + t < q.n;       // of a row behind the piece, `before` is the last state, which may be infinite
                     float r = 0.0f, s = 0.0f;
 #pragma unroll
                     for (int m = 0; m < NS / 4; ++m) {
@@ -369,7 +370,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
                             const int i = 4 * m + j;
                             g[i] *= as[k][i];                      // what reaches the row before
                             const float qi = g[i] * before[i];
-                            da[i] = __builtin_fmaf(dv[k][0], qi, da[i]);
+                            if (own) da[i] = __builtin_fmaf(dv[k][0], qi, da[i]);
                             r = i ? __builtin_fmaf(a2[i], qi, r) : a2[i] * qi;
                         }
                         across.put(step, vb, vc);

@@ -67,6 +67,30 @@ def test_a_tap_reaches_the_rows_under_it_alone(rows, W):
         assert torch.equal(grads, want), j
 
 
+@pytest.mark.parametrize("rows", [5, 16, 33, 250])
+@pytest.mark.parametrize("N", [4, 8, 16, 32, 64])
+def test_the_last_state_reaches_no_rate(rows, N):
+    """The gradient at a decay rate holds the states before each row: the one behind the last row is not among them."""
+    g = torch.Generator().manual_seed(rows)
+    D, at = 70, 11
+    x, dt, dy, z = (randn(g, rows, D) for _ in range(4))
+    b, c = randn(g, rows, 1, N), randn(g, rows, 1, N)
+    a = -(torch.rand(D, N, generator=g) + 0.1).cuda()
+    dlast = randn(g, 1, D, N)
+
+    def back():
+        marks = ssam.ssam_scan_selective_marks(x, a)
+        ssam.ssam_scan_selective(x, dt, a, b, c, gate=z, softplus=True, d_marks=marks)
+        return ssam.ssam_scan_selective_backward(dy, x, dt, a, b, c, marks, gate=z, softplus=True, d_grad_final=dlast, state_grad=True)
+
+    clean = back()
+    x[-1, at] = INF
+    got = back()
+    assert torch.isfinite(clean.a).all() and torch.equal(got.a, clean.a)
+    assert torch.equal(got.state, clean.state) and torch.equal(got.dt[:-1], clean.dt[:-1]) and torch.equal(got.x, clean.x)
+    assert torch.equal(got.c[:-1], clean.c[:-1]) and not torch.isfinite(got.c[-1]).any()
+
+
 STATES = [8, 16, 32, 64]
 
 
