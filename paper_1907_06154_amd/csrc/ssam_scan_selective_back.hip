@@ -102,6 +102,9 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
     // Rows whose states and decays are kept at a time, half of what spills (fp32 with eight values a thread: 456 us, 377 with four rows).
     constexpr int kKept = NS == 16 || (E >= 8 && sizeof(T) == 4) ? 4 : 32 / NS;
     constexpr bool kMarkAhead = NS < 16;                 // the next tile's mark is requested with its rows
+    // Whether a row counts for the rates' gradient is a branch behind the row, with more states a lane a selection each, whose values need
+    // not be held so long (8 states 235 us, by selections 239; 20 states fp32 674 and 654).
+    constexpr bool kRowBranch = NS == 4;
     constexpr int kRow = CB + CB / E;                    // a row in LDS, padded: see scan_rows
     // A thread's eight values' parameters, 16 registers, come from LDS: those would spill (8 states 396 -> 330 us; four values' do not, and are held).
     constexpr bool kFromLds = E >= 8;
@@ -350,7 +353,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
                     const int t = part * kKept + k;
                     const float* before = k ? hs[k - 1] : h;
                     const bool own = row + t < q.n;       // of a row behind the piece, `before` is the last state, which may be infinite
-                    float r = 0.0f, s = 0.0f;
+                    float r = 0.0f, s = 0.0f, qs[kRowBranch ? NS : 1];
 #pragma unroll
                     for (int m = 0; m < NS / 4; ++m) {
                         const int step = (kKept - 1 - k) * (NS / 4) + m;
@@ -370,7 +373,8 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
                             const int i = 4 * m + j;
                             g[i] *= as[k][i];                      // what reaches the row before
                             const float qi = g[i] * before[i];
-                            if (own) da[i] = __builtin_fmaf(dv[k][0], qi, da[i]);
+                            if constexpr (kRowBranch) qs[i] = qi;
+                            else da[i] = own ? __builtin_fmaf(dv[k][0], qi, da[i]) : da[i];
                             r = i ? __builtin_fmaf(a2[i], qi, r) : a2[i] * qi;
                         }
                         across.put(step, vb, vc);
@@ -381,6 +385,13 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
                     }
                     group_sums<GL>(r, s);
                     rs[t][place] = Pair{r, s};
+                    if constexpr (kRowBranch) {
+                        if (own) {
+                            asm volatile("");           // (else the compiler makes selections of it)
+#pragma unroll
+                            for (int i = 0; i < NS; ++i) da[i] = __builtin_fmaf(dv[k][0], qs[i], da[i]);
+                        }
+                    }
                 }
                 across.take(kKept * (NS / 4) - 1, terms_of);
                 sum_bc[wave][part * kKept][across.which][across.template state<NS>(NS / 4 - 1)] = across.sum(terms_of);
