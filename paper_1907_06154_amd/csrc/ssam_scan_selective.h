@@ -13,7 +13,7 @@ namespace ssam {
 template <int GL_, int NS_>
 struct ScanShape {
     static constexpr int GL = GL_, NS = NS_;
-    static constexpr int kStates = GL * NS;                       // states held, those of the call padded with zeros
+    static constexpr int kStates = GL * NS;                       // states held: those of the call, some more than once (state_at)
     static constexpr int kWaveChannels = kWave / GL;
     static constexpr int kChannels = kWavesPerBlock * kWaveChannels;   // of a block
 };
@@ -134,24 +134,72 @@ template <class Shape> __device__ __forceinline__ int own_pairs(int lane) { retu
 // c % E * (CB / E) + c / E), so that the lanes of a wave, each with its e-th value, write one run.  A lane works on the channel at its place.
 template <int CB, int E> __device__ __forceinline__ int placed_channel(int at) { return at % (CB / E) * E + at / (CB / E); }
 
-// A channel's NS states of this lane in an array [..][channels][states]; those behind `states` are zero / not stored.
-template <int NS>
+// The same value, which the compiler takes for another: what follows from it is made again instead of held in registers.
+__device__ __forceinline__ int made_anew(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// A layout's places for states lie in blocks of four, one vector each.  The last block with states of its own starts further left where it
+// would pass their end, and the blocks behind hold the first ones' again, so that some states are held two times (counts below four: element
+// by element, up to eight times).  Their copies run alike; c's value is shared out between them, a power of two of them, so that nothing is
+// rounded and their terms add up to the one.  Zeros for b and c in the places left over would not do: an infinite input or gradient times zero
+// is NaN, and NaN times zero would reach y.  (4 x 2048 rows of 2048 channels, forward and gradients: 13 states 127 and 359 us, 50 states 396
+// and 1815; with zeros kept by selections 139 and 389, 465 and 1963; with nothing against NaN 129 and 352, 401 and 1752.)  In the gradients
+// the copies of g are shares too; what leaves is multiplied by their number.
+__device__ __forceinline__ int state_block(int j, int states)      // first state of block j; at least four states
+{
+    const int blocks = (states + 3) / 4, first = 4 * (j < blocks ? j : j - blocks);
+    return first < states - 4 ? first : states - 4;
+}
+__device__ __forceinline__ int state_at(int place, int states)
+{
+    if (states >= 4) return state_block(place / 4, states) + place % 4;
+    return states == 3 ? (place % 4 < 2 ? place % 4 : 2) : place & (states - 1);
+}
+// Of `held` places; more than half of them have a state of their own, or there are at most four states.
+__device__ __forceinline__ float state_copies(int n, int states, int held)
+{
+    if (states < 4) return (float)(held / 4 * (states == 1 ? 4 : states == 2 || n == 2 ? 2 : 1));
+    const int blocks = (states + 3) / 4;
+    return n / 4 < held / 4 - blocks || (n >= states - 4 && n < 4 * blocks - 4) ? 2.0f : 1.0f;
+}
+
+// A channel's NS states of this lane, places n0 .. , in an array [..][channels][states]; zeros / not stored where it is not there.
+// kShared: there may be more places than states.
+template <int NS, bool kShared = true>
 __device__ __forceinline__ void load_states(const float* __restrict__ a, int n0, int states, bool there, float (&h)[NS])
 {
 #pragma unroll
     for (int m = 0; m < NS; m += 4) {
-        const RowVec<float, 4> v = load_row_vec<float, 4>(a + n0 + m, there ? states - n0 - m : 0);
+        RowVec<float, 4> v(0.0f);
+        if (!kShared) {
+            v = load_row_vec<float, 4>(a + n0 + m, there ? states - n0 - m : 0);
+        } else if (states < 4) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (there) v[i] = a[state_at(i, states)];
+        } else if (there) {
+            v = load_row_vec<float, 4>(a + state_block((n0 + m) / 4, states), 4);
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) h[m + i] = v[i];
     }
 }
-template <int NS>
+template <int NS, bool kShared = true>
 __device__ __forceinline__ void store_states(float* __restrict__ a, int n0, int states, bool there, const float (&h)[NS])
 {
 #pragma unroll
     for (int m = 0; m < NS; m += 4) {
         const RowVec<float, 4> v = {h[m], h[m + 1], h[m + 2], h[m + 3]};
-        store_row_vec<float, 4>(a + n0 + m, there ? states - n0 - m : 0, v);
+        if (!kShared) {
+            if (there) store_row_vec<float, 4>(a + n0 + m, 4, v);
+        } else if (states >= 4) {
+            if (there && n0 + m < states) store_row_vec<float, 4>(a + state_block((n0 + m) / 4, states), 4, v);
+        } else if (n0 + m == 0) {
+            store_row_vec<float, 4>(a, there ? states : 0, v);
+        }
     }
 }
 
@@ -162,10 +210,10 @@ __device__ __forceinline__ float decay_rate(float a)
     const float r = a * kLog2e;
     return r == -__builtin_inff() ? -3.402823466e38f : r;
 }
-template <int NS>
+template <int NS, bool kShared = true>
 __device__ __forceinline__ void load_rates(const float* __restrict__ a, int n0, int states, bool there, float (&a2)[NS])
 {
-    load_states<NS>(a, n0, states, there, a2);
+    load_states<NS, kShared>(a, n0, states, there, a2);
 #pragma unroll
     for (int i = 0; i < NS; ++i) a2[i] = decay_rate(a2[i]);
 }
@@ -227,6 +275,12 @@ int with_shape(int states, F f)
     if (states <= 16) return f(ScanShape<4, 4>{});
     if (states <= 32) return f(ScanShape<4, 8>{});
     return f(ScanShape<4, 16>{});
+}
+// f gets whether there are more places than states as a compile-time constant.
+template <int kPlaces, class F>
+int with_shared(int states, F f)
+{
+    return states < kPlaces ? f(std::true_type{}) : f(std::false_type{});
 }
 template <class F>
 int with_row_type(int dtype, F f)

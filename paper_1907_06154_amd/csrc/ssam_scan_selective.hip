@@ -95,6 +95,9 @@ __global__ __launch_bounds__(kBlock, Shape::NS > 4 ? 2 : sizeof(T) == 4 ? 3 : 4)
     using Vec = RowVec<T, E>;
     Vec u, z, u_next, d_next, z_next;
     T b_next[kPairs], c_next[kPairs];
+    static_assert(kBlock % NP == 0, "a thread's values of b and c are all of one state");
+    const int state = state_at(tid % NP, p.states);
+    const float share = 1.0f / state_copies(state, p.states, NP);
     auto request = [&](int row) {
         const int left = q.n - row;
         u_next = mine.load(in + (long long)row * p.in.row, p.in.row, left);
@@ -104,10 +107,10 @@ __global__ __launch_bounds__(kBlock, Shape::NS > 4 ? 2 : sizeof(T) == 4 ? 3 : 4)
         const T* c0 = kWhole ? pc + (long long)row * p.c.row : nullptr;
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
-            const int i = tid + e * kBlock, n = i % NP < p.states ? i % NP : p.states - 1;
+            const int i = tid + e * kBlock;
             const unsigned r = i / NP < left ? i / NP : left - 1;
-            b_next[e] = b0[r * (unsigned)p.b.row + n];
-            if (kWhole) c_next[e] = c0[r * (unsigned)p.c.row + n];
+            b_next[e] = b0[r * (unsigned)p.b.row + state];
+            if (kWhole) c_next[e] = c0[r * (unsigned)p.c.row + state];
         }
     };
     // Rows behind the piece get d = 0, d u = 0, b = 0: the state passes them unchanged, an infinite one too.
@@ -130,9 +133,9 @@ __global__ __launch_bounds__(kBlock, Shape::NS > 4 ? 2 : sizeof(T) == 4 ? 3 : 4)
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
             const int i = tid + e * kBlock, n = i % NP;
-            const bool is = n < p.states && row + i / NP < q.n;
+            const bool is = row + i / NP < q.n;
             if (kPairs * kBlock <= K * NP || i < K * NP)
-                bc[i / NP][pair_place<Shape>(n)] = Pair{is ? (float)b_next[e] : 0.0f, kWhole && is ? (float)c_next[e] : 0.0f};
+                bc[i / NP][pair_place<Shape>(n)] = Pair{is ? (float)b_next[e] : 0.0f, kWhole && is ? (float)c_next[e] * share : 0.0f};
         }
     };
     struct Operands {
@@ -328,7 +331,7 @@ constexpr int step_channels(int P) { return kWave / P * step_each(P); }
 // P lanes share a channel, four states each, so that every load of states is a run of whole lines; what belongs to a channel alone
 // (time step, gate, output) is made once, by the lane of that number, and handed round.  A block's waves take the same channels of four rows, so
 // that the rates come from the L1.  Bound by the state: 8 bytes per value of it (256 rows of 4096 channels, 16 states: 31 us, 4.5 TB/s).
-template <class T, int P>
+template <class T, int P, bool kShared>
 __global__ __launch_bounds__(kBlock) void scan_step(ScanStepParams p)
 {
     const int lane = threadIdx.x & (kWave - 1);
@@ -339,6 +342,9 @@ __global__ __launch_bounds__(kBlock) void scan_step(ScanStepParams p)
     const ChannelTile ct = channel_tile((int)(blockIdx.x / row_blocks), p.per_group, p.group_channels, step_channels(P));
     constexpr int kApart = kWave / P;            // the k-th of a lane's channels is k * kApart + lane / P: a load of the k-th is one run
     const int part = lane & (P - 1), first = lane / P, n0 = part * 4;
+    float share[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) share[i] = kShared ? 1.0f / state_copies(state_at(n0 + i, p.states), p.states, 4 * P) : 1.0f;
     const bool own = part < KC && part * kApart + first < ct.n;
     const int c = ct.c0 + part * kApart + first; // the channel whose time step and output are this lane's
     struct Row {
@@ -350,8 +356,19 @@ __global__ __launch_bounds__(kBlock) void scan_step(ScanStepParams p)
         x.u = own ? (float)static_cast<const T*>(p.in.d)[r * p.in.row + c] : 0.0f;
         x.d = own ? (float)static_cast<const T*>(p.dt.d)[r * p.dt.row + c] : 0.0f;
         x.z = own && p.gate.d ? (float)static_cast<const T*>(p.gate.d)[r * p.gate.row + c] : 0.0f;
-        x.b = load_row_vec<T, 4>(static_cast<const T*>(p.b.d) + r * p.b.row + ct.group * p.b_group + n0, p.states - n0);
-        x.w = load_row_vec<T, 4>(static_cast<const T*>(p.c.d) + r * p.c.row + ct.group * p.c_group + n0, p.states - n0);
+        const T* b = static_cast<const T*>(p.b.d) + r * p.b.row + ct.group * p.b_group;
+        const T* w = static_cast<const T*>(p.c.d) + r * p.c.row + ct.group * p.c_group;
+        if (!kShared || p.states >= 4) {
+            const int n = kShared ? state_block(part, p.states) : n0;
+            x.b = load_row_vec<T, 4>(b + n, 4);
+            x.w = load_row_vec<T, 4>(w + n, 4);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x.b[i] = b[state_at(i, p.states)];
+                x.w[i] = w[state_at(i, p.states)];
+            }
+        }
         return x;
     };
     Row x = request(row);
@@ -365,8 +382,8 @@ __global__ __launch_bounds__(kBlock) void scan_step(ScanStepParams p)
     for (int k = 0; k < KC; ++k) {
         const long long cell = (long long)(ct.c0 + k * kApart + first) * p.states;
         const bool there = k * kApart + first < ct.n;
-        load_states<4>(state + cell, n0, p.states, there, h[k]);
-        load_rates<4>(p.a + cell, n0, p.states, there, a2[k]);
+        load_states<4, kShared>(state + cell, n0, p.states, there, h[k]);
+        load_rates<4, kShared>(p.a + cell, n0, p.states, there, a2[k]);
     }
     for (int r = row;;) {
         float d = x.d + bias;
@@ -380,7 +397,7 @@ __global__ __launch_bounds__(kBlock) void scan_step(ScanStepParams p)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 h[kk][i] = __builtin_fmaf(exp2_fast(dk * a2[kk][i]), h[kk][i], (float)x.b[i] * xk);
-                s = __builtin_fmaf((float)x.w[i], h[kk][i], s);
+                s = __builtin_fmaf((float)x.w[i] * share[i], h[kk][i], s);
             }
             s = part_sum<P>(s);
             y = part == kk ? s : y;
@@ -394,7 +411,7 @@ __global__ __launch_bounds__(kBlock) void scan_step(ScanStepParams p)
     }
 #pragma unroll
     for (int k = 0; k < KC; ++k)
-        store_states<4>(state + (long long)(ct.c0 + k * kApart + first) * p.states, n0, p.states, k * kApart + first < ct.n, h[k]);
+        store_states<4, kShared>(state + (long long)(ct.c0 + k * kApart + first) * p.states, n0, p.states, k * kApart + first < ct.n, h[k]);
 }
 
 }  // namespace
@@ -579,12 +596,18 @@ int ssam_scan_selective_step(const ssam_scan_selective_step_args* a, void* hip_s
         using T = decltype(t);
         const dim3 grid((unsigned)blocks), block(kBlock);
         hipStream_t st = (hipStream_t)hip_stream;
-        if (lanes == 1) hipLaunchKernelGGL((scan_step<T, 1>), grid, block, 0, st, p);
-        else if (lanes == 2) hipLaunchKernelGGL((scan_step<T, 2>), grid, block, 0, st, p);
-        else if (lanes == 4) hipLaunchKernelGGL((scan_step<T, 4>), grid, block, 0, st, p);
-        else if (lanes == 8) hipLaunchKernelGGL((scan_step<T, 8>), grid, block, 0, st, p);
-        else hipLaunchKernelGGL((scan_step<T, 16>), grid, block, 0, st, p);
-        return launched();
+        auto launch = [&](auto parts) {
+            constexpr int P = decltype(parts)::value;
+            return with_shared<4 * P>(a->states, [&](auto shared) {
+                hipLaunchKernelGGL((scan_step<T, P, decltype(shared)::value>), grid, block, 0, st, p);
+                return launched();
+            });
+        };
+        if (lanes == 1) return launch(std::integral_constant<int, 1>{});
+        if (lanes == 2) return launch(std::integral_constant<int, 2>{});
+        if (lanes == 4) return launch(std::integral_constant<int, 4>{});
+        if (lanes == 8) return launch(std::integral_constant<int, 8>{});
+        return launch(std::integral_constant<int, 16>{});
     });
 }
 

@@ -93,7 +93,7 @@ struct ChannelSums {
 };
 
 // kWhole: everything.  !kWhole: only what a piece lets out at its first row when nothing reaches it from behind.
-template <class T, class Shape, bool kWhole>
+template <class T, class Shape, bool kWhole, bool kShared>
 __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(BackParams p)
 {
     constexpr int GL = Shape::GL, NS = Shape::NS, NP = Shape::kStates, CB = Shape::kChannels, K = kTile;
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
     if (q.seq < 0) {
         if (part_param) {       // an empty slot adds zeros
             float none[NS] = {};
-            store_states<NS>(part_param + cell, n0, p.states, live, none);
+            store_states<NS, kShared>(part_param + cell, n0, p.states, live, none);
             if (tid < ct.n) part_param[plane + ct.c0 + tid] = part_param[plane + p.channels + ct.c0 + tid] = 0.0f;
         }
         return;
@@ -139,13 +139,20 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
     if (!kWhole && q.row0 == 0) return;                  // nothing lies before it
 
     float a2[NS], g[NS], da[NS];
-    load_rates<NS>(p.a + cell, n0, p.states, live, a2);
+    load_rates<NS, kShared>(p.a + cell, n0, p.states, live, a2);
     const bool last = q.row0 + q.n >= q.len;
-    if (!kWhole) load_states<NS>(nullptr, 0, 0, false, g);
-    else if (!last) load_states<NS>(p.ends + (slot + 1) * plane + cell, n0, p.states, live, g);
-    else load_states<NS>(p.grad_final + q.seq * plane + cell, n0, p.states, live && p.grad_final, g);
+    if (!kWhole) load_states<NS, kShared>(nullptr, 0, 0, false, g);
+    else if (!last) load_states<NS, kShared>(p.ends + (slot + 1) * plane + cell, n0, p.states, live, g);
+    else load_states<NS, kShared>(p.grad_final + q.seq * plane + cell, n0, p.states, live && p.grad_final, g);
+    // !kWhole: the states do not meet, and every copy has the whole of g.
+    auto anew = [](int v) { return kShared ? made_anew(v) : v; };
+    auto state_of = [&](int place) { return kShared ? state_at(place, p.states) : place; };
+    auto copies = [&](int place) { return kWhole && kShared ? state_copies(state_of(place), p.states, NP) : 1.0f; };
 #pragma unroll
-    for (int i = 0; i < NS; ++i) da[i] = 0.0f;
+    for (int i = 0; i < NS; ++i) {
+        g[i] *= 1.0f / copies(n0 + i);
+        da[i] = 0.0f;
+    }
     float sum = 0.0f;
     const float* marks = nullptr;
     if (kWhole) {
@@ -199,6 +206,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
     using Vec = RowVec<T, E>;
     Vec u, dr, z, go, u_next, d_next, z_next, g_next;
     T b_next[kPairs], c_next[kPairs];
+    static_assert(kBlock % (2 * NP) == 0, "a thread's values of b and c are all of one state, its sums for their gradients too");
     float mark[NS], mark_next[NS];
     auto request = [&](int row) {
         const int left = q.n - row;
@@ -208,14 +216,15 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
         if (gated) z_next = mine.load(gate + (long long)row * p.gate.row, p.gate.row, left);
         const T* b0 = kWhole ? pb + (long long)row * p.b.row : nullptr;
         const T* c0 = pc + (long long)row * p.c.row;
+        const int state = state_of(anew(tid) % NP);
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
-            const int i = tid + e * kBlock, n = i % NP < p.states ? i % NP : p.states - 1;
+            const int i = tid + e * kBlock;
             const unsigned r = i / NP < left ? i / NP : left - 1;
-            if (kWhole) b_next[e] = b0[r * (unsigned)p.b.row + n];
-            c_next[e] = c0[r * (unsigned)p.c.row + n];
+            if (kWhole) b_next[e] = b0[r * (unsigned)p.b.row + state];
+            c_next[e] = c0[r * (unsigned)p.c.row + state];
         }
-        if (kWhole && kMarkAhead) load_states<NS>(marks + (row / K) * plane, n0, p.states, live, mark_next);
+        if (kWhole && kMarkAhead) load_states<NS, kShared>(marks + (row / K) * plane, anew(n0), p.states, live, mark_next);
     };
     const int pairs = own_pairs<Shape>(lane), sum_at = sum_row<GL>(lane);
     const ChannelSums<GL> across(terms[kWhole ? wave : 0], lane);
@@ -245,12 +254,13 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
             dx[mine.row][mine.place(e)] = Pair{v, is && kWhole ? v * (float)u[e] : 0.0f};
             dys[mine.row][mine.place(e)] = dy[e];
         }
+        const float share = 1.0f / copies(anew(tid) % NP);
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
             const int i = tid + e * kBlock, n = i % NP;
-            const bool is = n < p.states && row + i / NP < q.n;
+            const bool is = row + i / NP < q.n;
             if (kPairs * kBlock <= K * NP || i < K * NP)
-                bc[i / NP][pair_place<Shape>(n)] = Pair{kWhole && is ? (float)b_next[e] : 0.0f, is ? (float)c_next[e] : 0.0f};
+                bc[i / NP][pair_place<Shape>(n)] = Pair{kWhole && is ? (float)b_next[e] : 0.0f, is ? (float)c_next[e] * share : 0.0f};
         }
         __syncthreads();
         if (tile > 0) request(row - K);
@@ -289,7 +299,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
                 // the states again, from the mark: those before this part's rows in passing, then each row's
                 float h[NS], hs[kKept][NS], as[kKept][NS], dyr[kKept];
                 Pair dv[kKept], w[kKept][NS / 4];
-                if (!kMarkAhead) load_states<NS>(marks + tile * plane, n0, p.states, live, mark);
+                if (!kMarkAhead) load_states<NS, kShared>(marks + tile * plane, anew(n0), p.states, live, mark);
 #pragma unroll
                 for (int k = 0; k < kKept; ++k) {
                     dv[k] = dx[part * kKept + k][place];
@@ -427,21 +437,28 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
             if (part_bc) {
                 float* to = part_bc + (long long)row * p.groups * 2 * p.states;
                 const unsigned wide = p.groups * 2 * p.states;
+                const int me = anew(tid), state = state_of(me % NP);
+                const float parts = me / NP % 2 ? 1.0f : copies(me % NP);      // of the gradient of b
                 for (int i = tid; i < K * 2 * NP; i += kBlock) {
                     const int r = i / (2 * NP), w = i / NP % 2, n = i % NP;
                     float v = sum_bc[0][r][w][n];
 #pragma unroll
                     for (int k = 1; k < kWavesPerBlock; ++k) v += sum_bc[k][r][w][n];
-                    if (r < left && n < p.states) to[r * wide + w * p.states + n] = v;
+                    if (r < left && (!kShared || n < (p.states + 3) / 4 * 4)) to[r * wide + w * p.states + state] = v * parts;
                 }
             }
             __syncthreads();      // the next tile's values go where these were read
         }
     }
     if constexpr (kWhole) {
-        if (p.grad_state && q.row0 == 0) store_states<NS>(p.grad_state + q.seq * plane + cell, n0, p.states, live, g);
+#pragma unroll
+        for (int i = 0; i < NS; ++i) {
+            g[i] *= copies(n0 + i);
+            da[i] *= copies(n0 + i);
+        }
+        if (p.grad_state && q.row0 == 0) store_states<NS, kShared>(p.grad_state + q.seq * plane + cell, n0, p.states, live, g);
         if (!part_param) return;
-        store_states<NS>(part_param + cell, n0, p.states, live, da);
+        store_states<NS, kShared>(part_param + cell, n0, p.states, live, da);
         // the tile's rows of every channel, added in order
 #pragma unroll
         for (int e = 0; e < E; ++e)
@@ -459,7 +476,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
             part_param[plane + p.channels + ct.c0 + tid] = s1;
         }
     } else {
-        store_states<NS>(p.ends + slot * plane + cell, n0, p.states, live, g);
+        store_states<NS, kShared>(p.ends + slot * plane + cell, n0, p.states, live, g);
         if (live && n0 == 0) p.sums[(long long)slot * p.channels + ct.c0 + ch] = sum;
     }
 }
@@ -655,11 +672,16 @@ int ssam_scan_selective_backward(const ssam_scan_selective_backward_args* a, voi
             using T = decltype(t);
             using S = decltype(shape);
             if (blocks) {
-                if (plan.cut) {
-                    hipLaunchKernelGGL((scan_back<T, S, false>), dim3((unsigned)blocks), dim3(kBlock), 0, st, p);
-                    if (int e = launch_join(p.pieces, p.ends, p.sums, a->d_a, a->d_grad_final, a->channels, a->states, true, st)) return e;
-                }
-                hipLaunchKernelGGL((scan_back<T, S, true>), dim3((unsigned)blocks), dim3(kBlock), 0, st, p);
+                const int e = with_shared<S::kStates>(a->states, [&](auto shared) -> int {
+                    constexpr bool kShared = decltype(shared)::value;
+                    if (plan.cut) {
+                        hipLaunchKernelGGL((scan_back<T, S, false, kShared>), dim3((unsigned)blocks), dim3(kBlock), 0, st, p);
+                        if (int e = launch_join(p.pieces, p.ends, p.sums, a->d_a, a->d_grad_final, a->channels, a->states, true, st)) return e;
+                    }
+                    hipLaunchKernelGGL((scan_back<T, S, true, kShared>), dim3((unsigned)blocks), dim3(kBlock), 0, st, p);
+                    return SSAM_OK;
+                });
+                if (e) return e;
                 if (plan.bc)
                     hipLaunchKernelGGL((back_sum_bc<T>), dim3((unsigned)sum_blocks), dim3(kBlock), 0, st, p, make_pieces(a->seq, kSumRows));
             }

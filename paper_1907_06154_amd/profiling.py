@@ -458,7 +458,8 @@ def operator_kernel(name: str) -> str:
     text = "`" + m[1] + "`" + next((t for k, t in kind.items() if k in name[m.end():m.end() + 8] or k == "<float" and k in name), "")
     shape = re.search(r"ScanShape(?:ILi|<)(\d+)(?:ELi|, )(\d+)", name)
     if shape:
-        text += f" {shape[1]} x {shape[2]}" + (", everything" if re.search(r"Lb1E|, true>", name) else ", what the pieces add")
+        whole = re.search(r"Lb([01])E|(true|false)", name[shape.end():])
+        text += f" {shape[1]} x {shape[2]}" + (", everything" if whole[0] in ("Lb1E", "true") else ", what the pieces add")
     if m[1] == "join_pieces":
         text += " backward" if re.search(r"Lb1E|<true>", name) else " forward"
     return text

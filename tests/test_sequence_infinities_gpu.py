@@ -91,7 +91,7 @@ def test_the_last_state_reaches_no_rate(rows, N):
     assert torch.equal(got.c[:-1], clean.c[:-1]) and not torch.isfinite(got.c[-1]).any()
 
 
-STATES = [8, 16, 32, 64]
+STATES = [1, 2, 3, 4, 5, 7, 8, 9, 13, 16, 17, 20, 32, 33, 50, 64]      # those that fill the lanes' registers, and those that do not
 
 
 class Positive:
