@@ -203,12 +203,12 @@ __device__ __forceinline__ void store_states(float* __restrict__ a, int n0, int 
     }
 }
 
-// A decay rate for exp2.  -inf (a state that forgets at once) becomes the lowest finite value, so that a time step of zero leaves
-// the state alone there too: rows behind a sequence pass as such.
+// A decay rate for exp2.  An infinity (-inf: a state that forgets at once) becomes the last finite value, so that a time step of zero
+// leaves the state alone there too: rows behind a sequence pass as such.
 __device__ __forceinline__ float decay_rate(float a)
 {
     const float r = a * kLog2e;
-    return r == -__builtin_inff() ? -3.402823466e38f : r;
+    return __builtin_fabsf(r) == __builtin_inff() ? __builtin_copysignf(3.402823466e38f, r) : r;
 }
 template <int NS, bool kShared = true>
 __device__ __forceinline__ void load_rates(const float* __restrict__ a, int n0, int states, bool there, float (&a2)[NS])

@@ -182,3 +182,19 @@ def test_an_infinite_gradient_and_an_infinite_state_on_the_way_back(N):
         got.dt[t:, at] = clean.dt[t:, at]
         assert torch.equal(got.dt, clean.dt) and torch.equal(got.x, clean.x)
         assert (got.c[t:] == INF).all() and torch.equal(got.c[:t], clean.c[:t])
+
+
+@pytest.mark.parametrize("rate", [INF, 3e38, -INF, -3e38])
+def test_an_infinite_rate_passes_the_end_of_its_sequence(rate):
+    """A state behind the last row is that of the last row, whatever its rate."""
+    for rows in (5, 16, 33):
+        k = Positive(rows, 16, torch.float32)
+        h, last = torch.ones(1, *k.a.shape, device="cuda"), torch.empty(1, *k.a.shape, device="cuda")
+        k.forward(d_state=h, d_final=last)
+        clean = last.clone()
+        k.a[11, 3] = rate
+        k.forward(d_state=h, d_final=last)
+        want = INF if rate > 0 else (k.dt[-1, 11] * k.x[-1, 11] * k.b[-1, 0, 3]).item()
+        assert last[0, 11, 3].item() == want
+        last[0, 11, 3] = clean[0, 11, 3]
+        assert torch.equal(last, clean)
