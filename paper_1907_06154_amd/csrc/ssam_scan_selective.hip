@@ -257,7 +257,10 @@ __global__ __launch_bounds__(kBlock) void join_pieces(Pieces pc, float* ends, co
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
             if (k + j >= n - 1) break;
-            e[j] = h = __builtin_fmaf(exp2_fast(a2 * s[j]), h, e[j]);
+            // The decay of many rows may come out as 0 though no row's is: an infinity passes it as it passes them.
+            const float x = a2 * s[j], decay = exp2_fast(x);
+            const bool passes = __builtin_fabsf(h) == __builtin_inff() && x > -__builtin_inff();
+            e[j] = h = __builtin_fmaf(passes ? __builtin_fmaxf(decay, 0x1p-126f) : decay, h, e[j]);
         }
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j)

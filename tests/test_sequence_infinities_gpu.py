@@ -198,3 +198,27 @@ def test_an_infinite_rate_passes_the_end_of_its_sequence(rate):
         assert last[0, 11, 3].item() == want
         last[0, 11, 3] = clean[0, 11, 3]
         assert torch.equal(last, clean)
+
+
+@pytest.mark.parametrize("N", [4, 8, 13, 16, 32, 64])
+def test_an_infinite_state_passes_pieces(N):
+    """Each row's decay is above zero, a piece's is not: an infinite state, or gradient, times it stays infinite all the same."""
+    rows, at = 300, 11
+    k = Positive(rows, N, torch.float32)
+    k.a = -30 * torch.ones_like(k.a)
+    k.dt = k.dt.clamp(min=0.12)
+    assert ssam.ssam_scan_selective_workspace_bytes(k.x, k.a) > 0         # it is cut
+    assert (k.dt.max() * 30 < 80) and (k.dt[:32].sum(0) * 30 > 110).all()
+    there = k.x[7, at].item()
+    k.x[7, at] = INF
+    last = torch.empty(1, *k.a.shape, device="cuda")
+    out = k.forward(d_final=last)
+    assert (out[7:, at] == INF).all() and (last[0, at] == INF).all()
+    out[7:, at], last[0, at] = 0, 0
+    assert torch.isfinite(out).all() and torch.isfinite(last).all()
+    k.x[7, at] = there
+    k.dy[290, at] = INF
+    got = k.back(k.marked())
+    assert (got.x[:291, at] == INF).all() and (got.state[0, at] == INF).all()
+    got.x[:291, at], got.state[0, at] = 0, 0
+    assert torch.isfinite(got.x).all() and torch.isfinite(got.state).all()
