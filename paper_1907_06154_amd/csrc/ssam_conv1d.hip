@@ -452,9 +452,12 @@ int piece_rows(const ssam_sequences& q, int strips, int longest)
 int back_piece_rows(const ssam_conv1d_backward_args& a) { return piece_rows(a.seq, strips_of(a.channels, kBackChan), 64); }
 long long back_parts(const ssam_conv1d_backward_args& a) { return (piece_slots(a.seq, back_piece_rows(a)) + kWavesPerBlock - 1) / kWavesPerBlock; }
 
+// Blocks of the march: more than a launch holds are refused, and need no workspace.
+long long back_blocks(const ssam_conv1d_backward_args& a) { return back_parts(a) * strips_of(a.channels, kBackChan); }
+
 size_t back_bytes(const ssam_conv1d_backward_args& a)
 {
-    if (!a.d_grad_weight && !a.d_grad_bias) return 0;
+    if ((!a.d_grad_weight && !a.d_grad_bias) || back_blocks(a) > kMaxGrid) return 0;
     return (size_t)back_parts(a) * (a.taps + 1) * a.channels * sizeof(float);
 }
 
@@ -472,7 +475,7 @@ int ssam_conv1d(const ssam_conv1d_args* a, void* hip_stream)
     if (a->seq.sequences == 0) return SSAM_OK;
     const int esz = type_bytes(a->dtype), psz = type_bytes(a->param_dtype);
     if (!a->d_weight) return SSAM_ERR_NULL;
-    if (int e = check_rows(a->in, a->seq, esz, false)) return e;
+    if (int e = check_rows(a->in, a->seq, a->channels, esz, false)) return e;
     if (int e = check_out_rows(a->out, a->seq, a->channels, esz, false)) return e;
     if (misaligned(a->d_weight, psz) || misaligned(a->d_bias, psz) || misaligned(a->d_state, esz) || misaligned(a->d_final, esz)) return SSAM_ERR_DIM;
     const long long state_bytes = (long long)a->seq.sequences * (a->taps - 1) * a->channels * esz;
@@ -522,8 +525,8 @@ int ssam_conv1d_backward(const ssam_conv1d_backward_args* a, void* hip_stream)
     const bool none = a->seq.sequences == 0;
     if (none && !sums) return SSAM_OK;
     if (!a->d_weight) return SSAM_ERR_NULL;
-    if (int e = check_rows(a->in, a->seq, esz, false)) return e;
-    if (int e = check_rows(a->grad_out, a->seq, esz, false)) return e;
+    if (int e = check_rows(a->in, a->seq, a->channels, esz, false)) return e;
+    if (int e = check_rows(a->grad_out, a->seq, a->channels, esz, false)) return e;
     if (int e = check_out_rows(a->grad_in, a->seq, a->channels, esz, true)) return e;
     if (misaligned(a->d_weight, psz) || misaligned(a->d_bias, psz) || misaligned(a->d_state, esz) || misaligned(a->d_grad_final, esz) ||
         misaligned(a->d_grad_weight, psz) || misaligned(a->d_grad_bias, psz) || misaligned(a->d_grad_state, esz))
@@ -556,7 +559,7 @@ int ssam_conv1d_backward(const ssam_conv1d_backward_args* a, void* hip_stream)
     p.silu = a->silu != 0;
     p.params_f32 = a->param_dtype == SSAM_F32;
     p.slots = piece_slots(a->seq, piece);
-    const long long parts = back_parts(*a), blocks = parts * p.strips;
+    const long long parts = back_parts(*a), blocks = back_blocks(*a);
     const long long sum_blocks = (long long)((a->channels + kWave - 1) / kWave) * (a->taps + 1);
     if (blocks > kMaxGrid || sum_blocks > kMaxGrid / 4) return SSAM_ERR_DIM;
     hipStream_t st = (hipStream_t)hip_stream;
@@ -579,11 +582,11 @@ int ssam_conv1d_step(const ssam_conv1d_step_args* a, void* hip_stream)
     const int esz = type_bytes(a->dtype), psz = type_bytes(a->param_dtype);
     const ssam_sequences q{1, a->rows, nullptr, nullptr};
     if (!a->d_weight || (!a->d_state && a->taps > 1)) return SSAM_ERR_NULL;
-    if (int e = check_rows(a->in, q, esz, false)) return e;
+    if (int e = check_rows(a->in, q, a->channels, esz, false)) return e;
     if (int e = check_out_rows(a->out, q, a->channels, esz, false)) return e;
     const long long slot = (long long)(a->taps - 1) * a->channels;
-    if (misaligned(a->d_weight, psz) || misaligned(a->d_bias, psz) || misaligned(a->d_state, esz) || a->slot_stride < slot || a->slot_stride > kMaxStride)
-        return SSAM_ERR_DIM;
+    if (int e = check_pool(a->slots, a->slot_stride, slot)) return e;
+    if (misaligned(a->d_weight, psz) || misaligned(a->d_bias, psz) || misaligned(a->d_state, esz)) return SSAM_ERR_DIM;
     const Cover outs[] = {cover_rows(a->out, q, a->channels, esz), cover_slots(a->d_state, a->slots, a->slot_stride, slot, esz)};
     const Cover ins[] = {cover_rows(a->in, q, a->channels, esz), cover_plain(a->d_weight, (long long)a->channels * a->taps * psz),
                          cover_plain(a->d_bias, (long long)a->channels * psz), cover_plain(a->d_slots, (long long)a->rows * 4)};

@@ -10,11 +10,6 @@
 
 namespace ssam {
 
-template <int CODE> struct RowTypeOf;
-template <> struct RowTypeOf<SSAM_F32> { using type = float; };
-template <> struct RowTypeOf<SSAM_F16> { using type = _Float16; };
-template <> struct RowTypeOf<SSAM_BF16> { using type = __bf16; };
-
 // V adjacent channels of a row, as they are in memory.
 template <class T, int V> using RowVec = T __attribute__((ext_vector_type(V)));
 
@@ -236,9 +231,21 @@ private:
 inline int type_bytes(int dtype) { return dtype == SSAM_F32 ? 4 : dtype == SSAM_F16 || dtype == SSAM_BF16 ? 2 : 0; }
 
 constexpr long long kMaxChannels = 1 << 24;
-constexpr long long kMaxStride = 1LL << 40;      // elements: offsets of any row then fit 64 bits
+constexpr long long kMaxStride = 1LL << 40;      // elements from row to row, sequence to sequence, group to group, slot to slot
+constexpr long long kMaxExtent = 1LL << 59;      // elements from a tensor's first to behind its last: offsets and bytes then fit 64 bits
 constexpr long long kMaxRows = 1LL << 40;        // of a batch: their products with tiles of channels then fit 64 bits
 constexpr long long kMaxTileStride = 1 << 24;    // elements from row to row where a tile's offsets (32 rows of 4 bytes) have 32 bits
+
+// Sums and products of what the caller says, held to 2^62.
+inline long long held_to_62(__int128 v) { return v > (1LL << 62) ? 1LL << 62 : (long long)v; }
+inline long long product(long long a, long long b) { return held_to_62((__int128)a * b); }
+// `count` runs of `width` elements, `step` apart.
+inline long long run_extent(long long count, long long step, long long width) { return held_to_62((__int128)(count - 1) * step + width); }
+inline long long rows_extent(const ssam_rows& r, const ssam_sequences& q, long long width)
+{
+    const long long rows = run_extent(q.rows, r.row, width);
+    return q.d_begin ? rows : run_extent(q.sequences, r.batch, rows);
+}
 
 // What a tensor covers: `count` rows (batch after batch) of `width` bytes, `step` bytes apart; one = a plain range.
 struct Cover {
@@ -253,13 +260,9 @@ inline Cover cover_rows(const ssam_rows& r, const ssam_sequences& q, long long w
 {
     if (!r.d || q.sequences <= 0 || q.rows <= 0) return Cover{(uintptr_t)r.d, 0, 0, 0};
     const long long width = width_elems * esz;
-    long long last = (long long)(q.rows - 1) * r.row * esz;
     bool comb = r.row * esz >= width;
-    if (!q.d_begin && q.sequences > 1) {
-        last += (long long)(q.sequences - 1) * r.batch * esz;
-        comb = comb && r.row > 0 && r.batch % r.row == 0;      // every row of every sequence lies on the same comb
-    }
-    return Cover{(uintptr_t)r.d, last + width, comb ? r.row * esz : 0, width};
+    if (!q.d_begin && q.sequences > 1) comb = comb && r.row > 0 && r.batch % r.row == 0;      // every row of every sequence lies on the same comb
+    return Cover{(uintptr_t)r.d, rows_extent(r, q, width_elems) * esz, comb ? r.row * esz : 0, width};
 }
 
 inline bool overlaps(const Cover& a, const Cover& b)
@@ -274,12 +277,13 @@ inline bool overlaps(const Cover& a, const Cover& b)
     return true;
 }
 
-// 0: fine, otherwise the error.  `optional`: a NULL tensor is fine.
-inline int check_rows(const ssam_rows& r, const ssam_sequences& q, int esz, bool optional)
+// 0: fine, otherwise the error.  `width`: elements of a row; `optional`: a NULL tensor is fine.
+inline int check_rows(const ssam_rows& r, const ssam_sequences& q, long long width, int esz, bool optional)
 {
-    if (!r.d) return optional || q.sequences == 0 || q.rows == 0 ? SSAM_OK : SSAM_ERR_NULL;
+    const bool empty = q.sequences == 0 || q.rows == 0;
+    if (!r.d) return optional || empty ? SSAM_OK : SSAM_ERR_NULL;
     if ((uintptr_t)r.d % esz || r.row < 0 || r.row > kMaxStride || (!q.d_begin && (r.batch < 0 || r.batch > kMaxStride))) return SSAM_ERR_DIM;
-    return SSAM_OK;
+    return !empty && rows_extent(r, q, width) > kMaxExtent ? SSAM_ERR_DIM : SSAM_OK;
 }
 
 // Rows that are read and written in tiles.
@@ -288,7 +292,7 @@ inline int check_tile_rows(const ssam_rows& r, const ssam_sequences& q) { return
 // A result's rows must not share elements with one another either.
 inline int check_out_rows(const ssam_rows& r, const ssam_sequences& q, long long width, int esz, bool optional)
 {
-    if (int e = check_rows(r, q, esz, optional)) return e;
+    if (int e = check_rows(r, q, width, esz, optional)) return e;
     if (!r.d) return SSAM_OK;
     if (q.rows > 1 && r.row < width) return SSAM_ERR_DIM;
     if (!q.d_begin && q.sequences > 1) {
@@ -312,10 +316,15 @@ inline int check_slots(int rows, int slots, const int* d_slots)
 {
     return rows < 0 || rows > SSAM_MAX_EXTENT || slots < 0 || slots > SSAM_MAX_EXTENT || (uintptr_t)d_slots % 4 ? SSAM_ERR_DIM : SSAM_OK;
 }
+// A pool of slots of `slot` elements, `stride` apart.
+inline int check_pool(int slots, long long stride, long long slot)
+{
+    return stride < slot || stride > kMaxStride || (slots > 0 && run_extent(slots, stride, slot) > kMaxExtent) ? SSAM_ERR_DIM : SSAM_OK;
+}
 
 inline Cover cover_slots(const void* p, int slots, long long stride, long long slot, int esz)
 {
-    return cover_plain(p, slots > 0 && slot > 0 ? ((slots - 1) * stride + slot) * esz : 0);
+    return cover_plain(p, slots > 0 && slot > 0 ? run_extent(slots, stride, slot) * esz : 0);
 }
 
 template <int NA, int NB>

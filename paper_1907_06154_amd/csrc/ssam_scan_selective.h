@@ -307,7 +307,16 @@ inline int tiles_per_group(int channels, int states, int groups)
 }
 
 // b and c: groups x states elements, `apart` from group to group.
-inline long long group_width(int groups, int states, long long apart) { return (groups - 1) * apart + states; }
+inline long long group_width(int groups, int states, long long apart) { return run_extent(groups, apart, states); }
+
+// b and c of a call, whichever.
+template <class Args>
+int check_group_rows(const Args& a, const ssam_sequences& q, int esz)
+{
+    if (a.b_group < 0 || a.b_group > kMaxStride || a.c_group < 0 || a.c_group > kMaxStride) return SSAM_ERR_DIM;
+    if (int e = check_rows(a.b, q, group_width(a.groups, a.states, a.b_group), esz, false)) return e;
+    return check_rows(a.c, q, group_width(a.groups, a.states, a.c_group), esz, false);
+}
 
 // ---- sequences in pieces ------------------------------------------------------------------------------------------------
 // Rows of a piece, a multiple of 32, so that sequences x channel tiles x pieces come to about `blocks` blocks; one piece a sequence

@@ -270,9 +270,9 @@ __global__ __launch_bounds__(kBlock) void join_pieces(Pieces pc, float* ends, co
 
 struct Plan {
     int tiles, piece;
-    long long slots;
+    long long slots, blocks;
     bool cut;              // sequences may be more than one piece
-    size_t ends, bytes;    // bytes of the pieces' states, and of the whole workspace
+    size_t ends, bytes;    // bytes of the pieces' states, and of the whole workspace (none for more blocks than a launch holds, which are refused)
 };
 
 Plan plan_of(const ssam_scan_selective_args& a)
@@ -281,7 +281,8 @@ Plan plan_of(const ssam_scan_selective_args& a)
     p.tiles = tiles_per_group(a.channels, a.states, a.groups) * a.groups;
     p.piece = scan_piece_rows(a.seq, p.tiles, kBlocks, kAlone);
     p.slots = piece_slots(a.seq, p.piece);
-    p.cut = a.seq.rows > p.piece;
+    p.blocks = p.slots * p.tiles;
+    p.cut = a.seq.rows > p.piece && p.blocks <= kMaxGrid;
     p.ends = p.cut ? (size_t)p.slots * a.channels * a.states * sizeof(float) : 0;
     p.bytes = p.cut ? p.ends + (size_t)p.slots * a.channels * sizeof(float) : 0;
     return p;
@@ -429,7 +430,7 @@ int scan_piece_rows(const ssam_sequences& q, int tiles, int blocks, int alone)
     // 16384 rows of 4096 channels: 446, 465 with 1.5 times as many), and are too many where there are not (64 in 8192 rows of 4096
     // channels with 1.5 times: 237, 206 without).
     if (q.d_begin && whole < blocks) blocks *= 2;
-    long long piece = (total * tiles + blocks - 1) / blocks;
+    long long piece = (product(total, tiles) + blocks - 1) / blocks;
     if (q.rows <= kWhole) piece = kWhole;
     else if (!q.d_begin && whole >= alone) piece = q.rows;
     piece = (piece + 31) / 32 * 32;
@@ -473,13 +474,13 @@ int ssam_scan_selective(const ssam_scan_selective_args* a, void* hip_stream)
     if (a->seq.sequences == 0) return SSAM_OK;
     const int esz = type_bytes(a->dtype);
     if (!a->d_a) return SSAM_ERR_NULL;
-    for (const ssam_rows* r : {&a->in, &a->dt, &a->b, &a->c})
-        if (int e = check_rows(*r, a->seq, esz, false)) return e;
-    if (int e = check_rows(a->gate, a->seq, esz, true)) return e;
+    if (int e = check_group_rows(*a, a->seq, esz)) return e;
+    for (const ssam_rows* r : {&a->in, &a->dt})
+        if (int e = check_rows(*r, a->seq, a->channels, esz, false)) return e;
+    if (int e = check_rows(a->gate, a->seq, a->channels, esz, true)) return e;
     if (int e = check_out_rows(a->out, a->seq, a->channels, esz, false)) return e;
     for (const ssam_rows* r : {&a->in, &a->dt, &a->gate, &a->out, &a->b, &a->c})
         if (int e = check_tile_rows(*r, a->seq)) return e;
-    if (a->b_group < 0 || a->b_group > kMaxStride || a->c_group < 0 || a->c_group > kMaxStride) return SSAM_ERR_DIM;
     for (const void* f : {(const void*)a->d_a, (const void*)a->d_skip, (const void*)a->d_dt_bias, (const void*)a->d_state, (const void*)a->d_final,
                           (const void*)a->d_marks})
         if ((uintptr_t)f % 4) return SSAM_ERR_DIM;
@@ -487,9 +488,11 @@ int ssam_scan_selective(const ssam_scan_selective_args* a, void* hip_stream)
     if (plan.bytes && !a->d_work) return SSAM_ERR_NULL;
     if (plan.bytes && (a->work_bytes < plan.bytes || (uintptr_t)a->d_work % 16)) return SSAM_ERR_DIM;
     const long long plane = (long long)a->channels * a->states * 4, state_bytes = a->seq.sequences * plane;
+    const long long mark_bytes = product(piece_slots(a->seq, SSAM_MARK_ROWS), plane);
+    if (a->d_marks && mark_bytes > 4 * kMaxExtent) return SSAM_ERR_DIM;
     const Cover state = cover_plain(a->d_state, state_bytes);
     const Cover outs[] = {cover_rows(a->out, a->seq, a->channels, esz), cover_plain(a->d_final, state_bytes),
-                          cover_plain(a->d_marks, piece_slots(a->seq, SSAM_MARK_ROWS) * plane),
+                          cover_plain(a->d_marks, mark_bytes),
                           cover_plain(plan.bytes ? a->d_work : nullptr, (long long)plan.bytes)};
     const Cover ins[] = {cover_rows(a->in, a->seq, a->channels, esz), cover_rows(a->dt, a->seq, a->channels, esz),
                          cover_rows(a->gate, a->seq, a->channels, esz),
@@ -523,9 +526,9 @@ int ssam_scan_selective(const ssam_scan_selective_args* a, void* hip_stream)
     p.per_group = tiles_per_group(a->channels, a->states, a->groups);
     p.tiles = plan.tiles;
     p.softplus = a->softplus != 0;
-    const long long blocks = plan.slots * plan.tiles;
+    const long long blocks = plan.blocks;
     const long long join = (plane / 4 + kBlock - 1) / kBlock * a->seq.sequences;
-    if (blocks > kMaxGrid || (plan.cut && join > kMaxGrid) || plane / 4 >= (1LL << 31)) return SSAM_ERR_DIM;
+    if (blocks > kMaxGrid || (plan.cut && join > kMaxGrid)) return SSAM_ERR_DIM;
     hipStream_t st = (hipStream_t)hip_stream;
     return with_row_type(a->dtype, [&](auto t) {
         return with_shape(a->states, [&](auto shape) {
@@ -553,15 +556,15 @@ int ssam_scan_selective_step(const ssam_scan_selective_step_args* a, void* hip_s
     const int esz = type_bytes(a->dtype);
     const ssam_sequences q{1, a->rows, nullptr, nullptr};
     if (!a->d_a || !a->d_state) return SSAM_ERR_NULL;
-    for (const ssam_rows* r : {&a->in, &a->dt, &a->b, &a->c})
-        if (int e = check_rows(*r, q, esz, false)) return e;
-    if (int e = check_rows(a->gate, q, esz, true)) return e;
+    if (int e = check_group_rows(*a, q, esz)) return e;
+    for (const ssam_rows* r : {&a->in, &a->dt})
+        if (int e = check_rows(*r, q, a->channels, esz, false)) return e;
+    if (int e = check_rows(a->gate, q, a->channels, esz, true)) return e;
     if (int e = check_out_rows(a->out, q, a->channels, esz, false)) return e;
-    if (a->b_group < 0 || a->b_group > kMaxStride || a->c_group < 0 || a->c_group > kMaxStride) return SSAM_ERR_DIM;
     for (const void* f : {(const void*)a->d_a, (const void*)a->d_skip, (const void*)a->d_dt_bias, (const void*)a->d_state})
         if ((uintptr_t)f % 4) return SSAM_ERR_DIM;
     const long long slot = (long long)a->channels * a->states;
-    if (a->slot_stride < slot || a->slot_stride > kMaxStride) return SSAM_ERR_DIM;
+    if (int e = check_pool(a->slots, a->slot_stride, slot)) return e;
     const Cover outs[] = {cover_rows(a->out, q, a->channels, esz), cover_slots(a->d_state, a->slots, a->slot_stride, slot, 4)};
     const Cover ins[] = {cover_rows(a->in, q, a->channels, esz), cover_rows(a->dt, q, a->channels, esz), cover_rows(a->gate, q, a->channels, esz),
                          cover_rows(a->b, q, group_width(a->groups, a->states, a->b_group), esz),

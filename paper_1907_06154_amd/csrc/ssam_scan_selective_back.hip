@@ -542,8 +542,8 @@ int with_back_shape(int states, F f)
 
 struct BackPlan {
     int per_group, tiles, piece;
-    long long slots, rows_total;
-    bool cut, params, bc;
+    long long slots, rows_total, blocks, sum_blocks;
+    bool fits, cut, params, bc;       // fits: no launch has more blocks than it may (without, the call is refused and needs no workspace)
     size_t ends, sums, part_bc, part_param, bytes;
 };
 
@@ -558,9 +558,13 @@ BackPlan plan_of(const ssam_scan_selective_backward_args& a)
     p.piece = scan_piece_rows(a.seq, p.tiles, kBackBlocks, kBackAlone);
     p.slots = piece_slots(a.seq, p.piece);
     p.rows_total = a.seq.d_begin ? a.seq.rows : (long long)a.seq.rows * a.seq.sequences;
-    p.cut = a.seq.rows > p.piece;
+    p.blocks = p.slots * p.tiles;
     p.params = a.d_grad_a || a.d_grad_skip || a.d_grad_dt_bias;
     p.bc = a.grad_b.d || a.grad_c.d;
+    p.sum_blocks = p.bc ? piece_slots(a.seq, kSumRows) : 0;
+    p.fits = p.blocks <= kMaxGrid && p.sum_blocks <= kMaxGrid;
+    if (!p.fits) return p;
+    p.cut = a.seq.rows > p.piece;
     const size_t plane = (size_t)a.channels * a.states;
     p.ends = p.cut ? whole_lines(p.slots * plane * 4) : 0;
     p.sums = p.cut ? whole_lines((size_t)p.slots * a.channels * 4) : 0;
@@ -592,9 +596,10 @@ int ssam_scan_selective_backward(const ssam_scan_selective_backward_args* a, voi
     if (a->seq.sequences == 0 && !plan.params) return SSAM_OK;
     const int esz = type_bytes(a->dtype);
     if (!a->d_a || (!a->d_marks && a->seq.sequences > 0)) return SSAM_ERR_NULL;
-    for (const ssam_rows* r : {&a->in, &a->dt, &a->b, &a->c, &a->grad_out})
-        if (int e = check_rows(*r, a->seq, esz, false)) return e;
-    if (int e = check_rows(a->gate, a->seq, esz, true)) return e;
+    if (int e = check_group_rows(*a, a->seq, esz)) return e;
+    for (const ssam_rows* r : {&a->in, &a->dt, &a->grad_out})
+        if (int e = check_rows(*r, a->seq, a->channels, esz, false)) return e;
+    if (int e = check_rows(a->gate, a->seq, a->channels, esz, true)) return e;
     for (const ssam_rows* r : {&a->grad_in, &a->grad_dt, &a->grad_gate})
         if (int e = check_out_rows(*r, a->seq, a->channels, esz, true)) return e;
     for (const ssam_rows* r : {&a->in, &a->dt, &a->gate, &a->b, &a->c, &a->grad_out, &a->grad_in, &a->grad_dt, &a->grad_gate})
@@ -603,13 +608,14 @@ int ssam_scan_selective_backward(const ssam_scan_selective_backward_args* a, voi
     if (bc_width >= kMaxGroupStates) return SSAM_ERR_DIM;
     for (const ssam_rows* r : {&a->grad_b, &a->grad_c})
         if (int e = check_out_rows(*r, a->seq, bc_width, esz, true)) return e;
-    if (a->b_group < 0 || a->b_group > kMaxStride || a->c_group < 0 || a->c_group > kMaxStride) return SSAM_ERR_DIM;
     for (const void* f : {(const void*)a->d_a, (const void*)a->d_skip, (const void*)a->d_dt_bias, (const void*)a->d_marks, (const void*)a->d_grad_final,
                           (const void*)a->d_grad_a, (const void*)a->d_grad_skip, (const void*)a->d_grad_dt_bias, (const void*)a->d_grad_state})
         if ((uintptr_t)f % 4) return SSAM_ERR_DIM;
     if (plan.bytes && !a->d_work) return SSAM_ERR_NULL;
     if (plan.bytes && (a->work_bytes < plan.bytes || (uintptr_t)a->d_work % 16)) return SSAM_ERR_DIM;
     const long long plane = (long long)a->channels * a->states * 4, state_bytes = a->seq.sequences * plane, wide = a->channels * 4LL;
+    const long long mark_bytes = product(piece_slots(a->seq, SSAM_MARK_ROWS), plane);
+    if (mark_bytes > 4 * kMaxExtent) return SSAM_ERR_DIM;
     const Cover outs[] = {cover_rows(a->grad_in, a->seq, a->channels, esz), cover_rows(a->grad_dt, a->seq, a->channels, esz),
                           cover_rows(a->grad_gate, a->seq, a->channels, esz), cover_rows(a->grad_b, a->seq, bc_width, esz),
                           cover_rows(a->grad_c, a->seq, bc_width, esz), cover_plain(a->d_grad_a, plane), cover_plain(a->d_grad_skip, wide),
@@ -620,7 +626,7 @@ int ssam_scan_selective_backward(const ssam_scan_selective_backward_args* a, voi
                          cover_rows(a->b, a->seq, group_width(a->groups, a->states, a->b_group), esz),
                          cover_rows(a->c, a->seq, group_width(a->groups, a->states, a->c_group), esz), cover_plain(a->d_a, plane),
                          cover_plain(a->d_skip, wide), cover_plain(a->d_dt_bias, wide),
-                         cover_plain(a->d_marks, piece_slots(a->seq, SSAM_MARK_ROWS) * plane), cover_plain(a->d_grad_final, state_bytes)};
+                         cover_plain(a->d_marks, mark_bytes), cover_plain(a->d_grad_final, state_bytes)};
     if (any_overlap(outs, ins)) return SSAM_ERR_ALIAS;
 
     BackParams p{};
@@ -660,12 +666,10 @@ int ssam_scan_selective_backward(const ssam_scan_selective_backward_args* a, voi
     p.per_group = plan.per_group;
     p.tiles = plan.tiles;
     p.softplus = a->softplus != 0;
-    const long long blocks = plan.slots * plan.tiles;
+    const long long blocks = plan.blocks, sum_blocks = plan.sum_blocks;
     const long long join = (plane / 4 + kBlock - 1) / kBlock * a->seq.sequences;
     const long long param_blocks = (plane / 4 + 2LL * a->channels + kWave - 1) / kWave;
-    const long long sum_blocks = plan.bc ? piece_slots(a->seq, kSumRows) : 0;
-    if (blocks > kMaxGrid || (plan.cut && join > kMaxGrid) || plane / 4 >= (1LL << 31) || param_blocks > kMaxGrid / 4 || sum_blocks > kMaxGrid)
-        return SSAM_ERR_DIM;
+    if (!plan.fits || (plan.cut && join > kMaxGrid) || param_blocks > kMaxGrid / 4) return SSAM_ERR_DIM;
     hipStream_t st = (hipStream_t)hip_stream;
     return with_row_type(a->dtype, [&](auto t) {
         return with_back_shape(a->states, [&](auto shape) {
