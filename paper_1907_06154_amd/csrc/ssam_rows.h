@@ -260,9 +260,17 @@ inline Cover cover_rows(const ssam_rows& r, const ssam_sequences& q, long long w
 {
     if (!r.d || q.sequences <= 0 || q.rows <= 0) return Cover{(uintptr_t)r.d, 0, 0, 0};
     const long long width = width_elems * esz;
-    bool comb = r.row * esz >= width;
-    if (!q.d_begin && q.sequences > 1) comb = comb && r.row > 0 && r.batch % r.row == 0;      // every row of every sequence lies on the same comb
-    return Cover{(uintptr_t)r.d, rows_extent(r, q, width_elems) * esz, comb ? r.row * esz : 0, width};
+    // All rows lie on one comb, whose step is the shorter of the strides that count, if the longer is a multiple of it: batches of whole
+    // sequences and buffers with all sequences' rows in turn alike.
+    const bool both = !q.d_begin && q.sequences > 1 && q.rows > 1 && r.row > 0 && r.batch > 0;
+    long long step = !q.d_begin && q.sequences > 1 && (q.rows == 1 || r.row == 0) ? r.batch : r.row;
+    bool comb = true;
+    if (both) {
+        step = r.row < r.batch ? r.row : r.batch;
+        comb = (r.row < r.batch ? r.batch : r.row) % step == 0;
+    }
+    comb = comb && step * esz >= width;
+    return Cover{(uintptr_t)r.d, rows_extent(r, q, width_elems) * esz, comb ? step * esz : 0, width};
 }
 
 inline bool overlaps(const Cover& a, const Cover& b)

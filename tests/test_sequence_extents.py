@@ -97,3 +97,18 @@ def test_scans(L):
     # the largest that fit a launch are planned as they are
     long = Scan(**{**base, "seq": Seq(1, ROWS, None, None)})
     assert size(L, "ssam_scan_selective_workspace_bytes", long) > 0 and f(seq=Seq(1, ROWS, None, None)) == NULL
+
+
+def test_columns_of_time_major_buffers(L):
+    """Halves of one buffer [rows][sequences][2 x channels] are no overlap: refused for what is checked last, not for aliasing."""
+    for lead, batch, row in ((Seq(4, 1 << 28, None, None), 2048, 4 * 2048), (Seq(4, 1 << 28, None, None), 2048 << 28, 2048),
+                             (Seq(1 << 30, 1, None, None), 2048, 7), (Seq(1, 1 << 30, None, None), 5, 2048)):
+        f = lambda x, out: call(L, "ssam_conv1d", conv(channels=1024, taps=1, seq=lead, x=Rows(at(0) + x, batch, row),  # noqa: E731
+                                                       out=Rows(at(0) + out, batch, row)))
+        assert f(0, 2048) == DIM and f(2048, 0) == DIM and f(0, 2046) == ALIAS and f(2046, 0) == ALIAS and f(2048, 2) == ALIAS, (batch, row)
+    # an input that all sequences share, and one that all rows share, beside a result in the other half
+    wide = dict(channels=1024, taps=1, seq=Seq(4, 1 << 28, None, None))
+    assert call(L, "ssam_conv1d", conv(x=Rows(at(0), 0, 4 * 2048), out=Rows(at(0) + 2048, 2048, 4 * 2048), **wide)) == ALIAS     # (other strides)
+    assert call(L, "ssam_conv1d", conv(x=Rows(at(0), 0, 2048), out=Rows(at(0) + 2048, 2048 << 28, 2048), **wide)) == DIM
+    assert call(L, "ssam_conv1d", conv(x=Rows(at(0), 2048, 0), out=Rows(at(0) + 2048, 2048, 4 * 2048), **wide)) == DIM
+    assert call(L, "ssam_conv1d", conv(x=Rows(at(0), 2048, 0), out=Rows(at(0) + 2046, 2048, 4 * 2048), **wide)) == ALIAS
