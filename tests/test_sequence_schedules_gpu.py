@@ -331,3 +331,13 @@ def test_steps_without_slots(rows, dt):
         results.append([ssam.ssam_conv1d_step(x, w, p, silu=True, slots=slots), p, ssam.ssam_scan_selective_step(x, raw, a, b, c, q, softplus=True, slots=slots), q])
     assert all(torch.equal(u, v) for u, v in zip(*results))
     assert torch.equal(results[0][1][rows:], conv_pool[rows:]) and torch.equal(results[0][3][rows:], pool[rows:])
+
+
+def test_time_steps():
+    """A single state that forgets everything shows the time step: softplus within the (6 + 1.3 |x|) u that the references' bounds count for it
+    (and half a step of the result), from time steps of 2e-9 on."""
+    x = torch.linspace(-20, 20, 160001, device="cuda")[:, None].contiguous()
+    one = torch.ones_like(x)
+    got = ssam.ssam_scan_selective(one, x, torch.full((1, 1), float("-inf"), device="cuda"), one[..., None], one[..., None], softplus=True)
+    want = torch.logaddexp(x.double(), torch.zeros_like(x, dtype=torch.float64))
+    check("softplus", got, want, (6 + 1.3 * x.double().abs() + 1) * ref.U * want)
