@@ -323,12 +323,29 @@ int check_group_rows(const Args& a, const ssam_sequences& q, int esz)
 // where `alone` sequences x channel tiles are there without.
 int scan_piece_rows(const ssam_sequences& q, int tiles, int blocks, int alone);
 
-// Turns what each piece adds to the state into the states between the pieces: `ends` holds [slot][channels][states], `sums`
-// [slot][channels] the time steps of a piece added up (its decay is exp(a * sum)).
-//   forward:  ends[slot] becomes the state behind the piece, from `initial` (zeros without) before the first; `initial`
-//             itself goes into the last piece's, for the first
-//   backward: ends[slot] becomes what the piece lets out at its first row, from `initial` (the gradient of the last state) behind the
-//             last piece; not for the first
+// Pieces that another follows, at most rows / piece of them in the packed form however many sequences there are, have an entry of
+// [channels][states] in `ends` and of [channels] in `sums`: the piece in slot `slot` of sequence `seq` this one.
+__device__ __forceinline__ int end_entry(const Pieces& q, int slot, int seq) { return q.begin ? slot - seq : slot; }
+// The forward direction keeps the states before cut sequences too: of the sequence whose first piece is in slot `slot` here.
+__device__ __forceinline__ int start_entry(const Pieces& q, int slot, int seq)
+{
+    if (!q.begin) return slot + q.per - 1;
+    const int followed = q.rows / q.piece;
+    return followed + (q.sequences <= followed ? seq : slot - seq);
+}
+inline long long end_entries(const ssam_sequences& q, int piece, bool starts)
+{
+    if (!q.d_begin) return piece_slots(q, piece);
+    const long long followed = q.rows / piece;
+    return followed + (starts ? q.sequences < followed ? q.sequences : followed : 0);
+}
+
+// Turns what each piece adds to the state into the states between the pieces: `ends` and `sums`, the time steps of a piece added up (its
+// decay is exp(a * sum)), by entries.
+//   forward:  the entry of a piece becomes the state behind it, from `initial` (zeros without) before the first, which itself goes into
+//             the sequence's start entry
+//   backward: the entry of a piece holds what the NEXT one lets out at its first row, and becomes all of that, from `initial` (the gradient
+//             of the last state) behind the last piece
 int launch_join(const Pieces& p, float* ends, const float* sums, const float* a, const float* initial, int channels, int states, bool backward,
                 hipStream_t stream);
 

@@ -23,7 +23,7 @@ struct ScanParams {
     ssam_rows in, dt, gate, out, b, c;
     long long b_group, c_group;
     const float *a, *skip, *dt_bias, *state;
-    float *final, *marks, *ends, *sums;   // ends: [slot][channels][states], sums: [slot][channels]
+    float *final, *marks, *ends, *sums;   // ends: [entry][channels][states], sums: [entry][channels]
     Pieces mark_slots;
     int channels, states, group_channels, per_group, tiles, softplus;
 };
@@ -63,9 +63,9 @@ __global__ __launch_bounds__(kBlock, Shape::NS > 4 ? 2 : sizeof(T) == 4 ? 3 : 4)
     float a2[NS], h[NS];
     load_rates<NS>(p.a + cell, n0, p.states, live, a2);
     if (!kWhole) load_states<NS>(nullptr, 0, 0, false, h);
-    else if (q.row0 > 0) load_states<NS>(p.ends + (slot - 1) * plane + cell, n0, p.states, live, h);
+    else if (q.row0 > 0) load_states<NS>(p.ends + end_entry(p.pieces, slot - 1, q.seq) * plane + cell, n0, p.states, live, h);
     else if (q.n < q.len)   // not from p.state: the last piece's block may have stored p.final over it by now
-        load_states<NS>(p.ends + (slot + (q.len - 1) / p.pieces.piece) * plane + cell, n0, p.states, live, h);
+        load_states<NS>(p.ends + start_entry(p.pieces, slot, q.seq) * plane + cell, n0, p.states, live, h);
     else load_states<NS>(p.state + q.seq * plane + cell, n0, p.states, live && p.state, h);
     float sum = 0.0f;
     float* marks = nullptr;
@@ -221,36 +221,39 @@ __global__ __launch_bounds__(kBlock, Shape::NS > 4 ? 2 : sizeof(T) == 4 ? 3 : 4)
     if (kWhole) {
         if (p.final && last) store_states<NS>(p.final + q.seq * plane + cell, n0, p.states, live, h);
     } else {
-        store_states<NS>(p.ends + slot * plane + cell, n0, p.states, live, h);
-        if (live && n0 == 0) p.sums[(long long)slot * p.channels + ct.c0 + ch] = sum;
+        const long long entry = end_entry(p.pieces, slot, q.seq);
+        store_states<NS>(p.ends + entry * plane + cell, n0, p.states, live, h);
+        if (live && n0 == 0) p.sums[entry * p.channels + ct.c0 + ch] = sum;
     }
 }
 
-// One thread per sequence, channel and state walks the pieces; their values are requested eight pieces at a time
+// One thread per channel and state walks a sequence's pieces; their values are requested eight pieces at a time
 // (1 x 16384 rows of 512 channels, 128 pieces: 84 us with all else, four at a time 87, 32 at a time 92).
 template <bool kBackward>
 __global__ __launch_bounds__(kBlock) void join_pieces(Pieces pc, float* ends, const float* __restrict__ sums, const float* __restrict__ a,
                                                       const float* initial, int channels, int states, unsigned blocks_each)
 {
+    const long long plane = (long long)channels * states;
+    const long long i = (long long)(blockIdx.x % blocks_each) * kBlock + threadIdx.x;
+    if (i >= plane) return;
     const int seq = blockIdx.x / blocks_each;
     int begin, len;
     span_of(pc, seq, begin, len);
     const int n = len > pc.piece ? (len + pc.piece - 1) / pc.piece : 1;
-    const long long plane = (long long)channels * states;
-    const long long i = (long long)(blockIdx.x % blocks_each) * kBlock + threadIdx.x;
-    if (n == 1 || i >= plane) return;
-    const long long slot0 = pc.begin ? first_slot(pc, seq) : (long long)seq * pc.per;
+    if (n == 1) return;
+    const int slot0 = pc.begin ? first_slot(pc, seq) : seq * pc.per;
+    const long long entry0 = end_entry(pc, slot0, seq);
     const int c = (int)(i / states);
     const float a2 = decay_rate(a[i]);
     float h = initial ? initial[seq * plane + i] : 0.0f;
-    if (!kBackward) ends[(slot0 + n - 1) * plane + i] = h;
+    if (!kBackward) ends[start_entry(pc, slot0, seq) * plane + i] = h;
     constexpr int kAtOnce = 8;
     for (int k = 0; k < n - 1; k += kAtOnce) {          // what the last adds nothing follows
         float e[kAtOnce], s[kAtOnce];
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
             const bool there = k + j < n - 1;
-            const long long at = slot0 + (kBackward ? n - 1 - (k + j) : k + j);
+            const long long at = entry0 + (kBackward ? n - 2 - (k + j) : k + j);
             e[j] = there ? ends[at * plane + i] : 0.0f;
             s[j] = there ? sums[at * channels + c] : 0.0f;
         }
@@ -264,7 +267,7 @@ __global__ __launch_bounds__(kBlock) void join_pieces(Pieces pc, float* ends, co
         }
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j)
-            if (k + j < n - 1) ends[(slot0 + (kBackward ? n - 1 - (k + j) : k + j)) * plane + i] = e[j];
+            if (k + j < n - 1) ends[(entry0 + (kBackward ? n - 2 - (k + j) : k + j)) * plane + i] = e[j];
     }
 }
 
@@ -283,8 +286,9 @@ Plan plan_of(const ssam_scan_selective_args& a)
     p.slots = piece_slots(a.seq, p.piece);
     p.blocks = p.slots * p.tiles;
     p.cut = a.seq.rows > p.piece && p.blocks <= kMaxGrid;
-    p.ends = p.cut ? (size_t)p.slots * a.channels * a.states * sizeof(float) : 0;
-    p.bytes = p.cut ? p.ends + (size_t)p.slots * a.channels * sizeof(float) : 0;
+    const size_t entries = p.cut ? end_entries(a.seq, p.piece, true) : 0;
+    p.ends = entries * a.channels * a.states * sizeof(float);
+    p.bytes = p.ends + entries * a.channels * sizeof(float);
     return p;
 }
 

@@ -142,7 +142,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
     load_rates<NS, kShared>(p.a + cell, n0, p.states, live, a2);
     const bool last = q.row0 + q.n >= q.len;
     if (!kWhole) load_states<NS, kShared>(nullptr, 0, 0, false, g);
-    else if (!last) load_states<NS, kShared>(p.ends + (slot + 1) * plane + cell, n0, p.states, live, g);
+    else if (!last) load_states<NS, kShared>(p.ends + end_entry(p.pieces, slot, q.seq) * plane + cell, n0, p.states, live, g);
     else load_states<NS, kShared>(p.grad_final + q.seq * plane + cell, n0, p.states, live && p.grad_final, g);
     // !kWhole: the states do not meet, and every copy has the whole of g.
     auto anew = [](int v) { return kShared ? made_anew(v) : v; };
@@ -476,8 +476,9 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
             part_param[plane + p.channels + ct.c0 + tid] = s1;
         }
     } else {
-        store_states<NS, kShared>(p.ends + slot * plane + cell, n0, p.states, live, g);
-        if (live && n0 == 0) p.sums[(long long)slot * p.channels + ct.c0 + ch] = sum;
+        const long long entry = end_entry(p.pieces, slot - 1, q.seq);
+        store_states<NS, kShared>(p.ends + entry * plane + cell, n0, p.states, live, g);
+        if (live && n0 == 0) p.sums[entry * p.channels + ct.c0 + ch] = sum;
     }
 }
 
@@ -566,8 +567,9 @@ BackPlan plan_of(const ssam_scan_selective_backward_args& a)
     if (!p.fits) return p;
     p.cut = a.seq.rows > p.piece;
     const size_t plane = (size_t)a.channels * a.states;
-    p.ends = p.cut ? whole_lines(p.slots * plane * 4) : 0;
-    p.sums = p.cut ? whole_lines((size_t)p.slots * a.channels * 4) : 0;
+    const size_t entries = p.cut ? end_entries(a.seq, p.piece, false) : 0;
+    p.ends = whole_lines(entries * plane * 4);
+    p.sums = whole_lines(entries * a.channels * 4);
     p.part_bc = p.bc ? whole_lines((size_t)p.per_group * p.rows_total * a.groups * 2 * a.states * 4) : 0;
     p.part_param = p.params ? whole_lines((size_t)p.slots * (plane + 2 * (size_t)a.channels) * 4) : 0;
     p.bytes = p.ends + p.sums + p.part_bc + p.part_param;

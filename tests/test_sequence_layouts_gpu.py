@@ -6,6 +6,34 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 import paper_1907_06154_amd as ssam  # noqa: E402
+import test_sequence_gpu as base  # noqa: E402
+
+
+def among_short_ones(longs, each):
+    """Offsets of packed sequences: `each` of 0 .. 4 rows before every long one and behind the last."""
+    starts = [3]
+    for n in [*longs, None]:
+        for i in range(each):
+            starts.append(starts[-1] + i * 7 % 5)
+        if n is not None:
+            starts.append(starts[-1] + n)
+    return starts
+
+
+# sequences of more pieces than one among several hundred that are shorter: more sequences than pieces that another follows
+MIXED = among_short_ones([500, 33, 700, 64, 32, 65, 96], 52)
+base.LAYOUTS["mixed"] = ((MIXED[-1] + 2,), MIXED, None)
+
+
+@pytest.mark.parametrize("spec", [("mixed", "float32", 70, 16, 1, True, True, True, True, "wide"), ("mixed", "bfloat16", 9, 4, 3, True, True, True, True, "dense"),
+                                  ("mixed", "float16", 12, 40, 1, True, False, True, False, "dense")], ids=lambda s: "-".join(map(str, s)))
+def test_long_sequences_among_many_short_ones(spec):
+    k = base.ScanCase(*spec)
+    pieces = k.rows // 32
+    assert len(k.spans) > pieces                        # (pieces of 32 rows)
+    assert ssam.ssam_scan_selective_workspace_bytes(k.x, k.a, spec[4], **k.seq) == 2 * pieces * (k.D * k.N + k.D) * 4
+    base.test_scan_selective(spec)
+    base.test_scan_selective_backward(spec)
 
 
 def test_halves_of_a_time_major_buffer():
