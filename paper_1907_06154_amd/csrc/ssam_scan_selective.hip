@@ -228,46 +228,48 @@ __global__ __launch_bounds__(kBlock, Shape::NS > 4 ? 2 : sizeof(T) == 4 ? 3 : 4)
 }
 
 // One thread per channel and state walks a sequence's pieces; their values are requested eight pieces at a time
-// (1 x 16384 rows of 512 channels, 128 pieces: 84 us with all else, four at a time 87, 32 at a time 92).
+// (1 x 16384 rows of 512 channels, 128 pieces: 84 us with all else, four at a time 87, 32 at a time 92).  A block takes every
+// `seqs_apart`-th sequence.
 template <bool kBackward>
 __global__ __launch_bounds__(kBlock) void join_pieces(Pieces pc, float* ends, const float* __restrict__ sums, const float* __restrict__ a,
-                                                      const float* initial, int channels, int states, unsigned blocks_each)
+                                                      const float* initial, int channels, int states, unsigned blocks_each, int seqs_apart)
 {
     const long long plane = (long long)channels * states;
     const long long i = (long long)(blockIdx.x % blocks_each) * kBlock + threadIdx.x;
     if (i >= plane) return;
-    const int seq = blockIdx.x / blocks_each;
-    int begin, len;
-    span_of(pc, seq, begin, len);
-    const int n = len > pc.piece ? (len + pc.piece - 1) / pc.piece : 1;
-    if (n == 1) return;
-    const int slot0 = pc.begin ? first_slot(pc, seq) : seq * pc.per;
-    const long long entry0 = end_entry(pc, slot0, seq);
-    const int c = (int)(i / states);
-    const float a2 = decay_rate(a[i]);
-    float h = initial ? initial[seq * plane + i] : 0.0f;
-    if (!kBackward) ends[start_entry(pc, slot0, seq) * plane + i] = h;
-    constexpr int kAtOnce = 8;
-    for (int k = 0; k < n - 1; k += kAtOnce) {          // what the last adds nothing follows
-        float e[kAtOnce], s[kAtOnce];
+    for (int seq = blockIdx.x / blocks_each; seq < pc.sequences; seq += seqs_apart) {
+        int begin, len;
+        span_of(pc, seq, begin, len);
+        const int n = len > pc.piece ? (len + pc.piece - 1) / pc.piece : 1;
+        if (n == 1) continue;
+        const int slot0 = pc.begin ? first_slot(pc, seq) : seq * pc.per;
+        const long long entry0 = end_entry(pc, slot0, seq);
+        const int c = (int)(i / states);
+        const float a2 = decay_rate(a[i]);
+        float h = initial ? initial[seq * plane + i] : 0.0f;
+        if (!kBackward) ends[start_entry(pc, slot0, seq) * plane + i] = h;
+        constexpr int kAtOnce = 8;
+        for (int k = 0; k < n - 1; k += kAtOnce) {          // what the last adds nothing follows
+            float e[kAtOnce], s[kAtOnce];
 #pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) {
-            const bool there = k + j < n - 1;
-            const long long at = entry0 + (kBackward ? n - 2 - (k + j) : k + j);
-            e[j] = there ? ends[at * plane + i] : 0.0f;
-            s[j] = there ? sums[at * channels + c] : 0.0f;
+            for (int j = 0; j < kAtOnce; ++j) {
+                const bool there = k + j < n - 1;
+                const long long at = entry0 + (kBackward ? n - 2 - (k + j) : k + j);
+                e[j] = there ? ends[at * plane + i] : 0.0f;
+                s[j] = there ? sums[at * channels + c] : 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                if (k + j >= n - 1) break;
+                // The decay of many rows may come out as 0 though no row's is: an infinity passes it as it passes them.
+                const float x = a2 * s[j], decay = exp2_fast(x);
+                const bool passes = __builtin_fabsf(h) == __builtin_inff() && x > -__builtin_inff();
+                e[j] = h = __builtin_fmaf(passes ? __builtin_fmaxf(decay, 0x1p-126f) : decay, h, e[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j)
+                if (k + j < n - 1) ends[(entry0 + (kBackward ? n - 2 - (k + j) : k + j)) * plane + i] = e[j];
         }
-#pragma unroll
-        for (int j = 0; j < kAtOnce; ++j) {
-            if (k + j >= n - 1) break;
-            // The decay of many rows may come out as 0 though no row's is: an infinity passes it as it passes them.
-            const float x = a2 * s[j], decay = exp2_fast(x);
-            const bool passes = __builtin_fabsf(h) == __builtin_inff() && x > -__builtin_inff();
-            e[j] = h = __builtin_fmaf(passes ? __builtin_fmaxf(decay, 0x1p-126f) : decay, h, e[j]);
-        }
-#pragma unroll
-        for (int j = 0; j < kAtOnce; ++j)
-            if (k + j < n - 1) ends[(entry0 + (kBackward ? n - 2 - (k + j) : k + j)) * plane + i] = e[j];
     }
 }
 
@@ -445,9 +447,10 @@ int launch_join(const Pieces& p, float* ends, const float* sums, const float* a,
                 hipStream_t stream)
 {
     const unsigned each = (unsigned)(((long long)channels * states + kBlock - 1) / kBlock);
-    const dim3 grid(each * (unsigned)p.sequences);
-    if (backward) hipLaunchKernelGGL((join_pieces<true>), grid, dim3(kBlock), 0, stream, p, ends, sums, a, initial, channels, states, each);
-    else hipLaunchKernelGGL((join_pieces<false>), grid, dim3(kBlock), 0, stream, p, ends, sums, a, initial, channels, states, each);
+    const int apart = (int)(p.sequences < kMaxGrid / each ? p.sequences : kMaxGrid / each);
+    const dim3 grid(each * (unsigned)apart);
+    if (backward) hipLaunchKernelGGL((join_pieces<true>), grid, dim3(kBlock), 0, stream, p, ends, sums, a, initial, channels, states, each, apart);
+    else hipLaunchKernelGGL((join_pieces<false>), grid, dim3(kBlock), 0, stream, p, ends, sums, a, initial, channels, states, each, apart);
     return launched();
 }
 
@@ -531,8 +534,7 @@ int ssam_scan_selective(const ssam_scan_selective_args* a, void* hip_stream)
     p.tiles = plan.tiles;
     p.softplus = a->softplus != 0;
     const long long blocks = plan.blocks;
-    const long long join = (plane / 4 + kBlock - 1) / kBlock * a->seq.sequences;
-    if (blocks > kMaxGrid || (plan.cut && join > kMaxGrid)) return SSAM_ERR_DIM;
+    if (blocks > kMaxGrid) return SSAM_ERR_DIM;
     hipStream_t st = (hipStream_t)hip_stream;
     return with_row_type(a->dtype, [&](auto t) {
         return with_shape(a->states, [&](auto shape) {

@@ -669,9 +669,8 @@ int ssam_scan_selective_backward(const ssam_scan_selective_backward_args* a, voi
     p.tiles = plan.tiles;
     p.softplus = a->softplus != 0;
     const long long blocks = plan.blocks, sum_blocks = plan.sum_blocks;
-    const long long join = (plane / 4 + kBlock - 1) / kBlock * a->seq.sequences;
     const long long param_blocks = (plane / 4 + 2LL * a->channels + kWave - 1) / kWave;
-    if (!plan.fits || (plan.cut && join > kMaxGrid) || param_blocks > kMaxGrid / 4) return SSAM_ERR_DIM;
+    if (!plan.fits || param_blocks > kMaxGrid / 4) return SSAM_ERR_DIM;
     hipStream_t st = (hipStream_t)hip_stream;
     return with_row_type(a->dtype, [&](auto t) {
         return with_back_shape(a->states, [&](auto shape) {

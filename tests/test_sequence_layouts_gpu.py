@@ -53,3 +53,29 @@ def test_halves_of_a_time_major_buffer():
     out = two[..., D:]
     assert ssam.ssam_scan_selective(x, dt, a, b, c, softplus=True, d_out=out) is out
     assert torch.equal(out, want) and torch.equal(x, kept)
+
+
+def test_more_sequences_than_a_launch_has_blocks_for_their_joins():
+    """4200 sequences x 2^20 states in blocks of 256 are more than 2^24 blocks; one sequence is long enough to be cut, the others have a row."""
+    S, D, N = 4200, 16384, 64
+    long = 2000
+    g = torch.Generator(device="cuda").manual_seed(1)
+    rand = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()  # noqa: E731
+    lengths = [1] * S
+    lengths[4111] = long
+    starts = torch.tensor([0, *lengths], device="cuda").cumsum(0).to(torch.int32)
+    T = int(starts[-1])
+    x, dt, b, c = rand(T, D), rand(T, D), rand(T, 1, N), rand(T, 1, N)
+    a = -torch.rand(D, N, generator=g, device="cuda") - 0.1
+    out = ssam.ssam_scan_selective(x, dt, a, b, c, softplus=True, starts=starts)
+    lo = int(starts[4111])
+    rows = slice(lo, lo + long)
+    # the same sequence alone is cut elsewhere: the same states up to fp32's roundings, results up to one of theirs
+    alone = ssam.ssam_scan_selective(x[rows], dt[rows], a, b[rows], c[rows], softplus=True)
+    assert ssam.ssam_scan_selective_workspace_bytes(x, a, starts=starts) > 0
+    assert (out[rows].float() - alone.float()).abs().max() <= 2 ** -7 * alone.float().abs().max()
+    # single rows: y = d u (b . c), products and sums of fp32
+    d = torch.nn.functional.softplus(dt[:lo].double())
+    want = d * x[:lo].double() * (b[:lo, 0].double() * c[:lo, 0].double()).sum(-1, keepdim=True)
+    mag = d * x[:lo].double().abs() * (b[:lo, 0].double() * c[:lo, 0].double()).abs().sum(-1, keepdim=True)
+    assert ((out[:lo].double() - want).abs() <= 2.0 ** -8 * want.abs() * 1.001 + 100 * 2.0 ** -24 * mag).all()
