@@ -19,6 +19,9 @@ namespace {
 
 constexpr int kTile = SSAM_MARK_ROWS;
 constexpr int kBackBlocks = 1024;     // two rounds of the two blocks per compute unit that 256 registers leave
+// The parameters' gradients of every slot are a workspace: of more blocks than this at once, launch after launch (32 to a compute unit are
+// enough for its ends not to matter; 4096 sequences of 8 rows, 4096 channels, 16 states: 151 MB for 1.2 GB).
+constexpr long long kPartBlocks = 1 << 15;
 constexpr long long kMaxGroupStates = 1 << 27;   // groups x states: offsets in a tile's rows of both then have 32 bits
 constexpr int kBackAlone = 512;       // sequences x channel tiles that are enough without cutting (8 x 8192 rows of 2048 channels, 256 of them: 505 us cut, 551 whole)
 
@@ -31,7 +34,8 @@ struct BackParams {
     float* grad_state;
     float *ends, *sums;               // pieces: what reaches each from behind
     float* part_bc;                   // [tile of the group][row][group][2][states]
-    float* part_param;                // [slot][channels x states, channels (skip), channels (bias)]
+    float* part_param;                // [slot of the launch][channels x states, channels (skip), channels (bias)]
+    int slot0;                        // of the launch
     long long rows_total;
     int channels, states, groups, group_channels, per_group, tiles, softplus;
 };
@@ -118,7 +122,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
     __shared__ __attribute__((aligned(16))) float terms[kWhole ? kWavesPerBlock : 1][2 * ChannelSums<GL>::kFloats];
 
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6;
-    const int slot = blockIdx.x / p.tiles;
+    const int slot = blockIdx.x / p.tiles + p.slot0;
     const ChannelTile ct = channel_tile(blockIdx.x % p.tiles, p.per_group, p.group_channels, CB);
     const Piece q = find_piece(p.pieces, slot);
     const long long plane = (long long)p.channels * p.states;
@@ -127,7 +131,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
     const bool live = ch < ct.n;
     const int n0 = lane_group<GL>(lane) * NS;
     const long long cell = (long long)(ct.c0 + ch) * p.states;
-    float* part_param = kWhole && p.part_param ? p.part_param + slot * (plane + 2LL * p.channels) : nullptr;
+    float* part_param = kWhole && p.part_param ? p.part_param + (slot - p.slot0) * (plane + 2LL * p.channels) : nullptr;
     if (q.seq < 0) {
         if (part_param) {       // an empty slot adds zeros
             float none[NS] = {};
@@ -505,10 +509,10 @@ __global__ __launch_bounds__(kBlock) void back_sum_bc(BackParams p, Pieces rows)
     }
 }
 
-// Sums over the slots, 16 interleaved runs of them and then the runs, always in the same order.
+// Sums over a launch's slots, 16 interleaved runs of them and then the runs, always in the same order; `more`: on top of the launches before.
 constexpr int kRuns = 16;
 __global__ __launch_bounds__(kWave* kRuns) void back_sum_params(const float* __restrict__ parts, long long slots, long long plane, int channels,
-                                                                float* grad_a, float* grad_skip, float* grad_dt_bias)
+                                                                float* grad_a, float* grad_skip, float* grad_dt_bias, bool more)
 {
     __shared__ float run[kRuns][kWave];
     const int lane = threadIdx.x & (kWave - 1), r = threadIdx.x >> 6;
@@ -522,13 +526,9 @@ __global__ __launch_bounds__(kWave* kRuns) void back_sum_params(const float* __r
     if (r != 0 || i >= wide) return;
 #pragma unroll
     for (int k = 1; k < kRuns; ++k) s += run[k][lane];
-    if (i < plane) {
-        if (grad_a) grad_a[i] = s;
-    } else if (i < plane + channels) {
-        if (grad_skip) grad_skip[i - plane] = s;
-    } else if (grad_dt_bias) {
-        grad_dt_bias[i - plane - channels] = s;
-    }
+    float* to = i < plane ? grad_a ? grad_a + i : nullptr : i < plane + channels ? grad_skip ? grad_skip + (i - plane) : nullptr
+                                                          : grad_dt_bias ? grad_dt_bias + (i - plane - channels) : nullptr;
+    if (to) *to = more ? *to + s : s;
 }
 
 // As with_shape, but for eight states from one on: a tile of 256 channels would not fit the LDS twice.
@@ -543,7 +543,7 @@ int with_back_shape(int states, F f)
 
 struct BackPlan {
     int per_group, tiles, piece;
-    long long slots, rows_total, blocks, sum_blocks;
+    long long slots, slots_each, rows_total, blocks, sum_blocks;     // slots_each: of a launch of the main kernel
     bool fits, cut, params, bc;       // fits: no launch has more blocks than it may (without, the call is refused and needs no workspace)
     size_t ends, sums, part_bc, part_param, bytes;
 };
@@ -562,6 +562,7 @@ BackPlan plan_of(const ssam_scan_selective_backward_args& a)
     p.blocks = p.slots * p.tiles;
     p.params = a.d_grad_a || a.d_grad_skip || a.d_grad_dt_bias;
     p.bc = a.grad_b.d || a.grad_c.d;
+    p.slots_each = p.params && p.blocks > kPartBlocks ? (kPartBlocks + p.tiles - 1) / p.tiles : p.slots;
     p.sum_blocks = p.bc ? piece_slots(a.seq, kSumRows) : 0;
     p.fits = p.blocks <= kMaxGrid && p.sum_blocks <= kMaxGrid;
     if (!p.fits) return p;
@@ -571,7 +572,7 @@ BackPlan plan_of(const ssam_scan_selective_backward_args& a)
     p.ends = whole_lines(entries * plane * 4);
     p.sums = whole_lines(entries * a.channels * 4);
     p.part_bc = p.bc ? whole_lines((size_t)p.per_group * p.rows_total * a.groups * 2 * a.states * 4) : 0;
-    p.part_param = p.params ? whole_lines((size_t)p.slots * (plane + 2 * (size_t)a.channels) * 4) : 0;
+    p.part_param = p.params ? whole_lines((size_t)p.slots_each * (plane + 2 * (size_t)a.channels) * 4) : 0;
     p.bytes = p.ends + p.sums + p.part_bc + p.part_param;
     return p;
 }
@@ -672,6 +673,10 @@ int ssam_scan_selective_backward(const ssam_scan_selective_backward_args* a, voi
     const long long param_blocks = (plane / 4 + 2LL * a->channels + kWave - 1) / kWave;
     if (!plan.fits || param_blocks > kMaxGrid / 4) return SSAM_ERR_DIM;
     hipStream_t st = (hipStream_t)hip_stream;
+    auto sum_params = [&](long long slots, bool more) {
+        hipLaunchKernelGGL(back_sum_params, dim3((unsigned)param_blocks), dim3(kWave * kRuns), 0, st, p.part_param, slots, plane / 4, a->channels,
+                           a->d_grad_a, a->d_grad_skip, a->d_grad_dt_bias, more);
+    };
     return with_row_type(a->dtype, [&](auto t) {
         return with_back_shape(a->states, [&](auto shape) {
             using T = decltype(t);
@@ -683,16 +688,19 @@ int ssam_scan_selective_backward(const ssam_scan_selective_backward_args* a, voi
                         hipLaunchKernelGGL((scan_back<T, S, false, kShared>), dim3((unsigned)blocks), dim3(kBlock), 0, st, p);
                         if (int e = launch_join(p.pieces, p.ends, p.sums, a->d_a, a->d_grad_final, a->channels, a->states, true, st)) return e;
                     }
-                    hipLaunchKernelGGL((scan_back<T, S, true, kShared>), dim3((unsigned)blocks), dim3(kBlock), 0, st, p);
+                    for (long long slot0 = 0; slot0 < plan.slots; slot0 += plan.slots_each) {
+                        const long long slots = plan.slots - slot0 < plan.slots_each ? plan.slots - slot0 : plan.slots_each;
+                        p.slot0 = (int)slot0;
+                        hipLaunchKernelGGL((scan_back<T, S, true, kShared>), dim3((unsigned)(slots * plan.tiles)), dim3(kBlock), 0, st, p);
+                        if (plan.params) sum_params(slots, slot0 > 0);
+                    }
                     return SSAM_OK;
                 });
                 if (e) return e;
                 if (plan.bc)
                     hipLaunchKernelGGL((back_sum_bc<T>), dim3((unsigned)sum_blocks), dim3(kBlock), 0, st, p, make_pieces(a->seq, kSumRows));
             }
-            if (plan.params)
-                hipLaunchKernelGGL(back_sum_params, dim3((unsigned)param_blocks), dim3(kWave * kRuns), 0, st, p.part_param, plan.slots, plane / 4,
-                                   a->channels, a->d_grad_a, a->d_grad_skip, a->d_grad_dt_bias);
+            if (plan.params && !blocks) sum_params(0, false);
             return launched();
         });
     });

@@ -39,6 +39,8 @@ SCANS = {
     "pieces_4": ((8, 333), None, None, 4160, 4, "float32", True, 64, 96),
     "whole_then_pieces_16": ((5, 333), None, None, 4160, 16, "bfloat16", True, None, 128),
     "pieces_16": ((1500,), None, None, 4160, 16, "float16", True, 96, 96),
+    # more sequences than one launch of the gradients takes
+    "many_16": ((11003, 3), None, [i * 5 % 4 for i in range(11003)], 130, 16, "bfloat16", True, None, None),
     "packed_4": ((6000,), [0, 17, 2900, 2900, 5000, 5990], None, 4160, 4, "bfloat16", True, 64, 128),
 }
 

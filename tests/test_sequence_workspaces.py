@@ -26,6 +26,9 @@ def test_many_short_sequences_take_no_more_than_long_ones(L):
         s = Seq(S, rows, at(0), at(1))
         assert forward(L, D, N, s) == 2 * 16 * (plane + line)          # pieces of 2048 rows
         assert back(L, D, N, s) == 16 * (plane + line)
+        # the parameters' gradients: 512 slots of 64 channel tiles are 2^15 blocks
+        assert back(L, D, N, s, grad_a=at(2)) == 16 * (plane + line) + 512 * (plane + 2 * line)
+        assert back(L, D, N, Seq(S, 8, None, None), grad_skip=at(2)) == 512 * (plane + 2 * line)
     # a batch has what its sequences are cut into
     assert forward(L, D, N, Seq(1, 4096, None, None)) == 16 * (plane + line)
     assert back(L, D, N, Seq(1, 4096, None, None)) == 16 * (plane + line)
