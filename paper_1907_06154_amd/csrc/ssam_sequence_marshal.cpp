@@ -195,8 +195,14 @@ PyObject* guarded(F f)
         PyErr_SetString(PyExc_ValueError, e.what());
     } catch (const BadType& e) {
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, e.what());
-    } catch (const std::exception& e) {      // the allocator's among them
-        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (const c10::OutOfMemoryError& e) {      // as torch's own functions raise it
+        PyObject* torch = PyImport_ImportModule("torch");
+        PyObject* kind = torch ? PyObject_GetAttrString(torch, "OutOfMemoryError") : nullptr;
+        if (kind) PyErr_SetString(kind, e.what_without_backtrace());
+        Py_XDECREF(kind);
+        Py_XDECREF(torch);
+    } catch (const std::exception& e) {
+        if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, e.what());
     }
     return nullptr;
 }

@@ -79,3 +79,12 @@ def test_more_sequences_than_a_launch_has_blocks_for_their_joins():
     want = d * x[:lo].double() * (b[:lo, 0].double() * c[:lo, 0].double()).sum(-1, keepdim=True)
     mag = d * x[:lo].double().abs() * (b[:lo, 0].double() * c[:lo, 0].double()).abs().sum(-1, keepdim=True)
     assert ((out[:lo].double() - want).abs() <= 2.0 ** -8 * want.abs() * 1.001 + 100 * 2.0 ** -24 * mag).all()
+
+
+def test_marks_that_no_card_holds():
+    """2^26 entries of a megabyte: torch's own error, before anything runs."""
+    x = torch.zeros(1, 4096, device="cuda").expand(1 << 30, 4096)
+    with pytest.raises(torch.OutOfMemoryError):
+        ssam.ssam_scan_selective_marks(x, torch.zeros(4096, 64, device="cuda"))
+    out = ssam.ssam_conv1d(x[:8], torch.ones(4096, 2, device="cuda"))      # and the next call is none the worse
+    assert not out.any()
