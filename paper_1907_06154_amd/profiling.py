@@ -437,6 +437,9 @@ FILTERS = "5x6x4 on 256x256x256, 7x7x7 on 53x256x202, 7x7x7 on 202x256x53, 9x9x9
           "4x4x4 on 256x256x256, 2x2x9 on 256x256x256"
 
 
+OPERATE_CALLS = 12
+
+
 def operate(name: str) -> None:
     sys.path[:0] = [ROOT, os.path.join(ROOT, "perf")]
     import torch
@@ -444,7 +447,8 @@ def operate(name: str) -> None:
     operators.own = True
     case = next(c for c in operators.listed() if c["name"] == name)
     sets = [operators.prepare(case, seed) for seed in range(3)]
-    for i in range(12):
+    torch.cuda.synchronize()
+    for i in range(OPERATE_CALLS):
         operators.run(sets[i % 3])
     torch.cuda.synchronize()
 
@@ -465,32 +469,39 @@ def operator_kernel(name: str) -> str:
     return text
 
 
+def torch_kernel(name: str) -> str:
+    """A kernel of torch's that a call launches."""
+    m = re.search(r"(FillFunctor|CatArray\w+|\w+_kernel\w*)", name)
+    return "torch: " + {"FillFunctor": "fill"}.get(m[1], m[1]) if m else "torch: " + name[:60].replace("|", "/")
+
+
 def operator_summary(runs: str, out_md: str) -> None:
     ctrs = "SQ_WAVES SQ_INSTS_VALU SQ_ACTIVE_INST_VALU SQ_WAVE_CYCLES SQ_WAIT_ANY SQ_INSTS_LDS SQ_LDS_BANK_CONFLICT SQ_LDS_IDX_ACTIVE"
     run = "--output-format csv -d <dir>/<case>{} -o c -- python3 -m paper_1907_06154_amd.profiling operate <case>\n"
     out = ["# Sequence operators: the kernels of a call (rocprofv3)\n", "One MI355X, per case of perf/operators.py:\n",
            "    rocprofv3 --kernel-trace " + run.format("") + f"    rocprofv3 --pmc {ctrs} " + run.format("_pmc") +
            "    python -m paper_1907_06154_amd.profiling operators <dir> profiles/sequence_operators.md\n",
-           "Medians over a kernel's dispatches, us from the trace, the rest from the counter run.  `vector busy` = 4 x SQ_ACTIVE_INST_VALU / (1024 SIMDs x "
+           "Every kernel of the calls, those of torch that a call launches among them, in the order of their first dispatch behind the first call's "
+           "start.  `launches` a call; medians over a kernel's dispatches, us from the trace, the rest from the counter run.  `vector busy` = 4 x SQ_ACTIVE_INST_VALU / (1024 SIMDs x "
            "duration x 2.2 GHz), `LDS busy` = SQ_LDS_IDX_ACTIVE / (256 CUs x duration x 2.2 GHz), of which `conflicts` replay, `waiting` = SQ_WAIT_ANY / "
            "SQ_WAVE_CYCLES.  These are a process's first twelve calls: the long scans take up to 15 % less once the clock has settled.\n",
-           "| case | kernel | us | waves | vector instructions | LDS instructions | vector busy | LDS busy | conflicts | waiting |\n" + "|---" * 10 + "|"]
+           "| case | kernel | launches | us | waves | vector instructions | LDS instructions | vector busy | LDS busy | conflicts | waiting |\n" + "|---" * 11 + "|"]
     middle = lambda v: sorted(v)[len(v) // 2]  # noqa: E731
     for trace in sorted(glob.glob(os.path.join(runs, "*"))):
         if trace.endswith("_pmc") or not os.path.isdir(trace):
             continue
         times, counts = collections.OrderedDict(), {}
-        rows = csv.DictReader(open(one(os.path.join(trace, "**", "*kernel_trace.csv"))))
-        for r in sorted(rows, key=lambda r: int(r["Start_Timestamp"])):
-            times.setdefault(operator_kernel(r["Kernel_Name"]), []).append((int(r["End_Timestamp"]) - int(r["Start_Timestamp"])) / 1e3)
+        rows = sorted(csv.DictReader(open(one(os.path.join(trace, "**", "*kernel_trace.csv")))), key=lambda r: int(r["Start_Timestamp"]))
+        first = next(i for i, r in enumerate(rows) if operator_kernel(r["Kernel_Name"]))     # what lies before prepares the case
+        for r in rows[first:]:
+            name = operator_kernel(r["Kernel_Name"]) or torch_kernel(r["Kernel_Name"])
+            times.setdefault(name, []).append((int(r["End_Timestamp"]) - int(r["Start_Timestamp"])) / 1e3)
         if os.path.isdir(trace + "_pmc"):
             for k, c, us in counter_dispatches(trace + "_pmc"):
                 for name, v in (*c.items(), ("us", us)):
                     counts.setdefault(operator_kernel(k), {}).setdefault(name, []).append(v)
         for k, v in times.items():
-            if not k:
-                continue
-            line = f"| {os.path.basename(trace)} | {k} | {middle(v):.1f} |"
+            line = f"| {os.path.basename(trace)} | {k} | {-(-len(v) // OPERATE_CALLS)} | {middle(v):.1f} |"
             if k in counts:
                 m = {name: middle(x) for name, x in counts[k].items()}
                 cycles = m["us"] * 2200
