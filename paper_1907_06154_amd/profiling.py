@@ -471,8 +471,10 @@ def operator_kernel(name: str) -> str:
 
 def torch_kernel(name: str) -> str:
     """A kernel of torch's that a call launches."""
-    m = re.search(r"(FillFunctor|CatArray\w+|\w+_kernel\w*)", name)
-    return "torch: " + {"FillFunctor": "fill"}.get(m[1], m[1]) if m else "torch: " + name[:60].replace("|", "/")
+    if "FillFunctor" in name:
+        return "torch: fill"
+    m = re.search(r"\w+_kernel\w*", name)
+    return "torch: " + (m[0] if m else name[:60].replace("|", "/"))
 
 
 def operator_summary(runs: str, out_md: str) -> None:
