@@ -258,17 +258,25 @@ __global__ __launch_bounds__(kBlock) void join_pieces(Pieces pc, float* ends, co
                 e[j] = there ? ends[at * plane + i] : 0.0f;
                 s[j] = there ? sums[at * channels + c] : 0.0f;
             }
+            // The decay of many rows may come out as 0 though no row's is: an infinity passes it as it passes them.  Where that makes NaN of
+            // it, the pieces are gone over again.
+            const float before = h;
+            float out[kAtOnce];
+            auto pass = [&](bool infinite) {
+                h = before;
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) {
-                if (k + j >= n - 1) break;
-                // The decay of many rows may come out as 0 though no row's is: an infinity passes it as it passes them.
-                const float x = a2 * s[j], decay = exp2_fast(x);
-                const bool passes = __builtin_fabsf(h) == __builtin_inff() && x > -__builtin_inff();
-                e[j] = h = __builtin_fmaf(passes ? __builtin_fmaxf(decay, 0x1p-126f) : decay, h, e[j]);
-            }
+                for (int j = 0; j < kAtOnce; ++j) {
+                    if (k + j >= n - 1) break;
+                    const float x = a2 * s[j], decay = exp2_fast(x);
+                    const bool passes = infinite && __builtin_fabsf(h) == __builtin_inff() && x > -__builtin_inff();
+                    out[j] = h = __builtin_fmaf(passes ? __builtin_fmaxf(decay, 0x1p-126f) : decay, h, e[j]);
+                }
+            };
+            pass(false);
+            if (h != h) pass(true);
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j)
-                if (k + j < n - 1) ends[(entry0 + (kBackward ? n - 2 - (k + j) : k + j)) * plane + i] = e[j];
+                if (k + j < n - 1) ends[(entry0 + (kBackward ? n - 2 - (k + j) : k + j)) * plane + i] = out[j];
         }
     }
 }

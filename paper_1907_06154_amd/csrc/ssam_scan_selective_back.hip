@@ -153,10 +153,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
     auto state_of = [&](int place) { return kShared ? state_at(place, p.states) : place; };
     auto copies = [&](int place) { return kWhole && kShared ? state_copies(state_of(place), p.states, NP) : 1.0f; };
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-        g[i] *= 1.0f / copies(n0 + i);
-        da[i] = 0.0f;
-    }
+    for (int i = 0; i < NS; ++i) da[i] = 0.0f;
     float sum = 0.0f;
     const float* marks = nullptr;
     if (kWhole) {
@@ -235,6 +232,8 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
 
     const int tiles = (q.n + K - 1) / K;
     if (tiles > 0) request((tiles - 1) * K);
+#pragma unroll
+    for (int i = 0; i < NS; ++i) g[i] *= 1.0f / copies(n0 + i);        // (waits for g, so behind the first tile's requests)
     for (int tile = tiles - 1; tile >= 0; --tile) {
         const int row = tile * K;
         const bool behind = row + mine.row >= q.n;       // a row behind the piece: d = 0, dy = 0, b = c = 0, it passes states and gradients unchanged
