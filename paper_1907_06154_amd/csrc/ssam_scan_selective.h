@@ -134,19 +134,12 @@ template <class Shape> __device__ __forceinline__ int own_pairs(int lane) { retu
 // c % E * (CB / E) + c / E), so that the lanes of a wave, each with its e-th value, write one run.  A lane works on the channel at its place.
 template <int CB, int E> __device__ __forceinline__ int placed_channel(int at) { return at % (CB / E) * E + at / (CB / E); }
 
-// The same value, which the compiler takes for another: what follows from it is made again instead of held in registers.
-__device__ __forceinline__ int made_anew(int v)
-{
-    asm volatile("" : "+v"(v));
-    return v;
-}
-
 // A layout's places for states lie in blocks of four, one vector each.  The last block with states of its own starts further left where it
 // would pass their end, and the blocks behind hold the first ones' again, so that some states are held two times (counts below four: element
 // by element, up to eight times).  Their copies run alike; c's value is shared out between them, a power of two of them, so that nothing is
 // rounded and their terms add up to the one.  Zeros for b and c in the places left over would not do: an infinite input or gradient times zero
-// is NaN, and NaN times zero would reach y.  (4 x 2048 rows of 2048 channels, forward and gradients: 13 states 127 and 359 us, 50 states 396
-// and 1815; with zeros kept by selections 139 and 389, 465 and 1963; with nothing against NaN 129 and 352, 401 and 1752.)  In the gradients
+// is NaN, and NaN times zero would reach y.  (4 x 2048 rows of 2048 channels, forward and gradients: 13 states 127 and 344 us, 50 states 396
+// and 1711; with zeros kept by selections 139 and 389, 465 and 1963; with nothing against NaN 129 and 352, 401 and 1752.)  In the gradients
 // the copies of g are shares too; what leaves is multiplied by their number.
 __device__ __forceinline__ int state_block(int j, int states)      // first state of block j; at least four states
 {
@@ -158,13 +151,22 @@ __device__ __forceinline__ int state_at(int place, int states)
     if (states >= 4) return state_block(place / 4, states) + place % 4;
     return states == 3 ? (place % 4 < 2 ? place % 4 : 2) : place & (states - 1);
 }
-// Of `held` places; more than half of them have a state of their own, or there are at most four states.
-__device__ __forceinline__ float state_copies(int n, int states, int held)
-{
-    if (states < 4) return (float)(held / 4 * (states == 1 ? 4 : states == 2 || n == 2 ? 2 : 1));
-    const int blocks = (states + 3) / 4;
-    return n / 4 < held / 4 - blocks || (n >= states - 4 && n < 4 * blocks - 4) ? 2.0f : 1.0f;
-}
+// How many of `held` places hold what place i of block j holds.  More than half of the places have a state of their own, or there are at most
+// four states, so of four and more it is two below `lo` and from `hi` on, else one.
+struct StateCopies {
+    int states, held, lo, hi;
+    __device__ __forceinline__ StateCopies(int j, int states_, int held_) : states(states_), held(held_)
+    {
+        const int blocks = (states + 3) / 4, again = held / 4 - blocks, b = j < blocks ? j : j - blocks, over = 4 * blocks - states;
+        lo = b < again ? 4 : b == blocks - 1 ? over : 0;
+        hi = b == blocks - 2 ? 4 - over : 4;
+    }
+    __device__ __forceinline__ float operator[](int i) const
+    {
+        if (states < 4) return (float)(held / 4 * (states == 1 ? 4 : states == 2 || i >= 2 ? 2 : 1));
+        return i < lo || i >= hi ? 2.0f : 1.0f;
+    }
+};
 
 // A channel's NS states of this lane, places n0 .. , in an array [..][channels][states]; zeros / not stored where it is not there.
 // kShared: there may be more places than states.

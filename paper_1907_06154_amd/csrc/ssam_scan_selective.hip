@@ -97,7 +97,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS > 4 ? 2 : sizeof(T) == 4 ? 3 : 4)
     T b_next[kPairs], c_next[kPairs];
     static_assert(kBlock % NP == 0, "a thread's values of b and c are all of one state");
     const int state = state_at(tid % NP, p.states);
-    const float share = 1.0f / state_copies(state, p.states, NP);
+    const float share = 1.0f / StateCopies(tid % NP / 4, p.states, NP)[tid % 4];
     auto request = [&](int row) {
         const int left = q.n - row;
         u_next = mine.load(in + (long long)row * p.in.row, p.in.row, left);
@@ -360,9 +360,10 @@ __global__ __launch_bounds__(kBlock) void scan_step(ScanStepParams p)
     const ChannelTile ct = channel_tile((int)(blockIdx.x / row_blocks), p.per_group, p.group_channels, step_channels(P));
     constexpr int kApart = kWave / P;            // the k-th of a lane's channels is k * kApart + lane / P: a load of the k-th is one run
     const int part = lane & (P - 1), first = lane / P, n0 = part * 4;
+    const StateCopies copies(part, p.states, 4 * P);
     float share[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) share[i] = kShared ? 1.0f / state_copies(state_at(n0 + i, p.states), p.states, 4 * P) : 1.0f;
+    for (int i = 0; i < 4; ++i) share[i] = kShared ? 1.0f / copies[i] : 1.0f;
     const bool own = part < KC && part * kApart + first < ct.n;
     const int c = ct.c0 + part * kApart + first; // the channel whose time step and output are this lane's
     struct Row {

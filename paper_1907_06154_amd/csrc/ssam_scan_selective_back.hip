@@ -149,9 +149,8 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
     else if (!last) load_states<NS, kShared>(p.ends + end_entry(p.pieces, slot, q.seq) * plane + cell, n0, p.states, live, g);
     else load_states<NS, kShared>(p.grad_final + q.seq * plane + cell, n0, p.states, live && p.grad_final, g);
     // !kWhole: the states do not meet, and every copy has the whole of g.
-    auto anew = [](int v) { return kShared ? made_anew(v) : v; };
     auto state_of = [&](int place) { return kShared ? state_at(place, p.states) : place; };
-    auto copies = [&](int place) { return kWhole && kShared ? state_copies(state_of(place), p.states, NP) : 1.0f; };
+    auto copies = [&](int place) { return kWhole && kShared ? StateCopies(place / 4, p.states, NP)[place % 4] : 1.0f; };
 #pragma unroll
     for (int i = 0; i < NS; ++i) da[i] = 0.0f;
     float sum = 0.0f;
@@ -217,7 +216,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
         if (gated) z_next = mine.load(gate + (long long)row * p.gate.row, p.gate.row, left);
         const T* b0 = kWhole ? pb + (long long)row * p.b.row : nullptr;
         const T* c0 = pc + (long long)row * p.c.row;
-        const int state = state_of(anew(tid) % NP);
+        const int state = state_of(tid % NP);
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
             const int i = tid + e * kBlock;
@@ -225,7 +224,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
             if (kWhole) b_next[e] = b0[r * (unsigned)p.b.row + state];
             c_next[e] = c0[r * (unsigned)p.c.row + state];
         }
-        if (kWhole && kMarkAhead) load_states<NS, kShared>(marks + (row / K) * plane, anew(n0), p.states, live, mark_next);
+        if (kWhole && kMarkAhead) load_states<NS, kShared>(marks + (row / K) * plane, n0, p.states, live, mark_next);
     };
     const int pairs = own_pairs<Shape>(lane), sum_at = sum_row<GL>(lane);
     const ChannelSums<GL> across(terms[kWhole ? wave : 0], lane);
@@ -257,7 +256,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
             dx[mine.row][mine.place(e)] = Pair{v, is && kWhole ? v * (float)u[e] : 0.0f};
             dys[mine.row][mine.place(e)] = dy[e];
         }
-        const float share = 1.0f / copies(anew(tid) % NP);
+        const float share = 1.0f / copies(tid % NP);
 #pragma unroll
         for (int e = 0; e < kPairs; ++e) {
             const int i = tid + e * kBlock, n = i % NP;
@@ -302,7 +301,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
                 // the states again, from the mark: those before this part's rows in passing, then each row's
                 float h[NS], hs[kKept][NS], as[kKept][NS], dyr[kKept];
                 Pair dv[kKept], w[kKept][NS / 4];
-                if (!kMarkAhead) load_states<NS, kShared>(marks + tile * plane, anew(n0), p.states, live, mark);
+                if (!kMarkAhead) load_states<NS, kShared>(marks + tile * plane, n0, p.states, live, mark);
 #pragma unroll
                 for (int k = 0; k < kKept; ++k) {
                     dv[k] = dx[part * kKept + k][place];
@@ -440,8 +439,8 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
             if (part_bc) {
                 float* to = part_bc + (long long)row * p.groups * 2 * p.states;
                 const unsigned wide = p.groups * 2 * p.states;
-                const int me = anew(tid), state = state_of(me % NP);
-                const float parts = me / NP % 2 ? 1.0f : copies(me % NP);      // of the gradient of b
+                const int state = state_of(tid % NP);
+                const float parts = tid / NP % 2 ? 1.0f : copies(tid % NP);      // of the gradient of b
                 for (int i = tid; i < K * 2 * NP; i += kBlock) {
                     const int r = i / (2 * NP), w = i / NP % 2, n = i % NP;
                     float v = sum_bc[0][r][w][n];
