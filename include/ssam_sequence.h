@@ -20,8 +20,13 @@
  * may run at the same time, must not share one.  Results do not depend on what a workspace held.  All sums over rows
  * and channels are added in a fixed order, so results are the same from run to run.
  *
+ * Infinities and NaN stay where the definitions have them: rows of no sequence, taps and states that do not exist and absent
+ * tensors add nothing, not even zero times an infinity.  (A single row's decay below 2^-126 counts as 0; an infinite state times it is NaN.)
+ *
+ * Tensors may reach over 2^59 elements at most, from the first to behind the last (SSAM_ERR_DIM).
+ *
  * An output may overlap neither an input nor another output (SSAM_ERR_ALIAS) except where a comment allows it; tensors
- * that are column ranges of one buffer do not overlap.
+ * that are column ranges of one buffer, of whole sequences or with all sequences' rows in turn, do not overlap.
  */
 #ifndef SSAM_SEQUENCE_H_
 #define SSAM_SEQUENCE_H_
@@ -103,8 +108,9 @@ int ssam_conv1d_step(const ssam_conv1d_step_args *args, void *hip_stream);
  * (zeros / not stored where NULL; d_final may be d_state); all of these fp32, contiguous.
  * Of sequences of more than one row, rows lie at most 2^24 elements apart (SSAM_ERR_DIM), here and for the gradients.
  * d_marks (NULL: not wanted): the state before rows 0, 16, 32 .. of every sequence, what ssam_scan_selective_backward
- * starts from; ssam_scan_selective_marks(args) entries of [channels][states] floats.
- * d_work: ssam_scan_selective_workspace_bytes(args) bytes, 16-byte aligned (NULL where that is 0).
+ * starts from; ssam_scan_selective_marks(args) entries of [channels][states] floats, one for each 16 rows and sequence.
+ * d_work: ssam_scan_selective_workspace_bytes(args) bytes, 16-byte aligned (NULL where that is 0): [channels][states + 1] floats for each piece
+ * of cut sequences, however many shorter sequences lie among them.
  * Schedules: one launch where sequences and channels fill the device; otherwise sequences are cut along time: the state
  * that each piece adds, the states between the pieces, then all rows (three launches). */
 typedef struct {
@@ -126,7 +132,8 @@ long long ssam_scan_selective_marks(const ssam_scan_selective_args *args);   /* 
  * grad_c contiguous within a row, [groups][states]), the others fp32 in the layout of what they belong to; each may be
  * absent (NULL).  d_grad_dt_bias is the sum of grad_dt over the rows, d_grad_state the gradient of d_state.  groups x
  * states must be below 2^27 (SSAM_ERR_DIM).
- * d_work: ssam_scan_selective_backward_workspace_bytes(args) bytes, 16-byte aligned. */
+ * d_work: ssam_scan_selective_backward_workspace_bytes(args) bytes, 16-byte aligned: as above, for grad_b and grad_c 2 x groups x states floats a
+ * row and 64 or 128 channels, for the parameters [channels][states + 2] floats a piece (of at most 2^15 blocks of 64 or 128 channels). */
 typedef struct {
     int dtype, channels, states, groups, softplus;
     ssam_sequences seq;

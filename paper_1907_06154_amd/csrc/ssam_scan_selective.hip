@@ -7,8 +7,8 @@
 // recurrence from there, leave y in LDS, and the threads that loaded the values finish them (skip, gate) and store them.
 //
 // Per state and row that is one exp, three products and two sums; the exp (8 cycles of a SIMD against 2.5 - 4 of the others) makes the
-// vector unit the bound, not memory (8 bytes a value): 8 x 4096 rows of 4096 channels, 16 states, bf16 600 us, of which the unit
-// is busy 77 % with the two waves per SIMD that there are, at 4.5 cycles an instruction; the bytes alone would take 219, the exps 119.
+// vector unit the bound, not memory (8 bytes a value): 8 x 4096 rows of 4096 channels, 16 states, bf16 590 us, of which the unit
+// is busy 71 - 79 % with the two waves per SIMD that there are, at 4.5 cycles an instruction; the bytes alone would take 211, the exps 119.
 #include "ssam_scan_selective.h"
 
 namespace ssam {

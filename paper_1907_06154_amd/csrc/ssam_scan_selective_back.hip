@@ -7,8 +7,9 @@
 // states again, part of a tile at a time: 8 rows' states and decays in registers (up to 16 states), 64 of them, and back over those.
 // (Marks every 8 rows would save the second half's way to its first row, 9 of 72 cycles a state, for 4 bytes more per row, channel and
 // 16 states, written and read; keeping 16 rows takes 128 registers and spills.)
-// Bound by vector issue: 22 instructions per row, channel and state, two waves a SIMD, which 235 registers leave; 4 x 2048 rows of 2048
-// channels and 16 states 268 us, what the pieces let out 60, the forward call 137.
+// Bound by vector issue: 22 instructions per row, channel and state, two waves a SIMD, which 233 registers leave; 4 x 2048 rows of 2048
+// channels and 16 states 274 us, what the pieces let out 61, the forward call 135.  With 16 states nothing spills; the kernels that do, by bytes
+// of scratch a lane: 8 states in 16 bits 52 and 80 (fewer than 8: 72 and 108), 32 states in fp32 28 (fewer: 48), fewer than 32 in 16 bits 16 - 24.
 //
 // The sums over channels: a wave's and the block's waves' through LDS, the blocks of a group through the workspace and a launch that
 // adds them in order.
@@ -103,14 +104,14 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
     constexpr int GL = Shape::GL, NS = Shape::NS, NP = Shape::kStates, CB = Shape::kChannels, K = kTile;
     constexpr int E = K * CB / kBlock;                   // values of a thread
     constexpr int kPairs = (K * NP + kBlock - 1) / kBlock;
-    // Rows whose states and decays are kept at a time, half of what spills (fp32 with eight values a thread: 456 us, 377 with four rows).
+    // Rows whose states and decays are kept at a time, half of what spills much more (fp32 with eight values a thread: 456 us, 377 with four rows).
     constexpr int kKept = NS == 16 || (E >= 8 && sizeof(T) == 4) ? 4 : 32 / NS;
     constexpr bool kMarkAhead = NS < 16;                 // the next tile's mark is requested with its rows
     // Whether a row counts for the rates' gradient is a branch behind the row, with more states a lane a selection each, whose values need
     // not be held so long (8 states 235 us, by selections 239; 20 states fp32 674 and 654).
     constexpr bool kRowBranch = NS == 4;
     constexpr int kRow = CB + CB / E;                    // a row in LDS, padded: see scan_rows
-    // A thread's eight values' parameters, 16 registers, come from LDS: those would spill (8 states 396 -> 330 us; four values' do not, and are held).
+    // A thread's eight values' parameters, 16 registers, come from LDS: those would spill too (8 states 396 -> 330 us; four values' do not, and are held).
     constexpr bool kFromLds = E >= 8;
     using Pair = RowVec<float, 2>;
     __shared__ Pair dx[K][kRow];                         // d, d u

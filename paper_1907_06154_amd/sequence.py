@@ -7,6 +7,9 @@ sequences + 1 offsets) or [sequences, rows, channels] (`lengths`: how many rows 
 any stride, channels are contiguous.  A result that is allocated here holds zeros in rows that belong to no sequence; one that
 is passed in keeps what it held there.  The kernels run on the device of their tensors, on its current stream or on `stream`;
 what a call allocates belongs to that stream, which orders its first use and its reuse.
+
+The calls are not recorded by autograd: results never require gradients, whatever their inputs do.  Gradients come from the
+`*_backward` calls, which a torch.autograd.Function's backward makes; d_final, d_state and pools are written in place unseen by it.
 """
 from __future__ import annotations
 
