@@ -20,8 +20,9 @@
  * may run at the same time, must not share one.  Results do not depend on what a workspace held.  All sums over rows
  * and channels are added in a fixed order, so results are the same from run to run.
  *
- * Infinities and NaN stay where the definitions have them: rows of no sequence, taps and states that do not exist and absent
- * tensors add nothing, not even zero times an infinity.  (A single row's decay below 2^-126 counts as 0; an infinite state times it is NaN.)
+ * Infinities and NaN stay where the definitions have them: rows of no sequence, an absent skip, and what kernels hold beyond the
+ * last row, state or channel add nothing, not even zero times an infinity.  (A single row's decay below 2^-126 counts as 0, which
+ * times an infinite state is NaN.)
  *
  * Tensors may reach over 2^59 elements at most, from the first to behind the last (SSAM_ERR_DIM).
  *

@@ -51,6 +51,7 @@ __device__ __forceinline__ float quad_moved(float v)
 // each, and every output -- 4 GL states of b, as many of c -- is added up by LP lanes, eight channels each: 8 vector instructions
 // where swaps between rows of lanes and DPP took 22.  A wave reads what itself wrote (the LDS keeps a wave's order), one step later,
 // so no barrier and no wait is needed.  The vectors lie so that eight lanes' writes and 32 lanes' reads each meet every bank once.
+// A lane without a channel writes beside them: its terms are zeros, or NaN where b or c is infinite, and the zeros in its own vectors stay.
 template <int GL>
 struct ChannelSums {
     static constexpr int kOutputs = 8 * GL, LP = kWave / kOutputs;
@@ -62,14 +63,14 @@ struct ChannelSums {
 
     // channel c of group g
     static __device__ __forceinline__ int vector(int c, int g) { return c % LP + LP * g + 12 * (c / LP % 2) + 24 * (c / (2 * LP)); }
-    __device__ __forceinline__ ChannelSums(float* buffer, int lane)
+    __device__ __forceinline__ ChannelSums(float* buffer, int lane, bool live)
     {
         const int o = lane / LP, part = lane % LP;
         i = o % 4;
         group = o / 4 % GL;
         which = o / (4 * GL);
         at = buffer;
-        to = vector(lane_channel<GL>(lane), lane_group<GL>(lane)) * 4;
+        to = (live ? vector(lane_channel<GL>(lane), lane_group<GL>(lane)) : 8 + lane % 4) * 4;      // (8 .. 11 are no lane's)
         from = which * kApart + vector(part, group) * 4 + i;
     }
     __device__ __forceinline__ void put(int step, const float (&vb)[4], const float (&vc)[4]) const
@@ -196,12 +197,14 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
     }
     auto bias = [&](int e) { return kFromLds ? per_channel[0][mine.col + e] : bias_held[e]; };
     auto skip = [&](int e) { return kFromLds ? per_channel[1][mine.col + e] : skip_held[e]; };
-    // Channels behind the tile keep zeros throughout: they add nothing to the sums over channels.
+    // Channels behind the tile keep d = 0, d u = 0, dy = 0 throughout.
     if (ct.n < CB)
         for (int i = tid; i < K * kRow; i += kBlock) {
             dx[i / kRow][i % kRow] = Pair{0.0f, 0.0f};
             dys[i / kRow][i % kRow] = 0.0f;
         }
+    if (kWhole && ct.n < CB)
+        for (int i = lane; i < 2 * ChannelSums<GL>::kFloats; i += kWave) terms[wave][i] = 0.0f;
     __syncthreads();                                     // before the first tile's values go there
 
     using Vec = RowVec<T, E>;
@@ -228,7 +231,7 @@ __global__ __launch_bounds__(kBlock, Shape::NS <= 8 ? 2 : 1) void scan_back(Back
         if (kWhole && kMarkAhead) load_states<NS, kShared>(marks + (row / K) * plane, n0, p.states, live, mark_next);
     };
     const int pairs = own_pairs<Shape>(lane), sum_at = sum_row<GL>(lane);
-    const ChannelSums<GL> across(terms[kWhole ? wave : 0], lane);
+    const ChannelSums<GL> across(terms[kWhole ? wave : 0], lane, live);
 
     const int tiles = (q.n + K - 1) / K;
     if (tiles > 0) request((tiles - 1) * K);

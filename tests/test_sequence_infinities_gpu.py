@@ -222,3 +222,25 @@ def test_an_infinite_state_passes_pieces(N):
     assert (got.x[:291, at] == INF).all() and (got.state[0, at] == INF).all()
     got.x[:291, at], got.state[0, at] = 0, 0
     assert torch.isfinite(got.x).all() and torch.isfinite(got.state).all()
+
+
+@pytest.mark.parametrize("D,N", [(70, 16), (6, 16), (70, 4), (130, 8), (33, 32), (1, 64), (64, 16), (128, 5)])
+def test_an_infinity_of_b_or_c_reaches_its_own_sums(D, N):
+    """The gradients of b and c are sums over channels: those that a tile has room for but the call does not have are not among them."""
+    for dtype, rows in zip(TYPES, (40, 20, 150)):
+        print(dtype, flush=True)
+        k = Positive(rows, N, dtype, D)
+        t, n = 17, N - 1
+        clean = k.back(k.marked())
+        there = k.b[t, 0, n].item()
+        k.b[t, 0, n] = INF                  # an infinite state of every channel from row t on
+        got = k.back(k.marked())
+        assert (got.c[t:, 0, n] == INF).all()
+        got.c[t:, 0, n] = clean.c[t:, 0, n]
+        assert torch.equal(got.c, clean.c) and torch.equal(got.b, clean.b)
+        k.b[t, 0, n] = there
+        k.c[t, 0, n] = INF                  # an infinite gradient of every channel's state up to row t
+        got = k.back(k.marked())
+        assert (got.b[:t + 1, 0, n] == INF).all()
+        got.b[:t + 1, 0, n] = clean.b[:t + 1, 0, n]
+        assert torch.equal(got.b, clean.b) and torch.equal(got.c, clean.c)
