@@ -8,8 +8,8 @@
 // (Marks every 8 rows would save the second half's way to its first row, 9 of 72 cycles a state, for 4 bytes more per row, channel and
 // 16 states, written and read; keeping 16 rows takes 128 registers and spills.)
 // Bound by vector issue: 22 instructions per row, channel and state, two waves a SIMD, which 233 registers leave; 4 x 2048 rows of 2048
-// channels and 16 states 274 us, what the pieces let out 61, the forward call 135.  With 16 states nothing spills; the kernels that do, by bytes
-// of scratch a lane: 8 states in 16 bits 52 and 80 (fewer than 8: 72 and 108), 32 states in fp32 28 (fewer: 48), fewer than 32 in 16 bits 16 - 24.
+// channels and 16 states 270 us, what the pieces let out 61, the forward call 135.  With 16 states nothing spills; the kernels that do, by bytes
+// of scratch a lane: 8 states in 16 bits 52 and 80 (fewer than 8: 72 and 100), 32 states in fp32 28 (fewer: 48), fewer than 32 in 16 bits 16 - 24.
 //
 // The sums over channels: a wave's and the block's waves' through LDS, the blocks of a group through the workspace and a launch that
 // adds them in order.
