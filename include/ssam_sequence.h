@@ -1,6 +1,6 @@
-/* ssam_sequence.h -- filters and scans along time, channel by channel: the two halves of a state space layer of a
- * language model, in the C ABI's manner (every convention of ssam.h holds here too, except where a line below says
- * otherwise).
+/* ssam_sequence.h -- filters and scans along time, channel by channel or with a matrix per head for a state, and the norm
+ * around them: the parts of a state space layer of a language model, in the C ABI's manner (every convention of ssam.h holds
+ * here too, except where a line below says otherwise).
  *
  * Data: rows are tokens, channels lie side by side.  A tensor of rows is described by ssam_rows: the address of row 0's
  * channel 0, and the elements from one row, and from one sequence, to the next; the channels of a row are contiguous.
@@ -41,6 +41,8 @@ extern "C" {
 #define SSAM_MAX_TAPS 8        /* longest filter of ssam_conv1d                               */
 #define SSAM_MAX_STATES 64     /* states per channel of ssam_scan_selective                    */
 #define SSAM_MARK_ROWS 16      /* ssam_scan_selective: rows from one mark to the next          */
+#define SSAM_DELTA_ROWS 64     /* ssam_scan_delta: rows that are taken together                */
+#define SSAM_MAX_KEY 256       /* ssam_scan_delta: longest key                                 */
 
 typedef struct {
     void *d;                   /* device; NULL: not there (where a tensor is optional)         */
@@ -162,6 +164,85 @@ typedef struct {
     long long slot_stride;     /* floats, >= channels * states                                 */
 } ssam_scan_selective_step_args;
 int ssam_scan_selective_step(const ssam_scan_selective_step_args *args, void *hip_stream);
+
+/* Scan whose state is a matrix per head, corrected by every row (the gated delta rule).  For every head h, which uses key head
+ * h / (heads / key_heads), with the state S [key_dim][value_dim] of the row before:
+ *     S' = exp(g_t) S,    u = beta_t (v_t - S'^T k_t),    S = S' + k_t u^T,    out_t = scale S^T q_t
+ * unit != 0: q_t and k_t are divided by sqrt(their squares' sum + 1e-6) first.  q, k: rows of key_heads x key_dim elements, v and
+ * out: of heads x value_dim, a head's elements contiguous, *_head elements from one head to the next; g, beta: rows of `heads`
+ * floats (g.d NULL: no decay).  d_state, d_final: [sequences][heads][key_dim][value_dim] floats, the state before the first and
+ * after the last row (zeros / not stored where NULL; d_final may be d_state).  g below -1000 counts as -1000, whose exponential is 0.
+ * Rows are taken 64 at a time: a value that is not finite makes the other rows of its 64, of its head, NaN too (rows behind them
+ * follow from the state); rows of no sequence reach nothing.
+ * d_marks (NULL: not wanted): what ssam_scan_delta_backward starts from, ssam_scan_delta_marks(args) entries of
+ * [heads][key_dim + 64][value_dim] floats: for each 64 rows and sequence the state before them and what the rows correct it by.
+ * Operands of the matrix products are held as pairs of fp16, scaled by powers of two, that keep 22 bits of an fp32 value.
+ * d_work: ssam_scan_delta_workspace_bytes(args) bytes, 16-byte aligned. */
+typedef struct {
+    int dtype, heads, key_heads, key_dim, value_dim, unit;
+    float scale;
+    ssam_sequences seq;
+    ssam_rows q, k, v, out, g, beta;
+    long long q_head, k_head, v_head, out_head;
+    const float *d_state;
+    float *d_final, *d_marks;
+    void *d_work;
+    size_t work_bytes;
+} ssam_scan_delta_args;
+int ssam_scan_delta(const ssam_scan_delta_args *args, void *hip_stream);
+size_t ssam_scan_delta_workspace_bytes(const ssam_scan_delta_args *args);
+long long ssam_scan_delta_marks(const ssam_scan_delta_args *args);   /* host only; 0 for invalid arguments */
+
+/* ssam_scan_delta for one more row of each of `rows` sequences; slots as in ssam_conv1d_step, slot i at
+ * d_state + i * slot_stride floats, [heads][key_dim][value_dim] contiguous, updated in place. */
+typedef struct {
+    int dtype, heads, key_heads, key_dim, value_dim, unit;
+    float scale;
+    int rows, slots;
+    const int *d_slots;
+    ssam_rows q, k, v, out, g, beta;   /* batch strides unused                                 */
+    long long q_head, k_head, v_head, out_head;
+    float *d_state;
+    long long slot_stride;     /* floats, >= heads * key_dim * value_dim                       */
+} ssam_scan_delta_step_args;
+int ssam_scan_delta_step(const ssam_scan_delta_step_args *args, void *hip_stream);
+
+/* Root-mean-square norm of the groups of a row, width = channels / groups elements each:
+ *     s = in + residual, rounded to dtype (in where there is no residual);   y = s / sqrt(mean(s^2) + eps) * weight
+ *     out = gate ? y * gate / (1 + exp(-gate)) : y
+ * `sequences` x `rows` rows (a batch's strides count from sequence to sequence).  sum (may be absent, or residual itself) receives s;
+ * the norm is that of s as it is stored, so that s is all that the gradients need.  weight: [width] in param_dtype (dtype or
+ * SSAM_F32), NULL: ones.
+ * ssam_rms_norm_e4m3: out is in 8 bits (e4m3, 448 at most) with a scale for every `block` channels, a divisor of width:
+ *     scale = max over the block of |y| / 448 (at least 2^-126; 1 where all are zero),   out = y / scale, rounded to nearest
+ * d_scales: [sequences * rows][channels / block] floats; out's strides count bytes.  (y / scale is made with the rounded reciprocal.) */
+typedef struct {
+    int dtype, param_dtype, channels, groups, block;   /* block: ssam_rms_norm_e4m3 only         */
+    int sequences, rows;
+    float eps;                 /* >= 0                                                         */
+    ssam_rows in, residual, sum, gate, out;
+    const void *d_weight;
+    float *d_scales;           /* ssam_rms_norm_e4m3 only                                      */
+} ssam_rms_norm_args;
+int ssam_rms_norm(const ssam_rms_norm_args *args, void *hip_stream);
+int ssam_rms_norm_e4m3(const ssam_rms_norm_args *args, void *hip_stream);
+
+/* Gradients of ssam_rms_norm.  in: what was normalised (its sum, where it had a residual); grad_out: gradient of its result;
+ * grad_sum (may be absent): of its sum, which is added to grad_in.  grad_in, that of in and of residual alike, and grad_gate are in
+ * dtype, d_grad_weight in param_dtype; each may be absent (NULL).
+ * d_work: ssam_rms_norm_backward_workspace_bytes(args) bytes (0 without d_grad_weight), 16-byte aligned. */
+typedef struct {
+    int dtype, param_dtype, channels, groups;
+    int sequences, rows;
+    float eps;
+    ssam_rows in, gate, grad_out, grad_sum, grad_in, grad_gate;
+    const void *d_weight;
+    void *d_grad_weight;
+    void *d_work;
+    size_t work_bytes;
+} ssam_rms_norm_backward_args;
+int ssam_rms_norm_backward(const ssam_rms_norm_backward_args *args, void *hip_stream);
+size_t ssam_rms_norm_backward_workspace_bytes(const ssam_rms_norm_backward_args *args);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,168 @@
+// What the kernels of the scan with matrix states (ssam_scan_delta) share.
+//
+// Rows are taken C = 64 at a time.  With G_t the sum of g over the block's rows up to t, D_ij = exp(G_i - G_j) for i >= j, 0 otherwise,
+// A = strictly lower part of (K K^T o D), S the state before the block and b = beta:
+//     X = V - exp(G) K S,    R = (I + A diag(b))^-1 X,    U = b R,    O = scale (exp(G) Q S + (Q K^T o D) U),
+//     state behind it = exp(G_C) S + (exp(G_C - G) K)^T U
+// R is what each row's value misses of what the state holds for its key.  Everything but S and V is known without the state, so it is made for all
+// blocks at once (delta_prepare); the rest follows the sequence.
+//
+// Matrix products run on v_mfma_f32_16x16x32_f16.  q, k of 16 bits are one fp16 operand, exact, with a power of two per row taken
+// out; everything else is a pair hi + lo of fp16 that keeps 22 bits of the fp32 value: two products against q or k, three
+// between two such pairs (lo lo is below 2^-22).  bf16 pairs keep 16 bits, which the state's fp32 would show.
+//
+// Operand layout: lane (g = lane / 16, r = lane % 16) of an A operand holds row r, elements 8 g .. 8 g + 7 of 32 along the sum; of a B
+// operand column r and the same elements; of a result rows 4 g .. 4 g + 3, column r.  What a row of a result tile stands for is free:
+// tiles 2 p and 2 p + 1 stand for indices 32 p + 8 g + (0 .. 3) and + (4 .. 7), so that a lane's eight values of both are the eight that
+// it holds of the next product's B operand, in order.  So S -> X -> R -> U -> S stays in a wave's registers, 16 columns of the values a
+// tile; only operands made from q, k and the block's matrices are loaded, and those are the same for every column.
+#pragma once
+#include "ssam_rows.h"
+
+namespace ssam {
+
+constexpr int kDeltaRows = SSAM_DELTA_ROWS;
+
+typedef _Float16 Half8 __attribute__((ext_vector_type(8)));
+typedef RowVec<float, 4> Float4;
+
+__device__ __forceinline__ Float4 mfma(Half8 a, Half8 b, Float4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+struct HalfPair {
+    Half8 hi, lo;
+};
+
+// A power of two that brings m (the largest magnitude of what it scales) to 2^10 .. 2^11, and its reciprocal; infinities and NaN pass.
+struct Scale {
+    float to, back;
+    __device__ __forceinline__ Scale() {}
+    __device__ __forceinline__ explicit Scale(float m)
+    {
+        unsigned e = (__builtin_bit_cast(unsigned, m) >> 23) & 255u;
+        e = e < 11u ? 11u : e;
+        to = __builtin_bit_cast(float, (264u - e) << 23);
+        back = __builtin_bit_cast(float, (e - 10u) << 23);
+    }
+};
+
+__device__ __forceinline__ void split2(float a, float b, Half8& hi, Half8& lo, int at)
+{
+    const auto h = __builtin_amdgcn_cvt_pkrtz(a, b);
+    const auto l = __builtin_amdgcn_cvt_pkrtz(a - (float)h[0], b - (float)h[1]);
+    hi[at] = (_Float16)h[0];
+    hi[at + 1] = (_Float16)h[1];
+    lo[at] = (_Float16)l[0];
+    lo[at + 1] = (_Float16)l[1];
+}
+// The values of two result tiles as a B operand.
+__device__ __forceinline__ HalfPair split(const Float4& a, const Float4& b, float to)
+{
+    HalfPair p;
+    split2(a[0] * to, a[1] * to, p.hi, p.lo, 0);
+    split2(a[2] * to, a[3] * to, p.hi, p.lo, 2);
+    split2(b[0] * to, b[1] * to, p.hi, p.lo, 4);
+    split2(b[2] * to, b[3] * to, p.hi, p.lo, 6);
+    return p;
+}
+
+// The larger of two magnitudes; a NaN may be passed over, as it reaches the products by itself.
+__device__ __forceinline__ float larger(float m, float v) { return __builtin_fmaxf(m, __builtin_fabsf(v)); }
+__device__ __forceinline__ float larger(float m, const Float4& v) { return larger(larger(larger(larger(m, v[0]), v[1]), v[2]), v[3]); }
+// Over the four lanes of a column, lane, lane ^ 16, ^ 32 and ^ 48.
+__device__ __forceinline__ float over_column(float m)
+{
+    m = __builtin_fmaxf(m, __shfl_xor(m, 16));
+    return __builtin_fmaxf(m, __shfl_xor(m, 32));
+}
+
+// What row r of result tile m stands for.
+__device__ __forceinline__ int tile_row(int m, int r) { return 32 * (m >> 1) + 8 * (r >> 2) + 4 * (m & 1) + (r & 3); }
+
+// ---- a block's matrices and factors, from delta_prepare --------------------------------------------------------------------
+// Lower triangular [64][64] as A operands: tile m's rows against 32 columns s, those with s <= m / 2; the transposed ones s >= m / 2.
+constexpr int kTriOperands = 6;
+__device__ __forceinline__ int lower_operand(int m, int s) { return m < 2 ? m : 2 * (m - 1) + s; }
+__device__ __forceinline__ int upper_operand(int m, int s) { return m < 2 ? 2 * m + s : 2 + m; }
+
+struct BlockFactors {
+    float reads[kDeltaRows];     // exp(G_t) x the key's factor
+    float beta[kDeltaRows];
+    float writes[kDeltaRows];    // exp(G_C - G_t) x the key's factor
+    float asks[kDeltaRows];      // scale x exp(G_t) x the query's factor
+    float key[kDeltaRows], query[kDeltaRows];   // what an element is multiplied by to become its fp16 operand
+    float total;                 // exp(G_C)
+    float solve_back, mix_back;  // what the two matrices' operands are to be multiplied by
+    float pad;
+};
+struct Block {
+    Half8 solve[2][kTriOperands][kWave];        // hi and lo of the system's inverse
+    Half8 mix[2][kTriOperands][kWave];          // and of scale (Q K^T o D)
+    BlockFactors f;
+};
+
+struct DeltaParams {
+    Pieces pieces;
+    ssam_rows q, k, v, out, g, beta;
+    long long q_head, k_head, v_head, out_head;
+    const float *state;
+    float *final, *marks;
+    Block* blocks;               // [slots][heads]
+    int heads, key_heads, key_dim, value_dim, unit;
+    float scale;
+    int tiles;                   // of the walk: blocks along the values
+};
+
+// A mark: the state before a block, [key_dim][value_dim], and its R, [64][value_dim].
+__device__ __forceinline__ float* mark_of(float* marks, const DeltaParams& p, long long slot, int head)
+{
+    return marks + (slot * p.heads + head) * (long long)(p.key_dim + kDeltaRows) * p.value_dim;
+}
+
+// ---- checks ----------------------------------------------------------------------------------------------------------------
+template <class Args>
+int check_delta(const Args& a)
+{
+    if (!type_bytes(a.dtype)) return SSAM_ERR_ENUM;
+    if (a.heads < 1 || a.key_heads < 1 || a.heads % a.key_heads || a.key_dim < 1 || a.key_dim > SSAM_MAX_KEY || a.value_dim < 1) return SSAM_ERR_SHAPE;
+    if (a.heads > kMaxChannels || a.value_dim > kMaxChannels || (long long)a.heads * a.value_dim > kMaxChannels) return SSAM_ERR_DIM;
+    return SSAM_OK;
+}
+inline long long heads_width(int heads, long long apart, int dim) { return run_extent(heads, apart, dim); }
+
+template <class Args>
+int check_delta_rows(const Args& a, const ssam_sequences& q)
+{
+    const int esz = type_bytes(a.dtype);
+    for (long long s : {a.q_head, a.k_head, a.v_head})
+        if (s < 0 || s > kMaxStride) return SSAM_ERR_DIM;
+    if (int e = check_rows(a.q, q, heads_width(a.key_heads, a.q_head, a.key_dim), esz, false)) return e;
+    if (int e = check_rows(a.k, q, heads_width(a.key_heads, a.k_head, a.key_dim), esz, false)) return e;
+    if (int e = check_rows(a.v, q, heads_width(a.heads, a.v_head, a.value_dim), esz, false)) return e;
+    if (int e = check_rows(a.g, q, a.heads, 4, true)) return e;
+    return check_rows(a.beta, q, a.heads, 4, false);
+}
+// A result's heads must not share elements either.
+inline int check_out_heads(const ssam_rows& r, const ssam_sequences& q, int heads, long long apart, int dim, int esz, bool optional)
+{
+    if (apart < 0 || apart > kMaxStride || (r.d && heads > 1 && apart < dim)) return SSAM_ERR_DIM;
+    return check_out_rows(r, q, heads_width(heads, apart, dim), esz, optional);
+}
+
+template <class F>
+int with_delta_type(int dtype, F f)
+{
+    if (dtype == SSAM_F32) return f(float());
+    if (dtype == SSAM_F16) return f(_Float16());
+    return f(__bf16());
+}
+// f gets the 32s of a key, rounded up to a power of two, as a compile-time constant.
+template <class F>
+int with_key(int key_dim, F f)
+{
+    if (key_dim <= 32) return f(std::integral_constant<int, 1>{});
+    if (key_dim <= 64) return f(std::integral_constant<int, 2>{});
+    if (key_dim <= 128) return f(std::integral_constant<int, 4>{});
+    return f(std::integral_constant<int, 8>{});
+}
+
+}  // namespace ssam

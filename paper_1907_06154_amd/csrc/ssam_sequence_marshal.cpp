@@ -7,8 +7,11 @@
 
 #include <ATen/Functions.h>
 
+#include <cmath>
+#include <cstring>
 #include <stdexcept>
 #include <string>
+#include <vector>
 
 #include "../../include/ssam_sequence.h"
 
@@ -27,6 +30,14 @@ struct {
     decltype(&ssam_scan_selective_backward) scan_backward;
     decltype(&ssam_scan_selective_backward_workspace_bytes) scan_backward_bytes;
     decltype(&ssam_scan_selective_step) scan_step;
+    decltype(&ssam_scan_delta) delta;
+    decltype(&ssam_scan_delta_workspace_bytes) delta_bytes;
+    decltype(&ssam_scan_delta_marks) delta_marks;
+    decltype(&ssam_scan_delta_step) delta_step;
+    decltype(&ssam_rms_norm) norm;
+    decltype(&ssam_rms_norm_e4m3) norm_e4m3;
+    decltype(&ssam_rms_norm_backward) norm_backward;
+    decltype(&ssam_rms_norm_backward_workspace_bytes) norm_backward_bytes;
 } entry;
 PyObject* status_error;      // the binding's exception class, called with (status, entry point)
 
@@ -47,7 +58,7 @@ std::string shape_text(at::IntArrayRef s)
 }
 std::string type_text(at::ScalarType t)
 {
-    return t == at::kFloat ? "torch.float32" : t == at::kHalf ? "torch.float16" : t == at::kBFloat16 ? "torch.bfloat16" : t == at::kInt ? "torch.int32" : c10::toString(t);
+    return t == at::kFloat8_e4m3fn ? "torch.float8_e4m3fn" : t == at::kFloat ? "torch.float32" : t == at::kHalf ? "torch.float16" : t == at::kBFloat16 ? "torch.bfloat16" : t == at::kInt ? "torch.int32" : c10::toString(t);
 }
 
 const Tensor& tensor(PyObject* o, const char* name)
@@ -119,11 +130,12 @@ int held_to_int(int64_t v, const char* name)
     return (int)v;
 }
 
-ssam_sequences sequences(const Tensor& like, const Tensor* starts, const Tensor* lengths)
+// `tail`: dimensions of a row.
+ssam_sequences sequences(const Tensor& like, const Tensor* starts, const Tensor* lengths, int tail = 1)
 {
     if (starts && lengths) fail("starts", "and lengths exclude one another");
-    ssam_sequences q{1, held_to_int(like.size(-2), "the number of rows"), nullptr, nullptr};
-    if (like.dim() == 2) {
+    ssam_sequences q{1, held_to_int(like.size(-1 - tail), "the number of rows"), nullptr, nullptr};
+    if (like.dim() == 1 + tail) {
         if (lengths) fail("lengths", "belongs to [sequences, rows, channels]");
         if (!starts) return q;
         if (starts->dim() != 1 || starts->numel() < 1 || !starts->is_contiguous()) fail("starts", "must be a contiguous 1D tensor of sequences + 1 offsets");
@@ -540,32 +552,301 @@ PyObject* scan_step(PyObject*, PyObject* const* v, Py_ssize_t n)
     });
 }
 
-// bind(exception class, addresses of the ten entry points in the order of `entry`)
-PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n)
+// ---- scan with matrix states -------------------------------------------------------------------------------------------
+const Tensor& main_heads(PyObject* o)
+{
+    const Tensor& t = tensor(o, "d_v");
+    if (!t.is_cuda()) fail("d_v", "must live in GPU memory");
+    if (t.dim() != 3 && t.dim() != 4) fail("d_v", "must be [rows, heads, width] or [sequences, rows, heads, width]");
+    return t;
+}
+
+// Rows of heads: v's type, device and leading extents, a head's elements contiguous.
+ssam_rows head_rows(const Tensor& t, const char* name, const Tensor& v, int64_t heads, int64_t width, long long* apart)
+{
+    same_kind(t, name, v.scalar_type(), v);
+    const auto lead = v.sizes().slice(0, v.dim() - 2);
+    if (t.dim() != v.dim() || t.sizes().slice(0, lead.size()) != lead || t.size(-2) != heads || t.size(-1) != width)
+        fail(name, "must have shape " + shape_text(lead) + " + (" + std::to_string(heads) + ", " + std::to_string(width) + "), not " + shape_text(t.sizes()));
+    const auto s = t.strides();
+    if (s.back() != 1 && t.sizes().back() != 1) fail(name, "must have contiguous elements of a head (stride 1)");
+    *apart = s[s.size() - 2];
+    return s.size() == 3 ? ssam_rows{t.data_ptr(), 0, s[0]} : ssam_rows{t.data_ptr(), s[0], s[1]};
+}
+// A float for every row and head.
+ssam_rows head_values(const Tensor* t, const char* name, const Tensor& v)
+{
+    if (!t) return ssam_rows{nullptr, 0, 0};
+    const auto want = v.sizes().slice(0, v.dim() - 1);
+    if (t->sizes() != want) fail(name, "must have shape " + shape_text(want) + ", not " + shape_text(t->sizes()));
+    same_kind(*t, name, at::kFloat, v);
+    const auto s = t->strides();
+    if (s.back() != 1 && t->sizes().back() != 1) fail(name, "must have contiguous heads (stride 1)");
+    return s.size() == 2 ? ssam_rows{t->data_ptr(), 0, s[0]} : ssam_rows{t->data_ptr(), s[0], s[1]};
+}
+
+// q, k, v, g, beta: five objects from v on; scale, unit.
+template <class Args>
+const Tensor& delta_inputs(Args* s, PyObject* const* o, PyObject* scale, PyObject* unit)
+{
+    const Tensor &k = tensor(o[1], "d_k"), &v = main_heads(o[2]);
+    s->dtype = code_of(v.scalar_type(), "d_v");
+    s->heads = held_to_int(v.size(-2), "the number of heads");
+    s->value_dim = held_to_int(v.size(-1), "a value's width");
+    if (k.dim() != v.dim()) fail("d_k", "must have as many dimensions as d_v, not shape " + shape_text(k.sizes()));
+    s->key_heads = held_to_int(k.size(-2), "the number of key heads");
+    s->key_dim = held_to_int(k.size(-1), "a key's width");
+    s->q = head_rows(tensor(o[0], "d_q"), "d_q", v, s->key_heads, s->key_dim, &s->q_head);
+    s->k = head_rows(k, "d_k", v, s->key_heads, s->key_dim, &s->k_head);
+    s->v = head_rows(v, "d_v", v, s->heads, s->value_dim, &s->v_head);
+    s->g = head_values(optional(o[3], "g"), "g", v);
+    s->beta = head_values(&tensor(o[4], "beta"), "beta", v);
+    s->unit = truth(unit);
+    if (scale == Py_None) {
+        s->scale = 1.0f / std::sqrt((float)(s->key_dim > 0 ? s->key_dim : 1));
+    } else {
+        s->scale = (float)PyFloat_AsDouble(scale);
+        if (PyErr_Occurred()) throw 0;
+    }
+    return v;
+}
+
+long long delta_marks_of(const Tensor& k, const Tensor& v, const ssam_sequences& q)
+{
+    ssam_scan_delta_args s{};
+    s.dtype = code_of(v.scalar_type(), "d_v");
+    s.heads = held_to_int(v.size(-2), "the number of heads");
+    s.key_heads = held_to_int(k.size(-2), "the number of key heads");
+    s.key_dim = held_to_int(k.size(-1), "a key's width");
+    s.value_dim = held_to_int(v.size(-1), "a value's width");
+    s.seq = q;
+    return entry.delta_marks(&s);
+}
+
+float* delta_marks_for(const Tensor* t, const Tensor& k, const Tensor& v, const ssam_sequences& q)
+{
+    if (!t) return nullptr;
+    if (t->dim() != 4 || t->size(0) < delta_marks_of(k, v, q) || t->size(1) != v.size(-2) || t->size(2) != k.size(-1) + SSAM_DELTA_ROWS || t->size(3) != v.size(-1))
+        fail("d_marks", "must come from ssam_scan_delta_marks for these sequences");
+    return dense<float>(t, "d_marks", v, at::kFloat, t->sizes());
+}
+
+// delta_marks(d_k, d_v, starts, lengths) -> d_marks
+PyObject* delta_marks(PyObject*, PyObject* const* o, Py_ssize_t n)
+{
+    if (!arity(n, 4)) return nullptr;
+    return guarded([&] {
+        const Tensor &k = tensor(o[0], "d_k"), &v = main_heads(o[1]);
+        if (k.dim() != v.dim()) fail("d_k", "must have as many dimensions as d_v, not shape " + shape_text(k.sizes()));
+        const long long count = delta_marks_of(k, v, sequences(v, optional(o[2], "starts"), optional(o[3], "lengths"), 2));
+        return wrap(at::empty({count, v.size(-2), k.size(-1) + SSAM_DELTA_ROWS, v.size(-1)}, v.options().dtype(at::kFloat)));
+    });
+}
+
+// delta_bytes(d_k, d_v, starts, lengths) -> bytes of workspace
+PyObject* delta_bytes(PyObject*, PyObject* const* o, Py_ssize_t n)
+{
+    if (!arity(n, 4)) return nullptr;
+    return guarded([&] {
+        const Tensor &k = tensor(o[0], "d_k"), &v = main_heads(o[1]);
+        if (k.dim() != v.dim()) fail("d_k", "must have as many dimensions as d_v, not shape " + shape_text(k.sizes()));
+        ssam_scan_delta_args s{};
+        s.dtype = code_of(v.scalar_type(), "d_v");
+        s.heads = held_to_int(v.size(-2), "the number of heads");
+        s.key_heads = held_to_int(k.size(-2), "the number of key heads");
+        s.key_dim = held_to_int(k.size(-1), "a key's width");
+        s.value_dim = held_to_int(v.size(-1), "a value's width");
+        s.seq = sequences(v, optional(o[2], "starts"), optional(o[3], "lengths"), 2);
+        return PyLong_FromSize_t(entry.delta_bytes(&s));
+    });
+}
+
+// delta(d_q, d_k, d_v, g, beta, scale, unit, d_state, d_final, d_marks, starts, lengths, d_out, d_work, stream) -> d_out
+PyObject* delta(PyObject*, PyObject* const* o, Py_ssize_t n)
+{
+    if (!arity(n, 15)) return nullptr;
+    return guarded([&] {
+        ssam_scan_delta_args s{};
+        const Tensor& v = delta_inputs(&s, o, o[5], o[6]);
+        s.seq = sequences(v, optional(o[10], "starts"), optional(o[11], "lengths"), 2);
+        const int64_t carried[] = {s.seq.sequences, s.heads, s.key_dim, s.value_dim};
+        s.d_state = dense<const float>(optional(o[7], "d_state"), "d_state", v, at::kFloat, carried);
+        s.d_final = dense<float>(optional(o[8], "d_final"), "d_final", v, at::kFloat, carried);
+        s.d_marks = delta_marks_for(optional(o[9], "d_marks"), tensor(o[1], "d_k"), v, s.seq);
+        const Tensor* given = optional(o[12], "d_out");
+        const Tensor out = result(given, v, s.seq.d_begin || s.seq.d_end);
+        s.out = head_rows(out, "d_out", v, s.heads, s.value_dim, &s.out_head);
+        const Tensor work = workspace(entry.delta_bytes(&s), optional(o[13], "d_work"), v);
+        if (work.defined()) {
+            s.d_work = work.data_ptr();
+            s.work_bytes = work.nbytes();
+        }
+        call(entry.delta, s, o[14], "ssam_scan_delta");
+        if (given) {
+            Py_INCREF(o[12]);
+            return o[12];
+        }
+        return wrap(out);
+    });
+}
+
+// delta_step(d_q, d_k, d_v, g, beta, d_state, scale, unit, slots, d_out, stream) -> d_out
+PyObject* delta_step(PyObject*, PyObject* const* o, Py_ssize_t n)
 {
     if (!arity(n, 11)) return nullptr;
-    void* p[10];
-    for (int i = 0; i < 10; ++i) p[i] = PyLong_AsVoidPtr(v[i + 1]);
+    return guarded([&] {
+        ssam_scan_delta_step_args s{};
+        const Tensor& v = delta_inputs(&s, o, o[6], o[7]);
+        if (v.dim() != 3) fail("d_v", "must be [rows, heads, width]");
+        const Tensor& state = tensor(o[5], "d_state");
+        pool(state, at::kFloat, v, {s.heads, s.key_dim, s.value_dim}, &s.slot_stride, &s.slots);
+        s.d_state = static_cast<float*>(state.data_ptr());
+        s.rows = held_to_int(v.size(0), "the number of rows");
+        s.d_slots = slot_of(o[8], v, s.rows, s.slots);
+        const Tensor* given = optional(o[9], "d_out");
+        const Tensor out = result(given, v, s.d_slots);
+        s.out = head_rows(out, "d_out", v, s.heads, s.value_dim, &s.out_head);
+        call(entry.delta_step, s, o[10], "ssam_scan_delta_step");
+        if (given) {
+            Py_INCREF(o[9]);
+            return o[9];
+        }
+        return wrap(out);
+    });
+}
+
+// ---- norm ----------------------------------------------------------------------------------------------------------------
+// d_in; weight, groups, eps.
+template <class Args>
+const Tensor& norm_inputs(Args* a, PyObject* in, PyObject* weight, PyObject* groups, PyObject* eps)
+{
+    const Tensor& x = main_rows(in, "d_in");
+    a->dtype = a->param_dtype = code_of(x.scalar_type(), "d_in");
+    a->channels = held_to_int(x.size(-1), "the number of channels");
+    const long many = PyLong_AsLong(groups);
+    if (PyErr_Occurred()) throw 0;
+    if (many < 1 || many > a->channels || a->channels % many) fail("groups", "must divide the " + std::to_string(a->channels) + " channels");
+    a->groups = (int)many;
+    a->eps = (float)PyFloat_AsDouble(eps);
+    if (PyErr_Occurred()) throw 0;
+    a->sequences = x.dim() == 3 ? held_to_int(x.size(0), "the number of sequences") : 1;
+    a->rows = held_to_int(x.size(-2), "the number of rows");
+    a->in = rows(&x, "d_in", x);
+    if (const Tensor* w = optional(weight, "weight")) {
+        if (w->scalar_type() != x.scalar_type() && w->scalar_type() != at::kFloat) fail("weight", "must be " + type_text(x.scalar_type()) + " or torch.float32");
+        a->param_dtype = code_of(w->scalar_type(), "weight");
+        a->d_weight = dense(w, "weight", x, w->scalar_type(), {a->channels / a->groups});
+    }
+    return x;
+}
+
+// d_residual, d_sum, gate: three objects from v on.
+const Tensor& norm_all(ssam_rms_norm_args* a, PyObject* in, PyObject* weight, PyObject* const* v, PyObject* groups, PyObject* eps)
+{
+    const Tensor& x = norm_inputs(a, in, weight, groups, eps);
+    a->residual = rows(optional(v[0], "d_residual"), "d_residual", x);
+    if (v[1] != Py_None && v[0] == Py_None) fail("d_sum", "belongs to a d_residual");
+    a->sum = rows(optional(v[1], "d_sum"), "d_sum", x);
+    a->gate = rows(optional(v[2], "gate"), "gate", x);
+    return x;
+}
+
+// norm(d_in, weight, d_residual, d_sum, gate, groups, eps, d_out, stream) -> d_out
+PyObject* norm(PyObject*, PyObject* const* v, Py_ssize_t n)
+{
+    if (!arity(n, 9)) return nullptr;
+    return guarded([&] {
+        ssam_rms_norm_args a{};
+        const Tensor& x = norm_all(&a, v[0], v[1], v + 2, v[5], v[6]);
+        const Tensor* given = optional(v[7], "d_out");
+        const Tensor out = result(given, x, false);
+        a.out = rows(&out, "d_out", x);
+        call(entry.norm, a, v[8], "ssam_rms_norm");
+        if (given) {
+            Py_INCREF(v[7]);
+            return v[7];
+        }
+        return wrap(out);
+    });
+}
+
+// norm_e4m3(d_in, weight, d_residual, d_sum, gate, groups, eps, block, d_out, d_scales, stream) -> (values, scales)
+PyObject* norm_e4m3(PyObject*, PyObject* const* v, Py_ssize_t n)
+{
+    if (!arity(n, 11)) return nullptr;
+    return guarded([&] {
+        ssam_rms_norm_args a{};
+        const Tensor& x = norm_all(&a, v[0], v[1], v + 2, v[5], v[6]);
+        const int width = a.channels / a.groups;
+        a.block = width;
+        if (v[7] != Py_None) {
+            const long block = PyLong_AsLong(v[7]);
+            if (PyErr_Occurred()) throw 0;
+            if (block < 1 || block > width || width % block || (block < 16 && block != width))
+                fail("block", "must divide the " + std::to_string(width) + " channels of a group, and be 16 at least or all of them");
+            a.block = (int)block;
+        }
+        const Tensor *given = optional(v[8], "d_out"), *given_scales = optional(v[9], "d_scales");
+        const Tensor out = given ? *given : at::empty(x.sizes(), x.options().dtype(at::kFloat8_e4m3fn));
+        if (out.sizes() != x.sizes()) fail("d_out", "must have shape " + shape_text(x.sizes()) + ", not " + shape_text(out.sizes()));
+        same_kind(out, "d_out", at::kFloat8_e4m3fn, x);
+        const auto s = out.strides();
+        if (s.back() != 1 && out.sizes().back() != 1) fail("d_out", "must have contiguous channels (stride 1)");
+        a.out = s.size() == 2 ? ssam_rows{out.data_ptr(), 0, s[0]} : ssam_rows{out.data_ptr(), s[0], s[1]};
+        std::vector<int64_t> shape(x.sizes().begin(), x.sizes().end());
+        shape.back() = a.channels / a.block;
+        const Tensor scales = given_scales ? *given_scales : at::empty(shape, x.options().dtype(at::kFloat));
+        a.d_scales = dense<float>(&scales, "d_scales", x, at::kFloat, shape);
+        call(entry.norm_e4m3, a, v[10], "ssam_rms_norm_e4m3");
+        return Py_BuildValue("(NN)", wrap(out), wrap(scales));
+    });
+}
+
+// norm_backward(d_grad, d_in, weight, d_grad_sum, gate, groups, eps, d_work, stream) -> (x, weight, gate)
+PyObject* norm_backward(PyObject*, PyObject* const* v, Py_ssize_t n)
+{
+    if (!arity(n, 9)) return nullptr;
+    return guarded([&] {
+        ssam_rms_norm_backward_args a{};
+        const Tensor& x = norm_inputs(&a, v[1], v[2], v[5], v[6]);
+        a.grad_out = rows(&tensor(v[0], "d_grad"), "d_grad", x);
+        a.grad_sum = rows(optional(v[3], "d_grad_sum"), "d_grad_sum", x);
+        a.gate = rows(optional(v[4], "gate"), "gate", x);
+        const Tensor gx = result(nullptr, x, false), gz = v[4] != Py_None ? result(nullptr, x, false) : Tensor();
+        const Tensor gw = v[2] != Py_None ? at::empty({a.channels / a.groups}, tensor(v[2], "weight").options()) : Tensor();
+        a.grad_in = rows(&gx, "x", x);
+        if (gz.defined()) a.grad_gate = rows(&gz, "gate", x);
+        if (gw.defined()) a.d_grad_weight = gw.data_ptr();
+        const Tensor work = workspace(entry.norm_backward_bytes(&a), optional(v[7], "d_work"), x);
+        if (work.defined()) {
+            a.d_work = work.data_ptr();
+            a.work_bytes = work.nbytes();
+        }
+        call(entry.norm_backward, a, v[8], "ssam_rms_norm_backward");
+        return Py_BuildValue("(NNN)", wrap(gx), wrap(gw), wrap(gz));
+    });
+}
+
+// bind(exception class, addresses of the entry points in the order of `entry`)
+PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n)
+{
+    constexpr int kCount = sizeof(entry) / sizeof(void*);
+    static_assert(sizeof(void*) == sizeof(entry.conv1d));
+    if (!arity(n, 1 + kCount)) return nullptr;
+    void* p[kCount];
+    for (int i = 0; i < kCount; ++i) p[i] = PyLong_AsVoidPtr(v[i + 1]);
     if (PyErr_Occurred()) return nullptr;
     Py_INCREF(v[0]);
     Py_XDECREF(status_error);
     status_error = v[0];
-    entry.conv1d = (decltype(entry.conv1d))p[0];
-    entry.conv1d_backward = (decltype(entry.conv1d_backward))p[1];
-    entry.conv1d_backward_bytes = (decltype(entry.conv1d_backward_bytes))p[2];
-    entry.conv1d_step = (decltype(entry.conv1d_step))p[3];
-    entry.scan = (decltype(entry.scan))p[4];
-    entry.scan_bytes = (decltype(entry.scan_bytes))p[5];
-    entry.scan_marks = (decltype(entry.scan_marks))p[6];
-    entry.scan_backward = (decltype(entry.scan_backward))p[7];
-    entry.scan_backward_bytes = (decltype(entry.scan_backward_bytes))p[8];
-    entry.scan_step = (decltype(entry.scan_step))p[9];
+    std::memcpy(&entry, p, sizeof(entry));       // nothing but pointers
     Py_RETURN_NONE;
 }
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(bind), FAST(conv1d), FAST(conv1d_backward), FAST(conv1d_step), FAST(scan), FAST(scan_bytes), FAST(scan_marks),
-                         FAST(scan_backward), FAST(scan_step), {nullptr, nullptr, 0, nullptr}};
+                         FAST(scan_backward), FAST(scan_step), FAST(delta), FAST(delta_bytes), FAST(delta_marks), FAST(delta_step), FAST(norm),
+                         FAST(norm_e4m3), FAST(norm_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_sequence", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

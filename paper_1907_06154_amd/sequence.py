@@ -1,5 +1,5 @@
-"""Binding of the sequence operators (include/ssam_sequence.h): per-channel filters and selective scans along time,
-their gradients and their single-row forms.  The extension module _sequence checks and marshals the arguments; there is no
+"""Binding of the sequence operators (include/ssam_sequence.h): per-channel filters and selective scans along time, scans with a
+matrix per head for a state, their gradients and their single-row forms, and the norm around them.  The extension module _sequence checks and marshals the arguments; there is no
 fallback, as in binding.py.
 
 Tensors of rows are [rows, channels] (one sequence, or several packed one behind the other: `starts`, a device tensor of
@@ -20,10 +20,13 @@ from . import binding
 
 MARK_ROWS = 16
 MAX_TAPS, MAX_STATES = 8, 64
+DELTA_ROWS, MAX_KEY = 64, 256
 
 EXPORTS = ["ssam_conv1d", "ssam_conv1d_backward", "ssam_conv1d_backward_workspace_bytes", "ssam_conv1d_step", "ssam_scan_selective",
            "ssam_scan_selective_workspace_bytes", "ssam_scan_selective_marks", "ssam_scan_selective_backward",
-           "ssam_scan_selective_backward_workspace_bytes", "ssam_scan_selective_step"]
+           "ssam_scan_selective_backward_workspace_bytes", "ssam_scan_selective_step", "ssam_scan_delta", "ssam_scan_delta_workspace_bytes",
+           "ssam_scan_delta_marks", "ssam_scan_delta_step", "ssam_rms_norm", "ssam_rms_norm_e4m3", "ssam_rms_norm_backward",
+           "ssam_rms_norm_backward_workspace_bytes"]
 
 _torch = None
 _fast = None          # the extension module, bound to the library's entry points
@@ -48,6 +51,17 @@ class ScanSelectiveGrads(NamedTuple):
     gate: Optional[object]
     dt_bias: Optional[object]
     state: Optional[object]
+
+
+class RmsNormQuantized(NamedTuple):
+    values: object
+    scales: object
+
+
+class RmsNormGrads(NamedTuple):
+    x: object
+    weight: Optional[object]
+    gate: Optional[object]
 
 
 def _load():
@@ -148,3 +162,55 @@ def ssam_scan_selective_step(d_in, d_dt, a, b, c, d_state, skip=None, gate=None,
     """ssam_scan_selective for one more row of each of d_in's [rows, channels] sequences; d_state [pool, channels, states], float32,
     is updated in place, slots as in ssam_conv1d_step."""
     return _run("scan_step", d_in, stream, (d_in, d_dt, a, b, c, skip, gate, dt_bias, softplus, d_state, slots, d_out))
+
+
+def ssam_scan_delta_marks(d_k, d_v, starts=None, lengths=None):
+    """A tensor for ssam_scan_delta's d_marks: the state before every 64 rows and what the rows correct it by, for
+    ssam_scan_delta_backward; made on the current stream."""
+    if _fast is None:
+        _load()
+    return _fast.delta_marks(d_k, d_v, starts, lengths)
+
+
+def ssam_scan_delta_workspace_bytes(d_k, d_v, starts=None, lengths=None) -> int:
+    """Bytes of d_work that ssam_scan_delta needs for such inputs."""
+    if _fast is None:
+        _load()
+    return _fast.delta_bytes(d_k, d_v, starts, lengths)
+
+
+def ssam_scan_delta(d_q, d_k, d_v, g, beta, scale=None, unit: bool = False, d_state=None, d_final=None, d_marks=None, starts=None, lengths=None,
+                    d_out=None, d_work=None, stream=None):
+    """Gated delta rule, per head with a matrix S [key, value]:  S' = exp(g_t) S,  u = beta_t (v_t - S'^T k_t),  S = S' + k_t u^T,
+    out_t = scale S^T q_t.  d_q, d_k: rows of [key heads, key width] (at most 256), d_v and the result: of [heads, value width], head h using key head
+    h // (heads // key heads); g (None: no decay), beta: float32 rows of heads.  unit: rows of q and k are divided by sqrt(their squares' sum
+    + 1e-6).  scale: 1 / sqrt(key width) if None.  d_state, d_final [sequences, heads, key, value], float32; d_final may be d_state.
+    d_marks (from ssam_scan_delta_marks) keeps what the gradients need."""
+    return _run("delta", d_v, stream, (d_q, d_k, d_v, g, beta, scale, unit, d_state, d_final, d_marks, starts, lengths, d_out, d_work))
+
+
+def ssam_scan_delta_step(d_q, d_k, d_v, g, beta, d_state, scale=None, unit: bool = False, slots=None, d_out=None, stream=None):
+    """ssam_scan_delta for one more row of each of d_v's [rows, heads, value] sequences; d_state [pool, heads, key, value], float32, is
+    updated in place, slots as in ssam_conv1d_step."""
+    return _run("delta_step", d_v, stream, (d_q, d_k, d_v, g, beta, d_state, scale, unit, slots, d_out))
+
+
+def ssam_rms_norm(d_in, weight=None, d_residual=None, d_sum=None, gate=None, groups: int = 1, eps: float = 1e-6, d_out=None, stream=None):
+    """s = d_in + d_residual, rounded to their type (d_in alone without);  out = s / sqrt(mean(s^2) + eps) * weight * silu(gate), the mean over each of
+    `groups` equal parts of a row (heads, say).  weight [channels / groups], d_in's type or float32 (None: ones); gate (None: absent): rows as
+    d_in's.  d_sum receives s and may be d_residual itself; the gradients start from it."""
+    return _run("norm", d_in, stream, (d_in, weight, d_residual, d_sum, gate, groups, eps, d_out))
+
+
+def ssam_rms_norm_e4m3(d_in, weight=None, d_residual=None, d_sum=None, gate=None, groups: int = 1, eps: float = 1e-6, block: Optional[int] = None,
+                       d_out=None, d_scales=None, stream=None) -> RmsNormQuantized:
+    """ssam_rms_norm with its result as torch.float8_e4m3fn and a float32 scale for every `block` channels (None: a group's), the largest
+    magnitude among them / 448; [.., channels / block] scales."""
+    return RmsNormQuantized(*_run("norm_e4m3", d_in, stream, (d_in, weight, d_residual, d_sum, gate, groups, eps, block, d_out, d_scales)))
+
+
+def ssam_rms_norm_backward(d_grad, d_in, weight=None, d_grad_sum=None, gate=None, groups: int = 1, eps: float = 1e-6, d_work=None,
+                           stream=None) -> RmsNormGrads:
+    """Gradients of ssam_rms_norm for d_grad, the gradient of its result, and d_grad_sum, that of its sum (none if absent).  d_in is what was
+    normalised: the sum, where there was a residual, whose gradient is x's too."""
+    return RmsNormGrads(*_run("norm_backward", d_in, stream, (d_grad, d_in, weight, d_grad_sum, gate, groups, eps, d_work)))

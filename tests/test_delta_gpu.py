@@ -1,0 +1,208 @@
+"""The scan with a matrix per head for a state, its gradients and its single-row form, against their definitions in 64 bits."""
+import numpy as np
+import pytest
+
+import delta_reference as ref
+import sequence_reference as seqref
+from test_sequence_gpu import LAYOUTS, NAME, SENTINEL, TYPES, f64, layout, randn  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+import paper_1907_06154_amd as ssam  # noqa: E402
+
+
+def near(what, got, want, noise, dtype, size=None):
+    """Each column (last axis) is `noise` of its size off, as a root mean square, besides the rounding of its type; a single value eight times
+    as much, which one in 10^14 values passes by chance."""
+    got = f64(got).reshape(want.shape)
+    assert np.isfinite(got).all(), f"{what}: not finite"
+    if not got.size:
+        return
+    size = np.abs(want) if size is None else size
+    axes = tuple(range(want.ndim - 1))
+    rms = np.sqrt((size * size).mean(axes, keepdims=True))
+    big = np.abs(size).max(axes, keepdims=True)
+    half = seqref.HALF_STEP[dtype] * np.abs(want) + seqref.TINY[dtype]
+    off = np.maximum(np.abs(got - want) - half, 0)
+    worst = np.sqrt((off * off).mean(axes, keepdims=True))
+    assert (worst <= noise * np.maximum(rms, 1e-30)).all(), (what, (worst / np.maximum(rms, 1e-30)).max(), noise)
+    assert (off <= 8 * noise * np.maximum(big, 1e-30)).all(), (what, (off / np.maximum(big, 1e-30)).max(), noise)
+
+
+def make(lead, dtype, Hk, H, K, V, unit, form, seed, gate=True):
+    """Column ranges of one buffer (dense: of their own); keys of unit length at most, rates from almost none to a few rows."""
+    g = torch.Generator().manual_seed(seed)
+    t = TYPES[dtype]
+    odd = 0 if form == "dense" else 3
+    both = torch.randn(*lead, 2 * Hk * K + H * V + odd, generator=g)
+    both = both * torch.sigmoid(both)
+    if not unit:
+        keys = both[..., odd:odd + 2 * Hk * K].view(*lead, 2 * Hk, K) if form == "dense" else both[..., odd:odd + 2 * Hk * K].unflatten(-1, (2 * Hk, K))
+        both[..., odd:odd + 2 * Hk * K] = (keys / keys.square().sum(-1, keepdim=True).add(1e-6).sqrt()).flatten(-2) * 0.999
+    both = both.to(t).cuda()[..., odd:]
+    own = (lambda x: x.contiguous()) if form == "dense" else (lambda x: x)
+    v = {"q": own(both[..., :Hk * K].unflatten(-1, (Hk, K))), "k": own(both[..., Hk * K:2 * Hk * K].unflatten(-1, (Hk, K))),
+         "v": own(both[..., 2 * Hk * K:].unflatten(-1, (H, V)))}
+    v["beta"] = torch.sigmoid(torch.randn(*lead, H, generator=g)).cuda()
+    v["g"] = (-torch.rand(H, generator=g) * 2 * torch.rand(*lead, H, generator=g) ** 4).cuda() if gate else None
+    return v
+
+
+def row(v, name, lead, many, unit):
+    """In 64 bits, [rows, heads, ..]: q and k for every head, as the rule takes them."""
+    x = f64(v[name])
+    x = x.reshape(int(np.prod(lead)), *x.shape[len(lead):])
+    if name in "qk":
+        x = np.repeat(ref.unit(x) if unit else x, many, 1)
+    return x
+
+
+def spans_of(name):
+    lead, dev, spans = layout(name)
+    return lead, dev, spans
+
+
+DELTA = [(lay, dt, Hk, H, K, V, unit, state, form)
+         for lay, dt, Hk, H, K, V, unit, state, form in [
+             ("one", "float32", 1, 1, 128, 128, True, True, "dense"), ("one", "bfloat16", 2, 4, 128, 128, True, True, "wide"),
+             ("single_row", "bfloat16", 1, 2, 64, 64, True, True, "dense"), ("single_row", "float32", 2, 2, 1, 1, False, False, "dense"),
+             ("batch", "float16", 1, 3, 96, 80, True, False, "wide"), ("batch", "float32", 2, 2, 41, 50, False, True, "wide"),
+             ("padded", "bfloat16", 2, 2, 32, 17, True, True, "dense"), ("padded", "float32", 1, 2, 64, 130, True, True, "wide"),
+             ("packed", "bfloat16", 2, 6, 128, 100, True, True, "wide"), ("packed", "float16", 1, 1, 33, 16, True, True, "dense"),
+             ("long", "float32", 1, 2, 64, 64, True, True, "dense"), ("long", "bfloat16", 1, 1, 256, 64, True, True, "dense"),
+             ("long", "float32", 1, 1, 200, 40, True, True, "wide"), ("packed_long", "float16", 2, 2, 16, 33, False, False, "wide"),
+             ("packed_long", "bfloat16", 1, 2, 130, 260, True, True, "wide"), ("crowd", "bfloat16", 1, 2, 24, 20, True, True, "dense"),
+             ("swarm", "float32", 1, 1, 8, 5, True, True, "dense"), ("pieces", "bfloat16", 1, 1, 64, 16, True, True, "dense")]]
+
+
+def case(lay, dt, Hk, H, K, V, unit, state, form, seed=1, gate=True):
+    lead, dev, spans = spans_of(lay)
+    v = make(lead, dt, Hk, H, K, V, unit, form, seed, gate)
+    S = lead[0] if len(lead) == 2 else len(spans)
+    h0 = randn(torch.Generator().manual_seed(seed + 5), S, H, K, V, scale=0.3) if state else None
+    flat = {n: row(v, n, lead, H // Hk, unit) for n in ("q", "k", "v", "beta")}
+    flat["g"] = row(v, "g", lead, 1, unit) if gate else np.zeros_like(flat["beta"])
+    return lead, dev, spans, v, h0, flat, S
+
+
+@pytest.mark.parametrize("lay,dt,Hk,H,K,V,unit,state,form", DELTA)
+def test_delta(lay, dt, Hk, H, K, V, unit, state, form):
+    lead, dev, spans, v, h0, flat, S = case(lay, dt, Hk, H, K, V, unit, state, form)
+    out = torch.full((*lead, H, V), SENTINEL, dtype=TYPES[dt], device="cuda")
+    final = torch.full((S, H, K, V), SENTINEL, device="cuda")
+    got = ssam.ssam_scan_delta(v["q"], v["k"], v["v"], v["g"], v["beta"], unit=unit, d_state=h0, d_final=final, d_out=out, **dev)
+    assert got is out
+    seen, rows = np.zeros(int(np.prod(lead)), bool), f64(out).reshape(-1, H, V)
+    wants, gots, lasts = [], [], []
+    longest = 1
+    for s, first, n in spans:
+        want, last, _ = ref.delta(*(flat[k][first:first + n] for k in ("q", "k", "v", "g", "beta")), K ** -0.5,
+                                  np.zeros((H, K, V)) if h0 is None else f64(h0[s]))
+        seen[first:first + n] = True
+        longest = max(longest, n)
+        wants.append(want)
+        gots.append(rows[first:first + n])
+        lasts.append(last)
+    noise = ref.delta_noise(longest)
+    if sum(map(len, wants)):
+        want = np.concatenate(wants).reshape(-1, H * V)
+        near("out", torch.from_numpy(np.concatenate(gots).reshape(-1, H * V)), want, noise, dt)
+    assert (rows[~seen] == SENTINEL).all()
+    last = np.stack(lasts).transpose(0, 2, 1, 3).reshape(-1, H * V)
+    near("final", torch.from_numpy(f64(final).transpose(0, 2, 1, 3).reshape(-1, H * V)), last, noise, "float32")
+    # allocated results hold zeros in rows of no sequence; the state in place; the same bits
+    if h0 is not None:
+        again = h0.clone()
+        out2 = ssam.ssam_scan_delta(v["q"], v["k"], v["v"], v["g"], v["beta"], unit=unit, d_state=again, d_final=again, **dev)
+        assert torch.equal(again, final)
+        assert torch.equal(out2.reshape(-1, H, V)[torch.from_numpy(seen).cuda()], out.reshape(-1, H, V)[torch.from_numpy(seen).cuda()])
+        assert (out2.reshape(-1, H, V)[torch.from_numpy(~seen).cuda()] == 0).all()
+
+
+@pytest.mark.parametrize("dt", TYPES)
+def test_delta_without_decay_and_with_a_scale(dt):
+    lead, dev, spans, v, h0, flat, S = case("batch", dt, 1, 2, 64, 48, True, True, "dense", gate=False)
+    got = ssam.ssam_scan_delta(v["q"], v["k"], v["v"], None, v["beta"], scale=0.7, unit=True, d_state=h0)
+    for s, first, n in spans:
+        want, _, _ = ref.delta(*(flat[k][first:first + n] for k in ("q", "k", "v", "g", "beta")), 0.7, f64(h0[s]))
+        near("out", got[s].reshape(n, -1), want.reshape(n, -1), ref.delta_noise(n), dt)
+
+
+def test_delta_forgets_all_at_a_row_and_keeps_the_digits_of_the_others():
+    """A decay of exp(-inf) or exp(-900) in a row: the rows on both sides are as exact as without it."""
+    for value in (-float("inf"), -900.0, -50.0):
+        lead, dev, spans, v, h0, flat, S = case("long", "float32", 1, 1, 64, 64, True, True, "dense")
+        v["g"][70], v["g"][71], v["g"][200] = value, value, value
+        flat["g"] = np.maximum(row(v, "g", lead, 1, True), -1000.0)
+        got = ssam.ssam_scan_delta(v["q"], v["k"], v["v"], v["g"], v["beta"], unit=True, d_state=h0)
+        want, _, _ = ref.delta(*(flat[k] for k in ("q", "k", "v", "g", "beta")), 64 ** -0.5, f64(h0[0]))
+        near("out", got.reshape(300, -1), want.reshape(300, -1), ref.delta_noise(300), "float32")
+
+
+@pytest.mark.parametrize("size", [1e-12, 1e12, 2.0 ** 60])
+def test_delta_at_any_magnitude(size):
+    """Values, states and queries of any size: the fp16 operands are scaled.  (bf16 and fp32; keys at unit length.)"""
+    for dt in ("float32", "bfloat16"):
+        lead, dev, spans, v, h0, flat, S = case("batch", dt, 1, 2, 32, 48, True, True, "dense")
+        v["v"] = (v["v"].float() * size).to(TYPES[dt])
+        got = ssam.ssam_scan_delta(v["q"], v["k"], v["v"], v["g"], v["beta"], unit=True, d_state=h0 * size)
+        flat["v"] = row(v, "v", lead, 1, True)
+        for s, first, n in spans:
+            want, _, _ = ref.delta(*(flat[k][first:first + n] for k in ("q", "k", "v", "g", "beta")), 32 ** -0.5, f64(h0[s]) * size)
+            near("out", got[s].reshape(n, -1), want.reshape(n, -1), ref.delta_noise(n), dt)
+
+
+STEP = [(rows, pool, dt, Hk, H, K, V, unit) for rows, pool, dt, Hk, H, K, V, unit in [
+    (1, 1, "bfloat16", 2, 4, 128, 128, True), (5, 9, "float32", 1, 3, 41, 50, False), (7, 8, "float16", 2, 2, 96, 80, True), (3, 3, "float32", 1, 1, 1, 1, True),
+    (4, 6, "bfloat16", 1, 2, 256, 200, True), (600, 700, "bfloat16", 1, 2, 64, 64, True), (600, 601, "float32", 1, 2, 33, 130, True),
+    (300, 301, "float16", 2, 4, 250, 40, True), (1100, 1100, "float32", 1, 1, 20, 36, True)]]
+
+
+@pytest.mark.parametrize("rows,pool,dt,Hk,H,K,V,unit", STEP)
+@pytest.mark.parametrize("form", ["dense", "wide"])
+def test_delta_step(rows, pool, dt, Hk, H, K, V, unit, form):
+    v = make((rows,), dt, Hk, H, K, V, unit, form, 3)
+    g = torch.Generator().manual_seed(4)
+    whole = randn(g, pool, H * K * V + 7)
+    state = whole[:, :H * K * V].unflatten(-1, (H, K, V)) if form == "wide" else randn(g, pool, H, K, V)
+    before = f64(state)
+    slots = torch.randperm(pool, generator=g)[:rows].to(torch.int32)
+    if rows > 2:                      # a row without a slot, one behind the pool, and a slot that gets three rows in order
+        slots[1], slots[rows - 1] = -1, pool
+    if rows > 5:
+        slots[2] = slots[4] = slots[0]
+    out = torch.full((rows, H, V), SENTINEL, dtype=TYPES[dt], device="cuda")
+    got = ssam.ssam_scan_delta_step(v["q"], v["k"], v["v"], v["g"], v["beta"], state, unit=unit, slots=slots.cuda(), d_out=out)
+    assert got is out
+    want_out, want_state, size = np.full((rows, H, V), SENTINEL), before.copy(), np.full((rows, H, V), SENTINEL)
+    flat = {n: row(v, n, (rows,), H // Hk, unit) for n in ("q", "k", "v", "beta")}
+    flat["g"] = row(v, "g", (rows,), 1, unit)
+    for r in range(rows):
+        s = int(slots[r])
+        if 0 <= s < pool:
+            o, h, _ = ref.delta(*(flat[k][r:r + 1] for k in ("q", "k", "v", "g", "beta")), K ** -0.5, want_state[s])
+            want_out[r], want_state[s] = o[0], h
+            size[r] = K ** -0.5 * np.sqrt((flat["q"][r] ** 2).sum(-1))[:, None] * np.sqrt((h * h).sum(1))
+    # fp32 all through: sums of at most 256 products, a dozen roundings, relative to the lengths of what is multiplied: a state's columns
+    columns = lambda a: np.asarray(a).transpose(0, 2, 1, 3).reshape(pool * K, H * V)  # noqa: E731
+    near("out", got.reshape(rows, -1), want_out.reshape(rows, -1), 2.0 ** -18, dt, size.reshape(rows, -1))
+    near("state", torch.from_numpy(columns(f64(state))), columns(want_state), 2.0 ** -18, "float32")
+    untouched = np.setdiff1d(np.arange(pool), slots.numpy())
+    assert np.array_equal(f64(state)[untouched], before[untouched])
+    if form == "wide":
+        assert torch.equal(whole[:, H * K * V:].cpu(), torch.randn(pool, H * K * V + 7, generator=torch.Generator().manual_seed(4))[:, H * K * V:])
+
+
+def test_delta_step_goes_on_where_the_scan_ends():
+    lead, dev, spans, v, h0, flat, S = case("batch", "bfloat16", 2, 4, 64, 64, True, True, "wide")
+    whole = ssam.ssam_scan_delta(v["q"], v["k"], v["v"], v["g"], v["beta"], unit=True, d_state=h0)
+    state = torch.empty_like(h0)
+    at = lambda lo, hi: [v[n][:, lo:hi] for n in ("q", "k", "v", "g", "beta")]  # noqa: E731
+    first = ssam.ssam_scan_delta(*at(0, 15), unit=True, d_state=h0, d_final=state)
+    rest = []
+    for t in range(15, lead[1]):
+        rest.append(ssam.ssam_scan_delta_step(*(v[n][:, t] for n in ("q", "k", "v", "g", "beta")), state, unit=True))
+    got = torch.cat([first, torch.stack(rest, 1)], 1)
+    near("out", got.reshape(-1, 4 * 64), f64(whole).reshape(-1, 4 * 64), 2 * ref.delta_noise(lead[1]) + 2.0 ** -8, "bfloat16")
