@@ -193,6 +193,25 @@ int ssam_scan_delta(const ssam_scan_delta_args *args, void *hip_stream);
 size_t ssam_scan_delta_workspace_bytes(const ssam_scan_delta_args *args);
 long long ssam_scan_delta_marks(const ssam_scan_delta_args *args);   /* host only; 0 for invalid arguments */
 
+/* Gradients of ssam_scan_delta, from the same inputs and its marks.  grad_out: gradient of its result; d_grad_final (may be
+ * NULL): of its d_final.  grad_q, grad_k, grad_v are in dtype, a row's elements contiguous, grad_g and grad_beta rows of `heads`
+ * floats; each may be absent (NULL).  d_grad_state is the gradient of d_state, or of the zeros that stand for it.
+ * d_work: ssam_scan_delta_backward_workspace_bytes(args) bytes, 16-byte aligned. */
+typedef struct {
+    int dtype, heads, key_heads, key_dim, value_dim, unit;
+    float scale;
+    ssam_sequences seq;
+    ssam_rows q, k, v, grad_out, g, beta;
+    long long q_head, k_head, v_head, grad_out_head;
+    const float *d_marks, *d_grad_final;
+    ssam_rows grad_q, grad_k, grad_v, grad_g, grad_beta;
+    float *d_grad_state;
+    void *d_work;
+    size_t work_bytes;
+} ssam_scan_delta_backward_args;
+int ssam_scan_delta_backward(const ssam_scan_delta_backward_args *args, void *hip_stream);
+size_t ssam_scan_delta_backward_workspace_bytes(const ssam_scan_delta_backward_args *args);
+
 /* ssam_scan_delta for one more row of each of `rows` sequences; slots as in ssam_conv1d_step, slot i at
  * d_state + i * slot_stride floats, [heads][key_dim][value_dim] contiguous, updated in place. */
 typedef struct {

@@ -8,8 +8,8 @@ loads nothing; the shared library is opened on the first call and a missing libr
 from .binding import (SsamError, lib, ssam_conv2d, ssam_conv3d, ssam_describe, ssam_probe_copy, ssam_probe_latency, ssam_scan, ssam_scan_static, ssam_scan_workspace_bytes,
                       ssam_set_tuning, ssam_stencil2d,
                       ssam_stencil3d, ssam_stencil_iterate, status_string)
-from .sequence import (Conv1dGrads, RmsNormGrads, RmsNormQuantized, ScanSelectiveGrads, ssam_conv1d, ssam_conv1d_backward, ssam_conv1d_step,
-                       ssam_rms_norm, ssam_rms_norm_backward, ssam_rms_norm_e4m3, ssam_scan_delta, ssam_scan_delta_marks, ssam_scan_delta_step,
+from .sequence import (Conv1dGrads, RmsNormGrads, RmsNormQuantized, ScanDeltaGrads, ScanSelectiveGrads, ssam_conv1d, ssam_conv1d_backward, ssam_conv1d_step,
+                       ssam_rms_norm, ssam_rms_norm_backward, ssam_rms_norm_e4m3, ssam_scan_delta, ssam_scan_delta_backward, ssam_scan_delta_marks, ssam_scan_delta_step,
                        ssam_scan_delta_workspace_bytes, ssam_scan_selective, ssam_scan_selective_backward, ssam_scan_selective_marks,
                        ssam_scan_selective_step, ssam_scan_selective_workspace_bytes)
 
@@ -17,5 +17,5 @@ __all__ = ["SsamError", "lib", "ssam_conv2d", "ssam_conv3d", "ssam_stencil2d", "
            "ssam_set_tuning", "ssam_describe", "ssam_probe_copy", "ssam_probe_latency", "ssam_scan", "ssam_scan_static", "ssam_scan_workspace_bytes",
            "status_string", "Conv1dGrads", "ScanSelectiveGrads", "ssam_conv1d", "ssam_conv1d_backward", "ssam_conv1d_step",
            "ssam_scan_selective", "ssam_scan_selective_backward", "ssam_scan_selective_marks", "ssam_scan_selective_step",
-           "ssam_scan_selective_workspace_bytes", "ssam_scan_delta", "ssam_scan_delta_marks", "ssam_scan_delta_step",
+           "ssam_scan_selective_workspace_bytes", "ScanDeltaGrads", "ssam_scan_delta", "ssam_scan_delta_backward", "ssam_scan_delta_marks", "ssam_scan_delta_step",
            "ssam_scan_delta_workspace_bytes", "RmsNormGrads", "RmsNormQuantized", "ssam_rms_norm", "ssam_rms_norm_backward", "ssam_rms_norm_e4m3"]

@@ -72,16 +72,7 @@ __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
         float back_s[NT];
         {
             HalfPair f[KT][NT];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                float m = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 2 * KT; ++j) m = larger(m, s[j][n]);
-                const Scale by(over_column(m));
-                back_s[n] = by.back;
-#pragma unroll
-                for (int k = 0; k < KT; ++k) f[k][n] = split(s[2 * k][n], s[2 * k + 1][n], by.to);
-            }
+            split_state<KT, NT>(s, f, back_s);
 #pragma unroll
             for (int m = 0; m < 4; ++m) {
                 Float4 a[NT];
@@ -107,13 +98,7 @@ __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
         // R = (I + A diag(b))^-1 X;  x becomes U = b R
         float back_u[NT];
         HalfPair f[2][NT];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const Scale by(over_column(larger(larger(larger(larger(0.0f, x[0][n]), x[1][n]), x[2][n]), x[3][n])));
-            back_u[n] = by.back * room.m.f.solve_back;
-            f[0][n] = split(x[0][n], x[1][n], by.to);
-            f[1][n] = split(x[2][n], x[3][n], by.to);
-        }
+        split_rows<NT>(x, f, back_u);
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
             lower_product<NT>(room.m.solve, m, lane, f, x[m]);
@@ -121,7 +106,7 @@ __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
             const Float4 beta = *reinterpret_cast<const Float4*>(&room.m.f.beta[t0]);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                x[m][n] *= back_u[n];
+                x[m][n] *= back_u[n] * room.m.f.solve_back;
                 if (mark && c0 + 16 * n < p.value_dim)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) mark[(long long)(p.key_dim + t0 + i) * p.value_dim + 16 * n] = x[m][n][i];
@@ -129,13 +114,7 @@ __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
             }
         }
         // O = scale (exp(G) Q S + (Q K^T o D) U)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const Scale by(over_column(larger(larger(larger(larger(0.0f, x[0][n]), x[1][n]), x[2][n]), x[3][n])));
-            back_u[n] = by.back * room.m.f.mix_back;
-            f[0][n] = split(x[0][n], x[1][n], by.to);
-            f[1][n] = split(x[2][n], x[3][n], by.to);
-        }
+        split_rows<NT>(x, f, back_u);
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
             Float4 a[NT];
@@ -148,18 +127,12 @@ __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (t0 + i < rows && c0 + 16 * n < p.value_dim)
-                        os[(long long)(row0 + t0 + i) * p.out.row + 16 * n] = (T)__builtin_fmaf(a[n][i], back_u[n], asks[i] * (o[m][n][i] * back_s[n]));
+                        os[(long long)(row0 + t0 + i) * p.out.row + 16 * n] = (T)__builtin_fmaf(a[n][i], back_u[n] * room.m.f.mix_back, asks[i] * (o[m][n][i] * back_s[n]));
                 x[m][n] *= writes;
             }
         }
         // S = exp(G_C) S + (exp(G_C - G) K)^T U
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const Scale by(over_column(larger(larger(larger(larger(0.0f, x[0][n]), x[1][n]), x[2][n]), x[3][n])));
-            back_u[n] = by.back;
-            f[0][n] = split(x[0][n], x[1][n], by.to);
-            f[1][n] = split(x[2][n], x[3][n], by.to);
-        }
+        split_rows<NT>(x, f, back_u);
         const float total = room.m.f.total;
 #pragma unroll
         for (int j = 0; j < 2 * KT; ++j) {

@@ -1,0 +1,723 @@
+// Gradients of the scan with matrix states (ssam_scan_delta_backward).  In a block of 64 rows, with the notation of ssam_scan_delta.h, P = scale
+// (Q K^T o D), T = (I + diag(b) A)^-1, dO the gradient of O and dS1 that of the state behind the block:
+//     dU = P^T dO + (exp(G_C - G) K) dS1,   dY = T^T dU,   dV = dX = b dY,
+//     dS0 = exp(G_C) dS1 + scale (exp(G) Q)^T dO - (exp(G) K)^T dX                                      (delta_back_walk, block after block)
+//     dbeta = rows of dY . R,   dP = scale (dO U^T) o D,   dA = -(dX U^T) o D, strictly lower,
+//     dQ = scale exp(G) (dO S0^T) + dP K,   reads = dA K - exp(G) (dX S0^T),
+//     last = exp(G_C - G) (U dS1^T),        writes = dP^T Q + dA^T K + last,   dK = reads + writes    (delta_back_rows, all blocks at once)
+// The decay of row t lies between every write j < t and every read i >= t, so dg_t is the sum over these pairs of dP P + dA A (their parts before
+// the keys' products), of what the rows i >= t have from S0, of the k.last of the rows j < t, and of exp(G_C) <S0, dS1>: no differences.
+#include "ssam_scan_delta_tiles.h"
+
+namespace ssam {
+namespace {
+
+struct DeltaBackParams {
+    DeltaParams f;               // final and out unused; marks: what the forward call left; state: the gradient of the last state
+    ssam_rows grad_out, grad_q, grad_k, grad_v, grad_g, grad_beta;
+    long long grad_out_head, grad_v_head, grad_key_head;
+    float* grad_state;
+    float* behind;               // as marks: dS1 and dY of every block and head
+};
+
+template <class T, int KT>
+__global__ __launch_bounds__(kBlock) void delta_back_prepare(DeltaParams p)
+{
+    __shared__ PrepareRoom<T, KT> room;
+    const int slot = (int)(blockIdx.x / p.key_heads), key_head = (int)(blockIdx.x % p.key_heads);
+    const Piece piece = find_piece(p.pieces, slot);
+    if (piece.seq < 0 || piece.n <= 0) return;
+    prepare_block<T, KT, true>(p, piece, slot, key_head, room);
+}
+
+// One wave: 16 NT columns of the gradient of a head's state, from the last block to the first.
+template <class T, int KT, int NT>
+__global__ __launch_bounds__(kBlock) void delta_back_walk(DeltaBackParams b)
+{
+    const DeltaParams& p = b.f;
+    __shared__ WalkRoom<T, KT> room;
+    constexpr bool kOnePlace = WalkRoom<T, KT>::kOnePlace;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, g = lane >> 4, r16 = lane & 15;
+    const int tile = (int)(blockIdx.x % p.tiles), head = (int)(blockIdx.x / p.tiles % p.heads), seq = (int)(blockIdx.x / p.tiles / p.heads);
+    const int key_head = head / (p.heads / p.key_heads);
+    int first, len;
+    span_of(p.pieces, seq, first, len);
+    const int blocks = (len + kDeltaRows - 1) / kDeltaRows;
+    const long long slot0 = p.pieces.begin ? first_slot(p.pieces, seq) : (long long)seq * p.pieces.per;
+    const int c0 = (tile * kWavesPerBlock + wave) * 16 * NT + r16;
+    const Piece whole{seq, first, len, 0, len};
+    const T* const qs = sequence_base<const T>(p.q, p.pieces, whole) + key_head * p.q_head;
+    const T* const ks = sequence_base<const T>(p.k, p.pieces, whole) + key_head * p.k_head;
+    const T* const dos = sequence_base<const T>(b.grad_out, p.pieces, whole) + head * b.grad_out_head + c0;
+    T* const dvs = b.grad_v.d ? sequence_base<T>(b.grad_v, p.pieces, whole) + head * b.grad_v_head + c0 : nullptr;
+    const long long state_at = ((long long)seq * p.heads + head) * p.key_dim * p.value_dim + c0;
+
+    Float4 s[2 * KT][NT];
+#pragma unroll
+    for (int j = 0; j < 2 * KT; ++j)
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int d = tile_row(j, 4 * g + i);
+                s[j][n][i] = p.state && d < p.key_dim && c0 + 16 * n < p.value_dim ? p.state[state_at + (long long)d * p.value_dim + 16 * n] : 0.0f;
+            }
+    for (int c = blocks - 1; c >= 0; --c) {
+        const int row0 = c * kDeltaRows, rows = len - row0 < kDeltaRows ? len - row0 : kDeltaRows;
+        const long long slot = slot0 + c;
+        __syncthreads();
+        const Block& from = p.blocks[slot * p.heads + head];
+        stage_rows<T, KT, true, !kOnePlace, true>(room, from.f, ks, p.k.row, qs, p.q.row, row0, rows, p.key_dim);
+        stage_block(room.m, from);
+        float* const behind = mark_of(b.behind, p, slot, head) + c0;
+#pragma unroll
+        for (int j = 0; j < 2 * KT; ++j)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int d = tile_row(j, 4 * g + i);
+                    if (d < p.key_dim && c0 + 16 * n < p.value_dim) behind[(long long)d * p.value_dim + 16 * n] = s[j][n][i];
+                }
+        Float4 o[4][NT], x[4][NT];       // dO; dU, dY, dX
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int t = tile_row(m, 4 * g + i);
+                    o[m][n][i] = t < rows && c0 + 16 * n < p.value_dim ? (float)dos[(long long)(row0 + t) * b.grad_out.row + 16 * n] : 0.0f;
+                }
+        __syncthreads();
+        {
+            HalfPair f[KT][NT];
+            float back[NT];
+            split_state<KT, NT>(s, f, back);
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                rows_product<KT, NT>(room.keys, m, lane, f, x[m]);
+                const Float4 writes = *reinterpret_cast<const Float4*>(&room.m.f.writes[tile_row(m, 4 * g)]);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) x[m][n] *= writes * back[n];
+            }
+        }
+        if constexpr (kOnePlace) {
+            __syncthreads();
+            stage_rows<T, KT, false, true, true>(room, from.f, ks, p.k.row, qs, p.q.row, row0, rows, p.key_dim);
+            __syncthreads();
+        }
+        HalfPair f[2][NT];
+        float back[NT];
+        split_rows<NT>(o, f, back);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            Float4 a[NT];
+            upper_product<NT>(room.m.mix, m, lane, f, a);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) x[m][n] += a[n] * (back[n] * room.m.f.mix_back);
+        }
+        split_rows<NT>(x, f, back);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            upper_product<NT>(room.m.solve, m, lane, f, x[m]);
+            const int t0 = tile_row(m, 4 * g);
+            const Float4 beta = *reinterpret_cast<const Float4*>(&room.m.f.beta[t0]), reads = *reinterpret_cast<const Float4*>(&room.m.f.reads[t0]),
+                         asks = *reinterpret_cast<const Float4*>(&room.m.f.asks[t0]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                x[m][n] *= back[n] * room.m.f.solve_back;
+                const bool there = c0 + 16 * n < p.value_dim;
+                if (there)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) behind[(long long)(p.key_dim + t0 + i) * p.value_dim + 16 * n] = x[m][n][i];
+                x[m][n] *= beta;
+                if (dvs && there)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (t0 + i < rows) dvs[(long long)(row0 + t0 + i) * b.grad_v.row + 16 * n] = (T)x[m][n][i];
+                x[m][n] *= -reads;
+                o[m][n] *= asks;
+            }
+        }
+        HalfPair fo[2][NT];
+        float back_o[NT];
+        split_rows<NT>(x, f, back);
+        split_rows<NT>(o, fo, back_o);
+        const float total = room.m.f.total;
+#pragma unroll
+        for (int j = 0; j < 2 * KT; ++j) {
+            Float4 a[NT], q[NT];
+            turned_product<KT, NT>(room.turned_keys, j, lane, f, a);
+            turned_product<KT, NT>(room.queries(), j, lane, fo, q);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[j][n][i] = __builtin_fmaf(total, s[j][n][i], __builtin_fmaf(a[n][i], back[n], q[n][i] * back_o[n]));
+        }
+    }
+    if (b.grad_state)
+#pragma unroll
+        for (int j = 0; j < 2 * KT; ++j)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int d = tile_row(j, 4 * g + i);
+                    if (d < p.key_dim && c0 + 16 * n < p.value_dim) b.grad_state[state_at + (long long)d * p.value_dim + 16 * n] = s[j][n][i];
+                }
+}
+
+// ---- gradients of q, k, g and beta ----------------------------------------------------------------------------------------
+constexpr int kAcross = 128;               // values taken together
+constexpr int kAcrossSteps = kAcross / 32;
+
+template <class T, int KT>
+struct RowsRoom {
+    static constexpr int kParts = kSplit<T> ? 2 : 1;
+    union {
+        struct {
+            Half8 keys[kParts][4 * KT][kDeltaRows], queries[kParts][4 * KT][kDeltaRows];      // 8 elements of every row
+        };
+        struct {                           // rows t (tile_row), 32 values
+            Half8 grad[kParts][4 * kAcrossSteps][kWave], x[2][4 * kAcrossSteps][kWave], u[2][4 * kAcrossSteps][kWave];
+        };
+        struct {
+            Half8 turned[kParts][4 * KT][kWave];
+            Half8 tri[4][2][kTriOperands][kWave];
+            float matrix[kDeltaRows][kTriStride];
+        };
+    };
+    double sum[kDeltaRows];
+    float back[3][kDeltaRows];             // powers of two of grad's, x's and u's rows
+    float up[kDeltaRows], rest[kDeltaRows], beta[kDeltaRows], dbeta[kDeltaRows];
+    float key[kDeltaRows], query[kDeltaRows], key_back[kDeltaRows], query_back[kDeltaRows];
+    float dots[2][kWavesPerBlock][kDeltaRows], pairs[kWavesPerBlock][kDeltaRows];
+    float most[2][kWavesPerBlock], inner[kWavesPerBlock], total;
+};
+
+// Tile and row in it of row t: the inverse of tile_row.
+__device__ __forceinline__ int tile_of(int t) { return 2 * (t >> 5) + (t >> 2 & 1); }
+__device__ __forceinline__ int row_in_tile(int t) { return 4 * (t >> 3 & 3) + (t & 3); }
+
+__device__ __forceinline__ float over_16(float v)
+{
+#pragma unroll
+    for (int x = 1; x < 16; x *= 2) v += __shfl_xor(v, x);
+    return v;
+}
+
+// Rows' sums over the lanes and waves of v[m][i], what a lane has for row tile_row(m, 4 g + i); to be read after a barrier.
+__device__ __forceinline__ void put_dots(const float (&v)[4][4], float (&to)[kWavesPerBlock][kDeltaRows])
+{
+    const int lane = threadIdx.x & (kWave - 1), g = lane >> 4;
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float s = over_16(v[m][i]);
+            if ((lane & 15) == 0) to[threadIdx.x >> 6][tile_row(m, 4 * g + i)] = s;
+        }
+}
+__device__ __forceinline__ float dot_of(const float (&from)[kWavesPerBlock][kDeltaRows], int t)
+{
+    float s = from[0][t];
+#pragma unroll
+    for (int w = 1; w < kWavesPerBlock; ++w) s += from[w][t];
+    return s;
+}
+
+template <class T, int KT>
+__global__ __launch_bounds__(kBlock) void delta_back_rows(DeltaBackParams b)
+{
+    const DeltaParams& p = b.f;
+    constexpr int kParts = kSplit<T> ? 2 : 1, kTiles = (2 * KT + kWavesPerBlock - 1) / kWavesPerBlock;      // of a wave, along the keys
+    __shared__ RowsRoom<T, KT> room;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, g = lane >> 4, r = lane & 15, many = p.heads / p.key_heads;
+    const int slot = (int)(blockIdx.x / p.key_heads), key_head = (int)(blockIdx.x % p.key_heads);
+    const Piece piece = find_piece(p.pieces, slot);
+    if (piece.seq < 0 || piece.n <= 0) return;
+    const T* const ks = sequence_base<const T>(p.k, p.pieces, piece) + piece.row0 * p.k.row + key_head * p.k_head;
+    const T* const qs = sequence_base<const T>(p.q, p.pieces, piece) + piece.row0 * p.q.row + key_head * p.q_head;
+    load_rows<T, KT>(ks, p.k.row, piece.n, p.key_dim, p.unit, room.keys, room.key_back, room.key);
+    load_rows<T, KT>(qs, p.q.row, piece.n, p.key_dim, p.unit, room.queries, room.query_back, room.query);
+    __syncthreads();
+    Float4 kk[4], qk[4];                      // K K^T and Q K^T, tile w's rows in wave w
+    key_products<T, KT, true>(room.keys, room.queries, kk, qk);
+    Float4 dq[4][kTiles], dk[4][kTiles];      // sums over the heads that share the key
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j) dq[m][j] = dk[m][j] = Float4(0.0f);
+
+    for (int h = key_head * many; h < (key_head + 1) * many; ++h) {
+        __syncthreads();
+        if (wave == 0) {
+            const bool there = lane < piece.n;
+            const long long at = piece.row0 + (there ? lane : 0);
+            float gate = 0.0f, beta = 0.0f;
+            if (there && p.g.d) gate = sequence_base<const float>(p.g, p.pieces, piece)[at * p.g.row + h];
+            if (there) beta = sequence_base<const float>(p.beta, p.pieces, piece)[at * p.beta.row + h];
+            double sum = gate < -1000.0f ? -1000.0 : (double)gate;
+#pragma unroll
+            for (int x = 1; x < kWave; x *= 2) {
+                const double before = __shfl_up(sum, x);
+                if (lane >= x) sum += before;
+            }
+            const double all = __shfl(sum, kWave - 1);
+            room.sum[lane] = sum;
+            room.beta[lane] = beta;
+            room.dbeta[lane] = 0.0f;
+            room.up[lane] = exp2_fast(kLog2e * (float)sum);
+            room.rest[lane] = exp2_fast(kLog2e * (float)(all - sum));
+            if (lane == 0) room.total = exp2_fast(kLog2e * (float)all);
+        }
+        const float* mark = mark_of(p.marks, p, slot, h);
+        const float* behind = mark_of(b.behind, p, slot, h);
+        const T* dos = sequence_base<const T>(b.grad_out, p.pieces, piece) + piece.row0 * b.grad_out.row + h * b.grad_out_head;
+        Float4 asked[4][kTiles], reads[4][kTiles], last[4][kTiles], pd[4], nd[4];
+        float inner = 0.0f;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            pd[m] = nd[m] = Float4(0.0f);
+#pragma unroll
+            for (int j = 0; j < kTiles; ++j) asked[m][j] = reads[m][j] = last[m][j] = Float4(0.0f);
+        }
+        for (int v0 = 0; v0 < p.value_dim; v0 += kAcross) {
+            __syncthreads();
+            // dO, dX = b dY and U = b R as operands, 16 lanes a row
+            {
+                const int e = tid & 15, at = v0 + 8 * e, have = p.value_dim - at;
+#pragma unroll
+                for (int t = tid >> 4; t < kDeltaRows; t += kBlock / 16) {
+                    const float beta = room.beta[t];
+                    const RowVec<T, 8> o = t < piece.n && have > 0 ? load_row_vec<T, 8>(dos + (long long)t * b.grad_out.row + at, have) : RowVec<T, 8>(T(0));
+                    const long long row = (long long)(p.key_dim + t) * p.value_dim + at;
+                    RowVec<float, 8> y(0.0f), u(0.0f);
+                    if (have > 0) {
+                        y = load_row_vec<float, 8>(behind + row, have);
+                        u = load_row_vec<float, 8>(mark + row, have);
+                    }
+                    float dot = 0.0f, mo = 0.0f, mx = 0.0f, mu = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        dot = __builtin_fmaf(y[i], u[i], dot);
+                        y[i] *= beta;
+                        u[i] *= beta;
+                        mo = larger(mo, (float)o[i]);
+                        mx = larger(mx, y[i]);
+                        mu = larger(mu, u[i]);
+                    }
+#pragma unroll
+                    for (int x = 1; x < 16; x *= 2) {
+                        dot += __shfl_xor(dot, x);
+                        mo = __builtin_fmaxf(mo, __shfl_xor(mo, x));
+                        mx = __builtin_fmaxf(mx, __shfl_xor(mx, x));
+                        mu = __builtin_fmaxf(mu, __shfl_xor(mu, x));
+                    }
+                    Scale so(mo);
+                    const Scale sx(mx), su(mu);
+                    if (__is_same(T, _Float16)) so.to = so.back = 1.0f;
+                    if (e == 0) {
+                        room.back[0][t] = so.back;
+                        room.back[1][t] = sx.back;
+                        room.back[2][t] = su.back;
+                        room.dbeta[t] += dot;
+                    }
+                    const int operand = tile_of(t) * kAcrossSteps + (e >> 2), entry = row_entry(e >> 2, e & 3, row_in_tile(t));
+                    Half8 hi, lo;
+                    to_halves<T>(o, so.to, hi, lo);
+                    room.grad[0][operand][entry] = hi;
+                    if constexpr (kParts > 1) room.grad[1][operand][entry] = lo;
+                    to_halves<float>(y, sx.to, hi, lo);
+                    room.x[0][operand][entry] = hi;
+                    room.x[1][operand][entry] = lo;
+                    to_halves<float>(u, su.to, hi, lo);
+                    room.u[0][operand][entry] = hi;
+                    room.u[1][operand][entry] = lo;
+                }
+            }
+            __syncthreads();
+            auto operand = [&](const Half8 (&a)[4 * kAcrossSteps][kWave], int m, int s) { return a[m * kAcrossSteps + s][row_entry(s, g, r)]; };
+            // dO U^T and dX U^T: wave w has tile w's rows
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+                if (n <= (wave | 1)) {
+                    Float4 a(0.0f), c(0.0f);
+#pragma unroll
+                    for (int s = 0; s < kAcrossSteps; ++s) {
+                        const Half8 uh = operand(room.u[0], n, s), ul = operand(room.u[1], n, s), xh = operand(room.x[0], wave, s);
+#pragma unroll
+                        for (int k = 0; k < kParts; ++k) {
+                            const Half8 o = operand(room.grad[k], wave, s);
+                            a = mfma(o, uh, a);
+                            if (k == 0) a = mfma(o, ul, a);
+                        }
+                        c = mfma(xh, uh, c);
+                        c = mfma(xh, ul, c);
+                        c = mfma(operand(room.x[1], wave, s), uh, c);
+                    }
+                    const float col = room.back[2][tile_row(n, r)];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int t = tile_row(wave, 4 * g + i);
+                        pd[n][i] += a[i] * (room.back[0][t] * col);
+                        nd[n][i] += c[i] * (room.back[1][t] * col);
+                    }
+                }
+            // dO S0^T, dX S0^T and U dS1^T: a wave has some of the keys' elements, for all rows
+#pragma unroll
+            for (int jj = 0; jj < kTiles; ++jj) {
+                const int j = wave * kTiles + jj, d = tile_row(j, r);
+                if (j >= 2 * KT) continue;
+                const bool there = d < p.key_dim;
+                RowVec<float, 8> s0[kAcrossSteps], s1[kAcrossSteps];
+                float m0 = 0.0f, m1 = 0.0f;
+#pragma unroll
+                for (int s = 0; s < kAcrossSteps; ++s) {
+                    const int at = v0 + 32 * s + 8 * g, have = p.value_dim - at;
+                    s0[s] = s1[s] = RowVec<float, 8>(0.0f);
+                    if (there && have > 0) {
+                        s0[s] = load_row_vec<float, 8>(mark + (long long)d * p.value_dim + at, have);
+                        s1[s] = load_row_vec<float, 8>(behind + (long long)d * p.value_dim + at, have);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        inner = __builtin_fmaf(s0[s][i], s1[s][i], inner);
+                        m0 = larger(m0, s0[s][i]);
+                        m1 = larger(m1, s1[s][i]);
+                    }
+                }
+                const Scale by0(over_column(m0)), by1(over_column(m1));
+                Float4 a[4], c[4], w[4];
+#pragma unroll
+                for (int m = 0; m < 4; ++m) a[m] = c[m] = w[m] = Float4(0.0f);
+#pragma unroll
+                for (int s = 0; s < kAcrossSteps; ++s) {
+                    Half8 h0, l0, h1, l1;
+                    to_halves<float>(s0[s], by0.to, h0, l0);
+                    to_halves<float>(s1[s], by1.to, h1, l1);
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+#pragma unroll
+                        for (int k = 0; k < kParts; ++k) {
+                            const Half8 o = operand(room.grad[k], m, s);
+                            a[m] = mfma(o, h0, a[m]);
+                            if (k == 0) a[m] = mfma(o, l0, a[m]);
+                        }
+                        const Half8 xh = operand(room.x[0], m, s), uh = operand(room.u[0], m, s);
+                        c[m] = mfma(xh, h0, c[m]);
+                        c[m] = mfma(xh, l0, c[m]);
+                        c[m] = mfma(operand(room.x[1], m, s), h0, c[m]);
+                        w[m] = mfma(uh, h1, w[m]);
+                        w[m] = mfma(uh, l1, w[m]);
+                        w[m] = mfma(operand(room.u[1], m, s), h1, w[m]);
+                    }
+                }
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int t = tile_row(m, 4 * g + i);
+                        const float up = room.up[t];
+                        asked[m][jj][i] += a[m][i] * (p.scale * up * room.back[0][t] * by0.back);
+                        reads[m][jj][i] -= c[m][i] * (up * room.back[1][t] * by0.back);
+                        last[m][jj][i] += w[m][i] * (room.rest[t] * room.back[2][t] * by1.back);
+                    }
+            }
+        }
+        // what the rows' decays have of S0, of dS1 and of one another's products
+        float dots[4][4], lasts[4][4];
+        auto element = [&](const T* x, long long stride, int t, int d) { return t < piece.n && d < p.key_dim ? (float)x[(long long)t * stride + d] : 0.0f; };
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int t = tile_row(m, 4 * g + i);
+                const float per_key = room.key[t] * room.key_back[t], per_query = room.query[t] * room.query_back[t];
+                float s = 0.0f, l = 0.0f;
+#pragma unroll
+                for (int jj = 0; jj < kTiles; ++jj) {
+                    const int d = tile_row(wave * kTiles + jj, r);
+                    if (wave * kTiles + jj >= 2 * KT) continue;
+                    const float k = element(ks, p.k.row, t, d) * per_key;
+                    s = __builtin_fmaf(element(qs, p.q.row, t, d) * per_query, asked[m][jj][i], s);
+                    s = __builtin_fmaf(k, reads[m][jj][i], s);
+                    l = __builtin_fmaf(k, last[m][jj][i], l);
+                }
+                dots[m][i] = s;
+                lasts[m][i] = l;
+            }
+        put_dots(dots, room.dots[0]);
+        put_dots(lasts, room.dots[1]);
+#pragma unroll
+        for (int x = 1; x < kWave; x *= 2) inner += __shfl_xor(inner, x);
+        if (lane == 0) room.inner[wave] = inner;
+        __syncthreads();                          // room.matrix lies over the operands
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = tile_row(wave, 4 * g + i), col = tile_row(n, r);
+                float v = 0.0f;
+                if (col < row) {
+                    const float d = exp2_fast(kLog2e * (float)(room.sum[row] - room.sum[col])) * room.key_back[col];
+                    v = d * (p.scale * pd[n][i] * qk[n][i] * room.query_back[row] - nd[n][i] * kk[n][i] * room.key_back[row]);
+                }
+                room.matrix[row][col] = v;
+            }
+        __syncthreads();
+        {                                         // each row's sums up to a column: 16 columns a lane, then the lanes before it
+            const int row = 16 * wave + r;
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                s += room.matrix[row][16 * g + i];
+                room.matrix[row][16 * g + i] = s;
+            }
+            const float s0 = __shfl(s, r), s1 = __shfl(s, r + 16), s2 = __shfl(s, r + 32);
+            const float before = g == 0 ? 0.0f : g == 1 ? s0 : g == 2 ? s0 + s1 : s0 + s1 + s2;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) room.matrix[row][16 * g + i] += before;
+        }
+        __syncthreads();
+        {
+            float s = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (16 * wave + i >= lane && lane > 0) s += room.matrix[16 * wave + i][lane - 1];
+            room.pairs[wave][lane] = s;
+        }
+        __syncthreads();
+        if (wave == 0) {
+            float from = dot_of(room.dots[0], lane), up_to = dot_of(room.dots[1], lane);
+#pragma unroll
+            for (int x = 1; x < kWave; x *= 2) {
+                const float a = __shfl_down(from, x), c = __shfl_up(up_to, x);
+                if (lane + x < kWave) from += a;
+                if (lane >= x) up_to += c;
+            }
+            const float before = __shfl_up(up_to, 1);
+            const float dg = dot_of(room.pairs, lane) + from + (lane ? before : 0.0f) + room.total * ((room.inner[0] + room.inner[1]) + (room.inner[2] + room.inner[3]));
+            const long long at = piece.row0 + lane;
+            if (lane < piece.n) {
+                if (b.grad_g.d) sequence_base<float>(b.grad_g, p.pieces, piece)[at * b.grad_g.row + h] = dg;
+                if (b.grad_beta.d) sequence_base<float>(b.grad_beta, p.pieces, piece)[at * b.grad_beta.row + h] = room.dbeta[lane];
+            }
+        }
+        // dP and dA as operands: their columns, transposed their rows, with the factor of the key or query that they meet
+        float back[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            __syncthreads();
+            float most = 0.0f;
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int row = tile_row(wave, 4 * g + i), col = tile_row(n, r);
+                    float v = 0.0f;
+                    if (k % 2 ? col < row : col <= row) {
+                        const float d = exp2_fast(kLog2e * (float)(room.sum[row] - room.sum[col]));
+                        v = (k % 2 ? -nd[n][i] : p.scale * pd[n][i]) * d * (k < 2 ? room.key_back[col] : k == 2 ? room.query_back[row] : room.key_back[row]);
+                    }
+                    most = larger(most, v);
+                    room.matrix[row][col] = v;
+                }
+            const Scale by(over_block(most, room.most[k % 2]));
+            back[k] = by.back;
+            if (k < 2) store_operands<false>(room.matrix, by.to, room.tri[k]);
+            else store_operands<true>(room.matrix, by.to, room.tri[k]);
+        }
+#pragma unroll
+        for (int query = 0; query < 2; ++query) {
+            if (query) __syncthreads();
+            for (int job = tid; job < 32 * KT; job += kBlock) {
+                const int sq = job / (4 * KT), e = job % (4 * KT);
+                RowVec<T, 8> v[8];
+                load_square(query ? qs : ks, query ? p.q.row : p.k.row, 0, piece.n, p.key_dim, sq, e, v);
+                Half8 hi[8], lo[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) to_halves<T>(v[i], __is_same(T, _Float16) ? 1.0f : (query ? room.query : room.key)[8 * sq + i], hi[i], lo[i]);
+                put_turned<T, KT>(hi, lo, sq, e, room.turned);
+            }
+            __syncthreads();
+#pragma unroll
+            for (int jj = 0; jj < kTiles; ++jj) {
+                const int j = wave * kTiles + jj;
+                if (j >= 2 * KT) continue;
+                HalfPair f[2][1];
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    f[s][0].hi = turned_of<KT>(room.turned[0], j, s, lane);
+                    f[s][0].lo = kParts > 1 ? turned_of<KT>(room.turned[kParts - 1], j, s, lane) : Half8((_Float16)0.0f);
+                }
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    Float4 a[1];
+                    if (!query) {
+                        lower_product<1>(room.tri[0], m, lane, f, a);
+                        asked[m][jj] += a[0] * back[0];
+                        lower_product<1>(room.tri[1], m, lane, f, a);
+                        reads[m][jj] += a[0] * back[1];
+                        upper_product<1>(room.tri[3], m, lane, f, a);
+                        last[m][jj] += a[0] * back[3];
+                    } else {
+                        upper_product<1>(room.tri[2], m, lane, f, a);
+                        last[m][jj] += a[0] * back[2];
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int j = 0; j < kTiles; ++j) {
+                dq[m][j] += asked[m][j];
+                dk[m][j] += reads[m][j] + last[m][j];
+            }
+    }
+    // through the rows' lengths: d - e (e . d) over the length, e the row at unit length
+#pragma unroll
+    for (int query = 0; query < 2; ++query) {
+        const ssam_rows& to = query ? b.grad_q : b.grad_k;
+        if (!to.d) continue;
+        const T* from = query ? qs : ks;
+        const long long stride = query ? p.q.row : p.k.row;
+        Float4(&d)[4][kTiles] = query ? dq : dk;
+        if (p.unit) {
+            float dots[4][4];
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int t = tile_row(m, 4 * g + i);
+                    const float per = query ? room.query[t] * room.query_back[t] : room.key[t] * room.key_back[t];
+                    float s = 0.0f;
+#pragma unroll
+                    for (int jj = 0; jj < kTiles; ++jj) {
+                        const int e = tile_row(wave * kTiles + jj, r);
+                        if (wave * kTiles + jj < 2 * KT && t < piece.n && e < p.key_dim) s = __builtin_fmaf((float)from[(long long)t * stride + e] * per, d[m][jj][i], s);
+                    }
+                    dots[m][i] = s;
+                }
+            __syncthreads();
+            put_dots(dots, room.dots[0]);
+            __syncthreads();
+        }
+        T* const out = sequence_base<T>(to, p.pieces, piece) + piece.row0 * to.row + key_head * b.grad_key_head;
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int t = tile_row(m, 4 * g + i);
+                if (t >= piece.n) continue;
+                const float per = query ? room.query[t] * room.query_back[t] : room.key[t] * room.key_back[t];
+                const float dot = p.unit ? dot_of(room.dots[0], t) : 0.0f;
+#pragma unroll
+                for (int jj = 0; jj < kTiles; ++jj) {
+                    const int e = tile_row(wave * kTiles + jj, r);
+                    if (wave * kTiles + jj >= 2 * KT || e >= p.key_dim) continue;
+                    float v = d[m][jj][i];
+                    if (p.unit) v = per * (v - (float)from[(long long)t * stride + e] * per * dot);
+                    out[(long long)t * to.row + e] = (T)v;
+                }
+            }
+    }
+}
+
+struct BackPlan {
+    long long slots;
+    size_t blocks, behind;      // bytes
+};
+BackPlan back_plan(const ssam_scan_delta_backward_args& a)
+{
+    BackPlan p;
+    p.slots = piece_slots(a.seq, kDeltaRows);
+    p.blocks = (size_t)product(product(p.slots, a.heads), sizeof(Block));
+    p.behind = (size_t)product(product(p.slots, a.heads), (long long)(a.key_dim + kDeltaRows) * a.value_dim * 4);
+    return p;
+}
+
+}  // namespace
+}  // namespace ssam
+
+extern "C" {
+
+size_t ssam_scan_delta_backward_workspace_bytes(const ssam_scan_delta_backward_args* a)
+{
+    using namespace ssam;
+    if (!a || check_delta(*a) || check_sequences(a->seq) || a->seq.sequences == 0) return 0;
+    const BackPlan p = back_plan(*a);
+    return (size_t)held_to_62((__int128)p.blocks + p.behind);
+}
+
+int ssam_scan_delta_backward(const ssam_scan_delta_backward_args* a, void* hip_stream)
+{
+    using namespace ssam;
+    if (!a) return SSAM_ERR_NULL;
+    if (int e = check_delta(*a)) return e;
+    if (int e = check_sequences(a->seq)) return e;
+    if (a->seq.sequences == 0) return SSAM_OK;
+    const int esz = type_bytes(a->dtype);
+    if (int e = check_delta_rows(*a, a->seq)) return e;
+    const long long keys = (long long)a->key_heads * a->key_dim, values = (long long)a->heads * a->value_dim;
+    if (a->grad_out_head < 0 || a->grad_out_head > kMaxStride) return SSAM_ERR_DIM;
+    if (int e = check_rows(a->grad_out, a->seq, heads_width(a->heads, a->grad_out_head, a->value_dim), esz, false)) return e;
+    for (const ssam_rows* r : {&a->grad_q, &a->grad_k})
+        if (int e = check_out_rows(*r, a->seq, keys, esz, true)) return e;
+    if (int e = check_out_rows(a->grad_v, a->seq, values, esz, true)) return e;
+    for (const ssam_rows* r : {&a->grad_g, &a->grad_beta})
+        if (int e = check_out_rows(*r, a->seq, a->heads, 4, true)) return e;
+    for (const void* f : {(const void*)a->d_marks, (const void*)a->d_grad_final, (const void*)a->d_grad_state})
+        if ((uintptr_t)f % 4) return SSAM_ERR_DIM;
+    if (!a->d_marks || !a->d_work) return SSAM_ERR_NULL;
+    const BackPlan plan = back_plan(*a);
+    const size_t bytes = ssam_scan_delta_backward_workspace_bytes(a);
+    if ((long long)bytes > kMaxExtent || a->work_bytes < bytes || (uintptr_t)a->d_work % 16) return SSAM_ERR_DIM;
+    const long long state_bytes = product(a->seq.sequences, values * a->key_dim * 4);
+    if (state_bytes > 4 * kMaxExtent) return SSAM_ERR_DIM;
+    const Cover outs[] = {cover_rows(a->grad_q, a->seq, keys, esz), cover_rows(a->grad_k, a->seq, keys, esz), cover_rows(a->grad_v, a->seq, values, esz),
+                          cover_rows(a->grad_g, a->seq, a->heads, 4), cover_rows(a->grad_beta, a->seq, a->heads, 4),
+                          cover_plain(a->d_grad_state, state_bytes), cover_plain(a->d_work, (long long)bytes)};
+    const Cover ins[] = {cover_rows(a->q, a->seq, heads_width(a->key_heads, a->q_head, a->key_dim), esz),
+                         cover_rows(a->k, a->seq, heads_width(a->key_heads, a->k_head, a->key_dim), esz),
+                         cover_rows(a->v, a->seq, heads_width(a->heads, a->v_head, a->value_dim), esz), cover_rows(a->g, a->seq, a->heads, 4),
+                         cover_rows(a->beta, a->seq, a->heads, 4), cover_rows(a->grad_out, a->seq, heads_width(a->heads, a->grad_out_head, a->value_dim), esz),
+                         cover_plain(a->d_grad_final, state_bytes), cover_plain(a->d_marks, (long long)plan.behind)};
+    if (any_overlap(outs, ins)) return SSAM_ERR_ALIAS;
+
+    DeltaBackParams b{};
+    b.f = DeltaParams{make_pieces(a->seq, kDeltaRows), a->q, a->k, a->v, ssam_rows{nullptr, 0, 0}, a->g, a->beta, a->q_head, a->k_head, a->v_head, 0,
+                      a->d_grad_final, nullptr, const_cast<float*>(a->d_marks), static_cast<Block*>(a->d_work), a->heads, a->key_heads, a->key_dim,
+                      a->value_dim, a->unit != 0, a->scale, (a->value_dim + 63) / 64};
+    b.grad_out = a->grad_out;
+    b.grad_q = a->grad_q;
+    b.grad_k = a->grad_k;
+    b.grad_v = a->grad_v;
+    b.grad_g = a->grad_g;
+    b.grad_beta = a->grad_beta;
+    b.grad_out_head = a->grad_out_head;
+    b.grad_v_head = a->value_dim;
+    b.grad_key_head = a->key_dim;
+    b.grad_state = a->d_grad_state;
+    b.behind = reinterpret_cast<float*>(static_cast<char*>(a->d_work) + plan.blocks);
+    const long long walks = product((long long)a->seq.sequences * a->heads, b.f.tiles), rows = product(plan.slots, a->key_heads);
+    if (walks > kMaxGrid || rows > kMaxGrid) return SSAM_ERR_DIM;
+    hipStream_t st = (hipStream_t)hip_stream;
+    return with_delta_type(a->dtype, [&](auto t) {
+        return with_key(a->key_dim, [&](auto kt) {
+            using T = decltype(t);
+            constexpr int KT = decltype(kt)::value;
+            hipLaunchKernelGGL((delta_back_prepare<T, KT>), dim3((unsigned)rows), dim3(kBlock), 0, st, b.f);
+            if (int e = launched()) return e;
+            hipLaunchKernelGGL((delta_back_walk<T, KT, 1>), dim3((unsigned)walks), dim3(kBlock), 0, st, b);
+            if (int e = launched()) return e;
+            if (!a->grad_q.d && !a->grad_k.d && !a->grad_g.d && !a->grad_beta.d) return (int)SSAM_OK;
+            hipLaunchKernelGGL((delta_back_rows<T, KT>), dim3((unsigned)rows), dim3(kBlock), 0, st, b);
+            return launched();
+        });
+    });
+}
+
+}  // extern "C"

@@ -190,6 +190,53 @@ __device__ __forceinline__ void lower_product(const Half8 (&matrix)[2][kTriOpera
         }
 }
 
+// The same for rows of tile m of an upper one.
+template <int NT>
+__device__ __forceinline__ void upper_product(const Half8 (&matrix)[2][kTriOperands][kWave], int m, int lane, const HalfPair (&f)[2][NT], Float4 (&y)[NT])
+{
+#pragma unroll
+    for (int n = 0; n < NT; ++n) y[n] = Float4(0.0f);
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+        if (s >= m >> 1) {
+            const Half8 hi = matrix[0][upper_operand(m, s)][lane], lo = matrix[1][upper_operand(m, s)][lane];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                y[n] = mfma(hi, f[s][n].hi, y[n]);
+                y[n] = mfma(hi, f[s][n].lo, y[n]);
+                y[n] = mfma(lo, f[s][n].hi, y[n]);
+            }
+        }
+}
+
+// 64 rows of a wave's columns as B operands; their power of two, per column.
+template <int NT>
+__device__ __forceinline__ void split_rows(const Float4 (&x)[4][NT], HalfPair (&f)[2][NT], float (&back)[NT])
+{
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const Scale by(over_column(larger(larger(larger(larger(0.0f, x[0][n]), x[1][n]), x[2][n]), x[3][n])));
+        back[n] = by.back;
+        f[0][n] = split(x[0][n], x[1][n], by.to);
+        f[1][n] = split(x[2][n], x[3][n], by.to);
+    }
+}
+// A state's.
+template <int KT, int NT>
+__device__ __forceinline__ void split_state(const Float4 (&s)[2 * KT][NT], HalfPair (&f)[KT][NT], float (&back)[NT])
+{
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        float m = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 2 * KT; ++j) m = larger(m, s[j][n]);
+        const Scale by(over_column(m));
+        back[n] = by.back;
+#pragma unroll
+        for (int k = 0; k < KT; ++k) f[k][n] = split(s[2 * k][n], s[2 * k + 1][n], by.to);
+    }
+}
+
 // ---- delta_prepare -----------------------------------------------------------------------------------------------------------
 constexpr int kTriStride = kDeltaRows + 1;      // floats of a row in LDS
 
@@ -241,6 +288,33 @@ __device__ __forceinline__ void load_rows(const T* __restrict__ base, long long 
             scale[t] = by.to;
             factor[t] = by.back * (unit ? 1.0f / __builtin_sqrtf(squares + 1e-6f) : 1.0f);
         }
+    }
+}
+
+// K K^T and Q K^T, without their factors: wave w has the rows of tile w (kTiles: tile_row, otherwise 16 w ..) and the columns up to them.
+template <class T, int KT, bool kTiles, int kParts>
+__device__ __forceinline__ void key_products(const Half8 (&keys)[kParts][4 * KT][kDeltaRows], const Half8 (&queries)[kParts][4 * KT][kDeltaRows],
+                                             Float4 (&kk)[4], Float4 (&qk)[4])
+{
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        kk[j] = qk[j] = Float4(0.0f);
+        if (j <= (kTiles ? wave | 1 : wave))
+#pragma unroll
+            for (int s = 0; s < KT; ++s) {
+                const int e = 4 * s + g, row = (kTiles ? tile_row(wave, r) : 16 * wave + r) ^ (e & 15), col = (kTiles ? tile_row(j, r) : 16 * j + r) ^ (e & 15);
+                const Half8 b = keys[0][e][col];
+                kk[j] = mfma(keys[0][e][row], b, kk[j]);
+                qk[j] = mfma(queries[0][e][row], b, qk[j]);
+                if constexpr (kParts == 2) {
+                    const Half8 c = keys[1][e][col];
+                    kk[j] = mfma(keys[0][e][row], c, kk[j]);
+                    qk[j] = mfma(queries[0][e][row], c, qk[j]);
+                    kk[j] = mfma(keys[1][e][row], b, kk[j]);
+                    qk[j] = mfma(queries[1][e][row], b, qk[j]);
+                }
+            }
     }
 }
 
@@ -323,34 +397,14 @@ __device__ __forceinline__ float over_block(float m, float* room)
 template <class T, int KT, bool kBack>
 __device__ __forceinline__ void prepare_block(const DeltaParams& p, const Piece& piece, long long slot, int key_head, PrepareRoom<T, KT>& room)
 {
-    constexpr int kParts = kSplit<T> ? 2 : 1;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, g = lane >> 4, r = lane & 15, many = p.heads / p.key_heads;
     load_rows<T, KT>(sequence_base<const T>(p.k, p.pieces, piece) + piece.row0 * p.k.row + key_head * p.k_head, p.k.row, piece.n, p.key_dim, p.unit, room.keys,
                      room.key, room.f.key);
     load_rows<T, KT>(sequence_base<const T>(p.q, p.pieces, piece) + piece.row0 * p.q.row + key_head * p.q_head, p.q.row, piece.n, p.key_dim, p.unit, room.queries,
                      room.query, room.f.query);
     __syncthreads();
-    // K K^T and Q K^T: wave w has rows 16 w .. and the columns up to them
     Float4 kk[4], qk[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        kk[j] = qk[j] = Float4(0.0f);
-        if (j <= wave)
-#pragma unroll
-            for (int s = 0; s < KT; ++s) {
-                const int e = 4 * s + g, row = (16 * wave + r) ^ (e & 15), col = (16 * j + r) ^ (e & 15);
-                const Half8 b = room.keys[0][e][col];
-                kk[j] = mfma(room.keys[0][e][row], b, kk[j]);
-                qk[j] = mfma(room.queries[0][e][row], b, qk[j]);
-                if constexpr (kParts == 2) {
-                    const Half8 c = room.keys[1][e][col];
-                    kk[j] = mfma(room.keys[0][e][row], c, kk[j]);
-                    qk[j] = mfma(room.queries[0][e][row], c, qk[j]);
-                    kk[j] = mfma(room.keys[1][e][row], b, kk[j]);
-                    qk[j] = mfma(room.queries[1][e][row], b, qk[j]);
-                }
-            }
-    }
+    key_products<T, KT, false>(room.keys, room.queries, kk, qk);
     for (int h = key_head * many; h < (key_head + 1) * many; ++h) {
         __syncthreads();                          // the operands, or the last head's matrices, are done with
         if (wave == 0) {

@@ -38,6 +38,8 @@ struct {
     decltype(&ssam_rms_norm_e4m3) norm_e4m3;
     decltype(&ssam_rms_norm_backward) norm_backward;
     decltype(&ssam_rms_norm_backward_workspace_bytes) norm_backward_bytes;
+    decltype(&ssam_scan_delta_backward) delta_backward;
+    decltype(&ssam_scan_delta_backward_workspace_bytes) delta_backward_bytes;
 } entry;
 PyObject* status_error;      // the binding's exception class, called with (status, entry point)
 
@@ -690,6 +692,41 @@ PyObject* delta(PyObject*, PyObject* const* o, Py_ssize_t n)
     });
 }
 
+// delta_backward(d_grad, d_q, d_k, d_v, g, beta, scale, unit, d_marks, d_grad_final, starts, lengths, state_grad, d_work, stream)
+//     -> (q, k, v, g, beta, state)
+PyObject* delta_backward(PyObject*, PyObject* const* o, Py_ssize_t n)
+{
+    if (!arity(n, 15)) return nullptr;
+    return guarded([&] {
+        ssam_scan_delta_backward_args s{};
+        const Tensor& v = delta_inputs(&s, o + 1, o[6], o[7]);
+        s.seq = sequences(v, optional(o[10], "starts"), optional(o[11], "lengths"), 2);
+        s.grad_out = head_rows(tensor(o[0], "d_grad"), "d_grad", v, s.heads, s.value_dim, &s.grad_out_head);
+        const Tensor &q = tensor(o[1], "d_q"), &k = tensor(o[2], "d_k"), &beta = tensor(o[5], "beta");
+        s.d_marks = delta_marks_for(&tensor(o[8], "d_marks"), k, v, s.seq);
+        const int64_t carried[] = {s.seq.sequences, s.heads, s.key_dim, s.value_dim};
+        s.d_grad_final = dense<const float>(optional(o[9], "d_grad_final"), "d_grad_final", v, at::kFloat, carried);
+        const bool ragged = s.seq.d_begin || s.seq.d_end;
+        const Tensor gq = result(nullptr, q, ragged), gk = result(nullptr, k, ragged), gv = result(nullptr, v, ragged), gb = result(nullptr, beta, ragged);
+        const Tensor gg = o[4] != Py_None ? result(nullptr, beta, ragged) : Tensor();
+        const Tensor gs = truth(o[12]) ? at::empty(carried, beta.options()) : Tensor();
+        long long apart;
+        s.grad_q = head_rows(gq, "q", v, s.key_heads, s.key_dim, &apart);
+        s.grad_k = head_rows(gk, "k", v, s.key_heads, s.key_dim, &apart);
+        s.grad_v = head_rows(gv, "v", v, s.heads, s.value_dim, &apart);
+        if (gg.defined()) s.grad_g = head_values(&gg, "g", v);
+        s.grad_beta = head_values(&gb, "beta", v);
+        if (gs.defined()) s.d_grad_state = static_cast<float*>(gs.data_ptr());
+        const Tensor work = workspace(entry.delta_backward_bytes(&s), optional(o[13], "d_work"), v);
+        if (work.defined()) {
+            s.d_work = work.data_ptr();
+            s.work_bytes = work.nbytes();
+        }
+        call(entry.delta_backward, s, o[14], "ssam_scan_delta_backward");
+        return Py_BuildValue("(NNNNNN)", wrap(gq), wrap(gk), wrap(gv), wrap(gg), wrap(gb), wrap(gs));
+    });
+}
+
 // delta_step(d_q, d_k, d_v, g, beta, d_state, scale, unit, slots, d_out, stream) -> d_out
 PyObject* delta_step(PyObject*, PyObject* const* o, Py_ssize_t n)
 {
@@ -846,7 +883,7 @@ PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n)
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(bind), FAST(conv1d), FAST(conv1d_backward), FAST(conv1d_step), FAST(scan), FAST(scan_bytes), FAST(scan_marks),
                          FAST(scan_backward), FAST(scan_step), FAST(delta), FAST(delta_bytes), FAST(delta_marks), FAST(delta_step), FAST(norm),
-                         FAST(norm_e4m3), FAST(norm_backward), {nullptr, nullptr, 0, nullptr}};
+                         FAST(norm_e4m3), FAST(norm_backward), FAST(delta_backward), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_sequence", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

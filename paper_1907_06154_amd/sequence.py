@@ -26,7 +26,7 @@ EXPORTS = ["ssam_conv1d", "ssam_conv1d_backward", "ssam_conv1d_backward_workspac
            "ssam_scan_selective_workspace_bytes", "ssam_scan_selective_marks", "ssam_scan_selective_backward",
            "ssam_scan_selective_backward_workspace_bytes", "ssam_scan_selective_step", "ssam_scan_delta", "ssam_scan_delta_workspace_bytes",
            "ssam_scan_delta_marks", "ssam_scan_delta_step", "ssam_rms_norm", "ssam_rms_norm_e4m3", "ssam_rms_norm_backward",
-           "ssam_rms_norm_backward_workspace_bytes"]
+           "ssam_rms_norm_backward_workspace_bytes", "ssam_scan_delta_backward", "ssam_scan_delta_backward_workspace_bytes"]
 
 _torch = None
 _fast = None          # the extension module, bound to the library's entry points
@@ -50,6 +50,15 @@ class ScanSelectiveGrads(NamedTuple):
     skip: Optional[object]
     gate: Optional[object]
     dt_bias: Optional[object]
+    state: Optional[object]
+
+
+class ScanDeltaGrads(NamedTuple):
+    q: object
+    k: object
+    v: object
+    g: Optional[object]
+    beta: object
     state: Optional[object]
 
 
@@ -187,6 +196,15 @@ def ssam_scan_delta(d_q, d_k, d_v, g, beta, scale=None, unit: bool = False, d_st
     + 1e-6).  scale: 1 / sqrt(key width) if None.  d_state, d_final [sequences, heads, key, value], float32; d_final may be d_state.
     d_marks (from ssam_scan_delta_marks) keeps what the gradients need."""
     return _run("delta", d_v, stream, (d_q, d_k, d_v, g, beta, scale, unit, d_state, d_final, d_marks, starts, lengths, d_out, d_work))
+
+
+def ssam_scan_delta_backward(d_grad, d_q, d_k, d_v, g, beta, d_marks, scale=None, unit: bool = False, d_grad_final=None, starts=None, lengths=None,
+                             state_grad: bool = False, d_work=None, stream=None) -> ScanDeltaGrads:
+    """Gradients of ssam_scan_delta for d_grad, the gradient of its result, and d_grad_final, that of its d_final (none if absent), from the
+    marks the forward call left.  q's, k's and v's come in d_v's type, g's and beta's in float32; state_grad: that of d_state (or of the
+    zeros in its place) too."""
+    return ScanDeltaGrads(*_run("delta_backward", d_v, stream, (d_grad, d_q, d_k, d_v, g, beta, scale, unit, d_marks, d_grad_final, starts, lengths,
+                                                                state_grad, d_work)))
 
 
 def ssam_scan_delta_step(d_q, d_k, d_v, g, beta, d_state, scale=None, unit: bool = False, slots=None, d_out=None, stream=None):

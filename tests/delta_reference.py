@@ -30,9 +30,10 @@ def delta(q, k, v, g, beta, scale, h0):
 
 
 def delta_back(dout, q, k, v, g, beta, scale, kept, dlast):
-    """Gradients of q, k, v, g, beta, h0, and the sizes of the terms that g's is a sum of."""
+    """Gradients of q, k, v, g, beta, h0, and the sizes of what g's, beta's, k's and v's are made of: products of the lengths of what is multiplied."""
     d = dlast.copy()
-    r = {n: np.zeros_like(a) for n, a in (("q", q), ("k", k), ("v", v), ("g", g), ("beta", beta), ("size", g))}
+    r = {n: np.zeros_like(a) for n, a in (("q", q), ("k", k), ("v", v), ("g", g), ("beta", beta), ("size", g), ("bsize", g), ("ksize", k), ("vsize", v))}
+    length = lambda a, axis: np.sqrt((a * a).sum(axis))  # noqa: E731
     for t in reversed(range(q.shape[0])):
         s, miss, h = kept[t]
         r["q"][t] = scale * (h * dout[t][:, None]).sum(-1)
@@ -42,6 +43,9 @@ def delta_back(dout, q, k, v, g, beta, scale, kept, dlast):
         dmiss = beta[t][:, None] * du
         r["k"][t] = (d * (beta[t][:, None] * miss)[:, None]).sum(-1) - (s * dmiss[:, None]).sum(-1)
         r["v"][t] = dmiss
+        r["vsize"][t] = beta[t][:, None] * length(d, 1) * length(k[t], -1)[:, None]
+        r["bsize"][t] = length(length(d, 1) * length(k[t], -1)[:, None], -1) * length(miss, -1)
+        r["ksize"][t] = length(d, -1) * length(beta[t][:, None] * miss, -1)[:, None] + length(s, -1) * length(dmiss, -1)[:, None]
         d = d - k[t][:, :, None] * dmiss[:, None]
         r["g"][t] = (d * s).sum((-1, -2))
         r["size"][t] = np.sqrt((d * d).sum((-1, -2)) * (s * s).sum((-1, -2)))

@@ -206,3 +206,67 @@ def test_delta_step_goes_on_where_the_scan_ends():
         rest.append(ssam.ssam_scan_delta_step(*(v[n][:, t] for n in ("q", "k", "v", "g", "beta")), state, unit=True))
     got = torch.cat([first, torch.stack(rest, 1)], 1)
     near("out", got.reshape(-1, 4 * 64), f64(whole).reshape(-1, 4 * 64), 2 * ref.delta_noise(lead[1]) + 2.0 ** -8, "bfloat16")
+
+
+@pytest.mark.parametrize("lay,dt,Hk,H,K,V,unit,state,form", DELTA)
+def test_delta_gradients(lay, dt, Hk, H, K, V, unit, state, form):
+    lead, dev, spans, v, h0, flat, S = case(lay, dt, Hk, H, K, V, unit, state, form)
+    g = torch.Generator().manual_seed(9)
+    dout = randn(g, *lead, H, V, dtype=TYPES[dt]) if form == "dense" else randn(g, *lead, H, V + 3, dtype=TYPES[dt])[..., 2:2 + V]
+    dlast = randn(g, S, H, K, V) if state else None
+    layer = (v["q"], v["k"], v["v"], v["g"], v["beta"])
+    marks = ssam.ssam_scan_delta_marks(v["k"], v["v"], **dev)
+    out = ssam.ssam_scan_delta(*layer, unit=unit, d_state=h0, d_marks=marks, **dev)
+    assert torch.equal(out, ssam.ssam_scan_delta(*layer, unit=unit, d_state=h0, **dev))
+    got = ssam.ssam_scan_delta_backward(dout, *layer, marks, unit=unit, d_grad_final=dlast, state_grad=True, **dev)
+    rows, many = int(np.prod(lead)), H // Hk
+    fd = f64(dout).reshape(rows, H, V)
+    seen = np.zeros(rows, bool)
+    parts, longest = {n: [] for n in ("q", "k", "v", "g", "beta", "size", "ksize", "bsize", "vsize")}, 1
+    states = []
+    for s, first, n in spans:
+        at = slice(first, first + n)
+        seen[at] = True
+        longest = max(longest, n)
+        start = np.zeros((H, K, V)) if h0 is None else f64(h0[s])
+        a = [flat[k][at] for k in ("q", "k", "v", "g", "beta")]
+        _, _, kept = ref.delta(*a, K ** -0.5, start)
+        r = ref.delta_back(fd[at], *a, K ** -0.5, kept, np.zeros((H, K, V)) if dlast is None else f64(dlast[s]))
+        states.append(r.pop("state"))
+        for k in parts:
+            parts[k].append(r[k])
+    noise = ref.delta_noise(longest)
+    whole = {k: np.concatenate(x) if x else np.zeros((0, H, 1)) for k, x in parts.items()}
+    if seen.any():
+        inner = {}
+        for n in "qk":
+            raw = f64(v[n]).reshape(rows, Hk, K)[seen]
+            d, m = whole[n].reshape(-1, Hk, many, K).sum(2), whole[n + "size"].reshape(-1, Hk, many, K).sum(2) if n == "k" else None
+            size = np.sqrt((raw * raw).sum(-1, keepdims=True) + 1e-6)
+            full = np.abs(d) if m is None else m
+            inner[n] = (ref.through_unit(raw, d), (full + np.abs(raw / size) * (np.abs(raw / size) * full).sum(-1, keepdims=True)) / size) if unit else (d, full)
+        for n, (want, size) in inner.items():
+            x = f64(getattr(got, n)).reshape(rows, Hk * K)[seen]
+            near(n, torch.from_numpy(x), want.reshape(-1, Hk * K), noise, dt, size.reshape(-1, Hk * K))
+        for n, size in (("v", whole["vsize"]), ("g", whole["size"]), ("beta", whole["bsize"])):
+            x = f64(getattr(got, n)).reshape(rows, -1)[seen]
+            near(n, torch.from_numpy(x), whole[n].reshape(len(x), -1), noise, dt if n == "v" else "float32", size.reshape(len(x), -1))
+    near("state", torch.from_numpy(f64(got.state).transpose(0, 2, 1, 3).reshape(-1, H * V)), np.stack(states).transpose(0, 2, 1, 3).reshape(-1, H * V), noise,
+         "float32")
+    for n in ("q", "k", "v", "g", "beta"):
+        x = getattr(got, n)
+        assert x.shape == v[n].shape and x.dtype == v[n].dtype and (x.reshape(rows, -1)[torch.from_numpy(~seen).cuda()] == 0).all()
+    again = ssam.ssam_scan_delta_backward(dout, *layer, marks, unit=unit, d_grad_final=dlast, state_grad=True, **dev)
+    assert all(torch.equal(a, b) for a, b in zip(got, again))
+
+
+def test_delta_gradients_without_decay():
+    lead, dev, spans, v, h0, flat, S = case("batch", "bfloat16", 1, 2, 64, 48, True, True, "dense", gate=False)
+    layer = (v["q"], v["k"], v["v"], None, v["beta"])
+    marks = ssam.ssam_scan_delta_marks(v["k"], v["v"])
+    ssam.ssam_scan_delta(*layer, unit=True, d_state=h0, d_marks=marks)
+    dout = randn(torch.Generator().manual_seed(1), *v["v"].shape, dtype=v["v"].dtype)
+    got = ssam.ssam_scan_delta_backward(dout, *layer, marks, unit=True)
+    assert got.g is None and got.state is None
+    zeros = ssam.ssam_scan_delta_backward(dout, *layer[:3], torch.zeros_like(v["beta"]), v["beta"], marks, unit=True)
+    assert all(torch.equal(getattr(got, n), getattr(zeros, n)) for n in ("q", "k", "v", "beta"))
