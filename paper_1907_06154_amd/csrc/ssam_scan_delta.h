@@ -68,11 +68,15 @@ __device__ __forceinline__ HalfPair split(const Float4& a, const Float4& b, floa
 // The larger of two magnitudes; a NaN may be passed over, as it reaches the products by itself.
 __device__ __forceinline__ float larger(float m, float v) { return __builtin_fmaxf(m, __builtin_fabsf(v)); }
 __device__ __forceinline__ float larger(float m, const Float4& v) { return larger(larger(larger(larger(m, v[0]), v[1]), v[2]), v[3]); }
-// Over the four lanes of a column, lane, lane ^ 16, ^ 32 and ^ 48.
+// Over the four lanes of a column, lane, lane ^ 16, ^ 32 and ^ 48: the instructions swap halves of two registers, of the wave or of its pairs of rows
+// of 16 lanes, which lie two wait states behind the write of either.  (The builtins' second result is the first one's copy in this compiler.)
 __device__ __forceinline__ float over_column(float m)
 {
-    m = __builtin_fmaxf(m, __shfl_xor(m, 16));
-    return __builtin_fmaxf(m, __shfl_xor(m, 32));
+    float a = m, b = m;
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(a), "+v"(b));
+    a = b = __builtin_fmaxf(a, b);
+    asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(a), "+v"(b));
+    return __builtin_fmaxf(a, b);
 }
 
 // What row r of result tile m stands for.
@@ -138,6 +142,8 @@ int check_delta_rows(const Args& a, const ssam_sequences& q)
     if (int e = check_rows(a.q, q, heads_width(a.key_heads, a.q_head, a.key_dim), esz, false)) return e;
     if (int e = check_rows(a.k, q, heads_width(a.key_heads, a.k_head, a.key_dim), esz, false)) return e;
     if (int e = check_rows(a.v, q, heads_width(a.heads, a.v_head, a.value_dim), esz, false)) return e;
+    for (const ssam_rows* r : {&a.q, &a.k, &a.v, &a.g, &a.beta})
+        if (int e = check_tile_rows(*r, q)) return e;
     if (int e = check_rows(a.g, q, a.heads, 4, true)) return e;
     return check_rows(a.beta, q, a.heads, 4, false);
 }
@@ -145,6 +151,7 @@ int check_delta_rows(const Args& a, const ssam_sequences& q)
 inline int check_out_heads(const ssam_rows& r, const ssam_sequences& q, int heads, long long apart, int dim, int esz, bool optional)
 {
     if (apart < 0 || apart > kMaxStride || (r.d && heads > 1 && apart < dim)) return SSAM_ERR_DIM;
+    if (int e = check_tile_rows(r, q)) return e;
     return check_out_rows(r, q, heads_width(heads, apart, dim), esz, optional);
 }
 

@@ -16,12 +16,13 @@ __global__ __launch_bounds__(kBlock) void delta_prepare(DeltaParams p)
 }
 
 // One wave: 16 NT columns of a head's state, from its sequence's first block to the last.  The operands made from q, k and the block's matrices
-// are in LDS, the same for the block's four waves.
+// are in LDS, the same for the block's four waves; the next block's are on their way in registers.
 template <class T, int KT, int NT>
 __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
 {
     __shared__ WalkRoom<T, KT> room;
-    constexpr bool kOnePlace = WalkRoom<T, KT>::kOnePlace;
+    typedef Stage<T, KT, false> S;
+    constexpr int kParts = kSplit<T> ? 2 : 1;       // of q and k
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, g = lane >> 4, r16 = lane & 15;
     const int tile = (int)(blockIdx.x % p.tiles), head = (int)(blockIdx.x / p.tiles % p.heads), seq = (int)(blockIdx.x / p.tiles / p.heads);
     const int key_head = head / (p.heads / p.key_heads);
@@ -29,131 +30,158 @@ __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
     span_of(p.pieces, seq, first, len);
     const int blocks = (len + kDeltaRows - 1) / kDeltaRows;
     const long long slot0 = p.pieces.begin ? first_slot(p.pieces, seq) : (long long)seq * p.pieces.per;
-    const int c0 = (tile * kWavesPerBlock + wave) * 16 * NT + r16;       // the lane's column of the first tile
+    const int c0 = (tile * kWavesPerBlock + wave) * 16 * NT + r16, left = p.value_dim - c0;      // the lane's first column; columns from there on
     const Piece whole{seq, first, len, 0, len};
-    const T* const qs = sequence_base<const T>(p.q, p.pieces, whole) + key_head * p.q_head;
-    const T* const ks = sequence_base<const T>(p.k, p.pieces, whole) + key_head * p.k_head;
-    const T* const vs = sequence_base<const T>(p.v, p.pieces, whole) + head * p.v_head + c0;
-    T* const os = sequence_base<T>(p.out, p.pieces, whole) + head * p.out_head + c0;
+    const T* qs = sequence_base<const T>(p.q, p.pieces, whole) + key_head * p.q_head;
+    const T* ks = sequence_base<const T>(p.k, p.pieces, whole) + key_head * p.k_head;
+    const T* vs = sequence_base<const T>(p.v, p.pieces, whole) + head * p.v_head + c0;
+    T* os = sequence_base<T>(p.out, p.pieces, whole) + head * p.out_head + c0;
     const long long state_at = ((long long)seq * p.heads + head) * p.key_dim * p.value_dim + c0;
+    const unsigned kstride = (unsigned)p.k.row, qstride = (unsigned)p.q.row, vstride = (unsigned)p.v.row, ostride = (unsigned)p.out.row;
+    const Block* from = p.blocks + slot0 * p.heads + head;
 
     Float4 s[2 * KT][NT];
+    if (p.state) {
+        load_state<KT, NT>(p.state + state_at, p.value_dim, p.key_dim, left, s);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 2 * KT; ++j)
+        for (int j = 0; j < 2 * KT; ++j)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int d = tile_row(j, 4 * g + i);
-                s[j][n][i] = p.state && d < p.key_dim && c0 + 16 * n < p.value_dim ? p.state[state_at + (long long)d * p.value_dim + 16 * n] : 0.0f;
-            }
+            for (int n = 0; n < NT; ++n) s[j][n] = Float4(0.0f);
+    }
+    S stage;
+    Columns<T, NT> v;
+    int rows = len < kDeltaRows ? len : kDeltaRows;
+    if (blocks > 0) {
+        stage.load(*from, ks, kstride, qs, qstride, rows, p.key_dim);
+        v.load(vs, vstride, rows, left);
+    }
     for (int c = 0; c < blocks; ++c) {
-        const int row0 = c * kDeltaRows, rows = len - row0 < kDeltaRows ? len - row0 : kDeltaRows;
-        const long long slot = slot0 + c;
         __syncthreads();
-        const Block& from = p.blocks[slot * p.heads + head];
-        stage_rows<T, KT, true, !kOnePlace, false>(room, from.f, ks, p.k.row, qs, p.q.row, row0, rows, p.key_dim);
-        stage_block(room.m, from);
-        float* const mark = p.marks ? mark_of(p.marks, p, slot, head) + c0 : nullptr;
-        if (mark)
-#pragma unroll
-            for (int j = 0; j < 2 * KT; ++j)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int d = tile_row(j, 4 * g + i);
-                        if (d < p.key_dim && c0 + 16 * n < p.value_dim) mark[(long long)d * p.value_dim + 16 * n] = s[j][n][i];
-                    }
+        stage.put(room, *from, ks, kstride, qs, qstride, rows, p.key_dim);
+        float* const mark = p.marks ? mark_of(p.marks, p, slot0 + c, head) + c0 : nullptr;
+        if (mark) store_state<KT, NT>(mark, p.value_dim, p.key_dim, left, s);
+        Float4 x[4][NT], o[4][NT];
+        v.values(rows, x);
         __syncthreads();
+        const T *const this_ks = ks, *const this_qs = qs;
+        const Block* const this_from = from;
+        const int this_rows = rows;
+        if (c + 1 < blocks) {
+            ks += (long long)kDeltaRows * p.k.row;
+            qs += (long long)kDeltaRows * p.q.row;
+            vs += (long long)kDeltaRows * p.v.row;
+            from += p.heads;
+            rows = len - (c + 1) * kDeltaRows;
+            rows = rows < kDeltaRows ? rows : kDeltaRows;
+            stage.load(*from, ks, kstride, qs, qstride, rows, p.key_dim);
+            v.load(vs, vstride, rows, left);
+        }
 
         // X = V - exp(G) K S and Q S
-        Float4 x[4][NT], o[4][NT];
         float back_s[NT];
         {
             HalfPair f[KT][NT];
+            Half8 key[2][kParts][KT], query[2][kParts][KT];
+            read_rows<KT, kParts>(room.keys, 0, lane, key[0]);
+            read_rows<KT, kParts>(S::kOnePlace ? room.keys : room.queries(), S::kOnePlace ? 1 : 0, lane, query[0]);
             split_state<KT, NT>(s, f, back_s);
+            if constexpr (S::kOnePlace) {
+                products<KT, NT, kParts>(key[0], query[0], f, o[0], o[1]);
+                read_rows<KT, kParts>(room.keys, 2, lane, key[0]);
+                read_rows<KT, kParts>(room.keys, 3, lane, query[0]);
+                products<KT, NT, kParts>(key[0], query[0], f, o[2], o[3]);
+            }
 #pragma unroll
             for (int m = 0; m < 4; ++m) {
                 Float4 a[NT];
-                rows_product<KT, NT>(room.keys, m, lane, f, a);
-                const int t0 = tile_row(m, 4 * g);
-                const Float4 reads = *reinterpret_cast<const Float4*>(&room.m.f.reads[t0]);
+                if constexpr (S::kOnePlace) {
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float v = t0 + i < rows && c0 + 16 * n < p.value_dim ? (float)vs[(long long)(row0 + t0 + i) * p.v.row + 16 * n] : 0.0f;
-                        x[m][n][i] = v - reads[i] * (a[n][i] * back_s[n]);
+                    for (int n = 0; n < NT; ++n) a[n] = o[m][n];
+                } else {
+                    if (m < 3) {
+                        read_rows<KT, kParts>(room.keys, m + 1, lane, key[(m + 1) & 1]);
+                        read_rows<KT, kParts>(room.queries(), m + 1, lane, query[(m + 1) & 1]);
                     }
-            }
-            if constexpr (kOnePlace) {
-                __syncthreads();
-                stage_rows<T, KT, false, true, false>(room, from.f, ks, p.k.row, qs, p.q.row, row0, rows, p.key_dim);
-                __syncthreads();
-            }
+                    in_order();
+                    products<KT, NT, kParts>(key[m & 1], query[m & 1], f, a, o[m]);
+                }
+                const Float4 reads = *reinterpret_cast<const Float4*>(&room.m.f.reads[tile_row(m, 4 * g)]);
 #pragma unroll
-            for (int m = 0; m < 4; ++m) rows_product<KT, NT>(room.queries(), m, lane, f, o[m]);
+                for (int n = 0; n < NT; ++n) x[m][n] -= reads * (a[n] * back_s[n]);
+            }
+            if constexpr (S::kOnePlace) {
+                __syncthreads();
+                S::put_now(room, *this_from, this_ks, kstride, this_qs, qstride, this_rows, p.key_dim, S::kSquares, 2 * S::kSquares);
+                __syncthreads();
+#pragma unroll
+                for (int m = 0; m < 4; m += 2) {
+                    read_rows<KT, kParts>(room.queries(), m, lane, key[0]);
+                    read_rows<KT, kParts>(room.queries(), m + 1, lane, query[0]);
+                    products<KT, NT, kParts>(key[0], query[0], f, o[m], o[m + 1]);
+                }
+            }
         }
         // R = (I + A diag(b))^-1 X;  x becomes U = b R
         float back_u[NT];
         HalfPair f[2][NT];
         split_rows<NT>(x, f, back_u);
+        tri_products<NT, false>(room.m.solve, lane, f, x);
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            lower_product<NT>(room.m.solve, m, lane, f, x[m]);
-            const int t0 = tile_row(m, 4 * g);
-            const Float4 beta = *reinterpret_cast<const Float4*>(&room.m.f.beta[t0]);
+            const Float4 beta = *reinterpret_cast<const Float4*>(&room.m.f.beta[tile_row(m, 4 * g)]);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                x[m][n] *= back_u[n] * room.m.f.solve_back;
-                if (mark && c0 + 16 * n < p.value_dim)
+            for (int n = 0; n < NT; ++n) x[m][n] *= back_u[n] * room.m.f.solve_back;
+            if (mark) store_tile<NT>(mark + (long long)p.key_dim * p.value_dim, p.value_dim, left, m, x[m]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) mark[(long long)(p.key_dim + t0 + i) * p.value_dim + 16 * n] = x[m][n][i];
-                x[m][n] *= beta;
-            }
+            for (int n = 0; n < NT; ++n) x[m][n] *= beta;
         }
         // O = scale (exp(G) Q S + (Q K^T o D) U)
         split_rows<NT>(x, f, back_u);
+        {
+            Float4 a[4][NT];
+            tri_products<NT, false>(room.m.mix, lane, f, a);
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            Float4 a[NT];
-            lower_product<NT>(room.m.mix, m, lane, f, a);
-            const int t0 = tile_row(m, 4 * g);
-            const Float4 asks = *reinterpret_cast<const Float4*>(&room.m.f.asks[t0]);
-            const Float4 writes = *reinterpret_cast<const Float4*>(&room.m.f.writes[t0]);
+            for (int m = 0; m < 4; ++m) {
+                const Float4 asks = *reinterpret_cast<const Float4*>(&room.m.f.asks[tile_row(m, 4 * g)]);
+                const Float4 writes = *reinterpret_cast<const Float4*>(&room.m.f.writes[tile_row(m, 4 * g)]);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
+                for (int n = 0; n < NT; ++n) {
+                    a[m][n] = a[m][n] * (back_u[n] * room.m.f.mix_back) + asks * (o[m][n] * back_s[n]);
+                    x[m][n] *= writes;
+                }
+            }
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (t0 + i < rows && c0 + 16 * n < p.value_dim)
-                        os[(long long)(row0 + t0 + i) * p.out.row + 16 * n] = (T)__builtin_fmaf(a[n][i], back_u[n] * room.m.f.mix_back, asks[i] * (o[m][n][i] * back_s[n]));
-                x[m][n] *= writes;
+            for (int m = 0; m < 4; ++m) store_columns<T, NT>(os, ostride, this_rows, left, m, a[m]);
+        }
+        os += (long long)kDeltaRows * p.out.row;
+        // S = exp(G_C) S + (exp(G_C - G) K)^T U
+        {
+            Half8 key[2][2][kParts][2];
+            read_turned<KT, kParts>(room.turned_keys, 0, lane, key[0][0]);
+            read_turned<KT, kParts>(room.turned_keys, 1, lane, key[0][1]);
+            split_rows<NT>(x, f, back_u);
+            const float total = room.m.f.total;
+#pragma unroll
+            for (int j = 0; j < 2 * KT; j += 2) {
+                const int now = j >> 1 & 1;
+                if (j + 2 < 2 * KT) {
+                    read_turned<KT, kParts>(room.turned_keys, j + 2, lane, key[now ^ 1][0]);
+                    read_turned<KT, kParts>(room.turned_keys, j + 3, lane, key[now ^ 1][1]);
+                }
+                in_order();
+                Float4 a[2][NT];
+                products<2, NT, kParts>(key[now][0], key[now][1], f, a[0], a[1]);
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s[j + k][n][i] = __builtin_fmaf(total, s[j + k][n][i], a[k][n][i] * back_u[n]);
             }
         }
-        // S = exp(G_C) S + (exp(G_C - G) K)^T U
-        split_rows<NT>(x, f, back_u);
-        const float total = room.m.f.total;
-#pragma unroll
-        for (int j = 0; j < 2 * KT; ++j) {
-            Float4 a[NT];
-            turned_product<KT, NT>(room.turned_keys, j, lane, f, a);
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[j][n][i] = __builtin_fmaf(total, s[j][n][i], a[n][i] * back_u[n]);
-        }
     }
-    if (p.final)
-#pragma unroll
-        for (int j = 0; j < 2 * KT; ++j)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int d = tile_row(j, 4 * g + i);
-                    if (d < p.key_dim && c0 + 16 * n < p.value_dim) p.final[state_at + (long long)d * p.value_dim + 16 * n] = s[j][n][i];
-                }
+    if (p.final) store_state<KT, NT>(p.final + state_at, p.value_dim, p.key_dim, left, s);
 }
 
 }  // namespace

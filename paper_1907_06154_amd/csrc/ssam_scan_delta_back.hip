@@ -36,7 +36,8 @@ __global__ __launch_bounds__(kBlock) void delta_back_walk(DeltaBackParams b)
 {
     const DeltaParams& p = b.f;
     __shared__ WalkRoom<T, KT> room;
-    constexpr bool kOnePlace = WalkRoom<T, KT>::kOnePlace;
+    typedef Stage<T, KT, true> S;
+    constexpr int kParts = kSplit<T> ? 2 : 1;       // of q and k
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, g = lane >> 4, r16 = lane & 15;
     const int tile = (int)(blockIdx.x % p.tiles), head = (int)(blockIdx.x / p.tiles % p.heads), seq = (int)(blockIdx.x / p.tiles / p.heads);
     const int key_head = head / (p.heads / p.key_heads);
@@ -46,126 +47,141 @@ __global__ __launch_bounds__(kBlock) void delta_back_walk(DeltaBackParams b)
     const long long slot0 = p.pieces.begin ? first_slot(p.pieces, seq) : (long long)seq * p.pieces.per;
     const int c0 = (tile * kWavesPerBlock + wave) * 16 * NT + r16;
     const Piece whole{seq, first, len, 0, len};
-    const T* const qs = sequence_base<const T>(p.q, p.pieces, whole) + key_head * p.q_head;
-    const T* const ks = sequence_base<const T>(p.k, p.pieces, whole) + key_head * p.k_head;
-    const T* const dos = sequence_base<const T>(b.grad_out, p.pieces, whole) + head * b.grad_out_head + c0;
-    T* const dvs = b.grad_v.d ? sequence_base<T>(b.grad_v, p.pieces, whole) + head * b.grad_v_head + c0 : nullptr;
+    const int left = p.value_dim - c0;
+    const long long end = (long long)(blocks - 1) * kDeltaRows;                                  // first row of the last block
+    const T* qs = sequence_base<const T>(p.q, p.pieces, whole) + key_head * p.q_head + end * p.q.row;
+    const T* ks = sequence_base<const T>(p.k, p.pieces, whole) + key_head * p.k_head + end * p.k.row;
+    const T* dos = sequence_base<const T>(b.grad_out, p.pieces, whole) + head * b.grad_out_head + c0 + end * b.grad_out.row;
+    T* dvs = b.grad_v.d ? sequence_base<T>(b.grad_v, p.pieces, whole) + head * b.grad_v_head + c0 + end * b.grad_v.row : nullptr;
     const long long state_at = ((long long)seq * p.heads + head) * p.key_dim * p.value_dim + c0;
+    const unsigned kstride = (unsigned)p.k.row, qstride = (unsigned)p.q.row, ostride = (unsigned)b.grad_out.row, vstride = (unsigned)b.grad_v.row;
+    const Block* from = p.blocks + (slot0 + blocks - 1) * p.heads + head;
 
     Float4 s[2 * KT][NT];
-#pragma unroll
-    for (int j = 0; j < 2 * KT; ++j)
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int d = tile_row(j, 4 * g + i);
-                s[j][n][i] = p.state && d < p.key_dim && c0 + 16 * n < p.value_dim ? p.state[state_at + (long long)d * p.value_dim + 16 * n] : 0.0f;
-            }
-    for (int c = blocks - 1; c >= 0; --c) {
-        const int row0 = c * kDeltaRows, rows = len - row0 < kDeltaRows ? len - row0 : kDeltaRows;
-        const long long slot = slot0 + c;
-        __syncthreads();
-        const Block& from = p.blocks[slot * p.heads + head];
-        stage_rows<T, KT, true, !kOnePlace, true>(room, from.f, ks, p.k.row, qs, p.q.row, row0, rows, p.key_dim);
-        stage_block(room.m, from);
-        float* const behind = mark_of(b.behind, p, slot, head) + c0;
+    if (p.state) {
+        load_state<KT, NT>(p.state + state_at, p.value_dim, p.key_dim, left, s);
+    } else {
 #pragma unroll
         for (int j = 0; j < 2 * KT; ++j)
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int d = tile_row(j, 4 * g + i);
-                    if (d < p.key_dim && c0 + 16 * n < p.value_dim) behind[(long long)d * p.value_dim + 16 * n] = s[j][n][i];
-                }
-        Float4 o[4][NT], x[4][NT];       // dO; dU, dY, dX
-#pragma unroll
-        for (int m = 0; m < 4; ++m)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int t = tile_row(m, 4 * g + i);
-                    o[m][n][i] = t < rows && c0 + 16 * n < p.value_dim ? (float)dos[(long long)(row0 + t) * b.grad_out.row + 16 * n] : 0.0f;
-                }
+            for (int n = 0; n < NT; ++n) s[j][n] = Float4(0.0f);
+    }
+    S stage;
+    Columns<T, NT> v;
+    int rows = len - (blocks - 1) * kDeltaRows;
+    if (blocks > 0) {
+        stage.load(*from, ks, kstride, qs, qstride, rows, p.key_dim);
+        v.load(dos, ostride, rows, left);
+    }
+    for (int c = blocks - 1; c >= 0; --c) {
         __syncthreads();
+        stage.put(room, *from, ks, kstride, qs, qstride, rows, p.key_dim);
+        float* const behind = mark_of(b.behind, p, slot0 + c, head) + c0;
+        store_state<KT, NT>(behind, p.value_dim, p.key_dim, left, s);
+        Float4 o[4][NT], x[4][NT];       // dO; dU, dY, dX
+        v.values(rows, o);
+        __syncthreads();
+        const T *const this_ks = ks, *const this_qs = qs;
+        const Block* const this_from = from;
+        const int this_rows = rows;
+        if (c > 0) {
+            ks -= (long long)kDeltaRows * p.k.row;
+            qs -= (long long)kDeltaRows * p.q.row;
+            dos -= (long long)kDeltaRows * b.grad_out.row;
+            from -= p.heads;
+            rows = kDeltaRows;
+            stage.load(*from, ks, kstride, qs, qstride, rows, p.key_dim);
+            v.load(dos, ostride, rows, left);
+        }
         {
             HalfPair f[KT][NT];
             float back[NT];
+            Half8 key[2][2][kParts][KT];
+            read_rows<KT, kParts>(room.keys, 0, lane, key[0][0]);
+            read_rows<KT, kParts>(room.keys, 1, lane, key[0][1]);
             split_state<KT, NT>(s, f, back);
 #pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                rows_product<KT, NT>(room.keys, m, lane, f, x[m]);
-                const Float4 writes = *reinterpret_cast<const Float4*>(&room.m.f.writes[tile_row(m, 4 * g)]);
+            for (int m = 0; m < 4; m += 2) {
+                if (m == 0 && !S::kOnePlace) {
+                    read_rows<KT, kParts>(room.keys, 2, lane, key[1][0]);
+                    read_rows<KT, kParts>(room.keys, 3, lane, key[1][1]);
+                }
+                in_order();
+                if (m == 2 && S::kOnePlace) {       // (pairs of long keys: no registers for two steps)
+                    read_rows<KT, kParts>(room.keys, 2, lane, key[0][0]);
+                    read_rows<KT, kParts>(room.keys, 3, lane, key[0][1]);
+                }
+                const int now = S::kOnePlace ? 0 : m >> 1;
+                products<KT, NT, kParts>(key[now][0], key[now][1], f, x[m], x[m + 1]);
 #pragma unroll
-                for (int n = 0; n < NT; ++n) x[m][n] *= writes * back[n];
+                for (int k = 0; k < 2; ++k) {
+                    const Float4 writes = *reinterpret_cast<const Float4*>(&room.m.f.writes[tile_row(m + k, 4 * g)]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) x[m + k][n] *= writes * back[n];
+                }
             }
         }
-        if constexpr (kOnePlace) {
+        if constexpr (S::kOnePlace) {
             __syncthreads();
-            stage_rows<T, KT, false, true, true>(room, from.f, ks, p.k.row, qs, p.q.row, row0, rows, p.key_dim);
+            S::put_now(room, *this_from, this_ks, kstride, this_qs, qstride, this_rows, p.key_dim, S::kSquares, 2 * S::kSquares);
             __syncthreads();
         }
         HalfPair f[2][NT];
         float back[NT];
         split_rows<NT>(o, f, back);
+        {
+            Float4 a[4][NT];
+            tri_products<NT, true>(room.m.mix, lane, f, a);
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            Float4 a[NT];
-            upper_product<NT>(room.m.mix, m, lane, f, a);
+            for (int m = 0; m < 4; ++m)
 #pragma unroll
-            for (int n = 0; n < NT; ++n) x[m][n] += a[n] * (back[n] * room.m.f.mix_back);
+                for (int n = 0; n < NT; ++n) x[m][n] += a[m][n] * (back[n] * room.m.f.mix_back);
         }
         split_rows<NT>(x, f, back);
+        tri_products<NT, true>(room.m.solve, lane, f, x);
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            upper_product<NT>(room.m.solve, m, lane, f, x[m]);
             const int t0 = tile_row(m, 4 * g);
             const Float4 beta = *reinterpret_cast<const Float4*>(&room.m.f.beta[t0]), reads = *reinterpret_cast<const Float4*>(&room.m.f.reads[t0]),
                          asks = *reinterpret_cast<const Float4*>(&room.m.f.asks[t0]);
 #pragma unroll
+            for (int n = 0; n < NT; ++n) x[m][n] *= back[n] * room.m.f.solve_back;
+            store_tile<NT>(behind + (long long)p.key_dim * p.value_dim, p.value_dim, left, m, x[m]);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) x[m][n] *= beta;
+            if (dvs) store_columns<T, NT>(dvs, vstride, this_rows, left, m, x[m]);
+#pragma unroll
             for (int n = 0; n < NT; ++n) {
-                x[m][n] *= back[n] * room.m.f.solve_back;
-                const bool there = c0 + 16 * n < p.value_dim;
-                if (there)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) behind[(long long)(p.key_dim + t0 + i) * p.value_dim + 16 * n] = x[m][n][i];
-                x[m][n] *= beta;
-                if (dvs && there)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (t0 + i < rows) dvs[(long long)(row0 + t0 + i) * b.grad_v.row + 16 * n] = (T)x[m][n][i];
                 x[m][n] *= -reads;
                 o[m][n] *= asks;
             }
         }
+        if (dvs) dvs -= (long long)kDeltaRows * b.grad_v.row;
         HalfPair fo[2][NT];
         float back_o[NT];
+        Half8 key[2][kParts][2], query[2][kParts][2];
+        read_turned<KT, kParts>(room.turned_keys, 0, lane, key[0]);
+        read_turned<KT, kParts>(room.queries(), 0, lane, query[0]);
         split_rows<NT>(x, f, back);
         split_rows<NT>(o, fo, back_o);
         const float total = room.m.f.total;
 #pragma unroll
         for (int j = 0; j < 2 * KT; ++j) {
+            const int now = j & 1;
+            if (j + 1 < 2 * KT) {
+                read_turned<KT, kParts>(room.turned_keys, j + 1, lane, key[now ^ 1]);
+                read_turned<KT, kParts>(room.queries(), j + 1, lane, query[now ^ 1]);
+            }
+            in_order();
             Float4 a[NT], q[NT];
-            turned_product<KT, NT>(room.turned_keys, j, lane, f, a);
-            turned_product<KT, NT>(room.queries(), j, lane, fo, q);
+            products_of<2, NT, kParts>(key[now], f, query[now], fo, a, q);
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[j][n][i] = __builtin_fmaf(total, s[j][n][i], __builtin_fmaf(a[n][i], back[n], q[n][i] * back_o[n]));
         }
     }
-    if (b.grad_state)
-#pragma unroll
-        for (int j = 0; j < 2 * KT; ++j)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int d = tile_row(j, 4 * g + i);
-                    if (d < p.key_dim && c0 + 16 * n < p.value_dim) b.grad_state[state_at + (long long)d * p.value_dim + 16 * n] = s[j][n][i];
-                }
+    if (b.grad_state) store_state<KT, NT>(b.grad_state + state_at, p.value_dim, p.key_dim, left, s);
 }
 
 // ---- gradients of q, k, g and beta ----------------------------------------------------------------------------------------
@@ -239,8 +255,13 @@ __global__ __launch_bounds__(kBlock) void delta_back_rows(DeltaBackParams b)
     if (piece.seq < 0 || piece.n <= 0) return;
     const T* const ks = sequence_base<const T>(p.k, p.pieces, piece) + piece.row0 * p.k.row + key_head * p.k_head;
     const T* const qs = sequence_base<const T>(p.q, p.pieces, piece) + piece.row0 * p.q.row + key_head * p.q_head;
-    load_rows<T, KT>(ks, p.k.row, piece.n, p.key_dim, p.unit, room.keys, room.key_back, room.key);
-    load_rows<T, KT>(qs, p.q.row, piece.n, p.key_dim, p.unit, room.queries, room.query_back, room.query);
+    {
+        RowLoad<T, KT> k, q;
+        k.load(ks, (unsigned)p.k.row, piece.n, p.key_dim);
+        q.load(qs, (unsigned)p.q.row, piece.n, p.key_dim);
+        k.put(p.unit, piece.n, p.key_dim, room.keys, room.key_back, room.key);
+        q.put(p.unit, piece.n, p.key_dim, room.queries, room.query_back, room.query);
+    }
     __syncthreads();
     Float4 kk[4], qk[4];                      // K K^T and Q K^T, tile w's rows in wave w
     key_products<T, KT, true>(room.keys, room.queries, kk, qk);
@@ -535,7 +556,8 @@ __global__ __launch_bounds__(kBlock) void delta_back_rows(DeltaBackParams b)
             for (int job = tid; job < 32 * KT; job += kBlock) {
                 const int sq = job / (4 * KT), e = job % (4 * KT);
                 RowVec<T, 8> v[8];
-                load_square(query ? qs : ks, query ? p.q.row : p.k.row, 0, piece.n, p.key_dim, sq, e, v);
+                load_square<T>(query ? qs : ks, (unsigned)(query ? p.q.row : p.k.row), piece.n, p.key_dim, sq, e, v);
+                clear_eights<T, 8>(8 * sq, 1, piece.n, e, p.key_dim, v);
                 Half8 hi[8], lo[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) to_halves<T>(v[i], __is_same(T, _Float16) ? 1.0f : (query ? room.query : room.key)[8 * sq + i], hi[i], lo[i]);
@@ -556,14 +578,14 @@ __global__ __launch_bounds__(kBlock) void delta_back_rows(DeltaBackParams b)
                 for (int m = 0; m < 4; ++m) {
                     Float4 a[1];
                     if (!query) {
-                        lower_product<1>(room.tri[0], m, lane, f, a);
+                        tri_product<1, false>(room.tri[0], m, lane, f, a);
                         asked[m][jj] += a[0] * back[0];
-                        lower_product<1>(room.tri[1], m, lane, f, a);
+                        tri_product<1, false>(room.tri[1], m, lane, f, a);
                         reads[m][jj] += a[0] * back[1];
-                        upper_product<1>(room.tri[3], m, lane, f, a);
+                        tri_product<1, true>(room.tri[3], m, lane, f, a);
                         last[m][jj] += a[0] * back[3];
                     } else {
-                        upper_product<1>(room.tri[2], m, lane, f, a);
+                        tri_product<1, true>(room.tri[2], m, lane, f, a);
                         last[m][jj] += a[0] * back[2];
                     }
                 }
@@ -663,6 +685,8 @@ int ssam_scan_delta_backward(const ssam_scan_delta_backward_args* a, void* hip_s
     if (int e = check_delta_rows(*a, a->seq)) return e;
     const long long keys = (long long)a->key_heads * a->key_dim, values = (long long)a->heads * a->value_dim;
     if (a->grad_out_head < 0 || a->grad_out_head > kMaxStride) return SSAM_ERR_DIM;
+    for (const ssam_rows* r : {&a->grad_out, &a->grad_q, &a->grad_k, &a->grad_v})
+        if (int e = check_tile_rows(*r, a->seq)) return e;
     if (int e = check_rows(a->grad_out, a->seq, heads_width(a->heads, a->grad_out_head, a->value_dim), esz, false)) return e;
     for (const ssam_rows* r : {&a->grad_q, &a->grad_k})
         if (int e = check_out_rows(*r, a->seq, keys, esz, true)) return e;

@@ -58,14 +58,145 @@ template <int KT> __device__ __forceinline__ Half8 turned_of(const Half8 (&a)[4 
     return a[turned_operand(j, k)][turned_entry(j, lane >> 4, lane & 15)];
 }
 
-// 8 rows x 8 elements, rows 8 b .. and elements 8 e .., zeros outside.
-template <class T>
-__device__ __forceinline__ void load_square(const T* __restrict__ base, long long stride, int row0, int rows, int dim, int b, int e, RowVec<T, 8> (&v)[8])
+// N rows of eight elements, rows row0, row0 + step .. and elements from 8 e on; rows >= 1.  There are no branches on what is there: a load that waits for
+// its turn in one costs its latency by itself.  clear_eights() makes zeros of what was not there, where the values are used.
+template <class T, int N>
+__device__ __forceinline__ void load_eights(const T* __restrict__ base, unsigned stride, int row0, int step, int rows, int e, int dim, RowVec<T, 8> (&v)[N])
 {
-    const int have = dim - 8 * e;
+    const bool across = 8 * e < dim;
+    base += across ? 8 * e : 0;
+    if (dim % 8 == 0) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        v[i] = 8 * b + i < rows && have > 0 ? load_row_vec<T, 8>(base + (long long)(row0 + 8 * b + i) * stride + 8 * e, have) : RowVec<T, 8>(T(0));
+        for (int i = 0; i < N; ++i) {
+            const int row = row0 + i * step;
+            __builtin_memcpy(&v[i], base + (unsigned)(row < rows ? row : rows - 1) * stride, sizeof(v[i]));
+        }
+    } else {
+        const int have = across ? dim - 8 * e : dim;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int row = row0 + i * step;
+            v[i] = load_row_vec<T, 8>(base + (unsigned)(row < rows ? row : rows - 1) * stride, have);
+        }
+    }
+}
+template <class T, int N>
+__device__ __forceinline__ void clear_eights(int row0, int step, int rows, int e, int dim, RowVec<T, 8> (&v)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        if (!(8 * e < dim && row0 + i * step < rows)) v[i] = RowVec<T, 8>(T(0));
+}
+// 8 rows x 8 elements, rows 8 b .. and elements 8 e ..
+template <class T>
+__device__ __forceinline__ void load_square(const T* __restrict__ base, unsigned stride, int rows, int dim, int b, int e, RowVec<T, 8> (&v)[8])
+{
+    load_eights<T, 8>(base, stride, 8 * b, 1, rows, e, dim, v);
+}
+
+// An element on its way in a register of its own: two of them packed into one would have to be waited for in turn.
+template <class T> struct Raw {
+    unsigned bits;
+    __device__ __forceinline__ void load(const T* p) { bits = *reinterpret_cast<const unsigned short*>(p); }
+    __device__ __forceinline__ float value() const { return (float)__builtin_bit_cast(T, (unsigned short)bits); }
+};
+template <> struct Raw<float> {
+    float bits;
+    __device__ __forceinline__ void load(const float* p) { bits = *p; }
+    __device__ __forceinline__ float value() const { return bits; }
+};
+
+// A wave's columns of 64 rows, as result tiles (tile_row); `base`: the rows' first, the lane's first column; `left`: columns from there on.  Rows that are not
+// there are the last one's copies until values() takes them.
+template <class T, int NT>
+struct Columns {
+    Raw<T> v[4][NT][4];
+
+    __device__ __forceinline__ void load(const T* __restrict__ base, unsigned stride, int rows, int left)
+    {
+        const int g = (threadIdx.x & (kWave - 1)) >> 4;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const T* const at = base + (left > 16 * n ? 16 * n : left > 0 ? 0 : left - 1);      // (columns that are not there are the last one's copies)
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int t = tile_row(m, 4 * g + i);
+                    v[m][n][i].load(at + (unsigned)(t < rows ? t : rows - 1) * stride);
+                }
+        }
+    }
+    __device__ __forceinline__ void values(int rows, Float4 (&x)[4][NT]) const
+    {
+        const int g = (threadIdx.x & (kWave - 1)) >> 4;
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[m][n][i] = tile_row(m, 4 * g + i) < rows ? v[m][n][i].value() : 0.0f;
+    }
+};
+template <class T, int NT>
+__device__ __forceinline__ void store_columns(T* __restrict__ base, unsigned stride, int rows, int left, int m, const Float4 (&v)[NT])
+{
+    const int g = (threadIdx.x & (kWave - 1)) >> 4;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        if (left <= 16 * n) continue;
+        T* const at = base + 16 * n;
+        const unsigned lane_at = 8u * g * stride;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (rows == kDeltaRows || tile_row(m, 4 * g + i) < rows) at[lane_at + (unsigned)tile_row(m, i) * stride] = (T)v[n][i];
+    }
+}
+
+// A wave's columns of a matrix [32 KT rows, of which `dim`] of floats.
+template <int KT, int NT>
+__device__ __forceinline__ void load_state(const float* __restrict__ base, unsigned stride, int dim, int left, Float4 (&s)[2 * KT][NT])
+{
+    const int g = (threadIdx.x & (kWave - 1)) >> 4;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const float* const at = base + (left > 16 * n ? 16 * n : left > 0 ? 0 : left - 1);
+#pragma unroll
+        for (int j = 0; j < 2 * KT; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int d = tile_row(j, 4 * g + i);
+                const float x = at[(unsigned)(d < dim ? d : dim - 1) * stride];
+                s[j][n][i] = d < dim ? x : 0.0f;
+            }
+    }
+}
+template <int KT, int NT>
+__device__ __forceinline__ void store_state(float* __restrict__ base, unsigned stride, int dim, int left, const Float4 (&s)[2 * KT][NT])
+{
+    const int g = (threadIdx.x & (kWave - 1)) >> 4;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        if (left <= 16 * n) continue;
+#pragma unroll
+        for (int j = 0; j < 2 * KT; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int d = tile_row(j, 4 * g + i);
+                if (dim == 32 * KT || d < dim) base[(unsigned)d * stride + 16 * n] = s[j][n][i];
+            }
+    }
+}
+// 64 rows of floats, all of them.
+template <int NT>
+__device__ __forceinline__ void store_tile(float* __restrict__ base, unsigned stride, int left, int m, const Float4 (&v)[NT])
+{
+    const int g = (threadIdx.x & (kWave - 1)) >> 4;
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+        if (left > 16 * n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) base[(unsigned)tile_row(m, 4 * g + i) * stride + 16 * n] = v[n][i];
 }
 
 template <class T, int KT, int kParts>
@@ -95,111 +226,177 @@ __device__ __forceinline__ void put_turned(const Half8 (&hi)[8], const Half8 (&l
     }
 }
 
-// The rows of a block as operands: k's in both forms, q's as rows (kTurn: turned).  kKeys, kQueries: which of them.
-template <class T, int KT, bool kKeys, bool kQueries, bool kTurn>
-__device__ __forceinline__ void stage_rows(WalkRoom<T, KT>& room, const BlockFactors& f, const T* __restrict__ ks, long long kstride, const T* __restrict__ qs,
-                                           long long qstride, int row0, int rows, int dim)
-{
-    constexpr int kAcross = 4 * KT, kSquares = 8 * kAcross;      // squares of 8 x 8 in a block's keys
-    for (int job = threadIdx.x; job < (kKeys && kQueries ? 2 : 1) * kSquares; job += kBlock) {
-        const bool query = kKeys && kQueries ? job >= kSquares : kQueries;
-        const int b = (job % kSquares) / kAcross, e = job % kAcross;
-        RowVec<T, 8> v[8];
-        load_square(query ? qs : ks, query ? qstride : kstride, row0, rows, dim, b, e, v);
-        const float* to = query ? f.query : f.key;
+// What a block of threads brings in of a block of rows: k's rows as operands in both forms, q's as rows (kTurn: turned), the block's matrices and factors.
+// load() requests it, put() writes it into LDS; kAhead: into registers, so that the loads of the next block's pass behind the work on this one.
+template <class T, int KT, bool kTurn>
+struct Stage {
+    static constexpr bool kOnePlace = WalkRoom<T, KT>::kOnePlace;
+    static constexpr int kAcross = 4 * KT, kSquares = 8 * kAcross;      // squares of 8 x 8 in a block's keys
+    static constexpr bool kAhead = !kSplit<T> && KT <= 4;
+    static constexpr int kVecs = (int)(sizeof(Block) / 16), kOfThread = (kVecs + kBlock - 1) / kBlock;
+    static_assert(sizeof(Block) % 16 == 0);
+    RowVec<T, 8> square[kAhead ? 8 : 1];
+    Float4 block[kAhead ? kOfThread : 1], scale[2];
+
+    static __device__ __forceinline__ void put_square(WalkRoom<T, KT>& room, bool query, int b, int e, int rows, int dim, RowVec<T, 8> (&v)[8], const Float4 (&to)[2])
+    {
+        if (rows < kDeltaRows || dim < 32 * KT) clear_eights<T, 8>(8 * b, 1, rows, e, dim, v);
         Half8 hi[8], lo[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) to_halves<T>(v[i], __is_same(T, _Float16) ? 1.0f : to[8 * b + i], hi[i], lo[i]);
+        for (int i = 0; i < 8; ++i) to_halves<T>(v[i], to[i >> 2][i & 3], hi[i], lo[i]);
         if (query) {
-            if constexpr (kQueries && kTurn) put_turned<T, KT>(hi, lo, b, e, room.queries());
-            else if constexpr (kQueries) put_rows<T, KT>(hi, lo, b, e, room.queries());
-        } else if constexpr (kKeys) {
+            if constexpr (kTurn) put_turned<T, KT>(hi, lo, b, e, room.queries());
+            else put_rows<T, KT>(hi, lo, b, e, room.queries());
+        } else {
             put_rows<T, KT>(hi, lo, b, e, room.keys);
             put_turned<T, KT>(hi, lo, b, e, room.turned_keys);
         }
     }
-}
-
-__device__ __forceinline__ void stage_block(Block& to, const Block& from)
-{
-    constexpr int kVecs = sizeof(Block) / 16;
-    static_assert(sizeof(Block) % 16 == 0);
-    const Float4* a = reinterpret_cast<const Float4*>(&from);
-    Float4* b = reinterpret_cast<Float4*>(&to);
-    for (int i = threadIdx.x; i < kVecs; i += kBlock) b[i] = a[i];
-}
-
-// y = a times the columns f: rows of tile m (32 KT elements each), or the turned ones of tile j (64 rows).
-template <int KT, int NT, int kParts>
-__device__ __forceinline__ void rows_product(const Half8 (&a)[kParts][4 * KT][kWave], int m, int lane, const HalfPair (&f)[KT][NT], Float4 (&y)[NT])
-{
-#pragma unroll
-    for (int n = 0; n < NT; ++n) y[n] = Float4(0.0f);
-#pragma unroll
-    for (int k = 0; k < KT; ++k) {
-        const Half8 hi = row_of<KT>(a[0], m, k, lane);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            y[n] = mfma(hi, f[k][n].hi, y[n]);
-            y[n] = mfma(hi, f[k][n].lo, y[n]);
-        }
-        if constexpr (kParts > 1) {
-            const Half8 lo = row_of<KT>(a[1], m, k, lane);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) y[n] = mfma(lo, f[k][n].hi, y[n]);
-        }
+    static __device__ __forceinline__ void load_scale(const BlockFactors& f, bool query, int b, Float4 (&to)[2])
+    {
+        const Float4* at = reinterpret_cast<const Float4*>((query ? f.query : f.key) + 8 * b);
+        to[0] = at[0];
+        to[1] = at[1];
     }
-}
-template <int KT, int NT, int kParts>
-__device__ __forceinline__ void turned_product(const Half8 (&a)[kParts][4 * KT][kWave], int j, int lane, const HalfPair (&f)[2][NT], Float4 (&y)[NT])
-{
+    // ks, qs: the block's first row
+    __device__ __forceinline__ void load(const Block& from, const T* ks, unsigned kstride, const T* qs, unsigned qstride, int rows, int dim)
+    {
+        if constexpr (kAhead) {
+            const int job = threadIdx.x, b = (job % kSquares) / kAcross, e = job % kAcross;
+            const bool query = job >= kSquares;
+            if (kBlock == 2 * kSquares || job < 2 * kSquares) {
+                load_square<T>(query ? qs : ks, query ? qstride : kstride, rows, dim, b, e, square);
+                load_scale(from.f, query, b, scale);
+            }
 #pragma unroll
-    for (int n = 0; n < NT; ++n) y[n] = Float4(0.0f);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const Half8 hi = turned_of<KT>(a[0], j, k, lane);
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            y[n] = mfma(hi, f[k][n].hi, y[n]);
-            y[n] = mfma(hi, f[k][n].lo, y[n]);
-        }
-        if constexpr (kParts > 1) {
-            const Half8 lo = turned_of<KT>(a[1], j, k, lane);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) y[n] = mfma(lo, f[k][n].hi, y[n]);
-        }
-    }
-}
-
-// y = rows of tile m of a lower triangular matrix times the columns f (of 64 rows).
-template <int NT>
-__device__ __forceinline__ void lower_product(const Half8 (&matrix)[2][kTriOperands][kWave], int m, int lane, const HalfPair (&f)[2][NT], Float4 (&y)[NT])
-{
-#pragma unroll
-    for (int n = 0; n < NT; ++n) y[n] = Float4(0.0f);
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-        if (s <= m >> 1) {
-            const Half8 hi = matrix[0][lower_operand(m, s)][lane], lo = matrix[1][lower_operand(m, s)][lane];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                y[n] = mfma(hi, f[s][n].hi, y[n]);
-                y[n] = mfma(hi, f[s][n].lo, y[n]);
-                y[n] = mfma(lo, f[s][n].hi, y[n]);
+            for (int i = 0; i < kOfThread; ++i) {
+                const int at = i * kBlock + threadIdx.x;
+                block[i] = reinterpret_cast<const Float4*>(&from)[at < kVecs ? at : kVecs - 1];
             }
         }
+    }
+    __device__ __forceinline__ void put(WalkRoom<T, KT>& room, const Block& from, const T* ks, unsigned kstride, const T* qs, unsigned qstride, int rows, int dim)
+    {
+        Float4* const to = reinterpret_cast<Float4*>(&room.m);
+        if constexpr (kAhead) {
+            const int job = threadIdx.x;
+            if (kBlock == 2 * kSquares || job < 2 * kSquares) put_square(room, job >= kSquares, (job % kSquares) / kAcross, job % kAcross, rows, dim, square, scale);
+#pragma unroll
+            for (int i = 0; i < kOfThread; ++i) {
+                const int at = i * kBlock + threadIdx.x;
+                if (at < kVecs) to[at] = block[i];
+            }
+        } else {
+            put_now(room, from, ks, kstride, qs, qstride, rows, dim, 0, kOnePlace ? kSquares : 2 * kSquares);
+            for (int at = threadIdx.x; at < kVecs; at += kBlock) to[at] = reinterpret_cast<const Float4*>(&from)[at];
+        }
+    }
+    // Squares first .. last - 1: the keys', then the queries'.
+    static __device__ __forceinline__ void put_now(WalkRoom<T, KT>& room, const Block& from, const T* ks, unsigned kstride, const T* qs, unsigned qstride, int rows,
+                                                   int dim, int first, int last)
+    {
+        for (int job = first + (int)threadIdx.x; job < last; job += kBlock) {
+            const bool query = job >= kSquares;
+            const int b = (job % kSquares) / kAcross, e = job % kAcross;
+            RowVec<T, 8> v[8];
+            Float4 to[2];
+            load_square<T>(query ? qs : ks, query ? qstride : kstride, rows, dim, b, e, v);
+            load_scale(from.f, query, b, to);
+            put_square(room, query, b, e, rows, dim, v, to);
+        }
+    }
+};
+
+// Operands are read from LDS a step ahead of the products that take them, and products on several results alternate: one waits for its own last sum.
+// (Left to itself the compiler reads an operand, waits for it and uses it, one after the other.)
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
+template <int KT, int P>
+__device__ __forceinline__ void read_rows(const Half8 (&a)[P][4 * KT][kWave], int m, int lane, Half8 (&to)[P][KT])
+{
+#pragma unroll
+    for (int h = 0; h < P; ++h)
+#pragma unroll
+        for (int k = 0; k < KT; ++k) to[h][k] = row_of<KT>(a[h], m, k, lane);
+}
+template <int KT, int P>
+__device__ __forceinline__ void read_turned(const Half8 (&a)[P][4 * KT][kWave], int j, int lane, Half8 (&to)[P][2])
+{
+#pragma unroll
+    for (int h = 0; h < P; ++h)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) to[h][k] = turned_of<KT>(a[h], j, k, lane);
+}
+// y = a f and z = b e: 32 K elements of the sum, a's and b's low parts where they have any.
+template <int K, int NT, int P>
+__device__ __forceinline__ void products_of(const Half8 (&a)[P][K], const HalfPair (&f)[K][NT], const Half8 (&b)[P][K], const HalfPair (&e)[K][NT], Float4 (&y)[NT],
+                                            Float4 (&z)[NT])
+{
+    Float4 yl[NT], zl[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) y[n] = z[n] = yl[n] = zl[n] = Float4(0.0f);
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            y[n] = mfma(a[0][k], f[k][n].hi, y[n]);
+            z[n] = mfma(b[0][k], e[k][n].hi, z[n]);
+            yl[n] = mfma(a[0][k], f[k][n].lo, yl[n]);
+            zl[n] = mfma(b[0][k], e[k][n].lo, zl[n]);
+            if constexpr (P > 1) {
+                yl[n] = mfma(a[1][k], f[k][n].hi, yl[n]);
+                zl[n] = mfma(b[1][k], e[k][n].hi, zl[n]);
+            }
+        }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        y[n] += yl[n];
+        z[n] += zl[n];
+    }
 }
 
-// The same for rows of tile m of an upper one.
-template <int NT>
-__device__ __forceinline__ void upper_product(const Half8 (&matrix)[2][kTriOperands][kWave], int m, int lane, const HalfPair (&f)[2][NT], Float4 (&y)[NT])
+template <int K, int NT, int P>
+__device__ __forceinline__ void products(const Half8 (&a)[P][K], const Half8 (&b)[P][K], const HalfPair (&f)[K][NT], Float4 (&y)[NT], Float4 (&z)[NT])
+{
+    products_of<K, NT, P>(a, f, b, f, y, z);
+}
+
+// y = a triangular matrix times the columns f (of 64 rows); kUpper: the transposed form.
+template <int NT, bool kUpper>
+__device__ __forceinline__ void tri_products(const Half8 (&matrix)[2][kTriOperands][kWave], int lane, const HalfPair (&f)[2][NT], Float4 (&y)[4][NT])
+{
+    Half8 a[2][kTriOperands];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int k = 0; k < kTriOperands; ++k) a[h][k] = matrix[h][k][lane];
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) y[m][n] = Float4(0.0f);
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int term = 0; term < 3; ++term)
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+                if (kUpper ? s >= m >> 1 : s <= m >> 1)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        y[m][n] = mfma(a[term == 2][kUpper ? upper_operand(m, s) : lower_operand(m, s)], term == 1 ? f[s][n].lo : f[s][n].hi, y[m][n]);
+}
+
+// One tile's.
+template <int NT, bool kUpper>
+__device__ __forceinline__ void tri_product(const Half8 (&matrix)[2][kTriOperands][kWave], int m, int lane, const HalfPair (&f)[2][NT], Float4 (&y)[NT])
 {
 #pragma unroll
     for (int n = 0; n < NT; ++n) y[n] = Float4(0.0f);
 #pragma unroll
     for (int s = 0; s < 2; ++s)
-        if (s >= m >> 1) {
-            const Half8 hi = matrix[0][upper_operand(m, s)][lane], lo = matrix[1][upper_operand(m, s)][lane];
+        if (kUpper ? s >= m >> 1 : s <= m >> 1) {
+            const int at = kUpper ? upper_operand(m, s) : lower_operand(m, s);
+            const Half8 hi = matrix[0][at][lane], lo = matrix[1][at][lane];
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 y[n] = mfma(hi, f[s][n].hi, y[n]);
@@ -259,37 +456,45 @@ struct PrepareRoom {
 
 // q's or k's rows as fp16, each with its largest magnitude's power of two taken out; sizes: what makes it up again.
 template <class T, int KT>
-__device__ __forceinline__ void load_rows(const T* __restrict__ base, long long stride, int rows, int dim, bool unit, Half8 (&to)[kSplit<T> ? 2 : 1][4 * KT][kDeltaRows],
-                                          float* factor, float* scale)
-{
-    constexpr int kLanes = 4 * KT;                // of a row
-    const int e = threadIdx.x % kLanes, have = dim - 8 * e;
+struct RowLoad {
+    static constexpr int kLanes = 4 * KT, kPasses = kDeltaRows * kLanes / kBlock > 0 ? kDeltaRows * kLanes / kBlock : 1;      // lanes of a row
+    RowVec<T, 8> v[kPasses];
+
+    __device__ __forceinline__ void load(const T* __restrict__ base, unsigned stride, int rows, int dim)
+    {
+        load_eights<T, kPasses>(base, stride, (int)(threadIdx.x / kLanes), kBlock / kLanes, rows, threadIdx.x % kLanes, dim, v);
+    }
+    __device__ __forceinline__ void put(bool unit, int rows, int dim, Half8 (&to)[kSplit<T> ? 2 : 1][4 * KT][kDeltaRows], float* factor, float* scale)
+    {
+        const int e = threadIdx.x % kLanes;
+        clear_eights<T, kPasses>((int)(threadIdx.x / kLanes), kBlock / kLanes, rows, e, dim, v);
 #pragma unroll
-    for (int t = threadIdx.x / kLanes; t < kDeltaRows; t += kBlock / kLanes) {
-        const RowVec<T, 8> v = t < rows && have > 0 ? load_row_vec<T, 8>(base + (long long)t * stride + 8 * e, have) : RowVec<T, 8>(T(0));
-        float m = 0.0f, squares = 0.0f;
+        for (int k = 0; k < kPasses; ++k) {
+            const int t = (int)(threadIdx.x / kLanes) + k * (kBlock / kLanes);
+            float m = 0.0f, squares = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            m = larger(m, (float)v[i]);
-            squares = __builtin_fmaf((float)v[i], (float)v[i], squares);
-        }
+            for (int i = 0; i < 8; ++i) {
+                m = larger(m, (float)v[k][i]);
+                squares = __builtin_fmaf((float)v[k][i], (float)v[k][i], squares);
+            }
 #pragma unroll
-        for (int x = 1; x < kLanes; x *= 2) {
-            m = __builtin_fmaxf(m, __shfl_xor(m, x));
-            squares += __shfl_xor(squares, x);
-        }
-        Scale by(m);
-        if (__is_same(T, _Float16)) by.to = by.back = 1.0f;
-        Half8 hi, lo;
-        to_halves<T>(v, by.to, hi, lo);
-        to[0][e][t ^ (e & 15)] = hi;
-        if constexpr (kSplit<T>) to[1][e][t ^ (e & 15)] = lo;
-        if (e == 0) {
-            scale[t] = by.to;
-            factor[t] = by.back * (unit ? 1.0f / __builtin_sqrtf(squares + 1e-6f) : 1.0f);
+            for (int x = 1; x < kLanes; x *= 2) {
+                m = __builtin_fmaxf(m, __shfl_xor(m, x));
+                squares += __shfl_xor(squares, x);
+            }
+            Scale by(m);
+            if (__is_same(T, _Float16)) by.to = by.back = 1.0f;
+            Half8 hi, lo;
+            to_halves<T>(v[k], by.to, hi, lo);
+            to[0][e][t ^ (e & 15)] = hi;
+            if constexpr (kSplit<T>) to[1][e][t ^ (e & 15)] = lo;
+            if (e == 0) {
+                scale[t] = by.to;
+                factor[t] = by.back * (unit ? 1.0f / __builtin_sqrtf(squares + 1e-6f) : 1.0f);
+            }
         }
     }
-}
+};
 
 // K K^T and Q K^T, without their factors: wave w has the rows of tile w (kTiles: tile_row, otherwise 16 w ..) and the columns up to them.
 template <class T, int KT, bool kTiles, int kParts>
@@ -398,10 +603,13 @@ template <class T, int KT, bool kBack>
 __device__ __forceinline__ void prepare_block(const DeltaParams& p, const Piece& piece, long long slot, int key_head, PrepareRoom<T, KT>& room)
 {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, g = lane >> 4, r = lane & 15, many = p.heads / p.key_heads;
-    load_rows<T, KT>(sequence_base<const T>(p.k, p.pieces, piece) + piece.row0 * p.k.row + key_head * p.k_head, p.k.row, piece.n, p.key_dim, p.unit, room.keys,
-                     room.key, room.f.key);
-    load_rows<T, KT>(sequence_base<const T>(p.q, p.pieces, piece) + piece.row0 * p.q.row + key_head * p.q_head, p.q.row, piece.n, p.key_dim, p.unit, room.queries,
-                     room.query, room.f.query);
+    {
+        RowLoad<T, KT> k, q;
+        k.load(sequence_base<const T>(p.k, p.pieces, piece) + piece.row0 * p.k.row + key_head * p.k_head, (unsigned)p.k.row, piece.n, p.key_dim);
+        q.load(sequence_base<const T>(p.q, p.pieces, piece) + piece.row0 * p.q.row + key_head * p.q_head, (unsigned)p.q.row, piece.n, p.key_dim);
+        k.put(p.unit, piece.n, p.key_dim, room.keys, room.key, room.f.key);
+        q.put(p.unit, piece.n, p.key_dim, room.queries, room.query, room.f.query);
+    }
     __syncthreads();
     Float4 kk[4], qk[4];
     key_products<T, KT, false>(room.keys, room.queries, kk, qk);
