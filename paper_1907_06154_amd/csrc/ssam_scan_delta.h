@@ -8,7 +8,7 @@
 // blocks at once (delta_prepare); the rest follows the sequence.
 //
 // Matrix products run on v_mfma_f32_16x16x32_f16.  q, k of 16 bits are one fp16 operand, exact, with a power of two per row taken
-// out; everything else is a pair hi + lo of fp16 that keeps 22 bits of the fp32 value: two products against q or k, three
+// out; everything else is a pair hi + lo of fp16 that keeps 23 bits of the fp32 value: two products against q or k, three
 // between two such pairs (lo lo is below 2^-22).  bf16 pairs keep 16 bits, which the state's fp32 would show.
 //
 // Operand layout: lane (g = lane / 16, r = lane % 16) of an A operand holds row r, elements 8 g .. 8 g + 7 of 32 along the sum; of a B
@@ -45,25 +45,27 @@ struct Scale {
     }
 };
 
-__device__ __forceinline__ void split2(float a, float b, Half8& hi, Half8& lo, int at)
+// Eight values as hi + lo, each rounded to nearest: two mixed-precision multiply-adds a value, to v and to v - hi.  A matrix instruction must lie two wait
+// states behind the write of what it reads, which the compiler does not count out of these blocks; what they read must not come straight from one.
+__device__ __forceinline__ HalfPair split(float a0, float a1, float a2, float a3, float a4, float a5, float a6, float a7, float to)
 {
-    const auto h = __builtin_amdgcn_cvt_pkrtz(a, b);
-    const auto l = __builtin_amdgcn_cvt_pkrtz(a - (float)h[0], b - (float)h[1]);
-    hi[at] = (_Float16)h[0];
-    hi[at + 1] = (_Float16)h[1];
-    lo[at] = (_Float16)l[0];
-    lo[at + 1] = (_Float16)l[1];
-}
-// The values of two result tiles as a B operand.
-__device__ __forceinline__ HalfPair split(const Float4& a, const Float4& b, float to)
-{
+    typedef unsigned Four __attribute__((ext_vector_type(4)));
+    unsigned h0, h1, h2, h3, l0, l1, l2, l3;
+#define SSAM_PAIR(H, L, A, B)                                                                                                          \
+    "v_fma_mixlo_f16 %" #H ", %" #A ", %16, 0\n\tv_fma_mixhi_f16 %" #H ", %" #B ", %16, 0\n\t"                                         \
+    "v_fma_mixlo_f16 %" #L ", %" #A ", %16, -%" #H " op_sel_hi:[0,0,1]\n\tv_fma_mixhi_f16 %" #L ", %" #B ", %16, -%" #H " op_sel:[0,0,1] op_sel_hi:[0,0,1]\n\t"
+    asm(SSAM_PAIR(0, 4, 8, 9) SSAM_PAIR(1, 5, 10, 11) SSAM_PAIR(2, 6, 12, 13) SSAM_PAIR(3, 7, 14, 15) "s_nop 1"
+        : "=&v"(h0), "=&v"(h1), "=&v"(h2), "=&v"(h3), "=&v"(l0), "=&v"(l1), "=&v"(l2), "=&v"(l3)
+        : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "v"(a4), "v"(a5), "v"(a6), "v"(a7), "v"(to));
+#undef SSAM_PAIR
     HalfPair p;
-    split2(a[0] * to, a[1] * to, p.hi, p.lo, 0);
-    split2(a[2] * to, a[3] * to, p.hi, p.lo, 2);
-    split2(b[0] * to, b[1] * to, p.hi, p.lo, 4);
-    split2(b[2] * to, b[3] * to, p.hi, p.lo, 6);
+    const Four h = {h0, h1, h2, h3}, l = {l0, l1, l2, l3};
+    p.hi = __builtin_bit_cast(Half8, h);
+    p.lo = __builtin_bit_cast(Half8, l);
     return p;
 }
+// The values of two result tiles as a B operand.
+__device__ __forceinline__ HalfPair split(const Float4& a, const Float4& b, float to) { return split(a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3], to); }
 
 // The larger of two magnitudes; a NaN may be passed over, as it reaches the products by itself.
 __device__ __forceinline__ float larger(float m, float v) { return __builtin_fmaxf(m, __builtin_fabsf(v)); }

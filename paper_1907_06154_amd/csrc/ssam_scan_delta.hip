@@ -22,6 +22,8 @@ __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
 {
     __shared__ WalkRoom<T, KT> room;
     typedef Stage<T, KT, false> S;
+    typedef Columns<T, NT, kSplit<T> && (KT > 4)> Cols;
+    __shared__ typename Cols::Room columns[kWavesPerBlock];
     constexpr int kParts = kSplit<T> ? 2 : 1;       // of q and k
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, g = lane >> 4, r16 = lane & 15;
     const int tile = (int)(blockIdx.x % p.tiles), head = (int)(blockIdx.x / p.tiles % p.heads), seq = (int)(blockIdx.x / p.tiles / p.heads);
@@ -30,19 +32,19 @@ __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
     span_of(p.pieces, seq, first, len);
     const int blocks = (len + kDeltaRows - 1) / kDeltaRows;
     const long long slot0 = p.pieces.begin ? first_slot(p.pieces, seq) : (long long)seq * p.pieces.per;
-    const int c0 = (tile * kWavesPerBlock + wave) * 16 * NT + r16, left = p.value_dim - c0;      // the lane's first column; columns from there on
+    const int col0 = (tile * kWavesPerBlock + __builtin_amdgcn_readfirstlane(wave)) * 16 * NT, c0 = col0 + r16;      // the lane's first column
     const Piece whole{seq, first, len, 0, len};
     const T* qs = sequence_base<const T>(p.q, p.pieces, whole) + key_head * p.q_head;
     const T* ks = sequence_base<const T>(p.k, p.pieces, whole) + key_head * p.k_head;
-    const T* vs = sequence_base<const T>(p.v, p.pieces, whole) + head * p.v_head + c0;
-    T* os = sequence_base<T>(p.out, p.pieces, whole) + head * p.out_head + c0;
-    const long long state_at = ((long long)seq * p.heads + head) * p.key_dim * p.value_dim + c0;
+    const T* vs = sequence_base<const T>(p.v, p.pieces, whole) + head * p.v_head;
+    T* os = sequence_base<T>(p.out, p.pieces, whole) + head * p.out_head;
+    const long long state_at = ((long long)seq * p.heads + head) * p.key_dim * p.value_dim;
     const unsigned kstride = (unsigned)p.k.row, qstride = (unsigned)p.q.row, vstride = (unsigned)p.v.row, ostride = (unsigned)p.out.row;
     const Block* from = p.blocks + slot0 * p.heads + head;
 
     Float4 s[2 * KT][NT];
     if (p.state) {
-        load_state<KT, NT>(p.state + state_at, p.value_dim, p.key_dim, left, s);
+        load_state<KT, NT>(p.state + state_at, p.value_dim, p.key_dim, c0, s);
     } else {
 #pragma unroll
         for (int j = 0; j < 2 * KT; ++j)
@@ -50,19 +52,19 @@ __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
             for (int n = 0; n < NT; ++n) s[j][n] = Float4(0.0f);
     }
     S stage;
-    Columns<T, NT> v;
+    Cols v;
     int rows = len < kDeltaRows ? len : kDeltaRows;
     if (blocks > 0) {
         stage.load(*from, ks, kstride, qs, qstride, rows, p.key_dim);
-        v.load(vs, vstride, rows, left);
+        v.load(vs, vstride, rows, col0, p.value_dim);
     }
     for (int c = 0; c < blocks; ++c) {
         __syncthreads();
         stage.put(room, *from, ks, kstride, qs, qstride, rows, p.key_dim);
-        float* const mark = p.marks ? mark_of(p.marks, p, slot0 + c, head) + c0 : nullptr;
-        if (mark) store_state<KT, NT>(mark, p.value_dim, p.key_dim, left, s);
+        float* const mark = p.marks ? mark_of(p.marks, p, slot0 + c, head) : nullptr;
+        if (mark) store_state<KT, NT>(mark, p.value_dim, p.key_dim, c0, s);
         Float4 x[4][NT], o[4][NT];
-        v.values(rows, x);
+        v.values(columns[wave], rows, x);
         __syncthreads();
         const T *const this_ks = ks, *const this_qs = qs;
         const Block* const this_from = from;
@@ -75,7 +77,7 @@ __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
             rows = len - (c + 1) * kDeltaRows;
             rows = rows < kDeltaRows ? rows : kDeltaRows;
             stage.load(*from, ks, kstride, qs, qstride, rows, p.key_dim);
-            v.load(vs, vstride, rows, left);
+            v.load(vs, vstride, rows, col0, p.value_dim);
         }
 
         // X = V - exp(G) K S and Q S
@@ -127,14 +129,23 @@ __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
         HalfPair f[2][NT];
         split_rows<NT>(x, f, back_u);
         tri_products<NT, false>(room.m.solve, lane, f, x);
+        if (mark) {
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) x[m][n] *= back_u[n] * room.m.f.solve_back;
+            store_tiles<NT>(mark + (size_t)p.key_dim * p.value_dim, p.value_dim, c0, x);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) back_u[n] = 1.0f;
+        } else {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) back_u[n] *= room.m.f.solve_back;
+        }
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
             const Float4 beta = *reinterpret_cast<const Float4*>(&room.m.f.beta[tile_row(m, 4 * g)]);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) x[m][n] *= back_u[n] * room.m.f.solve_back;
-            if (mark) store_tile<NT>(mark + (long long)p.key_dim * p.value_dim, p.value_dim, left, m, x[m]);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) x[m][n] *= beta;
+            for (int n = 0; n < NT; ++n) x[m][n] *= beta * back_u[n];
         }
         // O = scale (exp(G) Q S + (Q K^T o D) U)
         split_rows<NT>(x, f, back_u);
@@ -151,8 +162,7 @@ __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
                     x[m][n] *= writes;
                 }
             }
-#pragma unroll
-            for (int m = 0; m < 4; ++m) store_columns<T, NT>(os, ostride, this_rows, left, m, a[m]);
+            Cols::store(columns[wave], os, ostride, this_rows, col0, p.value_dim, a);
         }
         os += (long long)kDeltaRows * p.out.row;
         // S = exp(G_C) S + (exp(G_C - G) K)^T U
@@ -181,7 +191,7 @@ __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
             }
         }
     }
-    if (p.final) store_state<KT, NT>(p.final + state_at, p.value_dim, p.key_dim, left, s);
+    if (p.final) store_state<KT, NT>(p.final + state_at, p.value_dim, p.key_dim, c0, s);
 }
 
 }  // namespace
@@ -235,7 +245,7 @@ int ssam_scan_delta(const ssam_scan_delta_args* a, void* hip_stream)
     DeltaParams p{make_pieces(a->seq, kDeltaRows), a->q, a->k, a->v, a->out, a->g, a->beta, a->q_head, a->k_head, a->v_head, a->out_head, a->d_state,
                   a->d_final, a->d_marks, static_cast<Block*>(a->d_work), a->heads, a->key_heads, a->key_dim, a->value_dim, a->unit != 0, a->scale, 1};
     const long long heads = (long long)a->seq.sequences * a->heads;
-    const bool wide = false;
+    const bool wide = heads * ((a->value_dim + 63) / 64) > 512 && a->value_dim > 64 && a->key_dim <= 128;
     p.tiles = (a->value_dim + (wide ? 127 : 63)) / (wide ? 128 : 64);
     if (product(slots, a->key_heads) > kMaxGrid || product(heads, p.tiles) > kMaxGrid) return SSAM_ERR_DIM;
     hipStream_t st = (hipStream_t)hip_stream;
@@ -245,7 +255,13 @@ int ssam_scan_delta(const ssam_scan_delta_args* a, void* hip_stream)
             constexpr int KT = decltype(kt)::value;
             hipLaunchKernelGGL((delta_prepare<T, KT>), dim3((unsigned)(slots * a->key_heads)), dim3(kBlock), 0, st, p);
             if (int e = launched()) return e;
-            hipLaunchKernelGGL((delta_walk<T, KT, 1>), dim3((unsigned)(heads * p.tiles)), dim3(kBlock), 0, st, p);
+            const dim3 walks((unsigned)(heads * p.tiles));
+            if constexpr (KT <= 4)
+                if (wide) {
+                    hipLaunchKernelGGL((delta_walk<T, KT, 2>), walks, dim3(kBlock), 0, st, p);
+                    return launched();
+                }
+            hipLaunchKernelGGL((delta_walk<T, KT, 1>), walks, dim3(kBlock), 0, st, p);
             return launched();
         });
     });

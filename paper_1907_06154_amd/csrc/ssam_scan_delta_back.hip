@@ -37,6 +37,8 @@ __global__ __launch_bounds__(kBlock) void delta_back_walk(DeltaBackParams b)
     const DeltaParams& p = b.f;
     __shared__ WalkRoom<T, KT> room;
     typedef Stage<T, KT, true> S;
+    typedef Columns<T, NT, kSplit<T> && (KT > 4)> Cols;
+    __shared__ typename Cols::Room columns[kWavesPerBlock];
     constexpr int kParts = kSplit<T> ? 2 : 1;       // of q and k
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, g = lane >> 4, r16 = lane & 15;
     const int tile = (int)(blockIdx.x % p.tiles), head = (int)(blockIdx.x / p.tiles % p.heads), seq = (int)(blockIdx.x / p.tiles / p.heads);
@@ -45,21 +47,20 @@ __global__ __launch_bounds__(kBlock) void delta_back_walk(DeltaBackParams b)
     span_of(p.pieces, seq, first, len);
     const int blocks = (len + kDeltaRows - 1) / kDeltaRows;
     const long long slot0 = p.pieces.begin ? first_slot(p.pieces, seq) : (long long)seq * p.pieces.per;
-    const int c0 = (tile * kWavesPerBlock + wave) * 16 * NT + r16;
+    const int col0 = (tile * kWavesPerBlock + __builtin_amdgcn_readfirstlane(wave)) * 16 * NT, c0 = col0 + r16;
     const Piece whole{seq, first, len, 0, len};
-    const int left = p.value_dim - c0;
     const long long end = (long long)(blocks - 1) * kDeltaRows;                                  // first row of the last block
     const T* qs = sequence_base<const T>(p.q, p.pieces, whole) + key_head * p.q_head + end * p.q.row;
     const T* ks = sequence_base<const T>(p.k, p.pieces, whole) + key_head * p.k_head + end * p.k.row;
-    const T* dos = sequence_base<const T>(b.grad_out, p.pieces, whole) + head * b.grad_out_head + c0 + end * b.grad_out.row;
-    T* dvs = b.grad_v.d ? sequence_base<T>(b.grad_v, p.pieces, whole) + head * b.grad_v_head + c0 + end * b.grad_v.row : nullptr;
-    const long long state_at = ((long long)seq * p.heads + head) * p.key_dim * p.value_dim + c0;
+    const T* dos = sequence_base<const T>(b.grad_out, p.pieces, whole) + head * b.grad_out_head + end * b.grad_out.row;
+    T* dvs = b.grad_v.d ? sequence_base<T>(b.grad_v, p.pieces, whole) + head * b.grad_v_head + end * b.grad_v.row : nullptr;
+    const long long state_at = ((long long)seq * p.heads + head) * p.key_dim * p.value_dim;
     const unsigned kstride = (unsigned)p.k.row, qstride = (unsigned)p.q.row, ostride = (unsigned)b.grad_out.row, vstride = (unsigned)b.grad_v.row;
     const Block* from = p.blocks + (slot0 + blocks - 1) * p.heads + head;
 
     Float4 s[2 * KT][NT];
     if (p.state) {
-        load_state<KT, NT>(p.state + state_at, p.value_dim, p.key_dim, left, s);
+        load_state<KT, NT>(p.state + state_at, p.value_dim, p.key_dim, c0, s);
     } else {
 #pragma unroll
         for (int j = 0; j < 2 * KT; ++j)
@@ -67,19 +68,19 @@ __global__ __launch_bounds__(kBlock) void delta_back_walk(DeltaBackParams b)
             for (int n = 0; n < NT; ++n) s[j][n] = Float4(0.0f);
     }
     S stage;
-    Columns<T, NT> v;
+    Cols v;
     int rows = len - (blocks - 1) * kDeltaRows;
     if (blocks > 0) {
         stage.load(*from, ks, kstride, qs, qstride, rows, p.key_dim);
-        v.load(dos, ostride, rows, left);
+        v.load(dos, ostride, rows, col0, p.value_dim);
     }
     for (int c = blocks - 1; c >= 0; --c) {
         __syncthreads();
         stage.put(room, *from, ks, kstride, qs, qstride, rows, p.key_dim);
-        float* const behind = mark_of(b.behind, p, slot0 + c, head) + c0;
-        store_state<KT, NT>(behind, p.value_dim, p.key_dim, left, s);
+        float* const behind = mark_of(b.behind, p, slot0 + c, head);
+        store_state<KT, NT>(behind, p.value_dim, p.key_dim, c0, s);
         Float4 o[4][NT], x[4][NT];       // dO; dU, dY, dX
-        v.values(rows, o);
+        v.values(columns[wave], rows, o);
         __syncthreads();
         const T *const this_ks = ks, *const this_qs = qs;
         const Block* const this_from = from;
@@ -91,7 +92,7 @@ __global__ __launch_bounds__(kBlock) void delta_back_walk(DeltaBackParams b)
             from -= p.heads;
             rows = kDeltaRows;
             stage.load(*from, ks, kstride, qs, qstride, rows, p.key_dim);
-            v.load(dos, ostride, rows, left);
+            v.load(dos, ostride, rows, col0, p.value_dim);
         }
         {
             HalfPair f[KT][NT];
@@ -140,16 +141,21 @@ __global__ __launch_bounds__(kBlock) void delta_back_walk(DeltaBackParams b)
         split_rows<NT>(x, f, back);
         tri_products<NT, true>(room.m.solve, lane, f, x);
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const int t0 = tile_row(m, 4 * g);
-            const Float4 beta = *reinterpret_cast<const Float4*>(&room.m.f.beta[t0]), reads = *reinterpret_cast<const Float4*>(&room.m.f.reads[t0]),
-                         asks = *reinterpret_cast<const Float4*>(&room.m.f.asks[t0]);
+        for (int m = 0; m < 4; ++m)
 #pragma unroll
             for (int n = 0; n < NT; ++n) x[m][n] *= back[n] * room.m.f.solve_back;
-            store_tile<NT>(behind + (long long)p.key_dim * p.value_dim, p.value_dim, left, m, x[m]);
+        store_tiles<NT>(behind + (size_t)p.key_dim * p.value_dim, p.value_dim, c0, x);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const Float4 beta = *reinterpret_cast<const Float4*>(&room.m.f.beta[tile_row(m, 4 * g)]);
 #pragma unroll
             for (int n = 0; n < NT; ++n) x[m][n] *= beta;
-            if (dvs) store_columns<T, NT>(dvs, vstride, this_rows, left, m, x[m]);
+        }
+        if (dvs) Cols::store(columns[wave], dvs, vstride, this_rows, col0, p.value_dim, x);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const Float4 reads = *reinterpret_cast<const Float4*>(&room.m.f.reads[tile_row(m, 4 * g)]),
+                         asks = *reinterpret_cast<const Float4*>(&room.m.f.asks[tile_row(m, 4 * g)]);
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 x[m][n] *= -reads;
@@ -181,7 +187,7 @@ __global__ __launch_bounds__(kBlock) void delta_back_walk(DeltaBackParams b)
                 for (int i = 0; i < 4; ++i) s[j][n][i] = __builtin_fmaf(total, s[j][n][i], __builtin_fmaf(a[n][i], back[n], q[n][i] * back_o[n]));
         }
     }
-    if (b.grad_state) store_state<KT, NT>(b.grad_state + state_at, p.value_dim, p.key_dim, left, s);
+    if (b.grad_state) store_state<KT, NT>(b.grad_state + state_at, p.value_dim, p.key_dim, c0, s);
 }
 
 // ---- gradients of q, k, g and beta ----------------------------------------------------------------------------------------

@@ -14,8 +14,9 @@ __device__ __forceinline__ void to_halves(const RowVec<T, 8>& v, float to, Half8
     if constexpr (__is_same(T, _Float16)) {
         hi = v;
     } else if constexpr (kSplit<T>) {
-#pragma unroll
-        for (int i = 0; i < 8; i += 2) split2(v[i] * to, v[i + 1] * to, hi, lo, i);
+        const HalfPair p = split(v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7], to);
+        hi = p.hi;
+        lo = p.lo;
     } else {
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
@@ -58,25 +59,40 @@ template <int KT> __device__ __forceinline__ Half8 turned_of(const Half8 (&a)[4 
     return a[turned_operand(j, k)][turned_entry(j, lane >> 4, lane & 15)];
 }
 
-// N rows of eight elements, rows row0, row0 + step .. and elements from 8 e on; rows >= 1.  There are no branches on what is there: a load that waits for
-// its turn in one costs its latency by itself.  clear_eights() makes zeros of what was not there, where the values are used.
+// A value, the same for all lanes, that the compiler takes for a new one here: what is made from it is not kept in registers over a loop.  (Rows' distances,
+// 16 to 64 of them, would be, and push everything else out.)
+__device__ __forceinline__ unsigned afresh(unsigned v)
+{
+    v = __builtin_amdgcn_readfirstlane(v);
+    asm volatile("" : "+s"(v));
+    return v;
+}
+
+// N rows of eight elements, rows row0, row0 + step .. and elements from 8 e on; rows >= 1, `base` the same for all lanes.  There are no branches on what is
+// there: a load that waits for its turn in one costs its latency by itself.  clear_eights() makes zeros of what was not there, where the values are used.
+// Where all rows are there, their distances are the same for all lanes too and cost no vector instructions.
 template <class T, int N>
 __device__ __forceinline__ void load_eights(const T* __restrict__ base, unsigned stride, int row0, int step, int rows, int e, int dim, RowVec<T, 8> (&v)[N])
 {
+    stride = afresh(stride);
     const bool across = 8 * e < dim;
-    base += across ? 8 * e : 0;
-    if (dim % 8 == 0) {
+    const unsigned at = across ? 8 * e : 0;
+    if (dim % 8 == 0 && rows == kDeltaRows) {
+        const unsigned lane_at = (unsigned)row0 * stride + at;
+#pragma unroll
+        for (int i = 0; i < N; ++i) __builtin_memcpy(&v[i], base + (unsigned)(i * step) * stride + lane_at, sizeof(v[i]));
+    } else if (dim % 8 == 0) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int row = row0 + i * step;
-            __builtin_memcpy(&v[i], base + (unsigned)(row < rows ? row : rows - 1) * stride, sizeof(v[i]));
+            __builtin_memcpy(&v[i], base + ((unsigned)(row < rows ? row : rows - 1) * stride + at), sizeof(v[i]));
         }
     } else {
         const int have = across ? dim - 8 * e : dim;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int row = row0 + i * step;
-            v[i] = load_row_vec<T, 8>(base + (unsigned)(row < rows ? row : rows - 1) * stride, have);
+            v[i] = load_row_vec<T, 8>(base + ((unsigned)(row < rows ? row : rows - 1) * stride + at), have);
         }
     }
 }
@@ -94,40 +110,130 @@ __device__ __forceinline__ void load_square(const T* __restrict__ base, unsigned
     load_eights<T, 8>(base, stride, 8 * b, 1, rows, e, dim, v);
 }
 
-// An element on its way in a register of its own: two of them packed into one would have to be waited for in turn.
-template <class T> struct Raw {
-    unsigned bits;
-    __device__ __forceinline__ void load(const T* p) { bits = *reinterpret_cast<const unsigned short*>(p); }
-    __device__ __forceinline__ float value() const { return (float)__builtin_bit_cast(T, (unsigned short)bits); }
-};
-template <> struct Raw<float> {
-    float bits;
-    __device__ __forceinline__ void load(const float* p) { bits = *p; }
-    __device__ __forceinline__ float value() const { return bits; }
-};
-
-// A wave's columns of 64 rows, as result tiles (tile_row); `base`: the rows' first, the lane's first column; `left`: columns from there on.  Rows that are not
-// there are the last one's copies until values() takes them.
-template <class T, int NT>
+// A wave's columns of 64 rows on their way between memory and result tiles: 16 bytes a lane from row to row, by way of a room in LDS that is the wave's own,
+// where the tiles' values lie one by one.  (Element by element from and to memory, 16 loads and 16 stores a block cost a wave 3000 of 12000 cycles.)
+// kDirect: without the room.
+template <class T, int NT, bool kDirect>
 struct Columns {
-    Raw<T> v[4][NT][4];
+    static constexpr int kWide = 16 * NT, E = 16 / (int)sizeof(T), kOfRow = kWide / E, kOfLane = kOfRow;
+    struct Room {
+        RowVec<T, E> rows[kDirect ? 1 : kDeltaRows][kDirect ? 1 : kOfRow + 1];
+    };
+    RowVec<T, E> v[kOfLane];
 
-    __device__ __forceinline__ void load(const T* __restrict__ base, unsigned stride, int rows, int left)
+    static __device__ __forceinline__ void place(int i, int& row, int& part)
     {
-        const int g = (threadIdx.x & (kWave - 1)) >> 4;
+        const int at = i * kWave + (int)(threadIdx.x & (kWave - 1));
+        row = at / kOfRow;
+        part = at % kOfRow;
+    }
+    // `base`: the rows' first, the same for all lanes; col0: the wave's first column of `dim`.  Rows that are not there are the last one's copies until values()
+    // takes them, columns the last one's.
+    __device__ __forceinline__ void load(const T* __restrict__ base, unsigned stride, int rows, int col0, int dim)
+    {
+        const bool whole = col0 + kWide <= dim;
+        if (whole && rows == kDeltaRows) {
+            int row, part;
+            place(0, row, part);
+            const unsigned lane_at = (unsigned)row * stride + (unsigned)(col0 + part * E);
+            const unsigned step = (unsigned)(kWave / kOfRow) * afresh(stride);
+#pragma unroll
+            for (int i = 0; i < kOfLane; ++i) __builtin_memcpy(&v[i], base + i * step + lane_at, 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kOfLane; ++i) {
+                int row, part;
+                place(i, row, part);
+                const T* const at = base + (unsigned)(row < rows ? row : rows - 1) * stride;
+                const int c = col0 + part * E;
+                if (whole) {
+                    __builtin_memcpy(&v[i], at + c, 16);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < E; ++k) v[i][k] = at[c + k < dim ? c + k : dim - 1];
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void values(Room& room, int rows, Float4 (&x)[4][NT]) const
+    {
+        const int lane = threadIdx.x & (kWave - 1), g = lane >> 4, r = lane & 15;
+#pragma unroll
+        for (int i = 0; i < kOfLane; ++i) {
+            int row, part;
+            place(i, row, part);
+            room.rows[row][part] = v[i];
+        }
+        __builtin_amdgcn_wave_barrier();       // (a wave's LDS instructions are done in their order)
+        const T* const at = reinterpret_cast<const T*>(&room.rows[8 * g][0]) + r;
+        constexpr int kPitch = (kOfRow + 1) * E;
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[m][n][i] = (float)at[tile_row(m, i) * kPitch + 16 * n];
+        if (rows < kDeltaRows) {
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[m][n][i] = tile_row(m, 4 * g + i) < rows ? x[m][n][i] : 0.0f;
+        }
+    }
+    static __device__ __forceinline__ void store(Room& room, T* __restrict__ base, unsigned stride, int rows, int col0, int dim, const Float4 (&x)[4][NT])
+    {
+        const int lane = threadIdx.x & (kWave - 1), g = lane >> 4, r = lane & 15;
+        constexpr int kPitch = (kOfRow + 1) * E;
+        __builtin_amdgcn_wave_barrier();
+        T* const to = reinterpret_cast<T*>(&room.rows[8 * g][0]) + r;
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) to[tile_row(m, i) * kPitch + 16 * n] = (T)x[m][n][i];
+        __builtin_amdgcn_wave_barrier();
+        const unsigned step = (unsigned)(kWave / kOfRow) * afresh(stride);
+        int row0, part;
+        place(0, row0, part);
+        const unsigned lane_at = (unsigned)row0 * stride + (unsigned)(col0 + part * E);
+        const int have = dim - (col0 + part * E);
+#pragma unroll
+        for (int i = 0; i < kOfLane; ++i) {
+            const int row = row0 + i * (kWave / kOfRow);
+            const RowVec<T, E> w = room.rows[row][part];
+            if (rows == kDeltaRows || row < rows) {
+                if (have >= E) __builtin_memcpy(base + i * step + lane_at, &w, 16);
+                else if (have > 0) store_row_vec<T, E>(base + i * step + lane_at, have, w);
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+};
+// Without the room; an element on its way in a register of its own: two of them packed into one would have to be waited for in turn.
+template <class T, int NT>
+struct Columns<T, NT, true> {
+    struct Room {};
+    T v[4][NT][4];
+    __device__ __forceinline__ void load(const T* __restrict__ base, unsigned stride, int rows, int col0, int dim)
+    {
+        stride = afresh(stride);
+        const int g = (threadIdx.x & (kWave - 1)) >> 4, col = col0 + (threadIdx.x & 15);
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const T* const at = base + (left > 16 * n ? 16 * n : left > 0 ? 0 : left - 1);      // (columns that are not there are the last one's copies)
+            const unsigned c = (unsigned)(col + 16 * n < dim ? col + 16 * n : dim - 1);
 #pragma unroll
             for (int m = 0; m < 4; ++m)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int t = tile_row(m, 4 * g + i);
-                    v[m][n][i].load(at + (unsigned)(t < rows ? t : rows - 1) * stride);
+                    v[m][n][i] = base[(unsigned)(t < rows ? t : rows - 1) * stride + c];
                 }
         }
     }
-    __device__ __forceinline__ void values(int rows, Float4 (&x)[4][NT]) const
+    __device__ __forceinline__ void values(Room&, int rows, Float4 (&x)[4][NT]) const
     {
         const int g = (threadIdx.x & (kWave - 1)) >> 4;
 #pragma unroll
@@ -135,68 +241,74 @@ struct Columns {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[m][n][i] = tile_row(m, 4 * g + i) < rows ? v[m][n][i].value() : 0.0f;
+                for (int i = 0; i < 4; ++i) x[m][n][i] = tile_row(m, 4 * g + i) < rows ? (float)v[m][n][i] : 0.0f;
+    }
+    static __device__ __forceinline__ void store(Room&, T* __restrict__ base, unsigned stride, int rows, int col0, int dim, const Float4 (&x)[4][NT])
+    {
+        stride = afresh(stride);
+        const int g = (threadIdx.x & (kWave - 1)) >> 4, col = col0 + (threadIdx.x & 15);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            if (col + 16 * n >= dim) continue;
+            const unsigned lane_at = 8u * g * stride + (unsigned)(col + 16 * n);
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (tile_row(m, 4 * g + i) < rows) *(base + (unsigned)tile_row(m, i) * stride + lane_at) = (T)x[m][n][i];
+        }
     }
 };
-template <class T, int NT>
-__device__ __forceinline__ void store_columns(T* __restrict__ base, unsigned stride, int rows, int left, int m, const Float4 (&v)[NT])
-{
-    const int g = (threadIdx.x & (kWave - 1)) >> 4;
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        if (left <= 16 * n) continue;
-        T* const at = base + 16 * n;
-        const unsigned lane_at = 8u * g * stride;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (rows == kDeltaRows || tile_row(m, 4 * g + i) < rows) at[lane_at + (unsigned)tile_row(m, i) * stride] = (T)v[n][i];
-    }
-}
 
 // A wave's columns of a matrix [32 KT rows, of which `dim`] of floats.
 template <int KT, int NT>
-__device__ __forceinline__ void load_state(const float* __restrict__ base, unsigned stride, int dim, int left, Float4 (&s)[2 * KT][NT])
+__device__ __forceinline__ void load_state(const float* __restrict__ base, unsigned stride, int dim, int col, Float4 (&s)[2 * KT][NT])
 {
     const int g = (threadIdx.x & (kWave - 1)) >> 4;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const float* const at = base + (left > 16 * n ? 16 * n : left > 0 ? 0 : left - 1);
+        const unsigned c = (unsigned)(col + 16 * n < (int)stride ? col + 16 * n : (int)stride - 1);
 #pragma unroll
         for (int j = 0; j < 2 * KT; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int d = tile_row(j, 4 * g + i);
-                const float x = at[(unsigned)(d < dim ? d : dim - 1) * stride];
+                const float x = base[(size_t)(d < dim ? d : dim - 1) * stride + c];
                 s[j][n][i] = d < dim ? x : 0.0f;
             }
     }
 }
 template <int KT, int NT>
-__device__ __forceinline__ void store_state(float* __restrict__ base, unsigned stride, int dim, int left, const Float4 (&s)[2 * KT][NT])
+__device__ __forceinline__ void store_state(float* __restrict__ base, unsigned stride, int dim, int col, const Float4 (&s)[2 * KT][NT])
 {
+    stride = afresh(stride);
     const int g = (threadIdx.x & (kWave - 1)) >> 4;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        if (left <= 16 * n) continue;
+        if (col + 16 * n >= (int)stride) continue;
+        const unsigned lane_at = 8u * g * stride + (unsigned)(col + 16 * n);
 #pragma unroll
         for (int j = 0; j < 2 * KT; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int d = tile_row(j, 4 * g + i);
-                if (dim == 32 * KT || d < dim) base[(unsigned)d * stride + 16 * n] = s[j][n][i];
-            }
+            for (int i = 0; i < 4; ++i)
+                if (dim == 32 * KT || tile_row(j, 4 * g + i) < dim) *(base + (unsigned)tile_row(j, i) * stride + lane_at) = s[j][n][i];
     }
 }
 // 64 rows of floats, all of them.
 template <int NT>
-__device__ __forceinline__ void store_tile(float* __restrict__ base, unsigned stride, int left, int m, const Float4 (&v)[NT])
+__device__ __forceinline__ void store_tiles(float* __restrict__ base, unsigned stride, int col, const Float4 (&v)[4][NT])
 {
+    stride = afresh(stride);
     const int g = (threadIdx.x & (kWave - 1)) >> 4;
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-        if (left > 16 * n)
+    for (int n = 0; n < NT; ++n) {
+        if (col + 16 * n >= (int)stride) continue;
+        const unsigned lane_at = 8u * g * stride + (unsigned)(col + 16 * n);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) base[(unsigned)tile_row(m, 4 * g + i) * stride + 16 * n] = v[n][i];
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *(base + (unsigned)tile_row(m, i) * stride + lane_at) = v[m][n][i];
+    }
 }
 
 template <class T, int KT, int kParts>
@@ -263,15 +375,15 @@ struct Stage {
     {
         if constexpr (kAhead) {
             const int job = threadIdx.x, b = (job % kSquares) / kAcross, e = job % kAcross;
-            const bool query = job >= kSquares;
+            const bool query = kSquares % kWave == 0 ? __builtin_amdgcn_readfirstlane(job) >= kSquares : job >= kSquares;
             if (kBlock == 2 * kSquares || job < 2 * kSquares) {
                 load_square<T>(query ? qs : ks, query ? qstride : kstride, rows, dim, b, e, square);
                 load_scale(from.f, query, b, scale);
             }
 #pragma unroll
             for (int i = 0; i < kOfThread; ++i) {
-                const int at = i * kBlock + threadIdx.x;
-                block[i] = reinterpret_cast<const Float4*>(&from)[at < kVecs ? at : kVecs - 1];
+                const int behind = (i + 1) * kBlock - kVecs;      // threads of the last round that have none: copies of others
+                block[i] = *(reinterpret_cast<const Float4*>(&from) + (behind > 0 ? i * kBlock - behind : i * kBlock) + threadIdx.x);
             }
         }
     }
@@ -283,8 +395,8 @@ struct Stage {
             if (kBlock == 2 * kSquares || job < 2 * kSquares) put_square(room, job >= kSquares, (job % kSquares) / kAcross, job % kAcross, rows, dim, square, scale);
 #pragma unroll
             for (int i = 0; i < kOfThread; ++i) {
-                const int at = i * kBlock + threadIdx.x;
-                if (at < kVecs) to[at] = block[i];
+                const int behind = (i + 1) * kBlock - kVecs;
+                to[(behind > 0 ? i * kBlock - behind : i * kBlock) + (int)threadIdx.x] = block[i];
             }
         } else {
             put_now(room, from, ks, kstride, qs, qstride, rows, dim, 0, kOnePlace ? kSquares : 2 * kSquares);
@@ -573,15 +685,12 @@ __device__ __forceinline__ void store_operands(const float (&a)[kDeltaRows][kTri
         // lower: (0, 0) (1, 0) (2, 0) (2, 1) (3, 0) (3, 1); upper: (0, 0) (0, 1) (1, 0) (1, 1) (2, 1) (3, 1)
         const int m = kUpper ? (k < 4 ? k >> 1 : k - 2) : (k < 2 ? k : 1 + (k >> 1)), s = kUpper ? (k < 4 ? k & 1 : 1) : (k < 2 ? 0 : k & 1);
         const int row = tile_row(m, r), col = 32 * s + 8 * g;
-        Half8 hi, lo;
+        float v[8];
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            const float u = kUpper ? (col + i >= row ? a[col + i][row] : 0.0f) : col + i <= row ? a[row][col + i] : 0.0f;
-            const float v = kUpper ? (col + i + 1 >= row ? a[col + i + 1][row] : 0.0f) : col + i + 1 <= row ? a[row][col + i + 1] : 0.0f;
-            split2(u * to, v * to, hi, lo, i);
-        }
-        out[0][k][lane] = hi;
-        out[1][k][lane] = lo;
+        for (int i = 0; i < 8; ++i) v[i] = kUpper ? (col + i >= row ? a[col + i][row] : 0.0f) : col + i <= row ? a[row][col + i] : 0.0f;
+        const HalfPair p = split(v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7], to);
+        out[0][k][lane] = p.hi;
+        out[1][k][lane] = p.lo;
     }
 }
 
