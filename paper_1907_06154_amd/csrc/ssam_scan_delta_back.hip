@@ -193,29 +193,43 @@ __global__ __launch_bounds__(kBlock) void delta_back_walk(DeltaBackParams b)
 // ---- gradients of q, k, g and beta ----------------------------------------------------------------------------------------
 constexpr int kAcross = 128;               // values taken together
 constexpr int kAcrossSteps = kAcross / 32;
+constexpr int kRowWaves = 8, kRowThreads = kRowWaves * kWave;      // half the registers of sums a wave, and two of them on a SIMD
 
 template <class T, int KT>
 struct RowsRoom {
     static constexpr int kParts = kSplit<T> ? 2 : 1;
-    union {
-        struct {
-            Half8 keys[kParts][4 * KT][kDeltaRows], queries[kParts][4 * KT][kDeltaRows];      // 8 elements of every row
-        };
-        struct {                           // rows t (tile_row), 32 values
-            Half8 grad[kParts][4 * kAcrossSteps][kWave], x[2][4 * kAcrossSteps][kWave], u[2][4 * kAcrossSteps][kWave];
-        };
-        struct {
-            Half8 turned[kParts][4 * KT][kWave];
-            Half8 tri[4][2][kTriOperands][kWave];
-            float matrix[kDeltaRows][kTriStride];
-        };
+    static constexpr bool kKept = kParts * KT <= 4;      // q's and k's rows stay in LDS beside everything else
+    typedef Half8 Rows[kParts][4 * KT][kDeltaRows];      // 8 elements of every row
+    struct Operands {                                    // rows t (tile_row), 32 values
+        Half8 grad[kParts][4 * kAcrossSteps][kWave], x[2][4 * kAcrossSteps][kWave], u[2][4 * kAcrossSteps][kWave];
     };
+    struct Triangles {
+        Half8 turned[kParts][4 * KT][kWave];
+        Half8 tri[4][2][kTriOperands][kWave];
+        float matrix[kDeltaRows][kTriStride];
+    };
+    struct Both {
+        Rows keys, queries;
+    };
+    struct Nothing {};
+    union {
+        std::conditional_t<kKept, Nothing, Both> first;
+        Operands o;
+        Triangles t;
+    };
+    std::conditional_t<kKept, Both, Nothing> kept;
     double sum[kDeltaRows];
     float back[3][kDeltaRows];             // powers of two of grad's, x's and u's rows
     float up[kDeltaRows], rest[kDeltaRows], beta[kDeltaRows], dbeta[kDeltaRows];
     float key[kDeltaRows], query[kDeltaRows], key_back[kDeltaRows], query_back[kDeltaRows];
-    float dots[2][kWavesPerBlock][kDeltaRows], pairs[kWavesPerBlock][kDeltaRows];
-    float most[2][kWavesPerBlock], inner[kWavesPerBlock], total;
+    float dots[2][kRowWaves][kDeltaRows], pairs[kRowWaves][kDeltaRows];
+    float most[2][kRowWaves], inner[kRowWaves], total;
+
+    __device__ __forceinline__ Both& rows()
+    {
+        if constexpr (kKept) return kept;
+        else return first;
+    }
 };
 
 // Tile and row in it of row t: the inverse of tile_row.
@@ -230,7 +244,7 @@ __device__ __forceinline__ float over_16(float v)
 }
 
 // Rows' sums over the lanes and waves of v[m][i], what a lane has for row tile_row(m, 4 g + i); to be read after a barrier.
-__device__ __forceinline__ void put_dots(const float (&v)[4][4], float (&to)[kWavesPerBlock][kDeltaRows])
+__device__ __forceinline__ void put_dots(const float (&v)[4][4], float (&to)[kRowWaves][kDeltaRows])
 {
     const int lane = threadIdx.x & (kWave - 1), g = lane >> 4;
 #pragma unroll
@@ -241,36 +255,120 @@ __device__ __forceinline__ void put_dots(const float (&v)[4][4], float (&to)[kWa
             if ((lane & 15) == 0) to[threadIdx.x >> 6][tile_row(m, 4 * g + i)] = s;
         }
 }
-__device__ __forceinline__ float dot_of(const float (&from)[kWavesPerBlock][kDeltaRows], int t)
+__device__ __forceinline__ float dot_of(const float (&from)[kRowWaves][kDeltaRows], int t)
 {
     float s = from[0][t];
 #pragma unroll
-    for (int w = 1; w < kWavesPerBlock; ++w) s += from[w][t];
+    for (int w = 1; w < kRowWaves; ++w) s += from[w][t];
     return s;
 }
 
-template <class T, int KT>
-__global__ __launch_bounds__(kBlock) void delta_back_rows(DeltaBackParams b)
+// dO, dY and R of a block's rows, 8 of kAcross values a lane, 16 lanes a row.
+template <class T>
+struct RowData {
+    static constexpr int kPasses = kDeltaRows * 16 / kRowThreads;
+    RowVec<T, 8> o[kPasses];
+    RowVec<float, 8> y[kPasses], u[kPasses];
+
+    __device__ __forceinline__ void load(const T* dos, unsigned stride, const float* ys, const float* us, int dim, int rows, int v0)
+    {
+        const int at = v0 + 8 * (int)(threadIdx.x & 15), have = dim - at;
+        const unsigned c = have > 0 ? at : 0;
+        if (dim % 8 == 0) {
+#pragma unroll
+            for (int k = 0; k < kPasses; ++k) {
+                const int t = (int)(threadIdx.x >> 4) + k * (kRowThreads / 16);
+                __builtin_memcpy(&o[k], dos + (unsigned)(t < rows ? t : rows - 1) * stride + c, sizeof(o[k]));
+                __builtin_memcpy(&y[k], ys + (unsigned)(t * dim) + c, sizeof(y[k]));
+                __builtin_memcpy(&u[k], us + (unsigned)(t * dim) + c, sizeof(u[k]));
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < kPasses; ++k) {
+                const int t = (int)(threadIdx.x >> 4) + k * (kRowThreads / 16);
+                o[k] = load_row_vec<T, 8>(dos + (unsigned)(t < rows ? t : rows - 1) * stride + c, have > 0 ? have : dim);
+                y[k] = load_row_vec<float, 8>(ys + (unsigned)(t * dim) + c, have > 0 ? have : dim);
+                u[k] = load_row_vec<float, 8>(us + (unsigned)(t * dim) + c, have > 0 ? have : dim);
+            }
+        }
+    }
+};
+// Some of a state's rows, 8 of 32 values a lane and step.
+struct StateRow {
+    RowVec<float, 8> v[kAcrossSteps];
+    __device__ __forceinline__ void load(const float* state, int d, int key_dim, int dim, int v0)
+    {
+        const int g = (threadIdx.x & (kWave - 1)) >> 4;
+        const float* const row = state + (size_t)(d < key_dim ? d : key_dim - 1) * dim;
+#pragma unroll
+        for (int s = 0; s < kAcrossSteps; ++s) {
+            const int at = v0 + 32 * s + 8 * g, have = dim - at;
+            if (dim % 8 == 0) __builtin_memcpy(&v[s], row + (have > 0 ? at : 0), 32);
+            else v[s] = load_row_vec<float, 8>(row + (have > 0 ? at : 0), have > 0 ? have : dim);
+        }
+    }
+    __device__ __forceinline__ float clear(int d, int key_dim, int dim, int v0)      // and the largest magnitude
+    {
+        const int g = (threadIdx.x & (kWave - 1)) >> 4;
+        float m = 0.0f;
+#pragma unroll
+        for (int s = 0; s < kAcrossSteps; ++s) {
+            if (!(d < key_dim && v0 + 32 * s + 8 * g < dim)) v[s] = RowVec<float, 8>(0.0f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = larger(m, v[s][i]);
+        }
+        return m;
+    }
+};
+
+// kShared: several heads share a key, whose gradients are summed.
+template <class T, int KT, bool kShared>
+__global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b)
 {
     const DeltaParams& p = b.f;
-    constexpr int kParts = kSplit<T> ? 2 : 1, kTiles = (2 * KT + kWavesPerBlock - 1) / kWavesPerBlock;      // of a wave, along the keys
-    __shared__ RowsRoom<T, KT> room;
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, g = lane >> 4, r = lane & 15, many = p.heads / p.key_heads;
-    const int slot = (int)(blockIdx.x / p.key_heads), key_head = (int)(blockIdx.x % p.key_heads);
+    typedef RowsRoom<T, KT> Room;
+    constexpr int kParts = kSplit<T> ? 2 : 1, kTiles = (2 * KT + kRowWaves - 1) / kRowWaves;      // of a wave, along the keys
+    __shared__ Room room;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int lane = tid & (kWave - 1), g = lane >> 4, r = lane & 15;
+    const int slot = (int)(blockIdx.x / p.key_heads), key_head = (int)(blockIdx.x % p.key_heads), many = kShared ? p.heads / p.key_heads : 1;
     const Piece piece = find_piece(p.pieces, slot);
     if (piece.seq < 0 || piece.n <= 0) return;
     const T* const ks = sequence_base<const T>(p.k, p.pieces, piece) + piece.row0 * p.k.row + key_head * p.k_head;
     const T* const qs = sequence_base<const T>(p.q, p.pieces, piece) + piece.row0 * p.q.row + key_head * p.q_head;
+    RowData<T> data;
+    const int tile = wave & 3, col0 = wave >> 2 << 1;      // of the 64 x 64 products: a wave's tile of rows and its two of columns
+    Float4 kk[2], qk[2];                      // K K^T and Q K^T
     {
-        RowLoad<T, KT> k, q;
+        RowLoad<T, KT, kRowThreads> k, q;
         k.load(ks, (unsigned)p.k.row, piece.n, p.key_dim);
         q.load(qs, (unsigned)p.q.row, piece.n, p.key_dim);
-        k.put(p.unit, piece.n, p.key_dim, room.keys, room.key_back, room.key);
-        q.put(p.unit, piece.n, p.key_dim, room.queries, room.query_back, room.query);
+        k.put(p.unit, piece.n, p.key_dim, room.rows().keys, room.key_back, room.key);
+        q.put(p.unit, piece.n, p.key_dim, room.rows().queries, room.query_back, room.query);
     }
     __syncthreads();
-    Float4 kk[4], qk[4];                      // K K^T and Q K^T, tile w's rows in wave w
-    key_products<T, KT, true>(room.keys, room.queries, kk, qk);
+    if constexpr (!Room::kKept) key_products<T, KT, true, 2>(room.rows().keys, room.rows().queries, tile, col0, kk, qk);
+    // Elements of the key's or query's row t that the wave's tiles have, as the rule takes them.
+    auto row_elements = [&](bool query, int t, float (&v)[kTiles]) {
+        const float per = query ? room.query_back[t] : room.key_back[t];
+#pragma unroll
+        for (int jj = 0; jj < kTiles; ++jj) {
+            const int d = tile_row(wave * kTiles + jj, r);
+            if constexpr (Room::kKept) {
+                v[jj] = 0.0f;
+                if (wave * kTiles + jj >= 2 * KT) continue;
+                const auto& from = query ? room.rows().queries : room.rows().keys;
+                auto element = [&](const Half8& eight) { return (float)reinterpret_cast<const _Float16*>(&eight)[d & 7]; };
+                v[jj] = element(from[0][d >> 3][t ^ (d >> 3 & 15)]);
+                if constexpr (kParts > 1) v[jj] += element(from[1][d >> 3][t ^ (d >> 3 & 15)]);
+                v[jj] *= per;
+            } else {
+                const T* const x = query ? qs : ks;
+                const float e = (float)x[(unsigned)(t < piece.n ? t : piece.n - 1) * (unsigned)(query ? p.q.row : p.k.row) + (unsigned)(d < p.key_dim ? d : p.key_dim - 1)];
+                v[jj] = t < piece.n && d < p.key_dim ? e * (per * (query ? room.query[t] : room.key[t])) : 0.0f;
+            }
+        }
+    };
     Float4 dq[4][kTiles], dk[4][kTiles];      // sums over the heads that share the key
 #pragma unroll
     for (int m = 0; m < 4; ++m)
@@ -278,6 +376,12 @@ __global__ __launch_bounds__(kBlock) void delta_back_rows(DeltaBackParams b)
         for (int j = 0; j < kTiles; ++j) dq[m][j] = dk[m][j] = Float4(0.0f);
 
     for (int h = key_head * many; h < (key_head + 1) * many; ++h) {
+        asm volatile("" : "+v"(lane), "+v"(g), "+v"(r));       // a head's addresses are made for it, not kept over all of them
+        const float* const mark = mark_of(p.marks, p, slot, h);
+        const float* const behind = mark_of(b.behind, p, slot, h);
+        const T* const dos = sequence_base<const T>(b.grad_out, p.pieces, piece) + piece.row0 * b.grad_out.row + h * b.grad_out_head;
+        const size_t below = (size_t)p.key_dim * p.value_dim;
+        data.load(dos, (unsigned)b.grad_out.row, behind + below, mark + below, p.value_dim, piece.n, 0);
         __syncthreads();
         if (wave == 0) {
             const bool there = lane < piece.n;
@@ -299,220 +403,212 @@ __global__ __launch_bounds__(kBlock) void delta_back_rows(DeltaBackParams b)
             room.rest[lane] = exp2_fast(kLog2e * (float)(all - sum));
             if (lane == 0) room.total = exp2_fast(kLog2e * (float)all);
         }
-        const float* mark = mark_of(p.marks, p, slot, h);
-        const float* behind = mark_of(b.behind, p, slot, h);
-        const T* dos = sequence_base<const T>(b.grad_out, p.pieces, piece) + piece.row0 * b.grad_out.row + h * b.grad_out_head;
-        Float4 asked[4][kTiles], reads[4][kTiles], last[4][kTiles], pd[4], nd[4];
+        Float4 asked[4][kTiles], reads[4][kTiles], last[4][kTiles], pd[2], nd[2];
         float inner = 0.0f;
 #pragma unroll
         for (int m = 0; m < 4; ++m) {
-            pd[m] = nd[m] = Float4(0.0f);
+            pd[m & 1] = nd[m & 1] = Float4(0.0f);
 #pragma unroll
             for (int j = 0; j < kTiles; ++j) asked[m][j] = reads[m][j] = last[m][j] = Float4(0.0f);
         }
         for (int v0 = 0; v0 < p.value_dim; v0 += kAcross) {
+            if (v0) data.load(dos, (unsigned)b.grad_out.row, behind + below, mark + below, p.value_dim, piece.n, v0);
             __syncthreads();
-            // dO, dX = b dY and U = b R as operands, 16 lanes a row
-            {
-                const int e = tid & 15, at = v0 + 8 * e, have = p.value_dim - at;
+            // dO, dX = b dY and U = b R as operands
+            const int e = tid & 15;
+            const bool across = v0 + 8 * e < p.value_dim;
 #pragma unroll
-                for (int t = tid >> 4; t < kDeltaRows; t += kBlock / 16) {
-                    const float beta = room.beta[t];
-                    const RowVec<T, 8> o = t < piece.n && have > 0 ? load_row_vec<T, 8>(dos + (long long)t * b.grad_out.row + at, have) : RowVec<T, 8>(T(0));
-                    const long long row = (long long)(p.key_dim + t) * p.value_dim + at;
-                    RowVec<float, 8> y(0.0f), u(0.0f);
-                    if (have > 0) {
-                        y = load_row_vec<float, 8>(behind + row, have);
-                        u = load_row_vec<float, 8>(mark + row, have);
-                    }
-                    float dot = 0.0f, mo = 0.0f, mx = 0.0f, mu = 0.0f;
+            for (int k = 0; k < RowData<T>::kPasses; ++k) {
+                const int t = (tid >> 4) + k * (kRowThreads / 16);
+                const float beta = room.beta[t];
+                RowVec<T, 8>& o = data.o[k];
+                RowVec<float, 8>&y = data.y[k], &u = data.u[k];
+                if (!across || t >= piece.n) o = RowVec<T, 8>(T(0));
+                if (!across) y = u = RowVec<float, 8>(0.0f);
+                float dot = 0.0f, mo = 0.0f, mx = 0.0f, mu = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        dot = __builtin_fmaf(y[i], u[i], dot);
-                        y[i] *= beta;
-                        u[i] *= beta;
-                        mo = larger(mo, (float)o[i]);
-                        mx = larger(mx, y[i]);
-                        mu = larger(mu, u[i]);
-                    }
-#pragma unroll
-                    for (int x = 1; x < 16; x *= 2) {
-                        dot += __shfl_xor(dot, x);
-                        mo = __builtin_fmaxf(mo, __shfl_xor(mo, x));
-                        mx = __builtin_fmaxf(mx, __shfl_xor(mx, x));
-                        mu = __builtin_fmaxf(mu, __shfl_xor(mu, x));
-                    }
-                    Scale so(mo);
-                    const Scale sx(mx), su(mu);
-                    if (__is_same(T, _Float16)) so.to = so.back = 1.0f;
-                    if (e == 0) {
-                        room.back[0][t] = so.back;
-                        room.back[1][t] = sx.back;
-                        room.back[2][t] = su.back;
-                        room.dbeta[t] += dot;
-                    }
-                    const int operand = tile_of(t) * kAcrossSteps + (e >> 2), entry = row_entry(e >> 2, e & 3, row_in_tile(t));
-                    Half8 hi, lo;
-                    to_halves<T>(o, so.to, hi, lo);
-                    room.grad[0][operand][entry] = hi;
-                    if constexpr (kParts > 1) room.grad[1][operand][entry] = lo;
-                    to_halves<float>(y, sx.to, hi, lo);
-                    room.x[0][operand][entry] = hi;
-                    room.x[1][operand][entry] = lo;
-                    to_halves<float>(u, su.to, hi, lo);
-                    room.u[0][operand][entry] = hi;
-                    room.u[1][operand][entry] = lo;
+                for (int i = 0; i < 8; ++i) {
+                    dot = __builtin_fmaf(y[i], u[i], dot);
+                    y[i] *= beta;
+                    u[i] *= beta;
+                    mo = larger(mo, (float)o[i]);
+                    mx = larger(mx, y[i]);
+                    mu = larger(mu, u[i]);
                 }
+#pragma unroll
+                for (int x = 1; x < 16; x *= 2) {
+                    dot += __shfl_xor(dot, x);
+                    mo = __builtin_fmaxf(mo, __shfl_xor(mo, x));
+                    mx = __builtin_fmaxf(mx, __shfl_xor(mx, x));
+                    mu = __builtin_fmaxf(mu, __shfl_xor(mu, x));
+                }
+                Scale so(mo);
+                const Scale sx(mx), su(mu);
+                if (__is_same(T, _Float16)) so.to = so.back = 1.0f;
+                if (e == 0) {
+                    room.back[0][t] = so.back;
+                    room.back[1][t] = sx.back;
+                    room.back[2][t] = su.back;
+                    room.dbeta[t] += dot;
+                }
+                const int operand = tile_of(t) * kAcrossSteps + (e >> 2), entry = row_entry(e >> 2, e & 3, row_in_tile(t));
+                Half8 hi, lo;
+                to_halves<T>(o, so.to, hi, lo);
+                room.o.grad[0][operand][entry] = hi;
+                if constexpr (kParts > 1) room.o.grad[1][operand][entry] = lo;
+                to_halves<float>(y, sx.to, hi, lo);
+                room.o.x[0][operand][entry] = hi;
+                room.o.x[1][operand][entry] = lo;
+                to_halves<float>(u, su.to, hi, lo);
+                room.o.u[0][operand][entry] = hi;
+                room.o.u[1][operand][entry] = lo;
             }
+            StateRow s0, s1;
+            s0.load(mark, tile_row(wave * kTiles, r), p.key_dim, p.value_dim, v0);
+            s1.load(behind, tile_row(wave * kTiles, r), p.key_dim, p.value_dim, v0);
             __syncthreads();
             auto operand = [&](const Half8 (&a)[4 * kAcrossSteps][kWave], int m, int s) { return a[m * kAcrossSteps + s][row_entry(s, g, r)]; };
-            // dO U^T and dX U^T: wave w has tile w's rows
+            // dO U^T and dX U^T
 #pragma unroll
-            for (int n = 0; n < 4; ++n)
-                if (n <= (wave | 1)) {
+            for (int k0 = 0; k0 < 2; ++k0)
+                if (const int n = col0 + k0; n <= (tile | 1)) {
                     Float4 a(0.0f), c(0.0f);
 #pragma unroll
                     for (int s = 0; s < kAcrossSteps; ++s) {
-                        const Half8 uh = operand(room.u[0], n, s), ul = operand(room.u[1], n, s), xh = operand(room.x[0], wave, s);
+                        const Half8 uh = operand(room.o.u[0], n, s), ul = operand(room.o.u[1], n, s), xh = operand(room.o.x[0], tile, s);
 #pragma unroll
                         for (int k = 0; k < kParts; ++k) {
-                            const Half8 o = operand(room.grad[k], wave, s);
+                            const Half8 o = operand(room.o.grad[k], tile, s);
                             a = mfma(o, uh, a);
                             if (k == 0) a = mfma(o, ul, a);
                         }
                         c = mfma(xh, uh, c);
                         c = mfma(xh, ul, c);
-                        c = mfma(operand(room.x[1], wave, s), uh, c);
+                        c = mfma(operand(room.o.x[1], tile, s), uh, c);
                     }
                     const float col = room.back[2][tile_row(n, r)];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int t = tile_row(wave, 4 * g + i);
-                        pd[n][i] += a[i] * (room.back[0][t] * col);
-                        nd[n][i] += c[i] * (room.back[1][t] * col);
-                    }
+                    const Float4 ro = *reinterpret_cast<const Float4*>(&room.back[0][tile_row(tile, 4 * g)]), rx = *reinterpret_cast<const Float4*>(&room.back[1][tile_row(tile, 4 * g)]);
+                    pd[k0] += a * (ro * col);
+                    nd[k0] += c * (rx * col);
                 }
+            in_order();
             // dO S0^T, dX S0^T and U dS1^T: a wave has some of the keys' elements, for all rows
 #pragma unroll
             for (int jj = 0; jj < kTiles; ++jj) {
                 const int j = wave * kTiles + jj, d = tile_row(j, r);
-                if (j >= 2 * KT) continue;
-                const bool there = d < p.key_dim;
-                RowVec<float, 8> s0[kAcrossSteps], s1[kAcrossSteps];
-                float m0 = 0.0f, m1 = 0.0f;
+                if (jj) in_order();
+                const float m0 = s0.clear(j < 2 * KT ? d : p.key_dim, p.key_dim, p.value_dim, v0), m1 = s1.clear(j < 2 * KT ? d : p.key_dim, p.key_dim, p.value_dim, v0);
 #pragma unroll
-                for (int s = 0; s < kAcrossSteps; ++s) {
-                    const int at = v0 + 32 * s + 8 * g, have = p.value_dim - at;
-                    s0[s] = s1[s] = RowVec<float, 8>(0.0f);
-                    if (there && have > 0) {
-                        s0[s] = load_row_vec<float, 8>(mark + (long long)d * p.value_dim + at, have);
-                        s1[s] = load_row_vec<float, 8>(behind + (long long)d * p.value_dim + at, have);
-                    }
+                for (int s = 0; s < kAcrossSteps; ++s)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        inner = __builtin_fmaf(s0[s][i], s1[s][i], inner);
-                        m0 = larger(m0, s0[s][i]);
-                        m1 = larger(m1, s1[s][i]);
-                    }
-                }
+                    for (int i = 0; i < 8; ++i) inner = __builtin_fmaf(s0.v[s][i], s1.v[s][i], inner);
                 const Scale by0(over_column(m0)), by1(over_column(m1));
-                Float4 a[4], c[4], w[4];
-#pragma unroll
-                for (int m = 0; m < 4; ++m) a[m] = c[m] = w[m] = Float4(0.0f);
+                HalfPair h0[kAcrossSteps], h1[kAcrossSteps];
 #pragma unroll
                 for (int s = 0; s < kAcrossSteps; ++s) {
-                    Half8 h0, l0, h1, l1;
-                    to_halves<float>(s0[s], by0.to, h0, l0);
-                    to_halves<float>(s1[s], by1.to, h1, l1);
+                    to_halves<float>(s0.v[s], by0.to, h0[s].hi, h0[s].lo);
+                    to_halves<float>(s1.v[s], by1.to, h1[s].hi, h1[s].lo);
+                }
+                if (jj + 1 < kTiles) {
+                    s0.load(mark, tile_row(j + 1, r), p.key_dim, p.value_dim, v0);
+                    s1.load(behind, tile_row(j + 1, r), p.key_dim, p.value_dim, v0);
+                }
+                in_order();
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) {
+                for (int m = 0; m < 4; ++m) {
+                    if (m) in_order();
+                    Float4 a(0.0f), c(0.0f), w(0.0f);
+#pragma unroll
+                    for (int s = 0; s < kAcrossSteps; ++s) {
+                        const Half8 xh = operand(room.o.x[0], m, s), uh = operand(room.o.u[0], m, s);
+                        c = mfma(xh, h0[s].hi, c);
+                        w = mfma(uh, h1[s].hi, w);
 #pragma unroll
                         for (int k = 0; k < kParts; ++k) {
-                            const Half8 o = operand(room.grad[k], m, s);
-                            a[m] = mfma(o, h0, a[m]);
-                            if (k == 0) a[m] = mfma(o, l0, a[m]);
+                            const Half8 o = operand(room.o.grad[k], m, s);
+                            a = mfma(o, h0[s].hi, a);
+                            if (k == 0) a = mfma(o, h0[s].lo, a);
                         }
-                        const Half8 xh = operand(room.x[0], m, s), uh = operand(room.u[0], m, s);
-                        c[m] = mfma(xh, h0, c[m]);
-                        c[m] = mfma(xh, l0, c[m]);
-                        c[m] = mfma(operand(room.x[1], m, s), h0, c[m]);
-                        w[m] = mfma(uh, h1, w[m]);
-                        w[m] = mfma(uh, l1, w[m]);
-                        w[m] = mfma(operand(room.u[1], m, s), h1, w[m]);
+                        c = mfma(xh, h0[s].lo, c);
+                        w = mfma(uh, h1[s].lo, w);
+                        c = mfma(operand(room.o.x[1], m, s), h0[s].hi, c);
+                        w = mfma(operand(room.o.u[1], m, s), h1[s].hi, w);
                     }
+                    const int t0 = tile_row(m, 4 * g);
+                    const Float4 up = *reinterpret_cast<const Float4*>(&room.up[t0]), rest = *reinterpret_cast<const Float4*>(&room.rest[t0]);
+                    const Float4 ro = *reinterpret_cast<const Float4*>(&room.back[0][t0]), rx = *reinterpret_cast<const Float4*>(&room.back[1][t0]),
+                                 ru = *reinterpret_cast<const Float4*>(&room.back[2][t0]);
+                    asked[m][jj] += a * (up * ro * (p.scale * by0.back));
+                    reads[m][jj] -= c * (up * rx * by0.back);
+                    last[m][jj] += w * (rest * ru * by1.back);
                 }
-#pragma unroll
-                for (int m = 0; m < 4; ++m)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int t = tile_row(m, 4 * g + i);
-                        const float up = room.up[t];
-                        asked[m][jj][i] += a[m][i] * (p.scale * up * room.back[0][t] * by0.back);
-                        reads[m][jj][i] -= c[m][i] * (up * room.back[1][t] * by0.back);
-                        last[m][jj][i] += w[m][i] * (room.rest[t] * room.back[2][t] * by1.back);
-                    }
             }
         }
         // what the rows' decays have of S0, of dS1 and of one another's products
-        float dots[4][4], lasts[4][4];
-        auto element = [&](const T* x, long long stride, int t, int d) { return t < piece.n && d < p.key_dim ? (float)x[(long long)t * stride + d] : 0.0f; };
+        {
+            float dots[4][4], lasts[4][4];
 #pragma unroll
-        for (int m = 0; m < 4; ++m)
+            for (int m = 0; m < 4; ++m)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = tile_row(m, 4 * g + i);
-                const float per_key = room.key[t] * room.key_back[t], per_query = room.query[t] * room.query_back[t];
-                float s = 0.0f, l = 0.0f;
+                for (int i = 0; i < 4; ++i) {
+                    const int t = tile_row(m, 4 * g + i);
+                    float k[kTiles], q[kTiles], s = 0.0f, l = 0.0f;
+                    row_elements(false, t, k);
+                    row_elements(true, t, q);
 #pragma unroll
-                for (int jj = 0; jj < kTiles; ++jj) {
-                    const int d = tile_row(wave * kTiles + jj, r);
-                    if (wave * kTiles + jj >= 2 * KT) continue;
-                    const float k = element(ks, p.k.row, t, d) * per_key;
-                    s = __builtin_fmaf(element(qs, p.q.row, t, d) * per_query, asked[m][jj][i], s);
-                    s = __builtin_fmaf(k, reads[m][jj][i], s);
-                    l = __builtin_fmaf(k, last[m][jj][i], l);
+                    for (int jj = 0; jj < kTiles; ++jj) {
+                        s = __builtin_fmaf(q[jj], asked[m][jj][i], s);
+                        s = __builtin_fmaf(k[jj], reads[m][jj][i], s);
+                        l = __builtin_fmaf(k[jj], last[m][jj][i], l);
+                    }
+                    dots[m][i] = s;
+                    lasts[m][i] = l;
                 }
-                dots[m][i] = s;
-                lasts[m][i] = l;
-            }
-        put_dots(dots, room.dots[0]);
-        put_dots(lasts, room.dots[1]);
+            put_dots(dots, room.dots[0]);
+            put_dots(lasts, room.dots[1]);
+        }
 #pragma unroll
         for (int x = 1; x < kWave; x *= 2) inner += __shfl_xor(inner, x);
         if (lane == 0) room.inner[wave] = inner;
-        __syncthreads();                          // room.matrix lies over the operands
+        if constexpr (Room::kKept) key_products<T, KT, true, 2>(room.rows().keys, room.rows().queries, tile, col0, kk, qk);
+        __syncthreads();                          // the matrix lies over the operands
+        // dP and dA without their keys' and queries' factors: in place
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
+        for (int n = 0; n < 2; ++n)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int row = tile_row(wave, 4 * g + i), col = tile_row(n, r);
-                float v = 0.0f;
-                if (col < row) {
-                    const float d = exp2_fast(kLog2e * (float)(room.sum[row] - room.sum[col])) * room.key_back[col];
-                    v = d * (p.scale * pd[n][i] * qk[n][i] * room.query_back[row] - nd[n][i] * kk[n][i] * room.key_back[row]);
-                }
-                room.matrix[row][col] = v;
+                const int row = tile_row(tile, 4 * g + i), col = tile_row(col0 + n, r);
+                const float d = col <= row ? exp2_fast(kLog2e * (float)(room.sum[row] - room.sum[col])) : 0.0f;
+                pd[n][i] = col <= row ? p.scale * pd[n][i] * d : 0.0f;
+                nd[n][i] = col < row ? -nd[n][i] * d : 0.0f;
+                const float both = pd[n][i] * qk[n][i] * room.query_back[row] + nd[n][i] * kk[n][i] * room.key_back[row];
+                room.t.matrix[row][col] = col < row ? both * room.key_back[col] : 0.0f;
             }
         __syncthreads();
-        {                                         // each row's sums up to a column: 16 columns a lane, then the lanes before it
-            const int row = 16 * wave + r;
-            float s = 0.0f;
+        {                                         // each row's sums up to a column: 8 columns a lane, then the lanes before it
+            const int row = 8 * wave + (lane & 7), part = lane >> 3;
+            float s = 0.0f, before = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s += room.matrix[row][16 * g + i];
-                room.matrix[row][16 * g + i] = s;
+            for (int i = 0; i < 8; ++i) {
+                s += room.t.matrix[row][8 * part + i];
+                room.t.matrix[row][8 * part + i] = s;
             }
-            const float s0 = __shfl(s, r), s1 = __shfl(s, r + 16), s2 = __shfl(s, r + 32);
-            const float before = g == 0 ? 0.0f : g == 1 ? s0 : g == 2 ? s0 + s1 : s0 + s1 + s2;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) room.matrix[row][16 * g + i] += before;
+            for (int k = 0; k < 7; ++k) {
+                const float one = __shfl(s, 8 * k + (lane & 7));
+                if (k < part) before += one;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) room.t.matrix[row][8 * part + i] += before;
         }
         __syncthreads();
         {
             float s = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (16 * wave + i >= lane && lane > 0) s += room.matrix[16 * wave + i][lane - 1];
+            for (int i = 0; i < 8; ++i) {
+                const float v = room.t.matrix[8 * wave + i][lane > 0 ? lane - 1 : 0];
+                if (8 * wave + i >= lane && lane > 0) s += v;
+            }
             room.pairs[wave][lane] = s;
         }
         __syncthreads();
@@ -525,49 +621,57 @@ __global__ __launch_bounds__(kBlock) void delta_back_rows(DeltaBackParams b)
                 if (lane >= x) up_to += c;
             }
             const float before = __shfl_up(up_to, 1);
-            const float dg = dot_of(room.pairs, lane) + from + (lane ? before : 0.0f) + room.total * ((room.inner[0] + room.inner[1]) + (room.inner[2] + room.inner[3]));
+            float inner_ = room.inner[0];
+#pragma unroll
+            for (int w = 1; w < kRowWaves; ++w) inner_ += room.inner[w];
+            const float dg = dot_of(room.pairs, lane) + from + (lane ? before : 0.0f) + room.total * inner_;
             const long long at = piece.row0 + lane;
             if (lane < piece.n) {
                 if (b.grad_g.d) sequence_base<float>(b.grad_g, p.pieces, piece)[at * b.grad_g.row + h] = dg;
                 if (b.grad_beta.d) sequence_base<float>(b.grad_beta, p.pieces, piece)[at * b.grad_beta.row + h] = room.dbeta[lane];
             }
         }
-        // dP and dA as operands: their columns, transposed their rows, with the factor of the key or query that they meet
+        // as operands: their columns, transposed their rows, with the factor of the key or query that they meet
         float back[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            __syncthreads();
+            if (k) __syncthreads();
             float most = 0.0f;
 #pragma unroll
-            for (int n = 0; n < 4; ++n)
+            for (int n = 0; n < 2; ++n)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int row = tile_row(wave, 4 * g + i), col = tile_row(n, r);
-                    float v = 0.0f;
-                    if (k % 2 ? col < row : col <= row) {
-                        const float d = exp2_fast(kLog2e * (float)(room.sum[row] - room.sum[col]));
-                        v = (k % 2 ? -nd[n][i] : p.scale * pd[n][i]) * d * (k < 2 ? room.key_back[col] : k == 2 ? room.query_back[row] : room.key_back[row]);
-                    }
+                    const int row = tile_row(tile, 4 * g + i), col = tile_row(col0 + n, r);
+                    const float v = (k % 2 ? nd[n][i] : pd[n][i]) * (k < 2 ? room.key_back[col] : k == 2 ? room.query_back[row] : room.key_back[row]);
                     most = larger(most, v);
-                    room.matrix[row][col] = v;
+                    room.t.matrix[row][col] = v;
                 }
-            const Scale by(over_block(most, room.most[k % 2]));
+            const Scale by(over_block<kRowWaves>(most, room.most[k % 2]));
             back[k] = by.back;
-            if (k < 2) store_operands<false>(room.matrix, by.to, room.tri[k]);
-            else store_operands<true>(room.matrix, by.to, room.tri[k]);
+            if (k < 2) store_operands<false, kRowWaves>(room.t.matrix, by.to, room.t.tri[k]);
+            else store_operands<true, kRowWaves>(room.t.matrix, by.to, room.t.tri[k]);
         }
 #pragma unroll
         for (int query = 0; query < 2; ++query) {
             if (query) __syncthreads();
-            for (int job = tid; job < 32 * KT; job += kBlock) {
+            for (int job = tid; job < 32 * KT; job += kRowThreads) {
                 const int sq = job / (4 * KT), e = job % (4 * KT);
-                RowVec<T, 8> v[8];
-                load_square<T>(query ? qs : ks, (unsigned)(query ? p.q.row : p.k.row), piece.n, p.key_dim, sq, e, v);
-                clear_eights<T, 8>(8 * sq, 1, piece.n, e, p.key_dim, v);
                 Half8 hi[8], lo[8];
+                if constexpr (Room::kKept) {
+                    const auto& from = query ? room.rows().queries : room.rows().keys;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) to_halves<T>(v[i], __is_same(T, _Float16) ? 1.0f : (query ? room.query : room.key)[8 * sq + i], hi[i], lo[i]);
-                put_turned<T, KT>(hi, lo, sq, e, room.turned);
+                    for (int i = 0; i < 8; ++i) {
+                        hi[i] = from[0][e][(8 * sq + i) ^ (e & 15)];
+                        if constexpr (kParts > 1) lo[i] = from[1][e][(8 * sq + i) ^ (e & 15)];
+                    }
+                } else {
+                    RowVec<T, 8> v[8];
+                    load_square<T>(query ? qs : ks, (unsigned)(query ? p.q.row : p.k.row), piece.n, p.key_dim, sq, e, v);
+                    clear_eights<T, 8>(8 * sq, 1, piece.n, e, p.key_dim, v);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) to_halves<T>(v[i], __is_same(T, _Float16) ? 1.0f : (query ? room.query : room.key)[8 * sq + i], hi[i], lo[i]);
+                }
+                put_turned<T, KT>(hi, lo, sq, e, room.t.turned);
             }
             __syncthreads();
 #pragma unroll
@@ -577,23 +681,27 @@ __global__ __launch_bounds__(kBlock) void delta_back_rows(DeltaBackParams b)
                 HalfPair f[2][1];
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
-                    f[s][0].hi = turned_of<KT>(room.turned[0], j, s, lane);
-                    f[s][0].lo = kParts > 1 ? turned_of<KT>(room.turned[kParts - 1], j, s, lane) : Half8((_Float16)0.0f);
+                    f[s][0].hi = turned_of<KT>(room.t.turned[0], j, s, lane);
+                    f[s][0].lo = kParts > 1 ? turned_of<KT>(room.t.turned[kParts - 1], j, s, lane) : Half8((_Float16)0.0f);
                 }
+                in_order();
+                Float4 a[4][1];
+                if (!query) {
+                    tri_products<1, false, kParts == 1>(room.t.tri[0], lane, f, a);
 #pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    Float4 a[1];
-                    if (!query) {
-                        tri_product<1, false>(room.tri[0], m, lane, f, a);
-                        asked[m][jj] += a[0] * back[0];
-                        tri_product<1, false>(room.tri[1], m, lane, f, a);
-                        reads[m][jj] += a[0] * back[1];
-                        tri_product<1, true>(room.tri[3], m, lane, f, a);
-                        last[m][jj] += a[0] * back[3];
-                    } else {
-                        tri_product<1, true>(room.tri[2], m, lane, f, a);
-                        last[m][jj] += a[0] * back[2];
-                    }
+                    for (int m = 0; m < 4; ++m) asked[m][jj] += a[m][0] * back[0];
+                    in_order();
+                    tri_products<1, false, kParts == 1>(room.t.tri[1], lane, f, a);
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) reads[m][jj] += a[m][0] * back[1];
+                    in_order();
+                    tri_products<1, true, kParts == 1>(room.t.tri[3], lane, f, a);
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) last[m][jj] += a[m][0] * back[3];
+                } else {
+                    tri_products<1, true, kParts == 1>(room.t.tri[2], lane, f, a);
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) last[m][jj] += a[m][0] * back[2];
                 }
             }
         }
@@ -610,8 +718,6 @@ __global__ __launch_bounds__(kBlock) void delta_back_rows(DeltaBackParams b)
     for (int query = 0; query < 2; ++query) {
         const ssam_rows& to = query ? b.grad_q : b.grad_k;
         if (!to.d) continue;
-        const T* from = query ? qs : ks;
-        const long long stride = query ? p.q.row : p.k.row;
         Float4(&d)[4][kTiles] = query ? dq : dk;
         if (p.unit) {
             float dots[4][4];
@@ -619,14 +725,10 @@ __global__ __launch_bounds__(kBlock) void delta_back_rows(DeltaBackParams b)
             for (int m = 0; m < 4; ++m)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int t = tile_row(m, 4 * g + i);
-                    const float per = query ? room.query[t] * room.query_back[t] : room.key[t] * room.key_back[t];
-                    float s = 0.0f;
+                    float e[kTiles], s = 0.0f;
+                    row_elements(query, tile_row(m, 4 * g + i), e);
 #pragma unroll
-                    for (int jj = 0; jj < kTiles; ++jj) {
-                        const int e = tile_row(wave * kTiles + jj, r);
-                        if (wave * kTiles + jj < 2 * KT && t < piece.n && e < p.key_dim) s = __builtin_fmaf((float)from[(long long)t * stride + e] * per, d[m][jj][i], s);
-                    }
+                    for (int jj = 0; jj < kTiles; ++jj) s = __builtin_fmaf(e[jj], d[m][jj][i], s);
                     dots[m][i] = s;
                 }
             __syncthreads();
@@ -639,16 +741,17 @@ __global__ __launch_bounds__(kBlock) void delta_back_rows(DeltaBackParams b)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int t = tile_row(m, 4 * g + i);
-                if (t >= piece.n) continue;
-                const float per = query ? room.query[t] * room.query_back[t] : room.key[t] * room.key_back[t];
-                const float dot = p.unit ? dot_of(room.dots[0], t) : 0.0f;
+                float e[kTiles], per = 1.0f, dot = 0.0f;
+                if (p.unit) {
+                    row_elements(query, t, e);
+                    per = query ? room.query[t] * room.query_back[t] : room.key[t] * room.key_back[t];
+                    dot = dot_of(room.dots[0], t);
+                }
 #pragma unroll
                 for (int jj = 0; jj < kTiles; ++jj) {
-                    const int e = tile_row(wave * kTiles + jj, r);
-                    if (wave * kTiles + jj >= 2 * KT || e >= p.key_dim) continue;
-                    float v = d[m][jj][i];
-                    if (p.unit) v = per * (v - (float)from[(long long)t * stride + e] * per * dot);
-                    out[(long long)t * to.row + e] = (T)v;
+                    const int at = tile_row(wave * kTiles + jj, r);
+                    if (t >= piece.n || wave * kTiles + jj >= 2 * KT || at >= p.key_dim) continue;
+                    out[(unsigned)t * (unsigned)to.row + (unsigned)at] = (T)(p.unit ? per * (d[m][jj][i] - e[jj] * dot) : d[m][jj][i]);
                 }
             }
     }
@@ -744,7 +847,8 @@ int ssam_scan_delta_backward(const ssam_scan_delta_backward_args* a, void* hip_s
             hipLaunchKernelGGL((delta_back_walk<T, KT, 1>), dim3((unsigned)walks), dim3(kBlock), 0, st, b);
             if (int e = launched()) return e;
             if (!a->grad_q.d && !a->grad_k.d && !a->grad_g.d && !a->grad_beta.d) return (int)SSAM_OK;
-            hipLaunchKernelGGL((delta_back_rows<T, KT>), dim3((unsigned)rows), dim3(kBlock), 0, st, b);
+            if (a->heads > a->key_heads) hipLaunchKernelGGL((delta_back_rows<T, KT, true>), dim3((unsigned)rows), dim3(kRowThreads), 0, st, b);
+            else hipLaunchKernelGGL((delta_back_rows<T, KT, false>), dim3((unsigned)rows), dim3(kRowThreads), 0, st, b);
             return launched();
         });
     });

@@ -473,8 +473,8 @@ __device__ __forceinline__ void products(const Half8 (&a)[P][K], const Half8 (&b
     products_of<K, NT, P>(a, f, b, f, y, z);
 }
 
-// y = a triangular matrix times the columns f (of 64 rows); kUpper: the transposed form.
-template <int NT, bool kUpper>
+// y = a triangular matrix times the columns f (of 64 rows); kUpper: the transposed form; kExact: f has no low parts.
+template <int NT, bool kUpper, bool kExact = false>
 __device__ __forceinline__ void tri_products(const Half8 (&matrix)[2][kTriOperands][kWave], int lane, const HalfPair (&f)[2][NT], Float4 (&y)[4][NT])
 {
     Half8 a[2][kTriOperands];
@@ -492,30 +492,10 @@ __device__ __forceinline__ void tri_products(const Half8 (&matrix)[2][kTriOperan
         for (int term = 0; term < 3; ++term)
 #pragma unroll
             for (int m = 0; m < 4; ++m)
-                if (kUpper ? s >= m >> 1 : s <= m >> 1)
+                if ((kUpper ? s >= m >> 1 : s <= m >> 1) && !(kExact && term == 1))
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
                         y[m][n] = mfma(a[term == 2][kUpper ? upper_operand(m, s) : lower_operand(m, s)], term == 1 ? f[s][n].lo : f[s][n].hi, y[m][n]);
-}
-
-// One tile's.
-template <int NT, bool kUpper>
-__device__ __forceinline__ void tri_product(const Half8 (&matrix)[2][kTriOperands][kWave], int m, int lane, const HalfPair (&f)[2][NT], Float4 (&y)[NT])
-{
-#pragma unroll
-    for (int n = 0; n < NT; ++n) y[n] = Float4(0.0f);
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-        if (kUpper ? s >= m >> 1 : s <= m >> 1) {
-            const int at = kUpper ? upper_operand(m, s) : lower_operand(m, s);
-            const Half8 hi = matrix[0][at][lane], lo = matrix[1][at][lane];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                y[n] = mfma(hi, f[s][n].hi, y[n]);
-                y[n] = mfma(hi, f[s][n].lo, y[n]);
-                y[n] = mfma(lo, f[s][n].hi, y[n]);
-            }
-        }
 }
 
 // 64 rows of a wave's columns as B operands; their power of two, per column.
@@ -567,22 +547,22 @@ struct PrepareRoom {
 };
 
 // q's or k's rows as fp16, each with its largest magnitude's power of two taken out; sizes: what makes it up again.
-template <class T, int KT>
+template <class T, int KT, int kThreads>
 struct RowLoad {
-    static constexpr int kLanes = 4 * KT, kPasses = kDeltaRows * kLanes / kBlock > 0 ? kDeltaRows * kLanes / kBlock : 1;      // lanes of a row
+    static constexpr int kLanes = 4 * KT, kAtOnce = kThreads / kLanes, kPasses = kDeltaRows > kAtOnce ? kDeltaRows / kAtOnce : 1;      // lanes of a row, rows
     RowVec<T, 8> v[kPasses];
 
     __device__ __forceinline__ void load(const T* __restrict__ base, unsigned stride, int rows, int dim)
     {
-        load_eights<T, kPasses>(base, stride, (int)(threadIdx.x / kLanes), kBlock / kLanes, rows, threadIdx.x % kLanes, dim, v);
+        load_eights<T, kPasses>(base, stride, (int)(threadIdx.x / kLanes), kAtOnce, rows, threadIdx.x % kLanes, dim, v);
     }
     __device__ __forceinline__ void put(bool unit, int rows, int dim, Half8 (&to)[kSplit<T> ? 2 : 1][4 * KT][kDeltaRows], float* factor, float* scale)
     {
         const int e = threadIdx.x % kLanes;
-        clear_eights<T, kPasses>((int)(threadIdx.x / kLanes), kBlock / kLanes, rows, e, dim, v);
+        clear_eights<T, kPasses>((int)(threadIdx.x / kLanes), kAtOnce, rows, e, dim, v);
 #pragma unroll
         for (int k = 0; k < kPasses; ++k) {
-            const int t = (int)(threadIdx.x / kLanes) + k * (kBlock / kLanes);
+            const int t = (int)(threadIdx.x / kLanes) + k * (kAtOnce);
             float m = 0.0f, squares = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -598,6 +578,7 @@ struct RowLoad {
             if (__is_same(T, _Float16)) by.to = by.back = 1.0f;
             Half8 hi, lo;
             to_halves<T>(v[k], by.to, hi, lo);
+            if (kAtOnce > kDeltaRows && t >= kDeltaRows) continue;
             to[0][e][t ^ (e & 15)] = hi;
             if constexpr (kSplit<T>) to[1][e][t ^ (e & 15)] = lo;
             if (e == 0) {
@@ -608,19 +589,20 @@ struct RowLoad {
     }
 };
 
-// K K^T and Q K^T, without their factors: wave w has the rows of tile w (kTiles: tile_row, otherwise 16 w ..) and the columns up to them.
-template <class T, int KT, bool kTiles, int kParts>
-__device__ __forceinline__ void key_products(const Half8 (&keys)[kParts][4 * KT][kDeltaRows], const Half8 (&queries)[kParts][4 * KT][kDeltaRows],
-                                             Float4 (&kk)[4], Float4 (&qk)[4])
+// K K^T and Q K^T, without their factors: N tiles of columns from tile n0 on (those up to the rows' own), against the rows of tile m.  kTiles: tiles are tile_row's,
+// otherwise rows 16 m ..
+template <class T, int KT, bool kTiles, int N, int kParts>
+__device__ __forceinline__ void key_products(const Half8 (&keys)[kParts][4 * KT][kDeltaRows], const Half8 (&queries)[kParts][4 * KT][kDeltaRows], int m, int n0,
+                                             Float4 (&kk)[N], Float4 (&qk)[N])
 {
-    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6, g = lane >> 4, r = lane & 15;
+    const int lane = threadIdx.x & (kWave - 1), g = lane >> 4, r = lane & 15;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < N; ++j) {
         kk[j] = qk[j] = Float4(0.0f);
-        if (j <= (kTiles ? wave | 1 : wave))
+        if (n0 + j <= (kTiles ? m | 1 : m))
 #pragma unroll
             for (int s = 0; s < KT; ++s) {
-                const int e = 4 * s + g, row = (kTiles ? tile_row(wave, r) : 16 * wave + r) ^ (e & 15), col = (kTiles ? tile_row(j, r) : 16 * j + r) ^ (e & 15);
+                const int e = 4 * s + g, row = (kTiles ? tile_row(m, r) : 16 * m + r) ^ (e & 15), col = (kTiles ? tile_row(n0 + j, r) : 16 * (n0 + j) + r) ^ (e & 15);
                 const Half8 b = keys[0][e][col];
                 kk[j] = mfma(keys[0][e][row], b, kk[j]);
                 qk[j] = mfma(queries[0][e][row], b, qk[j]);
@@ -677,11 +659,11 @@ __device__ __forceinline__ void invert(Room& room)
 }
 
 // A triangular matrix in LDS as operands, hi and lo; kUpper: its transpose.
-template <bool kUpper>
+template <bool kUpper, int kWaves = kWavesPerBlock>
 __device__ __forceinline__ void store_operands(const float (&a)[kDeltaRows][kTriStride], float to, Half8 (&out)[2][kTriOperands][kWave])
 {
     const int lane = threadIdx.x & (kWave - 1), g = lane >> 4, r = lane & 15;
-    for (int k = threadIdx.x >> 6; k < kTriOperands; k += kWavesPerBlock) {
+    for (int k = threadIdx.x >> 6; k < kTriOperands; k += kWaves) {
         // lower: (0, 0) (1, 0) (2, 0) (2, 1) (3, 0) (3, 1); upper: (0, 0) (0, 1) (1, 0) (1, 1) (2, 1) (3, 1)
         const int m = kUpper ? (k < 4 ? k >> 1 : k - 2) : (k < 2 ? k : 1 + (k >> 1)), s = kUpper ? (k < 4 ? k & 1 : 1) : (k < 2 ? 0 : k & 1);
         const int row = tile_row(m, r), col = 32 * s + 8 * g;
@@ -695,6 +677,7 @@ __device__ __forceinline__ void store_operands(const float (&a)[kDeltaRows][kTri
 }
 
 // Over the block; `room`: a float a wave.
+template <int kWaves = kWavesPerBlock>
 __device__ __forceinline__ float over_block(float m, float* room)
 {
 #pragma unroll
@@ -703,7 +686,7 @@ __device__ __forceinline__ float over_block(float m, float* room)
     __syncthreads();
     m = room[0];
 #pragma unroll
-    for (int w = 1; w < kWavesPerBlock; ++w) m = __builtin_fmaxf(m, room[w]);
+    for (int w = 1; w < kWaves; ++w) m = __builtin_fmaxf(m, room[w]);
     return m;
 }
 
@@ -713,7 +696,7 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, const Piece&
 {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, g = lane >> 4, r = lane & 15, many = p.heads / p.key_heads;
     {
-        RowLoad<T, KT> k, q;
+        RowLoad<T, KT, kBlock> k, q;
         k.load(sequence_base<const T>(p.k, p.pieces, piece) + piece.row0 * p.k.row + key_head * p.k_head, (unsigned)p.k.row, piece.n, p.key_dim);
         q.load(sequence_base<const T>(p.q, p.pieces, piece) + piece.row0 * p.q.row + key_head * p.q_head, (unsigned)p.q.row, piece.n, p.key_dim);
         k.put(p.unit, piece.n, p.key_dim, room.keys, room.key, room.f.key);
@@ -721,7 +704,7 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, const Piece&
     }
     __syncthreads();
     Float4 kk[4], qk[4];
-    key_products<T, KT, false>(room.keys, room.queries, kk, qk);
+    key_products<T, KT, false, 4>(room.keys, room.queries, wave, 0, kk, qk);
     for (int h = key_head * many; h < (key_head + 1) * many; ++h) {
         __syncthreads();                          // the operands, or the last head's matrices, are done with
         if (wave == 0) {
