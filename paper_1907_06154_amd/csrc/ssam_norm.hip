@@ -18,17 +18,6 @@ struct NormParams {
     float eps;
 };
 
-// Sums (or the larger) over aligned groups of N <= 16 lanes, and over all 64; every lane gets the result.  Rotations within 16 lanes
-// add in another order on each lane, so the sum is made by exchanging halves, in which both sides add the same two values.
-template <int kXor> __device__ __forceinline__ float lane_xor(float v)
-{
-    if constexpr (kXor == 1) return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0xb1, 0xf, 0xf, true));
-    else if constexpr (kXor == 2) return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x4e, 0xf, 0xf, true));
-    else return __shfl_xor(v, kXor);
-}
-struct Add {
-    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
-};
 // The larger of two values >= 0; NaN stays, as its bits are above infinity's.
 struct Larger {
     __device__ __forceinline__ float operator()(float a, float b) const
@@ -37,14 +26,12 @@ struct Larger {
         return __builtin_bit_cast(float, x > y ? x : y);
     }
 };
+// Over aligned groups of n lanes, a power of two; every lane gets the same result.
 template <class Op> __device__ __forceinline__ float over_lanes(float v, int n, Op op)
 {
-    if (n > 1) v = op(v, lane_xor<1>(v));
-    if (n > 2) v = op(v, lane_xor<2>(v));
-    if (n > 4) v = op(v, lane_xor<4>(v));
-    if (n > 8) v = op(v, lane_xor<8>(v));
-    if (n > 16) v = op(v, lane_xor<16>(v));
-    if (n > 32) v = op(v, lane_xor<32>(v));
+    v = over_few(v, n, op);
+    if (n > 16) v = op(v, __shfl_xor(v, 16));
+    if (n > 32) v = op(v, __shfl_xor(v, 32));
     return v;
 }
 

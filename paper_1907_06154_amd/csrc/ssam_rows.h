@@ -60,6 +60,28 @@ __device__ __forceinline__ RowVec<T, V> rounded(const float (&x)[V])
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
+// The value of lane ^ 1, of lane ^ 2, of a lane of the other quad of 8 and of the other half of 16 lanes, by DPP.  (The last two are mirror images: for values
+// that are the same over a quad, or over 8 lanes.)
+template <int kControl> __device__ __forceinline__ float dpp_of(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), kControl, 0xf, 0xf, true));
+}
+// op over aligned groups of n = 2, 4, 8 or 16 lanes (1: none), for all of them.
+template <class Op> __device__ __forceinline__ float over_few(float v, int n, Op op)
+{
+    if (n > 1) v = op(v, dpp_of<0xb1>(v));
+    if (n > 2) v = op(v, dpp_of<0x4e>(v));
+    if (n > 4) v = op(v, dpp_of<0x141>(v));
+    if (n > 8) v = op(v, dpp_of<0x140>(v));
+    return v;
+}
+struct Add {
+    __device__ __forceinline__ float operator()(float a, float b) const { return a + b; }
+};
+struct Max {
+    __device__ __forceinline__ float operator()(float a, float b) const { return __builtin_fmaxf(a, b); }
+};
+
 // 2^x by the hardware instruction (1 ulp; results below 2^-126 become 0, which only ever scales a sum).
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 

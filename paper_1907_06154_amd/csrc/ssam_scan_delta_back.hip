@@ -236,13 +236,6 @@ struct RowsRoom {
 __device__ __forceinline__ int tile_of(int t) { return 2 * (t >> 5) + (t >> 2 & 1); }
 __device__ __forceinline__ int row_in_tile(int t) { return 4 * (t >> 3 & 3) + (t & 3); }
 
-__device__ __forceinline__ float over_16(float v)
-{
-#pragma unroll
-    for (int x = 1; x < 16; x *= 2) v += __shfl_xor(v, x);
-    return v;
-}
-
 // Rows' sums over the lanes and waves of v[m][i], what a lane has for row tile_row(m, 4 g + i); to be read after a barrier.
 __device__ __forceinline__ void put_dots(const float (&v)[4][4], float (&to)[kRowWaves][kDeltaRows])
 {
@@ -251,7 +244,7 @@ __device__ __forceinline__ void put_dots(const float (&v)[4][4], float (&to)[kRo
     for (int m = 0; m < 4; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float s = over_16(v[m][i]);
+            const float s = over_few(v[m][i], 16, Add());
             if ((lane & 15) == 0) to[threadIdx.x >> 6][tile_row(m, 4 * g + i)] = s;
         }
 }
@@ -286,9 +279,13 @@ struct RowData {
 #pragma unroll
             for (int k = 0; k < kPasses; ++k) {
                 const int t = (int)(threadIdx.x >> 4) + k * (kRowThreads / 16);
-                o[k] = load_row_vec<T, 8>(dos + (unsigned)(t < rows ? t : rows - 1) * stride + c, have > 0 ? have : dim);
-                y[k] = load_row_vec<float, 8>(ys + (unsigned)(t * dim) + c, have > 0 ? have : dim);
-                u[k] = load_row_vec<float, 8>(us + (unsigned)(t * dim) + c, have > 0 ? have : dim);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const unsigned e = (unsigned)(at + i < dim ? at + i : dim - 1);
+                    o[k][i] = dos[(unsigned)(t < rows ? t : rows - 1) * stride + e];
+                    y[k][i] = ys[(unsigned)(t * dim) + e];
+                    u[k][i] = us[(unsigned)(t * dim) + e];
+                }
             }
         }
     }
@@ -300,11 +297,20 @@ struct StateRow {
     {
         const int g = (threadIdx.x & (kWave - 1)) >> 4;
         const float* const row = state + (size_t)(d < key_dim ? d : key_dim - 1) * dim;
+        if (dim % 8 == 0) {
 #pragma unroll
-        for (int s = 0; s < kAcrossSteps; ++s) {
-            const int at = v0 + 32 * s + 8 * g, have = dim - at;
-            if (dim % 8 == 0) __builtin_memcpy(&v[s], row + (have > 0 ? at : 0), 32);
-            else v[s] = load_row_vec<float, 8>(row + (have > 0 ? at : 0), have > 0 ? have : dim);
+            for (int s = 0; s < kAcrossSteps; ++s) {
+                const int at = v0 + 32 * s + 8 * g;
+                __builtin_memcpy(&v[s], row + (at < dim ? at : 0), 32);
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < kAcrossSteps; ++s)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int at = v0 + 32 * s + 8 * g + i;
+                    v[s][i] = row[at < dim ? at : dim - 1];
+                }
         }
     }
     __device__ __forceinline__ float clear(int d, int key_dim, int dim, int v0)      // and the largest magnitude
@@ -313,9 +319,11 @@ struct StateRow {
         float m = 0.0f;
 #pragma unroll
         for (int s = 0; s < kAcrossSteps; ++s) {
-            if (!(d < key_dim && v0 + 32 * s + 8 * g < dim)) v[s] = RowVec<float, 8>(0.0f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) m = larger(m, v[s][i]);
+            for (int i = 0; i < 8; ++i) {
+                if (!(d < key_dim && v0 + 32 * s + 8 * g + i < dim)) v[s][i] = 0.0f;
+                m = larger(m, v[s][i]);
+            }
         }
         return m;
     }
@@ -336,13 +344,27 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
     if (piece.seq < 0 || piece.n <= 0) return;
     const T* const ks = sequence_base<const T>(p.k, p.pieces, piece) + piece.row0 * p.k.row + key_head * p.k_head;
     const T* const qs = sequence_base<const T>(p.q, p.pieces, piece) + piece.row0 * p.q.row + key_head * p.q_head;
+    const size_t below = (size_t)p.key_dim * p.value_dim;      // a mark's second part
+    const T* const grads = sequence_base<const T>(b.grad_out, p.pieces, piece) + piece.row0 * b.grad_out.row;
     RowData<T> data;
+    float gate = 0.0f, beta_ = 0.0f;
+    auto load_head = [&](int h) {
+        const bool there = wave == 0 && lane < piece.n;
+        const long long at = piece.row0 + (there ? lane : 0);
+        if (wave == 0) {
+            gate = p.g.d ? sequence_base<const float>(p.g, p.pieces, piece)[at * p.g.row + h] : 0.0f;
+            beta_ = sequence_base<const float>(p.beta, p.pieces, piece)[at * p.beta.row + h];
+        }
+        data.load(grads + h * b.grad_out_head, (unsigned)b.grad_out.row, mark_of(b.behind, p, slot, h) + below, mark_of(p.marks, p, slot, h) + below, p.value_dim,
+                  piece.n, 0);
+    };
     const int tile = wave & 3, col0 = wave >> 2 << 1;      // of the 64 x 64 products: a wave's tile of rows and its two of columns
     Float4 kk[2], qk[2];                      // K K^T and Q K^T
     {
         RowLoad<T, KT, kRowThreads> k, q;
         k.load(ks, (unsigned)p.k.row, piece.n, p.key_dim);
         q.load(qs, (unsigned)p.q.row, piece.n, p.key_dim);
+        load_head(key_head * many);
         k.put(p.unit, piece.n, p.key_dim, room.rows().keys, room.key_back, room.key);
         q.put(p.unit, piece.n, p.key_dim, room.rows().queries, room.query_back, room.query);
     }
@@ -369,6 +391,8 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
             }
         }
     };
+    // Addresses in LDS are made anew for every step of the work: all of them together, kept over the loops, would take the registers of everything else.
+    auto fresh_lane = [&] { asm volatile("" : "+v"(lane), "+v"(g), "+v"(r)); };
     Float4 dq[4][kTiles], dk[4][kTiles];      // sums over the heads that share the key
 #pragma unroll
     for (int m = 0; m < 4; ++m)
@@ -376,19 +400,13 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
         for (int j = 0; j < kTiles; ++j) dq[m][j] = dk[m][j] = Float4(0.0f);
 
     for (int h = key_head * many; h < (key_head + 1) * many; ++h) {
-        asm volatile("" : "+v"(lane), "+v"(g), "+v"(r));       // a head's addresses are made for it, not kept over all of them
+        fresh_lane();
         const float* const mark = mark_of(p.marks, p, slot, h);
         const float* const behind = mark_of(b.behind, p, slot, h);
-        const T* const dos = sequence_base<const T>(b.grad_out, p.pieces, piece) + piece.row0 * b.grad_out.row + h * b.grad_out_head;
-        const size_t below = (size_t)p.key_dim * p.value_dim;
-        data.load(dos, (unsigned)b.grad_out.row, behind + below, mark + below, p.value_dim, piece.n, 0);
+        if (kShared && h > key_head * many) load_head(h);
         __syncthreads();
         if (wave == 0) {
-            const bool there = lane < piece.n;
-            const long long at = piece.row0 + (there ? lane : 0);
-            float gate = 0.0f, beta = 0.0f;
-            if (there && p.g.d) gate = sequence_base<const float>(p.g, p.pieces, piece)[at * p.g.row + h];
-            if (there) beta = sequence_base<const float>(p.beta, p.pieces, piece)[at * p.beta.row + h];
+            if (lane >= piece.n) gate = beta_ = 0.0f;
             double sum = gate < -1000.0f ? -1000.0 : (double)gate;
 #pragma unroll
             for (int x = 1; x < kWave; x *= 2) {
@@ -397,7 +415,7 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
             }
             const double all = __shfl(sum, kWave - 1);
             room.sum[lane] = sum;
-            room.beta[lane] = beta;
+            room.beta[lane] = beta_;
             room.dbeta[lane] = 0.0f;
             room.up[lane] = exp2_fast(kLog2e * (float)sum);
             room.rest[lane] = exp2_fast(kLog2e * (float)(all - sum));
@@ -412,19 +430,26 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
             for (int j = 0; j < kTiles; ++j) asked[m][j] = reads[m][j] = last[m][j] = Float4(0.0f);
         }
         for (int v0 = 0; v0 < p.value_dim; v0 += kAcross) {
-            if (v0) data.load(dos, (unsigned)b.grad_out.row, behind + below, mark + below, p.value_dim, piece.n, v0);
+            fresh_lane();
+            if (v0) data.load(grads + h * b.grad_out_head, (unsigned)b.grad_out.row, behind + below, mark + below, p.value_dim, piece.n, v0);
             __syncthreads();
             // dO, dX = b dY and U = b R as operands
             const int e = tid & 15;
-            const bool across = v0 + 8 * e < p.value_dim;
+            const bool whole = v0 + kAcross <= p.value_dim;
 #pragma unroll
             for (int k = 0; k < RowData<T>::kPasses; ++k) {
                 const int t = (tid >> 4) + k * (kRowThreads / 16);
                 const float beta = room.beta[t];
                 RowVec<T, 8>& o = data.o[k];
                 RowVec<float, 8>&y = data.y[k], &u = data.u[k];
-                if (!across || t >= piece.n) o = RowVec<T, 8>(T(0));
-                if (!across) y = u = RowVec<float, 8>(0.0f);
+                if (t >= piece.n) o = RowVec<T, 8>(T(0));
+                if (!whole)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (v0 + 8 * e + i >= p.value_dim) {
+                            o[i] = T(0);
+                            y[i] = u[i] = 0.0f;
+                        }
                 float dot = 0.0f, mo = 0.0f, mx = 0.0f, mu = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -435,13 +460,10 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
                     mx = larger(mx, y[i]);
                     mu = larger(mu, u[i]);
                 }
-#pragma unroll
-                for (int x = 1; x < 16; x *= 2) {
-                    dot += __shfl_xor(dot, x);
-                    mo = __builtin_fmaxf(mo, __shfl_xor(mo, x));
-                    mx = __builtin_fmaxf(mx, __shfl_xor(mx, x));
-                    mu = __builtin_fmaxf(mu, __shfl_xor(mu, x));
-                }
+                dot = over_few(dot, 16, Add());
+                mo = over_few(mo, 16, Max());
+                mx = over_few(mx, 16, Max());
+                mu = over_few(mu, 16, Max());
                 Scale so(mo);
                 const Scale sx(mx), su(mu);
                 if (__is_same(T, _Float16)) so.to = so.back = 1.0f;
@@ -465,10 +487,10 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
             }
             StateRow s0, s1;
             s0.load(mark, tile_row(wave * kTiles, r), p.key_dim, p.value_dim, v0);
-            s1.load(behind, tile_row(wave * kTiles, r), p.key_dim, p.value_dim, v0);
             __syncthreads();
             auto operand = [&](const Half8 (&a)[4 * kAcrossSteps][kWave], int m, int s) { return a[m * kAcrossSteps + s][row_entry(s, g, r)]; };
             // dO U^T and dX U^T
+            fresh_lane();
 #pragma unroll
             for (int k0 = 0; k0 < 2; ++k0)
                 if (const int n = col0 + k0; n <= (tile | 1)) {
@@ -495,57 +517,72 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
             // dO S0^T, dX S0^T and U dS1^T: a wave has some of the keys' elements, for all rows
 #pragma unroll
             for (int jj = 0; jj < kTiles; ++jj) {
+                fresh_lane();
                 const int j = wave * kTiles + jj, d = tile_row(j, r);
                 if (jj) in_order();
-                const float m0 = s0.clear(j < 2 * KT ? d : p.key_dim, p.key_dim, p.value_dim, v0), m1 = s1.clear(j < 2 * KT ? d : p.key_dim, p.key_dim, p.value_dim, v0);
+                const int row = j < 2 * KT ? d : p.key_dim;
+                HalfPair f[kAcrossSteps];
+                float back;
+                auto to_operands = [&](StateRow& s) {
+                    const Scale by(over_column(s.clear(row, p.key_dim, p.value_dim, v0)));
+                    back = by.back;
 #pragma unroll
-                for (int s = 0; s < kAcrossSteps; ++s)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) inner = __builtin_fmaf(s0.v[s][i], s1.v[s][i], inner);
-                const Scale by0(over_column(m0)), by1(over_column(m1));
-                HalfPair h0[kAcrossSteps], h1[kAcrossSteps];
-#pragma unroll
-                for (int s = 0; s < kAcrossSteps; ++s) {
-                    to_halves<float>(s0.v[s], by0.to, h0[s].hi, h0[s].lo);
-                    to_halves<float>(s1.v[s], by1.to, h1[s].hi, h1[s].lo);
-                }
-                if (jj + 1 < kTiles) {
-                    s0.load(mark, tile_row(j + 1, r), p.key_dim, p.value_dim, v0);
-                    s1.load(behind, tile_row(j + 1, r), p.key_dim, p.value_dim, v0);
-                }
+                    for (int k = 0; k < kAcrossSteps; ++k) to_halves<float>(s.v[k], by.to, f[k].hi, f[k].lo);
+                };
+                to_operands(s0);
+                s1.load(behind, d, p.key_dim, p.value_dim, v0);
                 in_order();
 #pragma unroll
                 for (int m = 0; m < 4; ++m) {
                     if (m) in_order();
-                    Float4 a(0.0f), c(0.0f), w(0.0f);
+                    Float4 a(0.0f), c(0.0f);
 #pragma unroll
                     for (int s = 0; s < kAcrossSteps; ++s) {
-                        const Half8 xh = operand(room.o.x[0], m, s), uh = operand(room.o.u[0], m, s);
-                        c = mfma(xh, h0[s].hi, c);
-                        w = mfma(uh, h1[s].hi, w);
+                        const Half8 xh = operand(room.o.x[0], m, s);
+                        c = mfma(xh, f[s].hi, c);
 #pragma unroll
                         for (int k = 0; k < kParts; ++k) {
                             const Half8 o = operand(room.o.grad[k], m, s);
-                            a = mfma(o, h0[s].hi, a);
-                            if (k == 0) a = mfma(o, h0[s].lo, a);
+                            a = mfma(o, f[s].hi, a);
+                            if (k == 0) a = mfma(o, f[s].lo, a);
                         }
-                        c = mfma(xh, h0[s].lo, c);
-                        w = mfma(uh, h1[s].lo, w);
-                        c = mfma(operand(room.o.x[1], m, s), h0[s].hi, c);
-                        w = mfma(operand(room.o.u[1], m, s), h1[s].hi, w);
+                        c = mfma(xh, f[s].lo, c);
+                        c = mfma(operand(room.o.x[1], m, s), f[s].hi, c);
                     }
                     const int t0 = tile_row(m, 4 * g);
-                    const Float4 up = *reinterpret_cast<const Float4*>(&room.up[t0]), rest = *reinterpret_cast<const Float4*>(&room.rest[t0]);
-                    const Float4 ro = *reinterpret_cast<const Float4*>(&room.back[0][t0]), rx = *reinterpret_cast<const Float4*>(&room.back[1][t0]),
-                                 ru = *reinterpret_cast<const Float4*>(&room.back[2][t0]);
-                    asked[m][jj] += a * (up * ro * (p.scale * by0.back));
-                    reads[m][jj] -= c * (up * rx * by0.back);
-                    last[m][jj] += w * (rest * ru * by1.back);
+                    const Float4 up = *reinterpret_cast<const Float4*>(&room.up[t0]), ro = *reinterpret_cast<const Float4*>(&room.back[0][t0]),
+                                 rx = *reinterpret_cast<const Float4*>(&room.back[1][t0]);
+                    asked[m][jj] += a * (up * ro * (p.scale * back));
+                    reads[m][jj] -= c * (up * rx * back);
+                }
+                in_order();
+                to_operands(s1);
+#pragma unroll
+                for (int s = 0; s < kAcrossSteps; ++s)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) inner = __builtin_fmaf(s0.v[s][i], s1.v[s][i], inner);
+                if (jj + 1 < kTiles) s0.load(mark, tile_row(j + 1, r), p.key_dim, p.value_dim, v0);
+                in_order();
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    if (m) in_order();
+                    Float4 w(0.0f);
+#pragma unroll
+                    for (int s = 0; s < kAcrossSteps; ++s) {
+                        const Half8 uh = operand(room.o.u[0], m, s);
+                        w = mfma(uh, f[s].hi, w);
+                        w = mfma(uh, f[s].lo, w);
+                        w = mfma(operand(room.o.u[1], m, s), f[s].hi, w);
+                    }
+                    const int t0 = tile_row(m, 4 * g);
+                    const Float4 rest = *reinterpret_cast<const Float4*>(&room.rest[t0]), ru = *reinterpret_cast<const Float4*>(&room.back[2][t0]);
+                    last[m][jj] += w * (rest * ru * back);
                 }
             }
         }
         // what the rows' decays have of S0, of dS1 and of one another's products
         {
+            fresh_lane();
             float dots[4][4], lasts[4][4];
 #pragma unroll
             for (int m = 0; m < 4; ++m)
@@ -572,6 +609,7 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
         if (lane == 0) room.inner[wave] = inner;
         if constexpr (Room::kKept) key_products<T, KT, true, 2>(room.rows().keys, room.rows().queries, tile, col0, kk, qk);
         __syncthreads();                          // the matrix lies over the operands
+        fresh_lane();
         // dP and dA without their keys' and queries' factors: in place
 #pragma unroll
         for (int n = 0; n < 2; ++n)
@@ -636,6 +674,7 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if (k) __syncthreads();
+            fresh_lane();
             float most = 0.0f;
 #pragma unroll
             for (int n = 0; n < 2; ++n)
@@ -654,6 +693,7 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
 #pragma unroll
         for (int query = 0; query < 2; ++query) {
             if (query) __syncthreads();
+            fresh_lane();
             for (int job = tid; job < 32 * KT; job += kRowThreads) {
                 const int sq = job / (4 * KT), e = job % (4 * KT);
                 Half8 hi[8], lo[8];
@@ -719,6 +759,7 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
         const ssam_rows& to = query ? b.grad_q : b.grad_k;
         if (!to.d) continue;
         Float4(&d)[4][kTiles] = query ? dq : dk;
+        fresh_lane();
         if (p.unit) {
             float dots[4][4];
 #pragma unroll
@@ -735,7 +776,11 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
             put_dots(dots, room.dots[0]);
             __syncthreads();
         }
-        T* const out = sequence_base<T>(to, p.pieces, piece) + piece.row0 * to.row + key_head * b.grad_key_head;
+        else __syncthreads();
+        // by way of LDS, so that whole rows leave
+        constexpr int E = 16 / (int)sizeof(T), kOfRow = 32 * KT / E;
+        RowVec<T, E>(*const out)[kOfRow] = reinterpret_cast<RowVec<T, E>(*)[kOfRow]>(&room.t.turned[0][0][0]);
+        static_assert(sizeof(room.t.turned) >= sizeof(T) * kDeltaRows * 32 * KT);
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -750,10 +795,17 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
 #pragma unroll
                 for (int jj = 0; jj < kTiles; ++jj) {
                     const int at = tile_row(wave * kTiles + jj, r);
-                    if (t >= piece.n || wave * kTiles + jj >= 2 * KT || at >= p.key_dim) continue;
-                    out[(unsigned)t * (unsigned)to.row + (unsigned)at] = (T)(p.unit ? per * (d[m][jj][i] - e[jj] * dot) : d[m][jj][i]);
+                    if (wave * kTiles + jj >= 2 * KT) continue;
+                    reinterpret_cast<T*>(&out[t][0])[at] = (T)(p.unit ? per * (d[m][jj][i] - e[jj] * dot) : d[m][jj][i]);
                 }
             }
+        __syncthreads();
+        T* const rows = sequence_base<T>(to, p.pieces, piece) + piece.row0 * to.row + key_head * b.grad_key_head;
+        for (int at = tid; at < kDeltaRows * kOfRow; at += kRowThreads) {
+            const int t = at / kOfRow, part = at % kOfRow;
+            if (t < piece.n && part * E < p.key_dim) store_row_vec<T, E>(rows + ((unsigned)t * (unsigned)to.row + (unsigned)(part * E)), p.key_dim - part * E, out[t][part]);
+        }
+        __syncthreads();
     }
 }
 

@@ -569,10 +569,11 @@ struct RowLoad {
                 m = larger(m, (float)v[k][i]);
                 squares = __builtin_fmaf((float)v[k][i], (float)v[k][i], squares);
             }
-#pragma unroll
-            for (int x = 1; x < kLanes; x *= 2) {
-                m = __builtin_fmaxf(m, __shfl_xor(m, x));
-                squares += __shfl_xor(squares, x);
+            m = over_few(m, kLanes, Max());
+            squares = over_few(squares, kLanes, Add());
+            if (kLanes > 16) {
+                m = __builtin_fmaxf(m, __shfl_xor(m, 16));
+                squares += __shfl_xor(squares, 16);
             }
             Scale by(m);
             if (__is_same(T, _Float16)) by.to = by.back = 1.0f;
