@@ -245,7 +245,7 @@ int ssam_scan_delta(const ssam_scan_delta_args* a, void* hip_stream)
     DeltaParams p{make_pieces(a->seq, kDeltaRows), a->q, a->k, a->v, a->out, a->g, a->beta, a->q_head, a->k_head, a->v_head, a->out_head, a->d_state,
                   a->d_final, a->d_marks, static_cast<Block*>(a->d_work), a->heads, a->key_heads, a->key_dim, a->value_dim, a->unit != 0, a->scale, 1};
     const long long heads = (long long)a->seq.sequences * a->heads;
-    const bool wide = heads * ((a->value_dim + 63) / 64) > 512 && a->value_dim > 64 && a->key_dim <= 128;
+    const bool wide = heads * ((a->value_dim + 63) / 64) >= 512 && a->value_dim > 64 && a->key_dim <= 128;
     p.tiles = (a->value_dim + (wide ? 127 : 63)) / (wide ? 128 : 64);
     if (product(slots, a->key_heads) > kMaxGrid || product(heads, p.tiles) > kMaxGrid) return SSAM_ERR_DIM;
     hipStream_t st = (hipStream_t)hip_stream;

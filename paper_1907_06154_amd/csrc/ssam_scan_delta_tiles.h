@@ -527,7 +527,7 @@ __device__ __forceinline__ void split_state(const Float4 (&s)[2 * KT][NT], HalfP
 }
 
 // ---- delta_prepare -----------------------------------------------------------------------------------------------------------
-constexpr int kTriStride = kDeltaRows + 1;      // floats of a row in LDS
+constexpr int kTriStride = kDeltaRows + 4;      // floats of a row in LDS: rows and columns alike meet all banks
 
 template <class T, int KT>
 struct PrepareRoom {
@@ -622,11 +622,13 @@ __device__ __forceinline__ void key_products(const Half8 (&keys)[kParts][4 * KT]
 __device__ __forceinline__ Float4 mfma_f32(float a, float b, Float4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
 // The inverse of I + system (strictly lower), 16 x 16 blocks: those of the diagonal by substitution, a column a lane; below it block (i, j) is
-// -inverse(i, i) times the sum over k of system(i, k) inverse(k, j), one diagonal after the other.  All in fp32.
+// -inverse(i, i) times the sum over k of system(i, k) inverse(k, j), one diagonal after the other.  All in fp32.  What lies above the diagonal in `inverse` is
+// zero before and after.  Returns the largest magnitude that the lane has seen.
 template <class Room>
-__device__ __forceinline__ void invert(Room& room)
+__device__ __forceinline__ float invert(Room& room)
 {
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, g = lane >> 4, r = lane & 15;
+    float most = 1.0f;
     {
         const int at = 16 * wave;
         float x[16];
@@ -634,8 +636,14 @@ __device__ __forceinline__ void invert(Room& room)
         for (int i = 0; i < 16; ++i) {
             float s = i == r ? 1.0f : 0.0f;
 #pragma unroll
-            for (int j = 0; j < i; ++j) s = __builtin_fmaf(-room.system[at + i][at + j], x[j], s);
+            for (int j = 0; j < i; j += 4) {
+                const Float4 row = *reinterpret_cast<const Float4*>(&room.system[at + i][at + j]);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (j + k < i) s = __builtin_fmaf(-row[k], x[j + k], s);
+            }
             x[i] = s;
+            most = larger(most, s);
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i)
@@ -647,19 +655,24 @@ __device__ __forceinline__ void invert(Room& room)
         const int i = wave + d, j = wave;
         if (i < 4) {
             Float4 s(0.0f), y(0.0f);
-            for (int k = j; k < i; ++k)
+            for (int k = j; k < i; ++k) {
+                const Float4 row = *reinterpret_cast<const Float4*>(&room.system[16 * i + r][16 * k + 4 * g]);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) s = mfma_f32(room.system[16 * i + r][16 * k + 4 * g + q], room.inverse[16 * k + 4 * g + q][16 * j + r], s);
+                for (int q = 0; q < 4; ++q) s = mfma_f32(row[q], room.inverse[16 * k + 4 * g + q][16 * j + r], s);
+            }
+            const Float4 row = *reinterpret_cast<const Float4*>(&room.inverse[16 * i + r][16 * i + 4 * g]);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) y = mfma_f32(room.inverse[16 * i + r][16 * i + 4 * g + q], s[q], y);
+            for (int q = 0; q < 4; ++q) y = mfma_f32(row[q], s[q], y);
 #pragma unroll
             for (int q = 0; q < 4; ++q) room.inverse[16 * i + 4 * g + q][16 * j + r] = -y[q];
+            most = larger(most, y);
         }
         __syncthreads();
     }
+    return most;
 }
 
-// A triangular matrix in LDS as operands, hi and lo; kUpper: its transpose.
+// A triangular matrix in LDS, zeros above its diagonal, as operands, hi and lo; kUpper: its transpose.
 template <bool kUpper, int kWaves = kWavesPerBlock>
 __device__ __forceinline__ void store_operands(const float (&a)[kDeltaRows][kTriStride], float to, Half8 (&out)[2][kTriOperands][kWave])
 {
@@ -669,8 +682,17 @@ __device__ __forceinline__ void store_operands(const float (&a)[kDeltaRows][kTri
         const int m = kUpper ? (k < 4 ? k >> 1 : k - 2) : (k < 2 ? k : 1 + (k >> 1)), s = kUpper ? (k < 4 ? k & 1 : 1) : (k < 2 ? 0 : k & 1);
         const int row = tile_row(m, r), col = 32 * s + 8 * g;
         float v[8];
+        if constexpr (kUpper) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = kUpper ? (col + i >= row ? a[col + i][row] : 0.0f) : col + i <= row ? a[row][col + i] : 0.0f;
+            for (int i = 0; i < 8; ++i) v[i] = a[col + i][row];
+        } else {
+            const Float4 u = *reinterpret_cast<const Float4*>(&a[row][col]), w = *reinterpret_cast<const Float4*>(&a[row][col + 4]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[i] = u[i];
+                v[i + 4] = w[i];
+            }
+        }
         const HalfPair p = split(v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7], to);
         out[0][k][lane] = p.hi;
         out[1][k][lane] = p.lo;
@@ -681,8 +703,7 @@ __device__ __forceinline__ void store_operands(const float (&a)[kDeltaRows][kTri
 template <int kWaves = kWavesPerBlock>
 __device__ __forceinline__ float over_block(float m, float* room)
 {
-#pragma unroll
-    for (int x = 1; x < kWave; x *= 2) m = __builtin_fmaxf(m, __shfl_xor(m, x));
+    m = over_column(over_few(m, 16, Max()));
     if ((threadIdx.x & (kWave - 1)) == 0) room[threadIdx.x >> 6] = m;
     __syncthreads();
     m = room[0];
@@ -732,32 +753,40 @@ __device__ __forceinline__ void prepare_block(const DeltaParams& p, const Piece&
             if (lane == 0) room.f.total = exp2_fast(kLog2e * (float)all);
         }
         __syncthreads();
-        float most = 0.0f;
+        float most = 0.0f, query[4], key[4];
+        double sum[4];
+        const int row0 = 16 * wave + 4 * g;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int i = 0; i < 4; ++i) {
+            sum[i] = room.sum[row0 + i];
+            query[i] = p.scale * room.query[row0 + i];
+            key[i] = room.key[row0 + i] * (kBack ? room.beta[row0 + i] : 1.0f);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int col = 16 * j + r;
+            if (j > wave) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) room.inverse[row0 + i][col] = 0.0f;
+                continue;
+            }
+            const double before = room.sum[col];
+            const float own = room.key[col], beta = kBack ? 1.0f : room.beta[col];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int row = 16 * wave + 4 * g + i, col = 16 * j + r;
-                float a = 0.0f, m = 0.0f;
-                if (col <= row) {
-                    const float d = exp2_fast(kLog2e * (float)(room.sum[row] - room.sum[col])) * room.key[col];
-                    m = p.scale * room.query[row] * qk[j][i] * d;
-                    if (col < row) a = room.key[row] * kk[j][i] * d * room.beta[kBack ? row : col];
-                }
+                const float d = col <= row0 + i ? exp2_fast(kLog2e * (float)(sum[i] - before)) * own : 0.0f;
+                const float m = query[i] * qk[j][i] * d;
                 most = larger(most, m);
-                room.system[row][col] = a;
-                room.inverse[row][col] = m;
+                room.system[row0 + i][col] = col < row0 + i ? key[i] * kk[j][i] * (d * beta) : 0.0f;
+                room.inverse[row0 + i][col] = col <= row0 + i ? m : 0.0f;
             }
+        }
         most = over_block(most, room.most[0]);
         Block& out = p.blocks[slot * p.heads + h];
         const Scale mix(most);
         store_operands<kBack>(room.inverse, mix.to, out.mix);
         __syncthreads();
-        invert(room);
-        most = 0.0f;
-        for (int i = tid; i < kDeltaRows * kDeltaRows; i += kBlock)
-            if (i / kDeltaRows >= i % kDeltaRows) most = larger(most, room.inverse[i / kDeltaRows][i % kDeltaRows]);
-        most = over_block(most, room.most[1]);
+        most = over_block(invert(room), room.most[1]);
         const Scale solve(most);
         store_operands<kBack>(room.inverse, solve.to, out.solve);
         if (tid == 0) {
