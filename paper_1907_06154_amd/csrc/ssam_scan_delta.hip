@@ -18,9 +18,10 @@ __global__ __launch_bounds__(kBlock) void delta_prepare(DeltaParams p)
 // One wave: 16 NT columns of a head's state, from its sequence's first block to the last.  The operands made from q, k and the block's matrices
 // are in LDS, the same for the block's four waves; the next block's are on their way in registers.
 template <class T, int KT, int NT>
-__global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
+__global__ __launch_bounds__((kWalkThreads<T, KT, NT>)) void delta_walk(DeltaParams p)
 {
-    __shared__ WalkRoom<T, KT> room;
+    constexpr bool kHelp = kHelped<T, KT, NT>;
+    __shared__ WalkRoom<T, KT> rooms[kHelp ? 2 : 1];
     typedef Stage<T, KT, false> S;
     typedef Columns<T, NT, kSplit<T> && (KT > 4)> Cols;
     __shared__ typename Cols::Room columns[kWavesPerBlock];
@@ -34,13 +35,16 @@ __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
     const long long slot0 = p.pieces.begin ? first_slot(p.pieces, seq) : (long long)seq * p.pieces.per;
     const int col0 = (tile * kWavesPerBlock + __builtin_amdgcn_readfirstlane(wave)) * 16 * NT, c0 = col0 + r16;      // the lane's first column
     const Piece whole{seq, first, len, 0, len};
-    const T* qs = sequence_base<const T>(p.q, p.pieces, whole) + key_head * p.q_head;
-    const T* ks = sequence_base<const T>(p.k, p.pieces, whole) + key_head * p.k_head;
+    const StageFrom<T> source{p.blocks + slot0 * p.heads + head, sequence_base<const T>(p.k, p.pieces, whole) + key_head * p.k_head,
+                              sequence_base<const T>(p.q, p.pieces, whole) + key_head * p.q_head, p.k.row, p.q.row, p.heads, len, p.key_dim};
+    if (kHelp && wave >= kWavesPerBlock) {
+        if (blocks > 0) stage_all<S>(source, rooms, 0, 1, blocks);
+        return;
+    }
     const T* vs = sequence_base<const T>(p.v, p.pieces, whole) + head * p.v_head;
     T* os = sequence_base<T>(p.out, p.pieces, whole) + head * p.out_head;
     const long long state_at = ((long long)seq * p.heads + head) * p.key_dim * p.value_dim;
-    const unsigned kstride = (unsigned)p.k.row, qstride = (unsigned)p.q.row, vstride = (unsigned)p.v.row, ostride = (unsigned)p.out.row;
-    const Block* from = p.blocks + slot0 * p.heads + head;
+    const unsigned vstride = (unsigned)p.v.row, ostride = (unsigned)p.out.row;
 
     Float4 s[2 * KT][NT];
     if (p.state) {
@@ -55,28 +59,27 @@ __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
     Cols v;
     int rows = len < kDeltaRows ? len : kDeltaRows;
     if (blocks > 0) {
-        stage.load(*from, ks, kstride, qs, qstride, rows, p.key_dim);
+        if (!kHelp) source.load(stage, 0);
         v.load(vs, vstride, rows, col0, p.value_dim);
+        if (kHelp) __syncthreads();
     }
     for (int c = 0; c < blocks; ++c) {
-        __syncthreads();
-        stage.put(room, *from, ks, kstride, qs, qstride, rows, p.key_dim);
+        WalkRoom<T, KT>& room = rooms[kHelp ? c & 1 : 0];
+        if (!kHelp) {
+            __syncthreads();
+            source.put(stage, room, c);
+        }
         float* const mark = p.marks ? mark_of(p.marks, p, slot0 + c, head) : nullptr;
         if (mark) store_state<KT, NT>(mark, p.value_dim, p.key_dim, c0, s);
         Float4 x[4][NT], o[4][NT];
         v.values(columns[wave], rows, x);
-        __syncthreads();
-        const T *const this_ks = ks, *const this_qs = qs;
-        const Block* const this_from = from;
+        if (!kHelp) __syncthreads();
         const int this_rows = rows;
         if (c + 1 < blocks) {
-            ks += (long long)kDeltaRows * p.k.row;
-            qs += (long long)kDeltaRows * p.q.row;
             vs += (long long)kDeltaRows * p.v.row;
-            from += p.heads;
             rows = len - (c + 1) * kDeltaRows;
             rows = rows < kDeltaRows ? rows : kDeltaRows;
-            stage.load(*from, ks, kstride, qs, qstride, rows, p.key_dim);
+            if (!kHelp) source.load(stage, c + 1);
             v.load(vs, vstride, rows, col0, p.value_dim);
         }
 
@@ -114,7 +117,7 @@ __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
             }
             if constexpr (S::kOnePlace) {
                 __syncthreads();
-                S::put_now(room, *this_from, this_ks, kstride, this_qs, qstride, this_rows, p.key_dim, S::kSquares, 2 * S::kSquares);
+                source.template put_queries<S>(room, c);
                 __syncthreads();
 #pragma unroll
                 for (int m = 0; m < 4; m += 2) {
@@ -190,6 +193,7 @@ __global__ __launch_bounds__(kBlock) void delta_walk(DeltaParams p)
                         for (int i = 0; i < 4; ++i) s[j + k][n][i] = __builtin_fmaf(total, s[j + k][n][i], a[k][n][i] * back_u[n]);
             }
         }
+        if (kHelp) __syncthreads();
     }
     if (p.final) store_state<KT, NT>(p.final + state_at, p.value_dim, p.key_dim, c0, s);
 }
@@ -258,10 +262,10 @@ int ssam_scan_delta(const ssam_scan_delta_args* a, void* hip_stream)
             const dim3 walks((unsigned)(heads * p.tiles));
             if constexpr (KT <= 4)
                 if (wide) {
-                    hipLaunchKernelGGL((delta_walk<T, KT, 2>), walks, dim3(kBlock), 0, st, p);
+                    hipLaunchKernelGGL((delta_walk<T, KT, 2>), walks, dim3(kWalkThreads<T, KT, 2>), 0, st, p);
                     return launched();
                 }
-            hipLaunchKernelGGL((delta_walk<T, KT, 1>), walks, dim3(kBlock), 0, st, p);
+            hipLaunchKernelGGL((delta_walk<T, KT, 1>), walks, dim3(kWalkThreads<T, KT, 1>), 0, st, p);
             return launched();
         });
     });

@@ -32,10 +32,11 @@ __global__ __launch_bounds__(kBlock) void delta_back_prepare(DeltaParams p)
 
 // One wave: 16 NT columns of the gradient of a head's state, from the last block to the first.
 template <class T, int KT, int NT>
-__global__ __launch_bounds__(kBlock) void delta_back_walk(DeltaBackParams b)
+__global__ __launch_bounds__((kWalkThreads<T, KT, NT>)) void delta_back_walk(DeltaBackParams b)
 {
     const DeltaParams& p = b.f;
-    __shared__ WalkRoom<T, KT> room;
+    constexpr bool kHelp = kHelped<T, KT, NT>;
+    __shared__ WalkRoom<T, KT> rooms[kHelp ? 2 : 1];
     typedef Stage<T, KT, true> S;
     typedef Columns<T, NT, kSplit<T> && (KT > 4)> Cols;
     __shared__ typename Cols::Room columns[kWavesPerBlock];
@@ -50,13 +51,16 @@ __global__ __launch_bounds__(kBlock) void delta_back_walk(DeltaBackParams b)
     const int col0 = (tile * kWavesPerBlock + __builtin_amdgcn_readfirstlane(wave)) * 16 * NT, c0 = col0 + r16;
     const Piece whole{seq, first, len, 0, len};
     const long long end = (long long)(blocks - 1) * kDeltaRows;                                  // first row of the last block
-    const T* qs = sequence_base<const T>(p.q, p.pieces, whole) + key_head * p.q_head + end * p.q.row;
-    const T* ks = sequence_base<const T>(p.k, p.pieces, whole) + key_head * p.k_head + end * p.k.row;
+    const StageFrom<T> source{p.blocks + slot0 * p.heads + head, sequence_base<const T>(p.k, p.pieces, whole) + key_head * p.k_head,
+                              sequence_base<const T>(p.q, p.pieces, whole) + key_head * p.q_head, p.k.row, p.q.row, p.heads, len, p.key_dim};
+    if (kHelp && wave >= kWavesPerBlock) {
+        if (blocks > 0) stage_all<S>(source, rooms, blocks - 1, -1, blocks);
+        return;
+    }
     const T* dos = sequence_base<const T>(b.grad_out, p.pieces, whole) + head * b.grad_out_head + end * b.grad_out.row;
     T* dvs = b.grad_v.d ? sequence_base<T>(b.grad_v, p.pieces, whole) + head * b.grad_v_head + end * b.grad_v.row : nullptr;
     const long long state_at = ((long long)seq * p.heads + head) * p.key_dim * p.value_dim;
-    const unsigned kstride = (unsigned)p.k.row, qstride = (unsigned)p.q.row, ostride = (unsigned)b.grad_out.row, vstride = (unsigned)b.grad_v.row;
-    const Block* from = p.blocks + (slot0 + blocks - 1) * p.heads + head;
+    const unsigned ostride = (unsigned)b.grad_out.row, vstride = (unsigned)b.grad_v.row;
 
     Float4 s[2 * KT][NT];
     if (p.state) {
@@ -71,27 +75,26 @@ __global__ __launch_bounds__(kBlock) void delta_back_walk(DeltaBackParams b)
     Cols v;
     int rows = len - (blocks - 1) * kDeltaRows;
     if (blocks > 0) {
-        stage.load(*from, ks, kstride, qs, qstride, rows, p.key_dim);
+        if (!kHelp) source.load(stage, blocks - 1);
         v.load(dos, ostride, rows, col0, p.value_dim);
+        if (kHelp) __syncthreads();
     }
     for (int c = blocks - 1; c >= 0; --c) {
-        __syncthreads();
-        stage.put(room, *from, ks, kstride, qs, qstride, rows, p.key_dim);
+        WalkRoom<T, KT>& room = rooms[kHelp ? (blocks - 1 - c) & 1 : 0];
+        if (!kHelp) {
+            __syncthreads();
+            source.put(stage, room, c);
+        }
         float* const behind = mark_of(b.behind, p, slot0 + c, head);
         store_state<KT, NT>(behind, p.value_dim, p.key_dim, c0, s);
         Float4 o[4][NT], x[4][NT];       // dO; dU, dY, dX
         v.values(columns[wave], rows, o);
-        __syncthreads();
-        const T *const this_ks = ks, *const this_qs = qs;
-        const Block* const this_from = from;
+        if (!kHelp) __syncthreads();
         const int this_rows = rows;
         if (c > 0) {
-            ks -= (long long)kDeltaRows * p.k.row;
-            qs -= (long long)kDeltaRows * p.q.row;
             dos -= (long long)kDeltaRows * b.grad_out.row;
-            from -= p.heads;
             rows = kDeltaRows;
-            stage.load(*from, ks, kstride, qs, qstride, rows, p.key_dim);
+            if (!kHelp) source.load(stage, c - 1);
             v.load(dos, ostride, rows, col0, p.value_dim);
         }
         {
@@ -124,7 +127,7 @@ __global__ __launch_bounds__(kBlock) void delta_back_walk(DeltaBackParams b)
         }
         if constexpr (S::kOnePlace) {
             __syncthreads();
-            S::put_now(room, *this_from, this_ks, kstride, this_qs, qstride, this_rows, p.key_dim, S::kSquares, 2 * S::kSquares);
+            source.template put_queries<S>(room, c);
             __syncthreads();
         }
         HalfPair f[2][NT];
@@ -186,6 +189,7 @@ __global__ __launch_bounds__(kBlock) void delta_back_walk(DeltaBackParams b)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[j][n][i] = __builtin_fmaf(total, s[j][n][i], __builtin_fmaf(a[n][i], back[n], q[n][i] * back_o[n]));
         }
+        if (kHelp) __syncthreads();
     }
     if (b.grad_state) store_state<KT, NT>(b.grad_state + state_at, p.value_dim, p.key_dim, c0, s);
 }
@@ -896,7 +900,7 @@ int ssam_scan_delta_backward(const ssam_scan_delta_backward_args* a, void* hip_s
             constexpr int KT = decltype(kt)::value;
             hipLaunchKernelGGL((delta_back_prepare<T, KT>), dim3((unsigned)rows), dim3(kBlock), 0, st, b.f);
             if (int e = launched()) return e;
-            hipLaunchKernelGGL((delta_back_walk<T, KT, 1>), dim3((unsigned)walks), dim3(kBlock), 0, st, b);
+            hipLaunchKernelGGL((delta_back_walk<T, KT, 1>), dim3((unsigned)walks), dim3(kWalkThreads<T, KT, 1>), 0, st, b);
             if (int e = launched()) return e;
             if (!a->grad_q.d && !a->grad_k.d && !a->grad_g.d && !a->grad_beta.d) return (int)SSAM_OK;
             if (a->heads > a->key_heads) hipLaunchKernelGGL((delta_back_rows<T, KT, true>), dim3((unsigned)rows), dim3(kRowThreads), 0, st, b);

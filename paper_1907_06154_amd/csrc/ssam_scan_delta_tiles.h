@@ -338,6 +338,9 @@ __device__ __forceinline__ void put_turned(const Half8 (&hi)[8], const Half8 (&l
     }
 }
 
+// kBlock threads, the last ones of a block of more, stage.
+__device__ __forceinline__ int stage_thread() { return (int)(threadIdx.x & (kBlock - 1)); }
+
 // What a block of threads brings in of a block of rows: k's rows as operands in both forms, q's as rows (kTurn: turned), the block's matrices and factors.
 // load() requests it, put() writes it into LDS; kAhead: into registers, so that the loads of the next block's pass behind the work on this one.
 template <class T, int KT, bool kTurn>
@@ -374,7 +377,7 @@ struct Stage {
     __device__ __forceinline__ void load(const Block& from, const T* ks, unsigned kstride, const T* qs, unsigned qstride, int rows, int dim)
     {
         if constexpr (kAhead) {
-            const int job = threadIdx.x, b = (job % kSquares) / kAcross, e = job % kAcross;
+            const int job = stage_thread(), b = (job % kSquares) / kAcross, e = job % kAcross;
             const bool query = kSquares % kWave == 0 ? __builtin_amdgcn_readfirstlane(job) >= kSquares : job >= kSquares;
             if (kBlock == 2 * kSquares || job < 2 * kSquares) {
                 load_square<T>(query ? qs : ks, query ? qstride : kstride, rows, dim, b, e, square);
@@ -383,7 +386,7 @@ struct Stage {
 #pragma unroll
             for (int i = 0; i < kOfThread; ++i) {
                 const int behind = (i + 1) * kBlock - kVecs;      // threads of the last round that have none: copies of others
-                block[i] = *(reinterpret_cast<const Float4*>(&from) + (behind > 0 ? i * kBlock - behind : i * kBlock) + threadIdx.x);
+                block[i] = *(reinterpret_cast<const Float4*>(&from) + (behind > 0 ? i * kBlock - behind : i * kBlock) + stage_thread());
             }
         }
     }
@@ -391,23 +394,23 @@ struct Stage {
     {
         Float4* const to = reinterpret_cast<Float4*>(&room.m);
         if constexpr (kAhead) {
-            const int job = threadIdx.x;
+            const int job = stage_thread();
             if (kBlock == 2 * kSquares || job < 2 * kSquares) put_square(room, job >= kSquares, (job % kSquares) / kAcross, job % kAcross, rows, dim, square, scale);
 #pragma unroll
             for (int i = 0; i < kOfThread; ++i) {
                 const int behind = (i + 1) * kBlock - kVecs;
-                to[(behind > 0 ? i * kBlock - behind : i * kBlock) + (int)threadIdx.x] = block[i];
+                to[(behind > 0 ? i * kBlock - behind : i * kBlock) + stage_thread()] = block[i];
             }
         } else {
             put_now(room, from, ks, kstride, qs, qstride, rows, dim, 0, kOnePlace ? kSquares : 2 * kSquares);
-            for (int at = threadIdx.x; at < kVecs; at += kBlock) to[at] = reinterpret_cast<const Float4*>(&from)[at];
+            for (int at = stage_thread(); at < kVecs; at += kBlock) to[at] = reinterpret_cast<const Float4*>(&from)[at];
         }
     }
     // Squares first .. last - 1: the keys', then the queries'.
     static __device__ __forceinline__ void put_now(WalkRoom<T, KT>& room, const Block& from, const T* ks, unsigned kstride, const T* qs, unsigned qstride, int rows,
                                                    int dim, int first, int last)
     {
-        for (int job = first + (int)threadIdx.x; job < last; job += kBlock) {
+        for (int job = first + stage_thread(); job < last; job += kBlock) {
             const bool query = job >= kSquares;
             const int b = (job % kSquares) / kAcross, e = job % kAcross;
             RowVec<T, 8> v[8];
@@ -496,6 +499,57 @@ __device__ __forceinline__ void tri_products(const Half8 (&matrix)[2][kTriOperan
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
                         y[m][n] = mfma(a[term == 2][kUpper ? upper_operand(m, s) : lower_operand(m, s)], term == 1 ? f[s][n].lo : f[s][n].hi, y[m][n]);
+}
+
+// Walks whose operands fit into LDS twice leave the staging to four waves of their own: the next block's operands are made while this one's are used, one
+// barrier a block, and loads, conversions and LDS writes (4300 of a block's 12300 cycles in one wave) pass beside the products.
+template <class T, int KT, int NT> constexpr bool kHelped = !kSplit<T> && KT <= 4 && NT == 1;
+template <class T, int KT, int NT> constexpr int kWalkThreads = kHelped<T, KT, NT> ? 2 * kBlock : kBlock;
+
+// Where a sequence's blocks are, for staging.
+template <class T>
+struct StageFrom {
+    const Block* blocks;
+    const T *ks, *qs;
+    long long krow, qrow;
+    int heads, len, dim;
+
+    template <class S> __device__ __forceinline__ void load(S& stage, int c) const
+    {
+        const int rows = len - c * kDeltaRows;
+        stage.load(blocks[(long long)c * heads], ks + (long long)c * kDeltaRows * krow, (unsigned)krow, qs + (long long)c * kDeltaRows * qrow, (unsigned)qrow,
+                   rows < kDeltaRows ? rows : kDeltaRows, dim);
+    }
+    template <class S, class Room> __device__ __forceinline__ void put(S& stage, Room& room, int c) const
+    {
+        const int rows = len - c * kDeltaRows;
+        stage.put(room, blocks[(long long)c * heads], ks + (long long)c * kDeltaRows * krow, (unsigned)krow, qs + (long long)c * kDeltaRows * qrow, (unsigned)qrow,
+                  rows < kDeltaRows ? rows : kDeltaRows, dim);
+    }
+    template <class S, class Room> __device__ __forceinline__ void put_queries(Room& room, int c) const
+    {
+        const int rows = len - c * kDeltaRows;
+        S::put_now(room, blocks[(long long)c * heads], ks + (long long)c * kDeltaRows * krow, (unsigned)krow, qs + (long long)c * kDeltaRows * qrow, (unsigned)qrow,
+                   rows < kDeltaRows ? rows : kDeltaRows, dim, S::kSquares, 2 * S::kSquares);
+    }
+};
+
+// The staging waves' part: blocks from, from + step .. (n of them), each into the room that the others are not reading.
+template <class S, class T, class Room>
+__device__ __forceinline__ void stage_all(const StageFrom<T>& source, Room* rooms, int from, int step, int n)
+{
+    S stage;
+    source.load(stage, from);
+    source.put(stage, rooms[0], from);
+    if (n > 1) source.load(stage, from + step);
+    __syncthreads();
+    for (int k = 1; k <= n; ++k) {
+        if (k < n) {
+            source.put(stage, rooms[k & 1], from + k * step);
+            if (k + 1 < n) source.load(stage, from + (k + 1) * step);
+        }
+        __syncthreads();
+    }
 }
 
 // 64 rows of a wave's columns as B operands; their power of two, per column.
