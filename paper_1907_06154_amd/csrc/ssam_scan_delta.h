@@ -124,6 +124,14 @@ __device__ __forceinline__ float* mark_of(float* marks, const DeltaParams& p, lo
     return marks + (slot * p.heads + head) * (long long)(p.key_dim + kDeltaRows) * p.value_dim;
 }
 
+// Blocks go to the eight XCDs in turn; neighbours, which read the same rows of q and k, are made those of one XCD and its L2.
+__device__ __forceinline__ unsigned near_block()
+{
+    constexpr unsigned kXcds = 8;
+    const unsigned each = gridDim.x / kXcds, whole = each * kXcds;
+    return blockIdx.x < whole ? blockIdx.x % kXcds * each + blockIdx.x / kXcds : blockIdx.x;
+}
+
 // ---- checks ----------------------------------------------------------------------------------------------------------------
 template <class Args>
 int check_delta(const Args& a)

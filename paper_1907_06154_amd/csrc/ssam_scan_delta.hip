@@ -27,7 +27,8 @@ __global__ __launch_bounds__((kWalkThreads<T, KT, NT>)) void delta_walk(DeltaPar
     __shared__ typename Cols::Room columns[kWavesPerBlock];
     constexpr int kParts = kSplit<T> ? 2 : 1;       // of q and k
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid >> 6, g = lane >> 4, r16 = lane & 15;
-    const int tile = (int)(blockIdx.x % p.tiles), head = (int)(blockIdx.x / p.tiles % p.heads), seq = (int)(blockIdx.x / p.tiles / p.heads);
+    const unsigned block = near_block();
+    const int tile = (int)(block % p.tiles), head = (int)(block / p.tiles % p.heads), seq = (int)(block / p.tiles / p.heads);
     const int key_head = head / (p.heads / p.key_heads);
     int first, len;
     span_of(p.pieces, seq, first, len);

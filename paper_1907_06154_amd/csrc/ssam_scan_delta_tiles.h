@@ -447,29 +447,18 @@ template <int K, int NT, int P>
 __device__ __forceinline__ void products_of(const Half8 (&a)[P][K], const HalfPair (&f)[K][NT], const Half8 (&b)[P][K], const HalfPair (&e)[K][NT], Float4 (&y)[NT],
                                             Float4 (&z)[NT])
 {
-    Float4 yl[NT], zl[NT];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) y[n] = z[n] = yl[n] = zl[n] = Float4(0.0f);
+    for (int n = 0; n < NT; ++n) y[n] = z[n] = Float4(0.0f);
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            y[n] = mfma(a[0][k], f[k][n].hi, y[n]);
-            z[n] = mfma(b[0][k], e[k][n].hi, z[n]);
-            yl[n] = mfma(a[0][k], f[k][n].lo, yl[n]);
-            zl[n] = mfma(b[0][k], e[k][n].lo, zl[n]);
-            if constexpr (P > 1) {
-                yl[n] = mfma(a[1][k], f[k][n].hi, yl[n]);
-                zl[n] = mfma(b[1][k], e[k][n].hi, zl[n]);
-            }
-        }
+        for (int term = 0; term < (P > 1 ? 3 : 2); ++term)
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        y[n] += yl[n];
-        z[n] += zl[n];
-    }
+            for (int n = 0; n < NT; ++n) {
+                y[n] = mfma(a[term == 2 ? P - 1 : 0][k], term == 1 ? f[k][n].lo : f[k][n].hi, y[n]);
+                z[n] = mfma(b[term == 2 ? P - 1 : 0][k], term == 1 ? e[k][n].lo : e[k][n].hi, z[n]);
+            }
 }
-
 template <int K, int NT, int P>
 __device__ __forceinline__ void products(const Half8 (&a)[P][K], const Half8 (&b)[P][K], const HalfPair (&f)[K][NT], Float4 (&y)[NT], Float4 (&z)[NT])
 {
