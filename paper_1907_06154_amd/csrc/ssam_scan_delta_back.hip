@@ -265,69 +265,82 @@ template <class T>
 struct RowData {
     static constexpr int kPasses = kDeltaRows * 16 / kRowThreads;
     RowVec<T, 8> o[kPasses];
-    RowVec<float, 8> y[kPasses], u[kPasses];
+    Eight y[kPasses], u[kPasses];
 
-    __device__ __forceinline__ void load(const T* dos, unsigned stride, const float* ys, const float* us, int dim, int rows, int v0)
+    __device__ __forceinline__ void load(int tid, const T* dos, unsigned stride, const float* ys, const float* us, int dim, int rows, int v0)
     {
-        const int at = v0 + 8 * (int)(threadIdx.x & 15), have = dim - at;
-        const unsigned c = have > 0 ? at : 0;
-        if (dim % 8 == 0) {
+        const int at = v0 + 8 * (tid & 15), row = (tid >> 4);
+        if (dim >= 8) {
+            const unsigned c = (unsigned)(at + 8 <= dim ? at : dim - 8);
 #pragma unroll
             for (int k = 0; k < kPasses; ++k) {
-                const int t = (int)(threadIdx.x >> 4) + k * (kRowThreads / 16);
-                __builtin_memcpy(&o[k], dos + (unsigned)(t < rows ? t : rows - 1) * stride + c, sizeof(o[k]));
-                __builtin_memcpy(&y[k], ys + (unsigned)(t * dim) + c, sizeof(y[k]));
-                __builtin_memcpy(&u[k], us + (unsigned)(t * dim) + c, sizeof(u[k]));
+                const int t = row + k * (kRowThreads / 16);
+                __builtin_memcpy(&o[k], dos + ((unsigned)(t < rows ? t : rows - 1) * stride + c), sizeof(o[k]));
+                y[k].load(ys + ((unsigned)(t * dim) + c));
+                u[k].load(us + ((unsigned)(t * dim) + c));
             }
         } else {
 #pragma unroll
             for (int k = 0; k < kPasses; ++k) {
-                const int t = (int)(threadIdx.x >> 4) + k * (kRowThreads / 16);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const unsigned e = (unsigned)(at + i < dim ? at + i : dim - 1);
-                    o[k][i] = dos[(unsigned)(t < rows ? t : rows - 1) * stride + e];
-                    y[k][i] = ys[(unsigned)(t * dim) + e];
-                    u[k][i] = us[(unsigned)(t * dim) + e];
-                }
+                const int t = row + k * (kRowThreads / 16);
+                o[k] = load_few(dos + (unsigned)(t < rows ? t : rows - 1) * stride, dim);
+                y[k].load(ys + (unsigned)(t * dim), dim);
+                u[k].load(us + (unsigned)(t * dim), dim);
             }
         }
+    }
+    // What pass k has, zeros where nothing is.
+    __device__ __forceinline__ void take(int tid, int k, int rows, int dim, int v0)
+    {
+        const int at = v0 + 8 * (tid & 15);
+        if ((tid >> 4) + k * (kRowThreads / 16) >= rows) o[k] = RowVec<T, 8>(T(0));
+        if (v0 + kAcross <= dim) return;
+        if (dim % 8) {
+            o[k] = shifted(o[k], shift_of(at, dim));
+            y[k].shift(shift_of(at, dim));
+            u[k].shift(shift_of(at, dim));
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (at + i >= dim) o[k][i] = T(0);
+        y[k].clear(dim - at);
+        u[k].clear(dim - at);
     }
 };
 // Some of a state's rows, 8 of 32 values a lane and step.
 struct StateRow {
-    RowVec<float, 8> v[kAcrossSteps];
+    Eight v[kAcrossSteps];
     __device__ __forceinline__ void load(const float* state, int d, int key_dim, int dim, int v0)
     {
         const int g = (threadIdx.x & (kWave - 1)) >> 4;
         const float* const row = state + (size_t)(d < key_dim ? d : key_dim - 1) * dim;
-        if (dim % 8 == 0) {
+        if (dim >= 8) {
 #pragma unroll
             for (int s = 0; s < kAcrossSteps; ++s) {
                 const int at = v0 + 32 * s + 8 * g;
-                __builtin_memcpy(&v[s], row + (at < dim ? at : 0), 32);
+                v[s].load(row + (unsigned)(at + 8 <= dim ? at : dim - 8));
             }
         } else {
 #pragma unroll
-            for (int s = 0; s < kAcrossSteps; ++s)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int at = v0 + 32 * s + 8 * g + i;
-                    v[s][i] = row[at < dim ? at : dim - 1];
-                }
+            for (int s = 0; s < kAcrossSteps; ++s) v[s].load(row, dim);
         }
     }
     __device__ __forceinline__ float clear(int d, int key_dim, int dim, int v0)      // and the largest magnitude
     {
         const int g = (threadIdx.x & (kWave - 1)) >> 4;
+        if (v0 + kAcross > dim) {
+#pragma unroll
+            for (int s = 0; s < kAcrossSteps; ++s) {
+                const int at = v0 + 32 * s + 8 * g;
+                if (dim % 8) v[s].shift(shift_of(at, dim));
+                v[s].clear(dim - at);
+            }
+        }
         float m = 0.0f;
 #pragma unroll
         for (int s = 0; s < kAcrossSteps; ++s) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (!(d < key_dim && v0 + 32 * s + 8 * g + i < dim)) v[s][i] = 0.0f;
-                m = larger(m, v[s][i]);
-            }
+            if (d >= key_dim) v[s].lo = v[s].hi = Float4(0.0f);
+            m = larger(larger(m, v[s].lo), v[s].hi);
         }
         return m;
     }
@@ -341,7 +354,8 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
     typedef RowsRoom<T, KT> Room;
     constexpr int kParts = kSplit<T> ? 2 : 1, kTiles = (2 * KT + kRowWaves - 1) / kRowWaves;      // of a wave, along the keys
     __shared__ Room room;
-    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int tid = threadIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int lane = tid & (kWave - 1), g = lane >> 4, r = lane & 15;
     const int slot = (int)(blockIdx.x / p.key_heads), key_head = (int)(blockIdx.x % p.key_heads), many = kShared ? p.heads / p.key_heads : 1;
     const Piece piece = find_piece(p.pieces, slot);
@@ -359,7 +373,7 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
             gate = p.g.d ? sequence_base<const float>(p.g, p.pieces, piece)[at * p.g.row + h] : 0.0f;
             beta_ = sequence_base<const float>(p.beta, p.pieces, piece)[at * p.beta.row + h];
         }
-        data.load(grads + h * b.grad_out_head, (unsigned)b.grad_out.row, mark_of(b.behind, p, slot, h) + below, mark_of(p.marks, p, slot, h) + below, p.value_dim,
+        data.load(tid, grads + h * b.grad_out_head, (unsigned)b.grad_out.row, mark_of(b.behind, p, slot, h) + below, mark_of(p.marks, p, slot, h) + below, p.value_dim,
                   piece.n, 0);
     };
     const int tile = wave & 3, col0 = wave >> 2 << 1;      // of the 64 x 64 products: a wave's tile of rows and its two of columns
@@ -396,7 +410,7 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
         }
     };
     // Addresses in LDS are made anew for every step of the work: all of them together, kept over the loops, would take the registers of everything else.
-    auto fresh_lane = [&] { asm volatile("" : "+v"(lane), "+v"(g), "+v"(r)); };
+    auto fresh_lane = [&] { asm volatile("" : "+v"(tid), "+v"(lane), "+v"(g), "+v"(r)); };
     Float4 dq[4][kTiles], dk[4][kTiles];      // sums over the heads that share the key
 #pragma unroll
     for (int m = 0; m < 4; ++m)
@@ -435,35 +449,27 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
         }
         for (int v0 = 0; v0 < p.value_dim; v0 += kAcross) {
             fresh_lane();
-            if (v0) data.load(grads + h * b.grad_out_head, (unsigned)b.grad_out.row, behind + below, mark + below, p.value_dim, piece.n, v0);
+            if (v0) data.load(tid, grads + h * b.grad_out_head, (unsigned)b.grad_out.row, behind + below, mark + below, p.value_dim, piece.n, v0);
             __syncthreads();
             // dO, dX = b dY and U = b R as operands
             const int e = tid & 15;
-            const bool whole = v0 + kAcross <= p.value_dim;
 #pragma unroll
             for (int k = 0; k < RowData<T>::kPasses; ++k) {
                 const int t = (tid >> 4) + k * (kRowThreads / 16);
                 const float beta = room.beta[t];
+                data.take(tid, k, piece.n, p.value_dim, v0);
                 RowVec<T, 8>& o = data.o[k];
-                RowVec<float, 8>&y = data.y[k], &u = data.u[k];
-                if (t >= piece.n) o = RowVec<T, 8>(T(0));
-                if (!whole)
+                Eight &y = data.y[k], &u = data.u[k];
+                float dot = 0.0f, mo = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (v0 + 8 * e + i >= p.value_dim) {
-                            o[i] = T(0);
-                            y[i] = u[i] = 0.0f;
-                        }
-                float dot = 0.0f, mo = 0.0f, mx = 0.0f, mu = 0.0f;
+                for (int i = 0; i < 4; ++i) dot = __builtin_fmaf(y.lo[i], u.lo[i], __builtin_fmaf(y.hi[i], u.hi[i], dot));
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    dot = __builtin_fmaf(y[i], u[i], dot);
-                    y[i] *= beta;
-                    u[i] *= beta;
-                    mo = larger(mo, (float)o[i]);
-                    mx = larger(mx, y[i]);
-                    mu = larger(mu, u[i]);
-                }
+                for (int i = 0; i < 8; ++i) mo = larger(mo, (float)o[i]);
+                y.lo *= beta;
+                y.hi *= beta;
+                u.lo *= beta;
+                u.hi *= beta;
+                float mx = larger(larger(0.0f, y.lo), y.hi), mu = larger(larger(0.0f, u.lo), u.hi);
                 dot = over_few(dot, 16, Add());
                 mo = over_few(mo, 16, Max());
                 mx = over_few(mx, 16, Max());
@@ -482,12 +488,11 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
                 to_halves<T>(o, so.to, hi, lo);
                 room.o.grad[0][operand][entry] = hi;
                 if constexpr (kParts > 1) room.o.grad[1][operand][entry] = lo;
-                to_halves<float>(y, sx.to, hi, lo);
-                room.o.x[0][operand][entry] = hi;
-                room.o.x[1][operand][entry] = lo;
-                to_halves<float>(u, su.to, hi, lo);
-                room.o.u[0][operand][entry] = hi;
-                room.o.u[1][operand][entry] = lo;
+                const HalfPair py = split(y.lo, y.hi, sx.to), pu = split(u.lo, u.hi, su.to);
+                room.o.x[0][operand][entry] = py.hi;
+                room.o.x[1][operand][entry] = py.lo;
+                room.o.u[0][operand][entry] = pu.hi;
+                room.o.u[1][operand][entry] = pu.lo;
             }
             StateRow s0, s1;
             s0.load(mark, tile_row(wave * kTiles, r), p.key_dim, p.value_dim, v0);
@@ -531,7 +536,7 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
                     const Scale by(over_column(s.clear(row, p.key_dim, p.value_dim, v0)));
                     back = by.back;
 #pragma unroll
-                    for (int k = 0; k < kAcrossSteps; ++k) to_halves<float>(s.v[k], by.to, f[k].hi, f[k].lo);
+                    for (int k = 0; k < kAcrossSteps; ++k) f[k] = split(s.v[k].lo, s.v[k].hi, by.to);
                 };
                 to_operands(s0);
                 s1.load(behind, d, p.key_dim, p.value_dim, v0);
@@ -564,7 +569,7 @@ __global__ __launch_bounds__(kRowThreads) void delta_back_rows(DeltaBackParams b
 #pragma unroll
                 for (int s = 0; s < kAcrossSteps; ++s)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) inner = __builtin_fmaf(s0.v[s][i], s1.v[s][i], inner);
+                    for (int i = 0; i < 4; ++i) inner = __builtin_fmaf(s0.v[s].lo[i], s1.v[s].lo[i], __builtin_fmaf(s0.v[s].hi[i], s1.v[s].hi[i], inner));
                 if (jj + 1 < kTiles) s0.load(mark, tile_row(j + 1, r), p.key_dim, p.value_dim, v0);
                 in_order();
 #pragma unroll

@@ -59,12 +59,29 @@ template <int KT> __device__ __forceinline__ Half8 turned_of(const Half8 (&a)[4 
     return a[turned_operand(j, k)][turned_entry(j, lane >> 4, lane & 15)];
 }
 
+// Operands are read from LDS a step ahead of the products that take them, and products on several results alternate: one waits for its own last sum.
+// (Left to itself the compiler reads an operand, waits for it and uses it, one after the other.)
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
 // A value, the same for all lanes, that the compiler takes for a new one here: what is made from it is not kept in registers over a loop.  (Rows' distances,
 // 16 to 64 of them, would be, and push everything else out.)
 __device__ __forceinline__ unsigned afresh(unsigned v)
 {
     v = __builtin_amdgcn_readfirstlane(v);
     asm volatile("" : "+s"(v));
+    return v;
+}
+
+// Eight elements of a row of fewer: copies of the last one behind it.  One after the other: a rare case that is to cost the others no registers.
+template <class T>
+__device__ __forceinline__ RowVec<T, 8> load_few(const T* __restrict__ row, int dim)
+{
+    RowVec<T, 8> v(T(0));
+#pragma unroll 1
+    for (int i = 7; i >= 0; --i) {
+        v = __builtin_shufflevector(v, v, 0, 0, 1, 2, 3, 4, 5, 6);
+        v[0] = row[i < dim ? i : dim - 1];
+    }
     return v;
 }
 
@@ -75,33 +92,91 @@ template <class T, int N>
 __device__ __forceinline__ void load_eights(const T* __restrict__ base, unsigned stride, int row0, int step, int rows, int e, int dim, RowVec<T, 8> (&v)[N])
 {
     stride = afresh(stride);
-    const bool across = 8 * e < dim;
-    const unsigned at = across ? 8 * e : 0;
-    if (dim % 8 == 0 && rows == kDeltaRows) {
+    // (a vector that would pass the last element starts further left)
+    const unsigned at = dim < 8 ? 0 : (unsigned)(8 * e + 8 <= dim ? 8 * e : dim - 8);
+    if (dim >= 8 && rows == kDeltaRows) {
         const unsigned lane_at = (unsigned)row0 * stride + at;
 #pragma unroll
         for (int i = 0; i < N; ++i) __builtin_memcpy(&v[i], base + (unsigned)(i * step) * stride + lane_at, sizeof(v[i]));
-    } else if (dim % 8 == 0) {
+    } else if (dim >= 8) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int row = row0 + i * step;
             __builtin_memcpy(&v[i], base + ((unsigned)(row < rows ? row : rows - 1) * stride + at), sizeof(v[i]));
         }
     } else {
-        const int have = across ? dim - 8 * e : dim;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int row = row0 + i * step;
-            v[i] = load_row_vec<T, 8>(base + ((unsigned)(row < rows ? row : rows - 1) * stride + at), have);
+            v[i] = load_few(base + (unsigned)(row < rows ? row : rows - 1) * stride, dim);
         }
     }
 }
+// Of eight elements that lie `by` places further left than they should: those to their places (copies of something behind them).
+template <class T>
+__device__ __forceinline__ RowVec<T, 8> shifted(RowVec<T, 8> w, int by)
+{
+    if (by & 4) w = __builtin_shufflevector(w, w, 4, 5, 6, 7, 4, 5, 6, 7);
+    if (by & 2) w = __builtin_shufflevector(w, w, 2, 3, 4, 5, 6, 7, 6, 7);
+    if (by & 1) w = __builtin_shufflevector(w, w, 1, 2, 3, 4, 5, 6, 7, 7);
+    return w;
+}
+// Eight floats in two registers of four (arrays of eight that are filled as a whole are left in memory by the compiler).
+struct Eight {
+    Float4 lo, hi;
+    __device__ __forceinline__ void load(const float* p)
+    {
+        typedef Float4 Loose __attribute__((aligned(4)));
+        lo = *reinterpret_cast<const Loose*>(p);
+        hi = *reinterpret_cast<const Loose*>(p + 4);
+    }
+    __device__ __forceinline__ void load(const float* p, int dim)      // of fewer than eight
+    {
+        lo = hi = Float4(0.0f);
+#pragma unroll 1
+        for (int i = 7; i >= 0; --i) {      // one after the other: a rare case that is to cost the others no registers
+            const float v = p[i < dim ? i : dim - 1];
+            hi = Float4{lo[3], hi[0], hi[1], hi[2]};
+            lo = Float4{v, lo[0], lo[1], lo[2]};
+        }
+    }
+    __device__ __forceinline__ void shift(int by)
+    {
+        if (by & 4) lo = hi;
+        if (by & 2) {
+            lo = Float4{lo[2], lo[3], hi[0], hi[1]};
+            hi = Float4{hi[2], hi[3], hi[2], hi[3]};
+        }
+        if (by & 1) {
+            lo = Float4{lo[1], lo[2], lo[3], hi[0]};
+            hi = Float4{hi[1], hi[2], hi[3], hi[3]};
+        }
+    }
+    __device__ __forceinline__ void clear(int from)      // elements from there on
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            lo[i] = i < from ? lo[i] : 0.0f;
+            hi[i] = i + 4 < from ? hi[i] : 0.0f;
+        }
+    }
+};
+// How far left of `at` eight elements of a row of `dim` start.
+__device__ __forceinline__ int shift_of(int at, int dim) { return dim < 8 ? at : at + 8 <= dim ? 0 : at - (dim - 8); }
+
+// Brings the elements to their places, and clears what is not there.
 template <class T, int N>
 __device__ __forceinline__ void clear_eights(int row0, int step, int rows, int e, int dim, RowVec<T, 8> (&v)[N])
 {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int i = 0; i < N; ++i) {
+        if (dim % 8 && dim >= 8) v[i] = shifted(v[i], shift_of(8 * e, dim));
         if (!(8 * e < dim && row0 + i * step < rows)) v[i] = RowVec<T, 8>(T(0));
+        if (dim % 8)
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (8 * e + k >= dim) v[i][k] = T(0);
+    }
 }
 // 8 rows x 8 elements, rows 8 b .. and elements 8 e ..
 template <class T>
@@ -347,7 +422,7 @@ template <class T, int KT, bool kTurn>
 struct Stage {
     static constexpr bool kOnePlace = WalkRoom<T, KT>::kOnePlace;
     static constexpr int kAcross = 4 * KT, kSquares = 8 * kAcross;      // squares of 8 x 8 in a block's keys
-    static constexpr bool kAhead = !kSplit<T> && KT <= 4;
+    static constexpr bool kAhead = (kSplit<T> ? 2 : 1) * KT <= 4;
     static constexpr int kVecs = (int)(sizeof(Block) / 16), kOfThread = (kVecs + kBlock - 1) / kBlock;
     static_assert(sizeof(Block) % 16 == 0);
     RowVec<T, 8> square[kAhead ? 8 : 1];
@@ -421,10 +496,6 @@ struct Stage {
         }
     }
 };
-
-// Operands are read from LDS a step ahead of the products that take them, and products on several results alternate: one waits for its own last sum.
-// (Left to itself the compiler reads an operand, waits for it and uses it, one after the other.)
-__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
 
 template <int KT, int P>
 __device__ __forceinline__ void read_rows(const Half8 (&a)[P][4 * KT][kWave], int m, int lane, Half8 (&to)[P][KT])
