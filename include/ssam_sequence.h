@@ -176,8 +176,12 @@ int ssam_scan_selective_step(const ssam_scan_selective_step_args *args, void *hi
  * follow from the state); rows of no sequence reach nothing.
  * d_marks (NULL: not wanted): what ssam_scan_delta_backward starts from, ssam_scan_delta_marks(args) entries of
  * [heads][key_dim + 64][value_dim] floats: for each 64 rows and sequence the state before them and what the rows correct it by.
- * Operands of the matrix products are held as pairs of fp16, scaled by powers of two, that keep 22 bits of an fp32 value.
- * d_work: ssam_scan_delta_workspace_bytes(args) bytes, 16-byte aligned. */
+ * Operands of the matrix products are held as pairs of fp16, scaled by powers of two, that keep 23 bits of an fp32 value.
+ * key_dim is at most SSAM_MAX_KEY (SSAM_ERR_SHAPE), heads x value_dim at most 2^24; of sequences of more than one row, and of a step's
+ * rows, rows lie at most 2^24 elements apart, here and for the gradients (SSAM_ERR_DIM).
+ * d_work: ssam_scan_delta_workspace_bytes(args) bytes, 16-byte aligned.
+ * Schedules: two launches, the 64 rows' own matrices for all of them at once, then the state's way through them, a block for each head and
+ * 64 or, where there are many, 128 of its values. */
 typedef struct {
     int dtype, heads, key_heads, key_dim, value_dim, unit;
     float scale;
@@ -231,8 +235,9 @@ int ssam_scan_delta_step(const ssam_scan_delta_step_args *args, void *hip_stream
  *     out = gate ? y * gate / (1 + exp(-gate)) : y
  * `sequences` x `rows` rows (a batch's strides count from sequence to sequence).  sum (may be absent, or residual itself) receives s;
  * the norm is that of s as it is stored, so that s is all that the gradients need.  weight: [width] in param_dtype (dtype or
- * SSAM_F32), NULL: ones.
- * ssam_rms_norm_e4m3: out is in 8 bits (e4m3, 448 at most) with a scale for every `block` channels, a divisor of width:
+ * SSAM_F32), NULL: ones.  width is at most 32768 (SSAM_ERR_SHAPE).
+ * ssam_rms_norm_e4m3: out is in 8 bits (e4m3, 448 at most) with a scale for every `block` channels, a divisor of width, 16 at least
+ * or the whole of it (SSAM_ERR_SHAPE):
  *     scale = max over the block of |y| / 448 (at least 2^-126; 1 where all are zero),   out = y / scale, rounded to nearest
  * d_scales: [sequences * rows][channels / block] floats; out's strides count bytes.  (y / scale is made with the rounded reciprocal.) */
 typedef struct {
