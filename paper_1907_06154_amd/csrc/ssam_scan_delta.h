@@ -165,6 +165,15 @@ inline int check_out_heads(const ssam_rows& r, const ssam_sequences& q, int head
     return check_out_rows(r, q, heads_width(heads, apart, dim), esz, optional);
 }
 
+// fp32: with two walks a compute unit or more, a wave takes 32 columns, so that half as many blocks make the same operands: 16 x 512 rows of 32
+// heads of 128 x 128 455 -> 353 us, their gradients 1792 -> 1671, but 4 x 1024 rows (256 walks) 207 -> 257.  16 bits have staging waves in place of it (778 and 793 us for
+// 8 x 4096 rows).  Keys beyond 128 leave no registers for it.
+template <class Args>
+bool wide_walks(const Args& a)
+{
+    return a.dtype == SSAM_F32 && (long long)a.seq.sequences * a.heads * ((a.value_dim + 63) / 64) >= 512 && a.value_dim > 64 && a.key_dim <= 128;
+}
+
 template <class F>
 int with_delta_type(int dtype, F f)
 {

@@ -18,9 +18,9 @@ __global__ __launch_bounds__(kBlock) void delta_prepare(DeltaParams p)
 // One wave: 16 NT columns of a head's state, from its sequence's first block to the last.  The operands made from q, k and the block's matrices
 // are in LDS, the same for the block's four waves; the next block's are on their way in registers.
 template <class T, int KT, int NT>
-__global__ __launch_bounds__((kWalkThreads<T, KT, NT>)) void delta_walk(DeltaParams p)
+__global__ __launch_bounds__((kWalkThreads<T, KT>)) void delta_walk(DeltaParams p)
 {
-    constexpr bool kHelp = kHelped<T, KT, NT>;
+    constexpr bool kHelp = kHelped<T, KT>;
     __shared__ WalkRoom<T, KT> rooms[kHelp ? 2 : 1];
     typedef Stage<T, KT, false> S;
     typedef Columns<T, NT, kSplit<T> && (KT > 4)> Cols;
@@ -250,7 +250,7 @@ int ssam_scan_delta(const ssam_scan_delta_args* a, void* hip_stream)
     DeltaParams p{make_pieces(a->seq, kDeltaRows), a->q, a->k, a->v, a->out, a->g, a->beta, a->q_head, a->k_head, a->v_head, a->out_head, a->d_state,
                   a->d_final, a->d_marks, static_cast<Block*>(a->d_work), a->heads, a->key_heads, a->key_dim, a->value_dim, a->unit != 0, a->scale, 1};
     const long long heads = (long long)a->seq.sequences * a->heads;
-    const bool wide = heads * ((a->value_dim + 63) / 64) >= 512 && a->value_dim > 64 && a->key_dim <= 128;
+    const bool wide = wide_walks(*a);
     p.tiles = (a->value_dim + (wide ? 127 : 63)) / (wide ? 128 : 64);
     if (product(slots, a->key_heads) > kMaxGrid || product(heads, p.tiles) > kMaxGrid) return SSAM_ERR_DIM;
     hipStream_t st = (hipStream_t)hip_stream;
@@ -261,12 +261,12 @@ int ssam_scan_delta(const ssam_scan_delta_args* a, void* hip_stream)
             hipLaunchKernelGGL((delta_prepare<T, KT>), dim3((unsigned)(slots * a->key_heads)), dim3(kBlock), 0, st, p);
             if (int e = launched()) return e;
             const dim3 walks((unsigned)(heads * p.tiles));
-            if constexpr (KT <= 4)
+            if constexpr (kSplit<T> && KT <= 4)
                 if (wide) {
-                    hipLaunchKernelGGL((delta_walk<T, KT, 2>), walks, dim3(kWalkThreads<T, KT, 2>), 0, st, p);
+                    hipLaunchKernelGGL((delta_walk<T, KT, 2>), walks, dim3(kWalkThreads<T, KT>), 0, st, p);
                     return launched();
                 }
-            hipLaunchKernelGGL((delta_walk<T, KT, 1>), walks, dim3(kWalkThreads<T, KT, 1>), 0, st, p);
+            hipLaunchKernelGGL((delta_walk<T, KT, 1>), walks, dim3(kWalkThreads<T, KT>), 0, st, p);
             return launched();
         });
     });

@@ -32,10 +32,10 @@ __global__ __launch_bounds__(kBlock) void delta_back_prepare(DeltaParams p)
 
 // One wave: 16 NT columns of the gradient of a head's state, from the last block to the first.
 template <class T, int KT, int NT>
-__global__ __launch_bounds__((kWalkThreads<T, KT, NT>)) void delta_back_walk(DeltaBackParams b)
+__global__ __launch_bounds__((kWalkThreads<T, KT>)) void delta_back_walk(DeltaBackParams b)
 {
     const DeltaParams& p = b.f;
-    constexpr bool kHelp = kHelped<T, KT, NT>;
+    constexpr bool kHelp = kHelped<T, KT>;
     __shared__ WalkRoom<T, KT> rooms[kHelp ? 2 : 1];
     typedef Stage<T, KT, true> S;
     typedef Columns<T, NT, kSplit<T> && (KT > 4)> Cols;
@@ -881,10 +881,11 @@ int ssam_scan_delta_backward(const ssam_scan_delta_backward_args* a, void* hip_s
                          cover_plain(a->d_grad_final, state_bytes), cover_plain(a->d_marks, (long long)plan.behind)};
     if (any_overlap(outs, ins)) return SSAM_ERR_ALIAS;
 
+    const bool wide = wide_walks(*a);
     DeltaBackParams b{};
     b.f = DeltaParams{make_pieces(a->seq, kDeltaRows), a->q, a->k, a->v, ssam_rows{nullptr, 0, 0}, a->g, a->beta, a->q_head, a->k_head, a->v_head, 0,
                       a->d_grad_final, nullptr, const_cast<float*>(a->d_marks), static_cast<Block*>(a->d_work), a->heads, a->key_heads, a->key_dim,
-                      a->value_dim, a->unit != 0, a->scale, (a->value_dim + 63) / 64};
+                      a->value_dim, a->unit != 0, a->scale, (a->value_dim + (wide ? 127 : 63)) / (wide ? 128 : 64)};
     b.grad_out = a->grad_out;
     b.grad_q = a->grad_q;
     b.grad_k = a->grad_k;
@@ -905,7 +906,9 @@ int ssam_scan_delta_backward(const ssam_scan_delta_backward_args* a, void* hip_s
             constexpr int KT = decltype(kt)::value;
             hipLaunchKernelGGL((delta_back_prepare<T, KT>), dim3((unsigned)rows), dim3(kBlock), 0, st, b.f);
             if (int e = launched()) return e;
-            hipLaunchKernelGGL((delta_back_walk<T, KT, 1>), dim3((unsigned)walks), dim3(kWalkThreads<T, KT, 1>), 0, st, b);
+            if constexpr (kSplit<T> && KT <= 4)
+                if (wide) hipLaunchKernelGGL((delta_back_walk<T, KT, 2>), dim3((unsigned)walks), dim3(kWalkThreads<T, KT>), 0, st, b);
+            if (!wide) hipLaunchKernelGGL((delta_back_walk<T, KT, 1>), dim3((unsigned)walks), dim3(kWalkThreads<T, KT>), 0, st, b);
             if (int e = launched()) return e;
             if (!a->grad_q.d && !a->grad_k.d && !a->grad_g.d && !a->grad_beta.d) return (int)SSAM_OK;
             if (a->heads > a->key_heads) hipLaunchKernelGGL((delta_back_rows<T, KT, true>), dim3((unsigned)rows), dim3(kRowThreads), 0, st, b);

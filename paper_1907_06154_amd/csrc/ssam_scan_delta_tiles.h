@@ -563,8 +563,8 @@ __device__ __forceinline__ void tri_products(const Half8 (&matrix)[2][kTriOperan
 
 // Walks whose operands fit into LDS twice leave the staging to four waves of their own: the next block's operands are made while this one's are used, one
 // barrier a block, and loads, conversions and LDS writes (4300 of a block's 12300 cycles in one wave) pass beside the products.
-template <class T, int KT, int NT> constexpr bool kHelped = !kSplit<T> && KT <= 4 && NT == 1;
-template <class T, int KT, int NT> constexpr int kWalkThreads = kHelped<T, KT, NT> ? 2 * kBlock : kBlock;
+template <class T, int KT> constexpr bool kHelped = !kSplit<T> && KT <= 4;
+template <class T, int KT> constexpr int kWalkThreads = kHelped<T, KT> ? 2 * kBlock : kBlock;
 
 // Where a sequence's blocks are, for staging.
 template <class T>

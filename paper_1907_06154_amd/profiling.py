@@ -8,7 +8,7 @@ profiles/measured_traffic.json, the HBM bytes per launch that bench.py reports a
     python -m paper_1907_06154_amd.profiling catalogue <single.json> <default.json> <out.md>
     python -m paper_1907_06154_amd.profiling sweep <default.json> <variant5.json> <out.md>
     python -m paper_1907_06154_amd.profiling scan <dir> <out.md>
-    python -m paper_1907_06154_amd.profiling operate <case of perf/operators.py>
+    python -m paper_1907_06154_amd.profiling operate <case of perf/operators.py or perf/more_operators.py>
     python -m paper_1907_06154_amd.profiling operators <dir> <out.md>
     python -m paper_1907_06154_amd.profiling against <other libssam.so> <commit it was built from> <out.md>
 
@@ -443,9 +443,10 @@ OPERATE_CALLS = 12
 def operate(name: str) -> None:
     sys.path[:0] = [ROOT, os.path.join(ROOT, "perf")]
     import torch
+    import more_operators
     import operators
+    operators, case = next((m, c) for m in (operators, more_operators) for c in m.listed() if c["name"] == name)
     operators.own = True
-    case = next(c for c in operators.listed() if c["name"] == name)
     sets = [operators.prepare(case, seed) for seed in range(3)]
     torch.cuda.synchronize()
     for i in range(OPERATE_CALLS):
@@ -454,8 +455,10 @@ def operate(name: str) -> None:
 
 
 def operator_kernel(name: str) -> str:
-    """A sequence operator's kernel: its name, element type and states (lane groups of a channel x states of a lane), or ''."""
-    m = re.search(r"(scan_step|scan_rows|scan_back|conv1d_step|conv1d_rows|conv1d_back_sums|conv1d_back|back_sum_bc|back_sum_params|join_pieces)", name)
+    """A sequence operator's kernel: its name, element type and states (lane groups of a channel x states of a lane), or its other template
+    arguments; or ''."""
+    m = re.search(r"(scan_step|scan_rows|scan_back|conv1d_step|conv1d_rows|conv1d_back_sums|conv1d_back|back_sum_bc|back_sum_params|join_pieces"
+                  r"|delta_prepare|delta_walk|delta_back_prepare|delta_back_walk|delta_back_rows|delta_step|rms_norm_back_sums|rms_norm_back|rms_norm)", name)
     if not m:
         return ""
     kind = {"DF16b": " bf16", "DF16_": " fp16", "<float": " fp32", "If": " fp32"}
@@ -464,6 +467,9 @@ def operator_kernel(name: str) -> str:
     if shape:
         whole = re.search(r"Lb([01])E|(true|false)", name[shape.end():])
         text += f" {shape[1]} x {shape[2]}" + (", everything" if whole[0] in ("Lb1E", "true") else ", what the pieces add")
+    if m[1].startswith(("delta_", "rms_norm")):
+        numbers = re.findall(r"L[ib](\d+)E|, (\d+|true|false)", name[m.end():].split("(")[0].split("Params")[0])
+        text += "".join(" " + (a or b) for a, b in numbers)
     if m[1] == "join_pieces":
         text += " backward" if re.search(r"Lb1E|<true>", name) else " forward"
     return text
@@ -480,9 +486,9 @@ def torch_kernel(name: str) -> str:
 def operator_summary(runs: str, out_md: str) -> None:
     ctrs = "SQ_WAVES SQ_INSTS_VALU SQ_ACTIVE_INST_VALU SQ_WAVE_CYCLES SQ_WAIT_ANY SQ_INSTS_LDS SQ_LDS_BANK_CONFLICT SQ_LDS_IDX_ACTIVE"
     run = "--output-format csv -d <dir>/<case>{} -o c -- python3 -m paper_1907_06154_amd.profiling operate <case>\n"
-    out = ["# Sequence operators: the kernels of a call (rocprofv3)\n", "One MI355X, per case of perf/operators.py:\n",
+    out = ["# Sequence operators: the kernels of a call (rocprofv3)\n", "One MI355X, per case of perf/operators.py or perf/more_operators.py:\n",
            "    rocprofv3 --kernel-trace " + run.format("") + f"    rocprofv3 --pmc {ctrs} " + run.format("_pmc") +
-           "    python -m paper_1907_06154_amd.profiling operators <dir> profiles/sequence_operators.md\n",
+           "    python -m paper_1907_06154_amd.profiling operators <dir> " + os.path.relpath(os.path.abspath(out_md), ROOT) + "\n",
            "Every kernel of the calls, those of torch that a call launches among them, in the order of their first dispatch behind the first call's "
            "start.  `launches` a call; medians over a kernel's dispatches, us from the trace, the rest from the counter run.  `vector busy` = 4 x SQ_ACTIVE_INST_VALU / (1024 SIMDs x "
            "duration x 2.2 GHz), `LDS busy` = SQ_LDS_IDX_ACTIVE / (256 CUs x duration x 2.2 GHz), of which `conflicts` replay, `waiting` = SQ_WAIT_ANY / "

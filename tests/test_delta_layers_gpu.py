@@ -253,10 +253,30 @@ def against_reference(v, lead, Hk, H, K, V, dt, **kw):
 
 
 @pytest.mark.parametrize("S,rows,Hk,H,K,V,dt", [(64, 70, 4, 8, 48, 100, "bfloat16"), (128, 5, 4, 4, 128, 65, "float32"), (128, 66, 2, 4, 20, 128, "float16"),
-                                               (85, 3, 1, 2, 33, 130, "float32"), (86, 3, 1, 2, 33, 130, "float32"), (64, 9, 1, 8, 256, 70, "bfloat16")])
+                                               (85, 3, 1, 2, 33, 130, "float32"), (86, 3, 1, 2, 33, 130, "float32"), (64, 9, 1, 8, 256, 70, "bfloat16"),
+                                               (128, 70, 4, 4, 41, 100, "float32")])
 def test_many_walks(S, rows, Hk, H, K, V, dt):
     """Sizes beside and past those from which a block walks with 128 values instead of 64."""
     against_reference(make((S, rows), dt, Hk, H, K, V, True, "wide", 12), (S, rows), Hk, H, K, V, dt)
+
+
+@pytest.mark.parametrize("V,K", [(130, 33), (100, 128)])
+def test_gradients_of_many_walks(V, K):
+    """A batch large enough for the wide schedule against its parts, which are not: each is delta_noise off the formulas, in its own way."""
+    S, rows, H = 128, 66, 4
+    v = make((S, rows), "float32", 2, H, K, V, True, "dense", 3)
+    d, last = randn(torch.Generator().manual_seed(8), S, rows, H, V), randn(torch.Generator().manual_seed(9), S, H, K, V)
+
+    def run(at):
+        x = {n: t[at] for n, t in v.items()}
+        marks = ssam.ssam_scan_delta_marks(x["k"], x["v"])
+        out = ssam.ssam_scan_delta(x["q"], x["k"], x["v"], x["g"], x["beta"], unit=True, d_marks=marks)
+        return [out, *ssam.ssam_scan_delta_backward(d[at], x["q"], x["k"], x["v"], x["g"], x["beta"], marks, unit=True, d_grad_final=last[at], state_grad=True)]
+    whole = run(slice(0, S))
+    parts = [torch.cat(t) for t in zip(*(run(slice(s, s + 8)) for s in range(0, S, 8)))]
+    for n, (a, b) in enumerate(zip(whole, parts)):
+        b = f64(b)
+        assert np.sqrt(np.square(f64(a) - b).mean()) <= 2 * ref.delta_noise(rows) * np.sqrt(np.square(b).mean()), n
 
 
 @pytest.mark.parametrize("K,H,dt", [(200, 4, "bfloat16"), (256, 3, "float32"), (129, 5, "float16")])
