@@ -167,11 +167,17 @@ inline int check_out_heads(const ssam_rows& r, const ssam_sequences& q, int head
 
 // fp32: with two walks a compute unit or more, a wave takes 32 columns, so that half as many blocks make the same operands: 16 x 512 rows of 32
 // heads of 128 x 128 455 -> 353 us, their gradients 1792 -> 1671, but 4 x 1024 rows (256 walks) 207 -> 257.  16 bits have staging waves in place of it (778 and 793 us for
-// 8 x 4096 rows).  Keys beyond 128 leave no registers for it.
+// 8 x 4096 rows); fewer columns a block, on more of them, gave 16 bits 4 % at 64 walks and cost the gradients' 6 %.  Keys beyond 128 leave no registers for it.
+struct WalkPlan {
+    bool wide;
+    int tiles;
+};
 template <class Args>
-bool wide_walks(const Args& a)
+WalkPlan walk_plan(const Args& a)
 {
-    return a.dtype == SSAM_F32 && (long long)a.seq.sequences * a.heads * ((a.value_dim + 63) / 64) >= 512 && a.value_dim > 64 && a.key_dim <= 128;
+    const int tiles = (a.value_dim + 63) / 64;
+    const bool wide = a.dtype == SSAM_F32 && (long long)a.seq.sequences * a.heads * tiles >= 512 && a.value_dim > 64 && a.key_dim <= 128;
+    return {wide, wide ? (a.value_dim + 127) / 128 : tiles};
 }
 
 template <class F>

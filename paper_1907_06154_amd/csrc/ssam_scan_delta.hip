@@ -1,5 +1,9 @@
 // The scan with matrix states along time (ssam_scan_delta): what the blocks' rows have to do with one another (delta_prepare, one launch over
 // all blocks), then the states from block to block and the outputs (delta_walk).
+// bf16, heads of 128 x 128: 1 x 4096 rows of 32 heads take 38 + 236 us, 8 x 4096 222 + 534.  A walk is bound by one wave's chain, 3.7 us for 64 rows:
+// five matrix products in line, some 130 matrix instructions (2100 of 8000 cycles), and between them the columns' largest values and the splits into
+// pairs of fp16.  Memory would take 26 and 215 us.  Waves without columns do nothing: 1 to 16 values beyond 64 cost no LDS reads of three
+// more waves (heads of 96 x 80, 8191 packed rows of 6: 93 -> 71 us).
 #include "ssam_scan_delta_tiles.h"
 
 namespace ssam {
@@ -40,6 +44,11 @@ __global__ __launch_bounds__((kWalkThreads<T, KT>)) void delta_walk(DeltaParams 
                               sequence_base<const T>(p.q, p.pieces, whole) + key_head * p.q_head, p.k.row, p.q.row, p.heads, len, p.key_dim};
     if (kHelp && wave >= kWavesPerBlock) {
         if (blocks > 0) stage_all<S>(source, rooms, 0, 1, blocks);
+        return;
+    }
+    if (kHelp && col0 >= p.value_dim) {        // no columns: the barriers alone, as many as stage_all has
+        if (blocks > 0)
+            for (int c = 0; c <= blocks; ++c) __syncthreads();
         return;
     }
     const T* vs = sequence_base<const T>(p.v, p.pieces, whole) + head * p.v_head;
@@ -247,11 +256,10 @@ int ssam_scan_delta(const ssam_scan_delta_args* a, void* hip_stream)
     for (int i = 0; i < 4; ++i)
         if (overlaps(outs[i], state) && !(i == 1 && a->d_final == a->d_state)) return SSAM_ERR_ALIAS;
 
-    DeltaParams p{make_pieces(a->seq, kDeltaRows), a->q, a->k, a->v, a->out, a->g, a->beta, a->q_head, a->k_head, a->v_head, a->out_head, a->d_state,
-                  a->d_final, a->d_marks, static_cast<Block*>(a->d_work), a->heads, a->key_heads, a->key_dim, a->value_dim, a->unit != 0, a->scale, 1};
+    const WalkPlan plan = walk_plan(*a);
+    const DeltaParams p{make_pieces(a->seq, kDeltaRows), a->q, a->k, a->v, a->out, a->g, a->beta, a->q_head, a->k_head, a->v_head, a->out_head, a->d_state,
+                  a->d_final, a->d_marks, static_cast<Block*>(a->d_work), a->heads, a->key_heads, a->key_dim, a->value_dim, a->unit != 0, a->scale, plan.tiles};
     const long long heads = (long long)a->seq.sequences * a->heads;
-    const bool wide = wide_walks(*a);
-    p.tiles = (a->value_dim + (wide ? 127 : 63)) / (wide ? 128 : 64);
     if (product(slots, a->key_heads) > kMaxGrid || product(heads, p.tiles) > kMaxGrid) return SSAM_ERR_DIM;
     hipStream_t st = (hipStream_t)hip_stream;
     return with_delta_type(a->dtype, [&](auto t) {
@@ -262,7 +270,7 @@ int ssam_scan_delta(const ssam_scan_delta_args* a, void* hip_stream)
             if (int e = launched()) return e;
             const dim3 walks((unsigned)(heads * p.tiles));
             if constexpr (kSplit<T> && KT <= 4)
-                if (wide) {
+                if (plan.wide) {
                     hipLaunchKernelGGL((delta_walk<T, KT, 2>), walks, dim3(kWalkThreads<T, KT>), 0, st, p);
                     return launched();
                 }

@@ -186,7 +186,7 @@ __device__ __forceinline__ void load_square(const T* __restrict__ base, unsigned
 }
 
 // A wave's columns of 64 rows on their way between memory and result tiles: 16 bytes a lane from row to row, by way of a room in LDS that is the wave's own,
-// where the tiles' values lie one by one.  (Element by element from and to memory, 16 loads and 16 stores a block cost a wave 3000 of 12000 cycles.)
+// where the tiles' values lie one by one.  (Element by element from and to memory, 16 loads and 16 stores a block cost a wave 3000 cycles.)
 // kDirect: without the room.
 template <class T, int NT, bool kDirect>
 struct Columns {
@@ -562,7 +562,7 @@ __device__ __forceinline__ void tri_products(const Half8 (&matrix)[2][kTriOperan
 }
 
 // Walks whose operands fit into LDS twice leave the staging to four waves of their own: the next block's operands are made while this one's are used, one
-// barrier a block, and loads, conversions and LDS writes (4300 of a block's 12300 cycles in one wave) pass beside the products.
+// barrier a block, and loads, conversions and LDS writes (4300 cycles a block, where each wave makes its share) pass beside the products: 304 -> 239 us for 1 x 4096 rows of 32 heads.
 template <class T, int KT> constexpr bool kHelped = !kSplit<T> && KT <= 4;
 template <class T, int KT> constexpr int kWalkThreads = kHelped<T, KT> ? 2 * kBlock : kBlock;
 
