@@ -393,3 +393,23 @@ def test_refusals_of_the_binding():
     refused("d_out", coded, x, d_out=z(6, 32))
     refused("d_grad", slopes, z(6, 31), x)
     refused(None, slopes, x, x, z(32), d_work=z(4), error=ssam.SsamError)
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16])
+def test_sequences_of_no_rows(dt):
+    """The state and its gradient pass; no sequences at all: nothing to do."""
+    z = lambda *s, t=dt: torch.zeros(*s, device="cuda", dtype=t)  # noqa: E731
+    for K in (32, 200):
+        q, v, r = z(3, 0, 1, K), z(3, 0, 2, 20), z(3, 0, 2, t=torch.float32)
+        state, final = randn(torch.Generator().manual_seed(1), 3, 2, K, 20), torch.full((3, 2, K, 20), float("nan"), device="cuda")
+        marks = ssam.ssam_scan_delta_marks(q, v)
+        assert ssam.ssam_scan_delta(q, q, v, r, r, unit=True, d_state=state, d_final=final, d_marks=marks).shape == v.shape
+        assert torch.equal(final, state)
+        ssam.ssam_scan_delta(q, q, v, r, r, d_final=final)
+        assert not final.any()
+        got = ssam.ssam_scan_delta_backward(v, q, q, v, r, r, marks, unit=True, d_grad_final=state, state_grad=True)
+        assert torch.equal(got.state, state) and got.q.shape == q.shape
+        q, v, r = z(0, 5, 1, K), z(0, 5, 2, 20), z(0, 5, 2, t=torch.float32)
+        assert ssam.ssam_scan_delta(q, q, v, r, r).shape == v.shape
+        q, v, r = z(0, 1, K), z(0, 2, 20), z(0, 2, t=torch.float32)
+        assert ssam.ssam_scan_delta_step(q, q, v, r, r, z(4, 2, K, 20, t=torch.float32), slots=torch.zeros(0, dtype=torch.int32, device="cuda")).shape == v.shape
