@@ -193,7 +193,8 @@ def ssam_scan_delta(d_q, d_k, d_v, g, beta, scale=None, unit: bool = False, d_st
     """Gated delta rule, per head with a matrix S [key, value]:  S' = exp(g_t) S,  u = beta_t (v_t - S'^T k_t),  S = S' + k_t u^T,
     out_t = scale S^T q_t.  d_q, d_k: rows of [key heads, key width] (at most 256), d_v and the result: of [heads, value width], head h using key head
     h // (heads // key heads); g (None: no decay), beta: float32 rows of heads.  unit: rows of q and k are divided by sqrt(their squares' sum
-    + 1e-6).  scale: 1 / sqrt(key width) if None.  d_state, d_final [sequences, heads, key, value], float32; d_final may be d_state.
+    + 1e-6).  scale: 1 / sqrt(key width) if None.  d_state, d_final [sequences, heads, key, value], float32; d_final may be d_state.  Rows are
+    taken 64 at a time: a value that is not finite makes the other rows of its 64, of its head, NaN too.
     d_marks (from ssam_scan_delta_marks) keeps what the gradients need."""
     return _run("delta", d_v, stream, (d_q, d_k, d_v, g, beta, scale, unit, d_state, d_final, d_marks, starts, lengths, d_out, d_work))
 
@@ -215,15 +216,15 @@ def ssam_scan_delta_step(d_q, d_k, d_v, g, beta, d_state, scale=None, unit: bool
 
 def ssam_rms_norm(d_in, weight=None, d_residual=None, d_sum=None, gate=None, groups: int = 1, eps: float = 1e-6, d_out=None, stream=None):
     """s = d_in + d_residual, rounded to their type (d_in alone without);  out = s / sqrt(mean(s^2) + eps) * weight * silu(gate), the mean over each of
-    `groups` equal parts of a row (heads, say).  weight [channels / groups], d_in's type or float32 (None: ones); gate (None: absent): rows as
+    `groups` equal parts of a row (heads, say; at most 32768 channels each).  weight [channels / groups], d_in's type or float32 (None: ones); gate (None: absent): rows as
     d_in's.  d_sum receives s and may be d_residual itself; the gradients start from it."""
     return _run("norm", d_in, stream, (d_in, weight, d_residual, d_sum, gate, groups, eps, d_out))
 
 
 def ssam_rms_norm_e4m3(d_in, weight=None, d_residual=None, d_sum=None, gate=None, groups: int = 1, eps: float = 1e-6, block: Optional[int] = None,
                        d_out=None, d_scales=None, stream=None) -> RmsNormQuantized:
-    """ssam_rms_norm with its result as torch.float8_e4m3fn and a float32 scale for every `block` channels (None: a group's), the largest
-    magnitude among them / 448; [.., channels / block] scales."""
+    """ssam_rms_norm with its result as torch.float8_e4m3fn and a float32 scale for every `block` channels (16 at least; None: a group's),
+    the largest magnitude among them / 448; [.., channels / block] scales."""
     return RmsNormQuantized(*_run("norm_e4m3", d_in, stream, (d_in, weight, d_residual, d_sum, gate, groups, eps, block, d_out, d_scales)))
 
 
