@@ -181,7 +181,7 @@ int ssam_scan_selective_step(const ssam_scan_selective_step_args *args, void *hi
  * rows, rows lie at most 2^24 elements apart, here and for the gradients (SSAM_ERR_DIM).
  * d_work: ssam_scan_delta_workspace_bytes(args) bytes, 16-byte aligned.
  * Schedules: two launches, the 64 rows' own matrices for all of them at once, then the state's way through them, a block for each head and
- * 64 or, where there are many, 128 of its values. */
+ * 64 of its values (fp32, where there are many: 128). */
 typedef struct {
     int dtype, heads, key_heads, key_dim, value_dim, unit;
     float scale;
