@@ -239,7 +239,8 @@ int ssam_scan_delta_step(const ssam_scan_delta_step_args *args, void *hip_stream
  * ssam_rms_norm_e4m3: out is in 8 bits (e4m3, 448 at most) with a scale for every `block` channels, a divisor of width, 16 at least
  * or the whole of it (SSAM_ERR_SHAPE):
  *     scale = max over the block of |y| / 448 (at least 2^-126; 1 where all are zero),   out = y / scale, rounded to nearest
- * d_scales: [sequences * rows][channels / block] floats; out's strides count bytes.  (y / scale is made with the rounded reciprocal.) */
+ * d_scales: [sequences * rows][channels / block] floats; out's strides count bytes.  The quotient is that of s * weight * gate's factor and the block's
+ * largest of them, from which the root has gone: halves between two codes are met as such and go to the even one. */
 typedef struct {
     int dtype, param_dtype, channels, groups, block;   /* block: ssam_rms_norm_e4m3 only         */
     int sequences, rows;

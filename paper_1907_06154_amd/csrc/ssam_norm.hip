@@ -91,6 +91,32 @@ __device__ __forceinline__ float scale_of(float most)
     return scale < 0x1p-126f ? 0x1p-126f : scale;
 }
 
+// Codes of a block whose largest magnitude is that of y = f z for values z that have not been through the root's rounding, 1 <= f < 2: y / scale is
+// 448 z / max|z|, whose halves between two codes are met exactly where z is (16 bits times a weight of 16 bits); y and scale would each be
+// rounded, and which side of a half their quotient falls on would be chance.  448 = 0.875 x 2^9: the quotient of c z and b, c = 0.875, from the rounded
+// reciprocal and one step of correction by its remainder, which is exact for a quotient that is a half.  (Three operations a value more than the product
+// with the reciprocal alone.)  Where the scale is held at its least value, or the largest value is not finite: of y and the scale itself.
+struct Quotient {
+    float scale, per, first, less, back;
+    __device__ __forceinline__ Quotient() {}
+    __device__ __forceinline__ Quotient(float most, float f)      // max|z|
+    {
+        const float y = most * f;
+        scale = scale_of(y);
+        const bool plain = y > 0x1p-90f && y < __builtin_inff();
+        const float c = plain ? 0.875f : f, b = plain ? most * 0x1p-9f : scale;
+        per = 1.0f / b;
+        first = c * per;
+        less = c - 1.0f;
+        back = __builtin_isinf(b) ? 0.0f : b;      // (finite values over an infinite scale are zero, not NaN)
+    }
+    __device__ __forceinline__ float of(float z) const
+    {
+        const float q = z * first;
+        return __builtin_fmaf(__builtin_fmaf(less, z, __builtin_fmaf(-q, back, z)), per, q);
+    }
+};
+
 // How a unit leaves.
 constexpr int kPlain = 0;       // in its own type
 constexpr int kLanes = 1;       // e4m3, a block being the unit or the vectors of an aligned group of 2^n <= 16 lanes: no division by element
@@ -142,7 +168,12 @@ __global__ __launch_bounds__(TP > kBlock ? TP : kBlock) void rms_norm(NormParams
                 squares = __builtin_fmaf(s[j][i], s[j][i], squares);
             }
         squares = over_unit<TP>(squares, room[0], Add());
-        const float r = 1.0f / __builtin_sqrtf(squares / (float)p.width + p.eps);
+        float r = 1.0f / __builtin_sqrtf(squares / (float)p.width + p.eps), f = 1.0f;
+        if (kE4m3 && r == r) {      // its power of two alone, exact; the rest joins the scale.  (Zero and infinity are their own, NaN stays.)
+            const unsigned bits = __builtin_bit_cast(unsigned, r);
+            f = __builtin_bit_cast(float, (bits & 0x7fffffu) | 0x3f800000u);
+            r = __builtin_bit_cast(float, bits & 0x7f800000u);
+        }
         const T* gate = p.gate.d ? unit_of<T>(p.gate, unit, p.groups, p.rows, p.width) : nullptr;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -150,7 +181,7 @@ __global__ __launch_bounds__(TP > kBlock ? TP : kBlock) void rms_norm(NormParams
             if (have <= 0) continue;
             const RowVec<float, V> w = load_weights<T, V>(p.weight, p.params_f32, c, have, true);
 #pragma unroll
-            for (int i = 0; i < V; ++i) s[j][i] *= r * w[i];
+            for (int i = 0; i < V; ++i) s[j][i] = kE4m3 ? s[j][i] * r * w[i] : s[j][i] * (r * w[i]);
             if (gate) {
                 const RowVec<T, V> z = load_row_vec<T, V>(gate + c, have);
 #pragma unroll
@@ -203,13 +234,13 @@ __global__ __launch_bounds__(TP > kBlock ? TP : kBlock) void rms_norm(NormParams
                         for (int i = 0; i < V; ++i) m = Larger()(m, __builtin_fabsf(s[j][i]));
                         m = over_lanes(m, lanes, Larger());
                     }
-                    const float scale = scale_of(m), per = 1.0f / scale;
+                    const Quotient by(m, f);
                     const int first_of = whole ? c : (j * TP + at) & (lanes - 1), b = whole ? 0 : (j * TP + at) >> doublings;
-                    if (there && have > 0 && first_of == 0) scales[b] = scale;
+                    if (there && have > 0 && first_of == 0) scales[b] = by.scale;
 #pragma unroll
-                    for (int i = 0; i < V; ++i) q[i] = s[j][i] * per;
+                    for (int i = 0; i < V; ++i) q[i] = by.of(s[j][i]);
                 } else {
-                    float scale = 1.0f, per = 1.0f;
+                    Quotient by;
                     int block = -1;
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
@@ -220,11 +251,10 @@ __global__ __launch_bounds__(TP > kBlock ? TP : kBlock) void rms_norm(NormParams
                         const int b = (c + i) / p.block;
                         if (b != block) {
                             block = b;
-                            scale = scale_of(__builtin_bit_cast(float, most_of[mine * (p.width / p.block) + b]));
-                            per = 1.0f / scale;
+                            by = Quotient(__builtin_bit_cast(float, most_of[mine * (p.width / p.block) + b]), f);
                         }
-                        q[i] = s[j][i] * per;
-                        if (there && (c + i) % p.block == 0) scales[b] = scale;
+                        q[i] = by.of(s[j][i]);
+                        if (there && (c + i) % p.block == 0) scales[b] = by.scale;
                     }
                 }
                 if (!there || have <= 0) continue;
