@@ -2,6 +2,7 @@
 // products with them.
 #pragma once
 #include "ssam_scan_delta.h"
+#include "ssam_scan_delta_layout.h"
 
 namespace ssam {
 
@@ -92,8 +93,7 @@ template <class T, int N>
 __device__ __forceinline__ void load_eights(const T* __restrict__ base, unsigned stride, int row0, int step, int rows, int e, int dim, RowVec<T, 8> (&v)[N])
 {
     stride = afresh(stride);
-    // (a vector that would pass the last element starts further left)
-    const unsigned at = dim < 8 ? 0 : (unsigned)(8 * e + 8 <= dim ? 8 * e : dim - 8);
+    const unsigned at = dim < 8 ? 0 : eights_at(e, dim);
     if (dim >= 8 && rows == kDeltaRows) {
         const unsigned lane_at = (unsigned)row0 * stride + at;
 #pragma unroll
@@ -102,13 +102,13 @@ __device__ __forceinline__ void load_eights(const T* __restrict__ base, unsigned
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int row = row0 + i * step;
-            __builtin_memcpy(&v[i], base + ((unsigned)(row < rows ? row : rows - 1) * stride + at), sizeof(v[i]));
+            __builtin_memcpy(&v[i], base + ((unsigned)eights_row(row, rows) * stride + at), sizeof(v[i]));
         }
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int row = row0 + i * step;
-            v[i] = load_few(base + (unsigned)(row < rows ? row : rows - 1) * stride, dim);
+            v[i] = load_few(base + (unsigned)eights_row(row, rows) * stride, dim);
         }
     }
 }
@@ -663,20 +663,21 @@ struct PrepareRoom {
 // q's or k's rows as fp16, each with its largest magnitude's power of two taken out; sizes: what makes it up again.
 template <class T, int KT, int kThreads>
 struct RowLoad {
-    static constexpr int kLanes = 4 * KT, kAtOnce = kThreads / kLanes, kPasses = kDeltaRows > kAtOnce ? kDeltaRows / kAtOnce : 1;      // lanes of a row, rows
+    typedef RowLanes<KT, kThreads> Lanes;
+    static constexpr int kLanes = Lanes::kLanes, kAtOnce = Lanes::kAtOnce, kPasses = Lanes::kPasses;
     RowVec<T, 8> v[kPasses];
 
     __device__ __forceinline__ void load(const T* __restrict__ base, unsigned stride, int rows, int dim)
     {
-        load_eights<T, kPasses>(base, stride, (int)(threadIdx.x / kLanes), kAtOnce, rows, threadIdx.x % kLanes, dim, v);
+        load_eights<T, kPasses>(base, stride, Lanes::row((int)threadIdx.x), kAtOnce, rows, threadIdx.x % kLanes, dim, v);
     }
     __device__ __forceinline__ void put(bool unit, int rows, int dim, Half8 (&to)[kSplit<T> ? 2 : 1][4 * KT][kDeltaRows], float* factor, float* scale)
     {
         const int e = threadIdx.x % kLanes;
-        clear_eights<T, kPasses>((int)(threadIdx.x / kLanes), kAtOnce, rows, e, dim, v);
+        clear_eights<T, kPasses>(Lanes::place((int)threadIdx.x), kAtOnce, rows, e, dim, v);
 #pragma unroll
         for (int k = 0; k < kPasses; ++k) {
-            const int t = (int)(threadIdx.x / kLanes) + k * (kAtOnce);
+            const int t = Lanes::place((int)threadIdx.x) + k * kAtOnce;
             float m = 0.0f, squares = 0.0f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
