@@ -21,4 +21,16 @@ struct RowLanes {
     static constexpr int row(int thread) { return kAtOnce > SSAM_DELTA_ROWS && place(thread) >= SSAM_DELTA_ROWS ? SSAM_DELTA_ROWS - 1 : place(thread); }
 };
 
+// How the threads share the squares of 8 rows x 8 elements of a block's k, and then of its q.  A wave's are of one of them, also where 32 squares
+// are half of it: the distance from row to row is one value for all lanes (load_eights), and those of q need not be k's.
+template <int KT>
+struct StageLanes {
+    static constexpr int kAcross = 4 * KT, kSquares = 8 * kAcross;
+    static constexpr int kSide = kSquares < 64 ? 64 : kSquares, kJobs = 2 * kSide;
+    static constexpr bool has(int job) { return job < kJobs && job % kSide < kSquares; }
+    static constexpr bool query(int job) { return job >= kSide; }
+    static constexpr int rows(int job) { return (job % kSide) / kAcross; }      // 8 of them
+    static constexpr int elements(int job) { return job % kAcross; }
+};
+
 }  // namespace ssam

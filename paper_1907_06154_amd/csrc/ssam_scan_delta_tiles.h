@@ -86,7 +86,7 @@ __device__ __forceinline__ RowVec<T, 8> load_few(const T* __restrict__ row, int 
     return v;
 }
 
-// N rows of eight elements, rows row0, row0 + step .. and elements from 8 e on; rows >= 1, `base` the same for all lanes.  There are no branches on what is
+// N rows of eight elements, rows row0, row0 + step .. and elements from 8 e on; rows >= 1, `base` and `stride` the same for all lanes of a wave.  There are no branches on what is
 // there: a load that waits for its turn in one costs its latency by itself.  clear_eights() makes zeros of what was not there, where the values are used.
 // Where all rows are there, their distances are the same for all lanes too and cost no vector instructions.
 template <class T, int N>
@@ -421,7 +421,8 @@ __device__ __forceinline__ int stage_thread() { return (int)(threadIdx.x & (kBlo
 template <class T, int KT, bool kTurn>
 struct Stage {
     static constexpr bool kOnePlace = WalkRoom<T, KT>::kOnePlace;
-    static constexpr int kAcross = 4 * KT, kSquares = 8 * kAcross;      // squares of 8 x 8 in a block's keys
+    typedef StageLanes<KT> Lanes;
+    static constexpr int kSquares = Lanes::kSquares;
     static constexpr bool kAhead = (kSplit<T> ? 2 : 1) * KT <= 4;
     static constexpr int kVecs = (int)(sizeof(Block) / 16), kOfThread = (kVecs + kBlock - 1) / kBlock;
     static_assert(sizeof(Block) % 16 == 0);
@@ -452,11 +453,11 @@ struct Stage {
     __device__ __forceinline__ void load(const Block& from, const T* ks, unsigned kstride, const T* qs, unsigned qstride, int rows, int dim)
     {
         if constexpr (kAhead) {
-            const int job = stage_thread(), b = (job % kSquares) / kAcross, e = job % kAcross;
-            const bool query = kSquares % kWave == 0 ? __builtin_amdgcn_readfirstlane(job) >= kSquares : job >= kSquares;
-            if (kBlock == 2 * kSquares || job < 2 * kSquares) {
-                load_square<T>(query ? qs : ks, query ? qstride : kstride, rows, dim, b, e, square);
-                load_scale(from.f, query, b, scale);
+            const int job = stage_thread();
+            const bool query = Lanes::query(__builtin_amdgcn_readfirstlane(job));
+            if (Lanes::has(job)) {
+                load_square<T>(query ? qs : ks, query ? qstride : kstride, rows, dim, Lanes::rows(job), Lanes::elements(job), square);
+                load_scale(from.f, query, Lanes::rows(job), scale);
             }
 #pragma unroll
             for (int i = 0; i < kOfThread; ++i) {
@@ -470,7 +471,7 @@ struct Stage {
         Float4* const to = reinterpret_cast<Float4*>(&room.m);
         if constexpr (kAhead) {
             const int job = stage_thread();
-            if (kBlock == 2 * kSquares || job < 2 * kSquares) put_square(room, job >= kSquares, (job % kSquares) / kAcross, job % kAcross, rows, dim, square, scale);
+            if (Lanes::has(job)) put_square(room, Lanes::query(job), Lanes::rows(job), Lanes::elements(job), rows, dim, square, scale);
 #pragma unroll
             for (int i = 0; i < kOfThread; ++i) {
                 const int behind = (i + 1) * kBlock - kVecs;
@@ -485,14 +486,14 @@ struct Stage {
     static __device__ __forceinline__ void put_now(WalkRoom<T, KT>& room, const Block& from, const T* ks, unsigned kstride, const T* qs, unsigned qstride, int rows,
                                                    int dim, int first, int last)
     {
+        static_assert(kSquares % kWave == 0);      // a wave's are of one side
         for (int job = first + stage_thread(); job < last; job += kBlock) {
-            const bool query = job >= kSquares;
-            const int b = (job % kSquares) / kAcross, e = job % kAcross;
+            const bool query = Lanes::query(job);
             RowVec<T, 8> v[8];
             Float4 to[2];
-            load_square<T>(query ? qs : ks, query ? qstride : kstride, rows, dim, b, e, v);
-            load_scale(from.f, query, b, to);
-            put_square(room, query, b, e, rows, dim, v, to);
+            load_square<T>(query ? qs : ks, query ? qstride : kstride, rows, dim, Lanes::rows(job), Lanes::elements(job), v);
+            load_scale(from.f, query, Lanes::rows(job), to);
+            put_square(room, query, Lanes::rows(job), Lanes::elements(job), rows, dim, v, to);
         }
     }
 };

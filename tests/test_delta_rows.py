@@ -54,8 +54,46 @@ int main()
 }
 """
 
+SQUARES = r"""
+#include "ssam_scan_delta_layout.h"
+#include <cstdio>
+using namespace ssam;
 
-@pytest.mark.parametrize("program", [ROWS], ids=["rows"])
+static int bad;
+template <int KT> void squares()
+{
+    typedef StageLanes<KT> L;
+    bool seen[2][8][4 * KT] = {};
+    for (int wave = 0; wave < (L::kJobs + 63) / 64; ++wave) {
+        int side = -1;      // a wave reads k or q: their rows' distance is one value for all of its lanes
+        for (int job = 64 * wave; job < 64 * wave + 64; ++job) {
+            if (!L::has(job)) continue;
+            if (side < 0) side = L::query(64 * wave);
+            if (L::query(job) != (side != 0) && bad++ < 3) std::printf("keys to %d: thread %d reads q, the wave's first %s\n", 32 * KT, job, side ? "q" : "k");
+            if (L::rows(job) < 0 || L::rows(job) >= 8 || L::elements(job) < 0 || L::elements(job) >= 4 * KT) {
+                if (bad++ < 3) std::printf("keys to %d: thread %d is outside\n", 32 * KT, job);
+                continue;
+            }
+            bool& there = seen[L::query(job)][L::rows(job)][L::elements(job)];
+            if (there && bad++ < 3) std::printf("keys to %d: thread %d again\n", 32 * KT, job);
+            there = true;
+        }
+    }
+    for (auto& s : seen)
+        for (auto& r : s)
+            for (bool there : r)
+                if (!there && bad++ < 3) std::printf("keys to %d: a square is missing\n", 32 * KT);
+}
+
+int main()
+{
+    squares<1>(), squares<2>(), squares<4>(), squares<8>();
+    return bad != 0;
+}
+"""
+
+
+@pytest.mark.parametrize("program", [ROWS, SQUARES], ids=["rows", "squares"])
 def test_what_the_threads_read(program, tmp_path):
     (tmp_path / "p.cpp").write_text(program)
     subprocess.run(["g++", "-std=c++17", "-Wall", "-Werror", "-I", CSRC, "-o", str(tmp_path / "p"), str(tmp_path / "p.cpp")], check=True)
