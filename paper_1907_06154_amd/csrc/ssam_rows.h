@@ -371,6 +371,7 @@ inline bool any_overlap(const Cover (&outs)[NA], const Cover (&ins)[NB])
 }
 
 constexpr long long kMaxGrid = (1LL << 24) - 1;   // blocks of 256 threads: a launch holds fewer than 2^32 threads
+constexpr long long max_grid(int threads) { return ((1LL << 32) - 1) / threads; }      // of others
 
 inline int launched() { return hipGetLastError() == hipSuccess ? SSAM_OK : SSAM_ERR_HIP; }
 

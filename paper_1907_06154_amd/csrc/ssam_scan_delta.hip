@@ -260,12 +260,13 @@ int ssam_scan_delta(const ssam_scan_delta_args* a, void* hip_stream)
     const DeltaParams p{make_pieces(a->seq, kDeltaRows), a->q, a->k, a->v, a->out, a->g, a->beta, a->q_head, a->k_head, a->v_head, a->out_head, a->d_state,
                   a->d_final, a->d_marks, static_cast<Block*>(a->d_work), a->heads, a->key_heads, a->key_dim, a->value_dim, a->unit != 0, a->scale, plan.tiles};
     const long long heads = (long long)a->seq.sequences * a->heads;
-    if (product(slots, a->key_heads) > kMaxGrid || product(heads, p.tiles) > kMaxGrid) return SSAM_ERR_DIM;
+    if (product(slots, a->key_heads) > max_grid(kBlock)) return SSAM_ERR_DIM;
     hipStream_t st = (hipStream_t)hip_stream;
     return with_delta_type(a->dtype, [&](auto t) {
         return with_key(a->key_dim, [&](auto kt) {
             using T = decltype(t);
             constexpr int KT = decltype(kt)::value;
+            if (product(heads, p.tiles) > max_grid(kWalkThreads<T, KT>)) return (int)SSAM_ERR_DIM;
             hipLaunchKernelGGL((delta_prepare<T, KT>), dim3((unsigned)(slots * a->key_heads)), dim3(kBlock), 0, st, p);
             if (int e = launched()) return e;
             const dim3 walks((unsigned)(heads * p.tiles));

@@ -906,19 +906,21 @@ int ssam_scan_delta_backward(const ssam_scan_delta_backward_args* a, void* hip_s
     b.grad_state = a->d_grad_state;
     b.behind = reinterpret_cast<float*>(static_cast<char*>(a->d_work) + plan.blocks);
     const long long walks = product((long long)a->seq.sequences * a->heads, b.f.tiles), rows = product(plan.slots, a->key_heads);
-    if (walks > kMaxGrid || rows > kMaxGrid) return SSAM_ERR_DIM;
+    const bool all = a->grad_q.d || a->grad_k.d || a->grad_g.d || a->grad_beta.d;      // or the state's and the values' alone
+    if (rows > max_grid(all ? kRowThreads : kBlock)) return SSAM_ERR_DIM;
     hipStream_t st = (hipStream_t)hip_stream;
     return with_delta_type(a->dtype, [&](auto t) {
         return with_key(a->key_dim, [&](auto kt) {
             using T = decltype(t);
             constexpr int KT = decltype(kt)::value;
+            if (walks > max_grid(kWalkThreads<T, KT>)) return (int)SSAM_ERR_DIM;
             hipLaunchKernelGGL((delta_back_prepare<T, KT>), dim3((unsigned)rows), dim3(kBlock), 0, st, b.f);
             if (int e = launched()) return e;
             if constexpr (kSplit<T> && KT <= 4)
                 if (walk.wide) hipLaunchKernelGGL((delta_back_walk<T, KT, 2>), dim3((unsigned)walks), dim3(kWalkThreads<T, KT>), 0, st, b);
             if (!walk.wide) hipLaunchKernelGGL((delta_back_walk<T, KT, 1>), dim3((unsigned)walks), dim3(kWalkThreads<T, KT>), 0, st, b);
             if (int e = launched()) return e;
-            if (!a->grad_q.d && !a->grad_k.d && !a->grad_g.d && !a->grad_beta.d) return (int)SSAM_OK;
+            if (!all) return (int)SSAM_OK;
             if (a->heads > a->key_heads) hipLaunchKernelGGL((delta_back_rows<T, KT, true>), dim3((unsigned)rows), dim3(kRowThreads), 0, st, b);
             else hipLaunchKernelGGL((delta_back_rows<T, KT, false>), dim3((unsigned)rows), dim3(kRowThreads), 0, st, b);
             return launched();
