@@ -176,7 +176,10 @@ int ssam_scan_selective_step(const ssam_scan_selective_step_args *args, void *hi
  * follow from the state); rows of no sequence reach nothing.
  * d_marks (NULL: not wanted): what ssam_scan_delta_backward starts from, ssam_scan_delta_marks(args) entries of
  * [heads][key_dim + 64][value_dim] floats: for each 64 rows and sequence the state before them and what the rows correct it by.
- * Operands of the matrix products are held as pairs of fp16, scaled by powers of two, that keep 23 bits of an fp32 value.
+ * Operands of the matrix products are held as pairs of fp16, scaled by powers of two: with an error of 2^-22 of a value or 2^-35 of the largest that
+ * shares its power of two, whichever is more.  Those are a value's 64 rows (of v, the corrections and their gradients), a state's column, a row
+ * of q or k in fp32: where sizes differ by more than 2^13, the small ones have fewer bits, also if a decay between the rows parts them.  q and k in bf16 are
+ * exact down to 2^-27 of a row's largest element and at most 2^-34 of that off below; in fp16 they are taken as they are.
  * key_dim is at most SSAM_MAX_KEY (SSAM_ERR_SHAPE), heads x value_dim at most 2^24; of sequences of more than one row, and of a step's
  * rows, rows lie at most 2^24 elements apart, here and for the gradients (SSAM_ERR_DIM).
  * d_work: ssam_scan_delta_workspace_bytes(args) bytes, 16-byte aligned.

@@ -7,9 +7,11 @@
 // R is what each row's value misses of what the state holds for its key.  Everything but S and V is known without the state, so it is made for all
 // blocks at once (delta_prepare); the rest follows the sequence.
 //
-// Matrix products run on v_mfma_f32_16x16x32_f16.  q, k of 16 bits are one fp16 operand, exact, with a power of two per row taken
-// out; everything else is a pair hi + lo of fp16 that keeps 23 bits of the fp32 value: two products against q or k, three
-// between two such pairs (lo lo is below 2^-22).  bf16 pairs keep 16 bits, which the state's fp32 would show.
+// Matrix products run on v_mfma_f32_16x16x32_f16.  q, k of 16 bits are one fp16 operand: fp16 as it is, bf16 with a power of two per row taken
+// out (to_halves says how exact that is).  Everything else is a pair hi + lo of fp16 under a power of two that brings the largest of what shares it, a column's
+// 64 rows, a state's column, a triangular matrix, a row of fp32 q or k, to 2^10 .. 2^11.  hi is within 2^-11 of a value and lo within 2^-11 of the rest, so that
+// the pair is 2^-22 of the value off, until lo is subnormal, 2^13 below the largest: from there on it is 2^-25 off, 2^-35 of the largest.  Two products
+// against q or k, three between two such pairs (lo lo is below 2^-22).  bf16 pairs keep 16 bits, which the state's fp32 would show.
 //
 // Operand layout: lane (g = lane / 16, r = lane % 16) of an A operand holds row r, elements 8 g .. 8 g + 7 of 32 along the sum; of a B
 // operand column r and the same elements; of a result rows 4 g .. 4 g + 3, column r.  What a row of a result tile stands for is free:

@@ -8,7 +8,8 @@ namespace ssam {
 
 template <class T> constexpr bool kSplit = sizeof(T) == 4;      // q and k are pairs of fp16 too
 
-// Eight elements of a row as fp16, `to` a power of two; the low parts where T has more bits than fp16.
+// Eight elements of a row as fp16, `to` a power of two; the low parts where T has more bits than fp16.  With the row's largest at 2^10 .. 2^11, eight bits of
+// bf16 fit fp16 down to 2^-17, 2^-27 of the largest; below, bits under fp16's last place, 2^-24, are cut off: at most 2^-34 of the largest.
 template <class T>
 __device__ __forceinline__ void to_halves(const RowVec<T, 8>& v, float to, Half8& hi, Half8& lo)
 {
@@ -21,7 +22,7 @@ __device__ __forceinline__ void to_halves(const RowVec<T, 8>& v, float to, Half8
     } else {
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
-            const auto h = __builtin_amdgcn_cvt_pkrtz((float)v[i] * to, (float)v[i + 1] * to);      // eight bits: exact
+            const auto h = __builtin_amdgcn_cvt_pkrtz((float)v[i] * to, (float)v[i + 1] * to);
             hi[i] = (_Float16)h[0];
             hi[i + 1] = (_Float16)h[1];
         }

@@ -194,7 +194,8 @@ def ssam_scan_delta(d_q, d_k, d_v, g, beta, scale=None, unit: bool = False, d_st
     out_t = scale S^T q_t.  d_q, d_k: rows of [key heads, key width] (at most 256), d_v and the result: of [heads, value width], head h using key head
     h // (heads // key heads); g (None: no decay), beta: float32 rows of heads.  unit: rows of q and k are divided by sqrt(their squares' sum
     + 1e-6).  scale: 1 / sqrt(key width) if None.  d_state, d_final [sequences, heads, key, value], float32; d_final may be d_state.  Rows are
-    taken 64 at a time: a value that is not finite makes the other rows of its 64, of its head, NaN too.
+    taken 64 at a time: a value that is not finite makes the other rows of its 64, of its head, NaN too, and
+    rows more than 2^13 times smaller than others of their 64 keep fewer of fp32's bits (2^-35 of the largest is the error).
     d_marks (from ssam_scan_delta_marks) keeps what the gradients need."""
     return _run("delta", d_v, stream, (d_q, d_k, d_v, g, beta, scale, unit, d_state, d_final, d_marks, starts, lengths, d_out, d_work))
 
