@@ -47,23 +47,32 @@ struct Scale {
     }
 };
 
-// Eight values as hi + lo, each rounded to nearest: two mixed-precision multiply-adds a value, to v and to v - hi.  A matrix instruction must lie two wait
-// states behind the write of what it reads, which the compiler does not count out of these blocks; what they read must not come straight from one.
+// Two values as hi + lo, each rounded to nearest: two mixed-precision multiply-adds a value, to v and to v - hi.  (The empty statements keep the halves of a
+// register where they are: without them the compiler makes fp32 values first and converts those.  Instructions in them would be unsafe: a matrix instruction
+// reads what it adds to up to three wait states after its issue, which the compiler keeps free for its own instructions and not for such.)
+typedef _Float16 Half2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void split(float a, float b, float to, unsigned& hi, unsigned& lo)
+{
+    _Float16 first = (_Float16)__builtin_fmaf(a, to, 0.0f);
+    asm("" : "+v"(first));
+    Half2 h{first, (_Float16)__builtin_fmaf(b, to, 0.0f)};
+    asm("" : "+v"(h));
+    first = (_Float16)__builtin_fmaf(a, to, -(float)h[0]);
+    asm("" : "+v"(first));
+    hi = __builtin_bit_cast(unsigned, h);
+    lo = __builtin_bit_cast(unsigned, Half2{first, (_Float16)__builtin_fmaf(b, to, -(float)h[1])});
+}
 __device__ __forceinline__ HalfPair split(float a0, float a1, float a2, float a3, float a4, float a5, float a6, float a7, float to)
 {
     typedef unsigned Four __attribute__((ext_vector_type(4)));
     unsigned h0, h1, h2, h3, l0, l1, l2, l3;
-#define SSAM_PAIR(H, L, A, B)                                                                                                          \
-    "v_fma_mixlo_f16 %" #H ", %" #A ", %16, 0\n\tv_fma_mixhi_f16 %" #H ", %" #B ", %16, 0\n\t"                                         \
-    "v_fma_mixlo_f16 %" #L ", %" #A ", %16, -%" #H " op_sel_hi:[0,0,1]\n\tv_fma_mixhi_f16 %" #L ", %" #B ", %16, -%" #H " op_sel:[0,0,1] op_sel_hi:[0,0,1]\n\t"
-    asm(SSAM_PAIR(0, 4, 8, 9) SSAM_PAIR(1, 5, 10, 11) SSAM_PAIR(2, 6, 12, 13) SSAM_PAIR(3, 7, 14, 15) "s_nop 1"
-        : "=&v"(h0), "=&v"(h1), "=&v"(h2), "=&v"(h3), "=&v"(l0), "=&v"(l1), "=&v"(l2), "=&v"(l3)
-        : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "v"(a4), "v"(a5), "v"(a6), "v"(a7), "v"(to));
-#undef SSAM_PAIR
+    split(a0, a1, to, h0, l0);
+    split(a2, a3, to, h1, l1);
+    split(a4, a5, to, h2, l2);
+    split(a6, a7, to, h3, l3);
     HalfPair p;
-    const Four h = {h0, h1, h2, h3}, l = {l0, l1, l2, l3};
-    p.hi = __builtin_bit_cast(Half8, h);
-    p.lo = __builtin_bit_cast(Half8, l);
+    p.hi = __builtin_bit_cast(Half8, Four{h0, h1, h2, h3});
+    p.lo = __builtin_bit_cast(Half8, Four{l0, l1, l2, l3});
     return p;
 }
 // The values of two result tiles as a B operand.
@@ -73,7 +82,8 @@ __device__ __forceinline__ HalfPair split(const Float4& a, const Float4& b, floa
 __device__ __forceinline__ float larger(float m, float v) { return __builtin_fmaxf(m, __builtin_fabsf(v)); }
 __device__ __forceinline__ float larger(float m, const Float4& v) { return larger(larger(larger(larger(m, v[0]), v[1]), v[2]), v[3]); }
 // Over the four lanes of a column, lane, lane ^ 16, ^ 32 and ^ 48: the instructions swap halves of two registers, of the wave or of its pairs of rows
-// of 16 lanes, which lie two wait states behind the write of either.  (The builtins' second result is the first one's copy in this compiler.)
+// of 16 lanes, which lie two wait states behind the write of either: `m` comes from a vector instruction, and so does its copy, so that no matrix instruction
+// is still at either register.  (The builtins' second result is the first one's copy in this compiler.)
 __device__ __forceinline__ float over_column(float m)
 {
     float a = m, b = m;
