@@ -171,7 +171,8 @@ int ssam_scan_selective_step(const ssam_scan_selective_step_args *args, void *hi
  * unit != 0: q_t and k_t are divided by sqrt(their squares' sum + 1e-6) first.  q, k: rows of key_heads x key_dim elements, v and
  * out: of heads x value_dim, a head's elements contiguous, *_head elements from one head to the next; g, beta: rows of `heads`
  * floats (g.d NULL: no decay).  d_state, d_final: [sequences][heads][key_dim][value_dim] floats, the state before the first and
- * after the last row (zeros / not stored where NULL; d_final may be d_state).  g below -1000 counts as -1000, whose exponential is 0.
+ * after the last row (zeros / not stored where NULL; d_final may be d_state).  g below -1000 counts as -1000, whose exponential is 0; where
+ * a sum of positive g over neighbouring rows passes 88, its exponential is infinite.
  * Rows are taken 64 at a time: a value that is not finite makes the other rows of its 64, of its head, NaN too (rows behind them
  * follow from the state); rows of no sequence reach nothing.
  * d_marks (NULL: not wanted): what ssam_scan_delta_backward starts from, ssam_scan_delta_marks(args) entries of

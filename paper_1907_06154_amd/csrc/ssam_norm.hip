@@ -95,7 +95,8 @@ __device__ __forceinline__ float scale_of(float most)
 // 448 z / max|z|, whose halves between two codes are met exactly where z is (16 bits times a weight of 16 bits); y and scale would each be
 // rounded, and which side of a half their quotient falls on would be chance.  448 = 0.875 x 2^9: the quotient of c z and b, c = 0.875, from the rounded
 // reciprocal and one step of correction by its remainder, which is exact for a quotient that is a half.  (Three operations a value more than the product
-// with the reciprocal alone.)  Where the scale is held at its least value, or the largest value is not finite: of y and the scale itself.
+// with the reciprocal alone.)  Near the scale's least value, where y has
+// fewer bits, and where the largest value is not finite: the quotient of y and the scale itself.
 struct Quotient {
     float scale, per, first, less, back;
     __device__ __forceinline__ Quotient() {}
