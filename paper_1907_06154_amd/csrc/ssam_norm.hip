@@ -93,9 +93,9 @@ __device__ __forceinline__ float scale_of(float most)
 
 // Codes of a block whose largest magnitude is that of y = f z for values z that have not been through the root's rounding, 1 <= f < 2: y / scale is
 // 448 z / max|z|, whose halves between two codes are met exactly where z is (16 bits times a weight of 16 bits); y and scale would each be
-// rounded, and which side of a half their quotient falls on would be chance.  448 = 0.875 x 2^9: the quotient of c z and b, c = 0.875, from the rounded
-// reciprocal and one step of correction by its remainder, which is exact for a quotient that is a half.  (Three operations a value more than the product
-// with the reciprocal alone.)  Near the scale's least value, where y has
+// rounded, and which side of a half their quotient falls on would be chance.  448 = 0.875 x 2^9: the quotient of c z and b, c = 0.875, from the
+// instruction's reciprocal (1 ulp) and one step of correction by the remainder: what is left is 2^-44 of the quotient, so that one that is a half comes out as
+// it.  (Three operations a value more than the product with a reciprocal alone, and a division for eight of them less.)  Near the scale's least value, where y has
 // fewer bits, and where the largest value is not finite: the quotient of y and the scale itself.
 struct Quotient {
     float scale, per, first, less, back;
@@ -106,7 +106,7 @@ struct Quotient {
         scale = scale_of(y);
         const bool plain = y > 0x1p-90f && y < __builtin_inff();
         const float c = plain ? 0.875f : f, b = plain ? most * 0x1p-9f : scale;
-        per = 1.0f / b;
+        per = __builtin_amdgcn_rcpf(b);
         first = c * per;
         less = c - 1.0f;
         back = __builtin_isinf(b) ? 0.0f : b;      // (finite values over an infinite scale are zero, not NaN)
