@@ -178,7 +178,7 @@ inline int check_out_heads(const ssam_rows& r, const ssam_sequences& q, int head
 }
 
 // fp32: with two walks a compute unit or more, a wave takes 32 columns, so that half as many blocks make the same operands: 16 x 512 rows of 32
-// heads of 128 x 128 455 -> 353 us, their gradients 1792 -> 1671, but 4 x 1024 rows (256 walks) 207 -> 257.  16 bits have staging waves in place of it (778 and 793 us for
+// heads of 128 x 128 451 -> 360 us, their gradients 1777 -> 1660, but 4 x 1024 rows (256 walks) 199 -> 247.  16 bits have staging waves in place of it (778 and 793 us for
 // 8 x 4096 rows); fewer columns a block, on more of them, gave 16 bits 4 % at 64 walks and cost the gradients' 6 %.  Keys beyond 128 leave no registers for it.
 struct WalkPlan {
     bool wide;

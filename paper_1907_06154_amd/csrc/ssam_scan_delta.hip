@@ -1,7 +1,7 @@
 // The scan with matrix states along time (ssam_scan_delta): what the blocks' rows have to do with one another (delta_prepare, one launch over
 // all blocks), then the states from block to block and the outputs (delta_walk).
-// bf16, heads of 128 x 128: 1 x 4096 rows of 32 heads take 38 + 236 us, 8 x 4096 222 + 534.  A walk is bound by one wave's chain, 3.7 us for 64 rows:
-// five matrix products in line, some 130 matrix instructions (2100 of 8000 cycles), and between them the columns' largest values and the splits into
+// bf16, heads of 128 x 128: 1 x 4096 rows of 32 heads take 38 + 223 us, 8 x 4096 242 + 568 (653 both, once the clock has settled).  A walk is bound by one wave's
+// chain, 3.5 us for 64 rows: five matrix products in line, some 130 matrix instructions (2100 of 7700 cycles), and between them the columns' largest values and the splits into
 // pairs of fp16.  The bytes would take 21 and 160 us.  Waves without columns do nothing: 1 to 16 values beyond 64 cost no LDS reads of three
 // more waves (heads of 96 x 80, 8191 packed rows of 6: 93 -> 71 us).
 #include "ssam_scan_delta_tiles.h"

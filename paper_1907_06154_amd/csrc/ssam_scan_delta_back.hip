@@ -7,9 +7,9 @@
 //     last = exp(G_C - G) (U dS1^T),        writes = dP^T Q + dA^T K + last,   dK = reads + writes    (delta_back_rows, all blocks at once)
 // The decay of row t lies between every write j < t and every read i >= t, so dg_t is the sum over these pairs of dP P + dA A (their parts before
 // the keys' products), of what the rows i >= t have from S0, of the k.last of the rows j < t, and of exp(G_C) <S0, dS1>: no differences.
-// bf16, 4 x 2048 rows of 16 heads of 128 x 128: 45 us for the blocks' matrices, 193 for the walk (bound as the forward one), 417 for the rows, one block
-// of eight waves a compute unit (125 KB of LDS) whose phases wait for memory and for one another: 106000 cycles a block, of which the two
-// states' products take 13, the products between rows 14, the turned products and what leaves 22, the first loads 12 %.
+// bf16, 4 x 2048 rows of 16 heads of 128 x 128: 45 us for the blocks' matrices, 184 for the walk (bound as the forward one), 376 for the rows, one block
+// of eight waves a compute unit (125 KB of LDS) whose phases wait for memory and for one another: some 100000 cycles a block, of which the two
+// states' products take about 13, the products between rows 14, the turned products and what leaves 22, the first loads 12 %.
 #include "ssam_scan_delta_tiles.h"
 
 namespace ssam {
